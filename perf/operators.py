@@ -113,7 +113,7 @@ def draw(rng):
     if op == "delta_step":
         B = min(_log_int(rng, 1, 256), max(1, 50_000_000 // (Hv * Dk * Dv)))
         return _step(B, rng.choice([1, 1, 1, 2, 4, 7]), Hk, Hv, Dk, Dv, dtype, rng.choice([0, B + rng.randint(1, 40)]))
-    most = (30_000_000 if op == "delta" else 16_000_000) // (Hv * max(Dk, Dv))
+    most = (30_000_000 if op == "delta" else 14_000_000) // (Hv * max(Dk, Dv))
     short = 1 if op == "delta" else 2  # (one token alone leaves no gradient of g)
     T = min(_log_int(rng, short, 16384), most) if rng.random() < 0.6 else min(rng.choice([49, 196, 784, 3136, 16384]), most)
     B = min(_log_int(rng, 1, 64), max(1, most // T))
