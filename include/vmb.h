@@ -481,6 +481,116 @@ size_t vmb_mean_scan_bwd_workspace_bytes(int B, int K, int D, int N, int H, int 
                                          vmb_dtype dtype);
 
 /*
+ * A channels-last token mixer over maps and videos: the gated delta rule (the recurrence over
+ * tokens with a matrix state, next to the diagonal one of the scans above), rotary positions with
+ * several axes for its queries and keys, and group norm with an activation.  None of the three is
+ * in the paper.  Activations have the storage type `dtype`; states, norm weights, their gradients
+ * and statistics are fp32, and so is all arithmetic.  Tokens (pixels) come before heads
+ * (channels).  A workspace of these calls serves them alone (not the scans, and the
+ * delta rule's not the norm); vmb_read_status reads its status word.
+ *
+ * vmb_delta_rule_fwd - the gated delta rule, from S_0 = initial_state (zeros if NULL), per
+ * sequence and value head, S [Dk, Dv], a_t = exp(g_t):
+ *     S_t = a_t (I - beta_t k_t k_t^T) S_{t-1} + beta_t k_t v_t^T,   o_t = scale S_t^T q_t
+ * (the state is decayed, what it returns for k_t is corrected towards v_t, then it is read),
+ * computed in chunks of 64 tokens.
+ *   q, k [B, T, Hk, Dk], v [B, T, Hv, Dv], g, beta [B, T, Hv], o [B, T, Hv, Dv] (dtype); Hv is a
+ *   multiple of Hk, value head h reads key head h / (Hv / Hk); initial_state, final_state
+ *   [B, Hv, Dk, Dv] fp32, either may be NULL; they may not overlap.
+ *   strides: NULL (dense), or six host values: the elements between batch rows and between tokens
+ *   of q, of k and of v (parts of one projection's output); heads and channels are dense.
+ *   offsets: NULL, or int32 [B + 1] on the device: B packed sequences, sequence b is rows
+ *   offsets[b] .. offsets[b + 1] - 1 of `total` tokens (the batch dimension of the tensors is
+ *   then 1, T a bound of the longest sequence, batch strides unused).  Without offsets total is
+ *   B * T.  Offsets that decrease, leave [0, total] or give a sequence longer than T are cut to
+ *   what is in range and reported as VMB_ERR_BOUNDS by vmb_read_status; rows that no sequence
+ *   holds are not written.
+ *   saved: NULL, or vmb_delta_rule_saved_bytes(...) bytes (16-byte aligned) that receive the
+ *   state before each chunk and the residuals v_t - S^T k_t, for vmb_delta_rule_bwd.
+ *   Keys of length above one with beta near one let the state grow, as the recurrence does.
+ *   g = -inf forgets the state exactly.  What is not finite in a token reaches the tokens after it,
+ *   as the recurrence has it, and no more than the 15 before it (those of its block of 16).  Dk in 1..128 (VMB_ERR_UNSUPPORTED above), any Dv >= 1.
+ *   workspace: >= vmb_delta_rule_workspace_bytes(..., grads = 0, ...) bytes, 256-byte aligned, the
+ *   first 256 zero-filled before its first use.
+ *   Rounding: bf16 storage takes products of the state and residuals with two bf16 values per
+ *   operand (16 bits) where they reach the state, one where they reach only o; fp32 storage takes
+ *   two tf32 values per operand (22 bits).  Sums, states and decays are fp32.
+ *
+ * vmb_delta_rule_bwd - the gradients, given dout = dLoss/do [B, T, Hv, Dv] and dfinal_state =
+ * dLoss/dS_T (or NULL): dq, dk, dv, dg, dbeta (shapes and type of the inputs, dense) and
+ * dinitial_state (fp32; NULL: not wanted).  saved: what the forward kept for the same inputs.  The
+ * gradients of a key head are summed over its value heads in order.  Deterministic.
+ *
+ * vmb_delta_rule_step - T tokens (a few) per sequence from the states in `state` [pool, Hv, Dk, Dv]
+ * fp32, updated in place: serving.  slots: NULL (row b uses state b; pool >= B), or int32 [B] on
+ * the device: the state of row b; rows whose slot is outside [0, pool) have none: their o is
+ * zero.  Slots in use are distinct.  The other arguments as above.  No workspace.
+ */
+size_t vmb_delta_rule_workspace_bytes(int B, int T, int64_t total, int packed, int Hk, int Hv, int Dk, int Dv,
+                                      int grads, vmb_dtype dtype);
+size_t vmb_delta_rule_saved_bytes(int B, int T, int64_t total, int packed, int Hv, int Dk, int Dv, vmb_dtype dtype);
+vmb_status vmb_delta_rule_fwd(const void* q, const void* k, const void* v, const void* g, const void* beta,
+                              const int64_t* strides, const float* initial_state, const int32_t* offsets,
+                              void* o, float* final_state, void* saved, int B, int T, int64_t total, int Hk,
+                              int Hv, int Dk, int Dv, float scale, vmb_dtype dtype, void* workspace,
+                              size_t workspace_bytes, cudaStream_t stream);
+vmb_status vmb_delta_rule_bwd(const void* q, const void* k, const void* g, const void* beta,
+                              const int64_t* strides, const int32_t* offsets, const void* dout,
+                              const float* dfinal_state, const void* saved, void* dq, void* dk, void* dv,
+                              void* dg, void* dbeta, float* dinitial_state, int B, int T, int64_t total,
+                              int Hk, int Hv, int Dk, int Dv, float scale, vmb_dtype dtype, void* workspace,
+                              size_t workspace_bytes, cudaStream_t stream);
+vmb_status vmb_delta_rule_step(const void* q, const void* k, const void* v, const void* g, const void* beta,
+                               const int64_t* strides, float* state, const int32_t* slots, void* o, int B,
+                               int T, int Hk, int Hv, int Dk, int Dv, int pool, float scale, vmb_dtype dtype,
+                               cudaStream_t stream);
+
+/*
+ * vmb_rotary_fwd - rotary positions with several axes (time, row, column, ...): the first 2P
+ * channels of every head are P pairs, pair i is turned by the angle p f_i, p the token's position
+ * on the pair's axis:  (x, y) -> (x cos - y sin, y cos + x sin); the other channels are copied.
+ *   q [B, T, Hq, D], k [B, T, Hk, D] or NULL (Hk = 0), q_out, k_out dense (dtype); an output may
+ *   be its (dense) input, otherwise outputs do not overlap inputs.
+ *   freq [P] fp32 (angle per position, of every pair); axes in 1..4; pairs[axes] (host): the
+ *   pairs of each axis, in the order of the channels, P their sum, 1 <= P, 2P <= D;
+ *   positions int32 [axes, B, T] on the device, or NULL: grid[axes] (host), whose product is T:
+ *   token t lies at its row-major place in that grid (a map: {H, W}; a video: {frames, H, W}).
+ *   strides: NULL (dense), or four host values: the elements between batch rows and between tokens
+ *   of q and of k.
+ *   flags: VMB_ROTARY_INTERLEAVED: pair i is channels (2i, 2i + 1), otherwise (i, i + P);
+ *          VMB_ROTARY_INVERSE: the opposite angle, which is the gradient with respect to q and k.
+ * Angles carry an error of about 2^-24 of a turn at any position (not 2^-24 of the angle).
+ */
+#define VMB_ROTARY_INTERLEAVED 0x1u
+#define VMB_ROTARY_INVERSE 0x2u
+vmb_status vmb_rotary_fwd(const void* q, const void* k, const float* freq, const int32_t* positions,
+                          void* q_out, void* k_out, int B, int T, int Hq, int Hk, int D, int axes,
+                          const int* pairs, const int* grid, const int64_t* strides, unsigned flags,
+                          vmb_dtype dtype, cudaStream_t stream);
+
+/*
+ * vmb_group_norm_fwd - group norm with an activation, channels last:
+ *   y = act(weight n + bias), n = (x - mean) rstd, mean and variance over the L pixels and the
+ *   C / G channels of a group, rstd = 1 / sqrt(variance + eps).
+ *   x, y [B, L, C] (dtype); weight, bias [C] fp32 or NULL (1 and 0); stats [B, G, 2] fp32 (mean,
+ *   rstd) or NULL.  G divides C; C <= 16384 (VMB_ERR_UNSUPPORTED above).
+ * vmb_group_norm_bwd - its gradients given dy [B, L, C]: dx (dtype), dweight, dbias [C] fp32
+ *   (either may be NULL); stats: the forward's.  Sums in a fixed order: deterministic (rows that are
+ *   not 16-byte aligned are summed in another order than aligned ones).
+ *   workspace: >= vmb_group_norm_workspace_bytes(...) bytes, 256-byte aligned, all of it
+ *   zero-filled before its first use; calls that share one must not overlap in time.
+ */
+typedef enum { VMB_ACT_NONE = 0, VMB_ACT_SILU = 1, VMB_ACT_GELU = 2 } vmb_act; /* GELU: z Phi(z), by erf */
+size_t vmb_group_norm_workspace_bytes(int B, int64_t L, int C, int G, int grads, vmb_dtype dtype);
+vmb_status vmb_group_norm_fwd(const void* x, const float* weight, const float* bias, void* y, float* stats,
+                              int B, int64_t L, int C, int G, float eps, vmb_act act, vmb_dtype dtype,
+                              void* workspace, size_t workspace_bytes, cudaStream_t stream);
+vmb_status vmb_group_norm_bwd(const void* x, const float* weight, const float* bias, const float* stats,
+                              const void* dy, void* dx, float* dweight, float* dbias, int B, int64_t L,
+                              int C, int G, vmb_act act, vmb_dtype dtype, void* workspace,
+                              size_t workspace_bytes, cudaStream_t stream);
+
+/*
  * vmb_read_status - synchronise `stream`, then return and clear the device
  * error word of `workspace` (VMB_OK, VMB_ERR_TIMEOUT or VMB_ERR_BOUNDS).  A
  * device-side error leaves the outputs of that call undefined but the CUDA

@@ -22,7 +22,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libvmb.so")
 BUILD_DIR = os.path.join(PKG, "_build")
 SOURCES = ["vmb_abi.cu", "cross_scan_merge.cu", "full_scan.cu", "full_ws_f32.cu", "full_ws_bf16.cu", "mean_scan.cu", "mean_backward.cu", "noalloc.cu",
-           "scan_only.cu", "selection.cu", "small_map.cu"]
+           "scan_only.cu", "selection.cu", "small_map.cu", "vmb_abi_mixer.cu", "delta.cu", "delta_f32.cu", "delta_bf16.cu",
+           "rotary.cu", "group_norm.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -1,0 +1,335 @@
+// delta.cu - the gated delta rule: plans, the kernel that joins the segments of a chain, the sum over
+// shared heads, and the recurrent step.
+#include "delta_common.cuh"
+#include "delta_internal.h"
+#include "vmb_internal.h"
+
+namespace vmb {
+
+namespace {
+
+// ------------------------------------------------------------------ joining segments
+
+// One CTA per chain and 16 rows of the transposed state: S' = S X + N from segment to segment (X the
+// segment's map, in reverse its transpose), fp32.  The sums N are replaced by the state at each
+// segment's start (in reverse: the gradient of the state at its end).
+constexpr int kJoinThreads = 128, kJoinRows = 16;
+__global__ void __launch_bounds__(kJoinThreads) delta_join_kernel(DeltaChain c, int reverse) {
+    extern __shared__ float sm[];
+    const DeltaArgs& a = c.a;
+    const int Dk = a.Dk, ld = Dk + 1, d = threadIdx.x;
+    float *X = sm, *S = sm + ((Dk * ld + 3) & ~3);  // S [Dk][16]
+    pdl_launch_dependents();
+    pdl_wait();
+    const int strips = (a.Dv + kJoinRows - 1) / kJoinRows;
+    const int row0 = (int)(blockIdx.x % strips) * kJoinRows;
+    const long long chain = blockIdx.x / strips;
+    const DeltaSeq seq = delta_seq(a.offsets, (int)(chain / a.Hv), a.T, a.total, c.err);
+    const int nseg = ((seq.len + kChunk - 1) / kChunk + c.seg_chunks - 1) / c.seg_chunks;
+    const float* init = reverse ? a.dfinal : a.initial;
+    float* last = reverse ? a.dinitial : a.final;
+    float s[kJoinRows];
+#pragma unroll
+    for (int r = 0; r < kJoinRows; ++r)
+        s[r] = init && d < Dk && row0 + r < a.Dv ? init[(chain * Dk + d) * a.Dv + row0 + r] : 0.0f;
+    for (int i = 0; i < nseg; ++i) {
+        const long long at = chain * c.segs + (reverse ? nseg - 1 - i : i);
+        const float* x = c.maps + at * Dk * Dk;
+        float* n = c.sums + at * a.Dv * Dk;
+        __syncthreads();
+        for (int j = threadIdx.x; j < Dk * Dk; j += kJoinThreads) X[(j / Dk) * ld + j % Dk] = x[j];
+        if (d < Dk) {
+#pragma unroll
+            for (int r = 0; r < kJoinRows; ++r) S[d * kJoinRows + r] = s[r];
+#pragma unroll
+            for (int r = 0; r < kJoinRows; ++r)
+                if (row0 + r < a.Dv) {
+                    float* p = n + (long long)(row0 + r) * Dk + d;
+                    const float sum = *p;
+                    *p = s[r];
+                    s[r] = sum;
+                }
+        }
+        __syncthreads();
+        if (d < Dk) {
+            const float* col = reverse ? X + d * ld : X + d;
+            const int step = reverse ? 1 : ld;
+#pragma unroll 4
+            for (int e = 0; e < Dk; ++e) {
+                const float v = col[e * step];
+#pragma unroll
+                for (int r = 0; r < kJoinRows; r += 4) {
+                    const float4 q = *reinterpret_cast<const float4*>(S + e * kJoinRows + r);
+                    s[r] = fmaf(q.x, v, s[r]);
+                    s[r + 1] = fmaf(q.y, v, s[r + 1]);
+                    s[r + 2] = fmaf(q.z, v, s[r + 2]);
+                    s[r + 3] = fmaf(q.w, v, s[r + 3]);
+                }
+            }
+        }
+    }
+    if (last && d < Dk) {
+#pragma unroll
+        for (int r = 0; r < kJoinRows; ++r)
+            if (row0 + r < a.Dv) last[(chain * Dk + d) * a.Dv + row0 + r] = s[r];
+    }
+}
+
+// ------------------------------------------------------------------ shared heads
+
+// dq and dk of a key head: the sum, in order, of those of its value heads.
+template <typename T>
+__global__ void __launch_bounds__(256) delta_share_kernel(const float* part, T* dq, T* dk, long long n, int Hk, int r, int Dk) {
+    pdl_launch_dependents();
+    pdl_wait();
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        const int d = (int)(i % Dk);
+        const long long head = i / Dk;  // token * Hk + key head
+        const float* p = part + head * r * 2 * Dk + d;
+        float q = 0.0f, k = 0.0f;
+        for (int j = 0; j < r; ++j) q += p[(long long)j * 2 * Dk], k += p[(long long)j * 2 * Dk + Dk];
+        dq[i] = io<T>::to(q);
+        dk[i] = io<T>::to(k);
+    }
+}
+
+// ------------------------------------------------------------------ the recurrent step
+
+// One warp per 32 value channels of a head: lane (p = lane / 8, c = lane % 8) holds rows 4i + p of the state
+// for channels 4c .. 4c + 3, so that the state is read once and written once, in 128-byte rows, and the
+// sums over the rows take two shuffles.  One pass over the old state gives both S^T k and S^T q:
+//   S_t^T q = a S^T q + (q.k) u,  u = b (v - a S^T k).
+// Bound by the state's bytes (8 Dk Dv per row of the batch and head).
+template <typename T, int RPL>
+__global__ void __launch_bounds__(128) delta_step_kernel(DeltaStep a) {
+    __shared__ float2 qk[4 * RPL];
+    __shared__ float red[4];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, p = lane >> 3, c = (lane & 7) * 4;
+    const int groups = (a.Dv + 127) / 128;
+    const int grp = blockIdx.x % groups;
+    const long long bh = blockIdx.x / groups;
+    const int h = (int)(bh % a.Hv), b = (int)(bh / a.Hv), hk = h / (a.Hv / a.Hk);
+    const int v0 = grp * 128 + w * 32 + c;
+    const long long slot = a.slots ? a.slots[b] : b;
+    T* op = (T*)a.o + ((long long)b * a.T * a.Hv + h) * a.Dv;
+    if (slot < 0 || slot >= a.pool) {  // no state: a row of padding
+        for (int t = 0; t < a.T; ++t)
+            if (grp * 128 + tid < a.Dv) op[(long long)t * a.Hv * a.Dv + grp * 128 + tid] = io<T>::to(0.0f);
+        return;
+    }
+    float* sp = a.state + (slot * a.Hv + h) * a.Dk * a.Dv + v0;
+    const bool vec = a.Dv % 4 == 0 && (reinterpret_cast<uintptr_t>(a.state) & 15) == 0;
+    float4 S[RPL];
+#pragma unroll
+    for (int i = 0; i < RPL; ++i) {
+        const int d = 4 * i + p;
+        S[i] = make_float4(0, 0, 0, 0);
+        if (d >= a.Dk) continue;
+        const float* s = sp + (long long)d * a.Dv;
+        if (vec) {
+            if (v0 < a.Dv) S[i] = *reinterpret_cast<const float4*>(s);
+        } else {
+            if (v0 < a.Dv) S[i].x = s[0];
+            if (v0 + 1 < a.Dv) S[i].y = s[1];
+            if (v0 + 2 < a.Dv) S[i].z = s[2];
+            if (v0 + 3 < a.Dv) S[i].w = s[3];
+        }
+    }
+    for (int t = 0; t < a.T; ++t) {
+        const T* qp = (const T*)a.q + b * a.q_b + t * a.q_t + (long long)hk * a.Dk;
+        const T* kp = (const T*)a.k + b * a.k_b + t * a.k_t + (long long)hk * a.Dk;
+        const T* vp = (const T*)a.v + b * a.v_b + t * a.v_t + (long long)h * a.Dv;
+        const long long gi = ((long long)b * a.T + t) * a.Hv + h;
+        const float gain = expf(io<T>::cvt(((const T*)a.g)[gi])), beta = io<T>::cvt(((const T*)a.beta)[gi]);
+        float v[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v[x] = v0 + x < a.Dv ? io<T>::cvt(vp[v0 + x]) : 0.0f;
+        __syncthreads();  // the previous token's q and k have been read
+        float dot = 0.0f;
+        if (tid < 4 * RPL) {
+            float2 x = make_float2(0, 0);
+            if (tid < a.Dk) x = make_float2(io<T>::cvt(qp[tid]), io<T>::cvt(kp[tid]));
+            qk[tid] = x;
+            dot = x.x * x.y;
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, d);
+        if (lane == 0) red[w] = dot;
+        __syncthreads();
+        dot = (red[0] + red[1]) + (red[2] + red[3]);
+        float4 sk = make_float4(0, 0, 0, 0), sq = sk;
+#pragma unroll
+        for (int i = 0; i < RPL; ++i) {
+            const float2 x = qk[4 * i + p];
+            sq.x = fmaf(S[i].x, x.x, sq.x), sq.y = fmaf(S[i].y, x.x, sq.y), sq.z = fmaf(S[i].z, x.x, sq.z), sq.w = fmaf(S[i].w, x.x, sq.w);
+            sk.x = fmaf(S[i].x, x.y, sk.x), sk.y = fmaf(S[i].y, x.y, sk.y), sk.z = fmaf(S[i].z, x.y, sk.z), sk.w = fmaf(S[i].w, x.y, sk.w);
+        }
+#pragma unroll
+        for (int d = 8; d <= 16; d <<= 1) {
+            sk.x += __shfl_xor_sync(0xffffffffu, sk.x, d), sk.y += __shfl_xor_sync(0xffffffffu, sk.y, d);
+            sk.z += __shfl_xor_sync(0xffffffffu, sk.z, d), sk.w += __shfl_xor_sync(0xffffffffu, sk.w, d);
+            sq.x += __shfl_xor_sync(0xffffffffu, sq.x, d), sq.y += __shfl_xor_sync(0xffffffffu, sq.y, d);
+            sq.z += __shfl_xor_sync(0xffffffffu, sq.z, d), sq.w += __shfl_xor_sync(0xffffffffu, sq.w, d);
+        }
+        const float4 u = make_float4(beta * (v[0] - gain * sk.x), beta * (v[1] - gain * sk.y), beta * (v[2] - gain * sk.z),
+                                     beta * (v[3] - gain * sk.w));
+#pragma unroll
+        for (int i = 0; i < RPL; ++i) {
+            const float k = qk[4 * i + p].y;
+            S[i].x = fmaf(gain, S[i].x, k * u.x), S[i].y = fmaf(gain, S[i].y, k * u.y);
+            S[i].z = fmaf(gain, S[i].z, k * u.z), S[i].w = fmaf(gain, S[i].w, k * u.w);
+        }
+        // each of the four lanes of a channel quad writes one channel
+        const float os = p == 0 ? fmaf(gain, sq.x, dot * u.x) : p == 1 ? fmaf(gain, sq.y, dot * u.y)
+                       : p == 2 ? fmaf(gain, sq.z, dot * u.z) : fmaf(gain, sq.w, dot * u.w);
+        if (v0 + p < a.Dv) op[(long long)t * a.Hv * a.Dv + v0 + p] = io<T>::to(a.scale * os);
+    }
+#pragma unroll
+    for (int i = 0; i < RPL; ++i) {
+        const int d = 4 * i + p;
+        if (d >= a.Dk) continue;
+        float* s = sp + (long long)d * a.Dv;
+        if (vec) {
+            if (v0 < a.Dv) *reinterpret_cast<float4*>(s) = S[i];
+        } else {
+            if (v0 < a.Dv) s[0] = S[i].x;
+            if (v0 + 1 < a.Dv) s[1] = S[i].y;
+            if (v0 + 2 < a.Dv) s[2] = S[i].z;
+            if (v0 + 3 < a.Dv) s[3] = S[i].w;
+        }
+    }
+}
+
+vmb_status chain(const DeltaChain& c, bool reverse, cudaStream_t stream) {
+    return c.a.dtype == VMB_BF16 ? launch_chain_bf16(c, reverse, stream) : launch_chain_f32(c, reverse, stream);
+}
+
+vmb_status join(const DeltaChain& c, bool reverse, cudaStream_t stream) {
+    const int strips = (c.a.Dv + kJoinRows - 1) / kJoinRows;
+    const size_t smem = 4 * (size_t)(((c.a.Dk * (c.a.Dk + 1) + 3) & ~3) + c.a.Dk * kJoinRows);
+    const void* fn = (const void*)delta_join_kernel;
+    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, 100 * 1024) != cudaSuccess) return VMB_ERR_CUDA;
+    DeltaChain arg = c;
+    int rev = reverse;
+    void* args[] = {&arg, &rev};
+    return launch_kernel(fn, dim3((unsigned)(c.a.B * (long long)c.a.Hv * strips)), dim3(kJoinThreads), smem, args, stream) == cudaSuccess
+               ? VMB_OK : VMB_ERR_CUDA;
+}
+
+DeltaChain chain_of(const DeltaArgs& a, const DeltaPlan& p) {
+    DeltaChain c{};
+    c.a = a;
+    c.segs = p.segs;
+    c.seg_chunks = p.seg_chunks;
+    c.slices = p.slices;
+    unsigned char* ws = (unsigned char*)a.ws;
+    c.maps = (float*)(ws + p.maps_off);
+    c.sums = (float*)(ws + p.sums_off);
+    c.ds = ws + p.ds_off;
+    c.dx = ws + p.dx_off;
+    c.err = a.offsets ? &reinterpret_cast<WsHeader*>(a.ws)->err : nullptr;
+    return c;
+}
+
+}  // namespace
+
+long long delta_slots(int B, int T, long long total, bool packed) {
+    return packed ? total / kChunk + B : (long long)B * ((T + kChunk - 1) / kChunk);
+}
+
+DeltaPlan plan_delta(const DeltaArgs& a, bool grads, int sms) {
+    DeltaPlan p{};
+    const long long chains = (long long)a.B * a.Hv;
+    p.chunks = (a.T + kChunk - 1) / kChunk;
+    p.slices = (a.Dv + kDeltaRows - 1) / kDeltaRows;
+    p.slots = delta_slots(a.B, a.T, a.total, a.offsets != nullptr);
+    p.segs = 1;
+    p.seg_chunks = p.chunks;
+    const long long ctas = chains * p.slices;
+    // Segments cost a second pass over the chunks (and Dk more rows in it): taken when the chains leave
+    // more than half of the SMs idle and each segment still has two chunks.
+    if (ctas * 2 <= sms && p.chunks >= 4) {
+        long long segs = sms / ctas;
+        if (segs > p.chunks / 2) segs = p.chunks / 2;
+        if (segs > 1) {
+            p.seg_chunks = (int)((p.chunks + segs - 1) / segs);
+            p.segs = (p.chunks + p.seg_chunks - 1) / p.seg_chunks;
+        }
+    }
+    const size_t es = a.dtype == VMB_BF16 ? 2 : 4;
+    size_t at = 256;
+    p.maps_off = at;
+    if (p.segs > 1) at += align_up((size_t)chains * p.segs * a.Dk * a.Dk * 4, 256);
+    p.sums_off = at;
+    if (p.segs > 1) at += align_up((size_t)chains * p.segs * a.Dv * a.Dk * 4, 256);
+    p.ds_off = p.dx_off = p.part_off = at;
+    if (grads) {
+        at += align_up((size_t)p.slots * a.Hv * a.Dv * a.Dk * es, 256);
+        p.dx_off = at;
+        at += align_up((size_t)a.total * a.Hv * a.Dv * es, 256);
+        p.part_off = at;
+        if (a.Hv != a.Hk) at += align_up((size_t)a.total * a.Hv * 2 * a.Dk * 4, 256);
+    }
+    p.bytes = at;
+    return p;
+}
+
+vmb_status launch_delta_fwd(const DeltaArgs& a, cudaStream_t stream) {
+    const DeltaPlan p = plan_delta(a, false, device_sm_count());
+    if (a.ws_bytes < p.bytes) return VMB_ERR_WORKSPACE;
+    DeltaChain c = chain_of(a, p);
+    if (p.segs > 1) {
+        c.summary = 1;
+        vmb_status s = chain(c, false, stream);
+        if (s == VMB_OK) s = join(c, false, stream);
+        if (s != VMB_OK) return s;
+        c.summary = 0;
+    }
+    return chain(c, false, stream);
+}
+
+vmb_status launch_delta_bwd(const DeltaArgs& a, cudaStream_t stream) {
+    const DeltaPlan p = plan_delta(a, true, device_sm_count());
+    if (a.ws_bytes < p.bytes) return VMB_ERR_WORKSPACE;
+    DeltaChain c = chain_of(a, p);
+    vmb_status s;
+    if (p.segs > 1) {
+        c.summary = c.maps_only = 1;
+        if ((s = chain(c, false, stream)) != VMB_OK) return s;
+        if ((s = chain(c, true, stream)) != VMB_OK) return s;
+        if ((s = join(c, true, stream)) != VMB_OK) return s;
+        c.summary = c.maps_only = 0;
+    }
+    if ((s = chain(c, true, stream)) != VMB_OK || a.T == 0 || a.total == 0) return s;
+    DeltaGrad g{};
+    g.a = a;
+    g.ds = c.ds;
+    g.dx = c.dx;
+    g.part = (float*)((unsigned char*)a.ws + p.part_off);
+    g.err = c.err;
+    if ((s = a.dtype == VMB_BF16 ? launch_grad_bf16(g, stream) : launch_grad_f32(g, stream)) != VMB_OK) return s;
+    if (a.Hv == a.Hk) return VMB_OK;
+    long long n = a.total * a.Hk * a.Dk;
+    int Hk = a.Hk, r = a.Hv / a.Hk, Dk = a.Dk;
+    const long long want = (n + 255) / 256, most = (long long)device_sm_count() * 8;
+    const void* part = g.part;
+    void *dq = a.dq, *dk = a.dk;
+    void* args[] = {&part, &dq, &dk, &n, &Hk, &r, &Dk};
+    const void* fn = a.dtype == VMB_BF16 ? (const void*)delta_share_kernel<__nv_bfloat16> : (const void*)delta_share_kernel<float>;
+    return launch_kernel(fn, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, args, stream) == cudaSuccess ? VMB_OK
+                                                                                                              : VMB_ERR_CUDA;
+}
+
+vmb_status launch_delta_step(const DeltaStep& a, cudaStream_t stream) {
+    const long long grid = (long long)a.B * a.Hv * ((a.Dv + 127) / 128);
+    const void* fn = a.dtype == VMB_BF16
+                         ? (a.Dk <= 64 ? (const void*)delta_step_kernel<__nv_bfloat16, 16> : (const void*)delta_step_kernel<__nv_bfloat16, 32>)
+                         : (a.Dk <= 64 ? (const void*)delta_step_kernel<float, 16> : (const void*)delta_step_kernel<float, 32>);
+    DeltaStep arg = a;
+    void* args[] = {&arg};
+    return launch_kernel(fn, dim3((unsigned)grid), dim3(128), 0, args, stream) == cudaSuccess ? VMB_OK : VMB_ERR_CUDA;
+}
+
+}  // namespace vmb

@@ -1,0 +1,466 @@
+// delta_common.cuh - device code shared by the kernels of the gated delta rule
+// (delta_chain.cuh, delta_grad.cuh): tiles in shared memory, matrix fragments,
+// the decays of a chunk and its triangular system.
+//
+// The recurrence of one head, S [Dk x Dv]:
+//   S_t = a_t (I - b_t k_t k_t^T) S_{t-1} + b_t k_t v_t^T,  a_t = e^(g_t),  o_t = scale S_t^T q_t
+// is computed in chunks of 64 tokens.  With c_i the log decays summed from the chunk's start to
+// token i, S the state before the chunk and r_i the residual that token i adds (u_i = b_i r_i):
+//   E_ij = e^(c_i - c_j) k_i.k_j (j < i),   r = v - e^c K S - E (b r),
+//   o_i = scale (e^(c_i) S^T q_i + sum_{j<=i} e^(c_i - c_j) (q_i.k_j) u_j),
+//   S' = e^(c_last) S + sum_j e^(c_last - c_j) k_j u_j^T.
+// The triangular system for r is solved in four blocks of 16 tokens, whose diagonal blocks are
+// inverted explicitly: 4 x (16 x 16), by forward substitution in fp32.
+//
+// Every product runs on the tensor cores through mma.sync, whose accumulator layout is that of its
+// A operand: with the states and residuals transposed (rows = value channels) a warp carries 16
+// rows from product to product in registers, without a barrier or a trip through shared memory
+// (measured on the GB300: 604 TFLOP/s in bf16, 302 in tf32 and 21 cycles of latency, against a
+// dependent chain of four products per chunk).  What a product rounds:
+//   bf16 storage: q, k, v and do are exact.  Intermediates (states, residuals, E, the diagonal
+//     inverses) enter as the sum of two bf16 values (16 bits, error about 2^-18) wherever they
+//     reach the state, as one where they only reach an output that is rounded to bf16 itself.
+//   fp32 storage: every operand is the sum of two tf32 values (22 bits), products hi.hi + hi.lo + lo.hi.
+// Accumulators, states, decays and the diagonal inverses are fp32 throughout.
+#pragma once
+
+#include "vmb_common.cuh"
+
+namespace vmb {
+
+constexpr int kChunk = 64;       // tokens per chunk
+constexpr int kDeltaThreads = 128;
+constexpr int kDeltaRows = 64;   // value channels (state rows) per CTA: 16 per warp
+
+// ------------------------------------------------------------------ fragments
+
+// acc is a 16 x 8 fp32 accumulator tile: lane (g = lane / 4, t = lane % 4) holds
+// (g, 2t), (g, 2t + 1), (g + 8, 2t), (g + 8, 2t + 1).
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float bf16_lo(uint32_t p) { return __uint_as_float(p << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t p) { return __uint_as_float(p & 0xffff0000u); }
+__device__ __forceinline__ uint32_t to_tf32(float x) {
+    uint32_t r;
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ void split_tf32(float x, uint32_t& hi, uint32_t& lo) {
+    hi = to_tf32(x);
+    lo = to_tf32(x - __uint_as_float(hi));
+}
+
+// Operands of a 16-deep step.  bf16: NT terms.  fp32: two 8-deep tf32 steps s; position k of step
+// s stands for column 8s + 2(k % 4) + k / 4, the same in A and B, so that an accumulator pair
+// (columns 2t, 2t + 1) is an A operand as it stands.
+template <typename T, int NT> struct FragA;
+template <typename T, int NT> struct FragB;
+template <int NT> struct FragA<__nv_bfloat16, NT> { uint32_t r[NT][4]; };
+template <int NT> struct FragB<__nv_bfloat16, NT> { uint32_t r[NT][2]; };
+template <int NT> struct FragA<float, NT> { uint32_t hi[2][4], lo[2][4]; };
+template <int NT> struct FragB<float, NT> { uint32_t hi[2][2], lo[2][2]; };
+
+// c += a b, the small products first; the product of two second terms is left out
+template <int NA, int NB>
+__device__ __forceinline__ void mma16(float (&c)[4], const FragA<__nv_bfloat16, NA>& a, const FragB<__nv_bfloat16, NB>& b) {
+    if constexpr (NA > 1) mma_bf16(c, a.r[1], b.r[0]);
+    if constexpr (NB > 1) mma_bf16(c, a.r[0], b.r[1]);
+    mma_bf16(c, a.r[0], b.r[0]);
+}
+// (fp32: the small products are summed on their own, because every product that is added to a large
+// accumulator on the tensor cores truncates it: 2 times instead of 6)
+template <int NA, int NB>
+__device__ __forceinline__ void mma16(float (&c)[4], const FragA<float, NA>& a, const FragB<float, NB>& b) {
+    float d[4] = {};
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        mma_tf32(d, a.lo[s], b.hi[s]);
+        mma_tf32(d, a.hi[s], b.lo[s]);
+        mma_tf32(c, a.hi[s], b.hi[s]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] += d[i];
+}
+
+// A from two neighbouring accumulator tiles (16 columns)
+template <int NT>
+__device__ __forceinline__ void frag_from_acc(FragA<__nv_bfloat16, NT>& a, const float (&c0)[4], const float (&c1)[4]) {
+    a.r[0][0] = pack_bf16(c0[0], c0[1]);
+    a.r[0][1] = pack_bf16(c0[2], c0[3]);
+    a.r[0][2] = pack_bf16(c1[0], c1[1]);
+    a.r[0][3] = pack_bf16(c1[2], c1[3]);
+    if constexpr (NT > 1) {
+        a.r[1][0] = pack_bf16(c0[0] - bf16_lo(a.r[0][0]), c0[1] - bf16_hi(a.r[0][0]));
+        a.r[1][1] = pack_bf16(c0[2] - bf16_lo(a.r[0][1]), c0[3] - bf16_hi(a.r[0][1]));
+        a.r[1][2] = pack_bf16(c1[0] - bf16_lo(a.r[0][2]), c1[1] - bf16_hi(a.r[0][2]));
+        a.r[1][3] = pack_bf16(c1[2] - bf16_lo(a.r[0][3]), c1[3] - bf16_hi(a.r[0][3]));
+    }
+}
+template <int NT>
+__device__ __forceinline__ void frag_from_acc(FragA<float, NT>& a, const float (&c0)[4], const float (&c1)[4]) {
+    split_tf32(c0[0], a.hi[0][0], a.lo[0][0]);
+    split_tf32(c0[2], a.hi[0][1], a.lo[0][1]);
+    split_tf32(c0[1], a.hi[0][2], a.lo[0][2]);
+    split_tf32(c0[3], a.hi[0][3], a.lo[0][3]);
+    split_tf32(c1[0], a.hi[1][0], a.lo[1][0]);
+    split_tf32(c1[2], a.hi[1][1], a.lo[1][1]);
+    split_tf32(c1[1], a.hi[1][2], a.lo[1][2]);
+    split_tf32(c1[3], a.hi[1][3], a.lo[1][3]);
+}
+
+// ------------------------------------------------------------------ tiles in shared memory
+
+// Row-major tiles.  bf16: NT planes, rows padded by 16 bytes, which puts the eight rows of an
+// ldmatrix on different banks.  fp32: no padding; the 8-column blocks of row r are permuted within
+// 32 columns by sw(r), which makes both the pair loads along a row (8 rows x 4 pairs) and the
+// loads down the columns (rows 2t and 2t + 1) free of conflicts.
+template <typename T, int COLS, int NT> struct Tile;
+
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+
+template <int COLS, int NT> struct Tile<__nv_bfloat16, COLS, NT> {
+    using T = __nv_bfloat16;
+    static constexpr int kLd = COLS + 8, kVec = 8;
+    static constexpr int bytes(int rows) { return NT * rows * kLd * 2; }
+    T* p;
+    int plane;  // elements between the planes
+    __device__ __forceinline__ Tile(void* s, int rows) : p((T*)s), plane(rows * kLd) {}
+    __device__ __forceinline__ T* vec_at(int r, int c) const { return p + r * kLd + c; }
+    __device__ __forceinline__ void set(int r, int c, float v) const {
+        const T h = __float2bfloat16_rn(v);
+        p[r * kLd + c] = h;
+        if constexpr (NT > 1) p[plane + r * kLd + c] = __float2bfloat16_rn(v - __bfloat162float(h));
+    }
+    __device__ __forceinline__ void set2(int r, int c, float v0, float v1) const {  // c even
+        const uint32_t h = pack_bf16(v0, v1);
+        *reinterpret_cast<uint32_t*>(p + r * kLd + c) = h;
+        if constexpr (NT > 1)
+            *reinterpret_cast<uint32_t*>(p + plane + r * kLd + c) = pack_bf16(v0 - bf16_lo(h), v1 - bf16_hi(h));
+    }
+    __device__ __forceinline__ void zero(int r, int c) const { p[r * kLd + c] = __float2bfloat16_rn(0.0f); }
+    __device__ __forceinline__ void put(int r, int c, T v) const { p[r * kLd + c] = v; }
+    __device__ __forceinline__ float get(int r, int c) const {
+        float v = __bfloat162float(p[r * kLd + c]);
+        if constexpr (NT > 1) v += __bfloat162float(p[plane + r * kLd + c]);
+        return v;
+    }
+    __device__ __forceinline__ uint32_t lane_addr(int term, int r0, int c0) const {
+        const int lane = threadIdx.x & 31;
+        return smem_u32(p + term * plane + (r0 + (lane & 15)) * kLd + c0 + (lane >> 4) * 8);
+    }
+    // A[m][k] = tile[m0 + m][k0 + k]
+    template <int N = NT> __device__ __forceinline__ void a_mk(FragA<T, N>& a, int m0, int k0) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) ldmatrix4(a.r[i], lane_addr(i, m0, k0));
+    }
+    // A[m][k] = tile[k0 + k][m0 + m]
+    template <int N = NT> __device__ __forceinline__ void a_km(FragA<T, N>& a, int m0, int k0) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t r[4];
+            ldmatrix4_t(r, lane_addr(i, k0, m0));
+            a.r[i][0] = r[0];
+            a.r[i][1] = r[2];
+            a.r[i][2] = r[1];
+            a.r[i][3] = r[3];
+        }
+    }
+    // two column tiles: B[k][n] = tile[n0 + n][k0 + k], n < 8 in b0, n >= 8 in b1
+    template <int N = NT> __device__ __forceinline__ void b_nk(FragB<T, N>& b0, FragB<T, N>& b1, int n0, int k0) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t r[4];
+            ldmatrix4(r, lane_addr(i, n0, k0));
+            b0.r[i][0] = r[0];
+            b0.r[i][1] = r[2];
+            b1.r[i][0] = r[1];
+            b1.r[i][1] = r[3];
+        }
+    }
+    // B[k][n] = tile[k0 + k][n0 + n]
+    template <int N = NT> __device__ __forceinline__ void b_kn(FragB<T, N>& b0, FragB<T, N>& b1, int k0, int n0) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t r[4];
+            ldmatrix4_t(r, lane_addr(i, k0, n0));
+            b0.r[i][0] = r[0];
+            b0.r[i][1] = r[1];
+            b1.r[i][0] = r[2];
+            b1.r[i][1] = r[3];
+        }
+    }
+    // the transposed 16 x 16 block as two accumulator tiles: c[j] holds columns k0 + 8j .. of rows m0 ..
+    __device__ __forceinline__ void acc_km(float (&c0)[4], float (&c1)[4], int m0, int k0) const {
+        FragA<T, 1> a;
+        a_km<1>(a, m0, k0);
+        c0[0] = bf16_lo(a.r[0][0]), c0[1] = bf16_hi(a.r[0][0]), c0[2] = bf16_lo(a.r[0][1]), c0[3] = bf16_hi(a.r[0][1]);
+        c1[0] = bf16_lo(a.r[0][2]), c1[1] = bf16_hi(a.r[0][2]), c1[2] = bf16_lo(a.r[0][3]), c1[3] = bf16_hi(a.r[0][3]);
+    }
+};
+
+template <int COLS, int NT> struct Tile<float, COLS, NT> {
+    using T = float;
+    static constexpr int kLd = COLS, kVec = 4;
+    static_assert(COLS % 32 == 0, "the permutation works within 32 columns");
+    static constexpr int bytes(int rows) { return rows * kLd * 4; }
+    T* p;
+    __device__ __forceinline__ Tile(void* s, int) : p((T*)s) {}
+    __device__ __forceinline__ static int at(int r, int c) { return r * kLd + (c ^ (((r & 3) ^ ((r >> 2) & 1)) << 3)); }
+    __device__ __forceinline__ T* vec_at(int r, int c) const { return p + at(r, c); }
+    __device__ __forceinline__ void set(int r, int c, float v) const { p[at(r, c)] = v; }
+    __device__ __forceinline__ void set2(int r, int c, float v0, float v1) const {
+        *reinterpret_cast<float2*>(p + at(r, c)) = make_float2(v0, v1);
+    }
+    __device__ __forceinline__ void zero(int r, int c) const { p[at(r, c)] = 0.0f; }
+    __device__ __forceinline__ void put(int r, int c, T v) const { p[at(r, c)] = v; }
+    __device__ __forceinline__ float get(int r, int c) const { return p[at(r, c)]; }
+    template <int N = NT> __device__ __forceinline__ void a_mk(FragA<T, N>& a, int m0, int k0) const {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const float2 u = *reinterpret_cast<const float2*>(p + at(m0 + g, k0 + 8 * s + 2 * t));
+            const float2 w = *reinterpret_cast<const float2*>(p + at(m0 + g + 8, k0 + 8 * s + 2 * t));
+            split_tf32(u.x, a.hi[s][0], a.lo[s][0]);
+            split_tf32(w.x, a.hi[s][1], a.lo[s][1]);
+            split_tf32(u.y, a.hi[s][2], a.lo[s][2]);
+            split_tf32(w.y, a.hi[s][3], a.lo[s][3]);
+        }
+    }
+    template <int N = NT> __device__ __forceinline__ void a_km(FragA<T, N>& a, int m0, int k0) const {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int k = k0 + 8 * s + 2 * t;
+            split_tf32(p[at(k, m0 + g)], a.hi[s][0], a.lo[s][0]);
+            split_tf32(p[at(k, m0 + g + 8)], a.hi[s][1], a.lo[s][1]);
+            split_tf32(p[at(k + 1, m0 + g)], a.hi[s][2], a.lo[s][2]);
+            split_tf32(p[at(k + 1, m0 + g + 8)], a.hi[s][3], a.lo[s][3]);
+        }
+    }
+    template <int N = NT> __device__ __forceinline__ void b_nk(FragB<T, N>& b0, FragB<T, N>& b1, int n0, int k0) const {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const float2 u = *reinterpret_cast<const float2*>(p + at(n0 + g, k0 + 8 * s + 2 * t));
+            const float2 w = *reinterpret_cast<const float2*>(p + at(n0 + 8 + g, k0 + 8 * s + 2 * t));
+            split_tf32(u.x, b0.hi[s][0], b0.lo[s][0]);
+            split_tf32(u.y, b0.hi[s][1], b0.lo[s][1]);
+            split_tf32(w.x, b1.hi[s][0], b1.lo[s][0]);
+            split_tf32(w.y, b1.hi[s][1], b1.lo[s][1]);
+        }
+    }
+    template <int N = NT> __device__ __forceinline__ void b_kn(FragB<T, N>& b0, FragB<T, N>& b1, int k0, int n0) const {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int k = k0 + 8 * s + 2 * t;
+            split_tf32(p[at(k, n0 + g)], b0.hi[s][0], b0.lo[s][0]);
+            split_tf32(p[at(k + 1, n0 + g)], b0.hi[s][1], b0.lo[s][1]);
+            split_tf32(p[at(k, n0 + 8 + g)], b1.hi[s][0], b1.lo[s][0]);
+            split_tf32(p[at(k + 1, n0 + 8 + g)], b1.hi[s][1], b1.lo[s][1]);
+        }
+    }
+    __device__ __forceinline__ void acc_km(float (&c0)[4], float (&c1)[4], int m0, int k0) const {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int k = k0 + 8 * j + 2 * t;
+            float(&c)[4] = j ? c1 : c0;
+            c[0] = p[at(k, m0 + g)], c[1] = p[at(k + 1, m0 + g)];
+            c[2] = p[at(k, m0 + g + 8)], c[3] = p[at(k + 1, m0 + g + 8)];
+        }
+    }
+};
+
+// ------------------------------------------------------------------ global <-> shared
+
+// A head's tile of `rows` x `cols` values at src (row stride in elements) into a tile of ROWS x COLS,
+// zeros outside: asynchronous 16-byte copies where the rows allow them (`vec`), single values otherwise.
+// The caller commits and waits.
+template <int ROWS, int COLS, typename TL>
+__device__ __forceinline__ void load_tile(const TL& s, const typename TL::T* src, long long stride, int rows, int cols,
+                                          bool vec, int tid, int threads) {
+    using T = typename TL::T;
+    constexpr int V = TL::kVec, P = COLS / V;
+    if (vec) {
+        for (int i = tid; i < ROWS * P; i += threads) {
+            const int r = i / P, c = (i % P) * V;
+            const int n = r < rows ? min(max(cols - c, 0), V) * (int)sizeof(T) : 0;
+            cp_async16(s.vec_at(r, c), n ? src + r * stride + c : src, n);
+        }
+    } else {
+        for (int i = tid; i < ROWS * COLS; i += threads) {
+            const int r = i / COLS, c = i % COLS;
+            if (r < rows && c < cols)
+                s.put(r, c, src[r * stride + c]);
+            else
+                s.zero(r, c);
+        }
+    }
+}
+// 16-byte copies are possible: pointer and row stride are multiples of 16 bytes
+template <typename T> __device__ __forceinline__ bool rows_aligned(const T* p, long long stride) {
+    return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(stride * (long long)sizeof(T))) & 15) == 0;
+}
+
+// ------------------------------------------------------------------ where a sequence lies
+
+struct DeltaSeq {
+    long long start;  // first token of the sequence (packed) or of its batch row
+    int len;          // tokens
+    int slot;         // first chunk's place among the kept states
+};
+// Packed sequences (offsets): rows offsets[b] .. offsets[b + 1] - 1 of the `total` tokens.  Offsets that
+// leave [0, total], decrease or exceed the stated longest length are cut to what is in range and
+// reported in the status word.
+__device__ __forceinline__ DeltaSeq delta_seq(const int* offsets, int b, int T, long long total, unsigned* err) {
+    if (!offsets) return {(long long)b * T, T, b * ((T + kChunk - 1) / kChunk)};
+    const long long a = offsets[b], e = offsets[b + 1];
+    const long long lo = a < 0 ? 0 : (a > total ? total : a), hi = e < lo ? lo : (e > total ? total : e);
+    const int len = (int)(hi - lo < T ? hi - lo : T);
+    if ((a != lo || e != hi || hi - lo != len) && err && threadIdx.x == 0) atomicOr(err, kErrBounds);
+    return {lo, len, (int)(lo / kChunk) + b};
+}
+
+// ------------------------------------------------------------------ decays of a chunk
+
+// Per token, in shared memory.  The log decays are summed as pairs of floats (hi + lo), so that a
+// difference c_i - c_j keeps fp32 accuracy however small c is: a token that resets the state (g = -inf,
+// taken as -200, whose exponential is 0 in fp32) does not cost the tokens after it any digits.
+struct ChunkGates {
+    float hi[kChunk], lo[kChunk];  // c
+    float beta[kChunk];
+    float ec[kChunk];    // e^c
+    float tail[kChunk];  // e^(c_last - c)
+    float last;          // e^(c_last)
+};
+__device__ __forceinline__ float decay(float hi, float lo) { return ex2((hi + lo) * kLog2e); }
+
+__device__ __forceinline__ void add_pair(float& h, float& l, float h2, float l2) {
+    // Knuth's two-sum, then the low parts
+    const float s = h + h2, bb = s - h;
+    const float e = (h - (s - bb)) + (h2 - bb);
+    const float lo = e + (l + l2);
+    h = s + lo;
+    l = lo - (h - s);
+}
+
+// Called by one whole warp: lane l holds tokens 2l and 2l + 1 (g = 0 and beta = 0 behind the end).
+__device__ __forceinline__ void chunk_gates(ChunkGates& G, float g0, float g1, float b0, float b1) {
+    const int lane = threadIdx.x & 31;
+    g0 = g0 < -200.0f ? -200.0f : g0;
+    g1 = g1 < -200.0f ? -200.0f : g1;
+    float h = g0, l = 0.0f;
+    add_pair(h, l, g1, 0.0f);  // both tokens
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const float h2 = __shfl_up_sync(0xffffffffu, h, d), l2 = __shfl_up_sync(0xffffffffu, l, d);
+        if (lane >= d) add_pair(h, l, h2, l2);
+    }
+    const float lh = __shfl_sync(0xffffffffu, h, 31), ll = __shfl_sync(0xffffffffu, l, 31);
+    float ph = __shfl_up_sync(0xffffffffu, h, 1), pl = __shfl_up_sync(0xffffffffu, l, 1);
+    if (lane == 0) ph = pl = 0.0f;
+    add_pair(ph, pl, g0, 0.0f);  // the first token's own sum
+    const int i = 2 * lane;
+    G.hi[i] = ph, G.lo[i] = pl, G.hi[i + 1] = h, G.lo[i + 1] = l;
+    G.beta[i] = b0, G.beta[i + 1] = b1;
+    G.ec[i] = decay(ph, pl), G.ec[i + 1] = decay(h, l);
+    G.tail[i] = decay(lh - ph, ll - pl), G.tail[i + 1] = decay(lh - h, ll - l);
+    if (lane == 0) G.last = decay(lh, ll);
+}
+
+// ------------------------------------------------------------------ the chunk's triangular system
+
+// The products of a chunk that do not depend on the state, one 16 x 16 block (bi >= bj) per warp and turn:
+//   sE: -E below the diagonal blocks, and on the diagonal the inverses (I + E_bb b)^-1
+//       (kRowBeta: (I + b E_bb)^-1, the transposed system's), zeros above the diagonal;
+//   sP (kWithP): scale e^(c_i - c_j) q_i.k_j for j <= i, zeros above.
+// diag: 4 x 16 x 20 floats of scratch.  Ends with a barrier; the gates and tiles are ready before it.
+template <typename T, int DK, bool kRowBeta, bool kWithP, int NE, int NP, int NK>
+__device__ __forceinline__ void chunk_system(const Tile<T, DK, NK>& sK, const Tile<T, DK, NK>& sQ, const Tile<T, kChunk, NE>& sE,
+                                             const Tile<T, kChunk, NP>& sP, float* diag, const ChunkGates& G, float scale,
+                                             int warps) {
+    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    for (int task = w; task < 10; task += warps) {
+        // blocks in the order (0,0) (1,0) (1,1) (2,0) ...
+        const int bi = task >= 6 ? 3 : task >= 3 ? 2 : task >= 1 ? 1 : 0;
+        const int bj = task - bi * (bi + 1) / 2;
+        float kk[2][4] = {}, qk[2][4] = {};
+#pragma unroll
+        for (int d = 0; d < DK; d += 16) {
+            FragA<T, NK> ak, aq;
+            FragB<T, NK> b0, b1;
+            sK.b_nk(b0, b1, 16 * bj, d);
+            sK.a_mk(ak, 16 * bi, d);
+            mma16(kk[0], ak, b0);
+            mma16(kk[1], ak, b1);
+            if constexpr (kWithP) {
+                sQ.a_mk(aq, 16 * bi, d);
+                mma16(qk[0], aq, b0);
+                mma16(qk[1], aq, b1);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int i = 16 * bi + g + 8 * h, j = 16 * bj + 8 * n + 2 * t;
+                float e[2], p[2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    // (above the diagonal the difference may be positive without bound: not taken)
+                    const float d = j + x <= i ? decay(G.hi[i] - G.hi[j + x], G.lo[i] - G.lo[j + x]) : 0.0f;
+                    e[x] = j + x < i ? d * kk[n][2 * h + x] : 0.0f;
+                    p[x] = j + x <= i ? scale * d * qk[n][2 * h + x] : 0.0f;
+                }
+                if (bi == bj) {
+                    float* row = diag + (bi * 16 + g + 8 * h) * 20 + 8 * n + 2 * t;
+                    row[0] = e[0] * G.beta[kRowBeta ? i : j];
+                    row[1] = e[1] * G.beta[kRowBeta ? i : j + 1];
+                } else {
+                    sE.set2(i, j, -e[0], -e[1]);
+                }
+                if constexpr (kWithP) sP.set2(i, j, p[0], p[1]);
+            }
+    }
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        // column c of (I + L)^-1, L the strictly lower block: x_i = [i = c] - sum_{j < i} L_ij x_j
+        const int b = threadIdx.x >> 4, c = threadIdx.x & 15;
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float s = i == c ? 1.0f : 0.0f;
+            const float* row = diag + (b * 16 + i) * 20;
+#pragma unroll
+            for (int j = 0; j < i; ++j) s = fmaf(-row[j], x[j], s);
+            x[i] = s;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sE.set(16 * b + i, 16 * b + c, x[i]);
+    }
+    __syncthreads();
+}
+
+}  // namespace vmb

@@ -1,0 +1,148 @@
+// rotary.cu - rotary positions with several axes.
+//
+// Pair i of a head's first 2P channels is turned by the angle p f_i, p the token's position on the axis
+// that pair i belongs to:  (x, y) -> (x cos - y sin, y cos + x sin).  The gradient is the turn by the
+// opposite angle.  Bound by the bytes of q and k, read and written once: the sines of a token are
+// computed once into shared memory and serve all of its heads.
+//
+// The error of an angle does not grow with the position (the product p f alone is off by 2^-24 p f: 2e-4 at
+// position 4096): up to 1024 radians the product's rounding error, lo = p f - hi, is turned by to first order
+// (lo^2 / 2 < 2^-31); larger angles, which few pairs of few tokens have, are brought into [-pi, pi] in 64 bits.
+#include "mixer_internal.h"
+#include "vmb_common.cuh"
+#include "vmb_internal.h"
+
+namespace vmb {
+
+namespace {
+
+constexpr int kRotThreads = 256;
+
+template <typename T, int V> struct alignas(sizeof(T) * V) Pack { T v[V]; };
+
+// cos and sin of p f
+__device__ __forceinline__ float2 turn(int p, float f) {
+    const float ph = (float)p;
+    float hi = ph * f, lo = fmaf(ph, f, -hi);
+    if (!(fabsf(hi) <= 1024.0f)) {
+        const double a = (double)p * (double)f, n = rint(a * 0.15915494309189535);  // turns
+        hi = (float)fma(-n, 2.4492935982947064e-16, fma(-n, 6.283185307179586, a)), lo = 0.0f;  // 2 pi in two parts
+    }
+    float s, c;
+    sincosf(hi, &s, &c);
+    return make_float2(fmaf(-lo, s, c), fmaf(lo, c, s));
+}
+// one pair turned: (u cos - v sin, v cos + u sin), the same operations on every path
+__device__ __forceinline__ float2 turned(float u, float v, float2 w) {
+    return make_float2(fmaf(u, w.x, -__fmul_rn(v, w.y)), fmaf(v, w.x, __fmul_rn(u, w.y)));
+}
+
+// Items of a head: the vectors of V pairs (half: V channels from each half; interleaved: 2 V channels), then the
+// vectors of V channels that stay as they are.
+template <typename T, int V, bool kInter>
+__device__ __forceinline__ void rotate_heads(const T* src, T* dst, const float2* table, int tokens, long long src_t, int H, int D, int P) {
+    const int turns = P / V, items = turns + (D - 2 * P) / V, per = H * items, n = tokens * per;
+#pragma unroll 2
+    for (int i = threadIdx.x; i < n; i += kRotThreads) {
+        const int tok = i / per, rest = i - tok * per, h = rest / items, j = rest - h * items;
+        const T* s = src + tok * src_t + (long long)h * D;
+        T* d = dst + ((long long)tok * H + h) * D;
+        if (j >= turns) {
+            const int c = 2 * P + (j - turns) * V;
+            *reinterpret_cast<Pack<T, V>*>(d + c) = *reinterpret_cast<const Pack<T, V>*>(s + c);
+            continue;
+        }
+        const float2* cs = table + tok * P + j * V;
+        const int c0 = kInter ? 2 * j * V : j * V, c1 = kInter ? c0 + V : P + j * V;
+        const Pack<T, V> a = *reinterpret_cast<const Pack<T, V>*>(s + c0), b = *reinterpret_cast<const Pack<T, V>*>(s + c1);
+        Pack<T, V> oa, ob;
+#pragma unroll
+        for (int x = 0; x < V; ++x) {
+            const float2 w = cs[x];
+            if (kInter) {
+                const T xe = 2 * x < V ? a.v[(2 * x) % V] : b.v[(2 * x) % V], ye = 2 * x + 1 < V ? a.v[(2 * x + 1) % V] : b.v[(2 * x + 1) % V];
+                const float2 o = turned(io<T>::cvt(xe), io<T>::cvt(ye), w);
+                const T ru = io<T>::to(o.x), rv = io<T>::to(o.y);
+                if (2 * x < V) oa.v[(2 * x) % V] = ru; else ob.v[(2 * x) % V] = ru;
+                if (2 * x + 1 < V) oa.v[(2 * x + 1) % V] = rv; else ob.v[(2 * x + 1) % V] = rv;
+            } else {
+                const float2 o = turned(io<T>::cvt(a.v[x]), io<T>::cvt(b.v[x]), w);
+                oa.v[x] = io<T>::to(o.x);
+                ob.v[x] = io<T>::to(o.y);
+            }
+        }
+        *reinterpret_cast<Pack<T, V>*>(d + c0) = oa;
+        *reinterpret_cast<Pack<T, V>*>(d + c1) = ob;
+    }
+}
+
+template <typename T, int V, bool kInter>
+__global__ void __launch_bounds__(kRotThreads) rotary_kernel(RotaryArgs a, int per_block, int blocks_per_row) {
+    extern __shared__ float2 table[];
+    const int P = a.pair_end[a.axes - 1];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int b = blockIdx.x / blocks_per_row, t0 = (blockIdx.x % blocks_per_row) * per_block;
+    const int n = min(per_block, a.T - t0);
+    for (int i = threadIdx.x; i < n * P; i += kRotThreads) {
+        const int tok = t0 + i / P, j = i % P;
+        int axis = 0;
+        while (axis < a.axes - 1 && j >= a.pair_end[axis]) ++axis;
+        int p;
+        if (a.positions) {
+            p = a.positions[((long long)axis * a.B + b) * a.T + tok];
+        } else {
+            int rest = tok;
+            for (int x = a.axes - 1; x > axis; --x) rest /= a.grid[x];
+            p = rest % a.grid[axis];
+        }
+        const float2 cs = turn(p, a.freq[j]);
+        table[i] = make_float2(cs.x, a.inverse ? -cs.y : cs.y);
+    }
+    __syncthreads();
+    rotate_heads<T, V, kInter>((const T*)a.q + b * a.q_b + t0 * a.q_t, (T*)a.q_out + ((long long)b * a.T + t0) * a.Hq * a.D, table, n, a.q_t,
+                               a.Hq, a.D, P);
+    if (a.k)
+        rotate_heads<T, V, kInter>((const T*)a.k + b * a.k_b + t0 * a.k_t, (T*)a.k_out + ((long long)b * a.T + t0) * a.Hk * a.D, table, n,
+                                   a.k_t, a.Hk, a.D, P);
+}
+
+template <typename T, int V>
+vmb_status launch_v(const RotaryArgs& a, cudaStream_t stream) {
+    const int P = a.pair_end[a.axes - 1];
+    // tokens per block: about four vectors per thread, within 32 KB of sines, and enough blocks for every SM
+    const long long per_token = (long long)(a.Hq + a.Hk) * (P / V + (a.D - 2 * P) / V);
+    long long per = (4 * kRotThreads + per_token - 1) / per_token;
+    const long long most = 32 * 1024 / (8 * (long long)P), spread = ((long long)a.B * a.T + 2 * device_sm_count() - 1) / (2 * device_sm_count());
+    per = per < most ? per : most;
+    per = per < spread ? per : spread;
+    if (per < 1) per = 1;
+    if (per > a.T) per = a.T;
+    int per_block = (int)per, blocks = (int)((a.T + per - 1) / per);
+    if ((long long)blocks * a.B > 2147483647LL) return VMB_ERR_UNSUPPORTED;
+    const void* fn = a.interleaved ? (const void*)rotary_kernel<T, V, true> : (const void*)rotary_kernel<T, V, false>;
+    RotaryArgs arg = a;
+    void* args[] = {&arg, &per_block, &blocks};
+    return launch_kernel(fn, dim3((unsigned)(blocks * (long long)a.B)), dim3(kRotThreads), (size_t)per_block * P * 8, args, stream) == cudaSuccess
+               ? VMB_OK : VMB_ERR_CUDA;
+}
+
+}  // namespace
+
+// The widest vectors (up to 16 bytes) that divide the halves of the turned channels, the others, the rows and
+// the addresses.
+vmb_status launch_rotary(const RotaryArgs& a, cudaStream_t stream) {
+    const int P = a.pair_end[a.axes - 1];
+    const unsigned es = a.dtype == VMB_BF16 ? 2 : 4;
+    const unsigned long long bytes = (reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.q_out) | reinterpret_cast<uintptr_t>(a.k) |
+                                      reinterpret_cast<uintptr_t>(a.k_out)) |
+                                     (unsigned long long)es * ((unsigned long long)P | (unsigned)a.D | (unsigned long long)a.q_b |
+                                                              (unsigned long long)a.q_t | (unsigned long long)(a.k ? a.k_b | a.k_t : 0));
+    const unsigned v = (bytes % 16 == 0 ? 16 : bytes % 8 == 0 ? 8 : bytes % 4 == 0 ? 4 : 2) / es;
+    if (a.dtype == VMB_BF16)
+        return v == 8 ? launch_v<__nv_bfloat16, 8>(a, stream) : v == 4 ? launch_v<__nv_bfloat16, 4>(a, stream)
+             : v == 2 ? launch_v<__nv_bfloat16, 2>(a, stream) : launch_v<__nv_bfloat16, 1>(a, stream);
+    return v == 4 ? launch_v<float, 4>(a, stream) : v == 2 ? launch_v<float, 2>(a, stream) : launch_v<float, 1>(a, stream);
+}
+
+}  // namespace vmb

@@ -44,6 +44,9 @@ EXPORTS = ["vmb_cross_scan", "vmb_cross_merge", "vmb_scan_workspace_bytes", "vmb
            "vmb_scan_only_fwd", "vmb_selection_fwd", "vmb_selection_lowrank_fwd", "vmb_selective_scan_lowrank_fwd",
            "vmb_mean_scan_lowrank_fwd", "vmb_mean_scan_train_fwd", "vmb_mean_scan_bwd",
            "vmb_mean_scan_bwd_workspace_bytes",
+           "vmb_delta_rule_fwd", "vmb_delta_rule_bwd", "vmb_delta_rule_step", "vmb_delta_rule_workspace_bytes",
+           "vmb_delta_rule_saved_bytes", "vmb_rotary_fwd", "vmb_group_norm_fwd", "vmb_group_norm_bwd",
+           "vmb_group_norm_workspace_bytes",
            "vmb_read_status", "vmb_status_string", "vmb_version"]
 
 
@@ -81,6 +84,19 @@ def _load() -> ctypes.CDLL:
     lib.vmb_mean_scan_bwd.argtypes = [vp] * 16 + [i] * 7 + [u, i, vp, sz, vp]
     lib.vmb_mean_scan_bwd_workspace_bytes.argtypes = [i] * 8
     lib.vmb_mean_scan_bwd_workspace_bytes.restype = sz
+    f, i64 = ctypes.c_float, ctypes.c_int64
+    lib.vmb_delta_rule_fwd.argtypes = [vp] * 11 + [i, i, i64, i, i, i, i, f, i, vp, sz, vp]
+    lib.vmb_delta_rule_bwd.argtypes = [vp] * 15 + [i, i, i64, i, i, i, i, f, i, vp, sz, vp]
+    lib.vmb_delta_rule_step.argtypes = [vp] * 9 + [i] * 7 + [f, i, vp]
+    lib.vmb_delta_rule_workspace_bytes.argtypes = [i, i, i64, i, i, i, i, i, i, i]
+    lib.vmb_delta_rule_workspace_bytes.restype = sz
+    lib.vmb_delta_rule_saved_bytes.argtypes = [i, i, i64, i, i, i, i, i]
+    lib.vmb_delta_rule_saved_bytes.restype = sz
+    lib.vmb_rotary_fwd.argtypes = [vp] * 6 + [i] * 6 + [vp, vp, vp, u, i, vp]
+    lib.vmb_group_norm_fwd.argtypes = [vp] * 5 + [i, i64, i, i, f, i, i, vp, sz, vp]
+    lib.vmb_group_norm_bwd.argtypes = [vp] * 8 + [i, i64, i, i, i, i, vp, sz, vp]
+    lib.vmb_group_norm_workspace_bytes.argtypes = [i, i64, i, i, i, i]
+    lib.vmb_group_norm_workspace_bytes.restype = sz
     lib.vmb_read_status.argtypes = [vp, vp]
     lib.vmb_status_string.argtypes = [i]
     lib.vmb_status_string.restype = ctypes.c_char_p
@@ -90,6 +106,8 @@ def _load() -> ctypes.CDLL:
                  "vmb_discretise_fwd",
                  "vmb_discretise_mean_fwd", "vmb_scan_only_fwd", "vmb_selection_fwd", "vmb_mean_scan_bwd",
                  "vmb_selection_lowrank_fwd", "vmb_selective_scan_lowrank_fwd", "vmb_mean_scan_lowrank_fwd",
+                 "vmb_delta_rule_fwd", "vmb_delta_rule_bwd", "vmb_delta_rule_step", "vmb_rotary_fwd",
+                 "vmb_group_norm_fwd", "vmb_group_norm_bwd",
                  "vmb_read_status", "vmb_version"]:
         getattr(lib, name).restype = i
     return lib
@@ -674,6 +692,298 @@ def vmb_mean_scan_bwd(u, delta, A, Bs, Cs, Dskip, delta_bias, gy, H: int, W: int
                                  _ptr(out["Cs"]), _ptr(out["Dskip"]), _ptr(out["delta_bias"]), B, K, D, N, H, W,
                                  groups, flags, _dtype_code(u.dtype), _ptr(workspace), workspace.numel(),
                                  _stream(stream)), "vmb_mean_scan_bwd")
+    return out
+
+
+# ------------------------------------------- the channels-last token mixer
+
+VMB_ACT_NONE, VMB_ACT_SILU, VMB_ACT_GELU = 0, 1, 2
+VMB_ROTARY_INTERLEAVED, VMB_ROTARY_INVERSE = 0x1, 0x2
+
+_ACTS = {"none": VMB_ACT_NONE, "silu": VMB_ACT_SILU, "gelu": VMB_ACT_GELU}
+# workspaces of their own: the scans' must keep what the scans left in theirs
+_delta_ws = Workspace()
+_norm_ws = Workspace()
+
+
+def delta_workspace(device=None) -> torch.Tensor:
+    """The default workspace of the delta rule's calls (for vmb_read_status)."""
+    dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    return _delta_ws.get(256, dev)
+
+
+def _heads(t: torch.Tensor, name: str):
+    """(batch stride, token stride) of [B, T, H, D] whose heads and channels are dense."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dim() != 4:
+        raise ValueError(f"{name} must be [B, T, heads, channels]")
+    (B, T, H, D), (sb, st, sh, sd) = t.shape, t.stride()
+    if (sd != 1 and D > 1) or (sh != D and H > 1):
+        raise ValueError(f"{name}: the heads and channels of a token must be dense")
+    return (sb if B > 1 else 0), (st if T > 1 else H * D)
+
+
+def _delta_inputs(q, k, v, g, beta):
+    """Checked sizes (B, T, Hk, Hv, Dk, Dv), dtype code and strides (None: dense) of the delta rule's inputs."""
+    code = _dtype_code(q.dtype)
+    if k.dtype != q.dtype or v.dtype != q.dtype or g.dtype != q.dtype or beta.dtype != q.dtype:
+        raise ValueError("q, k, v, g, beta must share one dtype")
+    if q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and q.dim() == 4 and v.dim() == 4:
+        strides = None
+        _dev(q, "q"), _dev(k, "k"), _dev(v, "v")
+    else:
+        strides = (ctypes.c_int64 * 6)(*_heads(q, "q"), *_heads(k, "k"), *_heads(v, "v"))
+    B, T, Hk, Dk = q.shape
+    Hv, Dv = v.shape[2:]
+    if k.shape != q.shape or v.shape[0] != B or v.shape[1] != T:
+        raise ValueError("q, k [B, T, Hk, Dk] and v [B, T, Hv, Dv] expected")
+    if Hk < 1 or Hv % Hk:
+        raise ValueError("the value heads must be a multiple of the key heads")
+    if g.shape != (B, T, Hv) or beta.shape != (B, T, Hv):
+        raise ValueError("g and beta must be [B, T, Hv]")
+    _dev(g, "g"), _dev(beta, "beta")
+    return B, T, Hk, Hv, Dk, Dv, code, strides
+
+
+def _delta_packed(offsets, max_len, B, T):
+    """(sequences, longest, tokens) of dense [B, T] or packed [1, tokens] inputs."""
+    if offsets is None:
+        return B, T, B * T
+    _dev(offsets, "offsets")
+    if B != 1 or offsets.dim() != 1 or offsets.numel() < 1 or offsets.dtype != torch.int32:
+        raise ValueError("packed sequences: a batch dimension of 1 and int32 offsets [sequences + 1] expected")
+    if max_len is None or max_len < 0:
+        raise ValueError("packed sequences: max_len, a bound of the longest sequence, is needed")
+    return offsets.numel() - 1, min(int(max_len), T), T
+
+
+def _state(t, name, shape):
+    if t is not None:
+        _dev(t, name)
+        if t.shape != shape or t.dtype != torch.float32:
+            raise ValueError(f"{name} must be float32 {tuple(shape)}")
+    return t
+
+
+def vmb_delta_rule_workspace_bytes(B: int, T: int, total: int, packed: bool, Hk: int, Hv: int, Dk: int, Dv: int,
+                                   grads: bool = False, dtype: torch.dtype = torch.float32) -> int:
+    return int(lib.vmb_delta_rule_workspace_bytes(B, T, total, int(packed), Hk, Hv, Dk, Dv, int(grads), _dtype_code(dtype)))
+
+
+def vmb_delta_rule_saved_bytes(B: int, T: int, total: int, packed: bool, Hv: int, Dk: int, Dv: int,
+                               dtype: torch.dtype = torch.float32) -> int:
+    return int(lib.vmb_delta_rule_saved_bytes(B, T, total, int(packed), Hv, Dk, Dv, _dtype_code(dtype)))
+
+
+def vmb_delta_rule_fwd(q, k, v, g, beta, *, initial_state=None, offsets=None, max_len=None, scale=None,
+                       want_state: bool = False, want_saved: bool = False, o=None, final_state=None, saved=None,
+                       workspace=None, stream=None):
+    """Gated delta rule over the tokens of every head: q, k [B, T, Hk, Dk], v [B, T, Hv, Dv] (rows of tokens may be
+    strided), g (log decay), beta [B, T, Hv], initial_state [B, Hv, Dk, Dv] float32 or None; packed sequences with
+    `offsets` int32 [sequences + 1] and `max_len` (the batch dimension is then 1, states are per sequence).  `scale`
+    defaults to Dk ** -0.5.  Returns (o [B, T, Hv, Dv], final_state or None, saved or None); `saved` is what
+    vmb_delta_rule_bwd needs."""
+    B, T, Hk, Hv, Dk, Dv, code, strides = _delta_inputs(q, k, v, g, beta)
+    N, longest, total = _delta_packed(offsets, max_len, B, T)
+    shape = (N, Hv, Dk, Dv)
+    _state(initial_state, "initial_state", shape)
+    if final_state is None and want_state:
+        final_state = torch.empty(shape, dtype=torch.float32, device=q.device)
+    _state(final_state, "final_state", shape)
+    if o is None:
+        o = torch.empty((B, T, Hv, Dv), dtype=q.dtype, device=q.device)
+    else:
+        _dev(o, "o")
+        if o.shape != (B, T, Hv, Dv) or o.dtype != q.dtype:
+            raise ValueError("o must be [B, T, Hv, Dv] in the dtype of q")
+    if saved is None and want_saved:
+        n = lib.vmb_delta_rule_saved_bytes(N, longest, total, offsets is not None, Hv, Dk, Dv, code)
+        saved = torch.empty(n, dtype=torch.uint8, device=q.device)
+    elif saved is not None:
+        _saved_bytes(saved, N, longest, total, offsets, Hv, Dk, Dv, code)
+    if workspace is None:
+        n = lib.vmb_delta_rule_workspace_bytes(N, longest, total, offsets is not None, Hk, Hv, Dk, Dv, 0, code)
+        workspace = _delta_ws.get(n, q.device)
+    _check(lib.vmb_delta_rule_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), strides,
+                                  _ptr(initial_state), _ptr(offsets), o.data_ptr(), _ptr(final_state), _ptr(saved), N,
+                                  longest, total, Hk, Hv, Dk, Dv, Dk ** -0.5 if scale is None else scale, code,
+                                  workspace.data_ptr(), workspace.numel(), _stream(stream)), "vmb_delta_rule_fwd")
+    return o, final_state, saved
+
+
+def _saved_bytes(saved, N, longest, total, offsets, Hv, Dk, Dv, code):
+    _dev(saved, "saved")
+    n = lib.vmb_delta_rule_saved_bytes(N, longest, total, offsets is not None, Hv, Dk, Dv, code)
+    if saved.dtype != torch.uint8 or saved.numel() < n:
+        raise ValueError(f"saved must be uint8 with at least {n} bytes")
+
+
+def vmb_delta_rule_bwd(q, k, v, g, beta, do, saved, *, dfinal_state=None, offsets=None, max_len=None, scale=None,
+                       want_initial: bool = False, workspace=None, stream=None) -> dict:
+    """Gradients of vmb_delta_rule_fwd given do = dLoss/do [B, T, Hv, Dv] and, optionally, dfinal_state: returns
+    dict(q, k, v, g, beta[, initial_state]).  `saved`: the forward's, for the same inputs."""
+    B, T, Hk, Hv, Dk, Dv, code, strides = _delta_inputs(q, k, v, g, beta)
+    N, longest, total = _delta_packed(offsets, max_len, B, T)
+    shape = (N, Hv, Dk, Dv)
+    _state(dfinal_state, "dfinal_state", shape)
+    _dev(do, "do")
+    if do.shape != (B, T, Hv, Dv) or do.dtype != q.dtype:
+        raise ValueError("do must be [B, T, Hv, Dv] in the dtype of q")
+    _saved_bytes(saved, N, longest, total, offsets, Hv, Dk, Dv, code)
+    dev = q.device
+    out = dict(q=torch.empty(q.shape, dtype=q.dtype, device=dev), k=torch.empty(k.shape, dtype=q.dtype, device=dev),
+               v=torch.empty(v.shape, dtype=q.dtype, device=dev), g=torch.empty_like(g), beta=torch.empty_like(beta))
+    if want_initial:
+        out["initial_state"] = torch.empty(shape, dtype=torch.float32, device=dev)
+    if workspace is None:
+        n = lib.vmb_delta_rule_workspace_bytes(N, longest, total, offsets is not None, Hk, Hv, Dk, Dv, 1, code)
+        workspace = _delta_ws.get(n, dev)
+    _check(lib.vmb_delta_rule_bwd(q.data_ptr(), k.data_ptr(), g.data_ptr(), beta.data_ptr(), strides, _ptr(offsets),
+                                  do.data_ptr(), _ptr(dfinal_state), saved.data_ptr(), out["q"].data_ptr(),
+                                  out["k"].data_ptr(), out["v"].data_ptr(), out["g"].data_ptr(), out["beta"].data_ptr(),
+                                  _ptr(out.get("initial_state")), N, longest, total, Hk, Hv, Dk, Dv,
+                                  Dk ** -0.5 if scale is None else scale, code, workspace.data_ptr(), workspace.numel(),
+                                  _stream(stream)), "vmb_delta_rule_bwd")
+    return out
+
+
+def vmb_delta_rule_step(q, k, v, g, beta, state, *, slots=None, scale=None, o=None, stream=None) -> torch.Tensor:
+    """The recurrence for T tokens (one, or a few) of every row from its state, updated in place: q, k [B, T, Hk, Dk],
+    v [B, T, Hv, Dv], g, beta [B, T, Hv], state float32 [pool, Hv, Dk, Dv]; slots int32 [B] (row b uses state
+    slots[b]; a negative slot is padding, its o is zero) or None (row b uses state b).  Returns o [B, T, Hv, Dv]."""
+    B, T, Hk, Hv, Dk, Dv, code, strides = _delta_inputs(q, k, v, g, beta)
+    _dev(state, "state")
+    pool = state.shape[0]
+    if state.shape != (pool, Hv, Dk, Dv) or state.dtype != torch.float32:
+        raise ValueError("state must be float32 [pool, Hv, Dk, Dv]")
+    if slots is not None:
+        _dev(slots, "slots")
+        if slots.shape != (B,) or slots.dtype != torch.int32:
+            raise ValueError("slots must be int32 [B]")
+    if o is None:
+        o = torch.empty((B, T, Hv, Dv), dtype=q.dtype, device=q.device)
+    else:
+        _dev(o, "o")
+        if o.shape != (B, T, Hv, Dv) or o.dtype != q.dtype:
+            raise ValueError("o must be [B, T, Hv, Dv] in the dtype of q")
+    _check(lib.vmb_delta_rule_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), strides,
+                                   state.data_ptr(), _ptr(slots), o.data_ptr(), B, T, Hk, Hv, Dk, Dv, pool,
+                                   Dk ** -0.5 if scale is None else scale, code, _stream(stream)), "vmb_delta_rule_step")
+    return o
+
+
+def vmb_rotary_fwd(q, k, freq, positions=None, *, sections, grid=None, interleaved: bool = False,
+                   inverse: bool = False, q_out=None, k_out=None, stream=None):
+    """Rotary positions with len(sections) axes on q [B, T, Hq, D] and k [B, T, Hk, D] (or None; rows of tokens may be
+    strided): sections gives each axis' pairs of channels, freq float32 [sum(sections)] the angle per position of
+    every pair, positions int32 [axes, B, T] the tokens' places, or `grid` the sizes of the axes when the tokens lie
+    in that row-major grid.  inverse: the opposite angles (the gradient).  Returns (q_out, k_out or None)."""
+    code = _dtype_code(q.dtype)
+    dense = q.is_contiguous() and (k is None or k.is_contiguous())
+    if dense and q.dim() == 4:
+        strides = None
+        _dev(q, "q")
+    else:
+        strides = (ctypes.c_int64 * 4)(*_heads(q, "q"), *((0, 0) if k is None else _heads(k, "k")))
+    B, T, Hq, D = q.shape
+    Hk = 0
+    if k is not None:
+        if not k.is_cuda or k.dim() != 4 or k.dtype != q.dtype or k.shape[:2] != q.shape[:2] or k.shape[3] != D:
+            raise ValueError("k must be [B, T, Hk, D] with the dtype, B, T and D of q")
+        Hk = k.shape[2]
+    _dev(freq, "freq")
+    axes = len(sections)
+    if not 1 <= axes <= 4:
+        raise ValueError("one to four axes")
+    if freq.dtype != torch.float32 or freq.dim() != 1 or freq.shape[0] != sum(sections):
+        raise ValueError("freq must be float32 [sum(sections)]")
+    if positions is not None:
+        _dev(positions, "positions")
+        if positions.dtype != torch.int32 or positions.shape != (axes, B, T):
+            raise ValueError("positions must be int32 [axes, B, T]")
+        cells = None
+    else:
+        if grid is None or len(grid) != axes:
+            raise ValueError("positions, or a grid with one size for each axis, is needed")
+        cells = (ctypes.c_int * axes)(*grid)
+    if q_out is None:
+        q_out = torch.empty((B, T, Hq, D), dtype=q.dtype, device=q.device)
+    if k is not None and k_out is None:
+        k_out = torch.empty((B, T, Hk, D), dtype=q.dtype, device=q.device)
+    for out, n, h in ((q_out, "q_out", Hq), (k_out, "k_out", Hk)):
+        if out is not None:
+            _dev(out, n)
+            if out.shape != (B, T, h, D) or out.dtype != q.dtype:
+                raise ValueError(f"{n} must be [B, T, {h}, D] in the dtype of q")
+    flags = (VMB_ROTARY_INTERLEAVED if interleaved else 0) | (VMB_ROTARY_INVERSE if inverse else 0)
+    _check(lib.vmb_rotary_fwd(q.data_ptr(), _ptr(k), freq.data_ptr(), _ptr(positions), q_out.data_ptr(), _ptr(k_out), B,
+                              T, Hq, Hk, D, axes, (ctypes.c_int * axes)(*sections), cells, strides, flags, code,
+                              _stream(stream)), "vmb_rotary_fwd")
+    return q_out, k_out
+
+
+def vmb_group_norm_workspace_bytes(B: int, L: int, C: int, groups: int, grads: bool = False,
+                                   dtype: torch.dtype = torch.float32) -> int:
+    return int(lib.vmb_group_norm_workspace_bytes(B, L, C, groups, int(grads), _dtype_code(dtype)))
+
+
+def _norm_inputs(x, weight, bias, groups, act):
+    _dev(x, "x")
+    if x.dim() < 2:
+        raise ValueError("x must be [B, ..., C]")
+    B, C = x.shape[0], x.shape[-1]
+    if groups < 1 or C % groups:
+        raise ValueError("groups must be >= 1 and divide the channels")
+    for t, n in ((weight, "weight"), (bias, "bias")):
+        if t is not None:
+            _dev(t, n)
+            if t.shape != (C,) or t.dtype != torch.float32:
+                raise ValueError(f"{n} must be float32 [C]")
+    if act not in _ACTS:
+        raise ValueError(f"act must be one of {sorted(_ACTS)}")
+    L = x.numel() // (B * C) if B * C else 0
+    return B, L, C, _dtype_code(x.dtype), _ACTS[act]
+
+
+def vmb_group_norm_fwd(x, weight, bias, groups: int, *, eps: float = 1e-5, act: str = "none", want_stats: bool = False,
+                       y=None, stats=None, workspace=None, stream=None):
+    """Group norm with an activation ("none", "silu", "gelu"), channels last: x [B, ..., C], weight and bias float32
+    [C] or None.  Returns (y, stats [B, groups, 2] float32 (mean, 1 / sqrt(variance + eps)) or None)."""
+    B, L, C, code, a = _norm_inputs(x, weight, bias, groups, act)
+    if y is None:
+        y = torch.empty_like(x)
+    else:
+        _dev(y, "y")
+        if y.shape != x.shape or y.dtype != x.dtype:
+            raise ValueError("y must match x")
+    if stats is None and want_stats:
+        stats = torch.empty((B, groups, 2), dtype=torch.float32, device=x.device)
+    _state(stats, "stats", (B, groups, 2))
+    if workspace is None:
+        workspace = _norm_ws.get(lib.vmb_group_norm_workspace_bytes(B, L, C, groups, 0, code), x.device)
+    _check(lib.vmb_group_norm_fwd(x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(stats), B, L, C, groups, eps,
+                                  a, code, workspace.data_ptr(), workspace.numel(), _stream(stream)), "vmb_group_norm_fwd")
+    return y, stats
+
+
+def vmb_group_norm_bwd(x, weight, bias, stats, dy, groups: int, *, act: str = "none", workspace=None, stream=None) -> dict:
+    """Gradients of vmb_group_norm_fwd given dy and the forward's stats: dict(x, weight, bias), the latter two float32
+    [C] (None where the input was None)."""
+    B, L, C, code, a = _norm_inputs(x, weight, bias, groups, act)
+    _dev(dy, "dy")
+    if dy.shape != x.shape or dy.dtype != x.dtype:
+        raise ValueError("dy must match x")
+    if stats is None:
+        raise ValueError("the forward's stats are needed")
+    _state(stats, "stats", (B, groups, 2))
+    new = torch.empty_like if x.numel() else torch.zeros_like  # (an empty problem launches nothing: sums of nothing)
+    out = dict(x=torch.empty_like(x), weight=None if weight is None else new(weight), bias=None if bias is None else new(bias))
+    if workspace is None:
+        workspace = _norm_ws.get(lib.vmb_group_norm_workspace_bytes(B, L, C, groups, 1, code), x.device)
+    _check(lib.vmb_group_norm_bwd(x.data_ptr(), _ptr(weight), _ptr(bias), stats.data_ptr(), dy.data_ptr(),
+                                  out["x"].data_ptr(), _ptr(out["weight"]), _ptr(out["bias"]), B, L, C, groups, a, code,
+                                  workspace.data_ptr(), workspace.numel(), _stream(stream)), "vmb_group_norm_bwd")
     return out
 
 
