@@ -23,16 +23,25 @@ __device__ __forceinline__ const FragA<__nv_bfloat16, 1>& lead(const FragA<__nv_
 __device__ __forceinline__ const FragA<__nv_bfloat16, 1>& lead(const FragA<__nv_bfloat16, 1>& a) { return a; }
 __device__ __forceinline__ const FragA<float, 1>& lead(const FragA<float, 1>& a) { return a; }
 
-// Shared memory of the chain kernels, in bytes from the start.
+// Roles: warps 0 to 3 carry the state (240 registers), warps 4 to 11 load the tiles of the chunks ahead and compute
+// their triangular systems (128 registers; 128 x 240 + 256 x 128 is within the 384 x 168 of the launch).  Done one
+// after the other by four warps, loads and system took 8400 of a chunk's 14400 cycles (bf16, Dk = 64).
+constexpr int kChainThreads = 384, kStateThreads = 128, kSystemThreads = 256;
+constexpr int kBarSystem = 1, kBarFull = 2, kBarEmpty = 4;  // named barriers; full and empty: + parity of the chunk
+__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ void bar_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+// Shared memory of the chain kernels, in bytes from the start: a ring of tiles, two systems.
 template <typename T, int DK> struct ChainSmem {
     static constexpr int mid = DeltaTerms<T>::mid;
     using KT = Tile<T, DK, 1>;
     using VT = Tile<T, kDeltaRows, 1>;
-    using ET = Tile<T, kChunk, mid>;
-    using PT = Tile<T, kChunk, mid>;
+    using ET = LowTile<T, mid>;
+    static constexpr int ring = sizeof(T) == 4 && DK == 128 ? 2 : 3;
     static constexpr int k = 0, q = k + KT::bytes(kChunk), v = q + KT::bytes(kChunk), stage = v + VT::bytes(kChunk);
-    static constexpr int e = 2 * stage, p = e + ET::bytes(kChunk), diag = p + PT::bytes(kChunk),
-                         gates = diag + 64 * 20 * 4, total = gates + (int)sizeof(ChunkGates);
+    static constexpr int e = 0, p = e + ET::kBytes, gates = p + ET::kBytes, system = (gates + (int)sizeof(ChunkGates) + 127) & ~127;
+    static constexpr int systems = ring * stage, diag = systems + 2 * system, total = diag + 64 * 20 * 4;
+    static_assert(total <= 227 * 1024 && system % 16 == 0 && stage % 16 == 0, "fits");
 };
 
 // 16 x 64 (channel, token) accumulators of a warp to [token][channel] in global memory through the
@@ -121,83 +130,143 @@ __device__ __forceinline__ void load_gates(const T* g, const T* beta, int rows, 
     }
 }
 
+// The loads and systems of the chunks of a chain, first to last (step = 1) or last to first, by the system warps.
+// `tiles` loads a chunk's tiles into a stage; `gates` gives the two tokens' g and beta of a lane.
+template <typename T, int DK, bool kRowBeta, bool kWithP, typename Tiles, typename Gates>
+__device__ __forceinline__ void system_warps(unsigned char* smem, int chunks, float scale, Tiles tiles, Gates gates) {
+    using SM = ChainSmem<T, DK>;
+    const int tid = threadIdx.x - kStateThreads, w = tid >> 5;
+    float* diag = reinterpret_cast<float*>(smem + SM::diag);
+    float gv[4];
+    constexpr bool kAhead = SM::ring == 3;
+    if (kAhead && chunks > 0) {
+        tiles(0, smem, tid);
+        cp_async_commit();
+    }
+    if (w == 4 && chunks > 0) gates(0, gv);
+    for (int i = 0; i < chunks; ++i) {
+        // the states are done with chunk i - 2: its system, and with it the ring's oldest stage, is free
+        if (i >= 2) bar_sync(kBarEmpty + (i & 1), kChainThreads);
+        if (kAhead ? i + 1 < chunks : true) {
+            const int next = kAhead ? i + 1 : i;
+            tiles(next, smem + (next % SM::ring) * SM::stage, tid);
+            cp_async_commit();
+        }
+        unsigned char *st = smem + (i % SM::ring) * SM::stage, *sy = smem + SM::systems + (i & 1) * SM::system;
+        ChunkGates& G = *reinterpret_cast<ChunkGates*>(sy + SM::gates);
+        if (w == 4) {
+            chunk_gates(G, gv[0], gv[1], gv[2], gv[3]);
+            if (i + 1 < chunks) gates(i + 1, gv);
+        }
+        if (kAhead && i + 1 < chunks) cp_async_wait<1>(); else cp_async_wait<0>();
+        bar_sync(kBarSystem, kSystemThreads);
+        chunk_system<T, DK, kRowBeta, kWithP>(typename SM::KT(st + SM::k, kChunk), typename SM::KT(st + SM::q, kChunk),
+                                              typename SM::ET(sy + SM::e), typename SM::ET(sy + SM::p), diag, G, scale, w);
+        bar_arrive(kBarFull + (i & 1), kChainThreads);
+    }
+    // the last two releases, so that every barrier is left complete
+    for (int i = chunks < 2 ? 0 : chunks - 2; i < chunks; ++i) bar_sync(kBarEmpty + (i & 1), kChainThreads);
+}
+
+// x[channel][token] += S^T rows^T for the 64 rows of a tile (K or Q): the state's rows against every token
+template <int DK, int NS, typename T, typename TL>
+__device__ __forceinline__ void state_times(float (&x)[8][4], const FragA<T, NS>& f, const TL& s, int d) {
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        FragB<T, 1> b[4];
+        s.b_nk(b[0], b[1], 32 * n, 16 * d);
+        s.b_nk(b[2], b[3], 32 * n + 16, 16 * d);
+        mma_quad(*reinterpret_cast<float(*)[4][4]>(&x[4 * n]), f, b);
+    }
+}
+// S += f K_b: the outer products of 16 tokens (block b of a tile) with the state's columns
+template <int DK, int NS, typename T, typename TL>
+__device__ __forceinline__ void state_add(float (&S)[DK / 8][4], const FragA<T, NS>& f, const TL& s, int b) {
+#pragma unroll
+    for (int d = 0; d < DK / 32; ++d) {
+        FragB<T, 1> k[4];
+        s.b_kn(k[0], k[1], 16 * b, 32 * d);
+        s.b_kn(k[2], k[3], 16 * b, 32 * d + 16);
+        mma_quad(*reinterpret_cast<float(*)[4][4]>(&S[4 * d]), f, k);
+    }
+}
+
 // kOut = false: the maps and sums of a segment (DeltaChain::summary).
 template <typename T, int DK, bool kOut>
-__global__ void __launch_bounds__(kDeltaThreads) delta_forward_kernel(DeltaChain c) {
+__global__ void __launch_bounds__(kChainThreads, 1) delta_forward_kernel(DeltaChain c) {
     using SM = ChainSmem<T, DK>;
     constexpr int M = SM::mid;
     extern __shared__ __align__(128) unsigned char smem[];
     const DeltaArgs& a = c.a;
-    const int w = threadIdx.x >> 5, t = threadIdx.x & 3;
     pdl_launch_dependents();
     pdl_wait();
     const int vslices = c.slices, mslices = kOut ? 0 : (a.Dk + kDeltaRows - 1) / kDeltaRows;
-    ChainPlace at = chain_place(c, kOut ? vslices : (c.maps_only ? mslices : vslices + mslices));
+    const ChainPlace at = chain_place(c, kOut ? vslices : (c.maps_only ? mslices : vslices + mslices));
     const bool map = !kOut && (c.maps_only || at.slice >= vslices);  // rows of the map: v = 0, S = identity
     const int slice = map && !c.maps_only ? at.slice - vslices : at.slice;
     const DeltaSeq seq = delta_seq(a.offsets, at.b, a.T, a.total, c.err);
     const int nc = (seq.len + kChunk - 1) / kChunk;
     const int c0 = at.seg * c.seg_chunks, c1 = min(nc, c0 + c.seg_chunks);
-    const int row0 = slice * kDeltaRows + 16 * w, rows = map ? a.Dk : a.Dv;
+    if ((!kOut || c.segs > 1) && c0 >= nc) return;
+    const long long hrow = (long long)a.Hv * a.Dv;
+
+    if (threadIdx.x >= kStateThreads) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 128;");
+        const int hk = at.h / (a.Hv / a.Hk);
+        const long long brow = a.offsets ? 0 : at.b, tok0 = a.offsets ? seq.start : 0;
+        const T* kp = (const T*)a.k + brow * a.k_b + tok0 * a.k_t + (long long)hk * a.Dk;
+        const T* qp = (const T*)a.q + brow * a.q_b + tok0 * a.q_t + (long long)hk * a.Dk;
+        const T* vp = (const T*)a.v + brow * a.v_b + tok0 * a.v_t + (long long)at.h * a.Dv + slice * kDeltaRows;
+        const T* gp = (const T*)a.g + seq.start * a.Hv + at.h;
+        const T* bp = (const T*)a.beta + seq.start * a.Hv + at.h;
+        const bool kvec = rows_aligned(kp, a.k_t), qvec = rows_aligned(qp, a.q_t), vvec = rows_aligned(vp, a.v_t);
+        const int vcols = min(a.Dv - slice * kDeltaRows, kDeltaRows);
+        system_warps<T, DK, false, kOut>(
+            smem, c1 - c0, a.scale,
+            [&](int i, unsigned char* s, int tid) {
+                const int n = min(seq.len - (c0 + i) * kChunk, kChunk);
+                const long long t0 = (long long)(c0 + i) * kChunk;
+                load_tile<kChunk, DK>(typename SM::KT(s + SM::k, kChunk), kp + t0 * a.k_t, a.k_t, n, a.Dk, kvec, tid, kSystemThreads);
+                if (kOut)
+                    load_tile<kChunk, DK>(typename SM::KT(s + SM::q, kChunk), qp + t0 * a.q_t, a.q_t, n, a.Dk, qvec, tid, kSystemThreads);
+                if (!map)
+                    load_tile<kChunk, kDeltaRows>(typename SM::VT(s + SM::v, kChunk), vp + t0 * a.v_t, a.v_t, n, vcols, vvec, tid,
+                                                  kSystemThreads);
+            },
+            [&](int i, float(&v)[4]) {
+                const long long t0 = (long long)(c0 + i) * kChunk * a.Hv;
+                load_gates(gp + t0, bp + t0, min(seq.len - (c0 + i) * kChunk, kChunk), a.Hv, v);
+            });
+        return;
+    }
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 240;");
+    const int w = threadIdx.x >> 5, t = threadIdx.x & 3, g = (threadIdx.x & 31) >> 2;
+    const int row0 = slice * kDeltaRows + 16 * w;
+    T* op = kOut ? (T*)a.o + seq.start * hrow + (long long)at.h * a.Dv : nullptr;
+    T* rp = kOut && a.saved_r ? (T*)a.saved_r + seq.start * hrow + (long long)at.h * a.Dv : nullptr;
+    const bool ovec = kOut && rows_aligned(op, hrow), rvec = kOut && rows_aligned(rp, hrow);
 
     float S[DK / 8][4];
     if (kOut && c.segs > 1) {
-        if (c0 >= nc) return;
-        load_state_rows<DK>(S, c.sums + (at.chain * c.segs + at.seg) * a.Dv * a.Dk, row0, rows, a.Dk, a.Dk, 1);
+        load_state_rows<DK>(S, c.sums + (at.chain * c.segs + at.seg) * a.Dv * a.Dk, row0, a.Dv, a.Dk, a.Dk, 1);
     } else if (kOut && a.initial) {
-        load_state_rows<DK>(S, a.initial + at.chain * a.Dk * a.Dv, row0, rows, a.Dk, 1, a.Dv);
+        load_state_rows<DK>(S, a.initial + at.chain * a.Dk * a.Dv, row0, a.Dv, a.Dk, 1, a.Dv);
     } else {
-        const int g = (threadIdx.x & 31) >> 2;
 #pragma unroll
         for (int n = 0; n < DK / 8; ++n)
 #pragma unroll
             for (int x = 0; x < 4; ++x)
                 S[n][x] = map && row0 + g + 8 * (x >> 1) == 8 * n + 2 * t + (x & 1) ? 1.0f : 0.0f;
     }
-    if (!kOut && c0 >= nc) return;
 
-    const int hk = at.h / (a.Hv / a.Hk);
-    const long long brow = a.offsets ? 0 : at.b, tok0 = a.offsets ? seq.start : 0;
-    const T* kp = (const T*)a.k + brow * a.k_b + tok0 * a.k_t + (long long)hk * a.Dk;
-    const T* qp = (const T*)a.q + brow * a.q_b + tok0 * a.q_t + (long long)hk * a.Dk;
-    const T* vp = (const T*)a.v + brow * a.v_b + tok0 * a.v_t + (long long)at.h * a.Dv + slice * kDeltaRows;
-    const T* gp = (const T*)a.g + seq.start * a.Hv + at.h;
-    const T* bp = (const T*)a.beta + seq.start * a.Hv + at.h;
-    T* op = kOut ? (T*)a.o + (seq.start * a.Hv + at.h) * a.Dv : nullptr;
-    const bool kvec = rows_aligned(kp, a.k_t), qvec = rows_aligned(qp, a.q_t), vvec = rows_aligned(vp, a.v_t);
-    T* rp = kOut && a.saved_r ? (T*)a.saved_r + (seq.start * a.Hv + at.h) * a.Dv : nullptr;
-    const bool rvec = kOut && rows_aligned(rp, (long long)a.Hv * a.Dv);
-    const bool ovec = kOut && rows_aligned(op, (long long)a.Hv * a.Dv);
-    const int vcols = min(a.Dv - slice * kDeltaRows, kDeltaRows);
-
-    const typename SM::ET sE(smem + SM::e, kChunk);
-    const typename SM::PT sP(smem + SM::p, kChunk);
-    float* diag = reinterpret_cast<float*>(smem + SM::diag);
-    ChunkGates& G = *reinterpret_cast<ChunkGates*>(smem + SM::gates);
-    float gv[4];
-
-    auto load = [&](int ch) {
-        unsigned char* s = smem + (ch & 1) * SM::stage;
-        const long long t0 = (long long)ch * kChunk;
-        const int n = min(seq.len - ch * kChunk, kChunk);
-        load_tile<kChunk, DK>(typename SM::KT(s + SM::k, kChunk), kp + t0 * a.k_t, a.k_t, n, a.Dk, kvec, threadIdx.x, kDeltaThreads);
-        if (kOut)
-            load_tile<kChunk, DK>(typename SM::KT(s + SM::q, kChunk), qp + t0 * a.q_t, a.q_t, n, a.Dk, qvec, threadIdx.x, kDeltaThreads);
-        if (!map)
-            load_tile<kChunk, kDeltaRows>(typename SM::VT(s + SM::v, kChunk), vp + t0 * a.v_t, a.v_t, n, vcols, vvec, threadIdx.x, kDeltaThreads);
-        cp_async_commit();
-        if (w == 0) load_gates(gp + t0 * a.Hv, bp + t0 * a.Hv, n, a.Hv, gv);
-    };
-    if (c0 < c1) load(c0);
-    for (int ch = c0; ch < c1; ++ch) {
-        unsigned char* s = smem + (ch & 1) * SM::stage;
-        const typename SM::KT sK(s + SM::k, kChunk), sQ(s + SM::q, kChunk);
-        const typename SM::VT sV(s + SM::v, kChunk);
-        if (w == 0) chunk_gates(G, gv[0], gv[1], gv[2], gv[3]);
-        if (ch + 1 < c1) load(ch + 1);
-        if (ch + 1 < c1) cp_async_wait<1>(); else cp_async_wait<0>();
-        __syncthreads();
-        chunk_system<T, DK, false, kOut>(sK, sQ, sE, sP, diag, G, a.scale, kDeltaThreads / 32);
+    for (int i = 0; i < c1 - c0; ++i) {
+        const int ch = c0 + i;
+        unsigned char *st = smem + (i % SM::ring) * SM::stage, *sy = smem + SM::systems + (i & 1) * SM::system;
+        const typename SM::KT sK(st + SM::k, kChunk), sQ(st + SM::q, kChunk);
+        const typename SM::VT sV(st + SM::v, kChunk);
+        const typename SM::ET sE(sy + SM::e), sP(sy + SM::p);
+        const ChunkGates& G = *reinterpret_cast<const ChunkGates*>(sy + SM::gates);
+        bar_sync(kBarFull + (i & 1), kChainThreads);
         if (kOut && a.saved)
             store_state_rows<DK>(S, (T*)a.saved + ((long long)(seq.slot + ch) * a.Hv + at.h) * a.Dv * a.Dk, row0, a.Dv, a.Dk);
 
@@ -206,98 +275,85 @@ __global__ void __launch_bounds__(kDeltaThreads) delta_forward_kernel(DeltaChain
         for (int d = 0; d < DK / 16; ++d) {
             FragA<T, M> f;
             frag_from_acc(f, S[2 * d], S[2 * d + 1]);
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                FragB<T, 1> b0, b1;
-                sK.b_nk(b0, b1, 16 * n, 16 * d);
-                mma16(x[2 * n], f, b0);
-                mma16(x[2 * n + 1], f, b1);
-                if constexpr (kOut) {
-                    sQ.b_nk(b0, b1, 16 * n, 16 * d);
-                    mma16(y[2 * n], lead(f), b0);
-                    mma16(y[2 * n + 1], lead(f), b1);
-                }
-            }
+            state_times<DK>(x, f, sK, d);
+            if constexpr (kOut) state_times<DK>(y, lead(f), sQ, d);
         }
 #pragma unroll
         for (int n = 0; n < DK / 8; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) S[n][i] *= G.last;
+            for (int j = 0; j < 4; ++j) S[n][j] *= G.last;
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
             float v0[4] = {}, v1[4] = {};
             if (!map) sV.acc_km(v0, v1, 16 * w, 16 * n);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float e0 = G.ec[16 * n + 2 * t + (i & 1)], e1 = G.ec[16 * n + 8 + 2 * t + (i & 1)];
-                x[2 * n][i] = v0[i] - e0 * x[2 * n][i];
-                x[2 * n + 1][i] = v1[i] - e1 * x[2 * n + 1][i];
+            for (int j = 0; j < 4; ++j) {
+                const float e0 = G.ec[16 * n + 2 * t + (j & 1)], e1 = G.ec[16 * n + 8 + 2 * t + (j & 1)];
+                x[2 * n][j] = v0[j] - e0 * x[2 * n][j];
+                x[2 * n + 1][j] = v1[j] - e1 * x[2 * n + 1][j];
                 if constexpr (kOut) {
-                    y[2 * n][i] *= a.scale * e0;
-                    y[2 * n + 1][i] *= a.scale * e1;
+                    y[2 * n][j] *= a.scale * e0;
+                    y[2 * n + 1][j] *= a.scale * e1;
                 }
             }
         }
         FragA<T, M> uf[4];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            float r0[4] = {}, r1[4] = {};
+            float r0[4] = {}, r1[4] = {}, w0[4] = {}, w1[4] = {};
             FragB<T, M> e0, e1;
 #pragma unroll
             for (int j = 0; j < b; ++j) {
-                sE.b_nk(e0, e1, 16 * b, 16 * j);
-                mma16(x[2 * b], uf[j], e0);
-                mma16(x[2 * b + 1], uf[j], e1);
+                sE.b_nk(e0, e1, b, j);
+                mma_pair(x[2 * b], x[2 * b + 1], w0, w1, uf[j], e0, e1);
             }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[2 * b][j] += w0[j], x[2 * b + 1][j] += w1[j], w0[j] = w1[j] = 0.0f;
             FragA<T, M> f;
             frag_from_acc(f, x[2 * b], x[2 * b + 1]);
-            sE.b_nk(e0, e1, 16 * b, 16 * b);
-            mma16(r0, f, e0);
-            mma16(r1, f, e1);
+            sE.b_nk(e0, e1, b, b);
+            mma_pair(r0, r1, w0, w1, f, e0, e1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r0[j] += w0[j], r1[j] += w1[j];
             if constexpr (kOut) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[2 * b][i] = r0[i], x[2 * b + 1][i] = r1[i];
+                for (int j = 0; j < 4; ++j) x[2 * b][j] = r0[j], x[2 * b + 1][j] = r1[j];
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                r0[i] *= G.beta[16 * b + 2 * t + (i & 1)];
-                r1[i] *= G.beta[16 * b + 8 + 2 * t + (i & 1)];
+            for (int j = 0; j < 4; ++j) {
+                r0[j] *= G.beta[16 * b + 2 * t + (j & 1)];
+                r1[j] *= G.beta[16 * b + 8 + 2 * t + (j & 1)];
             }
             frag_from_acc(uf[b], r0, r1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                r0[i] *= G.tail[16 * b + 2 * t + (i & 1)];
-                r1[i] *= G.tail[16 * b + 8 + 2 * t + (i & 1)];
+            for (int j = 0; j < 4; ++j) {
+                r0[j] *= G.tail[16 * b + 2 * t + (j & 1)];
+                r1[j] *= G.tail[16 * b + 8 + 2 * t + (j & 1)];
             }
             frag_from_acc(f, r0, r1);
-#pragma unroll
-            for (int d = 0; d < DK / 16; ++d) {
-                FragB<T, 1> k0, k1;
-                sK.b_kn(k0, k1, 16 * b, 16 * d);
-                mma16(S[2 * d], f, k0);
-                mma16(S[2 * d + 1], f, k1);
-            }
+            state_add<DK>(S, f, sK, b);
             if constexpr (kOut) {
 #pragma unroll
                 for (int n = b; n < 4; ++n) {
                     FragB<T, M> p0, p1;
-                    sP.b_nk(p0, p1, 16 * n, 16 * b);
-                    mma16(y[2 * n], uf[b], p0);
-                    mma16(y[2 * n + 1], uf[b], p1);
+                    sP.b_nk(p0, p1, n, b);
+                    float z0[4] = {}, z1[4] = {};
+                    mma_pair(y[2 * n], y[2 * n + 1], z0, z1, uf[b], p0, p1);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) y[2 * n][j] += z0[j], y[2 * n + 1][j] += z1[j];
                 }
             }
         }
         if constexpr (kOut) {
-            const long long hrow = (long long)a.Hv * a.Dv, at0 = (long long)ch * kChunk * hrow;
+            const long long at0 = (long long)ch * kChunk * hrow;
             const int n = min(seq.len - ch * kChunk, kChunk);
             store_tokens<T>(sV, y, op + at0, hrow, n, slice * kDeltaRows, a.Dv, ovec);
             if (rp) store_tokens<T>(sV, x, rp + at0, hrow, n, slice * kDeltaRows, a.Dv, rvec);
         }
-        __syncthreads();  // the tiles of this chunk are rewritten two loads from here
+        bar_arrive(kBarEmpty + (i & 1), kChainThreads);
     }
     if constexpr (kOut) {
         if (a.final && c.segs == 1) {
-            const int g = (threadIdx.x & 31) >> 2;
             float* dst = a.final + at.chain * a.Dk * a.Dv;
 #pragma unroll
             for (int n = 0; n < DK / 8; ++n)
@@ -321,22 +377,56 @@ __global__ void __launch_bounds__(kDeltaThreads) delta_forward_kernel(DeltaChain
 //   dS <- e^(c_last) dS + (scale e^c Q)^T do - (e^c K)^T dR.
 // Writes dS at each chunk's end, dX and dv = dR of every token; with DeltaChain::summary only the segment's sum.
 template <typename T, int DK>
-__global__ void __launch_bounds__(kDeltaThreads) delta_reverse_kernel(DeltaChain c) {
+__global__ void __launch_bounds__(kChainThreads, 1) delta_reverse_kernel(DeltaChain c) {
     using SM = ChainSmem<T, DK>;
     constexpr int M = SM::mid;
     extern __shared__ __align__(128) unsigned char smem[];
     const DeltaArgs& a = c.a;
-    const int w = threadIdx.x >> 5, t = threadIdx.x & 3, g = (threadIdx.x & 31) >> 2;
     pdl_launch_dependents();
     pdl_wait();
     const ChainPlace at = chain_place(c, c.slices);
     const DeltaSeq seq = delta_seq(a.offsets, at.b, a.T, a.total, c.err);
     const int nc = (seq.len + kChunk - 1) / kChunk;
     const int c0 = at.seg * c.seg_chunks, c1 = min(nc, c0 + c.seg_chunks);
+    if (c.segs > 1 && c0 >= nc) return;
+    const long long hrow = (long long)a.Hv * a.Dv;  // do, dX and dv are dense
+
+    if (threadIdx.x >= kStateThreads) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 128;");
+        const int hk = at.h / (a.Hv / a.Hk);
+        const long long brow = a.offsets ? 0 : at.b, tok0 = a.offsets ? seq.start : 0;
+        const T* kp = (const T*)a.k + brow * a.k_b + tok0 * a.k_t + (long long)hk * a.Dk;
+        const T* qp = (const T*)a.q + brow * a.q_b + tok0 * a.q_t + (long long)hk * a.Dk;
+        const T* dp = (const T*)a.dout + seq.start * hrow + (long long)at.h * a.Dv + at.slice * kDeltaRows;
+        const T* gp = (const T*)a.g + seq.start * a.Hv + at.h;
+        const T* bp = (const T*)a.beta + seq.start * a.Hv + at.h;
+        const bool kvec = rows_aligned(kp, a.k_t), qvec = rows_aligned(qp, a.q_t), dvec = rows_aligned(dp, hrow);
+        const int vcols = min(a.Dv - at.slice * kDeltaRows, kDeltaRows);
+        system_warps<T, DK, true, true>(
+            smem, c1 - c0, a.scale,
+            [&](int i, unsigned char* s, int tid) {
+                const int ch = c1 - 1 - i, n = min(seq.len - ch * kChunk, kChunk);
+                const long long t0 = (long long)ch * kChunk;
+                load_tile<kChunk, DK>(typename SM::KT(s + SM::k, kChunk), kp + t0 * a.k_t, a.k_t, n, a.Dk, kvec, tid, kSystemThreads);
+                load_tile<kChunk, DK>(typename SM::KT(s + SM::q, kChunk), qp + t0 * a.q_t, a.q_t, n, a.Dk, qvec, tid, kSystemThreads);
+                load_tile<kChunk, kDeltaRows>(typename SM::VT(s + SM::v, kChunk), dp + t0 * hrow, hrow, n, vcols, dvec, tid,
+                                              kSystemThreads);
+            },
+            [&](int i, float(&v)[4]) {
+                const int ch = c1 - 1 - i;
+                const long long t0 = (long long)ch * kChunk * a.Hv;
+                load_gates(gp + t0, bp + t0, min(seq.len - ch * kChunk, kChunk), a.Hv, v);
+            });
+        return;
+    }
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 240;");
+    const int w = threadIdx.x >> 5, t = threadIdx.x & 3, g = (threadIdx.x & 31) >> 2;
     const int row0 = at.slice * kDeltaRows + 16 * w;
+    T* xp = (T*)c.dx + seq.start * hrow + (long long)at.h * a.Dv;
+    T* rp = (T*)a.dv + seq.start * hrow + (long long)at.h * a.Dv;
+    const bool xvec = rows_aligned(xp, hrow), rvec = rows_aligned(rp, hrow);
 
     float S[DK / 8][4];
-    if (c.segs > 1 && c0 >= nc) return;
     if (!c.summary && c.segs > 1) {
         load_state_rows<DK>(S, c.sums + (at.chain * c.segs + at.seg) * a.Dv * a.Dk, row0, a.Dv, a.Dk, a.Dk, 1);
     } else if (!c.summary && a.dfinal) {
@@ -348,46 +438,14 @@ __global__ void __launch_bounds__(kDeltaThreads) delta_reverse_kernel(DeltaChain
             for (int x = 0; x < 4; ++x) S[n][x] = 0.0f;
     }
 
-    const int hk = at.h / (a.Hv / a.Hk);
-    const long long brow = a.offsets ? 0 : at.b, tok0 = a.offsets ? seq.start : 0;
-    const T* kp = (const T*)a.k + brow * a.k_b + tok0 * a.k_t + (long long)hk * a.Dk;
-    const T* qp = (const T*)a.q + brow * a.q_b + tok0 * a.q_t + (long long)hk * a.Dk;
-    const long long hrow = (long long)a.Hv * a.Dv;  // do and dX are dense
-    const T* dp = (const T*)a.dout + seq.start * hrow + (long long)at.h * a.Dv + at.slice * kDeltaRows;
-    T* xp = (T*)c.dx + seq.start * hrow + (long long)at.h * a.Dv;
-    const T* gp = (const T*)a.g + seq.start * a.Hv + at.h;
-    const T* bp = (const T*)a.beta + seq.start * a.Hv + at.h;
-    const bool kvec = rows_aligned(kp, a.k_t), qvec = rows_aligned(qp, a.q_t), dvec = rows_aligned(dp, hrow);
-    T* rp = (T*)a.dv + seq.start * hrow + (long long)at.h * a.Dv;
-    const bool xvec = rows_aligned(xp, hrow), rvec = rows_aligned(rp, hrow);
-    const int vcols = min(a.Dv - at.slice * kDeltaRows, kDeltaRows);
-
-    const typename SM::ET sE(smem + SM::e, kChunk);
-    const typename SM::PT sP(smem + SM::p, kChunk);
-    float* diag = reinterpret_cast<float*>(smem + SM::diag);
-    ChunkGates& G = *reinterpret_cast<ChunkGates*>(smem + SM::gates);
-    float gv[4];
-
-    auto load = [&](int ch) {
-        unsigned char* s = smem + (ch & 1) * SM::stage;
-        const long long t0 = (long long)ch * kChunk;
-        const int n = min(seq.len - ch * kChunk, kChunk);
-        load_tile<kChunk, DK>(typename SM::KT(s + SM::k, kChunk), kp + t0 * a.k_t, a.k_t, n, a.Dk, kvec, threadIdx.x, kDeltaThreads);
-        load_tile<kChunk, DK>(typename SM::KT(s + SM::q, kChunk), qp + t0 * a.q_t, a.q_t, n, a.Dk, qvec, threadIdx.x, kDeltaThreads);
-        load_tile<kChunk, kDeltaRows>(typename SM::VT(s + SM::v, kChunk), dp + t0 * hrow, hrow, n, vcols, dvec, threadIdx.x, kDeltaThreads);
-        cp_async_commit();
-        if (w == 0) load_gates(gp + t0 * a.Hv, bp + t0 * a.Hv, n, a.Hv, gv);
-    };
-    if (c0 < c1) load(c1 - 1);
-    for (int ch = c1 - 1; ch >= c0; --ch) {
-        unsigned char* s = smem + (ch & 1) * SM::stage;
-        const typename SM::KT sK(s + SM::k, kChunk), sQ(s + SM::q, kChunk);
-        const typename SM::VT sD(s + SM::v, kChunk);
-        if (w == 0) chunk_gates(G, gv[0], gv[1], gv[2], gv[3]);
-        if (ch > c0) load(ch - 1);
-        if (ch > c0) cp_async_wait<1>(); else cp_async_wait<0>();
-        __syncthreads();
-        chunk_system<T, DK, true, true>(sK, sQ, sE, sP, diag, G, a.scale, kDeltaThreads / 32);
+    for (int i = 0; i < c1 - c0; ++i) {
+        const int ch = c1 - 1 - i;
+        unsigned char *st = smem + (i % SM::ring) * SM::stage, *sy = smem + SM::systems + (i & 1) * SM::system;
+        const typename SM::KT sK(st + SM::k, kChunk), sQ(st + SM::q, kChunk);
+        const typename SM::VT sD(st + SM::v, kChunk);
+        const typename SM::ET sE(sy + SM::e), sP(sy + SM::p);
+        const ChunkGates& G = *reinterpret_cast<const ChunkGates*>(sy + SM::gates);
+        bar_sync(kBarFull + (i & 1), kChainThreads);
         if (!c.summary)
             store_state_rows<DK>(S, (T*)c.ds + ((long long)(seq.slot + ch) * a.Hv + at.h) * a.Dv * a.Dk, row0, a.Dv, a.Dk);
 
@@ -396,22 +454,16 @@ __global__ void __launch_bounds__(kDeltaThreads) delta_reverse_kernel(DeltaChain
         for (int d = 0; d < DK / 16; ++d) {
             FragA<T, M> f;
             frag_from_acc(f, S[2 * d], S[2 * d + 1]);
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                FragB<T, 1> b0, b1;
-                sK.b_nk(b0, b1, 16 * n, 16 * d);
-                mma16(x[2 * n], f, b0);
-                mma16(x[2 * n + 1], f, b1);
-            }
+            state_times<DK>(x, f, sK, d);
         }
 #pragma unroll
         for (int n = 0; n < DK / 8; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) S[n][i] *= G.last;
+            for (int j = 0; j < 4; ++j) S[n][j] *= G.last;
 #pragma unroll
         for (int n = 0; n < 8; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[n][i] *= G.tail[8 * n + 2 * t + (i & 1)];
+            for (int j = 0; j < 4; ++j) x[n][j] *= G.tail[8 * n + 2 * t + (j & 1)];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {  // token block b of do: P^T do into dU, (scale e^c Q)^T do into dS
             FragA<T, 1> f;
@@ -419,75 +471,66 @@ __global__ void __launch_bounds__(kDeltaThreads) delta_reverse_kernel(DeltaChain
 #pragma unroll
             for (int n = 0; n <= b; ++n) {
                 FragB<T, M> p0, p1;
-                sP.b_kn(p0, p1, 16 * b, 16 * n);
-                mma16(x[2 * n], f, p0);
-                mma16(x[2 * n + 1], f, p1);
+                sP.b_kn(p0, p1, b, n);
+                float z0[4] = {}, z1[4] = {};
+                mma_pair(x[2 * n], x[2 * n + 1], z0, z1, f, p0, p1);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[2 * n][j] += z0[j], x[2 * n + 1][j] += z1[j];
             }
             float d0[4], d1[4];
             sD.acc_km(d0, d1, 16 * w, 16 * b);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                d0[i] *= a.scale * G.ec[16 * b + 2 * t + (i & 1)];
-                d1[i] *= a.scale * G.ec[16 * b + 8 + 2 * t + (i & 1)];
+            for (int j = 0; j < 4; ++j) {
+                d0[j] *= a.scale * G.ec[16 * b + 2 * t + (j & 1)];
+                d1[j] *= a.scale * G.ec[16 * b + 8 + 2 * t + (j & 1)];
             }
             FragA<T, M> fs;
             frag_from_acc(fs, d0, d1);
-#pragma unroll
-            for (int d = 0; d < DK / 16; ++d) {
-                FragB<T, 1> q0, q1;
-                sQ.b_kn(q0, q1, 16 * b, 16 * d);
-                mma16(S[2 * d], fs, q0);
-                mma16(S[2 * d + 1], fs, q1);
-            }
+            state_add<DK>(S, fs, sQ, b);
         }
         FragA<T, M> rf[4];
 #pragma unroll
         for (int b = 3; b >= 0; --b) {
+            float r0[4] = {}, r1[4] = {}, w0[4] = {}, w1[4] = {};
             FragB<T, M> e0, e1;
 #pragma unroll
             for (int j = 3; j > b; --j) {
-                sE.b_kn(e0, e1, 16 * j, 16 * b);
-                mma16(x[2 * b], rf[j], e0);
-                mma16(x[2 * b + 1], rf[j], e1);
+                sE.b_kn(e0, e1, j, b);
+                mma_pair(x[2 * b], x[2 * b + 1], w0, w1, rf[j], e0, e1);
             }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[2 * b][j] += w0[j], x[2 * b + 1][j] += w1[j], w0[j] = w1[j] = 0.0f;
             FragA<T, M> f;
             frag_from_acc(f, x[2 * b], x[2 * b + 1]);
-            float r0[4] = {}, r1[4] = {};
-            sE.b_kn(e0, e1, 16 * b, 16 * b);
-            mma16(r0, f, e0);
-            mma16(r1, f, e1);
+            sE.b_kn(e0, e1, b, b);
+            mma_pair(r0, r1, w0, w1, f, e0, e1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[2 * b][i] = r0[i];
-                x[2 * b + 1][i] = r1[i];
-                r0[i] *= G.beta[16 * b + 2 * t + (i & 1)];
-                r1[i] *= G.beta[16 * b + 8 + 2 * t + (i & 1)];
+            for (int j = 0; j < 4; ++j) {
+                r0[j] += w0[j], r1[j] += w1[j];
+                x[2 * b][j] = r0[j];
+                x[2 * b + 1][j] = r1[j];
+                r0[j] *= G.beta[16 * b + 2 * t + (j & 1)];
+                r1[j] *= G.beta[16 * b + 8 + 2 * t + (j & 1)];
             }
             frag_from_acc(rf[b], r0, r1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                r0[i] *= -G.ec[16 * b + 2 * t + (i & 1)];
-                r1[i] *= -G.ec[16 * b + 8 + 2 * t + (i & 1)];
+            for (int j = 0; j < 4; ++j) {
+                r0[j] *= -G.ec[16 * b + 2 * t + (j & 1)];
+                r1[j] *= -G.ec[16 * b + 8 + 2 * t + (j & 1)];
             }
             frag_from_acc(f, r0, r1);
-#pragma unroll
-            for (int d = 0; d < DK / 16; ++d) {
-                FragB<T, 1> k0, k1;
-                sK.b_kn(k0, k1, 16 * b, 16 * d);
-                mma16(S[2 * d], f, k0);
-                mma16(S[2 * d + 1], f, k1);
-            }
+            state_add<DK>(S, f, sK, b);
         }
         if (!c.summary) {
             const int n = min(seq.len - ch * kChunk, kChunk);
             store_tokens<T>(sD, x, xp + (long long)ch * kChunk * hrow, hrow, n, at.slice * kDeltaRows, a.Dv, xvec);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int m = 0; m < 8; ++m)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[i][j] *= G.beta[8 * i + 2 * t + (j & 1)];
+                for (int j = 0; j < 4; ++j) x[m][j] *= G.beta[8 * m + 2 * t + (j & 1)];
             store_tokens<T>(sD, x, rp + (long long)ch * kChunk * hrow, hrow, n, at.slice * kDeltaRows, a.Dv, rvec);
         }
-        __syncthreads();
+        bar_arrive(kBarEmpty + (i & 1), kChainThreads);
     }
     if (c.summary) {
         store_state_rows<DK>(S, c.sums + (at.chain * c.segs + at.seg) * a.Dv * a.Dk, row0, a.Dv, a.Dk);
@@ -514,7 +557,7 @@ vmb_status launch_chain_dk(const DeltaChain& c, bool reverse, cudaStream_t strea
     if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return VMB_ERR_CUDA;
     DeltaChain arg = c;
     void* args[] = {&arg};
-    return launch_kernel(fn, dim3((unsigned)grid), dim3(kDeltaThreads), smem, args, stream) == cudaSuccess ? VMB_OK : VMB_ERR_CUDA;
+    return launch_kernel(fn, dim3((unsigned)grid), dim3(kChainThreads), smem, args, stream) == cudaSuccess ? VMB_OK : VMB_ERR_CUDA;
 }
 
 template <typename T>

@@ -29,7 +29,6 @@
 namespace vmb {
 
 constexpr int kChunk = 64;       // tokens per chunk
-constexpr int kDeltaThreads = 128;
 constexpr int kDeltaRows = 64;   // value channels (state rows) per CTA: 16 per warp
 
 // ------------------------------------------------------------------ fragments
@@ -54,14 +53,10 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 __device__ __forceinline__ float bf16_lo(uint32_t p) { return __uint_as_float(p << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t p) { return __uint_as_float(p & 0xffff0000u); }
-__device__ __forceinline__ uint32_t to_tf32(float x) {
-    uint32_t r;
-    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
-    return r;
-}
+// x = hi + lo up to 2^-21 |x|, both tf32 (19 leading bits): by masks, at the full rate of the integer pipe
 __device__ __forceinline__ void split_tf32(float x, uint32_t& hi, uint32_t& lo) {
-    hi = to_tf32(x);
-    lo = to_tf32(x - __uint_as_float(hi));
+    hi = __float_as_uint(x) & 0xffffe000u;
+    lo = __float_as_uint(x - __uint_as_float(hi)) & 0xffffe000u;
 }
 
 // Operands of a 16-deep step.  bf16: NT terms.  fp32: two 8-deep tf32 steps s; position k of step
@@ -74,26 +69,75 @@ template <int NT> struct FragB<__nv_bfloat16, NT> { uint32_t r[NT][2]; };
 template <int NT> struct FragA<float, NT> { uint32_t hi[2][4], lo[2][4]; };
 template <int NT> struct FragB<float, NT> { uint32_t hi[2][2], lo[2][2]; };
 
-// c += a b, the small products first; the product of two second terms is left out
+// c += a b for four neighbouring tiles of 8 columns.  A product waits for the one before it on the same
+// accumulator (21 cycles, against 8 per product when the pipe is full): the terms go round the tiles.  bf16: the
+// product of two second terms is left out.  fp32: the small products are summed on their own, because every
+// product added to a large accumulator on the tensor cores truncates it (2 times instead of 6).
 template <int NA, int NB>
-__device__ __forceinline__ void mma16(float (&c)[4], const FragA<__nv_bfloat16, NA>& a, const FragB<__nv_bfloat16, NB>& b) {
-    if constexpr (NA > 1) mma_bf16(c, a.r[1], b.r[0]);
-    if constexpr (NB > 1) mma_bf16(c, a.r[0], b.r[1]);
-    mma_bf16(c, a.r[0], b.r[0]);
-}
-// (fp32: the small products are summed on their own, because every product that is added to a large
-// accumulator on the tensor cores truncates it: 2 times instead of 6)
-template <int NA, int NB>
-__device__ __forceinline__ void mma16(float (&c)[4], const FragA<float, NA>& a, const FragB<float, NB>& b) {
-    float d[4] = {};
+__device__ __forceinline__ void mma_quad(float (&c)[4][4], const FragA<__nv_bfloat16, NA>& a, const FragB<__nv_bfloat16, NB> (&b)[4]) {
+    if constexpr (NA > 1) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        mma_tf32(d, a.lo[s], b.hi[s]);
-        mma_tf32(d, a.hi[s], b.lo[s]);
-        mma_tf32(c, a.hi[s], b.hi[s]);
+        for (int i = 0; i < 4; ++i) mma_bf16(c[i], a.r[1], b[i].r[0]);
+    }
+    if constexpr (NB > 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mma_bf16(c[i], a.r[0], b[i].r[1]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] += d[i];
+    for (int i = 0; i < 4; ++i) mma_bf16(c[i], a.r[0], b[i].r[0]);
+}
+template <int NA, int NB>
+__device__ __forceinline__ void mma_quad(float (&c)[4][4], const FragA<float, NA>& a, const FragB<float, NB> (&b)[4]) {
+    float d[4][4] = {};
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mma_tf32(d[i], a.lo[s], b[i].hi[s]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mma_tf32(c[i], a.hi[s], b[i].hi[s]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mma_tf32(d[i], a.hi[s], b[i].lo[s]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) c[i][x] += d[i][x];
+}
+// Two tiles, the small products in an accumulator of their own (w), so that a chain of such products is half as long.
+template <int NA, int NB>
+__device__ __forceinline__ void mma_pair(float (&c0)[4], float (&c1)[4], float (&w0)[4], float (&w1)[4], const FragA<__nv_bfloat16, NA>& a,
+                                         const FragB<__nv_bfloat16, NB>& b0, const FragB<__nv_bfloat16, NB>& b1) {
+    if constexpr (NA > 1) mma_bf16(w0, a.r[1], b0.r[0]), mma_bf16(w1, a.r[1], b1.r[0]);
+    mma_bf16(c0, a.r[0], b0.r[0]), mma_bf16(c1, a.r[0], b1.r[0]);
+    if constexpr (NB > 1) mma_bf16(w0, a.r[0], b0.r[1]), mma_bf16(w1, a.r[0], b1.r[1]);
+}
+template <int NA, int NB>
+__device__ __forceinline__ void mma_pair(float (&c0)[4], float (&c1)[4], float (&w0)[4], float (&w1)[4], const FragA<float, NA>& a,
+                                         const FragB<float, NB>& b0, const FragB<float, NB>& b1) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        mma_tf32(w0, a.lo[s], b0.hi[s]), mma_tf32(w1, a.lo[s], b1.hi[s]);
+        mma_tf32(c0, a.hi[s], b0.hi[s]), mma_tf32(c1, a.hi[s], b1.hi[s]);
+        mma_tf32(w0, a.hi[s], b0.lo[s]), mma_tf32(w1, a.hi[s], b1.lo[s]);
+    }
+}
+// c += a b for one tile
+template <typename T, int NA, int NB> __device__ __forceinline__ void mma16(float (&c)[4], const FragA<T, NA>& a, const FragB<T, NB>& b) {
+    float w[4] = {};
+    if constexpr (sizeof(T) == 2) {
+        if constexpr (NA > 1) mma_bf16(c, a.r[1], b.r[0]);
+        if constexpr (NB > 1) mma_bf16(c, a.r[0], b.r[1]);
+        mma_bf16(c, a.r[0], b.r[0]);
+    } else {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            mma_tf32(w, a.lo[s], b.hi[s]);
+            mma_tf32(c, a.hi[s], b.hi[s]);
+            mma_tf32(w, a.hi[s], b.lo[s]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] += w[i];
+    }
 }
 
 // A from two neighbouring accumulator tiles (16 columns)
@@ -293,6 +337,88 @@ template <int COLS, int NT> struct Tile<float, COLS, NT> {
     }
 };
 
+// The ten 16 x 16 blocks on and below the diagonal of a 64 x 64 matrix, block (i, j) at i (i + 1) / 2 + j.
+// bf16: rows of 48 bytes (eight rows of an ldmatrix on different banks); fp32: the halves of rows 2, 3, 6, 7, ...
+// swapped, which leaves the pair loads along rows free of conflicts.
+template <typename T, int NT> struct LowTile;
+template <int NT> struct LowTile<__nv_bfloat16, NT> {
+    using T = __nv_bfloat16;
+    static constexpr int kLd = 24, kBlock = 16 * kLd, kBytes = NT * 10 * kBlock * 2;
+    T* p;
+    __device__ __forceinline__ explicit LowTile(void* s) : p((T*)s) {}
+    __device__ __forceinline__ static int base(int bi, int bj) { return (bi * (bi + 1) / 2 + bj) * NT * kBlock; }
+    __device__ __forceinline__ void set(int bi, int bj, int r, int c, float v) const {
+        T* q = p + base(bi, bj) + r * kLd + c;
+        const T h = __float2bfloat16_rn(v);
+        q[0] = h;
+        if constexpr (NT > 1) q[kBlock] = __float2bfloat16_rn(v - __bfloat162float(h));
+    }
+    __device__ __forceinline__ void set2(int bi, int bj, int r, int c, float v0, float v1) const {
+        T* q = p + base(bi, bj) + r * kLd + c;
+        const uint32_t h = pack_bf16(v0, v1);
+        *reinterpret_cast<uint32_t*>(q) = h;
+        if constexpr (NT > 1) *reinterpret_cast<uint32_t*>(q + kBlock) = pack_bf16(v0 - bf16_lo(h), v1 - bf16_hi(h));
+    }
+    __device__ __forceinline__ uint32_t lane_addr(int term, int bi, int bj) const {
+        const int lane = threadIdx.x & 31;
+        return smem_u32(p + base(bi, bj) + term * kBlock + (lane & 15) * kLd + (lane >> 4) * 8);
+    }
+    // B[k][n] = block[n][k]
+    __device__ __forceinline__ void b_nk(FragB<T, NT>& b0, FragB<T, NT>& b1, int bi, int bj) const {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            uint32_t r[4];
+            ldmatrix4(r, lane_addr(i, bi, bj));
+            b0.r[i][0] = r[0], b0.r[i][1] = r[2], b1.r[i][0] = r[1], b1.r[i][1] = r[3];
+        }
+    }
+    // B[k][n] = block[k][n]
+    __device__ __forceinline__ void b_kn(FragB<T, NT>& b0, FragB<T, NT>& b1, int bi, int bj) const {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            uint32_t r[4];
+            ldmatrix4_t(r, lane_addr(i, bi, bj));
+            b0.r[i][0] = r[0], b0.r[i][1] = r[1], b1.r[i][0] = r[2], b1.r[i][1] = r[3];
+        }
+    }
+};
+template <int NT> struct LowTile<float, NT> {
+    using T = float;
+    static constexpr int kBlock = 256, kBytes = 10 * kBlock * 4;
+    T* p;
+    __device__ __forceinline__ explicit LowTile(void* s) : p((T*)s) {}
+    __device__ __forceinline__ static int at(int bi, int bj, int r, int c) {
+        return (bi * (bi + 1) / 2 + bj) * kBlock + r * 16 + (c ^ ((r & 2) << 2));
+    }
+    __device__ __forceinline__ void set(int bi, int bj, int r, int c, float v) const { p[at(bi, bj, r, c)] = v; }
+    __device__ __forceinline__ void set2(int bi, int bj, int r, int c, float v0, float v1) const {
+        *reinterpret_cast<float2*>(p + at(bi, bj, r, c)) = make_float2(v0, v1);
+    }
+    __device__ __forceinline__ void b_nk(FragB<T, NT>& b0, FragB<T, NT>& b1, int bi, int bj) const {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const float2 u = *reinterpret_cast<const float2*>(p + at(bi, bj, g, 8 * s + 2 * t));
+            const float2 w = *reinterpret_cast<const float2*>(p + at(bi, bj, g + 8, 8 * s + 2 * t));
+            split_tf32(u.x, b0.hi[s][0], b0.lo[s][0]);
+            split_tf32(u.y, b0.hi[s][1], b0.lo[s][1]);
+            split_tf32(w.x, b1.hi[s][0], b1.lo[s][0]);
+            split_tf32(w.y, b1.hi[s][1], b1.lo[s][1]);
+        }
+    }
+    __device__ __forceinline__ void b_kn(FragB<T, NT>& b0, FragB<T, NT>& b1, int bi, int bj) const {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int k = 8 * s + 2 * t;
+            split_tf32(p[at(bi, bj, k, g)], b0.hi[s][0], b0.lo[s][0]);
+            split_tf32(p[at(bi, bj, k + 1, g)], b0.hi[s][1], b0.lo[s][1]);
+            split_tf32(p[at(bi, bj, k, 8 + g)], b1.hi[s][0], b1.lo[s][0]);
+            split_tf32(p[at(bi, bj, k + 1, 8 + g)], b1.hi[s][1], b1.lo[s][1]);
+        }
+    }
+};
+
 // ------------------------------------------------------------------ global <-> shared
 
 // A head's tile of `rows` x `cols` values at src (row stride in elements) into a tile of ROWS x COLS,
@@ -392,20 +518,21 @@ __device__ __forceinline__ void chunk_gates(ChunkGates& G, float g0, float g1, f
 
 // ------------------------------------------------------------------ the chunk's triangular system
 
-// The products of a chunk that do not depend on the state, one 16 x 16 block (bi >= bj) per warp and turn:
+// The products of a chunk that do not depend on the state, by eight warps (w = 0 .. 7):
 //   sE: -E below the diagonal blocks, and on the diagonal the inverses (I + E_bb b)^-1
-//       (kRowBeta: (I + b E_bb)^-1, the transposed system's), zeros above the diagonal;
+//       (kRowBeta: (I + b E_bb)^-1, the transposed system's);
 //   sP (kWithP): scale e^(c_i - c_j) q_i.k_j for j <= i, zeros above.
-// diag: 4 x 16 x 20 floats of scratch.  Ends with a barrier; the gates and tiles are ready before it.
-template <typename T, int DK, bool kRowBeta, bool kWithP, int NE, int NP, int NK>
-__device__ __forceinline__ void chunk_system(const Tile<T, DK, NK>& sK, const Tile<T, DK, NK>& sQ, const Tile<T, kChunk, NE>& sE,
-                                             const Tile<T, kChunk, NP>& sP, float* diag, const ChunkGates& G, float scale,
-                                             int warps) {
-    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    for (int task = w; task < 10; task += warps) {
-        // blocks in the order (0,0) (1,0) (1,1) (2,0) ...
-        const int bi = task >= 6 ? 3 : task >= 3 ? 2 : task >= 1 ? 1 : 0;
-        const int bj = task - bi * (bi + 1) / 2;
+// Warps 0 to 3 compute one diagonal block each and invert it, warps 4 to 7 the six blocks below the diagonal.
+// diag: 4 x 16 x 20 floats of scratch.  The gates and tiles are ready before the call; no barrier inside.
+template <typename T, int DK, bool kRowBeta, bool kWithP, int NE, int NK>
+__device__ __forceinline__ void chunk_system(const Tile<T, DK, NK>& sK, const Tile<T, DK, NK>& sQ, const LowTile<T, NE>& sE,
+                                             const LowTile<T, NE>& sP, float* diag, const ChunkGates& G, float scale, int w) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    for (int task = w; task < 10; task += task < 4 ? 10 : 4) {
+        const bool on = task < 4;
+        // (0,0) (1,1) (2,2) (3,3), then (3,0) (3,1) (3,2) (2,0) (2,1) (1,0)
+        const int bi = on ? task : task < 7 ? 3 : task < 9 ? 2 : 1;
+        const int bj = on ? task : task < 7 ? task - 4 : task < 9 ? task - 7 : 0;
         float kk[2][4] = {}, qk[2][4] = {};
 #pragma unroll
         for (int d = 0; d < DK; d += 16) {
@@ -421,46 +548,63 @@ __device__ __forceinline__ void chunk_system(const Tile<T, DK, NK>& sK, const Ti
                 mma16(qk[1], aq, b1);
             }
         }
+        float jh[4], jl[4], jb[4];
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int x = 0; x < 4; ++x) {
+            const int j = 16 * bj + 8 * (x >> 1) + 2 * t + (x & 1);
+            jh[x] = G.hi[j], jl[x] = G.lo[j], jb[x] = G.beta[j];
+        }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int i = 16 * bi + g + 8 * h, j = 16 * bj + 8 * n + 2 * t;
+        for (int h = 0; h < 2; ++h) {
+            const int r = g + 8 * h, i = 16 * bi + r;
+            const float ih = G.hi[i], il = G.lo[i], ib = G.beta[i];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
                 float e[2], p[2];
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
+                    const int j = 16 * bj + 8 * n + 2 * t + x;
                     // (above the diagonal the difference may be positive without bound: not taken)
-                    const float d = j + x <= i ? decay(G.hi[i] - G.hi[j + x], G.lo[i] - G.lo[j + x]) : 0.0f;
-                    e[x] = j + x < i ? d * kk[n][2 * h + x] : 0.0f;
-                    p[x] = j + x <= i ? scale * d * qk[n][2 * h + x] : 0.0f;
+                    const float d = j <= i ? decay(ih - jh[2 * n + x], il - jl[2 * n + x]) : 0.0f;
+                    e[x] = j < i ? d * kk[n][2 * h + x] : 0.0f;
+                    p[x] = j <= i ? scale * d * qk[n][2 * h + x] : 0.0f;
                 }
-                if (bi == bj) {
-                    float* row = diag + (bi * 16 + g + 8 * h) * 20 + 8 * n + 2 * t;
-                    row[0] = e[0] * G.beta[kRowBeta ? i : j];
-                    row[1] = e[1] * G.beta[kRowBeta ? i : j + 1];
+                if constexpr (kWithP) sP.set2(bi, bj, r, 8 * n + 2 * t, p[0], p[1]);
+                if (on) {  // transposed: the columns of the block side by side
+                    float* col = diag + (bi * 16 + 8 * n + 2 * t) * 20 + r;
+                    col[0] = e[0] * (kRowBeta ? ib : jb[2 * n]);
+                    col[20] = e[1] * (kRowBeta ? ib : jb[2 * n + 1]);
                 } else {
-                    sE.set2(i, j, -e[0], -e[1]);
+                    sE.set2(bi, bj, r, 8 * n + 2 * t, -e[0], -e[1]);
                 }
-                if constexpr (kWithP) sP.set2(i, j, p[0], p[1]);
             }
-    }
-    __syncthreads();
-    if (threadIdx.x < 64) {
-        // column c of (I + L)^-1, L the strictly lower block: x_i = [i = c] - sum_{j < i} L_ij x_j
-        const int b = threadIdx.x >> 4, c = threadIdx.x & 15;
-        float x[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float s = i == c ? 1.0f : 0.0f;
-            const float* row = diag + (b * 16 + i) * 20;
-#pragma unroll
-            for (int j = 0; j < i; ++j) s = fmaf(-row[j], x[j], s);
-            x[i] = s;
         }
+        if (on) {
+            __syncwarp();
+            // column c of (I + L)^-1, L the strictly lower block: x_i = [i = c] - sum_{j < i} L_ij x_j, taken off column
+            // by column of L so that the chain is 15 products long
+            const int c = lane & 15;
+            float x[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sE.set(16 * b + i, 16 * b + c, x[i]);
+            for (int i = 0; i < 16; ++i) x[i] = i == c ? 1.0f : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 15; ++j) {
+                const float* col = diag + (bi * 16 + j) * 20;
+#pragma unroll
+                for (int i4 = (j + 1) / 4; i4 < 4; ++i4) {
+                    const float4 l = *reinterpret_cast<const float4*>(col + 4 * i4);
+                    if (4 * i4 > j) x[4 * i4] = fmaf(-l.x, x[j], x[4 * i4]);
+                    if (4 * i4 + 1 > j) x[4 * i4 + 1] = fmaf(-l.y, x[j], x[4 * i4 + 1]);
+                    if (4 * i4 + 2 > j) x[4 * i4 + 2] = fmaf(-l.z, x[j], x[4 * i4 + 2]);
+                    if (4 * i4 + 3 > j) x[4 * i4 + 3] = fmaf(-l.w, x[j], x[4 * i4 + 3]);
+                }
+            }
+            if (lane < 16) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sE.set(bi, bi, i, c, x[i]);
+            }
+        }
     }
-    __syncthreads();
 }
 
 }  // namespace vmb
