@@ -39,8 +39,9 @@ template <typename T, int DK> struct ChainSmem {
     using ET = LowTile<T, mid>;
     static constexpr int ring = sizeof(T) == 4 && DK == 128 ? 2 : 3;
     static constexpr int k = 0, q = k + KT::bytes(kChunk), v = q + KT::bytes(kChunk), stage = v + VT::bytes(kChunk);
-    static constexpr int e = 0, p = e + ET::kBytes, gates = p + ET::kBytes, system = (gates + (int)sizeof(ChunkGates) + 127) & ~127;
-    static constexpr int systems = ring * stage, diag = systems + 2 * system, total = diag + 64 * 20 * 4;
+    static constexpr int e = 0, p = e + ET::kBytes, system = p + ET::kBytes;
+    static constexpr int gate = (sizeof(ChunkGates) + 15) & ~15;  // three of them: a chunk's are computed ahead
+    static constexpr int systems = ring * stage, diag = systems + 2 * system, gates = diag + 64 * 20 * 4, total = gates + 3 * gate;
     static_assert(total <= 227 * 1024 && system % 16 == 0 && stage % 16 == 0, "fits");
 };
 
@@ -49,13 +50,11 @@ template <typename T, int DK> struct ChainSmem {
 template <typename T>
 __device__ __forceinline__ void store_tokens(const Tile<T, kDeltaRows, 1>& s, const float (&y)[8][4], T* dst, long long stride,
                                              int rows, int ch0, int channels, bool vec) {
-    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
     constexpr int V = Tile<T, kDeltaRows, 1>::kVec, P = 16 / V;
     __syncwarp();
 #pragma unroll
-    for (int n = 0; n < 8; ++n)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) s.set(8 * n + 2 * t + (x & 1), 16 * w + g + 8 * (x >> 1), y[n][x]);
+    for (int n = 0; n < 4; ++n) s.set_t(16 * n, 16 * w, y[2 * n], y[2 * n + 1]);
     __syncwarp();
     if (vec && ch0 + 16 * w + 16 <= channels) {
 #pragma unroll
@@ -135,17 +134,23 @@ __device__ __forceinline__ void load_gates(const T* g, const T* beta, int rows, 
 template <typename T, int DK, bool kRowBeta, bool kWithP, typename Tiles, typename Gates>
 __device__ __forceinline__ void system_warps(unsigned char* smem, int chunks, float scale, Tiles tiles, Gates gates) {
     using SM = ChainSmem<T, DK>;
+    constexpr int kGateWarp = 7;  // has one block of the system, others up to two or an inverse
     const int tid = threadIdx.x - kStateThreads, w = tid >> 5;
     float* diag = reinterpret_cast<float*>(smem + SM::diag);
+    auto gate = [&](int i) -> ChunkGates& { return *reinterpret_cast<ChunkGates*>(smem + SM::gates + (i % 3) * SM::gate); };
     float gv[4];
     constexpr bool kAhead = SM::ring == 3;
     if (kAhead && chunks > 0) {
         tiles(0, smem, tid);
         cp_async_commit();
     }
-    if (w == 4 && chunks > 0) gates(0, gv);
+    if (w == kGateWarp && chunks > 0) {
+        gates(0, gv);
+        chunk_gates(gate(0), gv[0], gv[1], gv[2], gv[3]);
+        if (chunks > 1) gates(1, gv);
+    }
     for (int i = 0; i < chunks; ++i) {
-        // the states are done with chunk i - 2: its system, and with it the ring's oldest stage, is free
+        // the states are done with chunk i - 2: its system, and with it the oldest stage and gates, are free
         if (i >= 2) bar_sync(kBarEmpty + (i & 1), kChainThreads);
         if (kAhead ? i + 1 < chunks : true) {
             const int next = kAhead ? i + 1 : i;
@@ -153,30 +158,43 @@ __device__ __forceinline__ void system_warps(unsigned char* smem, int chunks, fl
             cp_async_commit();
         }
         unsigned char *st = smem + (i % SM::ring) * SM::stage, *sy = smem + SM::systems + (i & 1) * SM::system;
-        ChunkGates& G = *reinterpret_cast<ChunkGates*>(sy + SM::gates);
-        if (w == 4) {
-            chunk_gates(G, gv[0], gv[1], gv[2], gv[3]);
-            if (i + 1 < chunks) gates(i + 1, gv);
-        }
         if (kAhead && i + 1 < chunks) cp_async_wait<1>(); else cp_async_wait<0>();
         bar_sync(kBarSystem, kSystemThreads);
         chunk_system<T, DK, kRowBeta, kWithP>(typename SM::KT(st + SM::k, kChunk), typename SM::KT(st + SM::q, kChunk),
-                                              typename SM::ET(sy + SM::e), typename SM::ET(sy + SM::p), diag, G, scale, w);
+                                              typename SM::ET(sy + SM::e), typename SM::ET(sy + SM::p), diag, gate(i), scale, w);
+        if (w == kGateWarp && i + 1 < chunks) {
+            chunk_gates(gate(i + 1), gv[0], gv[1], gv[2], gv[3]);
+            if (i + 2 < chunks) gates(i + 2, gv);
+        }
         bar_arrive(kBarFull + (i & 1), kChainThreads);
     }
     // the last two releases, so that every barrier is left complete
     for (int i = chunks < 2 ? 0 : chunks - 2; i < chunks; ++i) bar_sync(kBarEmpty + (i & 1), kChainThreads);
 }
 
-// x[channel][token] += S^T rows^T for the 64 rows of a tile (K or Q): the state's rows against every token
-template <int DK, int NS, typename T, typename TL>
-__device__ __forceinline__ void state_times(float (&x)[8][4], const FragA<T, NS>& f, const TL& s, int d) {
+// x[channel][token] += S^T K^T and, with kTwo, y += S^T Q^T (leading terms of S), the rows of the state against every
+// token; the operands of the next four tiles are read before the products of these.
+template <int DK, bool kTwo, int NS, typename T, typename TL>
+__device__ __forceinline__ void state_times(const float (&S)[DK / 8][4], float (&x)[8][4], float (*y)[4], const TL& sK, const TL& sQ) {
+    constexpr int kSteps = DK / 16 * (kTwo ? 4 : 2);
+    FragB<T, 1> b[2][4];
+    auto read = [&](int i, FragB<T, 1>(&f)[4]) {
+        const int d = kTwo ? i >> 2 : i >> 1, n = 32 * (kTwo ? (i >> 1) & 1 : i & 1);
+        const TL& s = kTwo && (i & 1) ? sQ : sK;
+        s.b_nk(f[0], f[1], n, 16 * d);
+        s.b_nk(f[2], f[3], n + 16, 16 * d);
+    };
+    read(0, b[0]);
+    FragA<T, NS> f;
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-        FragB<T, 1> b[4];
-        s.b_nk(b[0], b[1], 32 * n, 16 * d);
-        s.b_nk(b[2], b[3], 32 * n + 16, 16 * d);
-        mma_quad(*reinterpret_cast<float(*)[4][4]>(&x[4 * n]), f, b);
+    for (int i = 0; i < kSteps; ++i) {
+        if (i + 1 < kSteps) read(i + 1, b[(i + 1) & 1]);
+        const int d = kTwo ? i >> 2 : i >> 1, n = 4 * (kTwo ? (i >> 1) & 1 : i & 1);
+        if (kTwo ? i % 4 == 0 : i % 2 == 0) frag_from_acc(f, S[2 * d], S[2 * d + 1]);
+        if (kTwo && (i & 1))
+            mma_quad(*reinterpret_cast<float(*)[4][4]>(&y[n]), lead(f), b[i & 1]);
+        else
+            mma_quad(*reinterpret_cast<float(*)[4][4]>(&x[n]), f, b[i & 1]);
     }
 }
 // S += f K_b: the outer products of 16 tokens (block b of a tile) with the state's columns
@@ -219,19 +237,16 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_forward_kernel(DeltaCh
         const T* vp = (const T*)a.v + brow * a.v_b + tok0 * a.v_t + (long long)at.h * a.Dv + slice * kDeltaRows;
         const T* gp = (const T*)a.g + seq.start * a.Hv + at.h;
         const T* bp = (const T*)a.beta + seq.start * a.Hv + at.h;
-        const bool kvec = rows_aligned(kp, a.k_t), qvec = rows_aligned(qp, a.q_t), vvec = rows_aligned(vp, a.v_t);
-        const int vcols = min(a.Dv - slice * kDeltaRows, kDeltaRows);
+        const int ptid = threadIdx.x - kStateThreads;
+        const TileCopy<typename SM::KT, DK, kSystemThreads> ck(kp, a.k_t, a.Dk, ptid), cq(qp, a.q_t, a.Dk, ptid);
+        const TileCopy<typename SM::VT, kDeltaRows, kSystemThreads> cv(vp, a.v_t, min(a.Dv - slice * kDeltaRows, kDeltaRows), ptid);
         system_warps<T, DK, false, kOut>(
             smem, c1 - c0, a.scale,
             [&](int i, unsigned char* s, int tid) {
-                const int n = min(seq.len - (c0 + i) * kChunk, kChunk);
-                const long long t0 = (long long)(c0 + i) * kChunk;
-                load_tile<kChunk, DK>(typename SM::KT(s + SM::k, kChunk), kp + t0 * a.k_t, a.k_t, n, a.Dk, kvec, tid, kSystemThreads);
-                if (kOut)
-                    load_tile<kChunk, DK>(typename SM::KT(s + SM::q, kChunk), qp + t0 * a.q_t, a.q_t, n, a.Dk, qvec, tid, kSystemThreads);
-                if (!map)
-                    load_tile<kChunk, kDeltaRows>(typename SM::VT(s + SM::v, kChunk), vp + t0 * a.v_t, a.v_t, n, vcols, vvec, tid,
-                                                  kSystemThreads);
+                const int first = (c0 + i) * kChunk, n = min(seq.len - first, kChunk);
+                ck.copy(s + SM::k, first, n, tid);
+                if (kOut) cq.copy(s + SM::q, first, n, tid);
+                if (!map) cv.copy(s + SM::v, first, n, tid);
             },
             [&](int i, float(&v)[4]) {
                 const long long t0 = (long long)(c0 + i) * kChunk * a.Hv;
@@ -265,19 +280,13 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_forward_kernel(DeltaCh
         const typename SM::KT sK(st + SM::k, kChunk), sQ(st + SM::q, kChunk);
         const typename SM::VT sV(st + SM::v, kChunk);
         const typename SM::ET sE(sy + SM::e), sP(sy + SM::p);
-        const ChunkGates& G = *reinterpret_cast<const ChunkGates*>(sy + SM::gates);
+        const ChunkGates& G = *reinterpret_cast<const ChunkGates*>(smem + SM::gates + (i % 3) * SM::gate);
         bar_sync(kBarFull + (i & 1), kChainThreads);
         if (kOut && a.saved)
             store_state_rows<DK>(S, (T*)a.saved + ((long long)(seq.slot + ch) * a.Hv + at.h) * a.Dv * a.Dk, row0, a.Dv, a.Dk);
 
         float x[8][4] = {}, y[kOut ? 8 : 1][4] = {};  // K S and Q S, transposed: [channel][token]
-#pragma unroll
-        for (int d = 0; d < DK / 16; ++d) {
-            FragA<T, M> f;
-            frag_from_acc(f, S[2 * d], S[2 * d + 1]);
-            state_times<DK>(x, f, sK, d);
-            if constexpr (kOut) state_times<DK>(y, lead(f), sQ, d);
-        }
+        state_times<DK, kOut, M, T>(S, x, y, sK, sQ);
 #pragma unroll
         for (int n = 0; n < DK / 8; ++n)
 #pragma unroll
@@ -297,34 +306,36 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_forward_kernel(DeltaCh
                 }
             }
         }
-        FragA<T, M> uf[4];
+        // Block by block: while the products of block b with the state's columns and with P run, the next block's
+        // residuals are corrected by the blocks before it and multiplied by its inverse.
+        FragA<T, M> uf[4], f;
+        float r0[4] = {}, r1[4] = {}, w0[4] = {}, w1[4] = {};
+        {
+            FragB<T, M> e0, e1;
+            sE.b_nk(e0, e1, 0, 0);
+            frag_from_acc(f, x[0], x[1]);
+            mma_pair(r0, r1, w0, w1, f, e0, e1);
+        }
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            float r0[4] = {}, r1[4] = {}, w0[4] = {}, w1[4] = {};
-            FragB<T, M> e0, e1;
-#pragma unroll
-            for (int j = 0; j < b; ++j) {
-                sE.b_nk(e0, e1, b, j);
-                mma_pair(x[2 * b], x[2 * b + 1], w0, w1, uf[j], e0, e1);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[2 * b][j] += w0[j], x[2 * b + 1][j] += w1[j], w0[j] = w1[j] = 0.0f;
-            FragA<T, M> f;
-            frag_from_acc(f, x[2 * b], x[2 * b + 1]);
-            sE.b_nk(e0, e1, b, b);
-            mma_pair(r0, r1, w0, w1, f, e0, e1);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) r0[j] += w0[j], r1[j] += w1[j];
-            if constexpr (kOut) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[2 * b][j] = r0[j], x[2 * b + 1][j] = r1[j];
-            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
+                r0[j] += w0[j], r1[j] += w1[j];
+                if constexpr (kOut) x[2 * b][j] = r0[j], x[2 * b + 1][j] = r1[j];
                 r0[j] *= G.beta[16 * b + 2 * t + (j & 1)];
                 r1[j] *= G.beta[16 * b + 8 + 2 * t + (j & 1)];
+                w0[j] = w1[j] = 0.0f;
             }
             frag_from_acc(uf[b], r0, r1);
+            FragB<T, M> e0, e1;
+            if (b < 3) {
+#pragma unroll
+                for (int j = 0; j <= b; ++j) {
+                    sE.b_nk(e0, e1, b + 1, j);
+                    mma_pair(x[(2 * b + 2) & 7], x[(2 * b + 3) & 7], w0, w1, uf[j], e0, e1);
+                }
+                sE.b_nk(e0, e1, b + 1, b + 1);
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 r0[j] *= G.tail[16 * b + 2 * t + (j & 1)];
@@ -332,15 +343,30 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_forward_kernel(DeltaCh
             }
             frag_from_acc(f, r0, r1);
             state_add<DK>(S, f, sK, b);
+            if (b < 3) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[(2 * b + 2) & 7][j] += w0[j], x[(2 * b + 3) & 7][j] += w1[j];
+                    r0[j] = r1[j] = w0[j] = w1[j] = 0.0f;
+                }
+                frag_from_acc(f, x[(2 * b + 2) & 7], x[(2 * b + 3) & 7]);
+                mma_pair(r0, r1, w0, w1, f, e0, e1);
+            }
             if constexpr (kOut) {
 #pragma unroll
-                for (int n = b; n < 4; ++n) {
+                for (int n = b; n + 1 < 4; n += 2) {
+                    FragB<T, M> p[4];
+                    sP.b_nk(p[0], p[1], n, b);
+                    sP.b_nk(p[2], p[3], n + 1, b);
+                    mma_quad(*reinterpret_cast<float(*)[4][4]>(&y[2 * n]), uf[b], p);
+                }
+                if ((4 - b) & 1) {
                     FragB<T, M> p0, p1;
-                    sP.b_nk(p0, p1, n, b);
                     float z0[4] = {}, z1[4] = {};
-                    mma_pair(y[2 * n], y[2 * n + 1], z0, z1, uf[b], p0, p1);
+                    sP.b_nk(p0, p1, 3, b);
+                    mma_pair(y[6], y[7], z0, z1, uf[b], p0, p1);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) y[2 * n][j] += z0[j], y[2 * n + 1][j] += z1[j];
+                    for (int j = 0; j < 4; ++j) y[6][j] += z0[j], y[7][j] += z1[j];
                 }
             }
         }
@@ -400,17 +426,16 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_reverse_kernel(DeltaCh
         const T* dp = (const T*)a.dout + seq.start * hrow + (long long)at.h * a.Dv + at.slice * kDeltaRows;
         const T* gp = (const T*)a.g + seq.start * a.Hv + at.h;
         const T* bp = (const T*)a.beta + seq.start * a.Hv + at.h;
-        const bool kvec = rows_aligned(kp, a.k_t), qvec = rows_aligned(qp, a.q_t), dvec = rows_aligned(dp, hrow);
-        const int vcols = min(a.Dv - at.slice * kDeltaRows, kDeltaRows);
+        const int ptid = threadIdx.x - kStateThreads;
+        const TileCopy<typename SM::KT, DK, kSystemThreads> ck(kp, a.k_t, a.Dk, ptid), cq(qp, a.q_t, a.Dk, ptid);
+        const TileCopy<typename SM::VT, kDeltaRows, kSystemThreads> cd(dp, hrow, min(a.Dv - at.slice * kDeltaRows, kDeltaRows), ptid);
         system_warps<T, DK, true, true>(
             smem, c1 - c0, a.scale,
             [&](int i, unsigned char* s, int tid) {
-                const int ch = c1 - 1 - i, n = min(seq.len - ch * kChunk, kChunk);
-                const long long t0 = (long long)ch * kChunk;
-                load_tile<kChunk, DK>(typename SM::KT(s + SM::k, kChunk), kp + t0 * a.k_t, a.k_t, n, a.Dk, kvec, tid, kSystemThreads);
-                load_tile<kChunk, DK>(typename SM::KT(s + SM::q, kChunk), qp + t0 * a.q_t, a.q_t, n, a.Dk, qvec, tid, kSystemThreads);
-                load_tile<kChunk, kDeltaRows>(typename SM::VT(s + SM::v, kChunk), dp + t0 * hrow, hrow, n, vcols, dvec, tid,
-                                              kSystemThreads);
+                const int first = (c1 - 1 - i) * kChunk, n = min(seq.len - first, kChunk);
+                ck.copy(s + SM::k, first, n, tid);
+                cq.copy(s + SM::q, first, n, tid);
+                cd.copy(s + SM::v, first, n, tid);
             },
             [&](int i, float(&v)[4]) {
                 const int ch = c1 - 1 - i;
@@ -444,18 +469,13 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_reverse_kernel(DeltaCh
         const typename SM::KT sK(st + SM::k, kChunk), sQ(st + SM::q, kChunk);
         const typename SM::VT sD(st + SM::v, kChunk);
         const typename SM::ET sE(sy + SM::e), sP(sy + SM::p);
-        const ChunkGates& G = *reinterpret_cast<const ChunkGates*>(sy + SM::gates);
+        const ChunkGates& G = *reinterpret_cast<const ChunkGates*>(smem + SM::gates + (i % 3) * SM::gate);
         bar_sync(kBarFull + (i & 1), kChainThreads);
         if (!c.summary)
             store_state_rows<DK>(S, (T*)c.ds + ((long long)(seq.slot + ch) * a.Hv + at.h) * a.Dv * a.Dk, row0, a.Dv, a.Dk);
 
         float x[8][4] = {};  // dU, then dX, transposed
-#pragma unroll
-        for (int d = 0; d < DK / 16; ++d) {
-            FragA<T, M> f;
-            frag_from_acc(f, S[2 * d], S[2 * d + 1]);
-            state_times<DK>(x, f, sK, d);
-        }
+        state_times<DK, false, M, T>(S, x, nullptr, sK, sK);
 #pragma unroll
         for (int n = 0; n < DK / 8; ++n)
 #pragma unroll
@@ -488,31 +508,34 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_reverse_kernel(DeltaCh
             frag_from_acc(fs, d0, d1);
             state_add<DK>(S, fs, sQ, b);
         }
-        FragA<T, M> rf[4];
+        FragA<T, M> rf[4], f;
+        float r0[4] = {}, r1[4] = {}, w0[4] = {}, w1[4] = {};
+        {
+            FragB<T, M> e0, e1;
+            sE.b_kn(e0, e1, 3, 3);
+            frag_from_acc(f, x[6], x[7]);
+            mma_pair(r0, r1, w0, w1, f, e0, e1);
+        }
 #pragma unroll
         for (int b = 3; b >= 0; --b) {
-            float r0[4] = {}, r1[4] = {}, w0[4] = {}, w1[4] = {};
-            FragB<T, M> e0, e1;
-#pragma unroll
-            for (int j = 3; j > b; --j) {
-                sE.b_kn(e0, e1, j, b);
-                mma_pair(x[2 * b], x[2 * b + 1], w0, w1, rf[j], e0, e1);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[2 * b][j] += w0[j], x[2 * b + 1][j] += w1[j], w0[j] = w1[j] = 0.0f;
-            FragA<T, M> f;
-            frag_from_acc(f, x[2 * b], x[2 * b + 1]);
-            sE.b_kn(e0, e1, b, b);
-            mma_pair(r0, r1, w0, w1, f, e0, e1);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 r0[j] += w0[j], r1[j] += w1[j];
-                x[2 * b][j] = r0[j];
-                x[2 * b + 1][j] = r1[j];
+                x[2 * b][j] = r0[j], x[2 * b + 1][j] = r1[j];
                 r0[j] *= G.beta[16 * b + 2 * t + (j & 1)];
                 r1[j] *= G.beta[16 * b + 8 + 2 * t + (j & 1)];
+                w0[j] = w1[j] = 0.0f;
             }
             frag_from_acc(rf[b], r0, r1);
+            FragB<T, M> e0, e1;
+            if (b > 0) {
+#pragma unroll
+                for (int j = 3; j >= b; --j) {
+                    sE.b_kn(e0, e1, j, b - 1);
+                    mma_pair(x[(2 * b - 2) & 7], x[(2 * b - 1) & 7], w0, w1, rf[j], e0, e1);
+                }
+                sE.b_kn(e0, e1, b - 1, b - 1);
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 r0[j] *= -G.ec[16 * b + 2 * t + (j & 1)];
@@ -520,6 +543,15 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_reverse_kernel(DeltaCh
             }
             frag_from_acc(f, r0, r1);
             state_add<DK>(S, f, sK, b);
+            if (b > 0) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[(2 * b - 2) & 7][j] += w0[j], x[(2 * b - 1) & 7][j] += w1[j];
+                    r0[j] = r1[j] = w0[j] = w1[j] = 0.0f;
+                }
+                frag_from_acc(f, x[(2 * b - 2) & 7], x[(2 * b - 1) & 7]);
+                mma_pair(r0, r1, w0, w1, f, e0, e1);
+            }
         }
         if (!c.summary) {
             const int n = min(seq.len - ch * kChunk, kChunk);

@@ -183,6 +183,12 @@ __device__ __forceinline__ void ldmatrix4_t(uint32_t (&r)[4], uint32_t addr) {
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 
+// four 8 x 8 matrices of 16-bit values, each written transposed: lane l gives row l % 8 of matrix l / 8
+__device__ __forceinline__ void stmatrix4_t(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3)
+                 : "memory");
+}
+
 template <int COLS, int NT> struct Tile<__nv_bfloat16, COLS, NT> {
     using T = __nv_bfloat16;
     static constexpr int kLd = COLS + 8, kVec = 8;
@@ -254,6 +260,12 @@ template <int COLS, int NT> struct Tile<__nv_bfloat16, COLS, NT> {
             b1.r[i][1] = r[3];
         }
     }
+    // two accumulator tiles (rows = tile columns c0 .., columns = tile rows r0 ..) written transposed
+    __device__ __forceinline__ void set_t(int r0, int c0, const float (&a)[4], const float (&b)[4]) const {
+        const int lane = threadIdx.x & 31;
+        stmatrix4_t(smem_u32(p + (r0 + (lane & 7) + ((lane >> 4) << 3)) * kLd + c0 + ((lane >> 3) & 1) * 8), pack_bf16(a[0], a[1]),
+                    pack_bf16(a[2], a[3]), pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3]));
+    }
     // the transposed 16 x 16 block as two accumulator tiles: c[j] holds columns k0 + 8j .. of rows m0 ..
     __device__ __forceinline__ void acc_km(float (&c0)[4], float (&c1)[4], int m0, int k0) const {
         FragA<T, 1> a;
@@ -323,6 +335,14 @@ template <int COLS, int NT> struct Tile<float, COLS, NT> {
             split_tf32(p[at(k + 1, n0 + g)], b0.hi[s][1], b0.lo[s][1]);
             split_tf32(p[at(k, n0 + 8 + g)], b1.hi[s][0], b1.lo[s][0]);
             split_tf32(p[at(k + 1, n0 + 8 + g)], b1.hi[s][1], b1.lo[s][1]);
+        }
+    }
+    __device__ __forceinline__ void set_t(int r0, int c0, const float (&a)[4], const float (&b)[4]) const {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            p[at(r0 + 2 * t + (x & 1), c0 + g + 8 * (x >> 1))] = a[x];
+            p[at(r0 + 8 + 2 * t + (x & 1), c0 + g + 8 * (x >> 1))] = b[x];
         }
     }
     __device__ __forceinline__ void acc_km(float (&c0)[4], float (&c1)[4], int m0, int k0) const {
@@ -449,6 +469,40 @@ __device__ __forceinline__ void load_tile(const TL& s, const typename TL::T* src
 template <typename T> __device__ __forceinline__ bool rows_aligned(const T* p, long long stride) {
     return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(stride * (long long)sizeof(T))) & 15) == 0;
 }
+
+// The same for tiles that a chain of chunks loads one after the other, by THREADS threads: every thread's rows and
+// columns are fixed, so that a copy costs a pointer and a comparison (worked out from scratch for each copy, the
+// addresses took 2300 of the 7500 cycles of a chunk).
+template <typename TL, int COLS, int THREADS> struct TileCopy {
+    using T = typename TL::T;
+    static constexpr int V = TL::kVec, P = COLS / V, kRows = THREADS / P, kTimes = kChunk / kRows;
+    static_assert(THREADS % P == 0 && kChunk % kRows == 0, "whole rows");
+    const T* src;      // the chain's first row
+    long long stride;
+    int row, off, bytes, cols;
+    bool vec;
+    __device__ __forceinline__ TileCopy(const T* s, long long st, int columns, int tid) : src(s), stride(st), cols(columns) {
+        vec = rows_aligned(s, st);
+        row = tid / P;
+        const int c = (tid % P) * V;
+        off = c;
+        bytes = min(max(columns - c, 0), V) * (int)sizeof(T);
+    }
+    // rows first .. first + rows - 1 of the chain
+    __device__ __forceinline__ void copy(unsigned char* tile, long long first, int rows, int tid) const {
+        const TL s(tile, kChunk);
+        if (vec) {
+            const T* p = src + (first + row) * stride + off;
+#pragma unroll
+            for (int i = 0; i < kTimes; ++i) {
+                const int n = row + i * kRows < rows ? bytes : 0;
+                cp_async16(s.vec_at(row + i * kRows, off), n ? p + i * kRows * stride : src, n);
+            }
+        } else {
+            load_tile<kChunk, COLS>(s, src + first * stride, stride, rows, cols, false, tid, THREADS);
+        }
+    }
+};
 
 // ------------------------------------------------------------------ where a sequence lies
 
