@@ -10,67 +10,83 @@ namespace {
 
 // ------------------------------------------------------------------ joining segments
 
-// One CTA per chain and 16 rows of the transposed state: S' = S X + N from segment to segment (X the
+// One CTA per chain and 8 rows of the transposed state: S' = S X + N from segment to segment (X the
 // segment's map, in reverse its transpose), fp32.  The sums N are replaced by the state at each
-// segment's start (in reverse: the gradient of the state at its end).
-constexpr int kJoinThreads = 128, kJoinRows = 16;
+// segment's start (in reverse: the gradient of the state at its end).  A serial walk that reads one map
+// after the other from the L2 cache: the next map and sum are on their way while this one is applied.
+constexpr int kJoinThreads = 256, kJoinRows = 8;
 __global__ void __launch_bounds__(kJoinThreads) delta_join_kernel(DeltaChain c, int reverse) {
-    extern __shared__ float sm[];
+    extern __shared__ __align__(16) float sm[];
     const DeltaArgs& a = c.a;
-    const int Dk = a.Dk, ld = Dk + 1, d = threadIdx.x;
-    float *X = sm, *S = sm + ((Dk * ld + 3) & ~3);  // S [Dk][16]
+    const int Dk = a.Dk, ld = Dk + 1, tid = threadIdx.x;
+    // thread: column d, rows 4 half .. 4 half + 3
+    const int d = tid & 127, half = tid >> 7;
+    float* S = sm;                          // [Dk][8]
+    float* X = sm + ((Dk * kJoinRows + 3) & ~3);  // two maps [Dk][Dk + 1]
+    const int map = (Dk * ld + 3) & ~3;
     pdl_launch_dependents();
     pdl_wait();
     const int strips = (a.Dv + kJoinRows - 1) / kJoinRows;
-    const int row0 = (int)(blockIdx.x % strips) * kJoinRows;
+    const int row0 = (int)(blockIdx.x % strips) * kJoinRows + 4 * half;
     const long long chain = blockIdx.x / strips;
     const DeltaSeq seq = delta_seq(a.offsets, (int)(chain / a.Hv), a.T, a.total, c.err);
     const int nseg = ((seq.len + kChunk - 1) / kChunk + c.seg_chunks - 1) / c.seg_chunks;
     const float* init = reverse ? a.dfinal : a.initial;
     float* last = reverse ? a.dinitial : a.final;
-    float s[kJoinRows];
+    const bool on = d < Dk;
+    auto place = [&](int i) { return chain * c.segs + (reverse ? nseg - 1 - i : i); };
+    auto fetch = [&](int i) {
+        const float* x = c.maps + place(i) * Dk * Dk;
+        float* to = X + (i & 1) * map;
+        for (int j = tid; j < Dk * Dk; j += kJoinThreads) cp_async4(to + (j / Dk) * ld + j % Dk, x + j, 4);
+        cp_async_commit();
+    };
+    float s[4], n[4];
+    auto sums = [&](int i) {
 #pragma unroll
-    for (int r = 0; r < kJoinRows; ++r)
-        s[r] = init && d < Dk && row0 + r < a.Dv ? init[(chain * Dk + d) * a.Dv + row0 + r] : 0.0f;
+        for (int r = 0; r < 4; ++r) n[r] = on && row0 + r < a.Dv ? c.sums[(place(i) * a.Dv + row0 + r) * Dk + d] : 0.0f;
+    };
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[r] = init && on && row0 + r < a.Dv ? init[(chain * Dk + d) * a.Dv + row0 + r] : 0.0f;
+    if (nseg > 0) {
+        fetch(0);
+        sums(0);
+    }
     for (int i = 0; i < nseg; ++i) {
-        const long long at = chain * c.segs + (reverse ? nseg - 1 - i : i);
-        const float* x = c.maps + at * Dk * Dk;
-        float* n = c.sums + at * a.Dv * Dk;
-        __syncthreads();
-        for (int j = threadIdx.x; j < Dk * Dk; j += kJoinThreads) X[(j / Dk) * ld + j % Dk] = x[j];
-        if (d < Dk) {
+        if (on) {
+            *reinterpret_cast<float4*>(S + d * kJoinRows + 4 * half) = make_float4(s[0], s[1], s[2], s[3]);
 #pragma unroll
-            for (int r = 0; r < kJoinRows; ++r) S[d * kJoinRows + r] = s[r];
-#pragma unroll
-            for (int r = 0; r < kJoinRows; ++r)
-                if (row0 + r < a.Dv) {
-                    float* p = n + (long long)(row0 + r) * Dk + d;
-                    const float sum = *p;
-                    *p = s[r];
-                    s[r] = sum;
-                }
-        }
-        __syncthreads();
-        if (d < Dk) {
-            const float* col = reverse ? X + d * ld : X + d;
-            const int step = reverse ? 1 : ld;
-#pragma unroll 4
-            for (int e = 0; e < Dk; ++e) {
-                const float v = col[e * step];
-#pragma unroll
-                for (int r = 0; r < kJoinRows; r += 4) {
-                    const float4 q = *reinterpret_cast<const float4*>(S + e * kJoinRows + r);
-                    s[r] = fmaf(q.x, v, s[r]);
-                    s[r + 1] = fmaf(q.y, v, s[r + 1]);
-                    s[r + 2] = fmaf(q.z, v, s[r + 2]);
-                    s[r + 3] = fmaf(q.w, v, s[r + 3]);
-                }
+            for (int r = 0; r < 4; ++r) {
+                if (row0 + r < a.Dv) c.sums[(place(i) * a.Dv + row0 + r) * Dk + d] = s[r];
+                s[r] = n[r];
             }
         }
+        if (i + 1 < nseg) {
+            fetch(i + 1);
+            sums(i + 1);
+            cp_async_wait<1>();
+        } else {
+            cp_async_wait<0>();
+        }
+        __syncthreads();
+        if (on) {
+            const float* col = X + (i & 1) * map + (reverse ? d * ld : d);
+            const int step = reverse ? 1 : ld;
+#pragma unroll 8
+            for (int e = 0; e < Dk; ++e) {
+                const float v = col[e * step];
+                const float4 q = *reinterpret_cast<const float4*>(S + e * kJoinRows + 4 * half);
+                s[0] = fmaf(q.x, v, s[0]);
+                s[1] = fmaf(q.y, v, s[1]);
+                s[2] = fmaf(q.z, v, s[2]);
+                s[3] = fmaf(q.w, v, s[3]);
+            }
+        }
+        __syncthreads();  // S and this map have been read
     }
-    if (last && d < Dk) {
+    if (last && on) {
 #pragma unroll
-        for (int r = 0; r < kJoinRows; ++r)
+        for (int r = 0; r < 4; ++r)
             if (row0 + r < a.Dv) last[(chain * Dk + d) * a.Dv + row0 + r] = s[r];
     }
 }
@@ -208,9 +224,9 @@ vmb_status chain(const DeltaChain& c, bool reverse, cudaStream_t stream) {
 
 vmb_status join(const DeltaChain& c, bool reverse, cudaStream_t stream) {
     const int strips = (c.a.Dv + kJoinRows - 1) / kJoinRows;
-    const size_t smem = 4 * (size_t)(((c.a.Dk * (c.a.Dk + 1) + 3) & ~3) + c.a.Dk * kJoinRows);
+    const size_t smem = 4 * (size_t)(2 * ((c.a.Dk * (c.a.Dk + 1) + 3) & ~3) + ((c.a.Dk * kJoinRows + 3) & ~3));
     const void* fn = (const void*)delta_join_kernel;
-    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, 100 * 1024) != cudaSuccess) return VMB_ERR_CUDA;
+    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, 140 * 1024) != cudaSuccess) return VMB_ERR_CUDA;
     DeltaChain arg = c;
     int rev = reverse;
     void* args[] = {&arg, &rev};
