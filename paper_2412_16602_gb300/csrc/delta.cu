@@ -1,8 +1,10 @@
 // delta.cu - the gated delta rule: plans, the kernel that joins the segments of a chain, the sum over
 // shared heads, and the recurrent step.
-#include "delta_common.cuh"
+#include "delta_grad.cuh"
 #include "delta_internal.h"
 #include "vmb_internal.h"
+
+#include <mutex>
 
 namespace vmb {
 
@@ -226,7 +228,7 @@ vmb_status join(const DeltaChain& c, bool reverse, cudaStream_t stream) {
     const int strips = (c.a.Dv + kJoinRows - 1) / kJoinRows;
     const size_t smem = 4 * (size_t)(2 * ((c.a.Dk * (c.a.Dk + 1) + 3) & ~3) + ((c.a.Dk * kJoinRows + 3) & ~3));
     const void* fn = (const void*)delta_join_kernel;
-    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, 140 * 1024) != cudaSuccess) return VMB_ERR_CUDA;
+    if (!allow_smem(fn, 140 * 1024)) return VMB_ERR_CUDA;
     DeltaChain arg = c;
     int rev = reverse;
     void* args[] = {&arg, &rev};
@@ -250,6 +252,26 @@ DeltaChain chain_of(const DeltaArgs& a, const DeltaPlan& p) {
 }
 
 }  // namespace
+
+// (the attribute costs about 1 us of host time to set: once per kernel and device)
+bool allow_smem(const void* fn, int bytes) {
+    struct Entry {
+        const void* fn;
+        int dev;
+    };
+    constexpr int kMax = 256;  // above the number of kernel instances; a full table only stops keeping answers
+    static std::mutex mu;
+    static Entry table[kMax];
+    static int used = 0;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    std::lock_guard<std::mutex> g(mu);
+    for (int i = 0; i < used; ++i)
+        if (table[i].fn == fn && table[i].dev == dev) return true;
+    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    if (used < kMax) table[used++] = {fn, dev};
+    return true;
+}
 
 long long delta_slots(int B, int T, long long total, bool packed) {
     return packed ? total / kChunk + B : (long long)B * ((T + kChunk - 1) / kChunk);
@@ -286,7 +308,7 @@ DeltaPlan plan_delta(const DeltaArgs& a, bool grads, int sms) {
         p.dx_off = at;
         at += align_up((size_t)a.total * a.Hv * a.Dv * es, 256);
         p.part_off = at;
-        if (a.Hv != a.Hk) at += align_up((size_t)a.total * a.Hv * 2 * a.Dk * 4, 256);
+        if (grad_leaves_parts(a)) at += align_up((size_t)a.total * a.Hv * 2 * a.Dk * 4, 256);
     }
     p.bytes = at;
     return p;
@@ -326,7 +348,7 @@ vmb_status launch_delta_bwd(const DeltaArgs& a, cudaStream_t stream) {
     g.part = (float*)((unsigned char*)a.ws + p.part_off);
     g.err = c.err;
     if ((s = a.dtype == VMB_BF16 ? launch_grad_bf16(g, stream) : launch_grad_f32(g, stream)) != VMB_OK) return s;
-    if (a.Hv == a.Hk) return VMB_OK;
+    if (!grad_leaves_parts(a)) return VMB_OK;
     long long n = a.total * a.Hk * a.Dk;
     int Hk = a.Hk, r = a.Hv / a.Hk, Dk = a.Dk;
     const long long want = (n + 255) / 256, most = (long long)device_sm_count() * 8;

@@ -586,7 +586,7 @@ vmb_status launch_chain_dk(const DeltaChain& c, bool reverse, cudaStream_t strea
     const long long per = reverse || !c.summary ? c.slices : c.maps_only ? mslices : c.slices + mslices;
     const long long grid = (long long)c.a.B * c.a.Hv * c.segs * per;
     const size_t smem = ChainSmem<T, DK>::total;
-    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return VMB_ERR_CUDA;
+    if (!allow_smem(fn, (int)smem)) return VMB_ERR_CUDA;
     DeltaChain arg = c;
     void* args[] = {&arg};
     return launch_kernel(fn, dim3((unsigned)grid), dim3(kChainThreads), smem, args, stream) == cudaSuccess ? VMB_OK : VMB_ERR_CUDA;

@@ -9,10 +9,11 @@
 // (The pairs within i, j >= t cancel in dg: taken from the same fp32 products they do so exactly up to
 // fp32 rounding, which q.dq - k.dk of the finished gradients, rounded through bf16 operands, would not.)
 //
-// One CTA per chunk and value head, eight warps: warp w computes the 16 tokens of block w % 4 for one half
-// of the Dk columns, and of the 64 x 64 products dP (first half) or dA (second).  The value channels come
-// in slices of 64.  Scales by token are applied to the accumulators, so that the operands are the kept
-// values themselves.
+// One CTA per chunk and key head takes the value heads that share it in turn and sums their dq and dk in shared
+// memory (fp32 with Dk > 64 has no room for the sums: one CTA per value head, the sums by delta_share_kernel).  Warp w
+// computes the 16 tokens of block w % 4 for a part of the Dk columns, and a part of the 64 x 64 products dP or dA.  The
+// value channels come in slices of 64, the next slice on its way while one is multiplied where it fits.  Scales by
+// token are applied to the accumulators, so that the operands are the kept values themselves.
 #pragma once
 
 #include "delta_common.cuh"
@@ -20,89 +21,126 @@
 
 namespace vmb {
 
-constexpr int kGradThreads = 256;
-
+// bf16 with Dk <= 64: eight warps and two CTAs per SM, whose loads and products overlap; otherwise 16 warps, or eight
+// of 255 registers where 128 are too few (fp32 with Dk > 64: 1.2 KB of spills per thread).
 template <typename T, int DK> struct GradSmem {
+    static constexpr bool small = sizeof(T) == 2 && DK == 64;
+    static constexpr int warps = small || (sizeof(T) == 4 && DK == 128) ? 8 : 16, threads = 32 * warps, groups = warps / 4;
     using KT = Tile<T, DK, 1>;
     using VT = Tile<T, 64, 1>;
     using PT = Tile<T, 64, sizeof(T) == 2 ? 2 : 1>;
-    static constexpr int k = 0, q = k + KT::bytes(64), d = q + KT::bytes(64), r = d + VT::bytes(64), x = r + VT::bytes(64),
-                         s = x + VT::bytes(64), ds = s + KT::bytes(64), tiles = ds + KT::bytes(64);
-    // dP and dA take the place of do .. dS
-    static constexpr int dp = d, da = dp + PT::bytes(64);
-    static_assert(da + PT::bytes(64) <= tiles, "dP and dA fit");
-    static constexpr int gates = tiles, sums = gates + (int)sizeof(ChunkGates);
-    // row sums [2][64], column sums [2][4][64], dots [2][3][64], dbeta [64], block sums [8]
-    static constexpr int total = sums + 4 * (128 + 512 + 384 + 64 + 8);
+    // a slice: do, r, dX, S, dS; dP and dA take the place of the last one read
+    static constexpr int d = 0, r = d + VT::bytes(64), x = r + VT::bytes(64), s = x + VT::bytes(64), ds = s + KT::bytes(64),
+                         slice = ds + KT::bytes(64);
+    static constexpr int dp = 0, da = dp + PT::bytes(64);
+    static_assert(da + PT::bytes(64) <= slice, "dP and dA fit");
+    // row sums [groups][64], column sums [2][4][64], dots [groups][3][64], dbeta [64], block sums [16]
+    static constexpr int sums = (groups * 64 + 512 + groups * 192 + 64 + 16) * 4;
+    static constexpr int k = 0, q = k + KT::bytes(64), gates = q + KT::bytes(64),
+                         sum0 = gates + (((int)sizeof(ChunkGates) + 15) & ~15), slices = (sum0 + sums + 127) & ~127;
+    static constexpr int limit = small ? 113 * 1024 : 227 * 1024;
+    static constexpr bool totals = slices + slice + 2 * 64 * DK * 4 <= limit;
+    static constexpr int tot = slices + slice, one = tot + (totals ? 2 * 64 * DK * 4 : 0);
+    static constexpr bool ahead = !small && one + slice <= limit;  // a second slice
+    static constexpr int slice2 = one, total = one + (ahead ? slice : 0);
+    static_assert(total <= limit, "fits");
 };
 
 template <typename T, int DK>
-__global__ void __launch_bounds__(kGradThreads) delta_grad_kernel(DeltaGrad c) {
+__global__ void __launch_bounds__(GradSmem<T, DK>::threads, GradSmem<T, DK>::small ? 2 : 1) delta_grad_kernel(DeltaGrad c) {
     using SM = GradSmem<T, DK>;
-    constexpr int HT = DK / 16;  // column tiles of 8 per warp
+    constexpr int N = SM::threads, NG = SM::groups, HC = DK / NG, HT = HC / 8;  // columns and column tiles per warp
+    constexpr int JB = 8 / NG;                                                   // blocks of dP or dA per warp
     extern __shared__ __align__(128) unsigned char smem[];
     const DeltaArgs& a = c.a;
     const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    const int tb = w & 3, hf = w >> 2, col0 = hf * (DK / 2);
+    const int tb = w & 3, qt = w >> 2, col0 = qt * HC;
+    const bool second = qt & 1;  // this warp's part of dA, otherwise of dP
+    auto block = [&](int i) { return NG == 2 ? i : 2 * i + (qt >> 1); };
     pdl_launch_dependents();
     pdl_wait();
-    const int chunks = (a.T + kChunk - 1) / kChunk;
+    const int chunks = (a.T + kChunk - 1) / kChunk, share = a.Hv / a.Hk, heads = SM::totals ? a.Hk : a.Hv;
     const int ch = blockIdx.x % chunks;
     const long long chain = blockIdx.x / chunks;
-    const int h = (int)(chain % a.Hv), b = (int)(chain / a.Hv);
+    const int head = (int)(chain % heads), b = (int)(chain / heads);
     const DeltaSeq seq = delta_seq(a.offsets, b, a.T, a.total, c.err);
     const int n = min(seq.len - ch * kChunk, kChunk);
     if (n <= 0) return;
-
-    const int hk = h / (a.Hv / a.Hk);
+    const int hk = SM::totals ? head : head / share, h0 = SM::totals ? head * share : head, turns = SM::totals ? share : 1;
     const long long brow = a.offsets ? 0 : b, tok0 = (a.offsets ? seq.start : 0) + (long long)ch * kChunk;
     const long long tok = seq.start + (long long)ch * kChunk;  // in the dense tensors
     const T* kp = (const T*)a.k + brow * a.k_b + tok0 * a.k_t + (long long)hk * a.Dk;
     const T* qp = (const T*)a.q + brow * a.q_b + tok0 * a.q_t + (long long)hk * a.Dk;
-    const long long hrow = (long long)a.Hv * a.Dv, off = tok * hrow + (long long)h * a.Dv;
-    const T *dp = (const T*)a.dout + off, *rp = (const T*)a.saved_r + off, *xp = (const T*)c.dx + off;
-    const long long srow = ((long long)(seq.slot + ch) * a.Hv + h) * a.Dv * a.Dk;
-    const T *sp = (const T*)a.saved + srow, *dsp = (const T*)c.ds + srow;
+    const long long hrow = (long long)a.Hv * a.Dv;
 
-    const typename SM::KT sK(smem + SM::k, 64), sQ(smem + SM::q, 64), sS(smem + SM::s, 64), sDS(smem + SM::ds, 64);
-    const typename SM::VT sD(smem + SM::d, 64), sR(smem + SM::r, 64), sX(smem + SM::x, 64);
-    const typename SM::PT sDP(smem + SM::dp, 64), sDA(smem + SM::da, 64);
+    const typename SM::KT sK(smem + SM::k, 64), sQ(smem + SM::q, 64);
     ChunkGates& G = *reinterpret_cast<ChunkGates*>(smem + SM::gates);
-    float* rowsum = reinterpret_cast<float*>(smem + SM::sums);
-    float *colsum = rowsum + 128, *dots = colsum + 512, *dbeta = dots + 384, *blocks = dbeta + 64;
+    float* rowsum = reinterpret_cast<float*>(smem + SM::sum0);
+    float *colsum = rowsum + NG * 64, *dots = colsum + 512, *dbeta = dots + NG * 192, *blocks = dbeta + 64;
+    float* tot = reinterpret_cast<float*>(smem + SM::tot);
+    const int vslices = (a.Dv + 63) / 64, steps = turns * vslices;
 
-    load_tile<64, DK>(sK, kp, a.k_t, n, a.Dk, rows_aligned(kp, a.k_t), tid, kGradThreads);
-    load_tile<64, DK>(sQ, qp, a.q_t, n, a.Dk, rows_aligned(qp, a.q_t), tid, kGradThreads);
-    if (w == 0) {
-        const T *gp = (const T*)a.g + tok * a.Hv + h, *bp = (const T*)a.beta + tok * a.Hv + h;
-        float v[4];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            v[i] = 2 * lane + i < n ? io<T>::cvt(gp[(long long)(2 * lane + i) * a.Hv]) : 0.0f;
-            v[2 + i] = 2 * lane + i < n ? io<T>::cvt(bp[(long long)(2 * lane + i) * a.Hv]) : 0.0f;
-        }
-        chunk_gates(G, v[0], v[1], v[2], v[3]);
-    }
-
-    float dq[HT][4] = {}, dkr[HT][4] = {}, dkt[HT][4] = {}, W[8][4] = {};
-    float sdot = 0.0f, bdot = 0.0f;
-    for (int v0 = 0; v0 < a.Dv; v0 += 64) {
-        const int cols = min(a.Dv - v0, 64);
-        if (v0) __syncthreads();
-        load_tile<64, 64>(sD, dp + v0, hrow, n, cols, rows_aligned(dp + v0, hrow), tid, kGradThreads);
-        load_tile<64, 64>(sR, rp + v0, hrow, n, cols, rows_aligned(rp + v0, hrow), tid, kGradThreads);
-        load_tile<64, 64>(sX, xp + v0, hrow, n, cols, rows_aligned(xp + v0, hrow), tid, kGradThreads);
-        const T *s0 = sp + (long long)v0 * a.Dk, *ds0 = dsp + (long long)v0 * a.Dk;
-        load_tile<64, DK>(sS, s0, a.Dk, cols, a.Dk, rows_aligned(s0, a.Dk), tid, kGradThreads);
-        load_tile<64, DK>(sDS, ds0, a.Dk, cols, a.Dk, rows_aligned(ds0, a.Dk), tid, kGradThreads);
+    // slice i of the CTA: value head h0 + i / vslices, channels from 64 (i % vslices)
+    auto load = [&](int i) {
+        const int h = h0 + i / vslices, v0 = (i % vslices) * 64, cols = min(a.Dv - v0, 64);
+        unsigned char* s = smem + (SM::ahead && (i & 1) ? SM::slice2 : SM::slices);
+        const long long off = tok * hrow + (long long)h * a.Dv + v0;
+        const T *dp = (const T*)a.dout + off, *rp = (const T*)a.saved_r + off, *xp = (const T*)c.dx + off;
+        load_tile<64, 64>(typename SM::VT(s + SM::d, 64), dp, hrow, n, cols, rows_aligned(dp, hrow), tid, N);
+        load_tile<64, 64>(typename SM::VT(s + SM::r, 64), rp, hrow, n, cols, rows_aligned(rp, hrow), tid, N);
+        load_tile<64, 64>(typename SM::VT(s + SM::x, 64), xp, hrow, n, cols, rows_aligned(xp, hrow), tid, N);
+        const long long srow = (((long long)(seq.slot + ch) * a.Hv + h) * a.Dv + v0) * a.Dk;
+        const T *sp = (const T*)a.saved + srow, *dsp = (const T*)c.ds + srow;
+        load_tile<64, DK>(typename SM::KT(s + SM::s, 64), sp, a.Dk, cols, a.Dk, rows_aligned(sp, a.Dk), tid, N);
+        load_tile<64, DK>(typename SM::KT(s + SM::ds, 64), dsp, a.Dk, cols, a.Dk, rows_aligned(dsp, a.Dk), tid, N);
         cp_async_commit();
-        cp_async_wait<0>();
+    };
+    load_tile<64, DK>(sK, kp, a.k_t, n, a.Dk, rows_aligned(kp, a.k_t), tid, N);
+    load_tile<64, DK>(sQ, qp, a.q_t, n, a.Dk, rows_aligned(qp, a.q_t), tid, N);
+    load(0);
+
+    float dq[HT][4], dkr[HT][4], dkt[HT][4], W[2 * JB][4];
+    float sdot = 0.0f, bdot = 0.0f;
+    for (int i = 0; i < steps; ++i) {
+        const int h = h0 + i / vslices, vs = i % vslices;
+        unsigned char* s = smem + (SM::ahead && (i & 1) ? SM::slice2 : SM::slices);
+        const typename SM::KT sS(s + SM::s, 64), sDS(s + SM::ds, 64);
+        const typename SM::VT sD(s + SM::d, 64), sR(s + SM::r, 64), sX(s + SM::x, 64);
+        if (vs == 0) {
+#pragma unroll
+            for (int j = 0; j < HT; ++j)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) dq[j][x] = dkr[j][x] = dkt[j][x] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 2 * JB; ++j)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) W[j][x] = 0.0f;
+            sdot = bdot = 0.0f;
+            if (w == 0) {
+                const T *gp = (const T*)a.g + tok * a.Hv + h, *bp = (const T*)a.beta + tok * a.Hv + h;
+                float v[4];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    v[x] = 2 * lane + x < n ? io<T>::cvt(gp[(long long)(2 * lane + x) * a.Hv]) : 0.0f;
+                    v[2 + x] = 2 * lane + x < n ? io<T>::cvt(bp[(long long)(2 * lane + x) * a.Hv]) : 0.0f;
+                }
+                chunk_gates(G, v[0], v[1], v[2], v[3]);
+            }
+        }
+        if (SM::ahead && i + 1 < steps) {
+            load(i + 1);
+            cp_async_wait<1>();
+        } else {
+            cp_async_wait<0>();
+        }
         __syncthreads();
-        {  // this thread's part of dbeta: token tid / 4, every fourth channel
-            const int i = tid >> 2, q4 = tid & 3;
+        {  // this thread's part of dbeta: token tid / (N / 64); and of <S, dS>
+            constexpr int per = N / 64;
+            const int tk = tid / per, p = tid % per;
 #pragma unroll 4
-            for (int j = 0; j < 16; ++j) bdot = fmaf(sX.get(i, q4 + 4 * j), sR.get(i, q4 + 4 * j), bdot);
-            for (int j = tid; j < 64 * DK; j += kGradThreads) sdot = fmaf(sS.get(j / DK, j % DK), sDS.get(j / DK, j % DK), sdot);
+            for (int j = 0; j < 64 / per; ++j) bdot = fmaf(sX.get(tk, p + per * j), sR.get(tk, p + per * j), bdot);
+#pragma unroll 4
+            for (int j = tid; j < 64 * DK; j += N) sdot = fmaf(sS.get(j / DK, j % DK), sDS.get(j / DK, j % DK), sdot);
         }
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
@@ -123,193 +161,243 @@ __global__ void __launch_bounds__(kGradThreads) delta_grad_kernel(DeltaGrad c) {
                 mma16(dkt[2 * j + 1], fr, b1);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j <= tb) {
-                    sR.b_nk(b0, b1, 16 * j, 16 * kk);
-                    mma16(W[2 * j], hf ? fx : fd, b0);
-                    mma16(W[2 * j + 1], hf ? fx : fd, b1);
+            for (int j = 0; j < JB; ++j)
+                if (block(j) <= tb) {
+                    sR.b_nk(b0, b1, 16 * block(j), 16 * kk);
+                    mma16(W[2 * j], second ? fx : fd, b0);
+                    mma16(W[2 * j + 1], second ? fx : fd, b1);
                 }
         }
-    }
-    // dP or dA, and their products with q k^T or k k^T
-    {
-        float m[8][4] = {};
-#pragma unroll
-        for (int d = 0; d < DK / 16; ++d) {
-            FragA<T, 1> f;
-            FragB<T, 1> b0, b1;
-            if (hf) sK.a_mk(f, 16 * tb, 16 * d); else sQ.a_mk(f, 16 * tb, 16 * d);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j <= tb) {
-                    sK.b_nk(b0, b1, 16 * j, 16 * d);
-                    mma16(m[2 * j], f, b0);
-                    mma16(m[2 * j + 1], f, b1);
-                }
+        if (vs + 1 < vslices) {
+            __syncthreads();  // this slice has been read
+            if (!SM::ahead) load(i + 1);
+            continue;
         }
-        __syncthreads();  // do, r, dX, S and dS have been read
+        // dP or dA, and their products with q k^T or k k^T
+        const typename SM::PT sDP(s + SM::dp, 64), sDA(s + SM::da, 64);
         float rs[2] = {};
+        {
+            float m[2 * JB][4] = {};
 #pragma unroll
-        for (int jt = 0; jt < 8; ++jt) {
-            float cs[2] = {};
-            if (jt / 2 <= tb) {
+            for (int d = 0; d < DK / 16; ++d) {
+                FragA<T, 1> f;
+                FragB<T, 1> b0, b1;
+                if (second) sK.a_mk(f, 16 * tb, 16 * d); else sQ.a_mk(f, 16 * tb, 16 * d);
 #pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    const int i = 16 * tb + g + 8 * hh;
-                    float v[2];
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int j = 8 * jt + 2 * t + x;
-                        const float e = j <= i ? decay(G.hi[i] - G.hi[j], G.lo[i] - G.lo[j]) * G.beta[j] : 0.0f;
-                        const float f = hf ? (j < i ? -e * G.beta[i] : 0.0f) : a.scale * e;
-                        v[x] = f * W[jt][2 * hh + x];
-                        const float p = v[x] * m[jt][2 * hh + x];
-                        rs[hh] += p;
-                        cs[x] += p;
+                for (int j = 0; j < JB; ++j)
+                    if (block(j) <= tb) {
+                        sK.b_nk(b0, b1, 16 * block(j), 16 * d);
+                        mma16(m[2 * j], f, b0);
+                        mma16(m[2 * j + 1], f, b1);
                     }
-                    (hf ? sDA : sDP).set2(i, 8 * jt + 2 * t, v[0], v[1]);
+            }
+            __syncthreads();  // do, r, dX, S and dS have been read
+#pragma unroll
+            for (int jt = 0; jt < 2 * JB; ++jt) {
+                const int bj = block(jt / 2), j0 = 16 * bj + 8 * (jt & 1) + 2 * t;
+                float cs[2] = {};
+                if (bj <= tb) {
+#pragma unroll
+                    for (int hh = 0; hh < 2; ++hh) {
+                        const int r = 16 * tb + g + 8 * hh;
+                        float v[2];
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const int j = j0 + x;
+                            const float e = j <= r ? decay(G.hi[r] - G.hi[j], G.lo[r] - G.lo[j]) * G.beta[j] : 0.0f;
+                            const float f = second ? (j < r ? -e * G.beta[r] : 0.0f) : a.scale * e;
+                            v[x] = f * W[jt][2 * hh + x];
+                            const float p = v[x] * m[jt][2 * hh + x];
+                            rs[hh] += p;
+                            cs[x] += p;
+                        }
+                        (second ? sDA : sDP).set2(r, j0, v[0], v[1]);
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    cs[x] += __shfl_xor_sync(0xffffffffu, cs[x], 4);
+                    cs[x] += __shfl_xor_sync(0xffffffffu, cs[x], 8);
+                    cs[x] += __shfl_xor_sync(0xffffffffu, cs[x], 16);
+                    if (g == 0) colsum[((second ? 4 : 0) + tb) * 64 + j0 + x] = cs[x];
                 }
             }
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                cs[x] += __shfl_xor_sync(0xffffffffu, cs[x], 4);
-                cs[x] += __shfl_xor_sync(0xffffffffu, cs[x], 8);
-                cs[x] += __shfl_xor_sync(0xffffffffu, cs[x], 16);
-                if (g == 0) colsum[(hf * 4 + tb) * 64 + 8 * jt + 2 * t + x] = cs[x];
-            }
         }
+        // the products with the states, scaled by token, and their dot products with q and k
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh) {
+            const int r = 16 * tb + g + 8 * hh;
+            const float sq = a.scale * G.ec[r], sr = -G.ec[r] * G.beta[r], st = G.tail[r] * G.beta[r];
+            float dot[3] = {};
+#pragma unroll
+            for (int j = 0; j < HT; ++j)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int cc = col0 + 8 * j + 2 * t + x;
+                    const float qv = sQ.get(r, cc), kv = sK.get(r, cc);
+                    float &eq = dq[j][2 * hh + x], &er = dkr[j][2 * hh + x];
+                    const float et = dkt[j][2 * hh + x] * st;
+                    eq *= sq;
+                    er *= sr;
+                    dot[0] = fmaf(qv, eq, dot[0]);
+                    dot[1] = fmaf(kv, er, dot[1]);
+                    dot[2] = fmaf(kv, et, dot[2]);
+                    er += et;
+                }
+#pragma unroll
+            for (int x = 0; x < 3; ++x) {
+                dot[x] += __shfl_xor_sync(0xffffffffu, dot[x], 1);
+                dot[x] += __shfl_xor_sync(0xffffffffu, dot[x], 2);
+                if (t == 0) dots[(qt * 3 + x) * 64 + r] = dot[x];
+            }
             rs[hh] += __shfl_xor_sync(0xffffffffu, rs[hh], 1);
             rs[hh] += __shfl_xor_sync(0xffffffffu, rs[hh], 2);
-            if (t == 0) rowsum[hf * 64 + 16 * tb + g + 8 * hh] = rs[hh];
+            if (t == 0) rowsum[qt * 64 + r] = rs[hh];
         }
-    }
-    // the products with the states, scaled by token, and their dot products with q and k
+        {
+            constexpr int per = N / 64;
+            float v = bdot;
 #pragma unroll
-    for (int hh = 0; hh < 2; ++hh) {
-        const int i = 16 * tb + g + 8 * hh;
-        const float sq = a.scale * G.ec[i], sr = -G.ec[i] * G.beta[i], st = G.tail[i] * G.beta[i];
-        float dot[3] = {};
+            for (int d = 1; d < per; d <<= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+            if (tid % per == 0) dbeta[tid / per] = v;
+            v = sdot;
 #pragma unroll
-        for (int j = 0; j < HT; ++j)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int cc = col0 + 8 * j + 2 * t + x;
-                const float qv = sQ.get(i, cc), kv = sK.get(i, cc);
-                float &eq = dq[j][2 * hh + x], &er = dkr[j][2 * hh + x];
-                const float et = dkt[j][2 * hh + x] * st;
-                eq *= sq;
-                er *= sr;
-                dot[0] = fmaf(qv, eq, dot[0]);
-                dot[1] = fmaf(kv, er, dot[1]);
-                dot[2] = fmaf(kv, et, dot[2]);
-                er += et;
-            }
-#pragma unroll
-        for (int x = 0; x < 3; ++x) {
-            dot[x] += __shfl_xor_sync(0xffffffffu, dot[x], 1);
-            dot[x] += __shfl_xor_sync(0xffffffffu, dot[x], 2);
-            if (t == 0) dots[(hf * 3 + x) * 64 + i] = dot[x];
+            for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+            if (lane == 0) blocks[w] = v;
         }
-    }
-    bdot += __shfl_xor_sync(0xffffffffu, bdot, 1);
-    bdot += __shfl_xor_sync(0xffffffffu, bdot, 2);
-    if ((tid & 3) == 0) dbeta[tid >> 2] = bdot;
+        __syncthreads();
 #pragma unroll
-    for (int d = 16; d; d >>= 1) sdot += __shfl_xor_sync(0xffffffffu, sdot, d);
-    if (lane == 0) blocks[w] = sdot;
-    __syncthreads();
-
+        for (int j = 0; j < 4; ++j) {
+            FragA<T, sizeof(T) == 2 ? 2 : 1> fp, fa;
+            FragB<T, 1> b0, b1;
+            if (j <= tb) {
+                sDP.a_mk(fp, 16 * tb, 16 * j);
+                sDA.a_mk(fa, 16 * tb, 16 * j);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        FragA<T, sizeof(T) == 2 ? 2 : 1> fp, fa, fpt, fat;
-        const bool low = j <= tb, high = j >= tb;
-        if (low) sDP.a_mk(fp, 16 * tb, 16 * j), sDA.a_mk(fa, 16 * tb, 16 * j);
-        if (high) sDP.a_km(fpt, 16 * tb, 16 * j), sDA.a_km(fat, 16 * tb, 16 * j);
-        FragB<T, 1> b0, b1;
-#pragma unroll
-        for (int d = 0; d < HT / 2; ++d) {
-            sK.b_kn(b0, b1, 16 * j, col0 + 16 * d);
-            if (low) {
-                mma16(dq[2 * d], fp, b0);
-                mma16(dq[2 * d + 1], fp, b1);
-                mma16(dkr[2 * d], fa, b0);
-                mma16(dkr[2 * d + 1], fa, b1);
-            }
-            if (high) {
-                mma16(dkr[2 * d], fat, b0);
-                mma16(dkr[2 * d + 1], fat, b1);
-                sQ.b_kn(b0, b1, 16 * j, col0 + 16 * d);
-                mma16(dkr[2 * d], fpt, b0);
-                mma16(dkr[2 * d + 1], fpt, b1);
-            }
-        }
-    }
-    const bool shared = a.Hv != a.Hk;
-#pragma unroll
-    for (int hh = 0; hh < 2; ++hh) {
-        const int i = 16 * tb + g + 8 * hh;
-        if (i >= n) continue;
-        const long long row = shared ? ((tok + i) * a.Hv + h) * 2 * a.Dk : ((tok + i) * a.Hk + hk) * a.Dk;
-#pragma unroll
-        for (int j = 0; j < HT; ++j)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int cc = col0 + 8 * j + 2 * t + x;
-                if (cc >= a.Dk) continue;
-                if (shared) {
-                    c.part[row + cc] = dq[j][2 * hh + x];
-                    c.part[row + a.Dk + cc] = dkr[j][2 * hh + x];
-                } else {
-                    ((T*)a.dq)[row + cc] = io<T>::to(dq[j][2 * hh + x]);
-                    ((T*)a.dk)[row + cc] = io<T>::to(dkr[j][2 * hh + x]);
+                for (int d = 0; d < HT / 2; ++d) {
+                    sK.b_kn(b0, b1, 16 * j, col0 + 16 * d);
+                    mma16(dq[2 * d], fp, b0);
+                    mma16(dq[2 * d + 1], fp, b1);
+                    mma16(dkr[2 * d], fa, b0);
+                    mma16(dkr[2 * d + 1], fa, b1);
                 }
             }
-    }
-    if (w == 0) {
-        // dg: the suffix sums of `suf`, the prefix sums (before t) of `pre`, and the chunk's own decay
-        float suf[2], pre[2], ds = 0.0f;
+            if (j >= tb) {
+                sDP.a_km(fp, 16 * tb, 16 * j);
+                sDA.a_km(fa, 16 * tb, 16 * j);
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const int i = 2 * lane + x;
-            float cs = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) cs += colsum[j * 64 + i];
-            suf[x] = (rowsum[i] + rowsum[64 + i] - cs) + (dots[i] + dots[192 + i]) + (dots[64 + i] + dots[256 + i]);
-            pre[x] = dots[128 + i] + dots[320 + i];
+                for (int d = 0; d < HT / 2; ++d) {
+                    sK.b_kn(b0, b1, 16 * j, col0 + 16 * d);
+                    mma16(dkr[2 * d], fa, b0);
+                    mma16(dkr[2 * d + 1], fa, b1);
+                    sQ.b_kn(b0, b1, 16 * j, col0 + 16 * d);
+                    mma16(dkr[2 * d], fp, b0);
+                    mma16(dkr[2 * d + 1], fp, b1);
+                }
+            }
         }
+        if (w == 0) {
+            // dg: the suffix sums of `suf`, the prefix sums (before t) of `pre`, and the chunk's own decay
+            float suf[2], pre[2], ds = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ds += blocks[i];
-        float s = suf[0] + suf[1], p = pre[0] + pre[1];
+            for (int x = 0; x < 2; ++x) {
+                const int r = 2 * lane + x;
+                float cs = 0.0f, up = 0.0f, dn = 0.0f;
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const float s2 = __shfl_down_sync(0xffffffffu, s, d), p2 = __shfl_up_sync(0xffffffffu, p, d);
-            if (lane + d < 32) s += s2;
-            if (lane >= d) p += p2;
+                for (int j = 0; j < 8; ++j) cs += colsum[j * 64 + r];
+#pragma unroll
+                for (int j = 0; j < NG; ++j) {
+                    up += rowsum[j * 64 + r] + (dots[j * 192 + r] + dots[j * 192 + 64 + r]);
+                    dn += dots[j * 192 + 128 + r];
+                }
+                suf[x] = up - cs;
+                pre[x] = dn;
+            }
+#pragma unroll
+            for (int j = 0; j < SM::warps; ++j) ds += blocks[j];
+            float sfx = suf[0] + suf[1], p = pre[0] + pre[1];
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const float s2 = __shfl_down_sync(0xffffffffu, sfx, d), p2 = __shfl_up_sync(0xffffffffu, p, d);
+                if (lane + d < 32) sfx += s2;
+                if (lane >= d) p += p2;
+            }
+            p -= pre[0] + pre[1];  // before this lane's tokens
+            const float tail = G.last * ds;
+            T *dgp = (T*)a.dg + tok * a.Hv + h, *dbp = (T*)a.dbeta + tok * a.Hv + h;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int r = 2 * lane + x;
+                if (r >= n) continue;
+                dgp[(long long)r * a.Hv] = io<T>::to((x ? sfx - suf[0] : sfx) + (x ? p + pre[0] : p) + tail);
+                dbp[(long long)r * a.Hv] = io<T>::to(dbeta[r]);
+            }
         }
-        p -= pre[0] + pre[1];  // before this lane's tokens
-        const float tail = G.last * ds;
-        T *dgp = (T*)a.dg + tok * a.Hv + h, *dbp = (T*)a.dbeta + tok * a.Hv + h;
+        // out: to the sums of the head's group, or (the last of it) to dq and dk
+        const bool part = !SM::totals && share > 1, done = i + 1 == steps;
+        const bool pairs = a.Dk % 2 == 0 && ((reinterpret_cast<uintptr_t>(a.dq) | reinterpret_cast<uintptr_t>(a.dk)) % (2 * sizeof(T))) == 0;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const int i = 2 * lane + x;
-            if (i >= n) continue;
-            dgp[(long long)i * a.Hv] = io<T>::to((x ? s - suf[0] : s) + (x ? p + pre[0] : p) + tail);
-            dbp[(long long)i * a.Hv] = io<T>::to(dbeta[i]);
+        for (int hh = 0; hh < 2; ++hh) {
+            const int r = 16 * tb + g + 8 * hh;
+#pragma unroll
+            for (int j = 0; j < HT; ++j) {
+                const int cc = col0 + 8 * j + 2 * t;
+                float2 vq = make_float2(dq[j][2 * hh], dq[j][2 * hh + 1]), vk = make_float2(dkr[j][2 * hh], dkr[j][2 * hh + 1]);
+                if (SM::totals && share > 1) {
+                    float2 *tq = reinterpret_cast<float2*>(tot + r * DK + cc), *tk = reinterpret_cast<float2*>(tot + (64 + r) * DK + cc);
+                    if (i >= vslices) {  // (this thread's own places)
+                        vq.x += tq->x, vq.y += tq->y, vk.x += tk->x, vk.y += tk->y;
+                    }
+                    if (!done) {
+                        *tq = vq, *tk = vk;
+                        continue;
+                    }
+                }
+                if (r >= n || cc >= a.Dk) continue;
+                if (part) {
+                    float* row = c.part + ((tok + r) * a.Hv + h) * 2 * a.Dk + cc;
+                    row[0] = vq.x, row[a.Dk] = vk.x;
+                    if (cc + 1 < a.Dk) row[1] = vq.y, row[a.Dk + 1] = vk.y;
+                    continue;
+                }
+                T *pq = (T*)a.dq + ((tok + r) * a.Hk + hk) * a.Dk + cc, *pk = (T*)a.dk + ((tok + r) * a.Hk + hk) * a.Dk + cc;
+                if (pairs) {
+                    if constexpr (sizeof(T) == 2) {
+                        *reinterpret_cast<uint32_t*>(pq) = pack_bf16(vq.x, vq.y);
+                        *reinterpret_cast<uint32_t*>(pk) = pack_bf16(vk.x, vk.y);
+                    } else {
+                        *reinterpret_cast<float2*>(pq) = vq;
+                        *reinterpret_cast<float2*>(pk) = vk;
+                    }
+                } else {
+                    pq[0] = io<T>::to(vq.x), pk[0] = io<T>::to(vk.x);
+                    if (cc + 1 < a.Dk) pq[1] = io<T>::to(vq.y), pk[1] = io<T>::to(vk.y);
+                }
+            }
+        }
+        if (!done) {
+            __syncthreads();  // dP, dA and the sums have been read
+            if (!SM::ahead) load(i + 1);
         }
     }
 }
 
 template <typename T, int DK>
 vmb_status launch_grad_dk(const DeltaGrad& c, cudaStream_t stream) {
+    using SM = GradSmem<T, DK>;
     const void* fn = (const void*)delta_grad_kernel<T, DK>;
-    const long long grid = (long long)c.a.B * c.a.Hv * ((c.a.T + kChunk - 1) / kChunk);
-    const size_t smem = GradSmem<T, DK>::total;
-    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return VMB_ERR_CUDA;
+    const long long grid = (long long)c.a.B * (SM::totals ? c.a.Hk : c.a.Hv) * ((c.a.T + kChunk - 1) / kChunk);
+    if (!allow_smem(fn, SM::total)) return VMB_ERR_CUDA;
     DeltaGrad arg = c;
     void* args[] = {&arg};
-    return launch_kernel(fn, dim3((unsigned)grid), dim3(kGradThreads), smem, args, stream) == cudaSuccess ? VMB_OK : VMB_ERR_CUDA;
+    return launch_kernel(fn, dim3((unsigned)grid), dim3(SM::threads), SM::total, args, stream) == cudaSuccess ? VMB_OK : VMB_ERR_CUDA;
+}
+
+// Whether the value heads of a key head leave their dq and dk to be summed by delta_share_kernel.
+inline bool grad_leaves_parts(const DeltaArgs& a) {
+    if (a.Hv == a.Hk) return false;
+    if (a.dtype == VMB_BF16) return a.Dk <= 64 ? !GradSmem<__nv_bfloat16, 64>::totals : !GradSmem<__nv_bfloat16, 128>::totals;
+    return a.Dk <= 64 ? !GradSmem<float, 64>::totals : !GradSmem<float, 128>::totals;
 }
 
 template <typename T>

@@ -78,6 +78,9 @@ struct DeltaStep {
     vmb_dtype dtype;
 };
 
+// Allow a kernel `bytes` of dynamic shared memory (always the same for one kernel) on the current device.
+bool allow_smem(const void* fn, int bytes);
+
 vmb_status launch_delta_fwd(const DeltaArgs& a, cudaStream_t stream);
 vmb_status launch_delta_bwd(const DeltaArgs& a, cudaStream_t stream);
 vmb_status launch_delta_step(const DeltaStep& a, cudaStream_t stream);

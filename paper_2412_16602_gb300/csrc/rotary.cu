@@ -18,7 +18,7 @@ namespace {
 
 constexpr int kRotThreads = 256;
 
-template <typename T, int V> struct alignas(sizeof(T) * V) Pack { T v[V]; };
+template <typename T, int V, bool kLoose> struct alignas(kLoose ? sizeof(T) : sizeof(T) * V) Pack { T v[V]; };
 
 // cos and sin of p f
 __device__ __forceinline__ float2 turn(int p, float f) {
@@ -37,46 +37,70 @@ __device__ __forceinline__ float2 turned(float u, float v, float2 w) {
     return make_float2(fmaf(u, w.x, -__fmul_rn(v, w.y)), fmaf(v, w.x, __fmul_rn(u, w.y)));
 }
 
-// Items of a head: the vectors of V pairs (half: V channels from each half; interleaved: 2 V channels), then the
-// vectors of V channels that stay as they are.
-template <typename T, int V, bool kInter>
+// A head's items: half: vectors of V pairs (V channels from each half); interleaved: vectors of V channels (V / 2 pairs);
+// then the vectors of V channels that stay as they are (kLoose, for pairs in rows of no alignment: single channels).
+// A thread keeps its items of a token and goes from token to
+// token, so that nothing is divided in the loop; four tokens' values are read before the first is written.
+template <typename T, int V, bool kInter, bool kLoose>
 __device__ __forceinline__ void rotate_heads(const T* src, T* dst, const float2* table, int tokens, long long src_t, int H, int D, int P) {
-    const int turns = P / V, items = turns + (D - 2 * P) / V, per = H * items, n = tokens * per;
-#pragma unroll 2
-    for (int i = threadIdx.x; i < n; i += kRotThreads) {
-        const int tok = i / per, rest = i - tok * per, h = rest / items, j = rest - h * items;
-        const T* s = src + tok * src_t + (long long)h * D;
-        T* d = dst + ((long long)tok * H + h) * D;
-        if (j >= turns) {
-            const int c = 2 * P + (j - turns) * V;
-            *reinterpret_cast<Pack<T, V>*>(d + c) = *reinterpret_cast<const Pack<T, V>*>(s + c);
-            continue;
-        }
-        const float2* cs = table + tok * P + j * V;
-        const int c0 = kInter ? 2 * j * V : j * V, c1 = kInter ? c0 + V : P + j * V;
-        const Pack<T, V> a = *reinterpret_cast<const Pack<T, V>*>(s + c0), b = *reinterpret_cast<const Pack<T, V>*>(s + c1);
-        Pack<T, V> oa, ob;
+    constexpr int U = 4;
+    const int turns = kInter ? 2 * P / V : P / V, items = turns + (D - 2 * P) / (kLoose ? 1 : V), per = H * items;
+    const int lanes = per < kRotThreads ? kRotThreads / per : 1;
+    const long long dst_t = (long long)H * D;
+    for (int e0 = threadIdx.x; e0 < per * lanes; e0 += kRotThreads) {
+        const int first = lanes > 1 ? e0 / per : 0, e = lanes > 1 ? e0 - first * per : e0, h = e / items, j = e - h * items;
+        const bool two = !kInter && j < turns;
+        const long long at = (long long)h * D + (j >= turns ? 2 * P + (j - turns) * (kLoose ? 1 : V) : j * V);
+        const T *s0 = src + at, *s1 = s0 + P;
+        T *d0 = dst + at, *d1 = d0 + P;
+        const float2* cs = table + j * (kInter ? V / 2 : V);
+        for (int t0 = first; t0 < tokens; t0 += U * lanes) {
+            Pack<T, V, kLoose> a[U], b[U];
 #pragma unroll
-        for (int x = 0; x < V; ++x) {
-            const float2 w = cs[x];
-            if (kInter) {
-                const T xe = 2 * x < V ? a.v[(2 * x) % V] : b.v[(2 * x) % V], ye = 2 * x + 1 < V ? a.v[(2 * x + 1) % V] : b.v[(2 * x + 1) % V];
-                const float2 o = turned(io<T>::cvt(xe), io<T>::cvt(ye), w);
-                const T ru = io<T>::to(o.x), rv = io<T>::to(o.y);
-                if (2 * x < V) oa.v[(2 * x) % V] = ru; else ob.v[(2 * x) % V] = ru;
-                if (2 * x + 1 < V) oa.v[(2 * x + 1) % V] = rv; else ob.v[(2 * x + 1) % V] = rv;
-            } else {
-                const float2 o = turned(io<T>::cvt(a.v[x]), io<T>::cvt(b.v[x]), w);
-                oa.v[x] = io<T>::to(o.x);
-                ob.v[x] = io<T>::to(o.y);
+            for (int u = 0; u < U; ++u) {
+                const int t = t0 + u * lanes;
+                if (t >= tokens) break;
+                if (kLoose && j >= turns) {
+                    a[u].v[0] = s0[t * src_t];
+                    continue;
+                }
+                a[u] = *reinterpret_cast<const Pack<T, V, kLoose>*>(s0 + t * src_t);
+                if (two) b[u] = *reinterpret_cast<const Pack<T, V, kLoose>*>(s1 + t * src_t);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int t = t0 + u * lanes;
+                if (t >= tokens) break;
+                if (kLoose && j >= turns) {
+                    d0[t * dst_t] = a[u].v[0];
+                    continue;
+                }
+                if (j < turns) {
+                    const float2* w = cs + t * P;
+                    if constexpr (kInter) {
+#pragma unroll
+                        for (int x = 0; x < V / 2; ++x) {
+                            const float2 o = turned(io<T>::cvt(a[u].v[2 * x]), io<T>::cvt(a[u].v[2 * x + 1]), w[x]);
+                            a[u].v[2 * x] = io<T>::to(o.x);
+                            a[u].v[2 * x + 1] = io<T>::to(o.y);
+                        }
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < V; ++x) {
+                            const float2 o = turned(io<T>::cvt(a[u].v[x]), io<T>::cvt(b[u].v[x]), w[x]);
+                            a[u].v[x] = io<T>::to(o.x);
+                            b[u].v[x] = io<T>::to(o.y);
+                        }
+                        *reinterpret_cast<Pack<T, V, kLoose>*>(d1 + t * dst_t) = b[u];
+                    }
+                }
+                *reinterpret_cast<Pack<T, V, kLoose>*>(d0 + t * dst_t) = a[u];
             }
         }
-        *reinterpret_cast<Pack<T, V>*>(d + c0) = oa;
-        *reinterpret_cast<Pack<T, V>*>(d + c1) = ob;
     }
 }
 
-template <typename T, int V, bool kInter>
+template <typename T, int V, bool kInter, bool kLoose>
 __global__ void __launch_bounds__(kRotThreads) rotary_kernel(RotaryArgs a, int per_block, int blocks_per_row) {
     extern __shared__ float2 table[];
     const int P = a.pair_end[a.axes - 1];
@@ -100,19 +124,19 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(RotaryArgs a, int p
         table[i] = make_float2(cs.x, a.inverse ? -cs.y : cs.y);
     }
     __syncthreads();
-    rotate_heads<T, V, kInter>((const T*)a.q + b * a.q_b + t0 * a.q_t, (T*)a.q_out + ((long long)b * a.T + t0) * a.Hq * a.D, table, n, a.q_t,
+    rotate_heads<T, V, kInter, kLoose>((const T*)a.q + b * a.q_b + t0 * a.q_t, (T*)a.q_out + ((long long)b * a.T + t0) * a.Hq * a.D, table, n, a.q_t,
                                a.Hq, a.D, P);
     if (a.k)
-        rotate_heads<T, V, kInter>((const T*)a.k + b * a.k_b + t0 * a.k_t, (T*)a.k_out + ((long long)b * a.T + t0) * a.Hk * a.D, table, n,
+        rotate_heads<T, V, kInter, kLoose>((const T*)a.k + b * a.k_b + t0 * a.k_t, (T*)a.k_out + ((long long)b * a.T + t0) * a.Hk * a.D, table, n,
                                    a.k_t, a.Hk, a.D, P);
 }
 
-template <typename T, int V>
+template <typename T, int V, bool kLoose = false>
 vmb_status launch_v(const RotaryArgs& a, cudaStream_t stream) {
     const int P = a.pair_end[a.axes - 1];
-    // tokens per block: about four vectors per thread, within 32 KB of sines, and enough blocks for every SM
-    const long long per_token = (long long)(a.Hq + a.Hk) * (P / V + (a.D - 2 * P) / V);
-    long long per = (4 * kRotThreads + per_token - 1) / per_token;
+    // tokens per block: about eight vectors per thread, within 32 KB of sines, and enough blocks for every SM
+    const long long per_token = (long long)(a.Hq + a.Hk) * ((a.interleaved ? 2 * P / V : P / V) + (a.D - 2 * P) / V);
+    long long per = (8 * kRotThreads + per_token - 1) / per_token;
     const long long most = 32 * 1024 / (8 * (long long)P), spread = ((long long)a.B * a.T + 2 * device_sm_count() - 1) / (2 * device_sm_count());
     per = per < most ? per : most;
     per = per < spread ? per : spread;
@@ -120,7 +144,13 @@ vmb_status launch_v(const RotaryArgs& a, cudaStream_t stream) {
     if (per > a.T) per = a.T;
     int per_block = (int)per, blocks = (int)((a.T + per - 1) / per);
     if ((long long)blocks * a.B > 2147483647LL) return VMB_ERR_UNSUPPORTED;
-    const void* fn = a.interleaved ? (const void*)rotary_kernel<T, V, true> : (const void*)rotary_kernel<T, V, false>;
+    const void* fn;
+    if constexpr (V == 1)
+        fn = (const void*)rotary_kernel<T, V, false, false>;
+    else if constexpr (kLoose)
+        fn = (const void*)rotary_kernel<T, V, true, true>;
+    else
+        fn = a.interleaved ? (const void*)rotary_kernel<T, V, true, false> : (const void*)rotary_kernel<T, V, false, false>;
     RotaryArgs arg = a;
     void* args[] = {&arg, &per_block, &blocks};
     return launch_kernel(fn, dim3((unsigned)(blocks * (long long)a.B)), dim3(kRotThreads), (size_t)per_block * P * 8, args, stream) == cudaSuccess
@@ -129,16 +159,18 @@ vmb_status launch_v(const RotaryArgs& a, cudaStream_t stream) {
 
 }  // namespace
 
-// The widest vectors (up to 16 bytes) that divide the halves of the turned channels, the others, the rows and
-// the addresses.
+// The widest vectors (up to 16 bytes) that divide the turned channels (each half of them, unless pairs are
+// neighbours), the rows and the addresses.
 vmb_status launch_rotary(const RotaryArgs& a, cudaStream_t stream) {
     const int P = a.pair_end[a.axes - 1];
     const unsigned es = a.dtype == VMB_BF16 ? 2 : 4;
     const unsigned long long bytes = (reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.q_out) | reinterpret_cast<uintptr_t>(a.k) |
                                       reinterpret_cast<uintptr_t>(a.k_out)) |
-                                     (unsigned long long)es * ((unsigned long long)P | (unsigned)a.D | (unsigned long long)a.q_b |
+                                     (unsigned long long)es * ((unsigned long long)(a.interleaved ? 2 * P : P) | (unsigned)a.D | (unsigned long long)a.q_b |
                                                               (unsigned long long)a.q_t | (unsigned long long)(a.k ? a.k_b | a.k_t : 0));
     const unsigned v = (bytes % 16 == 0 ? 16 : bytes % 8 == 0 ? 8 : bytes % 4 == 0 ? 4 : 2) / es;
+    if (a.interleaved && v == 1)  // rows of no alignment: pairs of single loads
+        return a.dtype == VMB_BF16 ? launch_v<__nv_bfloat16, 2, true>(a, stream) : launch_v<float, 2, true>(a, stream);
     if (a.dtype == VMB_BF16)
         return v == 8 ? launch_v<__nv_bfloat16, 8>(a, stream) : v == 4 ? launch_v<__nv_bfloat16, 4>(a, stream)
              : v == 2 ? launch_v<__nv_bfloat16, 2>(a, stream) : launch_v<__nv_bfloat16, 1>(a, stream);

@@ -9,6 +9,7 @@ fallback, and a missing library raises at import.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import threading
 
@@ -706,6 +707,24 @@ _delta_ws = Workspace()
 _norm_ws = Workspace()
 
 
+# (a step of one token takes 2.5 us on the device: the marshalling below keeps to what it needs)
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _stream_of(t: torch.Tensor, stream) -> int:
+    return _raw_stream(t.device.index) if stream is None else stream.cuda_stream
+
+
+@functools.lru_cache(maxsize=4096)
+def _delta_bytes(device, *sizes) -> int:
+    return lib.vmb_delta_rule_workspace_bytes(*sizes)
+
+
+@functools.lru_cache(maxsize=4096)
+def _norm_bytes(device, *sizes) -> int:
+    return lib.vmb_group_norm_workspace_bytes(*sizes)
+
+
 def delta_workspace(device=None) -> torch.Tensor:
     """The default workspace of the delta rule's calls (for vmb_read_status)."""
     dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
@@ -726,23 +745,28 @@ def _heads(t: torch.Tensor, name: str):
 
 def _delta_inputs(q, k, v, g, beta):
     """Checked sizes (B, T, Hk, Hv, Dk, Dv), dtype code and strides (None: dense) of the delta rule's inputs."""
-    code = _dtype_code(q.dtype)
-    if k.dtype != q.dtype or v.dtype != q.dtype or g.dtype != q.dtype or beta.dtype != q.dtype:
+    dt = q.dtype
+    code = _dtype_code(dt)
+    if k.dtype != dt or v.dtype != dt or g.dtype != dt or beta.dtype != dt:
         raise ValueError("q, k, v, g, beta must share one dtype")
-    if q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and q.dim() == 4 and v.dim() == 4:
+    if not (q.is_cuda and k.is_cuda and v.is_cuda and g.is_cuda and beta.is_cuda):
+        raise ValueError("q, k, v, g, beta must be CUDA tensors")
+    if q.dim() != 4 or v.dim() != 4 or k.shape != q.shape:
+        raise ValueError("q, k [B, T, Hk, Dk] and v [B, T, Hv, Dv] expected")
+    if q.is_contiguous() and k.is_contiguous() and v.is_contiguous():
         strides = None
-        _dev(q, "q"), _dev(k, "k"), _dev(v, "v")
     else:
         strides = (ctypes.c_int64 * 6)(*_heads(q, "q"), *_heads(k, "k"), *_heads(v, "v"))
     B, T, Hk, Dk = q.shape
-    Hv, Dv = v.shape[2:]
-    if k.shape != q.shape or v.shape[0] != B or v.shape[1] != T:
+    vB, vT, Hv, Dv = v.shape
+    if vB != B or vT != T:
         raise ValueError("q, k [B, T, Hk, Dk] and v [B, T, Hv, Dv] expected")
     if Hk < 1 or Hv % Hk:
         raise ValueError("the value heads must be a multiple of the key heads")
-    if g.shape != (B, T, Hv) or beta.shape != (B, T, Hv):
+    if g.shape != (B, T, Hv) or beta.shape != g.shape:
         raise ValueError("g and beta must be [B, T, Hv]")
-    _dev(g, "g"), _dev(beta, "beta")
+    if not (g.is_contiguous() and beta.is_contiguous()):
+        raise ValueError("g and beta must be contiguous")
     return B, T, Hk, Hv, Dk, Dv, code, strides
 
 
@@ -792,7 +816,7 @@ def vmb_delta_rule_fwd(q, k, v, g, beta, *, initial_state=None, offsets=None, ma
         final_state = torch.empty(shape, dtype=torch.float32, device=q.device)
     _state(final_state, "final_state", shape)
     if o is None:
-        o = torch.empty((B, T, Hv, Dv), dtype=q.dtype, device=q.device)
+        o = torch.empty_like(v) if strides is None else v.new_empty((B, T, Hv, Dv))
     else:
         _dev(o, "o")
         if o.shape != (B, T, Hv, Dv) or o.dtype != q.dtype:
@@ -803,12 +827,12 @@ def vmb_delta_rule_fwd(q, k, v, g, beta, *, initial_state=None, offsets=None, ma
     elif saved is not None:
         _saved_bytes(saved, N, longest, total, offsets, Hv, Dk, Dv, code)
     if workspace is None:
-        n = lib.vmb_delta_rule_workspace_bytes(N, longest, total, offsets is not None, Hk, Hv, Dk, Dv, 0, code)
-        workspace = _delta_ws.get(n, q.device)
+        dev = q.device
+        workspace = _delta_ws.get(_delta_bytes(dev.index, N, longest, total, offsets is not None, Hk, Hv, Dk, Dv, 0, code), dev)
     _check(lib.vmb_delta_rule_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), strides,
                                   _ptr(initial_state), _ptr(offsets), o.data_ptr(), _ptr(final_state), _ptr(saved), N,
                                   longest, total, Hk, Hv, Dk, Dv, Dk ** -0.5 if scale is None else scale, code,
-                                  workspace.data_ptr(), workspace.numel(), _stream(stream)), "vmb_delta_rule_fwd")
+                                  workspace.data_ptr(), workspace.numel(), _stream_of(q, stream)), "vmb_delta_rule_fwd")
     return o, final_state, saved
 
 
@@ -837,14 +861,13 @@ def vmb_delta_rule_bwd(q, k, v, g, beta, do, saved, *, dfinal_state=None, offset
     if want_initial:
         out["initial_state"] = torch.empty(shape, dtype=torch.float32, device=dev)
     if workspace is None:
-        n = lib.vmb_delta_rule_workspace_bytes(N, longest, total, offsets is not None, Hk, Hv, Dk, Dv, 1, code)
-        workspace = _delta_ws.get(n, dev)
+        workspace = _delta_ws.get(_delta_bytes(dev.index, N, longest, total, offsets is not None, Hk, Hv, Dk, Dv, 1, code), dev)
     _check(lib.vmb_delta_rule_bwd(q.data_ptr(), k.data_ptr(), g.data_ptr(), beta.data_ptr(), strides, _ptr(offsets),
                                   do.data_ptr(), _ptr(dfinal_state), saved.data_ptr(), out["q"].data_ptr(),
                                   out["k"].data_ptr(), out["v"].data_ptr(), out["g"].data_ptr(), out["beta"].data_ptr(),
                                   _ptr(out.get("initial_state")), N, longest, total, Hk, Hv, Dk, Dv,
                                   Dk ** -0.5 if scale is None else scale, code, workspace.data_ptr(), workspace.numel(),
-                                  _stream(stream)), "vmb_delta_rule_bwd")
+                                  _stream_of(q, stream)), "vmb_delta_rule_bwd")
     return out
 
 
@@ -862,15 +885,29 @@ def vmb_delta_rule_step(q, k, v, g, beta, state, *, slots=None, scale=None, o=No
         if slots.shape != (B,) or slots.dtype != torch.int32:
             raise ValueError("slots must be int32 [B]")
     if o is None:
-        o = torch.empty((B, T, Hv, Dv), dtype=q.dtype, device=q.device)
+        o = torch.empty_like(v) if strides is None else v.new_empty((B, T, Hv, Dv))
     else:
         _dev(o, "o")
         if o.shape != (B, T, Hv, Dv) or o.dtype != q.dtype:
             raise ValueError("o must be [B, T, Hv, Dv] in the dtype of q")
     _check(lib.vmb_delta_rule_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), strides,
                                    state.data_ptr(), _ptr(slots), o.data_ptr(), B, T, Hk, Hv, Dk, Dv, pool,
-                                   Dk ** -0.5 if scale is None else scale, code, _stream(stream)), "vmb_delta_rule_step")
+                                   Dk ** -0.5 if scale is None else scale, code, _stream_of(q, stream)), "vmb_delta_rule_step")
     return o
+
+
+@functools.lru_cache(maxsize=256)
+def _ints(values):
+    return (ctypes.c_int * len(values))(*values)
+
+
+def _rotary_out(x, out, name, dense):
+    if out is None:
+        return torch.empty_like(x) if dense else x.new_empty(x.shape)
+    _dev(out, name)
+    if out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError(f"{name} must have the shape and dtype of its input")
+    return out
 
 
 def vmb_rotary_fwd(q, k, freq, positions=None, *, sections, grid=None, interleaved: bool = False,
@@ -906,20 +943,14 @@ def vmb_rotary_fwd(q, k, freq, positions=None, *, sections, grid=None, interleav
     else:
         if grid is None or len(grid) != axes:
             raise ValueError("positions, or a grid with one size for each axis, is needed")
-        cells = (ctypes.c_int * axes)(*grid)
-    if q_out is None:
-        q_out = torch.empty((B, T, Hq, D), dtype=q.dtype, device=q.device)
-    if k is not None and k_out is None:
-        k_out = torch.empty((B, T, Hk, D), dtype=q.dtype, device=q.device)
-    for out, n, h in ((q_out, "q_out", Hq), (k_out, "k_out", Hk)):
-        if out is not None:
-            _dev(out, n)
-            if out.shape != (B, T, h, D) or out.dtype != q.dtype:
-                raise ValueError(f"{n} must be [B, T, {h}, D] in the dtype of q")
+        cells = _ints(tuple(grid))
+    q_out = _rotary_out(q, q_out, "q_out", strides is None)
+    if k is not None:
+        k_out = _rotary_out(k, k_out, "k_out", strides is None)
     flags = (VMB_ROTARY_INTERLEAVED if interleaved else 0) | (VMB_ROTARY_INVERSE if inverse else 0)
     _check(lib.vmb_rotary_fwd(q.data_ptr(), _ptr(k), freq.data_ptr(), _ptr(positions), q_out.data_ptr(), _ptr(k_out), B,
-                              T, Hq, Hk, D, axes, (ctypes.c_int * axes)(*sections), cells, strides, flags, code,
-                              _stream(stream)), "vmb_rotary_fwd")
+                              T, Hq, Hk, D, axes, _ints(tuple(sections)), cells, strides, flags, code,
+                              _stream_of(q, stream)), "vmb_rotary_fwd")
     return q_out, k_out
 
 
@@ -961,9 +992,9 @@ def vmb_group_norm_fwd(x, weight, bias, groups: int, *, eps: float = 1e-5, act: 
         stats = torch.empty((B, groups, 2), dtype=torch.float32, device=x.device)
     _state(stats, "stats", (B, groups, 2))
     if workspace is None:
-        workspace = _norm_ws.get(lib.vmb_group_norm_workspace_bytes(B, L, C, groups, 0, code), x.device)
+        workspace = _norm_ws.get(_norm_bytes(x.device.index, B, L, C, groups, 0, code), x.device)
     _check(lib.vmb_group_norm_fwd(x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(stats), B, L, C, groups, eps,
-                                  a, code, workspace.data_ptr(), workspace.numel(), _stream(stream)), "vmb_group_norm_fwd")
+                                  a, code, workspace.data_ptr(), workspace.numel(), _stream_of(x, stream)), "vmb_group_norm_fwd")
     return y, stats
 
 
@@ -980,10 +1011,10 @@ def vmb_group_norm_bwd(x, weight, bias, stats, dy, groups: int, *, act: str = "n
     new = torch.empty_like if x.numel() else torch.zeros_like  # (an empty problem launches nothing: sums of nothing)
     out = dict(x=torch.empty_like(x), weight=None if weight is None else new(weight), bias=None if bias is None else new(bias))
     if workspace is None:
-        workspace = _norm_ws.get(lib.vmb_group_norm_workspace_bytes(B, L, C, groups, 1, code), x.device)
+        workspace = _norm_ws.get(_norm_bytes(x.device.index, B, L, C, groups, 1, code), x.device)
     _check(lib.vmb_group_norm_bwd(x.data_ptr(), _ptr(weight), _ptr(bias), stats.data_ptr(), dy.data_ptr(),
                                   out["x"].data_ptr(), _ptr(out["weight"]), _ptr(out["bias"]), B, L, C, groups, a, code,
-                                  workspace.data_ptr(), workspace.numel(), _stream(stream)), "vmb_group_norm_bwd")
+                                  workspace.data_ptr(), workspace.numel(), _stream_of(x, stream)), "vmb_group_norm_bwd")
     return out
 
 
