@@ -4,13 +4,18 @@
 //   dz = dy act'(w n + b);  dweight = sum dz n, dbias = sum dz (over batch and pixels);
 //   dx = rstd (w dz - mean(w dz) - n mean(w dz n)), the means over the group.
 //
-// Two passes each way, both in the same tiles (a run of pixels of one sample, all channels): the first leaves a
-// tile's sums per channel, and the last tile of a sample to finish joins them; the second applies them.  What
-// bounds both is memory: x (and dy) read, y (dx) written.  The second pass finds x in the L2 cache, because a
-// launch covers only as many samples as its share of the cache holds.
+// What bounds both is memory: x (and dy) read, y (dx) written, once each where the pixels of a few groups fit the
+// shared memory of a cluster of CTAs: every CTA holds a run of pixels, the cluster exchanges its sums through
+// distributed shared memory, and the results are formed from the tile (norm_cluster_kernel, norm_cluster_grad_kernel).
+// Larger samples take two passes over the same tiles (a run of pixels of one sample, all channels): the first leaves a
+// tile's sums per channel, and the last tile of a sample to finish joins them; the second applies them.  It finds x in
+// the L2 cache, because a launch covers only as many samples as its share of the cache holds.
 //
-// Variances are formed from sums of differences to the tile's first pixel and joined as (mean, M2) pairs
+// Variances are formed from sums of differences to a tile's first pixel and joined as (mean, M2) pairs
 // (Chan, Golub & LeVeque 1979), so a mean far from zero costs no digits.  All sums are fp32 in a fixed order.
+#include <cooperative_groups.h>
+
+#include "delta_internal.h"
 #include "mixer_internal.h"
 #include "vmb_common.cuh"
 #include "vmb_internal.h"
@@ -292,7 +297,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_sums_kernel(NormLaunch c) {
     float2* chan = reinterpret_cast<float2*>((char*)a.ws + c.p.chan) + (long long)b * C;
     for (int k = tid; k < C; k += kNormThreads) {
         float t1 = 0.0f, t2 = 0.0f;
-#pragma unroll 4
+#pragma unroll 16
         for (int i = 0; i < c.p.tiles; ++i) {
             const float2 v = __ldcg(&part[(long long)i * C + k]);
             t1 += v.x;
@@ -319,7 +324,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_sums_kernel(NormLaunch c) {
     const float2* all = reinterpret_cast<const float2*>((const char*)a.ws + c.p.chan);
     for (int k = tid; k < C; k += kNormThreads) {
         float t1 = 0.0f, t2 = 0.0f;
-#pragma unroll 4
+#pragma unroll 16
         for (int i = 0; i < a.B; ++i) {
             const float2 v = __ldcg(&all[(long long)i * C + k]);
             t1 += v.x;
@@ -374,10 +379,335 @@ __global__ void __launch_bounds__(kNormThreads) norm_dx_kernel(NormLaunch c) {
     }
 }
 
+// ------------------------------------------------------------------ samples that fit a cluster
+
+// A slab: the pixels of one sample and `width` neighbouring channels (whole groups), cut into `ctas` runs of `rows`
+// pixels, one per CTA of a cluster.
+struct NormSlab {
+    int width, slabs, ctas, rows;
+};
+// Two CTAs per SM, so that one loads or stores while the other computes; a cluster of eight is the portable limit.
+constexpr size_t kSlabSmem = 113 * 1024;
+constexpr int kSlabThreads = 256;
+// The tile, a vector of sums per thread, two sums per channel and one pair per group.
+inline size_t slab_smem(long long rows, int width, int groups, size_t es, bool grads) {
+    return (((size_t)rows * width * es * (grads ? 2 : 1) + 15) & ~(size_t)15) + kSlabThreads * (16 / es) * 4 + (size_t)width * 8 + (size_t)groups * 8;
+}
+
+// Channels per slab: as many groups as a cluster holds, at least 32 bytes of every pixel (a sector of memory), fewer as
+// long as that gives every SM two CTAs and a pixel still 64 bytes; then CTAs per slab likewise, of 16 pixels or more.
+bool norm_slab(int B, long long L, int C, int G, vmb_dtype dtype, bool grads, int sms, NormSlab* out) {
+    const size_t es = dtype == VMB_BF16 ? 2 : 4;
+    const int m = C / G, v = (int)(16 / es);
+    if (C % v || L > 1 << 24) return false;
+    int best = 0;
+    for (int g = 1; g <= G; ++g) {
+        if (G % g || (g * m) % v || g * m / v > kSlabThreads || g * m > 2048) continue;
+        if (slab_smem((L + 7) / 8, g * m, g, es, grads) > kSlabSmem) break;
+        const long long ctas = (long long)B * (G / g) * 8;
+        if (best && (size_t)best * es >= 64 && ctas < 2LL * sms) break;
+        best = g * m;
+    }
+    if (!best || (size_t)best * es < 32) return false;
+    out->width = best;
+    out->slabs = C / best;
+    int n = 1;
+    while (n < 8 && (slab_smem((L + n - 1) / n, best, best / m, es, grads) > kSlabSmem ||
+                     ((long long)B * out->slabs * n < 2LL * sms && L / (2 * n) >= 16)))
+        n *= 2;
+    out->ctas = n;
+    out->rows = (int)((L + n - 1) / n);
+    return true;
+}
+
+struct SlabLaunch {
+    NormArgs a;
+    NormSlab s;
+    float2* chan;        // gradients: [B][C] sums of a sample
+    unsigned* counter;
+};
+
+// Per-channel values of a thread (one vector of V channels) summed over the threads of its column, in order, and handed
+// to `put(channel, sum)`.
+template <int V, typename Put>
+__device__ __forceinline__ void column_sums(const float (&v)[V], float* scratch, int width, int cols, int lanes, Put put) {
+    const int tid = threadIdx.x;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < V; ++i) scratch[tid * V + i] = v[i];
+    __syncthreads();
+    for (int ch = tid; ch < width; ch += kSlabThreads) {
+        float s = 0.0f;
+        for (int l = 0; l < lanes; ++l) s += scratch[(l * cols) * V + ch];
+        put(ch, s);
+    }
+}
+
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_kernel(SlabLaunch c) {
+    namespace cg = cooperative_groups;
+    extern __shared__ __align__(16) unsigned char shm[];
+    const NormArgs& a = c.a;
+    const cg::cluster_group cl = cg::this_cluster();
+    const int ctas = c.s.ctas, rank = (int)cl.block_rank(), width = c.s.width, tid = threadIdx.x;
+    const int m = a.C / a.G, groups = width / m, cols = width / V, lanes = kSlabThreads / cols;
+    T* tile = reinterpret_cast<T*>(shm);
+    float* scratch = reinterpret_cast<float*>(shm + (((size_t)c.s.rows * width * sizeof(T) + 15) & ~(size_t)15));
+    float *sum1 = scratch + kSlabThreads * V, *sum2 = sum1 + width;  // per channel
+    float2* stat = reinterpret_cast<float2*>(sum2 + width);          // per group: read by the cluster
+    pdl_launch_dependents();
+    pdl_wait();
+    const long long slab = blockIdx.x / ctas;
+    const int b = (int)(slab / c.s.slabs), ch0 = (int)(slab % c.s.slabs) * width;
+    const long long r0 = (long long)rank * c.s.rows;
+    const int rows = (int)max(0LL, min((long long)c.s.rows, a.L - r0));
+    const T* x = (const T*)a.x + (b * a.L + r0) * a.C + ch0;
+    const int col = tid % cols, rl = tid / cols;
+    const bool on = rl < lanes;
+    if (on)
+        for (int r = rl; r < rows; r += lanes) cp_async16(tile + (long long)r * width + col * V, x + (long long)r * a.C + col * V, 16);
+    cp_async_commit();
+    cp_async_wait<0>();
+    float mean[V], rstd[V], wt[V], bs[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        wt[i] = a.weight && on ? a.weight[ch0 + col * V + i] : 1.0f;
+        bs[i] = a.bias && on ? a.bias[ch0 + col * V + i] : 0.0f;
+    }
+    __syncthreads();
+    {  // sums of the differences to the tile's first pixel, and of their squares
+        float s1[V] = {}, s2[V] = {}, pivot[V];
+        if (on && rows > 0) {
+            const NPack<T, V> f = *reinterpret_cast<const NPack<T, V>*>(tile + col * V);
+#pragma unroll
+            for (int i = 0; i < V; ++i) pivot[i] = io<T>::cvt(f.v[i]);
+#pragma unroll 4
+            for (int r = rl; r < rows; r += lanes) {
+                const NPack<T, V> e = *reinterpret_cast<const NPack<T, V>*>(tile + (long long)r * width + col * V);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float d = io<T>::cvt(e.v[i]) - pivot[i];
+                    s1[i] += d;
+                    s2[i] = fmaf(d, d, s2[i]);
+                }
+            }
+        }
+        const float inv = 1.0f / (float)max(rows, 1);
+        column_sums<V>(s1, scratch, width, cols, lanes, [&](int ch, float s) { sum1[ch] = s; });
+        column_sums<V>(s2, scratch, width, cols, lanes, [&](int ch, float s) {
+            const float d = sum1[ch], p = rows > 0 ? io<T>::cvt(tile[ch]) : 0.0f;
+            sum2[ch] = s - d * d * inv;  // M2 of the channel
+            sum1[ch] = p + d * inv;      // its mean
+        });
+        __syncthreads();
+        const int w = tid >> 5, lane = tid & 31;
+        for (int g = w; g < groups; g += kSlabThreads / 32) {
+            float s = 0.0f, q = 0.0f;
+            for (int i = lane; i < m; i += 32) s += sum1[g * m + i];
+            const float mu = warp_sum(s) / m;
+            for (int i = lane; i < m; i += 32) {
+                const float d = sum1[g * m + i] - mu;
+                q += fmaf(d * d, (float)rows, sum2[g * m + i]);
+            }
+            q = warp_sum(q);
+            if (lane == 0) stat[g] = make_float2(mu, q);
+        }
+    }
+    cl.sync();
+    // every CTA joins the cluster's means and M2 for itself
+    float2* all = reinterpret_cast<float2*>(sum1);
+    for (int g = tid; g < groups; g += kSlabThreads) {
+        float2 v[8];
+        float mu = 0.0f, q = 0.0f;
+        for (int i = 0; i < ctas; ++i) {
+            v[i] = *cl.map_shared_rank(stat + g, i);
+            mu = fmaf((float)max(0LL, min((long long)c.s.rows, a.L - (long long)i * c.s.rows)), v[i].x, mu);
+        }
+        mu /= (float)a.L;
+        for (int i = 0; i < ctas; ++i) {
+            const float d = v[i].x - mu;
+            q += fmaf(d * d, (float)max(0LL, min((long long)c.s.rows, a.L - (long long)i * c.s.rows)) * m, v[i].y);
+        }
+        const float2 out = make_float2(mu, 1.0f / sqrtf(q / ((float)a.L * m) + a.eps));
+        all[g] = out;
+        if (a.stats && rank == 0) reinterpret_cast<float2*>(a.stats)[(long long)b * a.G + ch0 / m + g] = out;
+    }
+    __syncthreads();
+    if (on) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float2 v = all[(col * V + i) / m];
+            mean[i] = v.x;
+            rstd[i] = v.y;
+        }
+        T* y = (T*)a.y + (b * a.L + r0) * a.C + ch0 + col * V;
+#pragma unroll 2
+        for (int r = rl; r < rows; r += lanes) {
+            const NPack<T, V> f = *reinterpret_cast<const NPack<T, V>*>(tile + (long long)r * width + col * V);
+            NPack<T, V> o;
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                o.v[i] = io<T>::to(act_value<ACT>(fmaf((io<T>::cvt(f.v[i]) - mean[i]) * rstd[i], wt[i], bs[i])));
+            *reinterpret_cast<NPack<T, V>*>(y + (long long)r * a.C) = o;
+        }
+    }
+    cl.sync();  // the others may still read this CTA's sums
+}
+
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_grad_kernel(SlabLaunch c) {
+    namespace cg = cooperative_groups;
+    extern __shared__ __align__(16) unsigned char shm[];
+    __shared__ unsigned flag;
+    const NormArgs& a = c.a;
+    const cg::cluster_group cl = cg::this_cluster();
+    const int ctas = c.s.ctas, rank = (int)cl.block_rank(), width = c.s.width, tid = threadIdx.x;
+    const int m = a.C / a.G, groups = width / m, cols = width / V, lanes = kSlabThreads / cols;
+    T *tx = reinterpret_cast<T*>(shm), *td = tx + (size_t)c.s.rows * width;
+    float* scratch = reinterpret_cast<float*>(shm + (((size_t)2 * c.s.rows * width * sizeof(T) + 15) & ~(size_t)15));
+    float *sum1 = scratch + kSlabThreads * V, *sum2 = sum1 + width;  // per channel: read by the cluster
+    float2* mine = reinterpret_cast<float2*>(sum2 + width);          // per group, the cluster's
+    pdl_launch_dependents();
+    pdl_wait();
+    const long long slab = blockIdx.x / ctas;
+    const int b = (int)(slab / c.s.slabs), ch0 = (int)(slab % c.s.slabs) * width;
+    const long long r0 = (long long)rank * c.s.rows, at = (b * a.L + r0) * a.C + ch0;
+    const int rows = (int)max(0LL, min((long long)c.s.rows, a.L - r0));
+    const int col = tid % cols, rl = tid / cols;
+    const bool on = rl < lanes;
+    if (on) {
+        const T *x = (const T*)a.x + at + col * V, *dy = (const T*)a.dy + at + col * V;
+        for (int r = rl; r < rows; r += lanes) {
+            cp_async16(tx + (long long)r * width + col * V, x + (long long)r * a.C, 16);
+            cp_async16(td + (long long)r * width + col * V, dy + (long long)r * a.C, 16);
+        }
+    }
+    cp_async_commit();
+    float mean[V], rstd[V], wt[V], bs[V];
+    const float2* st = reinterpret_cast<const float2*>(a.stats) + (long long)b * a.G;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int ch = ch0 + (on ? col * V + i : 0);
+        const float2 v = st[ch / m];
+        mean[i] = v.x;
+        rstd[i] = v.y;
+        wt[i] = a.weight ? a.weight[ch] : 1.0f;
+        bs[i] = a.bias ? a.bias[ch] : 0.0f;
+    }
+    cp_async_wait<0>();  // (a thread reads back what it copied itself)
+    {
+        float s1[V] = {}, s2[V] = {};
+        if (on) {
+#pragma unroll 2
+            for (int r = rl; r < rows; r += lanes) {
+                const NPack<T, V> f = *reinterpret_cast<const NPack<T, V>*>(tx + (long long)r * width + col * V);
+                NPack<T, V> d = *reinterpret_cast<const NPack<T, V>*>(td + (long long)r * width + col * V);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float n = (io<T>::cvt(f.v[i]) - mean[i]) * rstd[i];
+                    const float dz = io<T>::cvt(d.v[i]) * act_slope<ACT>(fmaf(n, wt[i], bs[i]));
+                    s1[i] += dz;
+                    s2[i] = fmaf(dz, n, s2[i]);
+                }
+            }
+        }
+        column_sums<V>(s1, scratch, width, cols, lanes, [&](int ch, float s) { sum1[ch] = s; });
+        column_sums<V>(s2, scratch, width, cols, lanes, [&](int ch, float s) { sum2[ch] = s; });
+    }
+    cl.sync();
+    // the cluster's sums: every CTA the groups' means, rank 0 also the channels'
+    {
+        const int w = tid >> 5, lane = tid & 31;
+        for (int g = w; g < groups; g += kSlabThreads / 32) {
+            float t1 = 0.0f, t2 = 0.0f;
+            for (int i = lane; i < m; i += 32) {
+                float u1 = 0.0f, u2 = 0.0f;
+                for (int k = 0; k < ctas; ++k) {
+                    u1 += *cl.map_shared_rank(sum1 + g * m + i, k);
+                    u2 += *cl.map_shared_rank(sum2 + g * m + i, k);
+                }
+                const float wv = a.weight ? a.weight[ch0 + g * m + i] : 1.0f;
+                t1 = fmaf(wv, u1, t1);
+                t2 = fmaf(wv, u2, t2);
+                if (rank == 0) c.chan[(long long)b * a.C + ch0 + g * m + i] = make_float2(u1, u2);
+            }
+            t1 = warp_sum(t1);
+            t2 = warp_sum(t2);
+            if (lane == 0) mine[g] = make_float2(t1 / ((float)a.L * m), t2 / ((float)a.L * m));
+        }
+    }
+    __syncthreads();
+    if (on) {
+        T* dx = (T*)a.dx + at + col * V;
+        float m1[V], m2[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float2 v = mine[(col * V + i) / m];
+            m1[i] = v.x;
+            m2[i] = v.y;
+        }
+#pragma unroll 2
+        for (int r = rl; r < rows; r += lanes) {
+            const NPack<T, V> f = *reinterpret_cast<const NPack<T, V>*>(tx + (long long)r * width + col * V);
+            const NPack<T, V> d = *reinterpret_cast<const NPack<T, V>*>(td + (long long)r * width + col * V);
+            NPack<T, V> o;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float n = (io<T>::cvt(f.v[i]) - mean[i]) * rstd[i];
+                const float dz = io<T>::cvt(d.v[i]) * act_slope<ACT>(fmaf(n, wt[i], bs[i]));
+                o.v[i] = io<T>::to(rstd[i] * (fmaf(wt[i], dz, -m1[i]) - n * m2[i]));
+            }
+            *reinterpret_cast<NPack<T, V>*>(dx + (long long)r * a.C) = o;
+        }
+    }
+    cl.sync();
+    if (rank != 0 || (!a.dweight && !a.dbias)) return;
+    if (!last_tile(c.counter, a.B * c.s.slabs, &flag)) return;  // the last slab of all: the sums over the batch
+    for (int k = tid; k < a.C; k += kSlabThreads) {
+        float t1 = 0.0f, t2 = 0.0f;
+#pragma unroll 16
+        for (int i = 0; i < a.B; ++i) {
+            const float2 v = __ldcg(&c.chan[(long long)i * a.C + k]);
+            t1 += v.x;
+            t2 += v.y;
+        }
+        if (a.dbias) a.dbias[k] = t1;
+        if (a.dweight) a.dweight[k] = t2;
+    }
+}
+
+template <typename T, int V, int ACT>
+vmb_status run_slabs(const NormArgs& a, const NormSlab& s, bool grads, size_t chan_off, cudaStream_t stream) {
+    SlabLaunch c{a, s, reinterpret_cast<float2*>((char*)a.ws + chan_off), reinterpret_cast<unsigned*>(a.ws) + kNormCounters - 1};
+    const void* fn = grads ? (const void*)norm_cluster_grad_kernel<T, V, ACT> : (const void*)norm_cluster_kernel<T, V, ACT>;
+    const size_t smem = slab_smem(s.rows, s.width, s.width / (a.C / a.G), sizeof(T), grads);
+    if (!allow_smem(fn, kSlabSmem)) return VMB_ERR_CUDA;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)((long long)a.B * s.slabs * s.ctas));
+    cfg.blockDim = dim3(kSlabThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)s.ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    void* args[] = {&c};
+    return cudaLaunchKernelExC(&cfg, fn, args) == cudaSuccess ? VMB_OK : VMB_ERR_CUDA;
+}
+
 template <typename T, int V, int ACT>
 vmb_status run_norm(const NormArgs& a, bool grads, cudaStream_t stream) {
     NormLaunch c{a, plan_norm(a.B, a.L, a.C, a.G, a.dtype, grads, device_sm_count()), 0};
     if (a.ws_bytes < c.p.total) return VMB_ERR_WORKSPACE;
+    NormSlab slab;
+    if constexpr (V * sizeof(T) == 16)
+        if (norm_slab(a.B, a.L, a.C, a.G, a.dtype, grads, device_sm_count(), &slab) &&
+            (long long)a.B * slab.slabs * slab.ctas <= 2147483647LL && (long long)a.B * slab.slabs <= 2147483647LL)
+            return run_slabs<T, V, ACT>(a, slab, grads, c.p.chan, stream);
     const void* one = grads ? (const void*)norm_sums_kernel<T, V, ACT> : (const void*)norm_stats_kernel<T, V>;
     const void* two = grads ? (const void*)norm_dx_kernel<T, V, ACT> : (const void*)norm_apply_kernel<T, V, ACT>;
     const size_t smem = grads ? 0 : (size_t)a.C * 8 + kNormThreads * V * 8;
