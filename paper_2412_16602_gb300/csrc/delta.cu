@@ -241,7 +241,7 @@ DeltaChain chain_of(const DeltaArgs& a, const DeltaPlan& p) {
     c.a = a;
     c.segs = p.segs;
     c.seg_chunks = p.seg_chunks;
-    c.slices = p.slices;
+    c.wide = p.wide;
     unsigned char* ws = (unsigned char*)a.ws;
     c.maps = (float*)(ws + p.maps_off);
     c.sums = (float*)(ws + p.sums_off);
@@ -281,11 +281,11 @@ DeltaPlan plan_delta(const DeltaArgs& a, bool grads, int sms) {
     DeltaPlan p{};
     const long long chains = (long long)a.B * a.Hv;
     p.chunks = (a.T + kChunk - 1) / kChunk;
-    p.slices = (a.Dv + kDeltaRows - 1) / kDeltaRows;
+    p.wide = a.dtype == VMB_BF16 && a.Dv > 64;
     p.slots = delta_slots(a.B, a.T, a.total, a.offsets != nullptr);
     p.segs = 1;
     p.seg_chunks = p.chunks;
-    const long long ctas = chains * p.slices;
+    const long long ctas = chains * ((a.Dv + (p.wide ? 127 : 63)) / (p.wide ? 128 : 64));
     // Segments cost a second pass over the chunks (and Dk more rows in it): taken when the chains leave
     // more than half of the SMs idle and each segment still has two chunks.
     if (ctas * 2 <= sms && p.chunks >= 4) {

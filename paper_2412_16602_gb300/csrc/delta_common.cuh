@@ -29,19 +29,19 @@
 namespace vmb {
 
 constexpr int kChunk = 64;       // tokens per chunk
-constexpr int kDeltaRows = 64;   // value channels (state rows) per CTA: 16 per warp
+
 
 // ------------------------------------------------------------------ fragments
 
 // acc is a 16 x 8 fp32 accumulator tile: lane (g = lane / 4, t = lane % 4) holds
 // (g, 2t), (g, 2t + 1), (g + 8, 2t), (g + 8, 2t + 1).
 __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
 __device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
-    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
@@ -528,13 +528,21 @@ __device__ __forceinline__ DeltaSeq delta_seq(const int* offsets, int b, int T, 
 // Per token, in shared memory.  The log decays are summed as pairs of floats (hi + lo), so that a
 // difference c_i - c_j keeps fp32 accuracy however small c is: a token that resets the state (g = -inf,
 // taken as -200, whose exponential is 0 in fp32) does not cost the tokens after it any digits.
-struct ChunkGates {
+struct alignas(16) ChunkGates {
     float hi[kChunk], lo[kChunk];  // c
     float beta[kChunk];
     float ec[kChunk];    // e^c
     float tail[kChunk];  // e^(c_last - c)
     float last;          // e^(c_last)
+    // an accumulator pair's tokens, 8 n + 2 t and the one after it
+    static __device__ __forceinline__ float2 pair(const float* v, int n) {
+        return *reinterpret_cast<const float2*>(v + 8 * n + 2 * (threadIdx.x & 3));
+    }
 };
+// c[x] *= (token of the pair's scale)
+__device__ __forceinline__ void scale_tokens(float (&c)[4], float2 s) {
+    c[0] *= s.x, c[1] *= s.y, c[2] *= s.x, c[3] *= s.y;
+}
 __device__ __forceinline__ float decay(float hi, float lo) { return ex2((hi + lo) * kLog2e); }
 
 __device__ __forceinline__ void add_pair(float& h, float& l, float h2, float l2) {
@@ -572,91 +580,105 @@ __device__ __forceinline__ void chunk_gates(ChunkGates& G, float g0, float g1, f
 
 // ------------------------------------------------------------------ the chunk's triangular system
 
-// The products of a chunk that do not depend on the state, by eight warps (w = 0 .. 7):
+// The products of a chunk that do not depend on the state, by WARPS (4 or 8) warps:
 //   sE: -E below the diagonal blocks, and on the diagonal the inverses (I + E_bb b)^-1
 //       (kRowBeta: (I + b E_bb)^-1, the transposed system's);
 //   sP (kWithP): scale e^(c_i - c_j) q_i.k_j for j <= i, zeros above.
-// Warps 0 to 3 compute one diagonal block each and invert it, warps 4 to 7 the six blocks below the diagonal.
+// Warps 0 to 3 compute one diagonal block of both and invert that of E; the six blocks below the diagonal of E and of P
+// are twelve tasks for the last four warps (the same ones where there are no others).
 // diag: 4 x 16 x 20 floats of scratch.  The gates and tiles are ready before the call; no barrier inside.
-template <typename T, int DK, bool kRowBeta, bool kWithP, int NE, int NK>
+template <typename T, int DK, bool kRowBeta, bool kWithP, int WARPS, int NE, int NK>
 __device__ __forceinline__ void chunk_system(const Tile<T, DK, NK>& sK, const Tile<T, DK, NK>& sQ, const LowTile<T, NE>& sE,
                                              const LowTile<T, NE>& sP, float* diag, const ChunkGates& G, float scale, int w) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    for (int task = w; task < 10; task += task < 4 ? 10 : 4) {
-        const bool on = task < 4;
-        // (0,0) (1,1) (2,2) (3,3), then (3,0) (3,1) (3,2) (2,0) (2,1) (1,0)
-        const int bi = on ? task : task < 7 ? 3 : task < 9 ? 2 : 1;
-        const int bj = on ? task : task < 7 ? task - 4 : task < 9 ? task - 7 : 0;
-        float kk[2][4] = {}, qk[2][4] = {};
-#pragma unroll
-        for (int d = 0; d < DK; d += 16) {
-            FragA<T, NK> ak, aq;
-            FragB<T, NK> b0, b1;
-            sK.b_nk(b0, b1, 16 * bj, d);
-            sK.a_mk(ak, 16 * bi, d);
-            mma16(kk[0], ak, b0);
-            mma16(kk[1], ak, b1);
-            if constexpr (kWithP) {
-                sQ.a_mk(aq, 16 * bi, d);
-                mma16(qk[0], aq, b0);
-                mma16(qk[1], aq, b1);
-            }
-        }
-        float jh[4], jl[4], jb[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const int j = 16 * bj + 8 * (x >> 1) + 2 * t + (x & 1);
-            jh[x] = G.hi[j], jl[x] = G.lo[j], jb[x] = G.beta[j];
-        }
+    // e^(c_i - c_j) of this lane's places of block (bi, bj), zero for j > i (where it may be large without bound)
+    auto decays = [&](int bi, int bj, float(&d)[2][4]) {
+        const float2 h0 = G.pair(G.hi, 2 * bj), h1 = G.pair(G.hi, 2 * bj + 1), l0 = G.pair(G.lo, 2 * bj), l1 = G.pair(G.lo, 2 * bj + 1);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int r = g + 8 * h, i = 16 * bi + r;
-            const float ih = G.hi[i], il = G.lo[i], ib = G.beta[i];
+            const float ih = G.hi[i], il = G.lo[i];
+            d[0][2 * h] = bi > bj || 2 * t <= r ? decay(ih - h0.x, il - l0.x) : 0.0f;
+            d[0][2 * h + 1] = bi > bj || 2 * t + 1 <= r ? decay(ih - h0.y, il - l0.y) : 0.0f;
+            d[1][2 * h] = bi > bj || 8 + 2 * t <= r ? decay(ih - h1.x, il - l1.x) : 0.0f;
+            d[1][2 * h + 1] = bi > bj || 9 + 2 * t <= r ? decay(ih - h1.y, il - l1.y) : 0.0f;
+        }
+    };
+    auto product = [&](const Tile<T, DK, NK>& sA, int bi, int bj, float(&c)[2][4]) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                float e[2], p[2];
+        for (int d = 0; d < DK; d += 16) {
+            FragA<T, NK> a;
+            FragB<T, NK> b0, b1;
+            sK.b_nk(b0, b1, 16 * bj, d);
+            sA.a_mk(a, 16 * bi, d);
+            mma16(c[0], a, b0);
+            mma16(c[1], a, b1);
+        }
+    };
+    if (w < 4) {
+        float kk[2][4] = {}, d[2][4];
+        product(sK, w, w, kk);
+        decays(w, w, d);
+        const float2 b0 = G.pair(G.beta, 2 * w), b1 = G.pair(G.beta, 2 * w + 1);
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int j = 16 * bj + 8 * n + 2 * t + x;
-                    // (above the diagonal the difference may be positive without bound: not taken)
-                    const float d = j <= i ? decay(ih - jh[2 * n + x], il - jl[2 * n + x]) : 0.0f;
-                    e[x] = j < i ? d * kk[n][2 * h + x] : 0.0f;
-                    p[x] = j <= i ? scale * d * qk[n][2 * h + x] : 0.0f;
-                }
-                if constexpr (kWithP) sP.set2(bi, bj, r, 8 * n + 2 * t, p[0], p[1]);
-                if (on) {  // transposed: the columns of the block side by side
-                    float* col = diag + (bi * 16 + 8 * n + 2 * t) * 20 + r;
-                    col[0] = e[0] * (kRowBeta ? ib : jb[2 * n]);
-                    col[20] = e[1] * (kRowBeta ? ib : jb[2 * n + 1]);
-                } else {
-                    sE.set2(bi, bj, r, 8 * n + 2 * t, -e[0], -e[1]);
-                }
+        for (int h = 0; h < 2; ++h) {
+            const int r = g + 8 * h;
+            const float ib = G.beta[16 * w + r];
+            // transposed: the columns of the block side by side (the diagonal itself is not read)
+            float* col = diag + (w * 16 + 2 * t) * 20 + r;
+            col[0] = kk[0][2 * h] * d[0][2 * h] * (kRowBeta ? ib : b0.x);
+            col[20] = kk[0][2 * h + 1] * d[0][2 * h + 1] * (kRowBeta ? ib : b0.y);
+            col[160] = kk[1][2 * h] * d[1][2 * h] * (kRowBeta ? ib : b1.x);
+            col[180] = kk[1][2 * h + 1] * d[1][2 * h + 1] * (kRowBeta ? ib : b1.y);
+        }
+        __syncwarp();
+        if constexpr (kWithP) {
+            float qk[2][4] = {};
+            product(sQ, w, w, qk);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+                    sP.set2(w, w, g + 8 * h, 8 * n + 2 * t, scale * d[n][2 * h] * qk[n][2 * h], scale * d[n][2 * h + 1] * qk[n][2 * h + 1]);
+        }
+        // column c of (I + L)^-1, L the strictly lower block: x_i = [i = c] - sum_{j < i} L_ij x_j, taken off column
+        // by column of L so that the chain is 15 products long
+        const int c = lane & 15;
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = i == c ? 1.0f : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 15; ++j) {
+            const float* col = diag + (w * 16 + j) * 20;
+#pragma unroll
+            for (int i4 = (j + 1) / 4; i4 < 4; ++i4) {
+                const float4 l = *reinterpret_cast<const float4*>(col + 4 * i4);
+                if (4 * i4 > j) x[4 * i4] = fmaf(-l.x, x[j], x[4 * i4]);
+                if (4 * i4 + 1 > j) x[4 * i4 + 1] = fmaf(-l.y, x[j], x[4 * i4 + 1]);
+                if (4 * i4 + 2 > j) x[4 * i4 + 2] = fmaf(-l.z, x[j], x[4 * i4 + 2]);
+                if (4 * i4 + 3 > j) x[4 * i4 + 3] = fmaf(-l.w, x[j], x[4 * i4 + 3]);
             }
         }
-        if (on) {
-            __syncwarp();
-            // column c of (I + L)^-1, L the strictly lower block: x_i = [i = c] - sum_{j < i} L_ij x_j, taken off column
-            // by column of L so that the chain is 15 products long
-            const int c = lane & 15;
-            float x[16];
+        if (lane < 16) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = i == c ? 1.0f : 0.0f;
+            for (int i = 0; i < 16; ++i) sE.set(w, w, i, c, x[i]);
+        }
+    }
+    if (w >= WARPS - 4) {
+        for (int task = w - (WARPS - 4); task < (kWithP ? 12 : 6); task += 4) {
+            const bool p = task >= 6;
+            const int b = p ? task - 6 : task;  // (3,0) (3,1) (3,2) (2,0) (2,1) (1,0)
+            const int bi = b < 3 ? 3 : b < 5 ? 2 : 1, bj = b < 3 ? b : b < 5 ? b - 3 : 0;
+            float c[2][4] = {}, d[2][4];
+            product(p ? sQ : sK, bi, bj, c);
+            decays(bi, bj, d);
+            const float f = p ? scale : -1.0f;
+            const LowTile<T, NE>& to = p ? sP : sE;
 #pragma unroll
-            for (int j = 0; j < 15; ++j) {
-                const float* col = diag + (bi * 16 + j) * 20;
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i4 = (j + 1) / 4; i4 < 4; ++i4) {
-                    const float4 l = *reinterpret_cast<const float4*>(col + 4 * i4);
-                    if (4 * i4 > j) x[4 * i4] = fmaf(-l.x, x[j], x[4 * i4]);
-                    if (4 * i4 + 1 > j) x[4 * i4 + 1] = fmaf(-l.y, x[j], x[4 * i4 + 1]);
-                    if (4 * i4 + 2 > j) x[4 * i4 + 2] = fmaf(-l.z, x[j], x[4 * i4 + 2]);
-                    if (4 * i4 + 3 > j) x[4 * i4 + 3] = fmaf(-l.w, x[j], x[4 * i4 + 3]);
-                }
-            }
-            if (lane < 16) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sE.set(bi, bi, i, c, x[i]);
-            }
+                for (int n = 0; n < 2; ++n)
+                    to.set2(bi, bj, g + 8 * h, 8 * n + 2 * t, f * d[n][2 * h] * c[n][2 * h], f * d[n][2 * h + 1] * c[n][2 * h + 1]);
         }
     }
 }

@@ -38,7 +38,7 @@ struct DeltaArgs {
 struct DeltaPlan {
     int chunks;      // chunks of the longest sequence
     int segs, seg_chunks;
-    int slices;      // 64-row slices of the value channels
+    bool wide;       // 128 rows of the state per CTA instead of 64
     long long slots; // chunk states kept
     size_t maps_off, sums_off;        // segment maps [chain][seg][Dk][Dk] and sums [chain][seg][Dv][Dk], fp32
     size_t ds_off, dx_off, part_off;  // gradients: chunk-end dS, dX, per-value-head dq and dk
@@ -51,6 +51,7 @@ long long delta_slots(int B, int T, long long total, bool packed);
 struct DeltaChain {
     DeltaArgs a;
     int segs, seg_chunks, slices;
+    bool wide;
     int summary;       // 1: write the sums (and, forward, the maps) of every segment and nothing else
     int maps_only;     // forward summary: the maps alone
     float* maps;       // [chain][seg][Dk][Dk]
