@@ -204,29 +204,31 @@ template <typename T, typename TL> __device__ __forceinline__ void read_columns(
 }
 
 // x[channel][token] += S^T K^T and, with kTwo, y += S^T Q^T (leading terms of S), the rows of the state against every
-// token; the operands are read two steps (of four tiles) ahead of their products.
+// token; the operands are read two steps (of four tiles) ahead of their products, one step where fp32
+// operands, four times the registers, leave no more.
 template <int DK, bool kTwo, int NS, typename T, typename TL>
 __device__ __forceinline__ void state_times(const float (&S)[DK / 8][4], float (&x)[8][4], float (*y)[4], const TL& sK, const TL& sQ) {
     constexpr int kSteps = DK / 16 * (kTwo ? 4 : 2);
-    FragB<T, 1> b[3][4];
+    constexpr int kAhead = sizeof(T) == 2 || DK == 64 ? 2 : 1;
+    FragB<T, 1> b[kAhead + 1][4];
     auto read = [&](int i, FragB<T, 1>(&f)[4]) {
         const int d = kTwo ? i >> 2 : i >> 1, n = 32 * (kTwo ? (i >> 1) & 1 : i & 1);
         const TL& s = kTwo && (i & 1) ? sQ : sK;
         s.b_nk(f[0], f[1], n, 16 * d);
         s.b_nk(f[2], f[3], n + 16, 16 * d);
     };
-    read(0, b[0]);
-    read(1, b[1]);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) read(i, b[i]);
     FragA<T, NS> f;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-        if (i + 2 < kSteps) read(i + 2, b[(i + 2) % 3]);
+        if (i + kAhead < kSteps) read(i + kAhead, b[(i + kAhead) % (kAhead + 1)]);
         const int d = kTwo ? i >> 2 : i >> 1, n = 4 * (kTwo ? (i >> 1) & 1 : i & 1);
         if (kTwo ? i % 4 == 0 : i % 2 == 0) frag_from_acc(f, S[2 * d], S[2 * d + 1]);
         if (kTwo && (i & 1))
-            mma_quad(*reinterpret_cast<float(*)[4][4]>(&y[n]), lead(f), b[i % 3]);
+            mma_quad(*reinterpret_cast<float(*)[4][4]>(&y[n]), lead(f), b[i % (kAhead + 1)]);
         else
-            mma_quad(*reinterpret_cast<float(*)[4][4]>(&x[n]), f, b[i % 3]);
+            mma_quad(*reinterpret_cast<float(*)[4][4]>(&x[n]), f, b[i % (kAhead + 1)]);
     }
 }
 // S += f K_b: the outer products of 16 tokens (block b of a tile) with the state's columns; `k` holds the operands of the
@@ -235,7 +237,11 @@ template <int DK, int NS, typename T, typename TL>
 __device__ __forceinline__ void state_add(float (&S)[DK / 8][4], const FragA<T, NS>& f, const TL& s, int b, FragB<T, 1> (&k)[2][4]) {
 #pragma unroll
     for (int d = 0; d < DK / 32; ++d) {
-        if (d + 1 < DK / 32) read_columns(s, b, d + 1, k[(d + 1) & 1]);
+        if (sizeof(T) == 2 || DK == 64) {
+            if (d + 1 < DK / 32) read_columns(s, b, d + 1, k[(d + 1) & 1]);
+        } else if (d > 0) {
+            read_columns(s, b, d, k[d & 1]);
+        }
         mma_quad(*reinterpret_cast<float(*)[4][4]>(&S[4 * d]), f, k[d & 1]);
     }
 }
@@ -245,6 +251,7 @@ template <typename T, int DK, int NST, bool kOut>
 __global__ void __launch_bounds__(kChainThreads, 1) delta_forward_kernel(DeltaChain c) {
     using SM = ChainSmem<T, DK, NST>;
     constexpr int M = SM::mid, kRows = SM::rows;
+    constexpr bool kPacked = sizeof(T) == 2;
     extern __shared__ __align__(128) unsigned char smem[];
     const DeltaArgs& a = c.a;
     pdl_launch_dependents();
@@ -322,26 +329,33 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_forward_kernel(DeltaCh
         float x[8][4] = {}, y[kOut ? 8 : 1][4] = {};  // K S and Q S, transposed: [channel][token]
         state_times<DK, kOut, M, T>(S, x, y, sK, sQ);
 #pragma unroll
-        for (int n = 0; n < DK / 8; ++n)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) S[n][j] *= G.last;
+        for (int n = 0; n < DK / 8; ++n) scale4<kPacked>(S[n], make_float2(G.last, G.last));
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
             float v0[4] = {}, v1[4] = {};
             if (!map) sV.acc_km(v0, v1, 16 * w, 16 * n);
             const float2 e0 = G.pair(G.ec, 2 * n), e1 = G.pair(G.ec, 2 * n + 1);
-            scale_tokens(x[2 * n], e0), scale_tokens(x[2 * n + 1], e1);
             if constexpr (kOut) {
-                scale_tokens(y[2 * n], make_float2(a.scale * e0.x, a.scale * e0.y));
-                scale_tokens(y[2 * n + 1], make_float2(a.scale * e1.x, a.scale * e1.y));
+                scale4<kPacked>(y[2 * n], make_float2(a.scale * e0.x, a.scale * e0.y));
+                scale4<kPacked>(y[2 * n + 1], make_float2(a.scale * e1.x, a.scale * e1.y));
             }
+            const float2 m0 = make_float2(-e0.x, -e0.y), m1 = make_float2(-e1.x, -e1.y);
+            if constexpr (kPacked) {
+                put4(x[2 * n], __ffma2_rn(lo2(x[2 * n]), m0, lo2(v0)), __ffma2_rn(hi2(x[2 * n]), m0, hi2(v0)));
+                put4(x[2 * n + 1], __ffma2_rn(lo2(x[2 * n + 1]), m1, lo2(v1)), __ffma2_rn(hi2(x[2 * n + 1]), m1, hi2(v1)));
+            } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[2 * n][j] = v0[j] - x[2 * n][j], x[2 * n + 1][j] = v1[j] - x[2 * n + 1][j];
+                for (int j = 0; j < 4; ++j) {
+                    x[2 * n][j] = fmaf(x[2 * n][j], j & 1 ? m0.y : m0.x, v0[j]);
+                    x[2 * n + 1][j] = fmaf(x[2 * n + 1][j], j & 1 ? m1.y : m1.x, v1[j]);
+                }
+            }
         }
         // Block by block: while the products of block b with the state's columns and with P run, the next block's
         // residuals are corrected by the blocks before it and multiplied by its inverse.  Operands that do not depend
         // on the residuals are read ahead.
         FragA<T, M> uf[4], f;
+        constexpr bool kEarly = sizeof(T) == 2 || DK == 64;
         FragB<T, M> e[4][2];
         FragB<T, 1> kc[2][4];
         float r0[4] = {}, r1[4] = {}, w0[4] = {}, w1[4] = {};
@@ -350,26 +364,30 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_forward_kernel(DeltaCh
         mma_pair(r0, r1, w0, w1, f, e[0][0], e[0][1]);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            read_columns(sK, b, 0, kc[0]);
-            if (b < 3) {
+            if (kEarly) read_columns(sK, b, 0, kc[0]);
+            if (kEarly && b < 3) {
 #pragma unroll
                 for (int j = 0; j <= b + 1; ++j) sE.b_nk(e[j][0], e[j][1], b + 1, j);
             }
             const float2 b0 = G.pair(G.beta, 2 * b), b1 = G.pair(G.beta, 2 * b + 1), t0 = G.pair(G.tail, 2 * b), t1 = G.pair(G.tail, 2 * b + 1);
+            add4<kPacked>(r0, w0), add4<kPacked>(r1, w1);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                r0[j] += w0[j], r1[j] += w1[j];
                 if constexpr (kOut) x[2 * b][j] = r0[j], x[2 * b + 1][j] = r1[j];
                 w0[j] = w1[j] = 0.0f;
             }
-            scale_tokens(r0, b0), scale_tokens(r1, b1);
+            scale4<kPacked>(r0, b0), scale4<kPacked>(r1, b1);
             frag_from_acc(uf[b], r0, r1);
             if (b < 3) {
 #pragma unroll
-                for (int j = 0; j <= b; ++j) mma_pair(x[(2 * b + 2) & 7], x[(2 * b + 3) & 7], w0, w1, uf[j], e[j][0], e[j][1]);
+                for (int j = 0; j <= b; ++j) {
+                    if (!kEarly) sE.b_nk(e[j][0], e[j][1], b + 1, j);
+                    mma_pair(x[(2 * b + 2) & 7], x[(2 * b + 3) & 7], w0, w1, uf[j], e[j][0], e[j][1]);
+                }
             }
-            scale_tokens(r0, t0), scale_tokens(r1, t1);
+            scale4<kPacked>(r0, t0), scale4<kPacked>(r1, t1);
             frag_from_acc(f, r0, r1);
+            if (!kEarly) read_columns(sK, b, 0, kc[0]);
             state_add<DK>(S, f, sK, b, kc);
             FragB<T, M> p[4];
             if constexpr (kOut) {
@@ -379,12 +397,11 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_forward_kernel(DeltaCh
                 }
             }
             if (b < 3) {
+                add4<kPacked>(x[(2 * b + 2) & 7], w0), add4<kPacked>(x[(2 * b + 3) & 7], w1);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[(2 * b + 2) & 7][j] += w0[j], x[(2 * b + 3) & 7][j] += w1[j];
-                    r0[j] = r1[j] = w0[j] = w1[j] = 0.0f;
-                }
+                for (int j = 0; j < 4; ++j) r0[j] = r1[j] = w0[j] = w1[j] = 0.0f;
                 frag_from_acc(f, x[(2 * b + 2) & 7], x[(2 * b + 3) & 7]);
+                if (!kEarly) sE.b_nk(e[(b + 1) & 3][0], e[(b + 1) & 3][1], b + 1, b + 1);
                 mma_pair(r0, r1, w0, w1, f, e[(b + 1) & 3][0], e[(b + 1) & 3][1]);
             }
             if constexpr (kOut) {
@@ -398,8 +415,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_forward_kernel(DeltaCh
                     float z0[4] = {}, z1[4] = {};
                     sP.b_nk(p[0], p[1], 3, b);
                     mma_pair(y[6], y[7], z0, z1, uf[b], p[0], p[1]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) y[6][j] += z0[j], y[7][j] += z1[j];
+                    add4<kPacked>(y[6], z0), add4<kPacked>(y[7], z1);
                 }
             }
         }
@@ -439,6 +455,7 @@ template <typename T, int DK, int NST>
 __global__ void __launch_bounds__(kChainThreads, 1) delta_reverse_kernel(DeltaChain c) {
     using SM = ChainSmem<T, DK, NST>;
     constexpr int M = SM::mid, kRows = SM::rows;
+    constexpr bool kPacked = sizeof(T) == 2;
     extern __shared__ __align__(128) unsigned char smem[];
     const DeltaArgs& a = c.a;
     pdl_launch_dependents();
@@ -513,11 +530,9 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_reverse_kernel(DeltaCh
         float x[8][4] = {};  // dU, then dX, transposed
         state_times<DK, false, M, T>(S, x, nullptr, sK, sK);
 #pragma unroll
-        for (int n = 0; n < DK / 8; ++n)
+        for (int n = 0; n < DK / 8; ++n) scale4<kPacked>(S[n], make_float2(G.last, G.last));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) S[n][j] *= G.last;
-#pragma unroll
-        for (int n = 0; n < 8; ++n) scale_tokens(x[n], G.pair(G.tail, n));
+        for (int n = 0; n < 8; ++n) scale4<kPacked>(x[n], G.pair(G.tail, n));
         FragB<T, 1> kc[2][4];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {  // token block b of do: P^T do into dU, (scale e^c Q)^T do into dS
@@ -527,8 +542,8 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_reverse_kernel(DeltaCh
             float d0[4], d1[4];
             sD.acc_km(d0, d1, 16 * w, 16 * b);
             const float2 e0 = G.pair(G.ec, 2 * b), e1 = G.pair(G.ec, 2 * b + 1);
-            scale_tokens(d0, make_float2(a.scale * e0.x, a.scale * e0.y));
-            scale_tokens(d1, make_float2(a.scale * e1.x, a.scale * e1.y));
+            scale4<kPacked>(d0, make_float2(a.scale * e0.x, a.scale * e0.y));
+            scale4<kPacked>(d1, make_float2(a.scale * e1.x, a.scale * e1.y));
             FragA<T, M> fs;
             frag_from_acc(fs, d0, d1);
 #pragma unroll
@@ -543,11 +558,11 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_reverse_kernel(DeltaCh
                 sP.b_kn(p0, p1, b, b);
                 float z0[4] = {}, z1[4] = {};
                 mma_pair(x[2 * b], x[2 * b + 1], z0, z1, f, p0, p1);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[2 * b][j] += z0[j], x[2 * b + 1][j] += z1[j];
+                add4<kPacked>(x[2 * b], z0), add4<kPacked>(x[2 * b + 1], z1);
             }
             state_add<DK>(S, fs, sQ, b, kc);
         }
+        constexpr bool kEarly = sizeof(T) == 2 || DK == 64;
         FragA<T, M> rf[4], f;
         FragB<T, M> e[4][2];
         float r0[4] = {}, r1[4] = {}, w0[4] = {}, w1[4] = {};
@@ -556,34 +571,37 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_reverse_kernel(DeltaCh
         mma_pair(r0, r1, w0, w1, f, e[3][0], e[3][1]);
 #pragma unroll
         for (int b = 3; b >= 0; --b) {
-            read_columns(sK, b, 0, kc[0]);
-            if (b > 0) {
+            if (kEarly) read_columns(sK, b, 0, kc[0]);
+            if (kEarly && b > 0) {
 #pragma unroll
                 for (int j = 3; j >= b - 1; --j) sE.b_kn(e[j][0], e[j][1], j, b - 1);
             }
             const float2 b0 = G.pair(G.beta, 2 * b), b1 = G.pair(G.beta, 2 * b + 1), t0 = G.pair(G.ec, 2 * b), t1 = G.pair(G.ec, 2 * b + 1);
+            add4<kPacked>(r0, w0), add4<kPacked>(r1, w1);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                r0[j] += w0[j], r1[j] += w1[j];
                 x[2 * b][j] = r0[j], x[2 * b + 1][j] = r1[j];
                 w0[j] = w1[j] = 0.0f;
             }
-            scale_tokens(r0, b0), scale_tokens(r1, b1);
+            scale4<kPacked>(r0, b0), scale4<kPacked>(r1, b1);
             frag_from_acc(rf[b], r0, r1);
             if (b > 0) {
 #pragma unroll
-                for (int j = 3; j >= b; --j) mma_pair(x[(2 * b - 2) & 7], x[(2 * b - 1) & 7], w0, w1, rf[j], e[j][0], e[j][1]);
+                for (int j = 3; j >= b; --j) {
+                    if (!kEarly) sE.b_kn(e[j][0], e[j][1], j, b - 1);
+                    mma_pair(x[(2 * b - 2) & 7], x[(2 * b - 1) & 7], w0, w1, rf[j], e[j][0], e[j][1]);
+                }
             }
-            scale_tokens(r0, make_float2(-t0.x, -t0.y)), scale_tokens(r1, make_float2(-t1.x, -t1.y));
+            scale4<kPacked>(r0, make_float2(-t0.x, -t0.y)), scale4<kPacked>(r1, make_float2(-t1.x, -t1.y));
             frag_from_acc(f, r0, r1);
+            if (!kEarly) read_columns(sK, b, 0, kc[0]);
             state_add<DK>(S, f, sK, b, kc);
             if (b > 0) {
+                add4<kPacked>(x[(2 * b - 2) & 7], w0), add4<kPacked>(x[(2 * b - 1) & 7], w1);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[(2 * b - 2) & 7][j] += w0[j], x[(2 * b - 1) & 7][j] += w1[j];
-                    r0[j] = r1[j] = w0[j] = w1[j] = 0.0f;
-                }
+                for (int j = 0; j < 4; ++j) r0[j] = r1[j] = w0[j] = w1[j] = 0.0f;
                 frag_from_acc(f, x[(2 * b - 2) & 7], x[(2 * b - 1) & 7]);
+                if (!kEarly) sE.b_kn(e[(b - 1) & 3][0], e[(b - 1) & 3][1], b - 1, b - 1);
                 mma_pair(r0, r1, w0, w1, f, e[(b - 1) & 3][0], e[(b - 1) & 3][1]);
             }
         }
@@ -591,7 +609,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_reverse_kernel(DeltaCh
             const int n = min(seq.len - ch * kChunk, kChunk);
             store_tokens<T, kRows>(sD, x, xp + (long long)ch * kChunk * hrow, hrow, n, at.slice * kRows, a.Dv, xvec);
 #pragma unroll
-            for (int m = 0; m < 8; ++m) scale_tokens(x[m], G.pair(G.beta, m));
+            for (int m = 0; m < 8; ++m) scale4<kPacked>(x[m], G.pair(G.beta, m));
             store_tokens<T, kRows>(sD, x, rp + (long long)ch * kChunk * hrow, hrow, n, at.slice * kRows, a.Dv, rvec);
         }
         bar_arrive(kBarEmpty + (i & 1), kChainThreads);

@@ -46,6 +46,26 @@ __device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
 
+// Accumulator pairs through the packed operations, half the instructions: in the bf16 kernels (176 -> 158 us for a batch of
+// 32 x 3136 tokens).  In the fp32 kernels, which use every register, the pairs cost more moves than they save (878 -> 1150 us
+// for a training pass of 32 x 784): kPacked = false.
+__device__ __forceinline__ float2 lo2(const float (&c)[4]) { return make_float2(c[0], c[1]); }
+__device__ __forceinline__ float2 hi2(const float (&c)[4]) { return make_float2(c[2], c[3]); }
+__device__ __forceinline__ void put4(float (&c)[4], float2 a, float2 b) { c[0] = a.x, c[1] = a.y, c[2] = b.x, c[3] = b.y; }
+__device__ __forceinline__ float2 minus(float2 a, float2 b) { return __ffma2_rn(b, make_float2(-1.0f, -1.0f), a); }
+template <bool kPacked> __device__ __forceinline__ void scale4(float (&c)[4], float2 s) {
+    if constexpr (kPacked)
+        put4(c, __fmul2_rn(lo2(c), s), __fmul2_rn(hi2(c), s));
+    else
+        c[0] *= s.x, c[1] *= s.y, c[2] *= s.x, c[3] *= s.y;
+}
+template <bool kPacked> __device__ __forceinline__ void add4(float (&c)[4], const float (&d)[4]) {
+    if constexpr (kPacked)
+        put4(c, __fadd2_rn(lo2(c), lo2(d)), __fadd2_rn(hi2(c), hi2(d)));
+    else
+        c[0] += d[0], c[1] += d[1], c[2] += d[2], c[3] += d[3];
+}
+
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -53,10 +73,23 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 __device__ __forceinline__ float bf16_lo(uint32_t p) { return __uint_as_float(p << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t p) { return __uint_as_float(p & 0xffff0000u); }
+__device__ __forceinline__ float2 bf16_pair(uint32_t p) { return make_float2(bf16_lo(p), bf16_hi(p)); }
+// v = hi + lo up to 2^-18 |v|
+__device__ __forceinline__ void split_bf16(float2 v, uint32_t& hi, uint32_t& lo) {
+    hi = pack_bf16(v.x, v.y);
+    const float2 d = minus(v, bf16_pair(hi));
+    lo = pack_bf16(d.x, d.y);
+}
 // x = hi + lo up to 2^-21 |x|, both tf32 (19 leading bits): by masks, at the full rate of the integer pipe
 __device__ __forceinline__ void split_tf32(float x, uint32_t& hi, uint32_t& lo) {
     hi = __float_as_uint(x) & 0xffffe000u;
     lo = __float_as_uint(x - __uint_as_float(hi)) & 0xffffe000u;
+}
+__device__ __forceinline__ void split_tf32(float x, float y, uint32_t& xh, uint32_t& xl, uint32_t& yh, uint32_t& yl) {
+    xh = __float_as_uint(x) & 0xffffe000u;
+    yh = __float_as_uint(y) & 0xffffe000u;
+    xl = __float_as_uint(x - __uint_as_float(xh)) & 0xffffe000u;
+    yl = __float_as_uint(y - __uint_as_float(yh)) & 0xffffe000u;
 }
 
 // Operands of a 16-deep step.  bf16: NT terms.  fp32: two 8-deep tf32 steps s; position k of step
@@ -99,9 +132,7 @@ __device__ __forceinline__ void mma_quad(float (&c)[4][4], const FragA<float, NA
         for (int i = 0; i < 4; ++i) mma_tf32(d[i], a.hi[s], b[i].lo[s]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) c[i][x] += d[i][x];
+    for (int i = 0; i < 4; ++i) add4<false>(c[i], d[i]);
 }
 // Two tiles, the small products in an accumulator of their own (w), so that a chain of such products is half as long.
 template <int NA, int NB>
@@ -135,35 +166,31 @@ template <typename T, int NA, int NB> __device__ __forceinline__ void mma16(floa
             mma_tf32(c, a.hi[s], b.hi[s]);
             mma_tf32(w, a.hi[s], b.lo[s]);
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c[i] += w[i];
+        add4<false>(c, w);
     }
 }
 
 // A from two neighbouring accumulator tiles (16 columns)
 template <int NT>
 __device__ __forceinline__ void frag_from_acc(FragA<__nv_bfloat16, NT>& a, const float (&c0)[4], const float (&c1)[4]) {
-    a.r[0][0] = pack_bf16(c0[0], c0[1]);
-    a.r[0][1] = pack_bf16(c0[2], c0[3]);
-    a.r[0][2] = pack_bf16(c1[0], c1[1]);
-    a.r[0][3] = pack_bf16(c1[2], c1[3]);
     if constexpr (NT > 1) {
-        a.r[1][0] = pack_bf16(c0[0] - bf16_lo(a.r[0][0]), c0[1] - bf16_hi(a.r[0][0]));
-        a.r[1][1] = pack_bf16(c0[2] - bf16_lo(a.r[0][1]), c0[3] - bf16_hi(a.r[0][1]));
-        a.r[1][2] = pack_bf16(c1[0] - bf16_lo(a.r[0][2]), c1[1] - bf16_hi(a.r[0][2]));
-        a.r[1][3] = pack_bf16(c1[2] - bf16_lo(a.r[0][3]), c1[3] - bf16_hi(a.r[0][3]));
+        split_bf16(lo2(c0), a.r[0][0], a.r[1][0]);
+        split_bf16(hi2(c0), a.r[0][1], a.r[1][1]);
+        split_bf16(lo2(c1), a.r[0][2], a.r[1][2]);
+        split_bf16(hi2(c1), a.r[0][3], a.r[1][3]);
+    } else {
+        a.r[0][0] = pack_bf16(c0[0], c0[1]);
+        a.r[0][1] = pack_bf16(c0[2], c0[3]);
+        a.r[0][2] = pack_bf16(c1[0], c1[1]);
+        a.r[0][3] = pack_bf16(c1[2], c1[3]);
     }
 }
 template <int NT>
 __device__ __forceinline__ void frag_from_acc(FragA<float, NT>& a, const float (&c0)[4], const float (&c1)[4]) {
-    split_tf32(c0[0], a.hi[0][0], a.lo[0][0]);
-    split_tf32(c0[2], a.hi[0][1], a.lo[0][1]);
-    split_tf32(c0[1], a.hi[0][2], a.lo[0][2]);
-    split_tf32(c0[3], a.hi[0][3], a.lo[0][3]);
-    split_tf32(c1[0], a.hi[1][0], a.lo[1][0]);
-    split_tf32(c1[2], a.hi[1][1], a.lo[1][1]);
-    split_tf32(c1[1], a.hi[1][2], a.lo[1][2]);
-    split_tf32(c1[3], a.hi[1][3], a.lo[1][3]);
+    split_tf32(c0[0], c0[1], a.hi[0][0], a.lo[0][0], a.hi[0][2], a.lo[0][2]);
+    split_tf32(c0[2], c0[3], a.hi[0][1], a.lo[0][1], a.hi[0][3], a.lo[0][3]);
+    split_tf32(c1[0], c1[1], a.hi[1][0], a.lo[1][0], a.hi[1][2], a.lo[1][2]);
+    split_tf32(c1[2], c1[3], a.hi[1][1], a.lo[1][1], a.hi[1][3], a.lo[1][3]);
 }
 
 // ------------------------------------------------------------------ tiles in shared memory
@@ -203,10 +230,12 @@ template <int COLS, int NT> struct Tile<__nv_bfloat16, COLS, NT> {
         if constexpr (NT > 1) p[plane + r * kLd + c] = __float2bfloat16_rn(v - __bfloat162float(h));
     }
     __device__ __forceinline__ void set2(int r, int c, float v0, float v1) const {  // c even
-        const uint32_t h = pack_bf16(v0, v1);
-        *reinterpret_cast<uint32_t*>(p + r * kLd + c) = h;
-        if constexpr (NT > 1)
-            *reinterpret_cast<uint32_t*>(p + plane + r * kLd + c) = pack_bf16(v0 - bf16_lo(h), v1 - bf16_hi(h));
+        if constexpr (NT > 1) {
+            split_bf16(make_float2(v0, v1), *reinterpret_cast<uint32_t*>(p + r * kLd + c),
+                       *reinterpret_cast<uint32_t*>(p + plane + r * kLd + c));
+        } else {
+            *reinterpret_cast<uint32_t*>(p + r * kLd + c) = pack_bf16(v0, v1);
+        }
     }
     __device__ __forceinline__ void zero(int r, int c) const { p[r * kLd + c] = __float2bfloat16_rn(0.0f); }
     __device__ __forceinline__ void put(int r, int c, T v) const { p[r * kLd + c] = v; }
@@ -297,10 +326,8 @@ template <int COLS, int NT> struct Tile<float, COLS, NT> {
         for (int s = 0; s < 2; ++s) {
             const float2 u = *reinterpret_cast<const float2*>(p + at(m0 + g, k0 + 8 * s + 2 * t));
             const float2 w = *reinterpret_cast<const float2*>(p + at(m0 + g + 8, k0 + 8 * s + 2 * t));
-            split_tf32(u.x, a.hi[s][0], a.lo[s][0]);
-            split_tf32(w.x, a.hi[s][1], a.lo[s][1]);
-            split_tf32(u.y, a.hi[s][2], a.lo[s][2]);
-            split_tf32(w.y, a.hi[s][3], a.lo[s][3]);
+            split_tf32(u.x, u.y, a.hi[s][0], a.lo[s][0], a.hi[s][2], a.lo[s][2]);
+            split_tf32(w.x, w.y, a.hi[s][1], a.lo[s][1], a.hi[s][3], a.lo[s][3]);
         }
     }
     template <int N = NT> __device__ __forceinline__ void a_km(FragA<T, N>& a, int m0, int k0) const {
@@ -320,10 +347,8 @@ template <int COLS, int NT> struct Tile<float, COLS, NT> {
         for (int s = 0; s < 2; ++s) {
             const float2 u = *reinterpret_cast<const float2*>(p + at(n0 + g, k0 + 8 * s + 2 * t));
             const float2 w = *reinterpret_cast<const float2*>(p + at(n0 + 8 + g, k0 + 8 * s + 2 * t));
-            split_tf32(u.x, b0.hi[s][0], b0.lo[s][0]);
-            split_tf32(u.y, b0.hi[s][1], b0.lo[s][1]);
-            split_tf32(w.x, b1.hi[s][0], b1.lo[s][0]);
-            split_tf32(w.y, b1.hi[s][1], b1.lo[s][1]);
+            split_tf32(u.x, u.y, b0.hi[s][0], b0.lo[s][0], b0.hi[s][1], b0.lo[s][1]);
+            split_tf32(w.x, w.y, b1.hi[s][0], b1.lo[s][0], b1.hi[s][1], b1.lo[s][1]);
         }
     }
     template <int N = NT> __device__ __forceinline__ void b_kn(FragB<T, N>& b0, FragB<T, N>& b1, int k0, int n0) const {
@@ -331,10 +356,8 @@ template <int COLS, int NT> struct Tile<float, COLS, NT> {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const int k = k0 + 8 * s + 2 * t;
-            split_tf32(p[at(k, n0 + g)], b0.hi[s][0], b0.lo[s][0]);
-            split_tf32(p[at(k + 1, n0 + g)], b0.hi[s][1], b0.lo[s][1]);
-            split_tf32(p[at(k, n0 + 8 + g)], b1.hi[s][0], b1.lo[s][0]);
-            split_tf32(p[at(k + 1, n0 + 8 + g)], b1.hi[s][1], b1.lo[s][1]);
+            split_tf32(p[at(k, n0 + g)], p[at(k + 1, n0 + g)], b0.hi[s][0], b0.lo[s][0], b0.hi[s][1], b0.lo[s][1]);
+            split_tf32(p[at(k, n0 + 8 + g)], p[at(k + 1, n0 + 8 + g)], b1.hi[s][0], b1.lo[s][0], b1.hi[s][1], b1.lo[s][1]);
         }
     }
     __device__ __forceinline__ void set_t(int r0, int c0, const float (&a)[4], const float (&b)[4]) const {
@@ -375,9 +398,12 @@ template <int NT> struct LowTile<__nv_bfloat16, NT> {
     }
     __device__ __forceinline__ void set2(int bi, int bj, int r, int c, float v0, float v1) const {
         T* q = p + base(bi, bj) + r * kLd + c;
-        const uint32_t h = pack_bf16(v0, v1);
+        uint32_t h = pack_bf16(v0, v1), l = 0;
+        if constexpr (NT > 1) {
+            split_bf16(make_float2(v0, v1), h, l);
+            *reinterpret_cast<uint32_t*>(q + kBlock) = l;
+        }
         *reinterpret_cast<uint32_t*>(q) = h;
-        if constexpr (NT > 1) *reinterpret_cast<uint32_t*>(q + kBlock) = pack_bf16(v0 - bf16_lo(h), v1 - bf16_hi(h));
     }
     __device__ __forceinline__ uint32_t lane_addr(int term, int bi, int bj) const {
         const int lane = threadIdx.x & 31;
@@ -420,10 +446,8 @@ template <int NT> struct LowTile<float, NT> {
         for (int s = 0; s < 2; ++s) {
             const float2 u = *reinterpret_cast<const float2*>(p + at(bi, bj, g, 8 * s + 2 * t));
             const float2 w = *reinterpret_cast<const float2*>(p + at(bi, bj, g + 8, 8 * s + 2 * t));
-            split_tf32(u.x, b0.hi[s][0], b0.lo[s][0]);
-            split_tf32(u.y, b0.hi[s][1], b0.lo[s][1]);
-            split_tf32(w.x, b1.hi[s][0], b1.lo[s][0]);
-            split_tf32(w.y, b1.hi[s][1], b1.lo[s][1]);
+            split_tf32(u.x, u.y, b0.hi[s][0], b0.lo[s][0], b0.hi[s][1], b0.lo[s][1]);
+            split_tf32(w.x, w.y, b1.hi[s][0], b1.lo[s][0], b1.hi[s][1], b1.lo[s][1]);
         }
     }
     __device__ __forceinline__ void b_kn(FragB<T, NT>& b0, FragB<T, NT>& b1, int bi, int bj) const {
@@ -431,10 +455,8 @@ template <int NT> struct LowTile<float, NT> {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const int k = 8 * s + 2 * t;
-            split_tf32(p[at(bi, bj, k, g)], b0.hi[s][0], b0.lo[s][0]);
-            split_tf32(p[at(bi, bj, k + 1, g)], b0.hi[s][1], b0.lo[s][1]);
-            split_tf32(p[at(bi, bj, k, 8 + g)], b1.hi[s][0], b1.lo[s][0]);
-            split_tf32(p[at(bi, bj, k + 1, 8 + g)], b1.hi[s][1], b1.lo[s][1]);
+            split_tf32(p[at(bi, bj, k, g)], p[at(bi, bj, k + 1, g)], b0.hi[s][0], b0.lo[s][0], b0.hi[s][1], b0.lo[s][1]);
+            split_tf32(p[at(bi, bj, k, 8 + g)], p[at(bi, bj, k + 1, 8 + g)], b1.hi[s][0], b1.lo[s][0], b1.hi[s][1], b1.lo[s][1]);
         }
     }
 };
@@ -529,7 +551,7 @@ __device__ __forceinline__ DeltaSeq delta_seq(const int* offsets, int b, int T, 
 // difference c_i - c_j keeps fp32 accuracy however small c is: a token that resets the state (g = -inf,
 // taken as -200, whose exponential is 0 in fp32) does not cost the tokens after it any digits.
 struct alignas(16) ChunkGates {
-    float hi[kChunk], lo[kChunk];  // c
+    float hi[kChunk], lo[kChunk];  // c / ln 2
     float beta[kChunk];
     float ec[kChunk];    // e^c
     float tail[kChunk];  // e^(c_last - c)
@@ -539,11 +561,9 @@ struct alignas(16) ChunkGates {
         return *reinterpret_cast<const float2*>(v + 8 * n + 2 * (threadIdx.x & 3));
     }
 };
-// c[x] *= (token of the pair's scale)
-__device__ __forceinline__ void scale_tokens(float (&c)[4], float2 s) {
-    c[0] *= s.x, c[1] *= s.y, c[2] *= s.x, c[3] *= s.y;
-}
-__device__ __forceinline__ float decay(float hi, float lo) { return ex2((hi + lo) * kLog2e); }
+
+// e^(c_i - c_j) from the differences of the parts
+__device__ __forceinline__ float decay(float hi, float lo) { return ex2(hi + lo); }
 
 __device__ __forceinline__ void add_pair(float& h, float& l, float h2, float l2) {
     // Knuth's two-sum, then the low parts
@@ -570,12 +590,21 @@ __device__ __forceinline__ void chunk_gates(ChunkGates& G, float g0, float g1, f
     float ph = __shfl_up_sync(0xffffffffu, h, 1), pl = __shfl_up_sync(0xffffffffu, l, 1);
     if (lane == 0) ph = pl = 0.0f;
     add_pair(ph, pl, g0, 0.0f);  // the first token's own sum
+    // in units of ln 2, as pairs again
+    auto units = [](float& a, float& b) {
+        constexpr float kLog2eLo = 1.925963033500e-8f;  // log2 e = kLog2e + kLog2eLo
+        const float p = a * kLog2e, e = fmaf(a, kLog2e, -p) + fmaf(b, kLog2e, a * kLog2eLo);
+        a = p + e;
+        b = e - (a - p);
+    };
+    float lth = lh, ltl = ll;
+    units(ph, pl), units(h, l), units(lth, ltl);
     const int i = 2 * lane;
     G.hi[i] = ph, G.lo[i] = pl, G.hi[i + 1] = h, G.lo[i + 1] = l;
     G.beta[i] = b0, G.beta[i + 1] = b1;
     G.ec[i] = decay(ph, pl), G.ec[i + 1] = decay(h, l);
-    G.tail[i] = decay(lh - ph, ll - pl), G.tail[i + 1] = decay(lh - h, ll - l);
-    if (lane == 0) G.last = decay(lh, ll);
+    G.tail[i] = decay(lth - ph, ltl - pl), G.tail[i + 1] = decay(lth - h, ltl - l);
+    if (lane == 0) G.last = decay(lth, ltl);
 }
 
 // ------------------------------------------------------------------ the chunk's triangular system
@@ -593,15 +622,17 @@ __device__ __forceinline__ void chunk_system(const Tile<T, DK, NK>& sK, const Ti
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     // e^(c_i - c_j) of this lane's places of block (bi, bj), zero for j > i (where it may be large without bound)
     auto decays = [&](int bi, int bj, float(&d)[2][4]) {
-        const float2 h0 = G.pair(G.hi, 2 * bj), h1 = G.pair(G.hi, 2 * bj + 1), l0 = G.pair(G.lo, 2 * bj), l1 = G.pair(G.lo, 2 * bj + 1);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = g + 8 * h, i = 16 * bi + r;
-            const float ih = G.hi[i], il = G.lo[i];
-            d[0][2 * h] = bi > bj || 2 * t <= r ? decay(ih - h0.x, il - l0.x) : 0.0f;
-            d[0][2 * h + 1] = bi > bj || 2 * t + 1 <= r ? decay(ih - h0.y, il - l0.y) : 0.0f;
-            d[1][2 * h] = bi > bj || 8 + 2 * t <= r ? decay(ih - h1.x, il - l1.x) : 0.0f;
-            d[1][2 * h + 1] = bi > bj || 9 + 2 * t <= r ? decay(ih - h1.y, il - l1.y) : 0.0f;
+        for (int n = 0; n < 2; ++n) {
+            const float2 jh = G.pair(G.hi, 2 * bj + n), jl = G.pair(G.lo, 2 * bj + n);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = g + 8 * h, j = 8 * n + 2 * t;
+                const float ih = G.hi[16 * bi + r], il = G.lo[16 * bi + r];
+                const float2 v = __fadd2_rn(minus(make_float2(ih, ih), jh), minus(make_float2(il, il), jl));
+                d[n][2 * h] = bi > bj || j <= r ? ex2(v.x) : 0.0f;
+                d[n][2 * h + 1] = bi > bj || j + 1 <= r ? ex2(v.y) : 0.0f;
+            }
         }
     };
     auto product = [&](const Tile<T, DK, NK>& sA, int bi, int bj, float(&c)[2][4]) {
@@ -624,12 +655,15 @@ __device__ __forceinline__ void chunk_system(const Tile<T, DK, NK>& sK, const Ti
         for (int h = 0; h < 2; ++h) {
             const int r = g + 8 * h;
             const float ib = G.beta[16 * w + r];
-            // transposed: the columns of the block side by side (the diagonal itself is not read)
+            // -L transposed: the columns of the block side by side (the diagonal itself is not read)
             float* col = diag + (w * 16 + 2 * t) * 20 + r;
-            col[0] = kk[0][2 * h] * d[0][2 * h] * (kRowBeta ? ib : b0.x);
-            col[20] = kk[0][2 * h + 1] * d[0][2 * h + 1] * (kRowBeta ? ib : b0.y);
-            col[160] = kk[1][2 * h] * d[1][2 * h] * (kRowBeta ? ib : b1.x);
-            col[180] = kk[1][2 * h + 1] * d[1][2 * h + 1] * (kRowBeta ? ib : b1.y);
+            const float2 s0 = kRowBeta ? make_float2(-ib, -ib) : make_float2(-b0.x, -b0.y), s1 = kRowBeta ? s0 : make_float2(-b1.x, -b1.y);
+            const float2 v0 = __fmul2_rn(__fmul2_rn(make_float2(kk[0][2 * h], kk[0][2 * h + 1]), make_float2(d[0][2 * h], d[0][2 * h + 1])), s0);
+            const float2 v1 = __fmul2_rn(__fmul2_rn(make_float2(kk[1][2 * h], kk[1][2 * h + 1]), make_float2(d[1][2 * h], d[1][2 * h + 1])), s1);
+            col[0] = v0.x;
+            col[20] = v0.y;
+            col[160] = v1.x;
+            col[180] = v1.y;
         }
         __syncwarp();
         if constexpr (kWithP) {
@@ -638,30 +672,30 @@ __device__ __forceinline__ void chunk_system(const Tile<T, DK, NK>& sK, const Ti
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
-                    sP.set2(w, w, g + 8 * h, 8 * n + 2 * t, scale * d[n][2 * h] * qk[n][2 * h], scale * d[n][2 * h + 1] * qk[n][2 * h + 1]);
+                for (int n = 0; n < 2; ++n) {
+                    const float2 v = __fmul2_rn(make_float2(qk[n][2 * h], qk[n][2 * h + 1]),
+                                                __fmul2_rn(make_float2(d[n][2 * h], d[n][2 * h + 1]), make_float2(scale, scale)));
+                    sP.set2(w, w, g + 8 * h, 8 * n + 2 * t, v.x, v.y);
+                }
         }
         // column c of (I + L)^-1, L the strictly lower block: x_i = [i = c] - sum_{j < i} L_ij x_j, taken off column
         // by column of L so that the chain is 15 products long
         const int c = lane & 15;
-        float x[16];
+        float2 x[8];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = i == c ? 1.0f : 0.0f;
+        for (int i = 0; i < 8; ++i) x[i] = make_float2(2 * i == c ? 1.0f : 0.0f, 2 * i + 1 == c ? 1.0f : 0.0f);
 #pragma unroll
         for (int j = 0; j < 15; ++j) {
             const float* col = diag + (w * 16 + j) * 20;
+            const float xj = j & 1 ? x[j / 2].y : x[j / 2].x;
+            if (j % 2 == 0) x[j / 2].y = fmaf(col[j + 1], xj, x[j / 2].y);
 #pragma unroll
-            for (int i4 = (j + 1) / 4; i4 < 4; ++i4) {
-                const float4 l = *reinterpret_cast<const float4*>(col + 4 * i4);
-                if (4 * i4 > j) x[4 * i4] = fmaf(-l.x, x[j], x[4 * i4]);
-                if (4 * i4 + 1 > j) x[4 * i4 + 1] = fmaf(-l.y, x[j], x[4 * i4 + 1]);
-                if (4 * i4 + 2 > j) x[4 * i4 + 2] = fmaf(-l.z, x[j], x[4 * i4 + 2]);
-                if (4 * i4 + 3 > j) x[4 * i4 + 3] = fmaf(-l.w, x[j], x[4 * i4 + 3]);
-            }
+            for (int i = j / 2 + 1; i < 8; ++i)
+                x[i] = __ffma2_rn(*reinterpret_cast<const float2*>(col + 2 * i), make_float2(xj, xj), x[i]);
         }
         if (lane < 16) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sE.set(w, w, i, c, x[i]);
+            for (int i = 0; i < 16; ++i) sE.set(w, w, i, c, i & 1 ? x[i / 2].y : x[i / 2].x);
         }
     }
     if (w >= WARPS - 4) {
@@ -677,8 +711,11 @@ __device__ __forceinline__ void chunk_system(const Tile<T, DK, NK>& sK, const Ti
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
-                    to.set2(bi, bj, g + 8 * h, 8 * n + 2 * t, f * d[n][2 * h] * c[n][2 * h], f * d[n][2 * h + 1] * c[n][2 * h + 1]);
+                for (int n = 0; n < 2; ++n) {
+                    const float2 v = __fmul2_rn(make_float2(c[n][2 * h], c[n][2 * h + 1]),
+                                                __fmul2_rn(make_float2(d[n][2 * h], d[n][2 * h + 1]), make_float2(f, f)));
+                    to.set2(bi, bj, g + 8 * h, 8 * n + 2 * t, v.x, v.y);
+                }
         }
     }
 }
