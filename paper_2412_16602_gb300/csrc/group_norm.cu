@@ -70,19 +70,124 @@ struct NormLaunch {
     int first;  // first sample of the launch
 };
 
-template <int ACT> __device__ __forceinline__ float act_value(float z) {
-    if (ACT == VMB_ACT_SILU) return z * rcp(1.0f + ex2(-z * kLog2e));
-    if (ACT == VMB_ACT_GELU) return z * 0.5f * (1.0f + erff(z * 0.70710678118654752f));
+// tanh on the MUFU pipe, good to 2^-11: used where the result is rounded to bf16 (2^-9)
+__device__ __forceinline__ float tanh_fast(float x) {
+    float y;
+    asm("tanh.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+// The logistic function of two values: 1 / (1 + e^-z), for bf16 storage (1 + tanh(z / 2)) / 2 (one MUFU operation for two).
+template <typename T> __device__ __forceinline__ float2 sigmoid2(float2 z) {
+    if constexpr (sizeof(T) == 2) {
+        const float2 h = __fmul2_rn(z, both(0.5f));
+        return __ffma2_rn(make_float2(tanh_fast(h.x), tanh_fast(h.y)), both(0.5f), both(0.5f));
+    } else {
+        const float2 e = __fmul2_rn(z, both(-kLog2e));
+        const float2 d = __fadd2_rn(make_float2(ex2(e.x), ex2(e.y)), both(1.0f));
+        return make_float2(rcp(d.x), rcp(d.y));
+    }
+}
+template <typename T, int ACT> __device__ __forceinline__ float2 act_value(float2 z) {
+    if constexpr (ACT == VMB_ACT_SILU) return __fmul2_rn(z, sigmoid2<T>(z));
+    if constexpr (ACT == VMB_ACT_GELU)
+        return __fmul2_rn(__fmul2_rn(z, both(0.5f)), make_float2(1.0f + erff(z.x * 0.70710678118654752f), 1.0f + erff(z.y * 0.70710678118654752f)));
     return z;
 }
-template <int ACT> __device__ __forceinline__ float act_slope(float z) {
-    if (ACT == VMB_ACT_SILU) {
-        const float s = rcp(1.0f + ex2(-z * kLog2e));
-        return s * fmaf(z, 1.0f - s, 1.0f);
+template <typename T, int ACT> __device__ __forceinline__ float2 act_slope(float2 z) {
+    if constexpr (ACT == VMB_ACT_SILU) {  // s (1 + z (1 - s)) = s + (z s) (1 - s)
+        const float2 s = sigmoid2<T>(z), r = __ffma2_rn(s, both(-1.0f), both(1.0f));
+        return __ffma2_rn(__fmul2_rn(z, s), r, s);
     }
-    if (ACT == VMB_ACT_GELU)
-        return fmaf(z * 0.39894228040143268f, expf(-0.5f * z * z), 0.5f * (1.0f + erff(z * 0.70710678118654752f)));
-    return 1.0f;
+    if constexpr (ACT == VMB_ACT_GELU)
+        return make_float2(fmaf(z.x * 0.39894228040143268f, expf(-0.5f * z.x * z.x), 0.5f * (1.0f + erff(z.x * 0.70710678118654752f))),
+                           fmaf(z.y * 0.39894228040143268f, expf(-0.5f * z.y * z.y), 0.5f * (1.0f + erff(z.y * 0.70710678118654752f))));
+    return both(1.0f);
+}
+
+// A thread's vector of V channels as pairs (V = 1: the pair's second value is not used).
+template <typename T, int V> struct Vec {
+    static constexpr int P = (V + 1) / 2;
+    float2 v[P];
+};
+template <typename T, int V> __device__ __forceinline__ Vec<T, V> load_vec(const T* p) {
+    const NPack<T, V> f = *reinterpret_cast<const NPack<T, V>*>(p);
+    Vec<T, V> r;
+#pragma unroll
+    for (int i = 0; i < Vec<T, V>::P; ++i) r.v[i] = make_float2(io<T>::cvt(f.v[2 * i]), V > 1 ? io<T>::cvt(f.v[(2 * i + 1) % V]) : 0.0f);
+    return r;
+}
+template <typename T, int V> __device__ __forceinline__ void store_vec(T* p, const Vec<T, V>& r) {
+    NPack<T, V> o;
+#pragma unroll
+    for (int i = 0; i < V; ++i) o.v[i] = io<T>::to(i & 1 ? r.v[i / 2].y : r.v[i / 2].x);
+    *reinterpret_cast<NPack<T, V>*>(p) = o;
+}
+template <int V, typename F> __device__ __forceinline__ void fill(float2 (&v)[(V + 1) / 2], F f) {  // v = f(channel of the vector)
+#pragma unroll
+    for (int i = 0; i < (V + 1) / 2; ++i) v[i] = make_float2(f(2 * i), V > 1 ? f(2 * i + 1) : 0.0f);
+}
+
+// y = act(a x + c) over a thread's pixels, a = weight rstd and c = bias - mean a of its channels.
+template <typename T, int V, int ACT>
+__device__ __forceinline__ void apply_rows(const T* x, long long x_step, T* y, long long y_step, int first, int rows, int lanes,
+                                           const float2 (&a)[(V + 1) / 2], const float2 (&c)[(V + 1) / 2]) {
+#pragma unroll 4
+    for (int r = first; r < rows; r += lanes) {
+        Vec<T, V> f = load_vec<T, V>(x + r * x_step);
+#pragma unroll
+        for (int i = 0; i < Vec<T, V>::P; ++i) f.v[i] = act_value<T, ACT>(__ffma2_rn(f.v[i], a[i], c[i]));
+        store_vec<T, V>(y + r * y_step, f);
+    }
+}
+// The sums of dz and of dz (x - mean) over a thread's pixels.
+template <typename T, int V, int ACT>
+__device__ __forceinline__ void slope_sums(const T* x, const T* dy, long long step, int first, int rows, int lanes, const float2 (&a)[(V + 1) / 2],
+                                           const float2 (&c)[(V + 1) / 2], const float2 (&mean)[(V + 1) / 2], float2 (&s1)[(V + 1) / 2],
+                                           float2 (&s2)[(V + 1) / 2]) {
+#pragma unroll 2
+    for (int r = first; r < rows; r += lanes) {
+        const Vec<T, V> f = load_vec<T, V>(x + r * step), d = load_vec<T, V>(dy + r * step);
+#pragma unroll
+        for (int i = 0; i < Vec<T, V>::P; ++i) {
+            const float2 dz = __fmul2_rn(d.v[i], act_slope<T, ACT>(__ffma2_rn(f.v[i], a[i], c[i])));
+            s1[i] = __fadd2_rn(s1[i], dz);
+            s2[i] = __ffma2_rn(dz, __ffma2_rn(mean[i], both(-1.0f), f.v[i]), s2[i]);
+        }
+    }
+}
+// dx = rstd (w dz - m1) - rstd^2 m2 (x - mean) = a dz - k1 - k2 (x - mean)
+template <typename T, int V, int ACT>
+__device__ __forceinline__ void dx_rows(const T* x, const T* dy, long long step, T* dx, long long dx_step, int first, int rows, int lanes,
+                                        const float2 (&a)[(V + 1) / 2], const float2 (&c)[(V + 1) / 2], const float2 (&mean)[(V + 1) / 2],
+                                        const float2 (&k1)[(V + 1) / 2], const float2 (&k2)[(V + 1) / 2]) {
+#pragma unroll 2
+    for (int r = first; r < rows; r += lanes) {
+        Vec<T, V> f = load_vec<T, V>(x + r * step);
+        const Vec<T, V> d = load_vec<T, V>(dy + r * step);
+#pragma unroll
+        for (int i = 0; i < Vec<T, V>::P; ++i) {
+            const float2 dz = __fmul2_rn(d.v[i], act_slope<T, ACT>(__ffma2_rn(f.v[i], a[i], c[i])));
+            const float2 t = __ffma2_rn(__ffma2_rn(mean[i], both(-1.0f), f.v[i]), k2[i], k1[i]);
+            f.v[i] = __ffma2_rn(t, both(-1.0f), __fmul2_rn(a[i], dz));
+        }
+        store_vec<T, V>(dx + r * dx_step, f);
+    }
+}
+// Differences to the tile's first pixel and their squares, summed over a thread's pixels.
+template <typename T, int V>
+__device__ __forceinline__ void pivot_sums(const T* x, long long step, int first, int rows, int lanes, const float2 (&pivot)[(V + 1) / 2],
+                                           float2 (&s1)[(V + 1) / 2], float2 (&s2)[(V + 1) / 2]) {
+#pragma unroll 4
+    for (int r = first; r < rows; r += lanes) {
+        const Vec<T, V> f = load_vec<T, V>(x + r * step);
+#pragma unroll
+        for (int i = 0; i < Vec<T, V>::P; ++i) {
+            const float2 d = __ffma2_rn(pivot[i], both(-1.0f), f.v[i]);
+            s1[i] = __fadd2_rn(s1[i], d);
+            s2[i] = __ffma2_rn(d, d, s2[i]);
+        }
+    }
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -124,29 +229,18 @@ __global__ void __launch_bounds__(kNormThreads) norm_stats_kernel(NormLaunch c) 
     for (int col0 = 0; col0 < Cv; col0 += kNormThreads) {
         const int cols = min(Cv - col0, kNormThreads), lanes = kNormThreads / cols;
         const int col = tid % cols, rl = tid / cols;
-        float s1[V] = {}, s2[V] = {}, pivot[V];
-        int n = 0;
         if (rl < lanes && rl < rows) {
             const T* p = x + (long long)(col0 + col) * V;
-            const NPack<T, V> f = *reinterpret_cast<const NPack<T, V>*>(p + (long long)rl * C);
-#pragma unroll
-            for (int i = 0; i < V; ++i) pivot[i] = io<T>::cvt(f.v[i]);
-            n = (rows - rl + lanes - 1) / lanes;
-#pragma unroll 4
-            for (int r = rl; r < rows; r += lanes) {
-                const NPack<T, V> f = *reinterpret_cast<const NPack<T, V>*>(p + (long long)r * C);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float d = io<T>::cvt(f.v[i]) - pivot[i];
-                    s1[i] += d;
-                    s2[i] = fmaf(d, d, s2[i]);
-                }
-            }
+            const Vec<T, V> f = load_vec<T, V>(p + (long long)rl * C);
+            float2 s1[Vec<T, V>::P] = {}, s2[Vec<T, V>::P] = {};
+            pivot_sums<T, V>(p, C, rl, rows, lanes, f.v, s1, s2);
+            const float inv = 1.0f / (float)((rows - rl + lanes - 1) / lanes);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float m = s1[i] / n;
-                scratch[(tid * V + i) * 2] = pivot[i] + m;
-                scratch[(tid * V + i) * 2 + 1] = fmaf(-m, s1[i], s2[i]);
+                const float t1 = i & 1 ? s1[i / 2].y : s1[i / 2].x, t2 = i & 1 ? s2[i / 2].y : s2[i / 2].x;
+                const float m = t1 * inv;
+                scratch[(tid * V + i) * 2] = (i & 1 ? f.v[i / 2].y : f.v[i / 2].x) + m;
+                scratch[(tid * V + i) * 2 + 1] = fmaf(-m, t1, t2);
             }
         }
         __syncthreads();
@@ -215,25 +309,25 @@ __global__ void __launch_bounds__(kNormThreads) norm_apply_kernel(NormLaunch c) 
         const int cols = min(Cv - col0, kNormThreads), lanes = kNormThreads / cols;
         const int ch = (col0 + tid % cols) * V, rl = tid / cols;
         if (rl >= lanes) continue;
-        float mean[V], rstd[V], wt[V], bs[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float2 s = __ldcg(&st[(ch + i) / m]);
-            mean[i] = s.x;
-            rstd[i] = s.y;
-            wt[i] = a.weight ? a.weight[ch + i] : 1.0f;
-            bs[i] = a.bias ? a.bias[ch + i] : 0.0f;
-        }
-#pragma unroll 4
-        for (int r = rl; r < rows; r += lanes) {
-            const NPack<T, V> f = *reinterpret_cast<const NPack<T, V>*>(x + (long long)r * C + ch);
-            NPack<T, V> o;
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                o.v[i] = io<T>::to(act_value<ACT>(fmaf((io<T>::cvt(f.v[i]) - mean[i]) * rstd[i], wt[i], bs[i])));
-            *reinterpret_cast<NPack<T, V>*>(y + (long long)r * C + ch) = o;
-        }
+        float2 ca[Vec<T, V>::P], cc[Vec<T, V>::P];
+        fill<V>(ca, [&](int i) { return __ldcg(&st[(ch + i) / m]).y * (a.weight ? a.weight[ch + i] : 1.0f); });
+        fill<V>(cc, [&](int i) {
+            const float v = i & 1 ? ca[i / 2].y : ca[i / 2].x;
+            return fmaf(-__ldcg(&st[(ch + i) / m]).x, v, a.bias ? a.bias[ch + i] : 0.0f);
+        });
+        apply_rows<T, V, ACT>(x + ch, C, y + ch, C, rl, rows, lanes, ca, cc);
     }
+}
+
+// Of a thread's channels: a = weight rstd, c = bias - mean a, mean.
+template <typename T, int V>
+__device__ __forceinline__ void channel_values(const NormArgs& n, const float2* st, int ch, int m, float2 (&a)[(V + 1) / 2], float2 (&c)[(V + 1) / 2],
+                                               float2 (&mean)[(V + 1) / 2]) {
+    fill<V>(mean, [&](int i) { return st[(ch + i) / m].x; });
+    fill<V>(a, [&](int i) { return st[(ch + i) / m].y * (n.weight ? n.weight[ch + i] : 1.0f); });
+    fill<V>(c, [&](int i) {
+        return fmaf(-(i & 1 ? mean[i / 2].y : mean[i / 2].x), i & 1 ? a[i / 2].y : a[i / 2].x, n.bias ? n.bias[ch + i] : 0.0f);
+    });
 }
 
 // First pass of the gradients: per channel sums of dz and dz n over a tile; the sample's last tile joins them,
@@ -255,32 +349,17 @@ __global__ void __launch_bounds__(kNormThreads) norm_sums_kernel(NormLaunch c) {
     for (int col0 = 0; col0 < Cv; col0 += kNormThreads) {
         const int cols = min(Cv - col0, kNormThreads), lanes = kNormThreads / cols;
         const int ch = (col0 + tid % cols) * V, rl = tid / cols;
-        float s1[V] = {}, s2[V] = {};
+        float2 s1[Vec<T, V>::P] = {}, s2[Vec<T, V>::P] = {};
         if (rl < lanes) {
-            float mean[V], rstd[V], wt[V], bs[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float2 s = st[(ch + i) / m];
-                mean[i] = s.x;
-                rstd[i] = s.y;
-                wt[i] = a.weight ? a.weight[ch + i] : 1.0f;
-                bs[i] = a.bias ? a.bias[ch + i] : 0.0f;
-            }
-#pragma unroll 2
-            for (int r = rl; r < rows; r += lanes) {
-                const NPack<T, V> f = *reinterpret_cast<const NPack<T, V>*>(x + (long long)r * C + ch);
-                const NPack<T, V> d = *reinterpret_cast<const NPack<T, V>*>(dy + (long long)r * C + ch);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float n = (io<T>::cvt(f.v[i]) - mean[i]) * rstd[i];
-                    const float dz = io<T>::cvt(d.v[i]) * act_slope<ACT>(fmaf(n, wt[i], bs[i]));
-                    s1[i] += dz;
-                    s2[i] = fmaf(dz, n, s2[i]);
-                }
-            }
+            float2 ca[Vec<T, V>::P], cc[Vec<T, V>::P], mu[Vec<T, V>::P];
+            channel_values<T, V>(a, st, ch, m, ca, cc, mu);
+            slope_sums<T, V, ACT>(x + ch, dy + ch, C, rl, rows, lanes, ca, cc, mu, s1, s2);
         }
 #pragma unroll
-        for (int i = 0; i < V; ++i) scratch[(tid * V + i) * 2] = s1[i], scratch[(tid * V + i) * 2 + 1] = s2[i];
+        for (int i = 0; i < V; ++i) {
+            scratch[(tid * V + i) * 2] = i & 1 ? s1[i / 2].y : s1[i / 2].x;
+            scratch[(tid * V + i) * 2 + 1] = (rl < lanes ? st[(ch + i) / m].y : 0.0f) * (i & 1 ? s2[i / 2].y : s2[i / 2].x);
+        }
         __syncthreads();
         for (int k = tid; k < cols * V; k += kNormThreads) {
             float t1 = 0.0f, t2 = 0.0f;
@@ -352,30 +431,11 @@ __global__ void __launch_bounds__(kNormThreads) norm_dx_kernel(NormLaunch c) {
         const int cols = min(Cv - col0, kNormThreads), lanes = kNormThreads / cols;
         const int ch = (col0 + tid % cols) * V, rl = tid / cols;
         if (rl >= lanes) continue;
-        float mean[V], rstd[V], wt[V], bs[V], m1[V], m2[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float2 s = st[(ch + i) / m], q = __ldcg(&mn[(ch + i) / m]);
-            mean[i] = s.x;
-            rstd[i] = s.y;
-            m1[i] = q.x;
-            m2[i] = q.y;
-            wt[i] = a.weight ? a.weight[ch + i] : 1.0f;
-            bs[i] = a.bias ? a.bias[ch + i] : 0.0f;
-        }
-#pragma unroll 2
-        for (int r = rl; r < rows; r += lanes) {
-            const NPack<T, V> f = *reinterpret_cast<const NPack<T, V>*>(x + (long long)r * C + ch);
-            const NPack<T, V> d = *reinterpret_cast<const NPack<T, V>*>(dy + (long long)r * C + ch);
-            NPack<T, V> o;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float n = (io<T>::cvt(f.v[i]) - mean[i]) * rstd[i];
-                const float dz = io<T>::cvt(d.v[i]) * act_slope<ACT>(fmaf(n, wt[i], bs[i]));
-                o.v[i] = io<T>::to(rstd[i] * (fmaf(wt[i], dz, -m1[i]) - n * m2[i]));
-            }
-            *reinterpret_cast<NPack<T, V>*>(dx + (long long)r * C + ch) = o;
-        }
+        float2 ca[Vec<T, V>::P], cc[Vec<T, V>::P], mu[Vec<T, V>::P], k1[Vec<T, V>::P], k2[Vec<T, V>::P];
+        channel_values<T, V>(a, st, ch, m, ca, cc, mu);
+        fill<V>(k1, [&](int i) { return st[(ch + i) / m].y * __ldcg(&mn[(ch + i) / m]).x; });
+        fill<V>(k2, [&](int i) { return st[(ch + i) / m].y * (st[(ch + i) / m].y * __ldcg(&mn[(ch + i) / m]).y); });
+        dx_rows<T, V, ACT>(x + ch, dy + ch, C, dx + ch, C, rl, rows, lanes, ca, cc, mu, k1, k2);
     }
 }
 
@@ -430,11 +490,11 @@ struct SlabLaunch {
 // Per-channel values of a thread (one vector of V channels) summed over the threads of its column, in order, and handed
 // to `put(channel, sum)`.
 template <int V, typename Put>
-__device__ __forceinline__ void column_sums(const float (&v)[V], float* scratch, int width, int cols, int lanes, Put put) {
+__device__ __forceinline__ void column_sums(const float2 (&v)[(V + 1) / 2], float* scratch, int width, int cols, int lanes, Put put) {
     const int tid = threadIdx.x;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < V; ++i) scratch[tid * V + i] = v[i];
+    for (int i = 0; i < V; ++i) scratch[tid * V + i] = i & 1 ? v[i / 2].y : v[i / 2].x;
     __syncthreads();
     for (int ch = tid; ch < width; ch += kSlabThreads) {
         float s = 0.0f;
@@ -468,29 +528,12 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_kernel(SlabLaunc
         for (int r = rl; r < rows; r += lanes) cp_async16(tile + (long long)r * width + col * V, x + (long long)r * a.C + col * V, 16);
     cp_async_commit();
     cp_async_wait<0>();
-    float mean[V], rstd[V], wt[V], bs[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        wt[i] = a.weight && on ? a.weight[ch0 + col * V + i] : 1.0f;
-        bs[i] = a.bias && on ? a.bias[ch0 + col * V + i] : 0.0f;
-    }
     __syncthreads();
     {  // sums of the differences to the tile's first pixel, and of their squares
-        float s1[V] = {}, s2[V] = {}, pivot[V];
+        float2 s1[Vec<T, V>::P] = {}, s2[Vec<T, V>::P] = {};
         if (on && rows > 0) {
-            const NPack<T, V> f = *reinterpret_cast<const NPack<T, V>*>(tile + col * V);
-#pragma unroll
-            for (int i = 0; i < V; ++i) pivot[i] = io<T>::cvt(f.v[i]);
-#pragma unroll 4
-            for (int r = rl; r < rows; r += lanes) {
-                const NPack<T, V> e = *reinterpret_cast<const NPack<T, V>*>(tile + (long long)r * width + col * V);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float d = io<T>::cvt(e.v[i]) - pivot[i];
-                    s1[i] += d;
-                    s2[i] = fmaf(d, d, s2[i]);
-                }
-            }
+            const Vec<T, V> f = load_vec<T, V>(tile + col * V);
+            pivot_sums<T, V>(tile + col * V, width, rl, rows, lanes, f.v, s1, s2);
         }
         const float inv = 1.0f / (float)max(rows, 1);
         column_sums<V>(s1, scratch, width, cols, lanes, [&](int ch, float s) { sum1[ch] = s; });
@@ -534,22 +577,13 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_kernel(SlabLaunc
     }
     __syncthreads();
     if (on) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float2 v = all[(col * V + i) / m];
-            mean[i] = v.x;
-            rstd[i] = v.y;
-        }
-        T* y = (T*)a.y + (b * a.L + r0) * a.C + ch0 + col * V;
-#pragma unroll 2
-        for (int r = rl; r < rows; r += lanes) {
-            const NPack<T, V> f = *reinterpret_cast<const NPack<T, V>*>(tile + (long long)r * width + col * V);
-            NPack<T, V> o;
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                o.v[i] = io<T>::to(act_value<ACT>(fmaf((io<T>::cvt(f.v[i]) - mean[i]) * rstd[i], wt[i], bs[i])));
-            *reinterpret_cast<NPack<T, V>*>(y + (long long)r * a.C) = o;
-        }
+        float2 ca[Vec<T, V>::P], cc[Vec<T, V>::P];
+        const int ch = ch0 + col * V;
+        fill<V>(ca, [&](int i) { return all[(col * V + i) / m].y * (a.weight ? a.weight[ch + i] : 1.0f); });
+        fill<V>(cc, [&](int i) {
+            return fmaf(-all[(col * V + i) / m].x, i & 1 ? ca[i / 2].y : ca[i / 2].x, a.bias ? a.bias[ch + i] : 0.0f);
+        });
+        apply_rows<T, V, ACT>(tile + col * V, width, (T*)a.y + (b * a.L + r0) * a.C + ch, a.C, rl, rows, lanes, ca, cc);
     }
     cl.sync();  // the others may still read this CTA's sums
 }
@@ -583,36 +617,16 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_grad_kernel(Slab
         }
     }
     cp_async_commit();
-    float mean[V], rstd[V], wt[V], bs[V];
+    float2 ca[Vec<T, V>::P], cc[Vec<T, V>::P], mu[Vec<T, V>::P];
     const float2* st = reinterpret_cast<const float2*>(a.stats) + (long long)b * a.G;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int ch = ch0 + (on ? col * V + i : 0);
-        const float2 v = st[ch / m];
-        mean[i] = v.x;
-        rstd[i] = v.y;
-        wt[i] = a.weight ? a.weight[ch] : 1.0f;
-        bs[i] = a.bias ? a.bias[ch] : 0.0f;
-    }
+    const int mych = ch0 + (on ? col * V : 0);
+    channel_values<T, V>(a, st, mych, m, ca, cc, mu);
     cp_async_wait<0>();  // (a thread reads back what it copied itself)
     {
-        float s1[V] = {}, s2[V] = {};
-        if (on) {
-#pragma unroll 2
-            for (int r = rl; r < rows; r += lanes) {
-                const NPack<T, V> f = *reinterpret_cast<const NPack<T, V>*>(tx + (long long)r * width + col * V);
-                NPack<T, V> d = *reinterpret_cast<const NPack<T, V>*>(td + (long long)r * width + col * V);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float n = (io<T>::cvt(f.v[i]) - mean[i]) * rstd[i];
-                    const float dz = io<T>::cvt(d.v[i]) * act_slope<ACT>(fmaf(n, wt[i], bs[i]));
-                    s1[i] += dz;
-                    s2[i] = fmaf(dz, n, s2[i]);
-                }
-            }
-        }
+        float2 s1[Vec<T, V>::P] = {}, s2[Vec<T, V>::P] = {};
+        if (on) slope_sums<T, V, ACT>(tx + col * V, td + col * V, width, rl, rows, lanes, ca, cc, mu, s1, s2);
         column_sums<V>(s1, scratch, width, cols, lanes, [&](int ch, float s) { sum1[ch] = s; });
-        column_sums<V>(s2, scratch, width, cols, lanes, [&](int ch, float s) { sum2[ch] = s; });
+        column_sums<V>(s2, scratch, width, cols, lanes, [&](int ch, float s) { sum2[ch] = st[(ch0 + ch) / m].y * s; });
     }
     cl.sync();
     // the cluster's sums: every CTA the groups' means, rank 0 also the channels'
@@ -638,27 +652,10 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_grad_kernel(Slab
     }
     __syncthreads();
     if (on) {
-        T* dx = (T*)a.dx + at + col * V;
-        float m1[V], m2[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float2 v = mine[(col * V + i) / m];
-            m1[i] = v.x;
-            m2[i] = v.y;
-        }
-#pragma unroll 2
-        for (int r = rl; r < rows; r += lanes) {
-            const NPack<T, V> f = *reinterpret_cast<const NPack<T, V>*>(tx + (long long)r * width + col * V);
-            const NPack<T, V> d = *reinterpret_cast<const NPack<T, V>*>(td + (long long)r * width + col * V);
-            NPack<T, V> o;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float n = (io<T>::cvt(f.v[i]) - mean[i]) * rstd[i];
-                const float dz = io<T>::cvt(d.v[i]) * act_slope<ACT>(fmaf(n, wt[i], bs[i]));
-                o.v[i] = io<T>::to(rstd[i] * (fmaf(wt[i], dz, -m1[i]) - n * m2[i]));
-            }
-            *reinterpret_cast<NPack<T, V>*>(dx + (long long)r * a.C) = o;
-        }
+        float2 k1[Vec<T, V>::P], k2[Vec<T, V>::P];
+        fill<V>(k1, [&](int i) { return st[(mych + i) / m].y * mine[(col * V + i) / m].x; });
+        fill<V>(k2, [&](int i) { return st[(mych + i) / m].y * (st[(mych + i) / m].y * mine[(col * V + i) / m].y); });
+        dx_rows<T, V, ACT>(tx + col * V, td + col * V, width, (T*)a.dx + at + col * V, a.C, rl, rows, lanes, ca, cc, mu, k1, k2);
     }
     cl.sync();
     if (rank != 0 || (!a.dweight && !a.dbias)) return;

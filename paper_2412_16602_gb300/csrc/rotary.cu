@@ -39,66 +39,73 @@ __device__ __forceinline__ float2 turned(float u, float v, float2 w) {
 
 // A head's items: half: vectors of V pairs (V channels from each half); interleaved: vectors of V channels (V / 2 pairs);
 // then the vectors of V channels that stay as they are (kLoose, for pairs in rows of no alignment: single channels).
-// A thread keeps its items of a token and goes from token to
-// token, so that nothing is divided in the loop; four tokens' values are read before the first is written.
-template <typename T, int V, bool kInter, bool kLoose>
-__device__ __forceinline__ void rotate_heads(const T* src, T* dst, const float2* table, int tokens, long long src_t, int H, int D, int P) {
-    constexpr int U = 4;
-    const int turns = kInter ? 2 * P / V : P / V, items = turns + (D - 2 * P) / (kLoose ? 1 : V), per = H * items;
-    const int lanes = per < kRotThreads ? kRotThreads / per : 1;
-    const long long dst_t = (long long)H * D;
-    for (int e0 = threadIdx.x; e0 < per * lanes; e0 += kRotThreads) {
-        const int first = lanes > 1 ? e0 / per : 0, e = lanes > 1 ? e0 - first * per : e0, h = e / items, j = e - h * items;
-        const bool two = !kInter && j < turns;
-        const long long at = (long long)h * D + (j >= turns ? 2 * P + (j - turns) * (kLoose ? 1 : V) : j * V);
-        const T *s0 = src + at, *s1 = s0 + P;
-        T *d0 = dst + at, *d1 = d0 + P;
-        const float2* cs = table + j * (kInter ? V / 2 : V);
-        for (int t0 = first; t0 < tokens; t0 += U * lanes) {
-            Pack<T, V, kLoose> a[U], b[U];
+// A thread keeps its items of a token, of q and k alike, and goes from token to token, so that nothing is divided in
+// the loop; kBatch tokens' values are read before the first is written, the first batch before the sines are computed.
+constexpr int kBatch = 4;
+template <typename T, int V, bool kInter, bool kLoose> struct Turner {
+    const T *s0, *s1;
+    T *d0, *d1;
+    const float2* cs;
+    long long src_t, dst_t;
+    int first, lanes;  // tokens first, first + lanes, ...
+    bool turns, two;
+    Pack<T, V, kLoose> a[kBatch], b[kBatch];
+
+    __device__ __forceinline__ void set(const T* src, T* dst, const float2* table, long long st, int H, int D, int P, int e, int items, int n) {
+        const int h = e / items, j = e - h * items;
+        turns = j < n;
+        two = !kInter && turns;
+        const long long at = (long long)h * D + (turns ? j * V : 2 * P + (j - n) * (kLoose ? 1 : V));
+        s0 = src + at, s1 = s0 + P;
+        d0 = dst + at, d1 = d0 + P;
+        cs = table + j * (kInter ? V / 2 : V);
+        src_t = st, dst_t = (long long)H * D;
+    }
+    __device__ __forceinline__ void read(int t0, int tokens) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int t = t0 + u * lanes;
-                if (t >= tokens) break;
-                if (kLoose && j >= turns) {
-                    a[u].v[0] = s0[t * src_t];
-                    continue;
-                }
-                a[u] = *reinterpret_cast<const Pack<T, V, kLoose>*>(s0 + t * src_t);
-                if (two) b[u] = *reinterpret_cast<const Pack<T, V, kLoose>*>(s1 + t * src_t);
+        for (int u = 0; u < kBatch; ++u) {
+            const int t = t0 + u * lanes;
+            if (t >= tokens) break;
+            if (kLoose && !turns) {
+                a[u].v[0] = s0[t * src_t];
+                continue;
             }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int t = t0 + u * lanes;
-                if (t >= tokens) break;
-                if (kLoose && j >= turns) {
-                    d0[t * dst_t] = a[u].v[0];
-                    continue;
-                }
-                if (j < turns) {
-                    const float2* w = cs + t * P;
-                    if constexpr (kInter) {
-#pragma unroll
-                        for (int x = 0; x < V / 2; ++x) {
-                            const float2 o = turned(io<T>::cvt(a[u].v[2 * x]), io<T>::cvt(a[u].v[2 * x + 1]), w[x]);
-                            a[u].v[2 * x] = io<T>::to(o.x);
-                            a[u].v[2 * x + 1] = io<T>::to(o.y);
-                        }
-                    } else {
-#pragma unroll
-                        for (int x = 0; x < V; ++x) {
-                            const float2 o = turned(io<T>::cvt(a[u].v[x]), io<T>::cvt(b[u].v[x]), w[x]);
-                            a[u].v[x] = io<T>::to(o.x);
-                            b[u].v[x] = io<T>::to(o.y);
-                        }
-                        *reinterpret_cast<Pack<T, V, kLoose>*>(d1 + t * dst_t) = b[u];
-                    }
-                }
-                *reinterpret_cast<Pack<T, V, kLoose>*>(d0 + t * dst_t) = a[u];
-            }
+            a[u] = *reinterpret_cast<const Pack<T, V, kLoose>*>(s0 + t * src_t);
+            if (two) b[u] = *reinterpret_cast<const Pack<T, V, kLoose>*>(s1 + t * src_t);
         }
     }
-}
+    __device__ __forceinline__ void write(int t0, int tokens, int P) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int t = t0 + u * lanes;
+            if (t >= tokens) break;
+            if (kLoose && !turns) {
+                d0[t * dst_t] = a[u].v[0];
+                continue;
+            }
+            if (turns) {
+                const float2* w = cs + t * P;
+                if constexpr (kInter) {
+#pragma unroll
+                    for (int x = 0; x < V / 2; ++x) {
+                        const float2 o = turned(io<T>::cvt(a[u].v[2 * x]), io<T>::cvt(a[u].v[2 * x + 1]), w[x]);
+                        a[u].v[2 * x] = io<T>::to(o.x);
+                        a[u].v[2 * x + 1] = io<T>::to(o.y);
+                    }
+                } else {
+#pragma unroll
+                    for (int x = 0; x < V; ++x) {
+                        const float2 o = turned(io<T>::cvt(a[u].v[x]), io<T>::cvt(b[u].v[x]), w[x]);
+                        a[u].v[x] = io<T>::to(o.x);
+                        b[u].v[x] = io<T>::to(o.y);
+                    }
+                    *reinterpret_cast<Pack<T, V, kLoose>*>(d1 + t * dst_t) = b[u];
+                }
+            }
+            *reinterpret_cast<Pack<T, V, kLoose>*>(d0 + t * dst_t) = a[u];
+        }
+    }
+};
 
 template <typename T, int V, bool kInter, bool kLoose>
 __global__ void __launch_bounds__(kRotThreads) rotary_kernel(RotaryArgs a, int per_block, int blocks_per_row) {
@@ -108,6 +115,26 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(RotaryArgs a, int p
     pdl_wait();
     const int b = blockIdx.x / blocks_per_row, t0 = (blockIdx.x % blocks_per_row) * per_block;
     const int n = min(per_block, a.T - t0);
+    const int turns = kInter ? 2 * P / V : P / V, items = turns + (a.D - 2 * P) / (kLoose ? 1 : V);
+    const int per_q = a.Hq * items, per = per_q + a.Hk * items;
+    Turner<T, V, kInter, kLoose> w;
+    w.lanes = per < kRotThreads ? kRotThreads / per : 1;
+    int e0 = threadIdx.x;
+    auto set = [&]() {
+        w.first = w.lanes > 1 ? e0 / per : 0;
+        const int e = w.lanes > 1 ? e0 - w.first * per : e0;
+        if (e < per_q)
+            w.set((const T*)a.q + b * a.q_b + t0 * a.q_t, (T*)a.q_out + ((long long)b * a.T + t0) * a.Hq * a.D, table, a.q_t, a.Hq, a.D, P, e,
+                  items, turns);
+        else
+            w.set((const T*)a.k + b * a.k_b + t0 * a.k_t, (T*)a.k_out + ((long long)b * a.T + t0) * a.Hk * a.D, table, a.k_t, a.Hk, a.D, P,
+                  e - per_q, items, turns);
+    };
+    const bool on = e0 < per * w.lanes;
+    if (on) {
+        set();
+        w.read(w.first, n);
+    }
     for (int i = threadIdx.x; i < n * P; i += kRotThreads) {
         const int tok = t0 + i / P, j = i % P;
         int axis = 0;
@@ -124,19 +151,27 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(RotaryArgs a, int p
         table[i] = make_float2(cs.x, a.inverse ? -cs.y : cs.y);
     }
     __syncthreads();
-    rotate_heads<T, V, kInter, kLoose>((const T*)a.q + b * a.q_b + t0 * a.q_t, (T*)a.q_out + ((long long)b * a.T + t0) * a.Hq * a.D, table, n, a.q_t,
-                               a.Hq, a.D, P);
-    if (a.k)
-        rotate_heads<T, V, kInter, kLoose>((const T*)a.k + b * a.k_b + t0 * a.k_t, (T*)a.k_out + ((long long)b * a.T + t0) * a.Hk * a.D, table, n,
-                                   a.k_t, a.Hk, a.D, P);
+    if (!on) return;
+    for (;;) {
+        for (int t = w.first;;) {
+            w.write(t, n, P);
+            t += kBatch * w.lanes;
+            if (t >= n) break;
+            w.read(t, n);
+        }
+        e0 += kRotThreads;
+        if (e0 >= per * w.lanes) return;
+        set();
+        w.read(w.first, n);
+    }
 }
 
 template <typename T, int V, bool kLoose = false>
 vmb_status launch_v(const RotaryArgs& a, cudaStream_t stream) {
     const int P = a.pair_end[a.axes - 1];
-    // tokens per block: about eight vectors per thread, within 32 KB of sines, and enough blocks for every SM
+    // tokens per block: two batches per thread, within 32 KB of sines, and enough blocks for every SM
     const long long per_token = (long long)(a.Hq + a.Hk) * ((a.interleaved ? 2 * P / V : P / V) + (a.D - 2 * P) / V);
-    long long per = (8 * kRotThreads + per_token - 1) / per_token;
+    long long per = per_token <= kRotThreads ? 2 * kBatch * (kRotThreads / per_token) : 2 * kBatch;
     const long long most = 32 * 1024 / (8 * (long long)P), spread = ((long long)a.B * a.T + 2 * device_sm_count() - 1) / (2 * device_sm_count());
     per = per < most ? per : most;
     per = per < spread ? per : spread;
