@@ -446,12 +446,15 @@ __global__ void __launch_bounds__(kNormThreads) norm_dx_kernel(NormLaunch c) {
 struct NormSlab {
     int width, slabs, ctas, rows;
 };
-// Two CTAs per SM, so that one loads or stores while the other computes; a cluster of eight is the portable limit.
+// Two CTAs per SM, so that one loads or stores while the other computes; a cluster of eight is the portable limit (16
+// CTAs of half the size were slower: 66 against 44 us for 8 x 128 x 128 x 192 in bf16).
+constexpr int kSlabCluster = 8, kSlabThreads = 256;
 constexpr size_t kSlabSmem = 113 * 1024;
-constexpr int kSlabThreads = 256;
-// The tile, a vector of sums per thread, two sums per channel and one pair per group.
-inline size_t slab_smem(long long rows, int width, int groups, size_t es, bool grads) {
-    return (((size_t)rows * width * es * (grads ? 2 : 1) + 15) & ~(size_t)15) + kSlabThreads * (16 / es) * 4 + (size_t)width * 8 + (size_t)groups * 8;
+// The tile, a sum per thread and channel of its vector, two partial sums per thread, and what the cluster's CTAs send:
+// forward one pair per group, gradients one per channel.
+inline size_t slab_smem(long long rows, int width, int groups, int ctas, size_t es, bool grads) {
+    return (((size_t)rows * width * es * (grads ? 2 : 1) + 15) & ~(size_t)15) + kSlabThreads * (16 / es) * 4 + (size_t)(width > kSlabThreads ? width : kSlabThreads) * 8 +
+           (size_t)ctas * (grads ? width : groups) * 8 + (size_t)groups * 8;
 }
 
 // Channels per slab: as many groups as a cluster holds, at least 32 bytes of every pixel (a sector of memory), fewer as
@@ -463,8 +466,8 @@ bool norm_slab(int B, long long L, int C, int G, vmb_dtype dtype, bool grads, in
     int best = 0;
     for (int g = 1; g <= G; ++g) {
         if (G % g || (g * m) % v || g * m / v > kSlabThreads || g * m > 2048) continue;
-        if (slab_smem((L + 7) / 8, g * m, g, es, grads) > kSlabSmem) break;
-        const long long ctas = (long long)B * (G / g) * 8;
+        if (slab_smem((L + kSlabCluster - 1) / kSlabCluster, g * m, g, kSlabCluster, es, grads) > kSlabSmem) break;
+        const long long ctas = (long long)B * (G / g) * kSlabCluster;
         if (best && (size_t)best * es >= 64 && ctas < 2LL * sms) break;
         best = g * m;
     }
@@ -472,8 +475,8 @@ bool norm_slab(int B, long long L, int C, int G, vmb_dtype dtype, bool grads, in
     out->width = best;
     out->slabs = C / best;
     int n = 1;
-    while (n < 8 && (slab_smem((L + n - 1) / n, best, best / m, es, grads) > kSlabSmem ||
-                     ((long long)B * out->slabs * n < 2LL * sms && L / (2 * n) >= 16)))
+    while (n < kSlabCluster && (slab_smem((L + n - 1) / n, best, best / m, n, es, grads) > kSlabSmem ||
+                                ((long long)B * out->slabs * n < 2LL * sms && L / (2 * n) >= 16)))
         n *= 2;
     out->ctas = n;
     out->rows = (int)((L + n - 1) / n);
@@ -487,20 +490,28 @@ struct SlabLaunch {
     unsigned* counter;
 };
 
-// Per-channel values of a thread (one vector of V channels) summed over the threads of its column, in order, and handed
-// to `put(channel, sum)`.
-template <int V, typename Put>
-__device__ __forceinline__ void column_sums(const float2 (&v)[(V + 1) / 2], float* scratch, int width, int cols, int lanes, Put put) {
-    const int tid = threadIdx.x;
-    __syncthreads();
+// A thread's sums of its V channels, two each, summed over the threads of a column in two steps, in order: afterwards
+// part[k width + ch], k < parts (the number returned), holds the partial sums of channel ch.
+template <typename T, int V>
+__device__ __forceinline__ int column_parts(const float2 (&s1)[(V + 1) / 2], const float2 (&s2)[(V + 1) / 2], float* scratch, float2* part, int width,
+                                            int cols, int lanes) {
+    const int tid = threadIdx.x, parts = width < kSlabThreads ? min(kSlabThreads / width, lanes) : 1;
 #pragma unroll
-    for (int i = 0; i < V; ++i) scratch[tid * V + i] = i & 1 ? v[i / 2].y : v[i / 2].x;
-    __syncthreads();
-    for (int ch = tid; ch < width; ch += kSlabThreads) {
-        float s = 0.0f;
-        for (int l = 0; l < lanes; ++l) s += scratch[(l * cols) * V + ch];
-        put(ch, s);
+    for (int round = 0; round < 2; ++round) {
+        const float2(&v)[(V + 1) / 2] = round ? s2 : s1;
+#pragma unroll
+        for (int i = 0; i < V; ++i) scratch[tid * V + i] = i & 1 ? v[i / 2].y : v[i / 2].x;
+        __syncthreads();
+        for (int i = tid; i < parts * width; i += kSlabThreads) {
+            const int ch = i % width, k = i / width;
+            float s = 0.0f;
+#pragma unroll 4
+            for (int l = k; l < lanes; l += parts) s += scratch[l * cols * V + ch];
+            (round ? part[i].y : part[i].x) = s;
+        }
+        __syncthreads();
     }
+    return parts;
 }
 
 template <typename T, int V, int ACT>
@@ -513,8 +524,8 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_kernel(SlabLaunc
     const int m = a.C / a.G, groups = width / m, cols = width / V, lanes = kSlabThreads / cols;
     T* tile = reinterpret_cast<T*>(shm);
     float* scratch = reinterpret_cast<float*>(shm + (((size_t)c.s.rows * width * sizeof(T) + 15) & ~(size_t)15));
-    float *sum1 = scratch + kSlabThreads * V, *sum2 = sum1 + width;  // per channel
-    float2* stat = reinterpret_cast<float2*>(sum2 + width);          // per group: read by the cluster
+    float2 *part = reinterpret_cast<float2*>(scratch + kSlabThreads * V), *sent = part + max(width, kSlabThreads);  // sent: [ctas][groups] mean and M2
+    float2* all = sent + ctas * groups;
     pdl_launch_dependents();
     pdl_wait();
     const long long slab = blockIdx.x / ctas;
@@ -529,63 +540,54 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_kernel(SlabLaunc
     cp_async_commit();
     cp_async_wait<0>();
     __syncthreads();
-    {  // sums of the differences to the tile's first pixel, and of their squares
-        float2 s1[Vec<T, V>::P] = {}, s2[Vec<T, V>::P] = {};
+    const int w = tid >> 5, lane = tid & 31;
+    {
+        // sums of the differences to the tile's first value of each group, and of their squares
+        float2 s1[Vec<T, V>::P] = {}, s2[Vec<T, V>::P] = {}, pivot[Vec<T, V>::P];
         if (on && rows > 0) {
-            const Vec<T, V> f = load_vec<T, V>(tile + col * V);
-            pivot_sums<T, V>(tile + col * V, width, rl, rows, lanes, f.v, s1, s2);
+            fill<V>(pivot, [&](int i) { return io<T>::cvt(tile[(col * V + i) / m * m]); });
+            pivot_sums<T, V>(tile + col * V, width, rl, rows, lanes, pivot, s1, s2);
         }
-        const float inv = 1.0f / (float)max(rows, 1);
-        column_sums<V>(s1, scratch, width, cols, lanes, [&](int ch, float s) { sum1[ch] = s; });
-        column_sums<V>(s2, scratch, width, cols, lanes, [&](int ch, float s) {
-            const float d = sum1[ch], p = rows > 0 ? io<T>::cvt(tile[ch]) : 0.0f;
-            sum2[ch] = s - d * d * inv;  // M2 of the channel
-            sum1[ch] = p + d * inv;      // its mean
-        });
-        __syncthreads();
-        const int w = tid >> 5, lane = tid & 31;
+        const int parts = column_parts<T, V>(s1, s2, scratch, part, width, cols, lanes);
+        const float inv = 1.0f / ((float)max(rows, 1) * m);
         for (int g = w; g < groups; g += kSlabThreads / 32) {
-            float s = 0.0f, q = 0.0f;
-            for (int i = lane; i < m; i += 32) s += sum1[g * m + i];
-            const float mu = warp_sum(s) / m;
-            for (int i = lane; i < m; i += 32) {
-                const float d = sum1[g * m + i] - mu;
-                q += fmaf(d * d, (float)rows, sum2[g * m + i]);
+            float t1 = 0.0f, t2 = 0.0f;
+            for (int i = lane; i < parts * m; i += 32) {
+                const float2 v = part[i / m * width + g * m + i % m];
+                t1 += v.x;
+                t2 += v.y;
             }
-            q = warp_sum(q);
-            if (lane == 0) stat[g] = make_float2(mu, q);
+            t1 = warp_sum(t1);
+            t2 = warp_sum(t2);
+            const float2 v = make_float2((rows > 0 ? io<T>::cvt(tile[g * m]) : 0.0f) + t1 * inv, fmaf(-t1 * inv, t1, t2));
+            if (lane < ctas) *cl.map_shared_rank(sent + rank * groups + g, lane) = v;  // to every CTA of the cluster
         }
     }
     cl.sync();
     // every CTA joins the cluster's means and M2 for itself
-    float2* all = reinterpret_cast<float2*>(sum1);
     for (int g = tid; g < groups; g += kSlabThreads) {
-        float2 v[8];
         float mu = 0.0f, q = 0.0f;
-        for (int i = 0; i < ctas; ++i) {
-            v[i] = *cl.map_shared_rank(stat + g, i);
-            mu = fmaf((float)max(0LL, min((long long)c.s.rows, a.L - (long long)i * c.s.rows)), v[i].x, mu);
-        }
+        for (int i = 0; i < ctas; ++i)
+            mu = fmaf((float)max(0LL, min((long long)c.s.rows, a.L - (long long)i * c.s.rows)), sent[i * groups + g].x, mu);
         mu /= (float)a.L;
         for (int i = 0; i < ctas; ++i) {
-            const float d = v[i].x - mu;
-            q += fmaf(d * d, (float)max(0LL, min((long long)c.s.rows, a.L - (long long)i * c.s.rows)) * m, v[i].y);
+            const float2 v = sent[i * groups + g];
+            const float d = v.x - mu;
+            q += fmaf(d * d, (float)max(0LL, min((long long)c.s.rows, a.L - (long long)i * c.s.rows)) * m, v.y);
         }
         const float2 out = make_float2(mu, 1.0f / sqrtf(q / ((float)a.L * m) + a.eps));
         all[g] = out;
         if (a.stats && rank == 0) reinterpret_cast<float2*>(a.stats)[(long long)b * a.G + ch0 / m + g] = out;
     }
     __syncthreads();
-    if (on) {
-        float2 ca[Vec<T, V>::P], cc[Vec<T, V>::P];
-        const int ch = ch0 + col * V;
-        fill<V>(ca, [&](int i) { return all[(col * V + i) / m].y * (a.weight ? a.weight[ch + i] : 1.0f); });
-        fill<V>(cc, [&](int i) {
-            return fmaf(-all[(col * V + i) / m].x, i & 1 ? ca[i / 2].y : ca[i / 2].x, a.bias ? a.bias[ch + i] : 0.0f);
-        });
-        apply_rows<T, V, ACT>(tile + col * V, width, (T*)a.y + (b * a.L + r0) * a.C + ch, a.C, rl, rows, lanes, ca, cc);
-    }
-    cl.sync();  // the others may still read this CTA's sums
+    if (!on) return;
+    float2 ca[Vec<T, V>::P], cc[Vec<T, V>::P];
+    const int ch = ch0 + col * V;
+    fill<V>(ca, [&](int i) { return all[(col * V + i) / m].y * (a.weight ? a.weight[ch + i] : 1.0f); });
+    fill<V>(cc, [&](int i) {
+        return fmaf(-all[(col * V + i) / m].x, i & 1 ? ca[i / 2].y : ca[i / 2].x, a.bias ? a.bias[ch + i] : 0.0f);
+    });
+    apply_rows<T, V, ACT>(tile + col * V, width, (T*)a.y + (b * a.L + r0) * a.C + ch, a.C, rl, rows, lanes, ca, cc);
 }
 
 template <typename T, int V, int ACT>
@@ -599,8 +601,8 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_grad_kernel(Slab
     const int m = a.C / a.G, groups = width / m, cols = width / V, lanes = kSlabThreads / cols;
     T *tx = reinterpret_cast<T*>(shm), *td = tx + (size_t)c.s.rows * width;
     float* scratch = reinterpret_cast<float*>(shm + (((size_t)2 * c.s.rows * width * sizeof(T) + 15) & ~(size_t)15));
-    float *sum1 = scratch + kSlabThreads * V, *sum2 = sum1 + width;  // per channel: read by the cluster
-    float2* mine = reinterpret_cast<float2*>(sum2 + width);          // per group, the cluster's
+    float2 *part = reinterpret_cast<float2*>(scratch + kSlabThreads * V), *sent = part + max(width, kSlabThreads);  // sent: [ctas][width] sums of dz, dz n
+    float2* mine = sent + ctas * width;
     pdl_launch_dependents();
     pdl_wait();
     const long long slab = blockIdx.x / ctas;
@@ -625,25 +627,27 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_grad_kernel(Slab
     {
         float2 s1[Vec<T, V>::P] = {}, s2[Vec<T, V>::P] = {};
         if (on) slope_sums<T, V, ACT>(tx + col * V, td + col * V, width, rl, rows, lanes, ca, cc, mu, s1, s2);
-        column_sums<V>(s1, scratch, width, cols, lanes, [&](int ch, float s) { sum1[ch] = s; });
-        column_sums<V>(s2, scratch, width, cols, lanes, [&](int ch, float s) { sum2[ch] = st[(ch0 + ch) / m].y * s; });
+        const int parts = column_parts<T, V>(s1, s2, scratch, part, width, cols, lanes);
+        for (int i = tid; i < width * ctas; i += kSlabThreads) {  // to every CTA of the cluster
+            const int ch = i % width;
+            float2 s = make_float2(0.0f, 0.0f);
+            for (int k = 0; k < parts; ++k) s = __fadd2_rn(s, part[k * width + ch]);
+            s.y *= st[(ch0 + ch) / m].y;
+            *cl.map_shared_rank(sent + rank * width + ch, i / width) = s;
+        }
     }
     cl.sync();
-    // the cluster's sums: every CTA the groups' means, rank 0 also the channels'
     {
         const int w = tid >> 5, lane = tid & 31;
         for (int g = w; g < groups; g += kSlabThreads / 32) {
             float t1 = 0.0f, t2 = 0.0f;
             for (int i = lane; i < m; i += 32) {
-                float u1 = 0.0f, u2 = 0.0f;
-                for (int k = 0; k < ctas; ++k) {
-                    u1 += *cl.map_shared_rank(sum1 + g * m + i, k);
-                    u2 += *cl.map_shared_rank(sum2 + g * m + i, k);
-                }
+                float2 u = make_float2(0.0f, 0.0f);
+                for (int k = 0; k < ctas; ++k) u = __fadd2_rn(u, sent[k * width + g * m + i]);
                 const float wv = a.weight ? a.weight[ch0 + g * m + i] : 1.0f;
-                t1 = fmaf(wv, u1, t1);
-                t2 = fmaf(wv, u2, t2);
-                if (rank == 0) c.chan[(long long)b * a.C + ch0 + g * m + i] = make_float2(u1, u2);
+                t1 = fmaf(wv, u.x, t1);
+                t2 = fmaf(wv, u.y, t2);
+                if (rank == 0) c.chan[(long long)b * a.C + ch0 + g * m + i] = u;
             }
             t1 = warp_sum(t1);
             t2 = warp_sum(t2);
@@ -657,7 +661,6 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_grad_kernel(Slab
         fill<V>(k2, [&](int i) { return st[(mych + i) / m].y * (st[(mych + i) / m].y * mine[(col * V + i) / m].y); });
         dx_rows<T, V, ACT>(tx + col * V, td + col * V, width, (T*)a.dx + at + col * V, a.C, rl, rows, lanes, ca, cc, mu, k1, k2);
     }
-    cl.sync();
     if (rank != 0 || (!a.dweight && !a.dbias)) return;
     if (!last_tile(c.counter, a.B * c.s.slabs, &flag)) return;  // the last slab of all: the sums over the batch
     for (int k = tid; k < a.C; k += kSlabThreads) {
@@ -677,7 +680,7 @@ template <typename T, int V, int ACT>
 vmb_status run_slabs(const NormArgs& a, const NormSlab& s, bool grads, size_t chan_off, cudaStream_t stream) {
     SlabLaunch c{a, s, reinterpret_cast<float2*>((char*)a.ws + chan_off), reinterpret_cast<unsigned*>(a.ws) + kNormCounters - 1};
     const void* fn = grads ? (const void*)norm_cluster_grad_kernel<T, V, ACT> : (const void*)norm_cluster_kernel<T, V, ACT>;
-    const size_t smem = slab_smem(s.rows, s.width, s.width / (a.C / a.G), sizeof(T), grads);
+    const size_t smem = slab_smem(s.rows, s.width, s.width / (a.C / a.G), s.ctas, sizeof(T), grads);
     if (!allow_smem(fn, kSlabSmem)) return VMB_ERR_CUDA;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)((long long)a.B * s.slabs * s.ctas));
