@@ -20,12 +20,13 @@ constexpr int kJoinThreads = 256, kJoinRows = 8;
 __global__ void __launch_bounds__(kJoinThreads) delta_join_kernel(DeltaChain c, int reverse) {
     extern __shared__ __align__(16) float sm[];
     const DeltaArgs& a = c.a;
-    const int Dk = a.Dk, ld = Dk + 1, tid = threadIdx.x;
+    // rows of 16-byte multiples and four words more: whole vectors in, and eight lanes' vectors of eight rows on all banks
+    const int Dk = a.Dk, Dk4 = (Dk + 3) & ~3, ld = Dk4 + 4, tid = threadIdx.x;
     // thread: column d, rows 4 half .. 4 half + 3
     const int d = tid & 127, half = tid >> 7;
-    float* S = sm;                          // [Dk][8]
-    float* X = sm + ((Dk * kJoinRows + 3) & ~3);  // two maps [Dk][Dk + 1]
-    const int map = (Dk * ld + 3) & ~3;
+    float* S = sm;                    // [Dk4][8]
+    float* X = sm + Dk4 * kJoinRows;  // two maps [Dk4][ld], zeros beyond Dk
+    const int map = Dk4 * ld;
     pdl_launch_dependents();
     pdl_wait();
     const int strips = (a.Dv + kJoinRows - 1) / kJoinRows;
@@ -40,7 +41,11 @@ __global__ void __launch_bounds__(kJoinThreads) delta_join_kernel(DeltaChain c, 
     auto fetch = [&](int i) {
         const float* x = c.maps + place(i) * Dk * Dk;
         float* to = X + (i & 1) * map;
-        for (int j = tid; j < Dk * Dk; j += kJoinThreads) cp_async4(to + (j / Dk) * ld + j % Dk, x + j, 4);
+        if (Dk % 4 == 0) {
+            for (int j = tid; j < Dk * (Dk / 4); j += kJoinThreads) cp_async16(to + (j / (Dk / 4)) * ld + j % (Dk / 4) * 4, x + 4 * j, 16);
+        } else {
+            for (int j = tid; j < Dk * Dk; j += kJoinThreads) cp_async4(to + (j / Dk) * ld + j % Dk, x + j, 4);
+        }
         cp_async_commit();
     };
     float s[4], n[4];
@@ -50,6 +55,8 @@ __global__ void __launch_bounds__(kJoinThreads) delta_join_kernel(DeltaChain c, 
     };
 #pragma unroll
     for (int r = 0; r < 4; ++r) s[r] = init && on && row0 + r < a.Dv ? init[(chain * Dk + d) * a.Dv + row0 + r] : 0.0f;
+    for (int j = tid; j < Dk4 * kJoinRows + 2 * map; j += kJoinThreads) sm[j] = 0.0f;
+    __syncthreads();
     if (nseg > 0) {
         fetch(0);
         sums(0);
@@ -72,16 +79,22 @@ __global__ void __launch_bounds__(kJoinThreads) delta_join_kernel(DeltaChain c, 
         }
         __syncthreads();
         if (on) {
-            const float* col = X + (i & 1) * map + (reverse ? d * ld : d);
-            const int step = reverse ? 1 : ld;
-#pragma unroll 8
-            for (int e = 0; e < Dk; ++e) {
-                const float v = col[e * step];
-                const float4 q = *reinterpret_cast<const float4*>(S + e * kJoinRows + 4 * half);
-                s[0] = fmaf(q.x, v, s[0]);
-                s[1] = fmaf(q.y, v, s[1]);
-                s[2] = fmaf(q.z, v, s[2]);
-                s[3] = fmaf(q.w, v, s[3]);
+            const float *m = X + (i & 1) * map + (reverse ? d * ld : d), *q = S + 4 * half;
+            auto step = [&](float v, const float* p) {
+                const float4 u = *reinterpret_cast<const float4*>(p);
+                s[0] = fmaf(u.x, v, s[0]);
+                s[1] = fmaf(u.y, v, s[1]);
+                s[2] = fmaf(u.z, v, s[2]);
+                s[3] = fmaf(u.w, v, s[3]);
+            };
+#pragma unroll 4
+            for (int e = 0; e < Dk4; e += 4) {
+                const float4 v = reverse ? *reinterpret_cast<const float4*>(m + e)
+                                         : make_float4(m[e * ld], m[(e + 1) * ld], m[(e + 2) * ld], m[(e + 3) * ld]);
+                step(v.x, q + e * kJoinRows);
+                step(v.y, q + (e + 1) * kJoinRows);
+                step(v.z, q + (e + 2) * kJoinRows);
+                step(v.w, q + (e + 3) * kJoinRows);
             }
         }
         __syncthreads();  // S and this map have been read
@@ -226,7 +239,7 @@ vmb_status chain(const DeltaChain& c, bool reverse, cudaStream_t stream) {
 
 vmb_status join(const DeltaChain& c, bool reverse, cudaStream_t stream) {
     const int strips = (c.a.Dv + kJoinRows - 1) / kJoinRows;
-    const size_t smem = 4 * (size_t)(2 * ((c.a.Dk * (c.a.Dk + 1) + 3) & ~3) + ((c.a.Dk * kJoinRows + 3) & ~3));
+    const size_t d4 = (c.a.Dk + 3) & ~3, smem = 4 * (2 * d4 * (d4 + 4) + d4 * kJoinRows);
     const void* fn = (const void*)delta_join_kernel;
     if (!allow_smem(fn, 140 * 1024)) return VMB_ERR_CUDA;
     DeltaChain arg = c;

@@ -491,19 +491,19 @@ struct SlabLaunch {
 };
 
 // A thread's sums of its V channels, two each, summed over the threads of a column in two steps, in order: afterwards
-// part[k width + ch], k < parts (the number returned), holds the partial sums of channel ch.
+// part[k width + ch], k < parts, holds the partial sums of channel ch.  ch0, k0: the thread's number as k0 width + ch0.
 template <typename T, int V>
-__device__ __forceinline__ int column_parts(const float2 (&s1)[(V + 1) / 2], const float2 (&s2)[(V + 1) / 2], float* scratch, float2* part, int width,
-                                            int cols, int lanes) {
-    const int tid = threadIdx.x, parts = width < kSlabThreads ? min(kSlabThreads / width, lanes) : 1;
+__device__ __forceinline__ void column_parts(const float2 (&s1)[(V + 1) / 2], const float2 (&s2)[(V + 1) / 2], float* scratch, float2* part, int width,
+                                            int cols, int lanes, int ch0, int k0, int parts) {
+    const int tid = threadIdx.x;
 #pragma unroll
     for (int round = 0; round < 2; ++round) {
         const float2(&v)[(V + 1) / 2] = round ? s2 : s1;
 #pragma unroll
         for (int i = 0; i < V; ++i) scratch[tid * V + i] = i & 1 ? v[i / 2].y : v[i / 2].x;
         __syncthreads();
-        for (int i = tid; i < parts * width; i += kSlabThreads) {
-            const int ch = i % width, k = i / width;
+        for (int i = tid, ch = ch0, k = k0; i < parts * width; i += kSlabThreads, ch += kSlabThreads) {
+            if (ch >= width) ch -= width, ++k;  // (more than one turn only where parts = 1)
             float s = 0.0f;
 #pragma unroll 4
             for (int l = k; l < lanes; l += parts) s += scratch[l * cols * V + ch];
@@ -511,7 +511,6 @@ __device__ __forceinline__ int column_parts(const float2 (&s1)[(V + 1) / 2], con
         }
         __syncthreads();
     }
-    return parts;
 }
 
 template <typename T, int V, int ACT>
@@ -538,9 +537,11 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_kernel(SlabLaunc
     if (on)
         for (int r = rl; r < rows; r += lanes) cp_async16(tile + (long long)r * width + col * V, x + (long long)r * a.C + col * V, 16);
     cp_async_commit();
+    const int parts = width < kSlabThreads ? min(kSlabThreads / width, lanes) : 1, ch1 = tid % width, k1 = tid / width;
+    const int w = tid >> 5, lane = tid & 31;
+    const int left = (int)a.L - (tid & 7) * c.s.rows, run = max(0, min(c.s.rows, left));  // pixels of CTA tid % 8
     cp_async_wait<0>();
     __syncthreads();
-    const int w = tid >> 5, lane = tid & 31;
     {
         // sums of the differences to the tile's first value of each group, and of their squares
         float2 s1[Vec<T, V>::P] = {}, s2[Vec<T, V>::P] = {}, pivot[Vec<T, V>::P];
@@ -548,14 +549,17 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_kernel(SlabLaunc
             fill<V>(pivot, [&](int i) { return io<T>::cvt(tile[(col * V + i) / m * m]); });
             pivot_sums<T, V>(tile + col * V, width, rl, rows, lanes, pivot, s1, s2);
         }
-        const int parts = column_parts<T, V>(s1, s2, scratch, part, width, cols, lanes);
+        column_parts<T, V>(s1, s2, scratch, part, width, cols, lanes, ch1, k1, parts);
         const float inv = 1.0f / ((float)max(rows, 1) * m);
         for (int g = w; g < groups; g += kSlabThreads / 32) {
             float t1 = 0.0f, t2 = 0.0f;
-            for (int i = lane; i < parts * m; i += 32) {
-                const float2 v = part[i / m * width + g * m + i % m];
-                t1 += v.x;
-                t2 += v.y;
+            for (int ch = g * m + lane; ch < g * m + m; ch += 32) {
+#pragma unroll 4
+                for (int k = 0; k < parts; ++k) {
+                    const float2 v = part[k * width + ch];
+                    t1 += v.x;
+                    t2 += v.y;
+                }
             }
             t1 = warp_sum(t1);
             t2 = warp_sum(t2);
@@ -564,20 +568,28 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_kernel(SlabLaunc
         }
     }
     cl.sync();
-    // every CTA joins the cluster's means and M2 for itself
-    for (int g = tid; g < groups; g += kSlabThreads) {
-        float mu = 0.0f, q = 0.0f;
-        for (int i = 0; i < ctas; ++i)
-            mu = fmaf((float)max(0LL, min((long long)c.s.rows, a.L - (long long)i * c.s.rows)), sent[i * groups + g].x, mu);
+    // every CTA joins the cluster's means and M2 for itself: eight threads per group, one for each CTA
+    static_assert(kSlabCluster == 8, "threads per group");
+    for (int g0 = 0; g0 < groups; g0 += kSlabThreads / 8) {
+        const int g = g0 + (tid >> 3), r = tid & 7;
+        const bool mine = g < groups && r < ctas;
+        const float2 v = mine ? sent[r * groups + g] : make_float2(0.0f, 0.0f);
+        const float n = mine ? (float)run : 0.0f;
+        float mu = n * v.x;
+        mu += __shfl_xor_sync(0xffffffffu, mu, 1);
+        mu += __shfl_xor_sync(0xffffffffu, mu, 2);
+        mu += __shfl_xor_sync(0xffffffffu, mu, 4);
         mu /= (float)a.L;
-        for (int i = 0; i < ctas; ++i) {
-            const float2 v = sent[i * groups + g];
-            const float d = v.x - mu;
-            q += fmaf(d * d, (float)max(0LL, min((long long)c.s.rows, a.L - (long long)i * c.s.rows)) * m, v.y);
+        const float d = v.x - mu;
+        float q = mine ? fmaf(d * d, n * m, v.y) : 0.0f;
+        q += __shfl_xor_sync(0xffffffffu, q, 1);
+        q += __shfl_xor_sync(0xffffffffu, q, 2);
+        q += __shfl_xor_sync(0xffffffffu, q, 4);
+        if (mine && r == 0) {
+            const float2 out = make_float2(mu, 1.0f / sqrtf(q / ((float)a.L * m) + a.eps));
+            all[g] = out;
+            if (a.stats && rank == 0) reinterpret_cast<float2*>(a.stats)[(long long)b * a.G + ch0 / m + g] = out;
         }
-        const float2 out = make_float2(mu, 1.0f / sqrtf(q / ((float)a.L * m) + a.eps));
-        all[g] = out;
-        if (a.stats && rank == 0) reinterpret_cast<float2*>(a.stats)[(long long)b * a.G + ch0 / m + g] = out;
     }
     __syncthreads();
     if (!on) return;
@@ -622,18 +634,19 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_grad_kernel(Slab
     float2 ca[Vec<T, V>::P], cc[Vec<T, V>::P], mu[Vec<T, V>::P];
     const float2* st = reinterpret_cast<const float2*>(a.stats) + (long long)b * a.G;
     const int mych = ch0 + (on ? col * V : 0);
+    const int parts = width < kSlabThreads ? min(kSlabThreads / width, lanes) : 1, ch1 = tid % width, k1 = tid / width;
     channel_values<T, V>(a, st, mych, m, ca, cc, mu);
     cp_async_wait<0>();  // (a thread reads back what it copied itself)
     {
         float2 s1[Vec<T, V>::P] = {}, s2[Vec<T, V>::P] = {};
         if (on) slope_sums<T, V, ACT>(tx + col * V, td + col * V, width, rl, rows, lanes, ca, cc, mu, s1, s2);
-        const int parts = column_parts<T, V>(s1, s2, scratch, part, width, cols, lanes);
-        for (int i = tid; i < width * ctas; i += kSlabThreads) {  // to every CTA of the cluster
-            const int ch = i % width;
+        column_parts<T, V>(s1, s2, scratch, part, width, cols, lanes, ch1, k1, parts);
+        for (int ch = tid; ch < width; ch += kSlabThreads) {  // to every CTA of the cluster
             float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll 4
             for (int k = 0; k < parts; ++k) s = __fadd2_rn(s, part[k * width + ch]);
             s.y *= st[(ch0 + ch) / m].y;
-            *cl.map_shared_rank(sent + rank * width + ch, i / width) = s;
+            for (int r = 0; r < ctas; ++r) *cl.map_shared_rank(sent + rank * width + ch, r) = s;
         }
     }
     cl.sync();
@@ -643,6 +656,7 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_grad_kernel(Slab
             float t1 = 0.0f, t2 = 0.0f;
             for (int i = lane; i < m; i += 32) {
                 float2 u = make_float2(0.0f, 0.0f);
+#pragma unroll 8
                 for (int k = 0; k < ctas; ++k) u = __fadd2_rn(u, sent[k * width + g * m + i]);
                 const float wv = a.weight ? a.weight[ch0 + g * m + i] : 1.0f;
                 t1 = fmaf(wv, u.x, t1);
@@ -656,10 +670,10 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_grad_kernel(Slab
     }
     __syncthreads();
     if (on) {
-        float2 k1[Vec<T, V>::P], k2[Vec<T, V>::P];
-        fill<V>(k1, [&](int i) { return st[(mych + i) / m].y * mine[(col * V + i) / m].x; });
-        fill<V>(k2, [&](int i) { return st[(mych + i) / m].y * (st[(mych + i) / m].y * mine[(col * V + i) / m].y); });
-        dx_rows<T, V, ACT>(tx + col * V, td + col * V, width, (T*)a.dx + at + col * V, a.C, rl, rows, lanes, ca, cc, mu, k1, k2);
+        float2 f1[Vec<T, V>::P], f2[Vec<T, V>::P];
+        fill<V>(f1, [&](int i) { return st[(mych + i) / m].y * mine[(col * V + i) / m].x; });
+        fill<V>(f2, [&](int i) { return st[(mych + i) / m].y * (st[(mych + i) / m].y * mine[(col * V + i) / m].y); });
+        dx_rows<T, V, ACT>(tx + col * V, td + col * V, width, (T*)a.dx + at + col * V, a.C, rl, rows, lanes, ca, cc, mu, f1, f2);
     }
     if (rank != 0 || (!a.dweight && !a.dbias)) return;
     if (!last_tile(c.counter, a.B * c.s.slabs, &flag)) return;  // the last slab of all: the sums over the batch
