@@ -244,6 +244,15 @@ template <int COLS, int NT> struct Tile<__nv_bfloat16, COLS, NT> {
         if constexpr (NT > 1) v += __bfloat162float(p[plane + r * kLd + c]);
         return v;
     }
+    __device__ __forceinline__ float2 get2(int r, int c) const { return bf16_pair(*reinterpret_cast<const uint32_t*>(p + r * kLd + c)); }  // c even
+    // sum += this(r, c ..) . o(r, c ..) over kVec columns
+    __device__ __forceinline__ void dot_vec(const Tile& o, int r, int c, float2& sum) const {
+        const uint4 u = *reinterpret_cast<const uint4*>(vec_at(r, c)), v = *reinterpret_cast<const uint4*>(o.vec_at(r, c));
+        sum = __ffma2_rn(bf16_pair(u.x), bf16_pair(v.x), sum);
+        sum = __ffma2_rn(bf16_pair(u.y), bf16_pair(v.y), sum);
+        sum = __ffma2_rn(bf16_pair(u.z), bf16_pair(v.z), sum);
+        sum = __ffma2_rn(bf16_pair(u.w), bf16_pair(v.w), sum);
+    }
     __device__ __forceinline__ uint32_t lane_addr(int term, int r0, int c0) const {
         const int lane = threadIdx.x & 31;
         return smem_u32(p + term * plane + (r0 + (lane & 15)) * kLd + c0 + (lane >> 4) * 8);
@@ -320,6 +329,12 @@ template <int COLS, int NT> struct Tile<float, COLS, NT> {
     __device__ __forceinline__ void zero(int r, int c) const { p[at(r, c)] = 0.0f; }
     __device__ __forceinline__ void put(int r, int c, T v) const { p[at(r, c)] = v; }
     __device__ __forceinline__ float get(int r, int c) const { return p[at(r, c)]; }
+    __device__ __forceinline__ float2 get2(int r, int c) const { return *reinterpret_cast<const float2*>(p + at(r, c)); }
+    __device__ __forceinline__ void dot_vec(const Tile& o, int r, int c, float2& sum) const {
+        const float4 u = *reinterpret_cast<const float4*>(vec_at(r, c)), v = *reinterpret_cast<const float4*>(o.vec_at(r, c));
+        sum.x = fmaf(u.x, v.x, sum.x), sum.y = fmaf(u.y, v.y, sum.y);
+        sum.x = fmaf(u.z, v.z, sum.x), sum.y = fmaf(u.w, v.w, sum.y);
+    }
     template <int N = NT> __device__ __forceinline__ void a_mk(FragA<T, N>& a, int m0, int k0) const {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 #pragma unroll

@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(GradSmem<T, DK>::threads, GradSmem<T, DK>::sma
     load(0);
 
     float dq[HT][4], dkr[HT][4], dkt[HT][4], W[2 * JB][4];
-    float sdot = 0.0f, bdot = 0.0f;
+    float2 sdot = make_float2(0.0f, 0.0f), bdot = sdot;
     for (int i = 0; i < steps; ++i) {
         const int h = h0 + i / vslices, vs = i % vslices;
         unsigned char* s = smem + (SM::ahead && (i & 1) ? SM::slice2 : SM::slices);
@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(GradSmem<T, DK>::threads, GradSmem<T, DK>::sma
             for (int j = 0; j < 2 * JB; ++j)
 #pragma unroll
                 for (int x = 0; x < 4; ++x) W[j][x] = 0.0f;
-            sdot = bdot = 0.0f;
+            sdot = bdot = make_float2(0.0f, 0.0f);
             if (w == 0) {
                 const T *gp = (const T*)a.g + tok * a.Hv + h, *bp = (const T*)a.beta + tok * a.Hv + h;
                 float v[4];
@@ -135,12 +135,12 @@ __global__ void __launch_bounds__(GradSmem<T, DK>::threads, GradSmem<T, DK>::sma
         }
         __syncthreads();
         {  // this thread's part of dbeta: token tid / (N / 64); and of <S, dS>
-            constexpr int per = N / 64;
+            constexpr int per = N / 64, Vv = SM::KT::kVec;
             const int tk = tid / per, p = tid % per;
-#pragma unroll 4
-            for (int j = 0; j < 64 / per; ++j) bdot = fmaf(sX.get(tk, p + per * j), sR.get(tk, p + per * j), bdot);
-#pragma unroll 4
-            for (int j = tid; j < 64 * DK; j += N) sdot = fmaf(sS.get(j / DK, j % DK), sDS.get(j / DK, j % DK), sdot);
+#pragma unroll
+            for (int j = 0; j < 64 / (per * Vv); ++j) sX.dot_vec(sR, tk, (p + per * j) * Vv, bdot);
+#pragma unroll 2
+            for (int j = tid; j < 64 * DK / Vv; j += N) sS.dot_vec(sDS, j / (DK / Vv), j % (DK / Vv) * Vv, sdot);
         }
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
@@ -197,20 +197,19 @@ __global__ void __launch_bounds__(GradSmem<T, DK>::threads, GradSmem<T, DK>::sma
                 const int bj = block(jt / 2), j0 = 16 * bj + 8 * (jt & 1) + 2 * t;
                 float cs[2] = {};
                 if (bj <= tb) {
+                    const float2 jh = *reinterpret_cast<const float2*>(G.hi + j0), jl = *reinterpret_cast<const float2*>(G.lo + j0),
+                                 jb = *reinterpret_cast<const float2*>(G.beta + j0);
 #pragma unroll
                     for (int hh = 0; hh < 2; ++hh) {
                         const int r = 16 * tb + g + 8 * hh;
-                        float v[2];
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const int j = j0 + x;
-                            const float e = j <= r ? decay(G.hi[r] - G.hi[j], G.lo[r] - G.lo[j]) * G.beta[j] : 0.0f;
-                            const float f = second ? (j < r ? -e * G.beta[r] : 0.0f) : a.scale * e;
-                            v[x] = f * W[jt][2 * hh + x];
-                            const float p = v[x] * m[jt][2 * hh + x];
-                            rs[hh] += p;
-                            cs[x] += p;
-                        }
+                        const float ih = G.hi[r], il = G.lo[r], sc = second ? -G.beta[r] : a.scale;
+                        const float e0 = ex2((ih - jh.x) + (il - jl.x)) * (sc * jb.x), e1 = ex2((ih - jh.y) + (il - jl.y)) * (sc * jb.y);
+                        // (above the diagonal the exponential may be anything: not taken)
+                        const float v[2] = {j0 + second <= r ? e0 * W[jt][2 * hh] : 0.0f, j0 + 1 + second <= r ? e1 * W[jt][2 * hh + 1] : 0.0f};
+                        const float p0 = v[0] * m[jt][2 * hh], p1 = v[1] * m[jt][2 * hh + 1];
+                        rs[hh] += p0 + p1;
+                        cs[0] += p0;
+                        cs[1] += p1;
                         (second ? sDA : sDP).set2(r, j0, v[0], v[1]);
                     }
                 }
@@ -230,20 +229,20 @@ __global__ void __launch_bounds__(GradSmem<T, DK>::threads, GradSmem<T, DK>::sma
             const float sq = a.scale * G.ec[r], sr = -G.ec[r] * G.beta[r], st = G.tail[r] * G.beta[r];
             float dot[3] = {};
 #pragma unroll
-            for (int j = 0; j < HT; ++j)
+            for (int j = 0; j < HT; ++j) {
+                const float2 qv = sQ.get2(r, col0 + 8 * j + 2 * t), kv = sK.get2(r, col0 + 8 * j + 2 * t);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const int cc = col0 + 8 * j + 2 * t + x;
-                    const float qv = sQ.get(r, cc), kv = sK.get(r, cc);
                     float &eq = dq[j][2 * hh + x], &er = dkr[j][2 * hh + x];
-                    const float et = dkt[j][2 * hh + x] * st;
+                    const float et = dkt[j][2 * hh + x] * st, kx = x ? kv.y : kv.x;
                     eq *= sq;
                     er *= sr;
-                    dot[0] = fmaf(qv, eq, dot[0]);
-                    dot[1] = fmaf(kv, er, dot[1]);
-                    dot[2] = fmaf(kv, et, dot[2]);
+                    dot[0] = fmaf(x ? qv.y : qv.x, eq, dot[0]);
+                    dot[1] = fmaf(kx, er, dot[1]);
+                    dot[2] = fmaf(kx, et, dot[2]);
                     er += et;
                 }
+            }
 #pragma unroll
             for (int x = 0; x < 3; ++x) {
                 dot[x] += __shfl_xor_sync(0xffffffffu, dot[x], 1);
@@ -256,11 +255,11 @@ __global__ void __launch_bounds__(GradSmem<T, DK>::threads, GradSmem<T, DK>::sma
         }
         {
             constexpr int per = N / 64;
-            float v = bdot;
+            float v = bdot.x + bdot.y;
 #pragma unroll
             for (int d = 1; d < per; d <<= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
             if (tid % per == 0) dbeta[tid / per] = v;
-            v = sdot;
+            v = sdot.x + sdot.y;
 #pragma unroll
             for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
             if (lane == 0) blocks[w] = v;
