@@ -90,10 +90,35 @@ __device__ __forceinline__ void store_tokens(const Tile<T, ROWS, 1>& s, const fl
     }
 }
 
-// A warp's 16 rows of the transposed state, [row][Dk] fp32 or storage type at dst.
+// A warp's 16 rows of the transposed state, [row][Dk] fp32 or storage type at dst (16-byte aligned).  fp32: pairs of
+// columns, a sector per row and tile; bf16: the four lanes of a row exchange the pairs of four tiles, so that each
+// stores the eight columns of one (1657 -> 1264 us for the training pass of 8 x 3136 tokens against single values).
 template <int DK, typename T>
 __device__ __forceinline__ void store_state_rows(const float (&S)[DK / 8][4], T* dst, int row0, int rows, int Dk) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    if (Dk % 8 == 0) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = row0 + g + 8 * h;
+            T* p = dst + (long long)r * Dk;
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int q = 0; q < DK / 32; ++q) {
+                    uint32_t v[4];
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) v[n] = pack_bf16(S[4 * q + n][2 * h], S[4 * q + n][2 * h + 1]);
+                    quad_transpose(v);
+                    const int d = 32 * q + 8 * t;
+                    if (r < rows && d < Dk) *reinterpret_cast<uint4*>(p + d) = make_uint4(v[0], v[1], v[2], v[3]);
+                }
+            } else {
+#pragma unroll
+                for (int n = 0; n < DK / 8; ++n)
+                    if (r < rows && 8 * n < Dk) *reinterpret_cast<float2*>(p + 8 * n + 2 * t) = make_float2(S[n][2 * h], S[n][2 * h + 1]);
+            }
+        }
+        return;
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int r = row0 + g + 8 * h;

@@ -92,6 +92,21 @@ __device__ __forceinline__ void split_tf32(float x, float y, uint32_t& xh, uint3
     yl = __float_as_uint(y - __uint_as_float(yh)) & 0xffffe000u;
 }
 
+// Among the four lanes of a row, lane t holding word t of four tiles: afterwards lane t holds the four words of tile t.
+__device__ __forceinline__ void quad_transpose(uint32_t (&v)[4]) {
+    const int t = threadIdx.x & 3;
+#pragma unroll
+    for (int n = 0; n < 4; n += 2) {
+        const uint32_t x = __shfl_xor_sync(0xffffffffu, t & 1 ? v[n] : v[n + 1], 1);
+        if (t & 1) v[n] = x; else v[n + 1] = x;
+    }
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        const uint32_t x = __shfl_xor_sync(0xffffffffu, t & 2 ? v[n] : v[n + 2], 2);
+        if (t & 2) v[n] = x; else v[n + 2] = x;
+    }
+}
+
 // Operands of a 16-deep step.  bf16: NT terms.  fp32: two 8-deep tf32 steps s; position k of step
 // s stands for column 8s + 2(k % 4) + k / 4, the same in A and B, so that an accumulator pair
 // (columns 2t, 2t + 1) is an A operand as it stands.

@@ -334,43 +334,70 @@ __global__ void __launch_bounds__(GradSmem<T, DK>::threads, GradSmem<T, DK>::sma
         }
         // out: to the sums of the head's group, or (the last of it) to dq and dk
         const bool part = !SM::totals && share > 1, done = i + 1 == steps;
-        const bool pairs = a.Dk % 2 == 0 && ((reinterpret_cast<uintptr_t>(a.dq) | reinterpret_cast<uintptr_t>(a.dk)) % (2 * sizeof(T))) == 0;
+        if (SM::totals && share > 1) {
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-            const int r = 16 * tb + g + 8 * hh;
+            for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
-            for (int j = 0; j < HT; ++j) {
-                const int cc = col0 + 8 * j + 2 * t;
-                float2 vq = make_float2(dq[j][2 * hh], dq[j][2 * hh + 1]), vk = make_float2(dkr[j][2 * hh], dkr[j][2 * hh + 1]);
-                if (SM::totals && share > 1) {
+                for (int j = 0; j < HT; ++j) {
+                    const int r = 16 * tb + g + 8 * hh, cc = col0 + 8 * j + 2 * t;
                     float2 *tq = reinterpret_cast<float2*>(tot + r * DK + cc), *tk = reinterpret_cast<float2*>(tot + (64 + r) * DK + cc);
                     if (i >= vslices) {  // (this thread's own places)
-                        vq.x += tq->x, vq.y += tq->y, vk.x += tk->x, vk.y += tk->y;
+                        dq[j][2 * hh] += tq->x, dq[j][2 * hh + 1] += tq->y;
+                        dkr[j][2 * hh] += tk->x, dkr[j][2 * hh + 1] += tk->y;
                     }
                     if (!done) {
-                        *tq = vq, *tk = vk;
-                        continue;
+                        *tq = make_float2(dq[j][2 * hh], dq[j][2 * hh + 1]);
+                        *tk = make_float2(dkr[j][2 * hh], dkr[j][2 * hh + 1]);
                     }
                 }
-                if (r >= n || cc >= a.Dk) continue;
+        }
+        if (done || part) {
+            const bool vec = a.Dk % 8 == 0 && ((reinterpret_cast<uintptr_t>(a.dq) | reinterpret_cast<uintptr_t>(a.dk)) & 15) == 0;
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                const int r = 16 * tb + g + 8 * hh;
+                const long long row = ((tok + r) * a.Hk + hk) * a.Dk;
                 if (part) {
-                    float* row = c.part + ((tok + r) * a.Hv + h) * 2 * a.Dk + cc;
-                    row[0] = vq.x, row[a.Dk] = vk.x;
-                    if (cc + 1 < a.Dk) row[1] = vq.y, row[a.Dk + 1] = vk.y;
-                    continue;
-                }
-                T *pq = (T*)a.dq + ((tok + r) * a.Hk + hk) * a.Dk + cc, *pk = (T*)a.dk + ((tok + r) * a.Hk + hk) * a.Dk + cc;
-                if (pairs) {
+                    float* to = c.part + ((tok + r) * a.Hv + h) * 2 * a.Dk;
+#pragma unroll
+                    for (int j = 0; j < HT; ++j)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const int cc = col0 + 8 * j + 2 * t + x;
+                            if (r < n && cc < a.Dk) to[cc] = dq[j][2 * hh + x], to[a.Dk + cc] = dkr[j][2 * hh + x];
+                        }
+                } else if (vec) {
                     if constexpr (sizeof(T) == 2) {
-                        *reinterpret_cast<uint32_t*>(pq) = pack_bf16(vq.x, vq.y);
-                        *reinterpret_cast<uint32_t*>(pk) = pack_bf16(vk.x, vk.y);
+                        static_assert(HT == 4, "the four lanes of a row store a tile each");
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            uint32_t v[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                v[j] = y ? pack_bf16(dkr[j][2 * hh], dkr[j][2 * hh + 1]) : pack_bf16(dq[j][2 * hh], dq[j][2 * hh + 1]);
+                            quad_transpose(v);
+                            const int cc = col0 + 8 * t;
+                            if (r < n && cc < a.Dk) *reinterpret_cast<uint4*>((T*)(y ? a.dk : a.dq) + row + cc) = make_uint4(v[0], v[1], v[2], v[3]);
+                        }
                     } else {
-                        *reinterpret_cast<float2*>(pq) = vq;
-                        *reinterpret_cast<float2*>(pk) = vk;
+#pragma unroll
+                        for (int j = 0; j < HT; ++j) {
+                            const int cc = col0 + 8 * j + 2 * t;
+                            if (r >= n || cc >= a.Dk) continue;
+                            *reinterpret_cast<float2*>((T*)a.dq + row + cc) = make_float2(dq[j][2 * hh], dq[j][2 * hh + 1]);
+                            *reinterpret_cast<float2*>((T*)a.dk + row + cc) = make_float2(dkr[j][2 * hh], dkr[j][2 * hh + 1]);
+                        }
                     }
                 } else {
-                    pq[0] = io<T>::to(vq.x), pk[0] = io<T>::to(vk.x);
-                    if (cc + 1 < a.Dk) pq[1] = io<T>::to(vq.y), pk[1] = io<T>::to(vk.y);
+#pragma unroll
+                    for (int j = 0; j < HT; ++j)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const int cc = col0 + 8 * j + 2 * t + x;
+                            if (r >= n || cc >= a.Dk) continue;
+                            ((T*)a.dq)[row + cc] = io<T>::to(dq[j][2 * hh + x]);
+                            ((T*)a.dk)[row + cc] = io<T>::to(dkr[j][2 * hh + x]);
+                        }
                 }
             }
         }
