@@ -1,6 +1,7 @@
 /*
  * vmb.h - C ABI of the GB300 (sm_103a) library for the VMamba SS2D selective
- * scan and its channel-mean variant VMeanba (arXiv 2412.16602).
+ * scan and its channel-mean variant VMeanba (arXiv 2412.16602), and for a
+ * channels-last token mixer (gated delta rule, rotary positions, group norm).
  *
  * The SS2D module (App. A, "VMamba" paragraph) is cross-scan -> selective scan
  * per direction -> cross-merge.  The selective scan is the discretised,
@@ -38,9 +39,9 @@
  *     (programmatic dependent launch): their blocks may be scheduled while
  *     the previous kernel of the stream is finishing, and each waits
  *     (griddepcontrol.wait) for that kernel to complete before it reads or
- *     writes global memory.  (Two exceptions: a warp-specialised full scan
- *     whose grid is smaller than one wave is launched normally, so that its
- *     blocks spread over every SM; and inside the calls that start from the map,
+ *     writes global memory.  (Two exceptions: a warp-specialised full scan or
+ *     a chain of the delta rule whose grid is smaller than one wave is launched
+ *     normally, so that its blocks spread over every SM; and inside the calls that start from the map,
  *     the scan's blocks that do not read the map's transpose run beside the
  *     kernel that writes it, which has itself waited for everything before the
  *     call.)  Stream order is therefore kept for any

@@ -62,7 +62,9 @@ def test_delta_backward_and_step_refuse(vmb):
 def test_delta_sizes(vmb):
     ws = vmb.vmb_delta_rule_workspace_bytes
     assert ws(1, 8, 9, False, 1, 1, 16, 16) == 0 and ws(1, 8, 8, False, 2, 3, 16, 16) == 0 and ws(0, 8, 0, False, 1, 1, 16, 16) == 256
-    assert ws(64, 64, 4096, False, 2, 4, 64, 64, True) > ws(64, 64, 4096, False, 4, 4, 64, 64, True) > ws(64, 64, 4096, False, 4, 4, 64, 64)
+    # gradients need dS and dX; in fp32 with Dk > 64 shared heads leave their dq and dk to be summed
+    assert ws(64, 64, 4096, False, 4, 4, 64, 64, True) > ws(64, 64, 4096, False, 4, 4, 64, 64)
+    assert ws(64, 64, 4096, False, 2, 4, 128, 64, True) > ws(64, 64, 4096, False, 4, 4, 128, 64, True)
     saved = vmb.vmb_delta_rule_saved_bytes
     # chunk states [2 chunks][Hv][Dv][Dk] and residuals [tokens][Hv][Dv]
     assert saved(1, 65, 65, False, 2, 64, 32) == 2 * 2 * 64 * 32 * 4 + 65 * 2 * 32 * 4
