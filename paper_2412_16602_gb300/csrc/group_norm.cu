@@ -15,6 +15,8 @@
 // (Chan, Golub & LeVeque 1979), so a mean far from zero costs no digits.  All sums are fp32 in a fixed order.
 #include <cooperative_groups.h>
 
+#include <initializer_list>
+
 #include "delta_internal.h"
 #include "mixer_internal.h"
 #include "vmb_common.cuh"
@@ -446,10 +448,10 @@ __global__ void __launch_bounds__(kNormThreads) norm_dx_kernel(NormLaunch c) {
 struct NormSlab {
     int width, slabs, ctas, rows;
 };
-// Two CTAs per SM, so that one loads or stores while the other computes; a cluster of eight is the portable limit (16
-// CTAs of half the size were slower: 66 against 44 us for 8 x 128 x 128 x 192 in bf16).
+// Several CTAs per SM, so that some load or store while others compute; a cluster of eight is the portable limit (16 CTAs
+// of half the size were slower: 66 against 44 us for 8 x 128 x 128 x 192 in bf16).
 constexpr int kSlabCluster = 8, kSlabThreads = 256;
-constexpr size_t kSlabSmem = 113 * 1024;
+constexpr size_t kSlabSmem = 113 * 1024, kSlabSmall = 57 * 1024;  // two CTAs per SM, three or four
 // The tile, a sum per thread and channel of its vector, two partial sums per thread, and what the cluster's CTAs send:
 // forward one pair per group, gradients one per channel.
 inline size_t slab_smem(long long rows, int width, int groups, int ctas, size_t es, bool grads) {
@@ -458,29 +460,36 @@ inline size_t slab_smem(long long rows, int width, int groups, int ctas, size_t 
 }
 
 // Channels per slab: as many groups as a cluster holds, at least 32 bytes of every pixel (a sector of memory), fewer as
-// long as that gives every SM two CTAs and a pixel still 64 bytes; then CTAs per slab likewise, of 16 pixels or more.
+// long as that gives every SM two CTAs and a pixel still 64 bytes.  CTAs per slab: as few as hold it, more where the
+// SMs would not have two each and the runs stay at 16 pixels or more.  Forward with small tiles where they fit (32 x 56 x
+// 56 x 192 in fp32: 36 us in six CTAs of 50 KB, 42 in eight of 75 KB); the gradients hold x and dy, and their CTAs use
+// more registers (73 us in six CTAs of 100 KB, 79 in clusters of 12 channels of 60 KB).
 bool norm_slab(int B, long long L, int C, int G, vmb_dtype dtype, bool grads, int sms, NormSlab* out) {
     const size_t es = dtype == VMB_BF16 ? 2 : 4;
     const int m = C / G, v = (int)(16 / es);
     if (C % v || L > 1 << 24) return false;
-    int best = 0;
-    for (int g = 1; g <= G; ++g) {
-        if (G % g || (g * m) % v || g * m / v > kSlabThreads || g * m > 2048) continue;
-        if (slab_smem((L + kSlabCluster - 1) / kSlabCluster, g * m, g, kSlabCluster, es, grads) > kSlabSmem) break;
-        const long long ctas = (long long)B * (G / g) * kSlabCluster;
-        if (best && (size_t)best * es >= 64 && ctas < 2LL * sms) break;
-        best = g * m;
+    for (const size_t limit : {kSlabSmall, kSlabSmem}) {
+        if (grads && limit == kSlabSmall) continue;
+        int best = 0;
+        for (int g = 1; g <= G; ++g) {
+            if (G % g || (g * m) % v || g * m / v > kSlabThreads || g * m > 2048) continue;
+            if (slab_smem((L + kSlabCluster - 1) / kSlabCluster, g * m, g, kSlabCluster, es, grads) > limit) break;
+            const long long ctas = (long long)B * (G / g) * kSlabCluster;
+            if (best && (size_t)best * es >= 64 && ctas < 2LL * sms) break;
+            best = g * m;
+        }
+        if (!best || (size_t)best * es < 32) continue;
+        out->width = best;
+        out->slabs = C / best;
+        int n = 1;
+        while (n < kSlabCluster && (slab_smem((L + n - 1) / n, best, best / m, n, es, grads) > limit ||
+                                    ((long long)B * out->slabs * n < 2LL * sms && L / (n + 1) >= 16)))
+            ++n;
+        out->ctas = n;
+        out->rows = (int)((L + n - 1) / n);
+        return true;
     }
-    if (!best || (size_t)best * es < 32) return false;
-    out->width = best;
-    out->slabs = C / best;
-    int n = 1;
-    while (n < kSlabCluster && (slab_smem((L + n - 1) / n, best, best / m, n, es, grads) > kSlabSmem ||
-                                ((long long)B * out->slabs * n < 2LL * sms && L / (2 * n) >= 16)))
-        n *= 2;
-    out->ctas = n;
-    out->rows = (int)((L + n - 1) / n);
-    return true;
+    return false;
 }
 
 struct SlabLaunch {
@@ -514,7 +523,7 @@ __device__ __forceinline__ void column_parts(const float2 (&s1)[(V + 1) / 2], co
 }
 
 template <typename T, int V, int ACT>
-__global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_kernel(SlabLaunch c) {
+__global__ void __launch_bounds__(kSlabThreads, 3) norm_cluster_kernel(SlabLaunch c) {
     namespace cg = cooperative_groups;
     extern __shared__ __align__(16) unsigned char shm[];
     const NormArgs& a = c.a;
@@ -542,11 +551,20 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_kernel(SlabLaunc
     const int left = (int)a.L - (tid & 7) * c.s.rows, run = max(0, min(c.s.rows, left));  // pixels of CTA tid % 8
     cp_async_wait<0>();
     __syncthreads();
+    // a pivot for every group, the mean of eight of its values: their sum's square then takes little from the squares' sum
+    float* pivots = reinterpret_cast<float*>(all);
+    for (int g = tid; g < groups; g += kSlabThreads) {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += rows > 0 ? io<T>::cvt(tile[(long long)(i * rows / 8) * width + g * m + (i & 1) * (m - 1)]) : 0.0f;
+        pivots[g] = 0.125f * s;
+    }
+    __syncthreads();
     {
-        // sums of the differences to the tile's first value of each group, and of their squares
+        // sums of the differences to the pivot of each group, and of their squares
         float2 s1[Vec<T, V>::P] = {}, s2[Vec<T, V>::P] = {}, pivot[Vec<T, V>::P];
         if (on && rows > 0) {
-            fill<V>(pivot, [&](int i) { return io<T>::cvt(tile[(col * V + i) / m * m]); });
+            fill<V>(pivot, [&](int i) { return pivots[(col * V + i) / m]; });
             pivot_sums<T, V>(tile + col * V, width, rl, rows, lanes, pivot, s1, s2);
         }
         column_parts<T, V>(s1, s2, scratch, part, width, cols, lanes, ch1, k1, parts);
@@ -563,7 +581,7 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_kernel(SlabLaunc
             }
             t1 = warp_sum(t1);
             t2 = warp_sum(t2);
-            const float2 v = make_float2((rows > 0 ? io<T>::cvt(tile[g * m]) : 0.0f) + t1 * inv, fmaf(-t1 * inv, t1, t2));
+            const float2 v = make_float2(pivots[g] + t1 * inv, fmaf(-t1 * inv, t1, t2));
             if (lane < ctas) *cl.map_shared_rank(sent + rank * groups + g, lane) = v;  // to every CTA of the cluster
         }
     }

@@ -94,6 +94,7 @@ def test_constant_group_and_large_values():
 
 def test_what_is_not_finite_stays_in_its_group():
     import paper_2412_16602_gb300 as vmb
+    torch.manual_seed(6)
     x = torch.randn(2, 40, 32, device="cuda")
     want = vmb.vmb_group_norm_fwd(x, None, None, 4, act="silu")[0]
     x[1, 3, 9] = float("inf")
@@ -124,6 +125,7 @@ def test_gradient_against_differences():
 def test_workspace_serves_calls_of_any_size_in_turn():
     """Odd addresses give the same values up to rounding, repeated calls the same bits."""
     import paper_2412_16602_gb300 as vmb
+    torch.manual_seed(7)
     shapes = [(1, 9, 64), (100, 30, 32), (3, 1000, 48), (70, 5, 16)]
     xs = [torch.randn(s, device="cuda") for s in shapes]
     first = [vmb.vmb_group_norm_fwd(x, None, None, 4)[0] for x in xs]

@@ -79,6 +79,7 @@ def test_far_and_negative_positions():
 def test_strided_odd_and_in_place(dtype):
     import paper_2412_16602_gb300 as vmb
     dt = TYPES[dtype]
+    torch.manual_seed(8)
     row = torch.randn(2, 12, 3 * 64 + 64 + 1, device="cuda").to(dt)
     q, k = row[..., :192].view(2, 12, 3, 64), row[..., 192:256].view(2, 12, 1, 64)
     freq = torch.rand(32, device="cuda")
