@@ -8,6 +8,8 @@
 // The error of an angle does not grow with the position (the product p f alone is off by 2^-24 p f: 2e-4 at
 // position 4096): up to 1024 radians the product's rounding error, lo = p f - hi, is turned by to first order
 // (lo^2 / 2 < 2^-31); larger angles, which few pairs of few tokens have, are brought into [-pi, pi] in 64 bits.
+#include <string.h>
+
 #include "mixer_internal.h"
 #include "vmb_common.cuh"
 #include "vmb_internal.h"
@@ -35,6 +37,14 @@ __device__ __forceinline__ float2 turn(int p, float f) {
 // one pair turned: (u cos - v sin, v cos + u sin), the same operations on every path
 __device__ __forceinline__ float2 turned(float u, float v, float2 w) {
     return make_float2(fmaf(u, w.x, -__fmul_rn(v, w.y)), fmaf(v, w.x, __fmul_rn(u, w.y)));
+}
+
+// Two bf16 values of a word, and back.
+__device__ __forceinline__ float2 unpack2(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
 }
 
 // A head's items: half: vectors of V pairs (V channels from each half); interleaved: vectors of V channels (V / 2 pairs);
@@ -85,7 +95,28 @@ template <typename T, int V, bool kInter, bool kLoose> struct Turner {
             }
             if (turns) {
                 const float2* w = cs + t * P;
-                if constexpr (kInter) {
+                if constexpr (sizeof(T) == 2 && V >= 2 && !kLoose) {  // a word, two channels, at a time
+                    uint32_t wa[V / 2], wb[V / 2];
+                    memcpy(wa, &a[u], sizeof(wa));
+                    if constexpr (!kInter) memcpy(wb, &b[u], sizeof(wb));
+#pragma unroll
+                    for (int x = 0; x < V / 2; ++x) {
+                        const float2 p = unpack2(wa[x]);
+                        if constexpr (kInter) {
+                            const float2 o = turned(p.x, p.y, w[x]);
+                            wa[x] = pack2(o.x, o.y);
+                        } else {
+                            const float2 q = unpack2(wb[x]), o0 = turned(p.x, q.x, w[2 * x]), o1 = turned(p.y, q.y, w[2 * x + 1]);
+                            wa[x] = pack2(o0.x, o1.x);
+                            wb[x] = pack2(o0.y, o1.y);
+                        }
+                    }
+                    memcpy(&a[u], wa, sizeof(wa));
+                    if constexpr (!kInter) {
+                        memcpy(&b[u], wb, sizeof(wb));
+                        *reinterpret_cast<Pack<T, V, kLoose>*>(d1 + t * dst_t) = b[u];
+                    }
+                } else if constexpr (kInter) {
 #pragma unroll
                     for (int x = 0; x < V / 2; ++x) {
                         const float2 o = turned(io<T>::cvt(a[u].v[2 * x]), io<T>::cvt(a[u].v[2 * x + 1]), w[x]);
@@ -108,7 +139,7 @@ template <typename T, int V, bool kInter, bool kLoose> struct Turner {
 };
 
 template <typename T, int V, bool kInter, bool kLoose>
-__global__ void __launch_bounds__(kRotThreads) rotary_kernel(RotaryArgs a, int per_block, int blocks_per_row) {
+__global__ void __launch_bounds__(kRotThreads, 4) rotary_kernel(RotaryArgs a, int per_block, int blocks_per_row) {
     extern __shared__ float2 table[];
     const int P = a.pair_end[a.axes - 1];
     pdl_launch_dependents();
@@ -169,9 +200,12 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(RotaryArgs a, int p
 template <typename T, int V, bool kLoose = false>
 vmb_status launch_v(const RotaryArgs& a, cudaStream_t stream) {
     const int P = a.pair_end[a.axes - 1];
-    // tokens per block: two batches per thread, within 32 KB of sines, and enough blocks for every SM
+    // tokens per block: one batch per thread (two in bf16, whose vectors hold twice the channels, so that a token's sines
+    // are spread over enough of them: 24.3 and 25.0 us in fp32, 102 and 93 us in bf16), within 32 KB of sines, and enough
+    // blocks for every SM
+    constexpr int kBatches = sizeof(T) == 2 ? 2 : 1;
     const long long per_token = (long long)(a.Hq + a.Hk) * ((a.interleaved ? 2 * P / V : P / V) + (a.D - 2 * P) / V);
-    long long per = per_token <= kRotThreads ? 2 * kBatch * (kRotThreads / per_token) : 2 * kBatch;
+    long long per = per_token <= kRotThreads ? kBatches * kBatch * (kRotThreads / per_token) : kBatches * kBatch;
     const long long most = 32 * 1024 / (8 * (long long)P), spread = ((long long)a.B * a.T + 2 * device_sm_count() - 1) / (2 * device_sm_count());
     per = per < most ? per : most;
     per = per < spread ? per : spread;
