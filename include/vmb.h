@@ -510,12 +510,15 @@ size_t vmb_mean_scan_bwd_workspace_bytes(int B, int K, int D, int N, int H, int 
  *   state before each chunk and the residuals v_t - S^T k_t, for vmb_delta_rule_bwd.
  *   Keys of length above one with beta near one let the state grow, as the recurrence does.
  *   g = -inf forgets the state exactly.  What is not finite in a token reaches the tokens after it,
- *   as the recurrence has it, and no more than the 15 before it (those of its block of 16).  Dk in 1..128 (VMB_ERR_UNSUPPORTED above), any Dv >= 1.
+ *   as the recurrence has it, and no more than the 15 before it (those of its block of 16).  Dk in
+ *   1..128 (VMB_ERR_UNSUPPORTED above), any Dv >= 1.
  *   workspace: >= vmb_delta_rule_workspace_bytes(..., grads = 0, ...) bytes, 256-byte aligned, the
  *   first 256 zero-filled before its first use.
- *   Rounding: bf16 storage takes products of the state and residuals with two bf16 values per
- *   operand (16 bits) where they reach the state, one where they reach only o; fp32 storage takes
- *   two tf32 values per operand (22 bits).  Sums, states and decays are fp32.
+ *   Rounding: with bf16 storage q, k, v and dout enter the products as they are, and what is computed
+ *   (states, residuals, the decayed products of keys and queries) as the sum of two bf16 values (16
+ *   bits), except that S^T q, which only o sees, takes the state's leading term; with fp32 storage
+ *   every operand is the sum of two tf32 values (21 bits).  Sums, states and decays are fp32.  What
+ *   is kept in `saved`, and what the reverse pass hands on per chunk, has the storage type.
  *
  * vmb_delta_rule_bwd - the gradients, given dout = dLoss/do [B, T, Hv, Dv] and dfinal_state =
  * dLoss/dS_T (or NULL): dq, dk, dv, dg, dbeta (shapes and type of the inputs, dense) and

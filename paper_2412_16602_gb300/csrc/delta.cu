@@ -13,96 +13,86 @@ namespace {
 // ------------------------------------------------------------------ joining segments
 
 // One CTA per chain and 8 rows of the transposed state: S' = S X + N from segment to segment (X the
-// segment's map, in reverse its transpose), fp32.  The sums N are replaced by the state at each
-// segment's start (in reverse: the gradient of the state at its end).  A serial walk that reads one map
-// after the other from the L2 cache: the next map and sum are on their way while this one is applied.
+// segment's map, in reverse its transpose, which the chains store for this), fp32.  The sums N are
+// replaced by the state at each segment's start (in reverse: the gradient of the state at its end).
+// A serial walk, bound by the latency of a step: every value of a map is used by one thread, which
+// reads it from the L2 cache one (Dk > 64) or three steps ahead into registers; a group of Dk / 4
+// threads takes every KG-th row of the map for all 8 rows of the state, and the groups' sums meet in
+// shared memory.
 constexpr int kJoinThreads = 256, kJoinRows = 8;
-__global__ void __launch_bounds__(kJoinThreads) delta_join_kernel(DeltaChain c, int reverse) {
-    extern __shared__ __align__(16) float sm[];
+template <int DK> __global__ void __launch_bounds__(kJoinThreads, 1) delta_join_kernel(DeltaChain c, int reverse) {
+    constexpr int L = DK / 4, KG = kJoinThreads / L, E = DK / KG, D = DK == 64 ? 4 : 2, LD = DK + 4;
+    __shared__ __align__(16) float S[DK * kJoinRows];         // [column][row]
+    __shared__ __align__(16) float part[KG * kJoinRows * LD]; // rows four words apart in the banks
     const DeltaArgs& a = c.a;
-    // rows of 16-byte multiples and four words more: whole vectors in, and eight lanes' vectors of eight rows on all banks
-    const int Dk = a.Dk, Dk4 = (Dk + 3) & ~3, ld = Dk4 + 4, tid = threadIdx.x;
-    // thread: column d, rows 4 half .. 4 half + 3
-    const int d = tid & 127, half = tid >> 7;
-    float* S = sm;                    // [Dk4][8]
-    float* X = sm + Dk4 * kJoinRows;  // two maps [Dk4][ld], zeros beyond Dk
-    const int map = Dk4 * ld;
+    const int tid = threadIdx.x, col = 4 * (tid % L), group = tid / L;
     pdl_launch_dependents();
     pdl_wait();
     const int strips = (a.Dv + kJoinRows - 1) / kJoinRows;
-    const int row0 = (int)(blockIdx.x % strips) * kJoinRows + 4 * half;
     const long long chain = blockIdx.x / strips;
+    // the state's values that this thread carries: four columns of one row
+    const int r = tid & 7, oc = 4 * (tid >> 3), row = (int)(blockIdx.x % strips) * kJoinRows + r;
+    const bool own = oc < DK, live = own && row < a.Dv;
     const DeltaSeq seq = delta_seq(a.offsets, (int)(chain / a.Hv), a.T, a.total, c.err);
     const int nseg = ((seq.len + kChunk - 1) / kChunk + c.seg_chunks - 1) / c.seg_chunks;
     const float* init = reverse ? a.dfinal : a.initial;
     float* last = reverse ? a.dinitial : a.final;
-    const bool on = d < Dk;
-    auto place = [&](int i) { return chain * c.segs + (reverse ? nseg - 1 - i : i); };
-    auto fetch = [&](int i) {
-        const float* x = c.maps + place(i) * Dk * Dk;
-        float* to = X + (i & 1) * map;
-        if (Dk % 4 == 0) {
-            for (int j = tid; j < Dk * (Dk / 4); j += kJoinThreads) cp_async16(to + (j / (Dk / 4)) * ld + j % (Dk / 4) * 4, x + 4 * j, 16);
-        } else {
-            for (int j = tid; j < Dk * Dk; j += kJoinThreads) cp_async4(to + (j / Dk) * ld + j % Dk, x + j, 4);
-        }
-        cp_async_commit();
-    };
-    float s[4], n[4];
-    auto sums = [&](int i) {
+    auto sums = [&](int i) { return reinterpret_cast<float4*>(c.sums + ((chain * c.segs + (reverse ? nseg - 1 - i : i)) * a.Dv + row) * DK + oc); };
+    float4 m[D][E], n[D];
+    auto fetch = [&](int i, float4(&x)[E], float4& y) {
+        if (i >= nseg) return;
+        const float* p = c.maps + ((chain * c.segs + (reverse ? nseg - 1 - i : i)) * DK + group) * DK + col;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) n[r] = on && row0 + r < a.Dv ? c.sums[(place(i) * a.Dv + row0 + r) * Dk + d] : 0.0f;
+        for (int e = 0; e < E; ++e) x[e] = *reinterpret_cast<const float4*>(p + e * KG * DK);
+        y = live ? *sums(i) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     };
 #pragma unroll
-    for (int r = 0; r < 4; ++r) s[r] = init && on && row0 + r < a.Dv ? init[(chain * Dk + d) * a.Dv + row0 + r] : 0.0f;
-    for (int j = tid; j < Dk4 * kJoinRows + 2 * map; j += kJoinThreads) sm[j] = 0.0f;
-    __syncthreads();
-    if (nseg > 0) {
-        fetch(0);
-        sums(0);
-    }
-    for (int i = 0; i < nseg; ++i) {
-        if (on) {
-            *reinterpret_cast<float4*>(S + d * kJoinRows + 4 * half) = make_float4(s[0], s[1], s[2], s[3]);
+    for (int u = 0; u < D - 1; ++u) fetch(u, m[u], n[u]);
+    float s[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if (row0 + r < a.Dv) c.sums[(place(i) * a.Dv + row0 + r) * Dk + d] = s[r];
-                s[r] = n[r];
+    for (int j = 0; j < 4; ++j) s[j] = init && live && oc + j < a.Dk ? init[(chain * a.Dk + oc + j) * a.Dv + row] : 0.0f;
+    for (int i0 = 0; i0 < nseg; i0 += D) {
+#pragma unroll
+        for (int u = 0; u < D; ++u) {
+            const int i = i0 + u;
+            if (i >= nseg) break;
+            if (own) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) S[(oc + j) * kJoinRows + r] = s[j];
+            }
+            if (live) *sums(i) = make_float4(s[0], s[1], s[2], s[3]);
+            __syncthreads();
+            fetch(i + D - 1, m[(u + D - 1) % D], n[(u + D - 1) % D]);
+            float2 acc[kJoinRows][2] = {};
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float4* q = reinterpret_cast<const float4*>(S + (e * KG + group) * kJoinRows);
+                const float4 q0 = q[0], q1 = q[1];
+                const float v[kJoinRows] = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
+#pragma unroll
+                for (int j = 0; j < kJoinRows; ++j) {
+                    acc[j][0] = __ffma2_rn(make_float2(v[j], v[j]), make_float2(m[u][e].x, m[u][e].y), acc[j][0]);
+                    acc[j][1] = __ffma2_rn(make_float2(v[j], v[j]), make_float2(m[u][e].z, m[u][e].w), acc[j][1]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kJoinRows; ++j)
+                *reinterpret_cast<float4*>(part + (group * kJoinRows + j) * LD + col) = make_float4(acc[j][0].x, acc[j][0].y, acc[j][1].x, acc[j][1].y);
+            __syncthreads();
+            if (own) {
+                s[0] = n[u].x, s[1] = n[u].y, s[2] = n[u].z, s[3] = n[u].w;
+#pragma unroll
+                for (int k = 0; k < KG; ++k) {
+                    const float4 t = *reinterpret_cast<const float4*>(part + (k * kJoinRows + r) * LD + oc);
+                    s[0] += t.x, s[1] += t.y, s[2] += t.z, s[3] += t.w;
+                }
             }
         }
-        if (i + 1 < nseg) {
-            fetch(i + 1);
-            sums(i + 1);
-            cp_async_wait<1>();
-        } else {
-            cp_async_wait<0>();
-        }
-        __syncthreads();
-        if (on) {
-            const float *m = X + (i & 1) * map + (reverse ? d * ld : d), *q = S + 4 * half;
-            auto step = [&](float v, const float* p) {
-                const float4 u = *reinterpret_cast<const float4*>(p);
-                s[0] = fmaf(u.x, v, s[0]);
-                s[1] = fmaf(u.y, v, s[1]);
-                s[2] = fmaf(u.z, v, s[2]);
-                s[3] = fmaf(u.w, v, s[3]);
-            };
-#pragma unroll 4
-            for (int e = 0; e < Dk4; e += 4) {
-                const float4 v = reverse ? *reinterpret_cast<const float4*>(m + e)
-                                         : make_float4(m[e * ld], m[(e + 1) * ld], m[(e + 2) * ld], m[(e + 3) * ld]);
-                step(v.x, q + e * kJoinRows);
-                step(v.y, q + (e + 1) * kJoinRows);
-                step(v.z, q + (e + 2) * kJoinRows);
-                step(v.w, q + (e + 3) * kJoinRows);
-            }
-        }
-        __syncthreads();  // S and this map have been read
     }
-    if (last && on) {
+    if (last && live) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (row0 + r < a.Dv) last[(chain * Dk + d) * a.Dv + row0 + r] = s[r];
+        for (int j = 0; j < 4; ++j)
+            if (oc + j < a.Dk) last[(chain * a.Dk + oc + j) * a.Dv + row] = s[j];
     }
 }
 
@@ -130,8 +120,9 @@ __global__ void __launch_bounds__(256) delta_share_kernel(const float* part, T* 
 // 4c .. 4c + 3, so that the state is read once and written once and the sums over the rows take three shuffles.  One
 // pass over the old state gives both S^T k and S^T q:
 //   S_t^T q = a S^T q + (q.k) u,  u = b (v - a S^T k).
-// Bound by the state's bytes (8 Dk Dv per row of the batch and head).  (32 channels per warp, twice the registers: 73.6 us
-// for 256 streams of 12 heads of 128 x 128; streaming cache hints: 75.9 us.)
+// Bound by the state's bytes (8 Dk Dv per row of the batch and head): 60.6 us for 256 streams of 12 heads of 128 x 128, 92%
+// of the copy rate; one stream of 6 heads of 64 x 64 takes 2.5 us on the device, less than its launch.  (32 channels per
+// warp, twice the registers: 73.6 us for the 256 streams; with streaming cache hints 75.9 us.)
 template <typename T, int RPL>
 __global__ void __launch_bounds__(128) delta_step_kernel(DeltaStep a) {
     __shared__ float2 qk[8 * RPL];
@@ -240,13 +231,11 @@ vmb_status chain(const DeltaChain& c, bool reverse, cudaStream_t stream) {
 
 vmb_status join(const DeltaChain& c, bool reverse, cudaStream_t stream) {
     const int strips = (c.a.Dv + kJoinRows - 1) / kJoinRows;
-    const size_t d4 = (c.a.Dk + 3) & ~3, smem = 4 * (2 * d4 * (d4 + 4) + d4 * kJoinRows);
-    const void* fn = (const void*)delta_join_kernel;
-    if (!allow_smem(fn, 140 * 1024)) return VMB_ERR_CUDA;
+    const void* fn = c.a.Dk <= 64 ? (const void*)delta_join_kernel<64> : (const void*)delta_join_kernel<128>;
     DeltaChain arg = c;
     int rev = reverse;
     void* args[] = {&arg, &rev};
-    return launch_kernel(fn, dim3((unsigned)(c.a.B * (long long)c.a.Hv * strips)), dim3(kJoinThreads), smem, args, stream) == cudaSuccess
+    return launch_kernel(fn, dim3((unsigned)(c.a.B * (long long)c.a.Hv * strips)), dim3(kJoinThreads), 0, args, stream) == cudaSuccess
                ? VMB_OK : VMB_ERR_CUDA;
 }
 
@@ -304,7 +293,7 @@ DeltaPlan plan_delta(const DeltaArgs& a, bool grads, int sms) {
     // more than half of the SMs idle and each segment still has two chunks.
     if (ctas * 2 <= sms && p.chunks >= 4) {
         long long segs = sms / ctas;
-        if (segs > p.chunks / 2) segs = p.chunks / 2;
+        if (segs > (p.chunks + 1) / 2) segs = (p.chunks + 1) / 2;
         if (segs > 1) {
             p.seg_chunks = (int)((p.chunks + segs - 1) / segs);
             p.segs = (p.chunks + p.seg_chunks - 1) / p.seg_chunks;
@@ -313,9 +302,10 @@ DeltaPlan plan_delta(const DeltaArgs& a, bool grads, int sms) {
     const size_t es = a.dtype == VMB_BF16 ? 2 : 4;
     size_t at = 256;
     p.maps_off = at;
-    if (p.segs > 1) at += align_up((size_t)chains * p.segs * a.Dk * a.Dk * 4, 256);
+    const size_t dk = a.Dk <= 64 ? 64 : 128;  // columns of the kernels' states, zeros behind Dk
+    if (p.segs > 1) at += align_up((size_t)chains * p.segs * dk * dk * 4, 256);
     p.sums_off = at;
-    if (p.segs > 1) at += align_up((size_t)chains * p.segs * a.Dv * a.Dk * 4, 256);
+    if (p.segs > 1) at += align_up((size_t)chains * p.segs * a.Dv * dk * 4, 256);
     p.ds_off = p.dx_off = p.part_off = at;
     if (grads) {
         at += align_up((size_t)p.slots * a.Hv * a.Dv * a.Dk * es, 256);

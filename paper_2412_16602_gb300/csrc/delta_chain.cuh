@@ -8,6 +8,11 @@
 // identity with v = 0 (the same kernel, with Dk more rows).  A first launch computes M and N of
 // every segment, delta_join_kernel (delta.cu) the state at every segment's start, a last launch the
 // outputs.  The gradient of the state runs through M's transpose.
+//
+// What bounds a chain is the length of a chunk's dependent products, issued by one or two state warps per scheduler next to
+// the system warps: in bf16 with Dk = 64 about 6400 cycles a chunk, 2240 of them on the tensor pipe, for some 12000
+// instructions of the CTA; in fp32, six tf32 products and the splits in place of two, about 16000.  HBM is far from it
+// (32 images of 3136 tokens, 3 heads of 64 in bf16: 157 us, 990 GB/s).
 #pragma once
 
 #include "delta_common.cuh"
@@ -329,7 +334,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_forward_kernel(DeltaCh
 
     float S[DK / 8][4];
     if (kOut && c.segs > 1) {
-        load_state_rows<DK>(S, c.sums + (at.chain * c.segs + at.seg) * a.Dv * a.Dk, row0, a.Dv, a.Dk, a.Dk, 1);
+        load_state_rows<DK>(S, c.sums + (at.chain * c.segs + at.seg) * a.Dv * DK, row0, a.Dv, DK, DK, 1);
     } else if (kOut && a.initial) {
         load_state_rows<DK>(S, a.initial + at.chain * a.Dk * a.Dv, row0, a.Dv, a.Dk, 1, a.Dv);
     } else {
@@ -465,10 +470,19 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_forward_kernel(DeltaCh
         }
     } else {
         const long long i = at.chain * c.segs + at.seg;
-        if (map)
-            store_state_rows<DK>(S, c.maps + i * a.Dk * a.Dk, row0, a.Dk, a.Dk);
-        else
-            store_state_rows<DK>(S, c.sums + i * a.Dv * a.Dk, row0, a.Dv, a.Dk);
+        if (map && c.maps_only) {  // for the reverse: transposed
+#pragma unroll
+            for (int n = 0; n < DK / 8; ++n)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int r = row0 + g + 8 * (x >> 1), d = 8 * n + 2 * t + (x & 1);
+                    if (r < DK) c.maps[(i * DK + d) * DK + r] = S[n][x];
+                }
+        } else if (map) {
+            store_state_rows<DK>(S, c.maps + i * DK * DK, row0, DK, DK);
+        } else {
+            store_state_rows<DK>(S, c.sums + i * a.Dv * DK, row0, a.Dv, DK);
+        }
     }
 }
 
@@ -531,7 +545,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_reverse_kernel(DeltaCh
 
     float S[DK / 8][4];
     if (!c.summary && c.segs > 1) {
-        load_state_rows<DK>(S, c.sums + (at.chain * c.segs + at.seg) * a.Dv * a.Dk, row0, a.Dv, a.Dk, a.Dk, 1);
+        load_state_rows<DK>(S, c.sums + (at.chain * c.segs + at.seg) * a.Dv * DK, row0, a.Dv, DK, DK, 1);
     } else if (!c.summary && a.dfinal) {
         load_state_rows<DK>(S, a.dfinal + at.chain * a.Dk * a.Dv, row0, a.Dv, a.Dk, 1, a.Dv);
     } else {
@@ -640,7 +654,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_reverse_kernel(DeltaCh
         bar_arrive(kBarEmpty + (i & 1), kChainThreads);
     }
     if (c.summary) {
-        store_state_rows<DK>(S, c.sums + (at.chain * c.segs + at.seg) * a.Dv * a.Dk, row0, a.Dv, a.Dk);
+        store_state_rows<DK>(S, c.sums + (at.chain * c.segs + at.seg) * a.Dv * DK, row0, a.Dv, DK);
     } else if (a.dinitial && c.segs == 1) {
         float* dst = a.dinitial + at.chain * a.Dk * a.Dv;
 #pragma unroll

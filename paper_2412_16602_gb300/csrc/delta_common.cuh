@@ -17,10 +17,10 @@
 // rows from product to product in registers, without a barrier or a trip through shared memory
 // (measured on the GB300: 604 TFLOP/s in bf16, 302 in tf32 and 21 cycles of latency, against a
 // dependent chain of four products per chunk).  What a product rounds:
-//   bf16 storage: q, k, v and do are exact.  Intermediates (states, residuals, E, the diagonal
-//     inverses) enter as the sum of two bf16 values (16 bits, error about 2^-18) wherever they
-//     reach the state, as one where they only reach an output that is rounded to bf16 itself.
-//   fp32 storage: every operand is the sum of two tf32 values (22 bits), products hi.hi + hi.lo + lo.hi.
+//   bf16 storage: q, k, v and do are exact.  Intermediates (states, residuals, E, P, the diagonal
+//     inverses) enter as the sum of two bf16 values (16 bits, error about 2^-18); only S^T q takes the
+//     state's leading term, because nothing but an output that is rounded to bf16 itself sees it.
+//   fp32 storage: every operand is the sum of two tf32 values (21 bits), products hi.hi + hi.lo + lo.hi.
 // Accumulators, states, decays and the diagonal inverses are fp32 throughout.
 #pragma once
 

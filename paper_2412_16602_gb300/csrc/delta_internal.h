@@ -40,7 +40,7 @@ struct DeltaPlan {
     int segs, seg_chunks;
     bool wide;       // 128 rows of the state per CTA instead of 64
     long long slots; // chunk states kept
-    size_t maps_off, sums_off;        // segment maps [chain][seg][Dk][Dk] and sums [chain][seg][Dv][Dk], fp32
+    size_t maps_off, sums_off;        // segment maps [chain][seg][dk][dk] and sums [chain][seg][Dv][dk], fp32, dk = 64 or 128
     size_t ds_off, dx_off, part_off;  // gradients: chunk-end dS, dX, per-value-head dq and dk
     size_t bytes;
 };
@@ -53,9 +53,9 @@ struct DeltaChain {
     int segs, seg_chunks, slices;
     bool wide;
     int summary;       // 1: write the sums (and, forward, the maps) of every segment and nothing else
-    int maps_only;     // forward summary: the maps alone
-    float* maps;       // [chain][seg][Dk][Dk]
-    float* sums;       // [chain][seg][Dv][Dk]: the sums, then the state at each segment's start (end in reverse)
+    int maps_only;     // forward summary: the maps alone, for the reverse
+    float* maps;       // [chain][seg][dk][dk], dk = 64 or 128 (maps_only: transposed)
+    float* sums;       // [chain][seg][Dv][dk]: the sums, then the state at each segment's start (end in reverse)
     void* ds;          // reverse: [slots][Hv][Dv][Dk] dS at each chunk's end
     void* dx;          // reverse: [tokens][Hv][Dv]
     unsigned* err;

@@ -502,6 +502,11 @@ struct SlabLaunch {
     unsigned* counter;
 };
 
+// A CTA's shared memory is written to by the others only once it has started: every CTA says so and, before it sends,
+// waits for the others.  Nothing but the start itself is passed on, so that the arrival orders no memory.
+__device__ __forceinline__ void cluster_started() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void wait_cluster_started() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
+
 // A thread's sums of its V channels, two each, summed over the threads of a column in two steps, in order: afterwards
 // part[k width + ch], k < parts, holds the partial sums of channel ch.  ch0, k0: the thread's number as k0 width + ch0.
 template <typename T, int V>
@@ -537,7 +542,7 @@ __global__ void __launch_bounds__(kSlabThreads, 3) norm_cluster_kernel(SlabLaunc
     float* scratch = reinterpret_cast<float*>(shm + (((size_t)c.s.rows * width * sizeof(T) + 15) & ~(size_t)15));
     float2 *part = reinterpret_cast<float2*>(scratch + kSlabThreads * V), *sent = part + max(width, kSlabThreads);  // sent: [ctas][groups] mean and M2
     float2* all = sent + ctas * groups;
-    cl.barrier_arrive();  // (a CTA's shared memory is written to by the others only once it has started)
+    cluster_started();
     pdl_launch_dependents();
     pdl_wait();
     const long long slab = blockIdx.x / ctas;
@@ -572,7 +577,7 @@ __global__ void __launch_bounds__(kSlabThreads, 3) norm_cluster_kernel(SlabLaunc
             pivot_sums<T, V>(tile + col * V, width, rl, rows, lanes, pivot, s1, s2);
         }
         column_parts<T, V>(s1, s2, scratch, part, width, cols, lanes, ch1, k1, parts);
-        cl.barrier_wait();
+        wait_cluster_started();
         const float inv = 1.0f / ((float)max(rows, 1) * m);
         for (int g = w; g < groups; g += kSlabThreads / 32) {
             float t1 = 0.0f, t2 = 0.0f;
@@ -638,7 +643,7 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_grad_kernel(Slab
     float* scratch = reinterpret_cast<float*>(shm + (((size_t)2 * c.s.rows * width * sizeof(T) + 15) & ~(size_t)15));
     float2 *part = reinterpret_cast<float2*>(scratch + kSlabThreads * V), *sent = part + max(width, kSlabThreads);  // sent: [ctas][width] sums of dz, dz n
     float2* mine = sent + ctas * width;
-    cl.barrier_arrive();  // (a CTA's shared memory is written to by the others only once it has started)
+    cluster_started();
     pdl_launch_dependents();
     pdl_wait();
     const long long slab = blockIdx.x / ctas;
@@ -665,7 +670,7 @@ __global__ void __launch_bounds__(kSlabThreads, 2) norm_cluster_grad_kernel(Slab
         float2 s1[Vec<T, V>::P] = {}, s2[Vec<T, V>::P] = {};
         if (on) slope_sums<T, V, ACT>(tx + col * V, td + col * V, width, rl, rows, lanes, ca, cc, mu, s1, s2);
         column_parts<T, V>(s1, s2, scratch, part, width, cols, lanes, ch1, k1, parts);
-        cl.barrier_wait();
+        wait_cluster_started();
         for (int ch = tid; ch < width; ch += kSlabThreads) {  // to every CTA of the cluster
             float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll 4
