@@ -289,9 +289,12 @@ DeltaPlan plan_delta(const DeltaArgs& a, bool grads, int sms) {
     p.segs = 1;
     p.seg_chunks = p.chunks;
     const long long ctas = chains * ((a.Dv + (p.wide ? 127 : 63)) / (p.wide ? 128 : 64));
-    // Segments cost a second pass over the chunks (and Dk more rows in it): taken when the chains leave
-    // more than half of the SMs idle and each segment still has two chunks.
-    if (ctas * 2 <= sms && p.chunks >= 4) {
+    // Segments cost a second pass over the chunks, with Dk more rows in it, and the walk that joins them.  Two chunks each or
+    // more; taken where they fill the SMs at least four times better, three times for sequences of 64 chunks.  Measured with
+    // and without: 36 CTAs (chains and slices of 64 or 128 channels) of 1568 tokens 165 and 212 us in fp32 (64 channels), 70 and
+    // 76 in bf16 (64), 173 and 165 (128); 48 CTAs 217 and 212, 85 and 77, 207 and 165, but for 4096 tokens 485 and 533, 178
+    // and 199, 404 and 409; 54 CTAs of 4096 tokens, two segments each, 635 and 542, 241 and 202, 538 and 409.
+    if (ctas * (p.chunks >= 64 ? 3 : 4) <= sms && p.chunks >= 4) {
         long long segs = sms / ctas;
         if (segs > (p.chunks + 1) / 2) segs = (p.chunks + 1) / 2;
         if (segs > 1) {
