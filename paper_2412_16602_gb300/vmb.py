@@ -159,9 +159,24 @@ def _stream(stream) -> int:
     return s.cuda_stream
 
 
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _on_its_stream(call):
+    """`call` with `stream` as the current stream: what it allocates and fills belongs to the stream that it launches on."""
+    @functools.wraps(call)
+    def wrapped(*args, stream=None, **kwargs):
+        if stream is None:
+            return call(*args, **kwargs)
+        with torch.cuda.stream(stream):
+            return call(*args, stream=stream, **kwargs)
+    return wrapped
+
+
 # ---------------------------------------------------------------- cross-scan / merge
 
 
+@_on_its_stream
 def vmb_cross_scan(x: torch.Tensor, xs: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """x [B, D, H, W] -> xs [B, 4, D, H*W] (bit-exact permutation)."""
     _dev(x, "x")
@@ -176,6 +191,7 @@ def vmb_cross_scan(x: torch.Tensor, xs: torch.Tensor | None = None, stream=None)
     return xs
 
 
+@_on_its_stream
 def vmb_cross_merge(ys: torch.Tensor, H: int, W: int, out: torch.Tensor | None = None,
                     stream=None) -> torch.Tensor:
     """ys [B, 4, D, H*W] -> out [B, D, H, W]."""
@@ -207,25 +223,36 @@ def vmb_scan_kernel_count(path: int, B: int, K: int, D: int, N: int, H: int, W: 
 
 
 class Workspace:
-    """A zero-initialised device workspace that grows on demand (one per device).
+    """Zero-initialised device workspaces that grow on demand: one per thread, device and current stream, so that calls
+    which may overlap in time never share one.
 
-    The library keeps a workspace ready for the next call by itself; only a
-    newly allocated buffer needs zero-filling, which torch.zeros does."""
+    A buffer is allocated and zero-filled on the stream whose calls use it, which also orders the reuse of the memory of
+    a buffer that was outgrown.  The library keeps a workspace ready for the next call by itself.  While the stream is
+    being captured into a graph every call gets a buffer of its own, which the graph fills and holds: a kept one would be
+    shared by the graph's replays and later calls, and one made during the capture is not filled before a replay."""
 
     def __init__(self):
-        self._bufs = {}
-        self._lock = threading.Lock()
+        self._local = threading.local()
+
+    def buffers(self) -> dict:
+        """(device index, raw stream) -> buffer, of the calling thread."""
+        try:
+            return self._local.bufs
+        except AttributeError:
+            self._local.bufs = {}
+            return self._local.bufs
 
     def get(self, nbytes: int, device: torch.device) -> torch.Tensor:
-        key = (device.type, device.index)
-        with self._lock:
-            buf = self._bufs.get(key)
-            if buf is None or buf.numel() < nbytes:
-                n = max(nbytes, 256)
-                n = (n + 255) // 256 * 256
-                buf = torch.zeros(n, dtype=torch.uint8, device=device)
-                self._bufs[key] = buf
-            return buf
+        index = torch.cuda.current_device() if device.index is None else device.index
+        bufs, key = self.buffers(), (index, _raw_stream(index))
+        capturing = torch.cuda.is_current_stream_capturing()
+        buf = bufs.get(key)
+        if buf is None or buf.numel() < nbytes or capturing:
+            n = (max(nbytes, 256) + 255) // 256 * 256
+            buf = torch.zeros(n, dtype=torch.uint8, device=torch.device("cuda", index))
+            if not capturing:
+                bufs[key] = buf
+        return buf
 
 
 _default_ws = Workspace()
@@ -250,6 +277,7 @@ def _scan_shapes(u, delta, A, Bs, Cs, Dskip, delta_bias, H, W):
     return B, K, D, N, L
 
 
+@_on_its_stream
 def vmb_selective_scan_fwd(u, delta, A, Bs, Cs, Dskip, delta_bias, H: int, W: int, *,
                            y=None, flags: int = VMB_FLAG_SOFTPLUS, workspace=None,
                            stream=None) -> torch.Tensor:
@@ -270,6 +298,7 @@ def vmb_selective_scan_fwd(u, delta, A, Bs, Cs, Dskip, delta_bias, H: int, W: in
     return y
 
 
+@_on_its_stream
 def vmb_mean_scan_fwd(u, delta, A, Bs, Cs, Dskip, delta_bias, H: int, W: int, *,
                       y=None, ybar=None, want_ybar: bool = False, flags: int = VMB_FLAG_SOFTPLUS,
                       workspace=None, stream=None):
@@ -296,6 +325,7 @@ def vmb_mean_scan_fwd(u, delta, A, Bs, Cs, Dskip, delta_bias, H: int, W: int, *,
     return y, ybar
 
 
+@_on_its_stream
 def vmb_mean_scan_grouped_fwd(u, delta, A, Bs, Cs, Dskip, delta_bias, H: int, W: int, groups: int, *,
                               y=None, ybar=None, want_ybar: bool = False, flags: int = VMB_FLAG_SOFTPLUS,
                               workspace=None, stream=None):
@@ -325,6 +355,7 @@ def vmb_mean_scan_grouped_fwd(u, delta, A, Bs, Cs, Dskip, delta_bias, H: int, W:
     return y, ybar
 
 
+@_on_its_stream
 def vmb_mean_scan_train_fwd(u, delta, A, Bs, Cs, Dskip, delta_bias, H: int, W: int, *, groups: int = 1,
                             y=None, ybar=None, saved=None, flags: int = VMB_FLAG_SOFTPLUS, workspace=None,
                             stream=None):
@@ -357,6 +388,7 @@ def vmb_mean_scan_train_fwd(u, delta, A, Bs, Cs, Dskip, delta_bias, H: int, W: i
     return y, saved, ybar
 
 
+@_on_its_stream
 def vmb_mean_scan_merge_fwd(u, delta, A, Bs, Cs, Dskip, delta_bias, x, H: int, W: int, *,
                             out=None, ybar=None, flags: int = VMB_FLAG_SOFTPLUS, workspace=None, stream=None):
     """Channel-mean path with the broadcast fused into the cross-merge:
@@ -387,6 +419,7 @@ def vmb_mean_scan_merge_fwd(u, delta, A, Bs, Cs, Dskip, delta_bias, x, H: int, W
     return out, ybar
 
 
+@_on_its_stream
 def vmb_ss2d_mean_fwd(x, delta, A, Bs, Cs, Dskip, delta_bias, *, out=None, ybar=None, xt=None,
                       flags: int = VMB_FLAG_SOFTPLUS, workspace=None, stream=None):
     """The scan side of a VMeanba SS2D block from the map: cross-scan, channel-mean scan and
@@ -432,6 +465,7 @@ def vmb_ss2d_mean_fwd(x, delta, A, Bs, Cs, Dskip, delta_bias, *, out=None, ybar=
     return out, ybar
 
 
+@_on_its_stream
 def vmb_ss2d_full_fwd(x, delta, A, Bs, Cs, Dskip, delta_bias, *, out=None, y=None, xt=None,
                       flags: int = VMB_FLAG_SOFTPLUS, workspace=None, stream=None):
     """The scan side of a full-channel SS2D block from the map: cross-scan, selective scan and
@@ -494,6 +528,7 @@ def _disc_shapes(u, delta, A, Bs, delta_bias, H, W):
     return B, K, D, N, L
 
 
+@_on_its_stream
 def vmb_discretise_fwd(u, delta, A, Bs, delta_bias, H: int, W: int, *, dA=None, dBu=None,
                        flags: int = VMB_FLAG_SOFTPLUS, stream=None):
     """Eqs. 4, 6 outside the scan: (dA, dBu), each float32 [B, K, D, N, H*W]."""
@@ -511,6 +546,7 @@ def vmb_discretise_fwd(u, delta, A, Bs, delta_bias, H: int, W: int, *, dA=None, 
     return dA, dBu
 
 
+@_on_its_stream
 def vmb_discretise_mean_fwd(u, delta, A, Bs, delta_bias, H: int, W: int, *, dAm=None, dBum=None,
                             flags: int = VMB_FLAG_SOFTPLUS, stream=None):
     """Channel means of the discretised operands (Eq. 9's T): (dAm, dBum), float32 [B, K, N, H*W]."""
@@ -528,6 +564,7 @@ def vmb_discretise_mean_fwd(u, delta, A, Bs, delta_bias, H: int, W: int, *, dAm=
     return dAm, dBum
 
 
+@_on_its_stream
 def vmb_scan_only_fwd(dA, dBu, Cs, H: int, W: int, *, y=None, stream=None):
     """The scan alone (Eq. 3 without the skip): dA, dBu float32 [B, K, Dm, N, L] (or
     [B, K, N, L] for one channel), Cs [B, K, N, L] -> y float32 [B, K, Dm, L] (or [B, K, L])."""
@@ -551,6 +588,7 @@ def vmb_scan_only_fwd(dA, dBu, Cs, H: int, W: int, *, y=None, stream=None):
     return y
 
 
+@_on_its_stream
 def vmb_selection_fwd(u, WB, WC, Wz, Wup, H: int, W: int, *, delta_raw=None, Bs=None, Cs=None, stream=None):
     """Eq. 6 selection functions: u [B, K, D, H*W] -> (delta_raw [B, K, D, L], Bs, Cs [B, K, N, L]),
     all in u's dtype; WB, WC [K, N, D], Wz [K, R, D], Wup [K, D, R] float32."""
@@ -576,6 +614,7 @@ def vmb_selection_fwd(u, WB, WC, Wz, Wup, H: int, W: int, *, delta_raw=None, Bs=
     return delta_raw, Bs, Cs
 
 
+@_on_its_stream
 def vmb_selection_lowrank_fwd(u, WB, WC, Wz, H: int, W: int, *, z=None, Bs=None, Cs=None, stream=None):
     """Eq. 6 selection functions with the Delta branch left low-rank: u [B, K, D, H*W] ->
     (z [B, K, R, L] float32, Bs, Cs [B, K, N, L] in u's dtype); WB, WC [K, N, D], Wz [K, R, D]."""
@@ -601,6 +640,7 @@ def vmb_selection_lowrank_fwd(u, WB, WC, Wz, H: int, W: int, *, z=None, Bs=None,
     return z, Bs, Cs
 
 
+@_on_its_stream
 def vmb_selective_scan_lowrank_fwd(u, z, Wup, A, Bs, Cs, Dskip, delta_bias, H: int, W: int, *, y=None,
                                    flags: int = VMB_FLAG_SOFTPLUS, workspace=None, stream=None) -> torch.Tensor:
     """Full-channel selective scan whose raw Deltas are Wup z, formed inside the scan:
@@ -629,6 +669,7 @@ def vmb_selective_scan_lowrank_fwd(u, z, Wup, A, Bs, Cs, Dskip, delta_bias, H: i
     return y
 
 
+@_on_its_stream
 def vmb_mean_scan_lowrank_fwd(u, z, Wup, A, Bs, Cs, Dskip, delta_bias, H: int, W: int, *, y=None, ybar=None,
                               want_ybar: bool = False, flags: int = VMB_FLAG_SOFTPLUS, workspace=None, stream=None):
     """Channel-mean scan whose raw Deltas are Wup z, formed inside the scan: z [B, K, R, H*W]
@@ -668,6 +709,7 @@ def vmb_mean_scan_bwd_workspace_bytes(B: int, K: int, D: int, N: int, H: int, W:
     return int(lib.vmb_mean_scan_bwd_workspace_bytes(B, K, D, N, H, W, groups, _dtype_code(dtype)))
 
 
+@_on_its_stream
 def vmb_mean_scan_bwd(u, delta, A, Bs, Cs, Dskip, delta_bias, gy, H: int, W: int, *, groups: int = 1,
                       saved=None, flags: int = VMB_FLAG_SOFTPLUS, workspace=None, stream=None) -> dict:
     """Gradients of the (grouped) channel-mean scan given gy = dLoss/dy [B, K, D, H*W]: returns
@@ -708,9 +750,6 @@ _norm_ws = Workspace()
 
 
 # (a step of one token takes 2.5 us on the device: the marshalling below keeps to what it needs)
-_raw_stream = torch._C._cuda_getCurrentRawStream
-
-
 def _stream_of(t: torch.Tensor, stream) -> int:
     return _raw_stream(t.device.index) if stream is None else stream.cuda_stream
 
@@ -725,10 +764,11 @@ def _norm_bytes(device, *sizes) -> int:
     return lib.vmb_group_norm_workspace_bytes(*sizes)
 
 
-def delta_workspace(device=None) -> torch.Tensor:
-    """The default workspace of the delta rule's calls (for vmb_read_status)."""
-    dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-    return _delta_ws.get(256, dev)
+@_on_its_stream
+def delta_workspace(device=None, stream=None) -> torch.Tensor:
+    """The default workspace of the calling thread's delta rule calls on a stream, the current one if none is given (for
+    vmb_read_status; autograd runs backward passes in a thread of its own)."""
+    return _delta_ws.get(256, torch.device("cuda" if device is None else device))
 
 
 def _heads(t: torch.Tensor, name: str):
@@ -800,6 +840,7 @@ def vmb_delta_rule_saved_bytes(B: int, T: int, total: int, packed: bool, Hv: int
     return int(lib.vmb_delta_rule_saved_bytes(B, T, total, int(packed), Hv, Dk, Dv, _dtype_code(dtype)))
 
 
+@_on_its_stream
 def vmb_delta_rule_fwd(q, k, v, g, beta, *, initial_state=None, offsets=None, max_len=None, scale=None,
                        want_state: bool = False, want_saved: bool = False, o=None, final_state=None, saved=None,
                        workspace=None, stream=None):
@@ -843,6 +884,7 @@ def _saved_bytes(saved, N, longest, total, offsets, Hv, Dk, Dv, code):
         raise ValueError(f"saved must be uint8 with at least {n} bytes")
 
 
+@_on_its_stream
 def vmb_delta_rule_bwd(q, k, v, g, beta, do, saved, *, dfinal_state=None, offsets=None, max_len=None, scale=None,
                        want_initial: bool = False, workspace=None, stream=None) -> dict:
     """Gradients of vmb_delta_rule_fwd given do = dLoss/do [B, T, Hv, Dv] and, optionally, dfinal_state: returns
@@ -871,6 +913,7 @@ def vmb_delta_rule_bwd(q, k, v, g, beta, do, saved, *, dfinal_state=None, offset
     return out
 
 
+@_on_its_stream
 def vmb_delta_rule_step(q, k, v, g, beta, state, *, slots=None, scale=None, o=None, stream=None) -> torch.Tensor:
     """The recurrence for T tokens (one, or a few) of every row from its state, updated in place: q, k [B, T, Hk, Dk],
     v [B, T, Hv, Dv], g, beta [B, T, Hv], state float32 [pool, Hv, Dk, Dv]; slots int32 [B] (row b uses state
@@ -910,6 +953,7 @@ def _rotary_out(x, out, name, dense):
     return out
 
 
+@_on_its_stream
 def vmb_rotary_fwd(q, k, freq, positions=None, *, sections, grid=None, interleaved: bool = False,
                    inverse: bool = False, q_out=None, k_out=None, stream=None):
     """Rotary positions with len(sections) axes on q [B, T, Hq, D] and k [B, T, Hk, D] (or None; rows of tokens may be
@@ -977,6 +1021,7 @@ def _norm_inputs(x, weight, bias, groups, act):
     return B, L, C, _dtype_code(x.dtype), _ACTS[act]
 
 
+@_on_its_stream
 def vmb_group_norm_fwd(x, weight, bias, groups: int, *, eps: float = 1e-5, act: str = "none", want_stats: bool = False,
                        y=None, stats=None, workspace=None, stream=None):
     """Group norm with an activation ("none", "silu", "gelu"), channels last: x [B, ..., C], weight and bias float32
@@ -998,6 +1043,7 @@ def vmb_group_norm_fwd(x, weight, bias, groups: int, *, eps: float = 1e-5, act: 
     return y, stats
 
 
+@_on_its_stream
 def vmb_group_norm_bwd(x, weight, bias, stats, dy, groups: int, *, act: str = "none", workspace=None, stream=None) -> dict:
     """Gradients of vmb_group_norm_fwd given dy and the forward's stats: dict(x, weight, bias), the latter two float32
     [C] (None where the input was None)."""
@@ -1018,14 +1064,21 @@ def vmb_group_norm_bwd(x, weight, bias, stats, dy, groups: int, *, act: str = "n
     return out
 
 
+@_on_its_stream
 def vmb_read_status(workspace=None, device=None, stream=None) -> int:
-    """Synchronise and return (then clear) the device error word of a workspace."""
-    if workspace is None:
-        dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-        workspace = _default_ws.get(256, dev)
-    return int(lib.vmb_read_status(_ptr(workspace), _stream(stream)))
+    """Synchronise and return (then clear) the device error word of a workspace; without one, of the default workspaces
+    that the calling thread's scans have used on the device (VMB_OK, or an error of one of them)."""
+    if workspace is not None:
+        return int(lib.vmb_read_status(_ptr(workspace), _stream(stream)))
+    dev = torch.device("cuda" if device is None else device)
+    index = torch.cuda.current_device() if dev.index is None else dev.index
+    _default_ws.get(256, dev)
+    torch.cuda.synchronize(index)
+    found = [int(lib.vmb_read_status(_ptr(buf), _stream(stream))) for (i, _), buf in _default_ws.buffers().items() if i == index]
+    return next((status for status in found if status != VMB_OK), VMB_OK)
 
 
-def default_workspace(device=None) -> torch.Tensor:
-    dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-    return _default_ws.get(256, dev)
+@_on_its_stream
+def default_workspace(device=None, stream=None) -> torch.Tensor:
+    """The default workspace of the calling thread's scans on a stream (the current one if none is given)."""
+    return _default_ws.get(256, torch.device("cuda" if device is None else device))
