@@ -75,33 +75,23 @@ struct NormLaunch {
     int first;  // first sample of the launch
 };
 
-// tanh on the MUFU pipe, good to 2^-11: used where the result is rounded to bf16 (2^-9)
-__device__ __forceinline__ float tanh_fast(float x) {
-    float y;
-    asm("tanh.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
-// The logistic function of two values: 1 / (1 + e^-z), for bf16 storage (1 + tanh(z / 2)) / 2 (one MUFU operation for two).
-template <typename T> __device__ __forceinline__ float2 sigmoid2(float2 z) {
-    if constexpr (sizeof(T) == 2) {
-        const float2 h = __fmul2_rn(z, both(0.5f));
-        return __ffma2_rn(make_float2(tanh_fast(h.x), tanh_fast(h.y)), both(0.5f), both(0.5f));
-    } else {
-        const float2 e = __fmul2_rn(z, both(-kLog2e));
-        const float2 d = __fadd2_rn(make_float2(ex2(e.x), ex2(e.y)), both(1.0f));
-        return make_float2(rcp(d.x), rcp(d.y));
-    }
+// The logistic function of two values, 1 / (1 + e^-z), to a few 2^-22 of itself: where z is far below zero the results are
+// small and keep their digits (half of 1 + tanh(z / 2), one operation of the MUFU pipe instead of two, does not: 2^-12 of one).
+__device__ __forceinline__ float2 sigmoid2(float2 z) {
+    const float2 e = __fmul2_rn(z, both(-kLog2e));
+    const float2 d = __fadd2_rn(make_float2(ex2(e.x), ex2(e.y)), both(1.0f));
+    return make_float2(rcp(d.x), rcp(d.y));
 }
-template <typename T, int ACT> __device__ __forceinline__ float2 act_value(float2 z) {
-    if constexpr (ACT == VMB_ACT_SILU) return __fmul2_rn(z, sigmoid2<T>(z));
+template <int ACT> __device__ __forceinline__ float2 act_value(float2 z) {
+    if constexpr (ACT == VMB_ACT_SILU) return __fmul2_rn(z, sigmoid2(z));
     if constexpr (ACT == VMB_ACT_GELU)
         return __fmul2_rn(__fmul2_rn(z, both(0.5f)), make_float2(1.0f + erff(z.x * 0.70710678118654752f), 1.0f + erff(z.y * 0.70710678118654752f)));
     return z;
 }
-template <typename T, int ACT> __device__ __forceinline__ float2 act_slope(float2 z) {
+template <int ACT> __device__ __forceinline__ float2 act_slope(float2 z) {
     if constexpr (ACT == VMB_ACT_SILU) {  // s (1 + z (1 - s)) = s + (z s) (1 - s)
-        const float2 s = sigmoid2<T>(z), r = __ffma2_rn(s, both(-1.0f), both(1.0f));
+        const float2 s = sigmoid2(z), r = __ffma2_rn(s, both(-1.0f), both(1.0f));
         return __ffma2_rn(__fmul2_rn(z, s), r, s);
     }
     if constexpr (ACT == VMB_ACT_GELU)
@@ -141,7 +131,7 @@ __device__ __forceinline__ void apply_rows(const T* x, long long x_step, T* y, l
     for (int r = first; r < rows; r += lanes) {
         Vec<T, V> f = load_vec<T, V>(x + r * x_step);
 #pragma unroll
-        for (int i = 0; i < Vec<T, V>::P; ++i) f.v[i] = act_value<T, ACT>(__ffma2_rn(f.v[i], a[i], c[i]));
+        for (int i = 0; i < Vec<T, V>::P; ++i) f.v[i] = act_value<ACT>(__ffma2_rn(f.v[i], a[i], c[i]));
         store_vec<T, V>(y + r * y_step, f);
     }
 }
@@ -155,7 +145,7 @@ __device__ __forceinline__ void slope_sums(const T* x, const T* dy, long long st
         const Vec<T, V> f = load_vec<T, V>(x + r * step), d = load_vec<T, V>(dy + r * step);
 #pragma unroll
         for (int i = 0; i < Vec<T, V>::P; ++i) {
-            const float2 dz = __fmul2_rn(d.v[i], act_slope<T, ACT>(__ffma2_rn(f.v[i], a[i], c[i])));
+            const float2 dz = __fmul2_rn(d.v[i], act_slope<ACT>(__ffma2_rn(f.v[i], a[i], c[i])));
             s1[i] = __fadd2_rn(s1[i], dz);
             s2[i] = __ffma2_rn(dz, __ffma2_rn(mean[i], both(-1.0f), f.v[i]), s2[i]);
         }
@@ -172,7 +162,7 @@ __device__ __forceinline__ void dx_rows(const T* x, const T* dy, long long step,
         const Vec<T, V> d = load_vec<T, V>(dy + r * step);
 #pragma unroll
         for (int i = 0; i < Vec<T, V>::P; ++i) {
-            const float2 dz = __fmul2_rn(d.v[i], act_slope<T, ACT>(__ffma2_rn(f.v[i], a[i], c[i])));
+            const float2 dz = __fmul2_rn(d.v[i], act_slope<ACT>(__ffma2_rn(f.v[i], a[i], c[i])));
             const float2 t = __ffma2_rn(__ffma2_rn(mean[i], both(-1.0f), f.v[i]), k2[i], k1[i]);
             f.v[i] = __ffma2_rn(t, both(-1.0f), __fmul2_rn(a[i], dz));
         }
