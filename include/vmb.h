@@ -584,7 +584,7 @@ vmb_status vmb_rotary_fwd(const void* q, const void* k, const float* freq, const
  *   workspace: >= vmb_group_norm_workspace_bytes(...) bytes, 256-byte aligned, all of it
  *   zero-filled before its first use; calls that share one must not overlap in time.
  */
-typedef enum { VMB_ACT_NONE = 0, VMB_ACT_SILU = 1, VMB_ACT_GELU = 2 } vmb_act; /* GELU: z Phi(z), by erf */
+typedef enum { VMB_ACT_NONE = 0, VMB_ACT_SILU = 1, VMB_ACT_GELU = 2 } vmb_act; /* GELU: z Phi(z), Phi the normal distribution */
 size_t vmb_group_norm_workspace_bytes(int B, int64_t L, int C, int G, int grads, vmb_dtype dtype);
 vmb_status vmb_group_norm_fwd(const void* x, const float* weight, const float* bias, void* y, float* stats,
                               int B, int64_t L, int C, int G, float eps, vmb_act act, vmb_dtype dtype,

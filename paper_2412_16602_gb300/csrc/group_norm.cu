@@ -83,10 +83,29 @@ __device__ __forceinline__ float2 sigmoid2(float2 z) {
     const float2 d = __fadd2_rn(make_float2(ex2(e.x), ex2(e.y)), both(1.0f));
     return make_float2(rcp(d.x), rcp(d.y));
 }
+// Of two values the normal distribution's tail, Phi(-|z|) = e^(-z^2 / 2) M(|z|), and that exponential.  M (Mills' ratio over
+// sqrt(2 pi)) is t times a polynomial in t = 1 / (1 + 0.28 |z|), fitted here to the smallest largest relative error over all
+// |z|: 1.7e-7, 4.8e-7 in fp32.  The tail keeps its digits, which (1 + erf) / 2 loses below -3.  The square's rounding
+// error enters the exponent beside it; beyond 16 everything is zero.
+__device__ __forceinline__ float2 normal_tail(float2 z, float2& e) {
+    const float2 y = make_float2(fminf(fabsf(z.x), 16.0f), fminf(fabsf(z.y), 16.0f));
+    const float2 d = __ffma2_rn(y, both(0.28f), both(1.0f)), t = make_float2(rcp(d.x), rcp(d.y));
+    const float2 h = __fmul2_rn(y, y), l = __ffma2_rn(y, y, make_float2(-h.x, -h.y));
+    const float2 x = __ffma2_rn(h, both(-0.5f * kLog2e), __fmul2_rn(l, both(-0.5f * kLog2e)));
+    e = make_float2(ex2(x.x), ex2(x.y));
+    constexpr float k[] = {0.0247199844f, -0.0935931646f, 0.0924281759f, -0.00644922176f, 0.0727750275f, 0.0836307883f, 0.103084665f, 0.111699803f, 0.111703858f};
+    float2 m = both(k[0]);
+#pragma unroll
+    for (int i = 1; i < 9; ++i) m = __ffma2_rn(m, t, both(k[i]));
+    return __fmul2_rn(__fmul2_rn(m, t), e);
+}
+__device__ __forceinline__ float2 normal_cdf(float2 z, float2 tail) { return make_float2(z.x < 0.0f ? tail.x : 1.0f - tail.x, z.y < 0.0f ? tail.y : 1.0f - tail.y); }
 template <int ACT> __device__ __forceinline__ float2 act_value(float2 z) {
     if constexpr (ACT == VMB_ACT_SILU) return __fmul2_rn(z, sigmoid2(z));
-    if constexpr (ACT == VMB_ACT_GELU)
-        return __fmul2_rn(__fmul2_rn(z, both(0.5f)), make_float2(1.0f + erff(z.x * 0.70710678118654752f), 1.0f + erff(z.y * 0.70710678118654752f)));
+    if constexpr (ACT == VMB_ACT_GELU) {
+        float2 e;
+        return __fmul2_rn(z, normal_cdf(z, normal_tail(z, e)));
+    }
     return z;
 }
 template <int ACT> __device__ __forceinline__ float2 act_slope(float2 z) {
@@ -94,9 +113,11 @@ template <int ACT> __device__ __forceinline__ float2 act_slope(float2 z) {
         const float2 s = sigmoid2(z), r = __ffma2_rn(s, both(-1.0f), both(1.0f));
         return __ffma2_rn(__fmul2_rn(z, s), r, s);
     }
-    if constexpr (ACT == VMB_ACT_GELU)
-        return make_float2(fmaf(z.x * 0.39894228040143268f, expf(-0.5f * z.x * z.x), 0.5f * (1.0f + erff(z.x * 0.70710678118654752f))),
-                           fmaf(z.y * 0.39894228040143268f, expf(-0.5f * z.y * z.y), 0.5f * (1.0f + erff(z.y * 0.70710678118654752f))));
+    if constexpr (ACT == VMB_ACT_GELU) {  // Phi(z) + z e^(-z^2 / 2) / sqrt(2 pi)
+        float2 e;
+        const float2 p = normal_cdf(z, normal_tail(z, e));
+        return __ffma2_rn(__fmul2_rn(z, both(0.39894228040143268f)), e, p);
+    }
     return both(1.0f);
 }
 

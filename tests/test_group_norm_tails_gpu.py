@@ -45,3 +45,9 @@ def run(act, dtype, C, L):
 @pytest.mark.parametrize("C,L", [(512, 20), (514, 20), (1024, 3000)])  # a cluster, single values, two passes over memory
 def test_silu(dtype, C, L):
     run("silu", dtype, C, L)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C,L", [(512, 20), (514, 20), (1024, 3000)])
+def test_gelu(dtype, C, L):
+    run("gelu", dtype, C, L)
