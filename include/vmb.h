@@ -502,7 +502,7 @@ size_t vmb_mean_scan_bwd_workspace_bytes(int B, int K, int D, int N, int H, int 
  *   of q, of k and of v (parts of one projection's output); heads and channels are dense.
  *   offsets: NULL, or int32 [B + 1] on the device: B packed sequences, sequence b is rows
  *   offsets[b] .. offsets[b + 1] - 1 of `total` tokens (the batch dimension of the tensors is
- *   then 1, T a bound of the longest sequence, batch strides unused).  Without offsets total is
+ *   then 1, T a bound of the longest sequence, as loose as INT_MAX, batch strides unused).  Without offsets total is
  *   B * T.  Offsets that decrease, leave [0, total] or give a sequence longer than T are cut to
  *   what is in range and reported as VMB_ERR_BOUNDS by vmb_read_status; rows that no sequence
  *   holds are not written.

@@ -34,7 +34,7 @@ template <int DK> __global__ void __launch_bounds__(kJoinThreads, 1) delta_join_
     const int r = tid & 7, oc = 4 * (tid >> 3), row = (int)(blockIdx.x % strips) * kJoinRows + r;
     const bool own = oc < DK, live = own && row < a.Dv;
     const DeltaSeq seq = delta_seq(a.offsets, (int)(chain / a.Hv), a.T, a.total, c.err);
-    const int nseg = ((seq.len + kChunk - 1) / kChunk + c.seg_chunks - 1) / c.seg_chunks;
+    const int nseg = (chunks_of(seq.len) + c.seg_chunks - 1) / c.seg_chunks;
     const float* init = reverse ? a.dfinal : a.initial;
     float* last = reverse ? a.dinitial : a.final;
     auto sums = [&](int i) { return reinterpret_cast<float4*>(c.sums + ((chain * c.segs + (reverse ? nseg - 1 - i : i)) * a.Dv + row) * DK + oc); };
@@ -277,13 +277,13 @@ bool allow_smem(const void* fn, int bytes) {
 }
 
 long long delta_slots(int B, int T, long long total, bool packed) {
-    return packed ? total / kChunk + B : (long long)B * ((T + kChunk - 1) / kChunk);
+    return packed ? total / kChunk + B : (long long)B * chunks_of(T);
 }
 
 DeltaPlan plan_delta(const DeltaArgs& a, bool grads, int sms) {
     DeltaPlan p{};
     const long long chains = (long long)a.B * a.Hv;
-    p.chunks = (a.T + kChunk - 1) / kChunk;
+    p.chunks = chunks_of(a.T);
     p.wide = a.dtype == VMB_BF16 && a.Dv > 64;
     p.slots = delta_slots(a.B, a.T, a.total, a.offsets != nullptr);
     p.segs = 1;

@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_forward_kernel(DeltaCh
     const bool map = !kOut && (c.maps_only || at.slice >= vslices);  // rows of the map: v = 0, S = identity
     const int slice = map && !c.maps_only ? at.slice - vslices : at.slice;
     const DeltaSeq seq = delta_seq(a.offsets, at.b, a.T, a.total, c.err);
-    const int nc = (seq.len + kChunk - 1) / kChunk;
+    const int nc = chunks_of(seq.len);
     const int c0 = at.seg * c.seg_chunks, c1 = min(nc, c0 + c.seg_chunks);
     if ((!kOut || c.segs > 1) && c0 >= nc) return;
     const long long hrow = (long long)a.Hv * a.Dv;
@@ -501,7 +501,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) delta_reverse_kernel(DeltaCh
     pdl_wait();
     const ChainPlace at = chain_place(c, c.slices);
     const DeltaSeq seq = delta_seq(a.offsets, at.b, a.T, a.total, c.err);
-    const int nc = (seq.len + kChunk - 1) / kChunk;
+    const int nc = chunks_of(seq.len);
     const int c0 = at.seg * c.seg_chunks, c1 = min(nc, c0 + c.seg_chunks);
     if (c.segs > 1 && c0 >= nc) return;
     const long long hrow = (long long)a.Hv * a.Dv;  // do, dX and dv are dense

@@ -29,7 +29,8 @@
 namespace vmb {
 
 constexpr int kChunk = 64;       // tokens per chunk
-
+// chunks of a sequence, whatever its length (tokens + 63 may not fit an int)
+__host__ __device__ __forceinline__ int chunks_of(int tokens) { return tokens / kChunk + (tokens % kChunk != 0); }
 
 // ------------------------------------------------------------------ fragments
 
@@ -567,7 +568,7 @@ struct DeltaSeq {
 // leave [0, total], decrease or exceed the stated longest length are cut to what is in range and
 // reported in the status word.
 __device__ __forceinline__ DeltaSeq delta_seq(const int* offsets, int b, int T, long long total, unsigned* err) {
-    if (!offsets) return {(long long)b * T, T, b * ((T + kChunk - 1) / kChunk)};
+    if (!offsets) return {(long long)b * T, T, b * chunks_of(T)};
     const long long a = offsets[b], e = offsets[b + 1];
     const long long lo = a < 0 ? 0 : (a > total ? total : a), hi = e < lo ? lo : (e > total ? total : e);
     const int len = (int)(hi - lo < T ? hi - lo : T);

@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(GradSmem<T, DK>::threads, GradSmem<T, DK>::sma
     auto block = [&](int i) { return NG == 2 ? i : 2 * i + (qt >> 1); };
     pdl_launch_dependents();
     pdl_wait();
-    const int chunks = (a.T + kChunk - 1) / kChunk, share = a.Hv / a.Hk, heads = SM::totals ? a.Hk : a.Hv;
+    const int chunks = chunks_of(a.T), share = a.Hv / a.Hk, heads = SM::totals ? a.Hk : a.Hv;
     const int ch = blockIdx.x % chunks;
     const long long chain = blockIdx.x / chunks;
     const int head = (int)(chain % heads), b = (int)(chain / heads);
@@ -419,7 +419,7 @@ template <typename T, int DK>
 vmb_status launch_grad_dk(const DeltaGrad& c, cudaStream_t stream) {
     using SM = GradSmem<T, DK>;
     const void* fn = (const void*)delta_grad_kernel<T, DK>;
-    const long long grid = (long long)c.a.B * (SM::totals ? c.a.Hk : c.a.Hv) * ((c.a.T + kChunk - 1) / kChunk);
+    const long long grid = (long long)c.a.B * (SM::totals ? c.a.Hk : c.a.Hv) * chunks_of(c.a.T);
     if (!allow_smem(fn, SM::total)) return VMB_ERR_CUDA;
     DeltaGrad arg = c;
     void* args[] = {&arg};

@@ -30,6 +30,9 @@ bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) %
 size_t esize(vmb_dtype dt) { return dt == VMB_BF16 ? 2 : 4; }
 bool dtype_ok(vmb_dtype dt) { return dt == VMB_F32 || dt == VMB_BF16; }
 
+// The longest sequence: of packed ones T is a bound, and none is longer than all tokens.
+int longest(int T, int64_t total, bool packed) { return packed && total >= 0 && T > total ? (int)total : T; }
+
 // Sizes shared by the delta rule's calls; *empty: no tokens and no states.
 vmb_status delta_sizes(int B, int T, int64_t total, bool packed, int Hk, int Hv, int Dk, int Dv, vmb_dtype dt, bool* empty) {
     if (!dtype_ok(dt) || B < 0 || T < 0 || total < 0 || Hk < 0 || Hv < 0 || Dk < 0 || Dv < 0) return VMB_ERR_INVALID_ARG;
@@ -87,6 +90,7 @@ extern "C" {
 size_t vmb_delta_rule_workspace_bytes(int B, int T, int64_t total, int packed, int Hk, int Hv, int Dk, int Dv, int grads,
                                       vmb_dtype dtype) {
     bool empty = false;
+    T = longest(T, total, packed != 0);
     if (delta_sizes(B, T, total, packed != 0, Hk, Hv, Dk, Dv, dtype, &empty) != VMB_OK) return 0;
     if (empty) return 256;
     DeltaArgs a;
@@ -97,6 +101,7 @@ size_t vmb_delta_rule_workspace_bytes(int B, int T, int64_t total, int packed, i
 
 size_t vmb_delta_rule_saved_bytes(int B, int T, int64_t total, int packed, int Hv, int Dk, int Dv, vmb_dtype dtype) {
     bool empty = false;
+    T = longest(T, total, packed != 0);
     if (delta_sizes(B, T, total, packed != 0, 1, Hv, Dk, Dv, dtype, &empty) != VMB_OK) return 0;
     if (empty) return 256;
     DeltaArgs a;
@@ -110,6 +115,7 @@ vmb_status vmb_delta_rule_fwd(const void* q, const void* k, const void* v, const
                               int T, int64_t total, int Hk, int Hv, int Dk, int Dv, float scale, vmb_dtype dtype, void* workspace,
                               size_t workspace_bytes, cudaStream_t stream) {
     bool empty = false;
+    T = longest(T, total, offsets != nullptr);
     vmb_status s = delta_sizes(B, T, total, offsets != nullptr, Hk, Hv, Dk, Dv, dtype, &empty);
     if (s != VMB_OK || empty) return s;
     const size_t es = esize(dtype);
@@ -138,6 +144,7 @@ vmb_status vmb_delta_rule_bwd(const void* q, const void* k, const void* g, const
                               int Hv, int Dk, int Dv, float scale, vmb_dtype dtype, void* workspace, size_t workspace_bytes,
                               cudaStream_t stream) {
     bool empty = false;
+    T = longest(T, total, offsets != nullptr);
     vmb_status s = delta_sizes(B, T, total, offsets != nullptr, Hk, Hv, Dk, Dv, dtype, &empty);
     if (s != VMB_OK || empty) return s;
     const size_t es = esize(dtype);
