@@ -9,7 +9,8 @@
 //
 // The error of an angle does not grow with the position (the product p f alone is off by 2^-24 p f: 2e-4 at
 // position 4096): up to 1024 radians the product's rounding error, lo = p f - hi, is turned by to first order
-// (lo^2 / 2 < 2^-31); larger angles, which few pairs of few tokens have, are brought into [-pi, pi] in 64 bits.
+// (lo^2 / 2 < 2^-31); larger angles, and positions that a float may not hold (from 2^24 on), which few tokens have, are
+// brought into [-pi, pi] in 64 bits, again with the product's rounding error.
 #include <string.h>
 
 #include "mixer_internal.h"
@@ -28,9 +29,9 @@ template <typename T, int V, bool kLoose> struct alignas(kLoose ? sizeof(T) : si
 __device__ __forceinline__ float2 turn(int p, float f) {
     const float ph = (float)p;
     float hi = ph * f, lo = fmaf(ph, f, -hi);
-    if (!(fabsf(hi) <= 1024.0f)) {
-        const double a = (double)p * (double)f, n = rint(a * 0.15915494309189535);  // turns
-        hi = (float)fma(-n, 2.4492935982947064e-16, fma(-n, 6.283185307179586, a)), lo = 0.0f;  // 2 pi in two parts
+    if (!(fabsf(hi) <= 1024.0f && fabsf(ph) < 16777216.0f)) {
+        const double a = (double)p * (double)f, n = rint(a * 0.15915494309189535), low = fma((double)p, (double)f, -a);  // turns
+        hi = (float)(fma(-n, 2.4492935982947064e-16, fma(-n, 6.283185307179586, a)) + low), lo = 0.0f;  // 2 pi in two parts
     }
     float s, c;
     sincosf(hi, &s, &c);
