@@ -221,7 +221,9 @@ vmb_status vmb_rotary_fwd(const void* q, const void* k, const float* freq, const
     if (strides) {
         for (int i = 0; i < 4; ++i)
             if (strides[i] < 0) return VMB_ERR_INVALID_ARG;
-        const bool dense_q = strides[0] == a.q_b && strides[1] == a.q_t, dense_k = strides[2] == a.k_b && strides[3] == a.k_t;
+        // (the stride of a dimension of one has no meaning)
+        const bool dense_q = (B == 1 || strides[0] == a.q_b) && (T == 1 || strides[1] == a.q_t),
+                   dense_k = (B == 1 || strides[2] == a.k_b) && (T == 1 || strides[3] == a.k_t);
         if ((q && q == q_out && !dense_q) || (k && Hk && k == k_out && !dense_k)) return VMB_ERR_INVALID_ARG;
         a.q_b = strides[0], a.q_t = strides[1], a.k_b = strides[2], a.k_t = strides[3];
     }
