@@ -505,7 +505,7 @@ size_t vmb_mean_scan_bwd_workspace_bytes(int B, int K, int D, int N, int H, int 
  *   then 1, T a bound of the longest sequence, as loose as INT_MAX, batch strides unused).  Without offsets total is
  *   B * T.  Offsets that decrease, leave [0, total] or give a sequence longer than T are cut to
  *   what is in range and reported as VMB_ERR_BOUNDS by vmb_read_status; rows that no sequence
- *   holds are not written.
+ *   holds (the padding of a token buffer) are zero in o and in the gradients.
  *   saved: NULL, or vmb_delta_rule_saved_bytes(...) bytes (16-byte aligned) that receive the
  *   state before each chunk and the residuals v_t - S^T k_t, for vmb_delta_rule_bwd.
  *   Keys of length above one with beta near one let the state grow, as the recurrence does.

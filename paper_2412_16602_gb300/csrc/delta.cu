@@ -98,19 +98,65 @@ template <int DK> __global__ void __launch_bounds__(kJoinThreads, 1) delta_join_
 
 // ------------------------------------------------------------------ shared heads
 
-// dq and dk of a key head: the sum, in order, of those of its value heads.
-template <typename T>
-__global__ void __launch_bounds__(256) delta_share_kernel(const float* part, T* dq, T* dk, long long n, int Hk, int r, int Dk) {
+// dq and dk of a key head in fp32: the sum, in order, of those of its value heads.  The CTAs go by chunks (kShareCtas to
+// one), so that rows which no sequence holds, and whose parts nothing has written, are left alone.
+constexpr int kShareCtas = 16;
+__global__ void __launch_bounds__(256) delta_share_kernel(DeltaGrad c) {
+    const DeltaArgs& a = c.a;
     pdl_launch_dependents();
     pdl_wait();
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
-        const int d = (int)(i % Dk);
-        const long long head = i / Dk;  // token * Hk + key head
-        const float* p = part + head * r * 2 * Dk + d;
+    const int chunks = chunks_of(a.T), ch = blockIdx.x % chunks, r = a.Hv / a.Hk, Dk = a.Dk, row = a.Hk * Dk;
+    const DeltaSeq seq = delta_seq(a.offsets, blockIdx.x / chunks, a.T, a.total, nullptr);
+    constexpr int kRows = kChunk / kShareCtas;
+    const int t0 = blockIdx.y * kRows, n = max(0, min(seq.len - ch * kChunk - t0, kRows)) * row;
+    const long long token = seq.start + (long long)ch * kChunk + t0;
+    const float* part = c.part + token * a.Hv * 2 * Dk;
+    float *dq = (float*)a.dq + token * row, *dk = (float*)a.dk + token * row;
+    for (int i = threadIdx.x; i < n; i += 256) {
+        const float* p = part + (long long)(i / Dk) * r * 2 * Dk + i % Dk;  // i / Dk: (token, key head)
         float q = 0.0f, k = 0.0f;
         for (int j = 0; j < r; ++j) q += p[(long long)j * 2 * Dk], k += p[(long long)j * 2 * Dk + Dk];
-        dq[i] = io<T>::to(q);
-        dk[i] = io<T>::to(k);
+        dq[i] = q;
+        dk[i] = k;
+    }
+}
+
+// ------------------------------------------------------------------ rows that no sequence holds
+
+// Zeros in the rows before the first packed sequence, behind the last one (the padding of a token buffer) and between them
+// (where one is longer than the stated bound).  The rows at the ends are shared by all CTAs; launched before the
+// chains, so that offsets out of order, which make these rows overlap a sequence's, cost no result.
+struct DeltaClear {
+    const int* offsets;
+    int B, T;
+    long long total;
+    char* p[5];
+    long long row[5];  // bytes of a token, a multiple of two
+};
+__device__ __forceinline__ void clear_bytes(char* p, long long n, long long i0, long long step) {
+    const long long odd = (16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15, head = odd < n ? odd : n, words = (n - head) / 16;
+    for (long long i = i0; i < head / 2; i += step) reinterpret_cast<unsigned short*>(p)[i] = 0;
+    for (long long i = i0; i < words; i += step) reinterpret_cast<uint4*>(p + head)[i] = make_uint4(0, 0, 0, 0);
+    p += head + 16 * words;
+    for (long long i = i0; i < (n - head - 16 * words) / 2; i += step) reinterpret_cast<unsigned short*>(p)[i] = 0;
+}
+__global__ void __launch_bounds__(256) delta_clear_kernel(DeltaClear c) {
+    pdl_launch_dependents();
+    pdl_wait();
+    auto clear = [&](long long r0, long long r1, long long i0, long long step) {
+        if (r1 <= r0) return;
+#pragma unroll
+        for (int k = 0; k < 5; ++k)
+            if (c.p[k]) clear_bytes(c.p[k] + r0 * c.row[k], (r1 - r0) * c.row[k], i0, step);
+    };
+    auto seq = [&](int b) { return delta_seq(c.offsets, b, c.T, c.total, nullptr); };
+    const long long thread = (long long)blockIdx.x * 256 + threadIdx.x, threads = (long long)gridDim.x * 256;
+    const DeltaSeq last = seq(c.B - 1);
+    clear(0, seq(0).start, thread, threads);
+    clear(last.start + last.len, c.total, thread, threads);
+    for (int b = blockIdx.x; b < c.B - 1; b += gridDim.x) {
+        const DeltaSeq s = seq(b);
+        clear(s.start + s.len, seq(b + 1).start, threadIdx.x, 256);
     }
 }
 
@@ -239,6 +285,18 @@ vmb_status join(const DeltaChain& c, bool reverse, cudaStream_t stream) {
                ? VMB_OK : VMB_ERR_CUDA;
 }
 
+// Of packed sequences: the rows of the outputs that none of them holds.
+vmb_status clear(const DeltaArgs& a, bool grads, cudaStream_t stream) {
+    if (!a.offsets) return VMB_OK;
+    const long long es = a.dtype == VMB_BF16 ? 2 : 4, keys = es * a.Hk * a.Dk, values = es * a.Hv * a.Dv, heads = es * a.Hv;
+    DeltaClear c = grads ? DeltaClear{a.offsets, a.B, a.T, a.total, {(char*)a.dq, (char*)a.dk, (char*)a.dv, (char*)a.dg, (char*)a.dbeta},
+                                      {keys, keys, values, heads, heads}}
+                         : DeltaClear{a.offsets, a.B, a.T, a.total, {(char*)a.o}, {values}};
+    void* args[] = {&c};
+    return launch_kernel((const void*)delta_clear_kernel, dim3((unsigned)device_sm_count()), dim3(256), 0, args, stream) == cudaSuccess
+               ? VMB_OK : VMB_ERR_CUDA;
+}
+
 DeltaChain chain_of(const DeltaArgs& a, const DeltaPlan& p) {
     DeltaChain c{};
     c.a = a;
@@ -325,9 +383,11 @@ vmb_status launch_delta_fwd(const DeltaArgs& a, cudaStream_t stream) {
     const DeltaPlan p = plan_delta(a, false, device_sm_count());
     if (a.ws_bytes < p.bytes) return VMB_ERR_WORKSPACE;
     DeltaChain c = chain_of(a, p);
+    vmb_status s = clear(a, false, stream);
+    if (s != VMB_OK) return s;
     if (p.segs > 1) {
         c.summary = 1;
-        vmb_status s = chain(c, false, stream);
+        s = chain(c, false, stream);
         if (s == VMB_OK) s = join(c, false, stream);
         if (s != VMB_OK) return s;
         c.summary = 0;
@@ -339,7 +399,8 @@ vmb_status launch_delta_bwd(const DeltaArgs& a, cudaStream_t stream) {
     const DeltaPlan p = plan_delta(a, true, device_sm_count());
     if (a.ws_bytes < p.bytes) return VMB_ERR_WORKSPACE;
     DeltaChain c = chain_of(a, p);
-    vmb_status s;
+    vmb_status s = clear(a, true, stream);
+    if (s != VMB_OK) return s;
     if (p.segs > 1) {
         c.summary = c.maps_only = 1;
         if ((s = chain(c, false, stream)) != VMB_OK) return s;
@@ -356,15 +417,9 @@ vmb_status launch_delta_bwd(const DeltaArgs& a, cudaStream_t stream) {
     g.err = c.err;
     if ((s = a.dtype == VMB_BF16 ? launch_grad_bf16(g, stream) : launch_grad_f32(g, stream)) != VMB_OK) return s;
     if (!grad_leaves_parts(a)) return VMB_OK;
-    long long n = a.total * a.Hk * a.Dk;
-    int Hk = a.Hk, r = a.Hv / a.Hk, Dk = a.Dk;
-    const long long want = (n + 255) / 256, most = (long long)device_sm_count() * 8;
-    const void* part = g.part;
-    void *dq = a.dq, *dk = a.dk;
-    void* args[] = {&part, &dq, &dk, &n, &Hk, &r, &Dk};
-    const void* fn = a.dtype == VMB_BF16 ? (const void*)delta_share_kernel<__nv_bfloat16> : (const void*)delta_share_kernel<float>;
-    return launch_kernel(fn, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, args, stream) == cudaSuccess ? VMB_OK
-                                                                                                              : VMB_ERR_CUDA;
+    void* args[] = {&g};
+    return launch_kernel((const void*)delta_share_kernel, dim3((unsigned)((long long)a.B * chunks_of(a.T)), kShareCtas), dim3(256), 0, args, stream) ==
+                   cudaSuccess ? VMB_OK : VMB_ERR_CUDA;
 }
 
 vmb_status launch_delta_step(const DeltaStep& a, cudaStream_t stream) {

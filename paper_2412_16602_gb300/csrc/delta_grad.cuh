@@ -427,11 +427,8 @@ vmb_status launch_grad_dk(const DeltaGrad& c, cudaStream_t stream) {
 }
 
 // Whether the value heads of a key head leave their dq and dk to be summed by delta_share_kernel.
-inline bool grad_leaves_parts(const DeltaArgs& a) {
-    if (a.Hv == a.Hk) return false;
-    if (a.dtype == VMB_BF16) return a.Dk <= 64 ? !GradSmem<__nv_bfloat16, 64>::totals : !GradSmem<__nv_bfloat16, 128>::totals;
-    return a.Dk <= 64 ? !GradSmem<float, 64>::totals : !GradSmem<float, 128>::totals;
-}
+static_assert(GradSmem<float, 64>::totals && GradSmem<__nv_bfloat16, 64>::totals && GradSmem<__nv_bfloat16, 128>::totals, "sums in the CTA");
+inline bool grad_leaves_parts(const DeltaArgs& a) { return a.Hv != a.Hk && a.dtype == VMB_F32 && a.Dk > 64 && !GradSmem<float, 128>::totals; }
 
 template <typename T>
 vmb_status launch_grad(const DeltaGrad& c, cudaStream_t stream) {

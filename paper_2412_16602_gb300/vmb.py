@@ -846,7 +846,8 @@ def vmb_delta_rule_fwd(q, k, v, g, beta, *, initial_state=None, offsets=None, ma
                        workspace=None, stream=None):
     """Gated delta rule over the tokens of every head: q, k [B, T, Hk, Dk], v [B, T, Hv, Dv] (rows of tokens may be
     strided), g (log decay), beta [B, T, Hv], initial_state [B, Hv, Dk, Dv] float32 or None; packed sequences with
-    `offsets` int32 [sequences + 1] and `max_len` (the batch dimension is then 1, states are per sequence).  `scale`
+    `offsets` int32 [sequences + 1] and `max_len` (the batch dimension is then 1, states are per sequence, and o is zero in
+    rows that no sequence holds, as the gradients are).  `scale`
     defaults to Dk ** -0.5.  Returns (o [B, T, Hv, Dv], final_state or None, saved or None); `saved` is what
     vmb_delta_rule_bwd needs."""
     B, T, Hk, Hv, Dk, Dv, code, strides = _delta_inputs(q, k, v, g, beta)
@@ -862,6 +863,8 @@ def vmb_delta_rule_fwd(q, k, v, g, beta, *, initial_state=None, offsets=None, ma
         _dev(o, "o")
         if o.shape != (B, T, Hv, Dv) or o.dtype != q.dtype:
             raise ValueError("o must be [B, T, Hv, Dv] in the dtype of q")
+    if N == 0:
+        o.zero_()  # (no sequences: nothing is launched)
     if saved is None and want_saved:
         n = lib.vmb_delta_rule_saved_bytes(N, longest, total, offsets is not None, Hv, Dk, Dv, code)
         saved = torch.empty(n, dtype=torch.uint8, device=q.device)
@@ -898,8 +901,8 @@ def vmb_delta_rule_bwd(q, k, v, g, beta, do, saved, *, dfinal_state=None, offset
         raise ValueError("do must be [B, T, Hv, Dv] in the dtype of q")
     _saved_bytes(saved, N, longest, total, offsets, Hv, Dk, Dv, code)
     dev = q.device
-    out = dict(q=torch.empty(q.shape, dtype=q.dtype, device=dev), k=torch.empty(k.shape, dtype=q.dtype, device=dev),
-               v=torch.empty(v.shape, dtype=q.dtype, device=dev), g=torch.empty_like(g), beta=torch.empty_like(beta))
+    new = torch.empty if N else torch.zeros
+    out = {n: new(t.shape, dtype=q.dtype, device=dev) for n, t in (("q", q), ("k", k), ("v", v), ("g", g), ("beta", beta))}
     if want_initial:
         out["initial_state"] = torch.empty(shape, dtype=torch.float32, device=dev)
     if workspace is None:
