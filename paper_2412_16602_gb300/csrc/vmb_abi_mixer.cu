@@ -181,6 +181,7 @@ vmb_status vmb_delta_rule_step(const void* q, const void* k, const void* v, cons
     if (!aligned(q, es) || !aligned(k, es) || !aligned(v, es) || !aligned(g, es) || !aligned(beta, es) || !aligned(o, es) ||
         !aligned(state, 4) || !aligned(slots, 4))
         return VMB_ERR_MISALIGNED;
+    if (o == q || o == k || o == v) return VMB_ERR_INVALID_ARG;
     DeltaArgs d;
     d.B = B, d.T = T, d.Hk = Hk, d.Hv = Hv, d.Dk = Dk, d.Dv = Dv;
     if ((s = delta_strides(d, strides)) != VMB_OK) return s;
