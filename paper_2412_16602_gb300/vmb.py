@@ -822,6 +822,10 @@ def _delta_packed(offsets, max_len, B, T):
     return offsets.numel() - 1, min(int(max_len), T), T
 
 
+def _scale(scale, Dk):
+    return max(Dk, 1) ** -0.5 if scale is None else scale
+
+
 def _state(t, name, shape):
     if t is not None:
         _dev(t, name)
@@ -863,8 +867,8 @@ def vmb_delta_rule_fwd(q, k, v, g, beta, *, initial_state=None, offsets=None, ma
         _dev(o, "o")
         if o.shape != (B, T, Hv, Dv) or o.dtype != q.dtype:
             raise ValueError("o must be [B, T, Hv, Dv] in the dtype of q")
-    if N == 0:
-        o.zero_()  # (no sequences: nothing is launched)
+    if not (N and Dk):
+        o.zero_()  # (no sequences, or keys without channels: nothing is launched)
     if saved is None and want_saved:
         n = lib.vmb_delta_rule_saved_bytes(N, longest, total, offsets is not None, Hv, Dk, Dv, code)
         saved = torch.empty(n, dtype=torch.uint8, device=q.device)
@@ -875,7 +879,7 @@ def vmb_delta_rule_fwd(q, k, v, g, beta, *, initial_state=None, offsets=None, ma
         workspace = _delta_ws.get(_delta_bytes(dev.index, N, longest, total, offsets is not None, Hk, Hv, Dk, Dv, 0, code), dev)
     _check(lib.vmb_delta_rule_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), strides,
                                   _ptr(initial_state), _ptr(offsets), o.data_ptr(), _ptr(final_state), _ptr(saved), N,
-                                  longest, total, Hk, Hv, Dk, Dv, Dk ** -0.5 if scale is None else scale, code,
+                                  longest, total, Hk, Hv, Dk, Dv, _scale(scale, Dk), code,
                                   workspace.data_ptr(), workspace.numel(), _stream_of(q, stream)), "vmb_delta_rule_fwd")
     return o, final_state, saved
 
@@ -901,7 +905,7 @@ def vmb_delta_rule_bwd(q, k, v, g, beta, do, saved, *, dfinal_state=None, offset
         raise ValueError("do must be [B, T, Hv, Dv] in the dtype of q")
     _saved_bytes(saved, N, longest, total, offsets, Hv, Dk, Dv, code)
     dev = q.device
-    new = torch.empty if N else torch.zeros
+    new = torch.empty if N and Hv and Dk and Dv else torch.zeros  # (an empty problem launches nothing)
     out = {n: new(t.shape, dtype=q.dtype, device=dev) for n, t in (("q", q), ("k", k), ("v", v), ("g", g), ("beta", beta))}
     if want_initial:
         out["initial_state"] = torch.empty(shape, dtype=torch.float32, device=dev)
@@ -911,7 +915,7 @@ def vmb_delta_rule_bwd(q, k, v, g, beta, do, saved, *, dfinal_state=None, offset
                                   do.data_ptr(), _ptr(dfinal_state), saved.data_ptr(), out["q"].data_ptr(),
                                   out["k"].data_ptr(), out["v"].data_ptr(), out["g"].data_ptr(), out["beta"].data_ptr(),
                                   _ptr(out.get("initial_state")), N, longest, total, Hk, Hv, Dk, Dv,
-                                  Dk ** -0.5 if scale is None else scale, code, workspace.data_ptr(), workspace.numel(),
+                                  _scale(scale, Dk), code, workspace.data_ptr(), workspace.numel(),
                                   _stream_of(q, stream)), "vmb_delta_rule_bwd")
     return out
 
@@ -936,9 +940,11 @@ def vmb_delta_rule_step(q, k, v, g, beta, state, *, slots=None, scale=None, o=No
         _dev(o, "o")
         if o.shape != (B, T, Hv, Dv) or o.dtype != q.dtype:
             raise ValueError("o must be [B, T, Hv, Dv] in the dtype of q")
+    if not Dk:
+        o.zero_()
     _check(lib.vmb_delta_rule_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), strides,
                                    state.data_ptr(), _ptr(slots), o.data_ptr(), B, T, Hk, Hv, Dk, Dv, pool,
-                                   Dk ** -0.5 if scale is None else scale, code, _stream_of(q, stream)), "vmb_delta_rule_step")
+                                   _scale(scale, Dk), code, _stream_of(q, stream)), "vmb_delta_rule_step")
     return o
 
 
