@@ -160,17 +160,41 @@ def _stream(stream) -> int:
 
 
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
+
+
+@functools.lru_cache(maxsize=None)
+def _several_devices() -> bool:
+    return torch.cuda.device_count() > 1
 
 
 def _on_its_stream(call):
-    """`call` with `stream` as the current stream: what it allocates and fills belongs to the stream that it launches on."""
+    """`call` on the device of its first tensor and with `stream` as the current stream: what it allocates and fills belongs
+    to the stream that it launches on."""
     @functools.wraps(call)
     def wrapped(*args, stream=None, **kwargs):
+        if stream is None and not _several_devices():
+            return call(*args, **kwargs)
+        index = next((t.get_device() for t in (*args, *kwargs.values()) if isinstance(t, torch.Tensor)), -1)
+        if index >= 0 and stream is not None and stream.device_index != index:
+            raise ValueError("the stream belongs to another device than the tensors")
+        if index >= 0 and index != _current_device():
+            with torch.cuda.device(index):
+                return wrapped(*args, stream=stream, **kwargs)
         if stream is None:
             return call(*args, **kwargs)
         with torch.cuda.stream(stream):
             return call(*args, stream=stream, **kwargs)
     return wrapped
+
+
+def _one_device(first, *others):
+    """All of these CUDA tensors (or None) are on one device."""
+    if _several_devices():
+        index = first.get_device()
+        for t in others:
+            if t is not None and t.get_device() != index:
+                raise ValueError("all tensors of a call must be on one device")
 
 
 # ---------------------------------------------------------------- cross-scan / merge
@@ -771,6 +795,11 @@ def delta_workspace(device=None, stream=None) -> torch.Tensor:
     return _delta_ws.get(256, torch.device("cuda" if device is None else device))
 
 
+def _given(workspace, t):
+    _dev(workspace, "workspace")
+    _one_device(t, workspace)
+
+
 def _heads(t: torch.Tensor, name: str):
     """(batch stride, token stride) of [B, T, H, D] whose heads and channels are dense."""
     if not t.is_cuda:
@@ -874,9 +903,12 @@ def vmb_delta_rule_fwd(q, k, v, g, beta, *, initial_state=None, offsets=None, ma
         saved = torch.empty(n, dtype=torch.uint8, device=q.device)
     elif saved is not None:
         _saved_bytes(saved, N, longest, total, offsets, Hv, Dk, Dv, code)
+    _one_device(q, k, v, g, beta, initial_state, offsets, o, final_state, saved)
     if workspace is None:
         dev = q.device
         workspace = _delta_ws.get(_delta_bytes(dev.index, N, longest, total, offsets is not None, Hk, Hv, Dk, Dv, 0, code), dev)
+    else:
+        _given(workspace, q)
     _check(lib.vmb_delta_rule_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), strides,
                                   _ptr(initial_state), _ptr(offsets), o.data_ptr(), _ptr(final_state), _ptr(saved), N,
                                   longest, total, Hk, Hv, Dk, Dv, _scale(scale, Dk), code,
@@ -909,8 +941,11 @@ def vmb_delta_rule_bwd(q, k, v, g, beta, do, saved, *, dfinal_state=None, offset
     out = {n: new(t.shape, dtype=q.dtype, device=dev) for n, t in (("q", q), ("k", k), ("v", v), ("g", g), ("beta", beta))}
     if want_initial:
         out["initial_state"] = torch.empty(shape, dtype=torch.float32, device=dev)
+    _one_device(q, k, v, g, beta, do, saved, dfinal_state, offsets)
     if workspace is None:
         workspace = _delta_ws.get(_delta_bytes(dev.index, N, longest, total, offsets is not None, Hk, Hv, Dk, Dv, 1, code), dev)
+    else:
+        _given(workspace, q)
     _check(lib.vmb_delta_rule_bwd(q.data_ptr(), k.data_ptr(), g.data_ptr(), beta.data_ptr(), strides, _ptr(offsets),
                                   do.data_ptr(), _ptr(dfinal_state), saved.data_ptr(), out["q"].data_ptr(),
                                   out["k"].data_ptr(), out["v"].data_ptr(), out["g"].data_ptr(), out["beta"].data_ptr(),
@@ -940,6 +975,7 @@ def vmb_delta_rule_step(q, k, v, g, beta, state, *, slots=None, scale=None, o=No
         _dev(o, "o")
         if o.shape != (B, T, Hv, Dv) or o.dtype != q.dtype:
             raise ValueError("o must be [B, T, Hv, Dv] in the dtype of q")
+    _one_device(q, k, v, g, beta, state, slots, o)
     if not Dk:
         o.zero_()
     _check(lib.vmb_delta_rule_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), strides,
@@ -1000,6 +1036,7 @@ def vmb_rotary_fwd(q, k, freq, positions=None, *, sections, grid=None, interleav
     q_out = _rotary_out(q, q_out, "q_out", strides is None)
     if k is not None:
         k_out = _rotary_out(k, k_out, "k_out", strides is None)
+    _one_device(q, k, freq, positions, q_out, k_out)
     flags = (VMB_ROTARY_INTERLEAVED if interleaved else 0) | (VMB_ROTARY_INVERSE if inverse else 0)
     _check(lib.vmb_rotary_fwd(q.data_ptr(), _ptr(k), freq.data_ptr(), _ptr(positions), q_out.data_ptr(), _ptr(k_out), B,
                               T, Hq, Hk, D, axes, _ints(tuple(sections)), cells, strides, flags, code,
@@ -1047,6 +1084,9 @@ def vmb_group_norm_fwd(x, weight, bias, groups: int, *, eps: float = 1e-5, act: 
     _state(stats, "stats", (B, groups, 2))
     if workspace is None:
         workspace = _norm_ws.get(_norm_bytes(x.device.index, B, L, C, groups, 0, code), x.device)
+    else:
+        _given(workspace, x)
+    _one_device(x, weight, bias, y, stats)
     _check(lib.vmb_group_norm_fwd(x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(stats), B, L, C, groups, eps,
                                   a, code, workspace.data_ptr(), workspace.numel(), _stream_of(x, stream)), "vmb_group_norm_fwd")
     return y, stats
@@ -1067,6 +1107,9 @@ def vmb_group_norm_bwd(x, weight, bias, stats, dy, groups: int, *, act: str = "n
     out = dict(x=torch.empty_like(x), weight=None if weight is None else new(weight), bias=None if bias is None else new(bias))
     if workspace is None:
         workspace = _norm_ws.get(_norm_bytes(x.device.index, B, L, C, groups, 1, code), x.device)
+    else:
+        _given(workspace, x)
+    _one_device(x, weight, bias, stats, dy)
     _check(lib.vmb_group_norm_bwd(x.data_ptr(), _ptr(weight), _ptr(bias), stats.data_ptr(), dy.data_ptr(),
                                   out["x"].data_ptr(), _ptr(out["weight"]), _ptr(out["bias"]), B, L, C, groups, a, code,
                                   workspace.data_ptr(), workspace.numel(), _stream_of(x, stream)), "vmb_group_norm_bwd")
