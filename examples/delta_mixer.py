@@ -13,6 +13,7 @@ import sys
 
 import torch
 import torch.nn.functional as F
+from torch.autograd.function import once_differentiable
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 import paper_2412_16602_gb300 as vmb  # noqa: E402
@@ -27,6 +28,7 @@ class GroupNormAct(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight, bias, stats = ctx.saved_tensors
         d = vmb.vmb_group_norm_bwd(x, weight, bias, stats, dy.contiguous(), ctx.groups, act=ctx.act)
@@ -40,6 +42,7 @@ class Rotary(torch.autograd.Function):
         return vmb.vmb_rotary_fwd(q, k, freq, **ctx.kw)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq, dk):
         dq, dk = vmb.vmb_rotary_fwd(dq.contiguous(), dk.contiguous(), ctx.freq, inverse=True, **ctx.kw)
         return dq, dk, None, None, None
@@ -53,6 +56,7 @@ class DeltaRule(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do):
         *inputs, saved = ctx.saved_tensors
         d = vmb.vmb_delta_rule_bwd(*inputs, do.contiguous(), saved)
