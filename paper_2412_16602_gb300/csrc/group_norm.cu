@@ -30,6 +30,7 @@ namespace vmb {
 namespace {
 
 constexpr int kNormThreads = 256;
+constexpr int kNormMostChannels = 16384;  // of the C ABI
 constexpr size_t kNormL2 = 40u << 20;  // bytes of x (and dy) per launch pair
 // Counters at a fixed place, so that calls of any sizes find them at zero: one per sample of a launch, and the
 // last for the samples of all launches of a call.
@@ -766,8 +767,8 @@ vmb_status run_norm(const NormArgs& a, bool grads, cudaStream_t stream) {
     const void* one = grads ? (const void*)norm_sums_kernel<T, V, ACT> : (const void*)norm_stats_kernel<T, V>;
     const void* two = grads ? (const void*)norm_dx_kernel<T, V, ACT> : (const void*)norm_apply_kernel<T, V, ACT>;
     const size_t smem = grads ? 0 : (size_t)a.C * 8 + kNormThreads * V * 8;
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(one, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
-        return VMB_ERR_CUDA;
+    // (a kernel's limit is set once, to what the widest map needs: another thread may be between its own and its launch)
+    if (smem > 48 * 1024 && !allow_smem(one, kNormMostChannels * 8 + kNormThreads * V * 8)) return VMB_ERR_CUDA;
     void* args[] = {&c};
     for (int b = 0; b < a.B; b += c.p.group) {
         c.first = b;
