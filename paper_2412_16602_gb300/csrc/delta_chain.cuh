@@ -26,7 +26,6 @@ template <> struct DeltaTerms<float> { static constexpr int mid = 1; };
 __device__ __forceinline__ const FragA<__nv_bfloat16, 1>& lead(const FragA<__nv_bfloat16, 2>& a) {
     return reinterpret_cast<const FragA<__nv_bfloat16, 1>&>(a);
 }
-__device__ __forceinline__ const FragA<__nv_bfloat16, 1>& lead(const FragA<__nv_bfloat16, 1>& a) { return a; }
 __device__ __forceinline__ const FragA<float, 1>& lead(const FragA<float, 1>& a) { return a; }
 
 // Roles: the first NST warps carry the state, 16 rows each, the others load the tiles of the chunks ahead and compute

@@ -244,11 +244,6 @@ template <int COLS, int NT> struct Tile<__nv_bfloat16, COLS, NT> {
     int plane;  // elements between the planes
     __device__ __forceinline__ Tile(void* s, int rows) : p((T*)s), plane(rows * kLd) {}
     __device__ __forceinline__ T* vec_at(int r, int c) const { return p + r * kLd + c; }
-    __device__ __forceinline__ void set(int r, int c, float v) const {
-        const T h = __float2bfloat16_rn(v);
-        p[r * kLd + c] = h;
-        if constexpr (NT > 1) p[plane + r * kLd + c] = __float2bfloat16_rn(v - __bfloat162float(h));
-    }
     __device__ __forceinline__ void set2(int r, int c, float v0, float v1) const {  // c even
         if constexpr (NT > 1) {
             split_bf16(make_float2(v0, v1), *reinterpret_cast<uint32_t*>(p + r * kLd + c),
@@ -259,11 +254,6 @@ template <int COLS, int NT> struct Tile<__nv_bfloat16, COLS, NT> {
     }
     __device__ __forceinline__ void zero(int r, int c) const { p[r * kLd + c] = __float2bfloat16_rn(0.0f); }
     __device__ __forceinline__ void put(int r, int c, T v) const { p[r * kLd + c] = v; }
-    __device__ __forceinline__ float get(int r, int c) const {
-        float v = __bfloat162float(p[r * kLd + c]);
-        if constexpr (NT > 1) v += __bfloat162float(p[plane + r * kLd + c]);
-        return v;
-    }
     __device__ __forceinline__ float2 get2(int r, int c) const { return bf16_pair(*reinterpret_cast<const uint32_t*>(p + r * kLd + c)); }  // c even
     // sum += this(r, c ..) . o(r, c ..) over kVec columns
     __device__ __forceinline__ void dot_vec(const Tile& o, int r, int c, float2& sum) const {
@@ -342,13 +332,11 @@ template <int COLS, int NT> struct Tile<float, COLS, NT> {
     __device__ __forceinline__ Tile(void* s, int) : p((T*)s) {}
     __device__ __forceinline__ static int at(int r, int c) { return r * kLd + (c ^ (((r & 3) ^ ((r >> 2) & 1)) << 3)); }
     __device__ __forceinline__ T* vec_at(int r, int c) const { return p + at(r, c); }
-    __device__ __forceinline__ void set(int r, int c, float v) const { p[at(r, c)] = v; }
     __device__ __forceinline__ void set2(int r, int c, float v0, float v1) const {
         *reinterpret_cast<float2*>(p + at(r, c)) = make_float2(v0, v1);
     }
     __device__ __forceinline__ void zero(int r, int c) const { p[at(r, c)] = 0.0f; }
     __device__ __forceinline__ void put(int r, int c, T v) const { p[at(r, c)] = v; }
-    __device__ __forceinline__ float get(int r, int c) const { return p[at(r, c)]; }
     __device__ __forceinline__ float2 get2(int r, int c) const { return *reinterpret_cast<const float2*>(p + at(r, c)); }
     __device__ __forceinline__ void dot_vec(const Tile& o, int r, int c, float2& sum) const {
         const float4 u = *reinterpret_cast<const float4*>(vec_at(r, c)), v = *reinterpret_cast<const float4*>(o.vec_at(r, c));
