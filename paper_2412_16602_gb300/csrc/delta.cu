@@ -1,5 +1,5 @@
 // delta.cu - the gated delta rule: plans, the kernel that joins the segments of a chain, the sum over
-// shared heads, and the recurrent step.
+// shared heads, the rows that no sequence holds, and the recurrent step.
 #include "delta_grad.cuh"
 #include "delta_internal.h"
 #include "vmb_internal.h"

@@ -10,9 +10,9 @@
 // outputs.  The gradient of the state runs through M's transpose.
 //
 // What bounds a chain is the length of a chunk's dependent products, issued by one or two state warps per scheduler next to
-// the system warps: in bf16 with Dk = 64 about 6400 cycles a chunk, 2240 of them on the tensor pipe, for some 12000
-// instructions of the CTA; in fp32, six tf32 products and the splits in place of two, about 16000.  HBM is far from it
-// (32 images of 3136 tokens, 3 heads of 64 in bf16: 157 us, 990 GB/s).
+// the system warps: in bf16 with Dk = 64 about 6200 cycles a chunk, 2560 of them on the tensor pipe, for 11000
+// instructions of the CTA; with Dk = Dv = 128 15300, 7700 and 24100; in fp32 with Dk = 64, six tf32 products and the splits in
+// place of two, 19900, 8400 and 30700.  HBM is far from it (32 images of 3136 tokens, 3 heads of 64 in bf16: 157 us, 990 GB/s).
 #pragma once
 
 #include "delta_common.cuh"

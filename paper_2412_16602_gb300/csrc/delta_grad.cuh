@@ -18,9 +18,9 @@
 // training pass moves, and their rounding reaches one chunk's gradients, never the state: dg and dbeta, sums of many of their
 // products, are off by 0.0029 of their size (rms) where rounding the results alone gives 0.0017; dq, dk and dv by that alone.
 //
-// Bound by latency within a chunk: at four warps per scheduler an instruction issues in 34 to 41% of the cycles, the tensor
-// pipe works in a quarter of them, DRAM at 9 to 15% (2 x 1568 tokens of 12 heads of 128 x 128 over 6 key heads in bf16: 70 us;
-// 8 x 784 tokens of 6 heads of 64 x 64 in fp32: 106 us, cold and on its own).
+// Bound by latency within a chunk: at four warps per scheduler an instruction issues in 40 to 47% of the cycles, the tensor
+// pipe works in 25 to 31% of them, DRAM at 13 to 19% (8 x 3136 tokens of 12 heads of 128 x 128 over 6 key heads in bf16: 457 us;
+// 32 x 784 tokens of 6 heads of 64 x 64 in fp32: 329 us, cold and on its own).
 #pragma once
 
 #include "delta_common.cuh"

@@ -10,8 +10,9 @@
 // Larger samples take two passes over the same tiles (a run of pixels of one sample, all channels): the first leaves a
 // tile's sums per channel, and the last tile of a sample to finish joins them; the second applies them.  It finds x in
 // the L2 cache, because a launch covers only as many samples as its share of the cache holds.
-// With one to three CTAs on an SM the phases of a cluster (load, sum, exchange, store) overlap only in part: DRAM works at 31 to
-// 43% (8 x 128 x 128 x 192 in bf16: 40 us forward; 32 x 56 x 56 x 192 in fp32, forward and gradients: 108 us).
+// With one to three CTAs on an SM the phases of a cluster (load, sum, exchange, store) overlap only in part: DRAM works at 36 to
+// 38% in fp32, 15 to 22% in bf16, where half the bytes meet the same instructions (8 x 128 x 128 x 192 in bf16: 41 us forward;
+// 32 x 56 x 56 x 192 in fp32, forward and gradients: 108 us).
 //
 // Variances are formed from sums of differences to a value of the tile (two passes: a thread's first pixel; clusters: the
 // mean of eight values of the group) and joined as (mean, M2) pairs

@@ -3,8 +3,8 @@
 // Pair i of a head's first 2P channels is turned by the angle p f_i, p the token's position on the axis
 // that pair i belongs to:  (x, y) -> (x cos - y sin, y cos + x sin).  The gradient is the turn by the
 // opposite angle.  Bound by the bytes of q and k, read and written once: the sines of a token are
-// computed once into shared memory and serve all of its heads.  (32 x 784 tokens of 6 heads of 64 in fp32: 24.2 us, 94% of
-// the copy rate.  4 videos of 12544 tokens, 12 + 6 heads of 96 in bf16 and three axes: 88.5 us, 58%: the 28 warps of an SM
+// computed once into shared memory and serve all of its heads.  (32 x 784 tokens of 6 heads of 64 in fp32: 24.4 us, 93% of
+// the copy rate.  4 videos of 12544 tokens, 12 + 6 heads of 96 in bf16 and three axes: 88.6 us, 58%: the 28 warps of an SM
 // have too few loads in flight, and a token's 36 sines serve half the bytes per value.)
 //
 // The error of an angle does not grow with the position (the product p f alone is off by 2^-24 p f: 2e-4 at
