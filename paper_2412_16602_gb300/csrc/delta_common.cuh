@@ -19,7 +19,9 @@
 // dependent chain of four products per chunk).  What a product rounds:
 //   bf16 storage: q, k, v and do are exact.  Intermediates (states, residuals, E, P, the diagonal
 //     inverses) enter as the sum of two bf16 values (16 bits, error about 2^-18); only S^T q takes the
-//     state's leading term, because nothing but an output that is rounded to bf16 itself sees it.
+//     state's leading term, because nothing but an output that is rounded to bf16 itself sees it: o is off by
+//     1.75e-3 (rms) where its own rounding alone is 1.66e-3.  Both terms take 160 -> 166 us for 32 x 3136 tokens,
+//     207 -> 219 for 24 ragged sequences, 1258 -> 1289 for a training pass of 8 x 3136.
 //   fp32 storage: every operand is the sum of two tf32 values (22 bits), products hi.hi + hi.lo + lo.hi.
 // Accumulators, states, decays and the diagonal inverses are fp32 throughout.
 #pragma once
