@@ -518,8 +518,8 @@ size_t vmb_mean_scan_bwd_workspace_bytes(int B, int K, int D, int N, int H, int 
  *   (states, residuals, the decayed products of keys and queries) as the sum of two bf16 values (16
  *   bits), except that S^T q, which only o sees, takes the state's leading term; with fp32 storage
  *   every operand is the sum of two tf32 values (22 bits; a product is off by 7.2e-7 at most).  Sums,
- *   states and decays are fp32.  What
- *   is kept in `saved`, and what the reverse pass hands on per chunk, has the storage type.
+ *   states and decays are fp32.  What is kept in `saved`, and what the reverse pass hands on per
+ *   chunk, has the storage type.
  *
  * vmb_delta_rule_bwd - the gradients, given dout = dLoss/do [B, T, Hv, Dv] and dfinal_state =
  * dLoss/dS_T (or NULL): dq, dk, dv, dg, dbeta (shapes and type of the inputs, dense) and
