@@ -1,7 +1,8 @@
 /*
  * vmb.h - C ABI of the GB300 (sm_103a) library for the VMamba SS2D selective
  * scan and its channel-mean variant VMeanba (arXiv 2412.16602), and for a
- * channels-last token mixer (gated delta rule, rotary positions, group norm).
+ * channels-last token mixer (gated delta rule, rotary positions, group norm), and for the layer
+ * around a scan over tokens (projections, short causal convolution, selective scan, root-mean-square norm).
  *
  * The SS2D module (App. A, "VMamba" paragraph) is cross-scan -> selective scan
  * per direction -> cross-merge.  The selective scan is the discretised,
@@ -594,6 +595,119 @@ vmb_status vmb_group_norm_bwd(const void* x, const float* weight, const float* b
                               const void* dy, void* dx, float* dweight, float* dbias, int B, int64_t L,
                               int C, int G, vmb_act act, vmb_dtype dtype, void* workspace,
                               size_t workspace_bytes, cudaStream_t stream);
+
+/*
+ * ---------------------------------------------------------------- a layer around a scan over tokens
+ *
+ * The operators of a state space layer over sequences of tokens (App. A's selective scan, Eqs. 3
+ * and 6, without the map's directions): the projections, the short causal convolution, the scan
+ * with its gate, and the norm before them.  Channels last: x [B, T, C].  Activations have the storage
+ * type `dtype`; filters, A, D, biases, norm weights, the states of the scan and the gradients of all these are fp32,
+ * and so is all arithmetic.
+ *   strides: NULL (dense), or host values, two for each tensor: the elements between batch rows and
+ *   between tokens (parts of one projection's output); channels are dense.
+ *   offsets: NULL, or int32 [B + 1] on the device: B packed sequences, sequence b is rows
+ *   offsets[b] .. offsets[b + 1] - 1 of `total` tokens (the batch dimension is then 1; T and batch
+ *   strides are unused).  Without offsets total is B * T.  Offsets that decrease or leave [0, total]
+ *   are cut to what is in range (the scan reports them as VMB_ERR_BOUNDS through vmb_read_status);
+ *   rows that no sequence holds are zero in the outputs and in the gradients.
+ *   slots: NULL (row b uses state b; pool >= B), or int32 [B] on the device: the state of row b; rows
+ *   whose slot is outside [0, pool) have none: their outputs are zero.  Slots in use are distinct.
+ *   Gradients are deterministic: sums in a fixed order.
+ *   Workspaces are 256-byte aligned, the first 256 bytes zero-filled before the first use; calls that
+ *   share one must not overlap in time.
+ *
+ * vmb_causal_conv_fwd - a filter of W taps for each channel along the tokens of a sequence:
+ *     z_t = bias + sum_j weight_j x_(t - W + 1 + j),   y_t = act(z_t)
+ *   with initial_state [B, W - 1, C] (dtype; NULL: zeros) before a sequence's first token.
+ *   weight [C, W] fp32, bias [C] fp32 or NULL, y [B, T, C] dense, final_state [B, W - 1, C] (dtype) or
+ *   NULL: the last W - 1 inputs of each sequence, of the initial state where it is shorter.
+ *   W in 1..4 (VMB_ERR_UNSUPPORTED above); act: VMB_ACT_NONE or VMB_ACT_SILU.
+ * vmb_causal_conv_bwd - given dy (dense) and dfinal_state (or NULL): dx [B, T, C] dense (dtype), dweight,
+ *   dbias (fp32; NULL: not wanted), dinitial_state (dtype; NULL: not wanted).
+ * vmb_causal_conv_step - T tokens (a few) of every row, `state` [pool, W - 1, C] (dtype) updated in place.
+ *
+ * vmb_token_scan_fwd - the selective scan of every channel, from h_0 = initial_state [B, D, N] fp32
+ * (NULL: zeros):
+ *     dt = softplus(delta + delta_bias)  (VMB_FLAG_SOFTPLUS; otherwise delta + delta_bias),
+ *     h_t = exp(dt A) h_(t-1) + dt B_t x_t,   y_t = (C_t . h_t + D x_t) silu(z_t)
+ *   x, delta, z [B, T, D], Bm, Cm [B, T, N] (dtype; z NULL: no gate), A [D, N], Dskip, delta_bias [D] fp32
+ *   (the latter two may be NULL); strides: ten values, of x, delta, Bm, Cm, z; y [B, T, D] dense,
+ *   final_state [B, D, N] fp32 or NULL.  N in 1..16 (VMB_ERR_UNSUPPORTED above).
+ *   saved: NULL, or vmb_token_scan_saved_bytes(...) bytes (16-byte aligned) for the state before every
+ *   64 tokens, which vmb_token_scan_bwd takes.
+ * vmb_token_scan_bwd - given dy (dense) and dfinal_state (or NULL): dx, ddelta, dBm, dCm, dz (shapes of the
+ *   inputs, dense, dtype; dz where z is), dA, dDskip, ddelta_bias, dinitial_state (fp32; the last three may be NULL).
+ * vmb_token_scan_step - T tokens (a few) of every row, `state` [pool, D, N] fp32 updated in place.
+ *
+ * vmb_rms_norm_fwd - rows of C channels:  s = x + residual (rounded to dtype; s = x without one),
+ *     y = s rstd weight,  rstd = 1 / sqrt(mean(s^2) + eps)
+ *   x, residual (or NULL), sum (with a residual) [rows, C] dense (dtype), weight [C] fp32 or NULL (1).
+ *   scale NULL: y [rows, C] (dtype).  scale [rows] fp32: y holds 8-bit e4m3 values whose products with
+ *   their row's scale are the norm's output: scale = max |y| / 448, 2^-100 at least.
+ *   rstd [rows] fp32 or NULL.  C <= 8192 (VMB_ERR_UNSUPPORTED above).
+ * vmb_rms_norm_bwd - given dy, and dsum (or NULL), the gradient that reaches s on its own: dx [rows, C], the
+ *   gradient of x and of the residual alike, and dweight [C] fp32 (or NULL).  x: what was normalised (the forward's sum,
+ *   if it had a residual); rstd: the forward's.
+ *
+ * vmb_linear_fwd - matrix product with the epilogue of a projection:
+ *     z = x weight^T + bias,   y = act(z) + residual
+ *   x [M, K] (x_stride elements between its rows), weight [N, K] dense, bias [N] fp32 or NULL, residual
+ *   [M, N] bf16 or NULL, y [M, N] bf16, pre [M, N] bf16 or NULL: z, for vmb_linear_bwd.
+ *   x_scale, weight_scale: both NULL: x and weight are bf16; x_scale [M] and weight_scale [N] fp32: they are e4m3
+ *   values to be multiplied by the scale of their row (what vmb_rms_norm_fwd writes in 8 bits).
+ *   Products are exact and summed in fp32 by the tensor cores; one rounding, to y.
+ * vmb_linear_bwd - given dy [M, N] bf16: dZ = dy act'(pre) (rounded to bf16; pre may be NULL without an
+ *   activation), dx = dZ weight [M, K], dweight = dZ^T x [N, K] (bf16; either may be NULL), dbias [N] fp32 (or NULL) the
+ *   sums of dZ before its rounding.
+ */
+size_t vmb_causal_conv_workspace_bytes(int B, int T, int64_t total, int packed, int C, int W, vmb_dtype dtype);
+vmb_status vmb_causal_conv_fwd(const void* x, const float* weight, const float* bias, const int64_t* strides,
+                               const void* initial_state, const int32_t* offsets, void* y, void* final_state, int B,
+                               int T, int64_t total, int C, int W, vmb_act act, vmb_dtype dtype, cudaStream_t stream);
+vmb_status vmb_causal_conv_bwd(const void* x, const float* weight, const float* bias, const int64_t* strides,
+                               const void* initial_state, const int32_t* offsets, const void* dy,
+                               const void* dfinal_state, void* dx, float* dweight, float* dbias, void* dinitial_state,
+                               int B, int T, int64_t total, int C, int W, vmb_act act, vmb_dtype dtype,
+                               void* workspace, size_t workspace_bytes, cudaStream_t stream);
+vmb_status vmb_causal_conv_step(const void* x, const float* weight, const float* bias, const int64_t* strides,
+                                void* state, const int32_t* slots, void* y, int B, int T, int C, int W, int pool,
+                                vmb_act act, vmb_dtype dtype, cudaStream_t stream);
+
+size_t vmb_token_scan_workspace_bytes(int B, int T, int64_t total, int packed, int D, int N, int grads, vmb_dtype dtype);
+size_t vmb_token_scan_saved_bytes(int B, int T, int64_t total, int packed, int D, int N);
+vmb_status vmb_token_scan_fwd(const void* x, const void* delta, const float* A, const void* Bm, const void* Cm,
+                              const float* Dskip, const float* delta_bias, const void* z, const int64_t* strides,
+                              const float* initial_state, const int32_t* offsets, void* y, float* final_state,
+                              void* saved, int B, int T, int64_t total, int D, int N, unsigned flags, vmb_dtype dtype,
+                              void* workspace, size_t workspace_bytes, cudaStream_t stream);
+vmb_status vmb_token_scan_bwd(const void* x, const void* delta, const float* A, const void* Bm, const void* Cm,
+                              const float* Dskip, const float* delta_bias, const void* z, const int64_t* strides,
+                              const int32_t* offsets, const void* dy, const float* dfinal_state, const void* saved,
+                              void* dx, void* ddelta, float* dA, void* dBm, void* dCm, float* dDskip,
+                              float* ddelta_bias, void* dz, float* dinitial_state, int B, int T, int64_t total, int D,
+                              int N, unsigned flags, vmb_dtype dtype, void* workspace, size_t workspace_bytes,
+                              cudaStream_t stream);
+vmb_status vmb_token_scan_step(const void* x, const void* delta, const float* A, const void* Bm, const void* Cm,
+                               const float* Dskip, const float* delta_bias, const void* z, const int64_t* strides,
+                               float* state, const int32_t* slots, void* y, int B, int T, int D, int N, int pool,
+                               unsigned flags, vmb_dtype dtype, cudaStream_t stream);
+
+size_t vmb_rms_norm_workspace_bytes(int64_t rows, int C, vmb_dtype dtype);
+vmb_status vmb_rms_norm_fwd(const void* x, const void* residual, const float* weight, void* y, void* sum, float* scale,
+                            float* rstd, int64_t rows, int C, float eps, vmb_dtype dtype, cudaStream_t stream);
+vmb_status vmb_rms_norm_bwd(const void* x, const float* weight, const float* rstd, const void* dy, const void* dsum,
+                            void* dx, float* dweight, int64_t rows, int C, vmb_dtype dtype, void* workspace,
+                            size_t workspace_bytes, cudaStream_t stream);
+
+size_t vmb_linear_workspace_bytes(int64_t M, int K, int N, int grads);
+vmb_status vmb_linear_fwd(const void* x, int64_t x_stride, const void* weight, const float* x_scale,
+                          const float* weight_scale, const float* bias, const void* residual, void* y, void* pre,
+                          int64_t M, int K, int N, vmb_act act, void* workspace, size_t workspace_bytes,
+                          cudaStream_t stream);
+vmb_status vmb_linear_bwd(const void* x, int64_t x_stride, const void* weight, const void* pre, const void* dy, void* dx,
+                          void* dweight, float* dbias, int64_t M, int K, int N, vmb_act act, void* workspace,
+                          size_t workspace_bytes, cudaStream_t stream);
 
 /*
  * vmb_read_status - synchronise `stream`, then return and clear the device

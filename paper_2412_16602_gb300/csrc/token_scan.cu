@@ -1,0 +1,280 @@
+// token_scan.cu - the selective scan over tokens, channels last: forward and the step of serving.
+//
+//   dt = softplus(delta + bias),  h_t = exp(dt A) h_(t-1) + dt x B_t,  y = C_t . h_t + D x,  y silu(z) with a gate.
+//
+// N exponentials, N / 2 packed products for each of four uses, and two more exponentials for the step size and the gate per
+// channel and token bound it: the MUFU and issue slots, not the bytes.  Sequences too few to fill the SMs are cut into segments:
+// a first launch takes each segment from a zero state and leaves its last state and the sum of its step sizes (the product of
+// its decays is the exponential of A times that sum), and each segment of the second launch joins those before it.
+#include "token_scan.cuh"
+
+namespace vmb {
+
+namespace {
+
+constexpr int kTok = 32;  // tokens of a stage
+
+template <typename T, int NP> struct ScanSmem {
+    static constexpr int array = kTok * scan_pitch<T>(), slot = 3 * array, bc = kTok * 2 * NP * 4;
+    static constexpr int bytes = 2 * slot + 2 * bc;
+};
+
+template <typename T, int NP, bool kLocal> __global__ void __launch_bounds__(kScanThreads, 2) token_scan_kernel(ScanKernel k) {
+    constexpr int SPL = NP / 4;
+    using L = ScanSmem<T, NP>;
+    extern __shared__ __align__(16) char smem[];
+    pdl_wait();
+    pdl_launch_dependents();
+    const TokenScanArgs& a = k.a;
+    const int tile = blockIdx.x % k.tiles, tid = threadIdx.x, q = tid & 3, ch = tid >> 2, c0 = tile * kScanCh, d = c0 + ch, n0 = q * SPL;
+    const int cols = min(kScanCh, a.D - c0);
+    const long long slot = blockIdx.x / k.tiles;
+    if (slot >= k.slots) {  // rows before the first and behind the last sequence
+        const long long lo = min(max((long long)a.offsets[0], 0LL), a.total), hi = min(max((long long)a.offsets[a.B], lo), a.total);
+        for (long long r = slot - k.slots; r < a.total - (hi - lo); r += kClearBlocks)
+            for (int c = tid; c < cols; c += kScanThreads) ((T*)a.y)[(r < lo ? r : r + hi - lo) * a.D + c0 + c] = io<T>::to(0.0f);
+        return;
+    }
+    const ScanSegment g = scan_segment(k, slot);
+    if (!g.live || (kLocal && g.s == g.segs - 1)) return;  // (nothing follows the last segment)
+    char* bcs = smem + 2 * L::slot;
+    const bool on = d < a.D, gate = !kLocal && a.z;
+    Pairs<SPL> A2, h;
+    A2.zero(), h.zero();
+    if (on) {
+        A2.load_some(a.A + (long long)d * a.N + n0, n0, a.N);
+#pragma unroll
+        for (int p = 0; p < Pairs<SPL>::P; ++p) A2.v[p] = __fmul2_rn(A2.v[p], twice(kLog2e));
+    }
+    const float bias = on && a.bias ? a.bias[d] : 0.0f, skip = on && a.skip ? a.skip[d] : 0.0f;
+    const T *x = scan_row<T>(a.x, a, g, a.x_b, a.x_t) + c0, *raw = scan_row<T>(a.delta, a, g, a.d_b, a.d_t) + c0;
+    const T* z = gate ? scan_row<T>(a.z, a, g, a.z_b, a.z_t) + c0 : nullptr;
+    const T *Bm = scan_row<T>(a.Bm, a, g, a.B_b, a.B_t), *Cm = scan_row<T>(a.Cm, a, g, a.C_b, a.C_t);
+    const int stages = (g.len + kTok - 1) / kTok;
+    RowsBC<T, NP, kTok> bc;
+    auto fetch = [&](int i) {  // copies of stage i under way, its B and C in registers
+        if (i < stages) {
+            char* s = smem + (i & 1) * L::slot;
+            const int t0 = i * kTok, left = g.len - t0;
+            stage_rows<T>(s, x + t0 * a.x_t, a.x_t, kTok, left, cols, k.vec);
+            stage_rows<T>(s + L::array, raw + t0 * a.d_t, a.d_t, kTok, left, cols, k.vec);
+            if (gate) stage_rows<T>(s + 2 * L::array, z + t0 * a.z_t, a.z_t, kTok, left, cols, k.vec);
+            bc.load(Bm + t0 * a.B_t, a.B_t, a.N, Cm + t0 * a.C_t, a.C_t, kLocal ? 0 : a.N, left);
+        }
+        cp_async_commit();
+    };
+    fetch(0);
+    bc.store((float*)bcs);
+    fetch(1);
+    if (!kLocal && on) {
+        if (a.initial) h.load_some(a.initial + ((long long)g.b * a.D + d) * a.N + n0, n0, a.N);
+        for (int s = 0; s < g.s; ++s) {
+            const long long at = (g.place + s) * a.D + d;
+            Pairs<SPL> l, e;
+            l.load(k.local + at * NP + n0);
+            decays(e, A2, k.decay[at]);
+#pragma unroll
+            for (int p = 0; p < Pairs<SPL>::P; ++p) h.v[p] = __ffma2_rn(e.v[p], h.v[p], l.v[p]);
+        }
+    }
+    cp_async_wait<1>();
+    __syncthreads();
+    float sum = 0.0f;  // of this lane's step sizes
+    for (int i = 0; i < stages; ++i) {
+        char* s = smem + (i & 1) * L::slot;
+        const float* rows = (const float*)(bcs + (i & 1) * L::bc);
+        const int t0 = i * kTok;
+        if (!kLocal && a.saved && on && t0 % kScanChunk == 0)
+            h.store_some(a.saved + ((g.chunk + ((long long)g.s * k.seg + t0) / kScanChunk) * a.D + d) * a.N + n0, n0, a.N);
+#pragma unroll 2
+        for (int t = 0; t < kTok; t += 4) {
+            const float xv = staged<T>(s, t + q, ch);
+            float dt = staged<T>(s + L::array, t + q, ch) + bias;
+            if (a.softplus) dt = softplus(dt);
+            if (t0 + t + q >= g.len) dt = 0.0f;
+            const float dtx = dt * xv;
+            float out[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float dtu = from_lane(dt, u), dxu = from_lane(dtx, u);
+                Pairs<SPL> B, C, e;
+                B.load(rows + (t + u) * 2 * NP + n0);
+                decays(e, A2, dtu);
+                float2 acc = make_float2(0.0f, 0.0f);
+                if (!kLocal) C.load(rows + (t + u) * 2 * NP + NP + n0);
+#pragma unroll
+                for (int p = 0; p < Pairs<SPL>::P; ++p) {
+                    h.v[p] = __ffma2_rn(e.v[p], h.v[p], __fmul2_rn(twice(dxu), B.v[p]));
+                    if (!kLocal) acc = __ffma2_rn(C.v[p], h.v[p], acc);
+                }
+                out[u] = acc.x + acc.y;
+            }
+            if constexpr (kLocal) {
+                sum += dt;
+            } else {
+                float y = fmaf(skip, xv, quad_sums(out[0], out[1], out[2], out[3]));
+                if (gate) y *= activate<VMB_ACT_SILU>(staged<T>(s + 2 * L::array, t + q, ch));
+                restage<T>(s, t + q, ch, y);
+            }
+        }
+        if (i + 1 < stages) bc.store((float*)(bcs + ((i + 1) & 1) * L::bc));
+        cp_async_wait<0>();
+        __syncthreads();
+        if (!kLocal) unstage_rows<T>((T*)a.y + (g.first + t0) * a.D + c0, s, a.D, kTok, g.len - t0, cols, k.vec);
+        fetch(i + 2);
+    }
+    if constexpr (kLocal) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        if (!on) return;
+        const long long at = slot * a.D + d;
+        h.store(k.local + at * NP + n0);
+        if (q == 0) k.decay[at] = sum;
+    } else if (on && a.final && g.s == g.segs - 1) {
+        h.store_some(a.final + ((long long)g.b * a.D + d) * a.N + n0, n0, a.N);
+    }
+}
+
+// A few tokens of every row from the state in its slot, updated in place; four lanes a channel.  Bound by the states' bytes.
+template <typename T, int NP> __global__ void __launch_bounds__(128) token_scan_step_kernel(TokenScanArgs a, int tiles) {
+    constexpr int SPL = NP / 4;
+    pdl_wait();
+    pdl_launch_dependents();
+    const int q = threadIdx.x & 3, d = (int)(blockIdx.x % tiles) * 32 + (threadIdx.x >> 2), n0 = q * SPL;
+    const long long b = blockIdx.x / tiles;
+    const bool on = d < a.D;
+    const long long slot = a.slots ? a.slots[b] : b;
+    T* y = (T*)a.y + b * a.T * a.D + d;
+    if (slot < 0 || slot >= a.pool) {
+        if (on && q == 0)
+            for (int t = 0; t < a.T; ++t) y[(long long)t * a.D] = io<T>::to(0.0f);
+        return;
+    }
+    const int dd = on ? d : 0;  // (lanes behind the last channel keep their warp's shuffles whole)
+    float* state = a.state + (slot * a.D + dd) * a.N + n0;
+    const bool whole = a.N == NP && (reinterpret_cast<uintptr_t>(a.state) & 15) == 0 && (reinterpret_cast<uintptr_t>(a.A) & 15) == 0;
+    Pairs<SPL> A2, h;
+    if (whole) h.load(state), A2.load(a.A + (long long)dd * a.N + n0);
+    else h.load_some(state, n0, a.N), A2.load_some(a.A + (long long)dd * a.N + n0, n0, a.N);
+#pragma unroll
+    for (int p = 0; p < Pairs<SPL>::P; ++p) A2.v[p] = __fmul2_rn(A2.v[p], twice(kLog2e));
+    const float bias = a.bias ? a.bias[dd] : 0.0f, skip = a.skip ? a.skip[dd] : 0.0f;
+    for (int t = 0; t < a.T; ++t) {
+        const float xv = io<T>::ld((const T*)a.x + b * a.x_b + t * a.x_t + dd);
+        float dt = io<T>::ld((const T*)a.delta + b * a.d_b + t * a.d_t + dd) + bias;
+        const T *Bm = (const T*)a.Bm + b * a.B_b + t * a.B_t, *Cm = (const T*)a.Cm + b * a.C_b + t * a.C_t;
+        const float zv = a.z ? io<T>::ld((const T*)a.z + b * a.z_b + t * a.z_t + dd) : 0.0f;
+        Pairs<SPL> B, C, e;
+#pragma unroll
+        for (int p = 0; p < Pairs<SPL>::P; ++p) {
+            const int n = n0 + 2 * p;
+            const bool two = SPL > 1 && n + 1 < a.N;
+            B.v[p] = make_float2(n < a.N ? io<T>::ld(Bm + n) : 0.0f, two ? io<T>::ld(Bm + n + 1) : 0.0f);
+            C.v[p] = make_float2(n < a.N ? io<T>::ld(Cm + n) : 0.0f, two ? io<T>::ld(Cm + n + 1) : 0.0f);
+        }
+        if (a.softplus) dt = softplus(dt);
+        const float dtx = dt * xv;
+        decays(e, A2, dt);
+        float2 acc = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int p = 0; p < Pairs<SPL>::P; ++p) {
+            h.v[p] = __ffma2_rn(e.v[p], h.v[p], __fmul2_rn(twice(dtx), B.v[p]));
+            acc = __ffma2_rn(C.v[p], h.v[p], acc);
+        }
+        float out = acc.x + acc.y;
+        out += __shfl_xor_sync(0xffffffffu, out, 1);
+        out += __shfl_xor_sync(0xffffffffu, out, 2);
+        out = fmaf(skip, xv, out);
+        if (a.z) out *= activate<VMB_ACT_SILU>(zv);
+        if (on && q == 0) y[(long long)t * a.D] = io<T>::to(out);
+    }
+    if (!on) return;
+    if (whole) h.store(state);
+    else h.store_some(state, n0, a.N);
+}
+
+bool vec16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+template <typename T, int NP> vmb_status run_scan(const ScanKernel& k0, unsigned grid, bool cut, cudaStream_t stream) {
+    ScanKernel k = k0;
+    constexpr int bytes = ScanSmem<T, NP>::bytes;
+    const void *local = (const void*)token_scan_kernel<T, NP, true>, *full = (const void*)token_scan_kernel<T, NP, false>;
+    if (bytes > 48 * 1024)
+        for (const void* fn : {local, full})
+            if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return VMB_ERR_CUDA;
+    void* args[] = {&k};
+    if (cut && launch_kernel(local, dim3((unsigned)((long long)k.slots * k.tiles)), dim3(kScanThreads), bytes, args, stream) != cudaSuccess)
+        return VMB_ERR_CUDA;
+    return launch_kernel(full, dim3(grid), dim3(kScanThreads), bytes, args, stream) == cudaSuccess ? VMB_OK : VMB_ERR_CUDA;
+}
+
+// Tokens of a forward segment: the whole sequence where the sequences fill the SMs, else such that there are about four CTAs on
+// each, at least two chunks long and at most 64 to a sequence (each joins those before it).
+int forward_segment(int B, int T, long long total, int D) {
+    const long long tiles = (D + kScanCh - 1) / kScanCh, fill = 2LL * device_sm_count();
+    const int whole = (T + kScanChunk - 1) / kScanChunk * kScanChunk;
+    if (B * tiles >= fill || T <= 4 * kScanChunk) return whole < kScanChunk ? kScanChunk : whole;
+    long long segs = (2 * fill + tiles - 1) / tiles;  // wanted over all sequences
+    long long seg = (total + segs - 1) / segs;
+    if (seg * 64 < T) seg = (T + 63) / 64;
+    seg = (seg + kScanChunk - 1) / kScanChunk * kScanChunk;
+    if (seg < 2 * kScanChunk) seg = 2 * kScanChunk;
+    return (int)(seg < whole ? seg : whole);
+}
+
+}  // namespace
+
+void token_scan_plan(ScanKernel& k, int seg) {
+    const TokenScanArgs& a = k.a;
+    k.seg = seg;
+    k.segs_per = (a.T + seg - 1) / seg;
+    if (k.segs_per < 1) k.segs_per = 1;
+    k.slots = (int)(a.offsets ? scan_slots(a.B, a.T, a.total, true, seg) : (long long)a.B * k.segs_per);
+    k.tiles = (a.D + kScanCh - 1) / kScanCh;
+    const int V = a.dtype == VMB_BF16 ? 8 : 4;
+    k.vec = a.D % V == 0 && a.x_t % V == 0 && a.d_t % V == 0 && (!a.z || a.z_t % V == 0) && vec16(a.x) && vec16(a.delta) && vec16(a.z) &&
+            vec16(a.y) && vec16(a.dy) && vec16(a.dx) && vec16(a.ddelta) && vec16(a.dz);
+    if (!a.offsets && a.B > 1) k.vec = k.vec && a.x_b % V == 0 && a.d_b % V == 0 && (!a.z || a.z_b % V == 0);
+}
+
+size_t token_scan_forward_bytes(int B, int T, long long total, bool packed, int D, int N) {
+    const int seg = forward_segment(B, T, total, D);
+    const long long slots = scan_slots(B, T, total, packed, seg);
+    return 256 + align_up((size_t)slots * D * padded_states(N) * 4, 256) + align_up((size_t)slots * D * 4, 256);
+}
+
+vmb_status launch_token_scan_fwd(const TokenScanArgs& a, cudaStream_t stream) {
+    ScanKernel k{a};
+    token_scan_plan(k, forward_segment(a.B, a.T, a.total, a.D));
+    if (a.ws_bytes < token_scan_forward_bytes(a.B, a.T, a.total, a.offsets != nullptr, a.D, a.N)) return VMB_ERR_WORKSPACE;
+    k.local = (float*)((char*)a.ws + 256);
+    k.decay = (float*)((char*)k.local + align_up((size_t)k.slots * a.D * padded_states(a.N) * 4, 256));
+    const bool cut = k.seg < a.T;
+    const unsigned grid = (unsigned)(((long long)k.slots + (a.offsets ? kClearBlocks : 0)) * k.tiles);
+    if (grid == 0) return VMB_OK;
+    const int np = padded_states(a.N);
+    if (a.dtype == VMB_BF16)
+        return np == 16  ? run_scan<__nv_bfloat16, 16>(k, grid, cut, stream)
+               : np == 8 ? run_scan<__nv_bfloat16, 8>(k, grid, cut, stream)
+                         : run_scan<__nv_bfloat16, 4>(k, grid, cut, stream);
+    return np == 16 ? run_scan<float, 16>(k, grid, cut, stream) : np == 8 ? run_scan<float, 8>(k, grid, cut, stream) : run_scan<float, 4>(k, grid, cut, stream);
+}
+
+vmb_status launch_token_scan_step(const TokenScanArgs& a, cudaStream_t stream) {
+    TokenScanArgs g = a;
+    int tiles = (a.D + 31) / 32;
+    void* args[] = {&g, &tiles};
+    const int np = padded_states(a.N);
+    const void* fn;
+    if (a.dtype == VMB_BF16)
+        fn = np == 16  ? (const void*)token_scan_step_kernel<__nv_bfloat16, 16>
+             : np == 8 ? (const void*)token_scan_step_kernel<__nv_bfloat16, 8>
+                       : (const void*)token_scan_step_kernel<__nv_bfloat16, 4>;
+    else
+        fn = np == 16  ? (const void*)token_scan_step_kernel<float, 16>
+             : np == 8 ? (const void*)token_scan_step_kernel<float, 8>
+                       : (const void*)token_scan_step_kernel<float, 4>;
+    return launch_kernel(fn, dim3((unsigned)((long long)a.B * tiles)), dim3(128), 0, args, stream) == cudaSuccess ? VMB_OK : VMB_ERR_CUDA;
+}
+
+}  // namespace vmb

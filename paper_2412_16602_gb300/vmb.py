@@ -48,6 +48,10 @@ EXPORTS = ["vmb_cross_scan", "vmb_cross_merge", "vmb_scan_workspace_bytes", "vmb
            "vmb_delta_rule_fwd", "vmb_delta_rule_bwd", "vmb_delta_rule_step", "vmb_delta_rule_workspace_bytes",
            "vmb_delta_rule_saved_bytes", "vmb_rotary_fwd", "vmb_group_norm_fwd", "vmb_group_norm_bwd",
            "vmb_group_norm_workspace_bytes",
+           "vmb_causal_conv_fwd", "vmb_causal_conv_bwd", "vmb_causal_conv_step", "vmb_causal_conv_workspace_bytes",
+           "vmb_token_scan_fwd", "vmb_token_scan_bwd", "vmb_token_scan_step", "vmb_token_scan_workspace_bytes",
+           "vmb_token_scan_saved_bytes", "vmb_rms_norm_fwd", "vmb_rms_norm_bwd", "vmb_rms_norm_workspace_bytes",
+           "vmb_linear_fwd", "vmb_linear_bwd", "vmb_linear_workspace_bytes",
            "vmb_read_status", "vmb_status_string", "vmb_version"]
 
 
@@ -98,6 +102,24 @@ def _load() -> ctypes.CDLL:
     lib.vmb_group_norm_bwd.argtypes = [vp] * 8 + [i, i64, i, i, i, i, vp, sz, vp]
     lib.vmb_group_norm_workspace_bytes.argtypes = [i, i64, i, i, i, i]
     lib.vmb_group_norm_workspace_bytes.restype = sz
+    lib.vmb_causal_conv_fwd.argtypes = [vp] * 8 + [i, i, i64, i, i, i, i, vp]
+    lib.vmb_causal_conv_bwd.argtypes = [vp] * 12 + [i, i, i64, i, i, i, i, vp, sz, vp]
+    lib.vmb_causal_conv_step.argtypes = [vp] * 7 + [i] * 7 + [vp]
+    lib.vmb_causal_conv_workspace_bytes.argtypes = [i, i, i64, i, i, i, i]
+    lib.vmb_token_scan_fwd.argtypes = [vp] * 14 + [i, i, i64, i, i, u, i, vp, sz, vp]
+    lib.vmb_token_scan_bwd.argtypes = [vp] * 22 + [i, i, i64, i, i, u, i, vp, sz, vp]
+    lib.vmb_token_scan_step.argtypes = [vp] * 12 + [i] * 5 + [u, i, vp]
+    lib.vmb_token_scan_workspace_bytes.argtypes = [i, i, i64, i, i, i, i, i]
+    lib.vmb_token_scan_saved_bytes.argtypes = [i, i, i64, i, i, i]
+    lib.vmb_rms_norm_fwd.argtypes = [vp] * 7 + [i64, i, f, i, vp]
+    lib.vmb_rms_norm_bwd.argtypes = [vp] * 7 + [i64, i, i, vp, sz, vp]
+    lib.vmb_rms_norm_workspace_bytes.argtypes = [i64, i, i]
+    lib.vmb_linear_fwd.argtypes = [vp, i64] + [vp] * 7 + [i64, i, i, i, vp, sz, vp]
+    lib.vmb_linear_bwd.argtypes = [vp, i64] + [vp] * 6 + [i64, i, i, i, vp, sz, vp]
+    lib.vmb_linear_workspace_bytes.argtypes = [i64, i, i, i]
+    for name in ["vmb_causal_conv_workspace_bytes", "vmb_token_scan_workspace_bytes", "vmb_token_scan_saved_bytes",
+                 "vmb_rms_norm_workspace_bytes", "vmb_linear_workspace_bytes"]:
+        getattr(lib, name).restype = sz
     lib.vmb_read_status.argtypes = [vp, vp]
     lib.vmb_status_string.argtypes = [i]
     lib.vmb_status_string.restype = ctypes.c_char_p
@@ -109,6 +131,9 @@ def _load() -> ctypes.CDLL:
                  "vmb_selection_lowrank_fwd", "vmb_selective_scan_lowrank_fwd", "vmb_mean_scan_lowrank_fwd",
                  "vmb_delta_rule_fwd", "vmb_delta_rule_bwd", "vmb_delta_rule_step", "vmb_rotary_fwd",
                  "vmb_group_norm_fwd", "vmb_group_norm_bwd",
+                 "vmb_causal_conv_fwd", "vmb_causal_conv_bwd", "vmb_causal_conv_step", "vmb_token_scan_fwd",
+                 "vmb_token_scan_bwd", "vmb_token_scan_step", "vmb_rms_norm_fwd", "vmb_rms_norm_bwd",
+                 "vmb_linear_fwd", "vmb_linear_bwd",
                  "vmb_read_status", "vmb_version"]:
         getattr(lib, name).restype = i
     return lib
@@ -771,6 +796,7 @@ _ACTS = {"none": VMB_ACT_NONE, "silu": VMB_ACT_SILU, "gelu": VMB_ACT_GELU}
 # workspaces of their own: the scans' must keep what the scans left in theirs
 _delta_ws = Workspace()
 _norm_ws = Workspace()
+_layer_ws = Workspace()
 
 
 # (a step of one token takes 2.5 us on the device: the marshalling below keeps to what it needs)
@@ -1113,6 +1139,437 @@ def vmb_group_norm_bwd(x, weight, bias, stats, dy, groups: int, *, act: str = "n
     _check(lib.vmb_group_norm_bwd(x.data_ptr(), _ptr(weight), _ptr(bias), stats.data_ptr(), dy.data_ptr(),
                                   out["x"].data_ptr(), _ptr(out["weight"]), _ptr(out["bias"]), B, L, C, groups, a, code,
                                   workspace.data_ptr(), workspace.numel(), _stream_of(x, stream)), "vmb_group_norm_bwd")
+    return out
+
+
+# ---------------------------------------------------------------- a layer around a scan over tokens
+
+
+def _rows(t, name: str, B: int, T: int, C: int, dtype):
+    """(batch stride, token stride) of [B, T, C] of the given type whose channels are dense."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.shape != (B, T, C) or t.dtype != dtype:
+        raise ValueError(f"{name} must be [{B}, {T}, {C}] in the dtype of x")
+    sb, st, sc = t.stride()
+    if sc != 1 and C > 1:
+        raise ValueError(f"{name}: the channels of a token must be dense")
+    return (sb if B > 1 else 0), (st if T > 1 else C)
+
+
+def _float(t, name: str, shape):
+    if t is not None:
+        _dev(t, name)
+        if t.shape != shape or t.dtype != torch.float32:
+            raise ValueError(f"{name} must be float32 {list(shape)}")
+
+
+def _like(t, name: str, shape, dtype):
+    """A given dense tensor (or None) of this shape and type."""
+    if t is not None:
+        _dev(t, name)
+        if t.shape != shape or t.dtype != dtype:
+            raise ValueError(f"{name} must be {list(shape)} in the dtype of x")
+
+
+def _sequences(offsets, B, T):
+    """(sequences, their length, tokens) of dense [B, T] or packed [1, tokens] inputs."""
+    if offsets is None:
+        return B, T, B * T
+    _dev(offsets, "offsets")
+    if B != 1 or offsets.dim() != 1 or offsets.numel() < 1 or offsets.dtype != torch.int32:
+        raise ValueError("packed sequences: a batch dimension of 1 and int32 offsets [sequences + 1] expected")
+    return offsets.numel() - 1, T, T
+
+
+def _pool(state, slots, B):
+    if slots is None:
+        if state.shape[0] < B:
+            raise ValueError("state: fewer rows than the batch, and no slots")
+        return
+    _dev(slots, "slots")
+    if slots.shape != (B,) or slots.dtype != torch.int32:
+        raise ValueError("slots must be int32 [B]")
+
+
+@functools.lru_cache(maxsize=4096)
+def _layer_bytes(device, name, *sizes) -> int:
+    return getattr(lib, name)(*sizes)
+
+
+def _layer_workspace(workspace, t, name, *sizes):
+    if workspace is None:
+        return _layer_ws.get(_layer_bytes(t.device.index, name, *sizes), t.device)
+    _given(workspace, t)
+    return workspace
+
+
+@_on_its_stream
+def layer_workspace(device=None, stream=None) -> torch.Tensor:
+    """The default workspace of the calling thread's convolutions, scans over tokens, norms and products on a stream, the
+    current one if none is given (for vmb_read_status)."""
+    return _layer_ws.get(256, torch.device("cuda" if device is None else device))
+
+
+def vmb_causal_conv_workspace_bytes(B: int, T: int, total: int, packed: bool, C: int, W: int,
+                                    dtype: torch.dtype = torch.float32) -> int:
+    return int(lib.vmb_causal_conv_workspace_bytes(B, T, total, int(packed), C, W, _dtype_code(dtype)))
+
+
+def _conv_inputs(x, weight, bias, act):
+    code = _dtype_code(x.dtype)
+    if x.dim() != 3 or weight.dim() != 2:
+        raise ValueError("x [B, T, C] and weight [C, W] expected")
+    B, T, C = x.shape
+    W = weight.shape[1]
+    strides = _rows(x, "x", B, T, C, x.dtype)
+    _float(weight, "weight", (C, W))
+    _float(bias, "bias", (C,))
+    if act not in ("none", "silu"):
+        raise ValueError("act must be 'none' or 'silu'")
+    return B, T, C, W, code, _ACTS[act], (None if x.is_contiguous() else (ctypes.c_int64 * 2)(*strides))
+
+
+@_on_its_stream
+def vmb_causal_conv_fwd(x, weight, bias=None, *, act: str = "silu", initial_state=None, offsets=None, want_state: bool = False,
+                        y=None, final_state=None, stream=None):
+    """Short causal convolution along the tokens, one filter per channel, with an activation ("silu" or "none"): x
+    [B, T, C] (rows of tokens may be strided), weight float32 [C, W], bias float32 [C] or None, initial_state
+    [B, W - 1, C] or None (zeros); packed sequences with `offsets` int32 [sequences + 1] (the batch dimension is then 1,
+    states are per sequence, rows that no sequence holds are zero).  Returns (y [B, T, C], final_state or None)."""
+    B, T, C, W, code, a, strides = _conv_inputs(x, weight, bias, act)
+    n, T1, total = _sequences(offsets, B, T)
+    _like(initial_state, "initial_state", (n, W - 1, C), x.dtype)
+    if final_state is None and want_state:
+        final_state = x.new_empty((n, W - 1, C))
+    _like(final_state, "final_state", (n, W - 1, C), x.dtype)
+    if y is None:
+        y = x.new_empty((B, T, C))
+    _like(y, "y", (B, T, C), x.dtype)
+    _one_device(x, weight, bias, initial_state, offsets, y, final_state)
+    _check(lib.vmb_causal_conv_fwd(x.data_ptr(), weight.data_ptr(), _ptr(bias), strides, _ptr(initial_state), _ptr(offsets),
+                                   y.data_ptr(), _ptr(final_state), n, T1, total, C, W, a, code, _stream_of(x, stream)),
+           "vmb_causal_conv_fwd")
+    return y, final_state
+
+
+@_on_its_stream
+def vmb_causal_conv_bwd(x, weight, bias, dy, *, act: str = "silu", initial_state=None, dfinal_state=None, offsets=None,
+                        want_initial: bool = False, workspace=None, stream=None) -> dict:
+    """Gradients of vmb_causal_conv_fwd given dy [B, T, C] and, optionally, dfinal_state: dict(x, weight, bias (None without
+    one)[, initial_state])."""
+    B, T, C, W, code, a, strides = _conv_inputs(x, weight, bias, act)
+    n, T1, total = _sequences(offsets, B, T)
+    _like(initial_state, "initial_state", (n, W - 1, C), x.dtype)
+    _like(dfinal_state, "dfinal_state", (n, W - 1, C), x.dtype)
+    if dy is None:
+        raise ValueError("dy is needed")
+    _like(dy, "dy", (B, T, C), x.dtype)
+    new = torch.empty_like if total or n else torch.zeros_like  # (an empty problem launches nothing)
+    out = dict(x=x.new_empty((B, T, C)), weight=new(weight), bias=None if bias is None else new(bias))
+    if want_initial:
+        out["initial_state"] = x.new_empty((n, W - 1, C))
+    _one_device(x, weight, bias, dy, initial_state, dfinal_state, offsets)
+    ws = _layer_workspace(workspace, x, "vmb_causal_conv_workspace_bytes", n, T1, total, offsets is not None, C, W, code)
+    _check(lib.vmb_causal_conv_bwd(x.data_ptr(), weight.data_ptr(), _ptr(bias), strides, _ptr(initial_state), _ptr(offsets),
+                                   dy.data_ptr(), _ptr(dfinal_state), out["x"].data_ptr(), out["weight"].data_ptr(),
+                                   _ptr(out["bias"]), _ptr(out.get("initial_state")), n, T1, total, C, W, a, code,
+                                   ws.data_ptr(), ws.numel(), _stream_of(x, stream)), "vmb_causal_conv_bwd")
+    return out
+
+
+@_on_its_stream
+def vmb_causal_conv_step(x, weight, bias, state, *, act: str = "silu", slots=None, y=None, stream=None) -> torch.Tensor:
+    """T tokens (one, or a few) of every row from the inputs kept in its state, which move on in place: x [B, T, C], state
+    [pool, W - 1, C]; slots int32 [B] (row b uses state slots[b]; a negative slot is padding, its y is zero) or None (row
+    b uses state b).  Returns y [B, T, C]."""
+    B, T, C, W, code, a, strides = _conv_inputs(x, weight, bias, act)
+    if state.dim() != 3:
+        raise ValueError("state must be [pool, W - 1, C]")
+    _like(state, "state", (state.shape[0], W - 1, C), x.dtype)
+    _pool(state, slots, B)
+    if y is None:
+        y = x.new_empty((B, T, C))
+    _like(y, "y", (B, T, C), x.dtype)
+    _one_device(x, weight, bias, state, slots, y)
+    _check(lib.vmb_causal_conv_step(x.data_ptr(), weight.data_ptr(), _ptr(bias), strides, state.data_ptr(), _ptr(slots),
+                                    y.data_ptr(), B, T, C, W, state.shape[0], a, code, _stream_of(x, stream)),
+           "vmb_causal_conv_step")
+    return y
+
+
+def vmb_token_scan_workspace_bytes(B: int, T: int, total: int, packed: bool, D: int, N: int, grads: bool = False,
+                                   dtype: torch.dtype = torch.float32) -> int:
+    return int(lib.vmb_token_scan_workspace_bytes(B, T, total, int(packed), D, N, int(grads), _dtype_code(dtype)))
+
+
+def vmb_token_scan_saved_bytes(B: int, T: int, total: int, packed: bool, D: int, N: int) -> int:
+    return int(lib.vmb_token_scan_saved_bytes(B, T, total, int(packed), D, N))
+
+
+def _token_scan_inputs(x, delta, A, Bm, Cm, Dskip, delta_bias, z):
+    code = _dtype_code(x.dtype)
+    if x.dim() != 3 or A.dim() != 2:
+        raise ValueError("x [B, T, D] and A [D, N] expected")
+    B, T, D = x.shape
+    N = A.shape[1]
+    strides = [*_rows(x, "x", B, T, D, x.dtype), *_rows(delta, "delta", B, T, D, x.dtype),
+               *_rows(Bm, "Bm", B, T, N, x.dtype), *_rows(Cm, "Cm", B, T, N, x.dtype)]
+    strides += [0, 0] if z is None else _rows(z, "z", B, T, D, x.dtype)
+    _float(A, "A", (D, N))
+    _float(Dskip, "Dskip", (D,))
+    _float(delta_bias, "delta_bias", (D,))
+    return B, T, D, N, code, (ctypes.c_int64 * 10)(*strides)
+
+
+def _token_scan_saved(saved, n, T, total, packed, D, N):
+    need = lib.vmb_token_scan_saved_bytes(n, T, total, packed, D, N)
+    if saved is True:
+        return need
+    _dev(saved, "saved")
+    if saved.dtype != torch.uint8 or saved.numel() < need:
+        raise ValueError(f"saved must be uint8 with at least {need} bytes")
+
+
+@_on_its_stream
+def vmb_token_scan_fwd(x, delta, A, Bm, Cm, Dskip=None, delta_bias=None, z=None, *, softplus: bool = True, initial_state=None,
+                       offsets=None, want_state: bool = False, want_saved: bool = False, y=None, final_state=None, saved=None,
+                       workspace=None, stream=None):
+    """Selective scan over tokens with its gate: x, delta, z (or None) [B, T, D], Bm, Cm [B, T, N] (rows of tokens may be
+    strided), A float32 [D, N], Dskip, delta_bias float32 [D] or None, initial_state float32 [B, D, N] or None (zeros);
+    packed sequences with `offsets` int32 [sequences + 1] (the batch dimension is then 1, states are per sequence, rows that
+    no sequence holds are zero).  Returns (y [B, T, D], final_state or None, saved or None); `saved` is what
+    vmb_token_scan_bwd needs."""
+    B, T, D, N, code, strides = _token_scan_inputs(x, delta, A, Bm, Cm, Dskip, delta_bias, z)
+    n, T1, total = _sequences(offsets, B, T)
+    packed = offsets is not None
+    _float(initial_state, "initial_state", (n, D, N))
+    if final_state is None and want_state:
+        final_state = torch.empty((n, D, N), dtype=torch.float32, device=x.device)
+    _float(final_state, "final_state", (n, D, N))
+    if y is None:
+        y = x.new_empty((B, T, D))
+    _like(y, "y", (B, T, D), x.dtype)
+    if saved is not None:
+        _token_scan_saved(saved, n, T1, total, packed, D, N)
+    elif want_saved:
+        saved = torch.empty(_token_scan_saved(True, n, T1, total, packed, D, N), dtype=torch.uint8, device=x.device)
+    _one_device(x, delta, A, Bm, Cm, Dskip, delta_bias, z, initial_state, offsets, y, final_state, saved)
+    ws = _layer_workspace(workspace, x, "vmb_token_scan_workspace_bytes", n, T1, total, packed, D, N, 0, code)
+    _check(lib.vmb_token_scan_fwd(x.data_ptr(), delta.data_ptr(), A.data_ptr(), Bm.data_ptr(), Cm.data_ptr(), _ptr(Dskip),
+                                  _ptr(delta_bias), _ptr(z), strides, _ptr(initial_state), _ptr(offsets), y.data_ptr(),
+                                  _ptr(final_state), _ptr(saved), n, T1, total, D, N, VMB_FLAG_SOFTPLUS if softplus else 0, code,
+                                  ws.data_ptr(), ws.numel(), _stream_of(x, stream)), "vmb_token_scan_fwd")
+    return y, final_state, saved
+
+
+@_on_its_stream
+def vmb_token_scan_bwd(x, delta, A, Bm, Cm, Dskip, delta_bias, z, dy, saved, *, softplus: bool = True, dfinal_state=None,
+                       offsets=None, want_initial: bool = False, workspace=None, stream=None) -> dict:
+    """Gradients of vmb_token_scan_fwd given dy [B, T, D] and, optionally, dfinal_state: dict(x, delta, A, B, C, Dskip,
+    delta_bias, z[, initial_state]), None where the input was None.  `saved`: the forward's, for the same inputs."""
+    B, T, D, N, code, strides = _token_scan_inputs(x, delta, A, Bm, Cm, Dskip, delta_bias, z)
+    n, T1, total = _sequences(offsets, B, T)
+    packed = offsets is not None
+    _float(dfinal_state, "dfinal_state", (n, D, N))
+    if dy is None or saved is None:
+        raise ValueError("dy and the forward's saved are needed")
+    _like(dy, "dy", (B, T, D), x.dtype)
+    _token_scan_saved(saved, n, T1, total, packed, D, N)
+    new = torch.empty if total or n else torch.zeros  # (an empty problem launches nothing)
+    dev = x.device
+    out = {k: None if t is None else new(t.shape, dtype=t.dtype, device=dev)
+           for k, t in (("x", x), ("delta", delta), ("A", A), ("B", Bm), ("C", Cm), ("Dskip", Dskip), ("delta_bias", delta_bias),
+                        ("z", z))}
+    if want_initial:
+        out["initial_state"] = torch.empty((n, D, N), dtype=torch.float32, device=dev)
+    _one_device(x, delta, A, Bm, Cm, Dskip, delta_bias, z, dy, saved, dfinal_state, offsets)
+    ws = _layer_workspace(workspace, x, "vmb_token_scan_workspace_bytes", n, T1, total, packed, D, N, 1, code)
+    _check(lib.vmb_token_scan_bwd(x.data_ptr(), delta.data_ptr(), A.data_ptr(), Bm.data_ptr(), Cm.data_ptr(), _ptr(Dskip),
+                                  _ptr(delta_bias), _ptr(z), strides, _ptr(offsets), dy.data_ptr(), _ptr(dfinal_state),
+                                  saved.data_ptr(), out["x"].data_ptr(), out["delta"].data_ptr(), out["A"].data_ptr(),
+                                  out["B"].data_ptr(), out["C"].data_ptr(), _ptr(out["Dskip"]), _ptr(out["delta_bias"]),
+                                  _ptr(out["z"]), _ptr(out.get("initial_state")), n, T1, total, D, N,
+                                  VMB_FLAG_SOFTPLUS if softplus else 0, code, ws.data_ptr(), ws.numel(),
+                                  _stream_of(x, stream)), "vmb_token_scan_bwd")
+    return out
+
+
+@_on_its_stream
+def vmb_token_scan_step(x, delta, A, Bm, Cm, Dskip, delta_bias, z, state, *, softplus: bool = True, slots=None, y=None,
+                        stream=None) -> torch.Tensor:
+    """The scan for T tokens (one, or a few) of every row from its state, updated in place: inputs as for
+    vmb_token_scan_fwd, state float32 [pool, D, N]; slots int32 [B] (row b uses state slots[b]; a negative slot is padding,
+    its y is zero) or None (row b uses state b).  Returns y [B, T, D]."""
+    B, T, D, N, code, strides = _token_scan_inputs(x, delta, A, Bm, Cm, Dskip, delta_bias, z)
+    if state.dim() != 3:
+        raise ValueError("state must be float32 [pool, D, N]")
+    _float(state, "state", (state.shape[0], D, N))
+    _pool(state, slots, B)
+    if y is None:
+        y = x.new_empty((B, T, D))
+    _like(y, "y", (B, T, D), x.dtype)
+    _one_device(x, delta, A, Bm, Cm, Dskip, delta_bias, z, state, slots, y)
+    _check(lib.vmb_token_scan_step(x.data_ptr(), delta.data_ptr(), A.data_ptr(), Bm.data_ptr(), Cm.data_ptr(), _ptr(Dskip),
+                                   _ptr(delta_bias), _ptr(z), strides, state.data_ptr(), _ptr(slots), y.data_ptr(), B, T, D, N,
+                                   state.shape[0], VMB_FLAG_SOFTPLUS if softplus else 0, code, _stream_of(x, stream)),
+           "vmb_token_scan_step")
+    return y
+
+
+def vmb_rms_norm_workspace_bytes(rows: int, C: int, dtype: torch.dtype = torch.float32) -> int:
+    return int(lib.vmb_rms_norm_workspace_bytes(rows, C, _dtype_code(dtype)))
+
+
+def _rms_inputs(x, weight):
+    _dev(x, "x")
+    if x.dim() < 1:
+        raise ValueError("x must be [..., C]")
+    C = x.shape[-1]
+    _float(weight, "weight", (C,))
+    return x.numel() // C if C else 0, C, _dtype_code(x.dtype)
+
+
+@_on_its_stream
+def vmb_rms_norm_fwd(x, weight=None, residual=None, *, eps: float = 1e-6, bits8: bool = False, want_stats: bool = False,
+                     y=None, total=None, scale=None, rstd=None, stream=None):
+    """Root-mean-square norm of the rows of x [..., C] after the residual's addition: returns (y, total, scale, rstd).
+    total = x + residual in the dtype of x (None without a residual), y = total * rstd * weight (float32 [C] or None) in
+    the dtype of x, or with `bits8` in torch.float8_e4m3fn, to be multiplied by scale (float32 [...], one per row; otherwise
+    None); rstd float32 [...] with `want_stats`, for vmb_rms_norm_bwd."""
+    rows, C, code = _rms_inputs(x, weight)
+    lead, kind = x.shape[:-1], torch.float8_e4m3fn if bits8 else x.dtype
+    _like(residual, "residual", x.shape, x.dtype)
+    if y is None:
+        y = torch.empty(x.shape, dtype=kind, device=x.device)
+    else:
+        _dev(y, "y")
+        if y.shape != x.shape or y.dtype != kind:
+            raise ValueError(f"y must be {list(x.shape)} in {kind}")
+    if residual is None:
+        if total is not None:
+            raise ValueError("total: without a residual it is x")
+    elif total is None:
+        total = torch.empty_like(x)
+    _like(total, "total", x.shape, x.dtype)
+    if not bits8 and scale is not None:
+        raise ValueError("scale: only 8-bit outputs have one")
+    if bits8 and scale is None:
+        scale = torch.empty(lead, dtype=torch.float32, device=x.device)
+    if rstd is None and want_stats:
+        rstd = torch.empty(lead, dtype=torch.float32, device=x.device)
+    _float(scale, "scale", lead)
+    _float(rstd, "rstd", lead)
+    _one_device(x, weight, residual, y, total, scale, rstd)
+    _check(lib.vmb_rms_norm_fwd(x.data_ptr(), _ptr(residual), _ptr(weight), y.data_ptr(), _ptr(total), _ptr(scale), _ptr(rstd),
+                                rows, C, eps, code, _stream_of(x, stream)), "vmb_rms_norm_fwd")
+    return y, total, scale, rstd
+
+
+@_on_its_stream
+def vmb_rms_norm_bwd(x, weight, rstd, dy, *, dsum=None, workspace=None, stream=None) -> dict:
+    """Gradients of vmb_rms_norm_fwd given dy and, optionally, dsum, the gradient that reaches the sum on its own:
+    dict(x, weight (None without one)).  x: what was normalised (the forward's total, if there was a residual); the
+    gradient of the residual is that of x."""
+    rows, C, code = _rms_inputs(x, weight)
+    if rstd is None or dy is None:
+        raise ValueError("dy and the forward's rstd are needed")
+    _float(rstd, "rstd", x.shape[:-1])
+    _like(dy, "dy", x.shape, x.dtype)
+    _like(dsum, "dsum", x.shape, x.dtype)
+    new = torch.empty_like if x.numel() else torch.zeros_like  # (an empty problem launches nothing: sums of nothing)
+    out = dict(x=torch.empty_like(x), weight=None if weight is None else new(weight))
+    _one_device(x, weight, rstd, dy, dsum)
+    ws = _layer_workspace(workspace, x, "vmb_rms_norm_workspace_bytes", rows, C, code)
+    _check(lib.vmb_rms_norm_bwd(x.data_ptr(), _ptr(weight), rstd.data_ptr(), dy.data_ptr(), _ptr(dsum), out["x"].data_ptr(),
+                                _ptr(out["weight"]), rows, C, code, ws.data_ptr(), ws.numel(), _stream_of(x, stream)),
+           "vmb_rms_norm_bwd")
+    return out
+
+
+def vmb_linear_workspace_bytes(M: int, K: int, N: int, grads: bool = False) -> int:
+    return int(lib.vmb_linear_workspace_bytes(M, K, N, int(grads)))
+
+
+def _linear_inputs(x, weight, kind, act):
+    """(rows, K, N, elements between rows) of x [..., K], whose rows may be strided evenly, and weight [N, K]."""
+    if not x.is_cuda:
+        raise ValueError("x must be a CUDA tensor")
+    _dev(weight, "weight")
+    if x.dim() < 1 or weight.dim() != 2 or x.shape[-1] != weight.shape[1]:
+        raise ValueError("x [..., K] and weight [N, K] expected")
+    if x.dtype != kind or weight.dtype != kind:
+        raise TypeError(f"x and weight must be {kind}")
+    if act not in _ACTS:
+        raise ValueError(f"act must be one of {sorted(_ACTS)}")
+    N, K = weight.shape
+    if x.is_contiguous():
+        return (x.numel() // K if K else x.shape[:-1].numel()), K, N, K
+    try:
+        flat = x.view(-1, K)
+    except RuntimeError:
+        raise ValueError("x: the rows must be evenly strided") from None
+    if flat.stride(1) != 1 and K > 1:
+        raise ValueError("x: the channels of a row must be dense")
+    return flat.shape[0], K, N, (flat.stride(0) if flat.shape[0] > 1 else K)
+
+
+@_on_its_stream
+def vmb_linear_fwd(x, weight, bias=None, *, act: str = "none", residual=None, x_scale=None, weight_scale=None,
+                   want_pre: bool = False, y=None, pre=None, workspace=None, stream=None):
+    """Matrix product of a projection: y = act(x weight^T + bias) + residual in bfloat16, act "none", "silu" or "gelu".
+    x [..., K] (rows may be strided evenly) and weight [N, K] bfloat16, or torch.float8_e4m3fn with x_scale float32 [...] and
+    weight_scale float32 [N], the scales of their rows; bias float32 [N] or None; residual [..., N] bfloat16 or None.
+    Returns (y [..., N], pre or None); pre = x weight^T + bias in bfloat16 with `want_pre`, for vmb_linear_bwd."""
+    if (x_scale is None) != (weight_scale is None):
+        raise ValueError("x_scale and weight_scale are given together")
+    M, K, N, x_t = _linear_inputs(x, weight, torch.bfloat16 if x_scale is None else torch.float8_e4m3fn, act)
+    lead = x.shape[:-1]
+    shape = (*lead, N)
+    _float(x_scale, "x_scale", lead)
+    _float(weight_scale, "weight_scale", (N,))
+    _float(bias, "bias", (N,))
+    for t, name in ((residual, "residual"), (y, "y"), (pre, "pre")):
+        if t is not None:
+            _dev(t, name)
+            if t.shape != shape or t.dtype != torch.bfloat16:
+                raise ValueError(f"{name} must be bfloat16 {list(shape)}")
+    if y is None:
+        y = torch.empty(shape, dtype=torch.bfloat16, device=x.device)
+    if pre is None and want_pre:
+        pre = torch.empty(shape, dtype=torch.bfloat16, device=x.device)
+    _one_device(x, weight, bias, residual, x_scale, weight_scale, y, pre)
+    ws = _layer_workspace(workspace, x, "vmb_linear_workspace_bytes", M, K, N, 0)
+    _check(lib.vmb_linear_fwd(x.data_ptr(), x_t, weight.data_ptr(), _ptr(x_scale), _ptr(weight_scale), _ptr(bias), _ptr(residual),
+                              y.data_ptr(), _ptr(pre), M, K, N, _ACTS[act], ws.data_ptr(), ws.numel(), _stream_of(x, stream)),
+           "vmb_linear_fwd")
+    return y, pre
+
+
+@_on_its_stream
+def vmb_linear_bwd(x, weight, dy, pre=None, *, act: str = "none", want_x: bool = True, want_weight: bool = True,
+                   want_bias: bool = False, workspace=None, stream=None) -> dict:
+    """Gradients of vmb_linear_fwd of bfloat16 given dy [..., N] and, with an activation, the forward's pre: dict(x [..., K],
+    weight [N, K] (bfloat16), bias (float32 [N])), None where not wanted; the residual's gradient is dy."""
+    M, K, N, x_t = _linear_inputs(x, weight, torch.bfloat16, act)
+    shape = (*x.shape[:-1], N)
+    if dy is None or (pre is None and act != "none"):
+        raise ValueError("dy and, with an activation, the forward's pre are needed")
+    for t, name in ((dy, "dy"), (pre, "pre")):
+        if t is not None:
+            _dev(t, name)
+            if t.shape != shape or t.dtype != torch.bfloat16:
+                raise ValueError(f"{name} must be bfloat16 {list(shape)}")
+    new = torch.empty if M and N else torch.zeros  # (an empty problem launches nothing: sums of nothing)
+    dev = x.device
+    out = dict(x=new(x.shape, dtype=x.dtype, device=dev) if want_x else None,
+               weight=new((N, K), dtype=x.dtype, device=dev) if want_weight else None,
+               bias=new((N,), dtype=torch.float32, device=dev) if want_bias else None)
+    _one_device(x, weight, dy, pre)
+    ws = _layer_workspace(workspace, x, "vmb_linear_workspace_bytes", M, K, N, 1)
+    _check(lib.vmb_linear_bwd(x.data_ptr(), x_t, weight.data_ptr(), _ptr(pre), dy.data_ptr(), _ptr(out["x"]), _ptr(out["weight"]),
+                              _ptr(out["bias"]), M, K, N, _ACTS[act], ws.data_ptr(), ws.numel(), _stream_of(x, stream)),
+           "vmb_linear_bwd")
     return out
 
 
