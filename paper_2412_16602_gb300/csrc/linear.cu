@@ -23,13 +23,6 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
 
-__device__ __forceinline__ float act_of(float z, int act) {
-    return act == VMB_ACT_SILU ? activate<VMB_ACT_SILU>(z) : act == VMB_ACT_GELU ? activate<VMB_ACT_GELU>(z) : z;
-}
-__device__ __forceinline__ float slope_of(float z, int act) {
-    return act == VMB_ACT_SILU ? activate_slope<VMB_ACT_SILU>(z) : act == VMB_ACT_GELU ? activate_slope<VMB_ACT_GELU>(z) : 1.0f;
-}
-
 // A CTA takes 64 x 64 outputs, a warp 32 x 32 of them; operands pass element by element through shared memory.
 template <typename T> __global__ void __launch_bounds__(kAnyThreads) gemm_any_kernel(GemmProblem p, int tiles_n) {
     __shared__ __align__(16) __nv_bfloat16 sa[kAnyTile * kAnyPitch], sb[kAnyTile * kAnyPitch];
@@ -143,15 +136,29 @@ DzGrid dz_grid(long long M, int N, int V) {
 }
 
 struct LinearLayout {
-    size_t dz, partial, bytes;
+    size_t dz, sums, parts, bytes;  // dZ; partial sums of its columns; parts of split contractions
 };
-LinearLayout linear_layout(long long M, int N, bool grads) {
-    LinearLayout l{256, 256, 256};
-    if (!grads) return l;
-    l.partial = l.dz + align_up((size_t)M * N * 2, 256);
-    const size_t rows = dz_grid(M, N, 1).y > dz_grid(M, N, 8).y ? dz_grid(M, N, 1).y : dz_grid(M, N, 8).y;
-    l.bytes = l.partial + align_up(rows * N * 4, 256);
+LinearLayout linear_layout(long long M, int K, int N, bool grads) {
+    LinearLayout l{256, 256, 256, 256};
+    size_t parts;
+    if (grads) {
+        l.sums = l.dz + align_up((size_t)M * N * 2, 256);
+        const size_t rows = dz_grid(M, N, 1).y > dz_grid(M, N, 8).y ? dz_grid(M, N, 1).y : dz_grid(M, N, 8).y;
+        l.parts = l.sums + align_up(rows * N * 4, 256);
+        const size_t a = K ? gemm_partial_bytes(M, K, N, false) : 0, b = K ? gemm_partial_bytes(N, K, M, false) : 0;
+        parts = a > b ? a : b;
+    } else {
+        const size_t a = gemm_partial_bytes(M, N, K, false), b = gemm_partial_bytes(M, N, K, true);
+        parts = a > b ? a : b;
+    }
+    l.bytes = l.parts + parts;
     return l;
+}
+
+vmb_status launch_gemm(const GemmProblem& p, bool bits8, const LinearArgs& a, const LinearLayout& l, cudaStream_t stream) {
+    bool taken = false;
+    const vmb_status s = launch_gemm_tc(p, bits8, (float*)((char*)a.ws + l.parts), &((WsHeader*)a.ws)->err, stream, &taken);
+    return s != VMB_OK || taken ? s : launch_gemm_any(p, bits8, stream);
 }
 
 }  // namespace
@@ -167,17 +174,18 @@ vmb_status launch_gemm_any(const GemmProblem& p0, bool bits8, cudaStream_t strea
     return launch_kernel(fn, dim3((unsigned)grid), dim3(kAnyThreads), 0, args, stream) == cudaSuccess ? VMB_OK : VMB_ERR_CUDA;
 }
 
-size_t linear_workspace_bytes(long long M, int, int N, bool grads) { return linear_layout(M, N, grads).bytes; }
+size_t linear_workspace_bytes(long long M, int K, int N, bool grads) { return linear_layout(M, K, N, grads).bytes; }
 
 vmb_status launch_linear_fwd(const LinearArgs& a, cudaStream_t stream) {
-    if (a.ws_bytes < linear_workspace_bytes(a.M, a.K, a.N, false)) return VMB_ERR_WORKSPACE;
+    const LinearLayout l = linear_layout(a.M, a.K, a.N, false);
+    if (a.ws_bytes < l.bytes) return VMB_ERR_WORKSPACE;
     const GemmProblem p{a.x, a.weight, a.M, a.N, a.K, a.x_t, 1, a.K, 1,
                         {a.x_scale, a.weight_scale, a.bias, (const __nv_bfloat16*)a.residual, (__nv_bfloat16*)a.y, (__nv_bfloat16*)a.pre, a.act}};
-    return launch_gemm_any(p, a.x_scale != nullptr, stream);
+    return launch_gemm(p, a.x_scale != nullptr, a, l, stream);
 }
 
 vmb_status launch_linear_bwd(const LinearArgs& a, cudaStream_t stream) {
-    const LinearLayout l = linear_layout(a.M, a.N, true);
+    const LinearLayout l = linear_layout(a.M, a.K, a.N, true);
     if (a.ws_bytes < l.bytes) return VMB_ERR_WORKSPACE;
     const __nv_bfloat16 *dy = (const __nv_bfloat16*)a.dy, *pre = (const __nv_bfloat16*)a.pre, *dz = dy;
     long long M = a.M;
@@ -186,7 +194,7 @@ vmb_status launch_linear_bwd(const LinearArgs& a, cudaStream_t stream) {
         const bool vec = N % 8 == 0 && ((reinterpret_cast<uintptr_t>(dy) | reinterpret_cast<uintptr_t>(pre)) & 15) == 0;
         const DzGrid g = dz_grid(M, N, vec ? 8 : 1);
         __nv_bfloat16* out = (__nv_bfloat16*)((char*)a.ws + l.dz);
-        float* partial = a.dbias ? (float*)((char*)a.ws + l.partial) : nullptr;
+        float* partial = a.dbias ? (float*)((char*)a.ws + l.sums) : nullptr;
         void* args[] = {&dy, &pre, &out, &partial, &M, &N, &act};
         const void* fn = vec ? (const void*)linear_dz_kernel<8> : (const void*)linear_dz_kernel<1>;
         if (launch_kernel(fn, dim3(g.x, g.y), dim3(32 * kDzRows), 0, args, stream) != cudaSuccess) return VMB_ERR_CUDA;
@@ -198,12 +206,12 @@ vmb_status launch_linear_bwd(const LinearArgs& a, cudaStream_t stream) {
     }
     if (a.dx && a.K > 0) {
         const GemmProblem p{dz, a.weight, M, a.K, N, N, 1, 1, a.K, {nullptr, nullptr, nullptr, nullptr, (__nv_bfloat16*)a.dx, nullptr, VMB_ACT_NONE}};
-        const vmb_status s = launch_gemm_any(p, false, stream);
+        const vmb_status s = launch_gemm(p, false, a, l, stream);
         if (s != VMB_OK) return s;
     }
     if (a.dweight && a.K > 0) {
         const GemmProblem p{dz, a.x, N, a.K, M, 1, N, 1, a.x_t, {nullptr, nullptr, nullptr, nullptr, (__nv_bfloat16*)a.dweight, nullptr, VMB_ACT_NONE}};
-        return launch_gemm_any(p, false, stream);
+        return launch_gemm(p, false, a, l, stream);
     }
     return VMB_OK;
 }

@@ -1,0 +1,457 @@
+// linear_tc.cu - the matrix product on the fifth-generation tensor cores: out [M][N] = epilogue(A B^T), A and B with the contraction
+// dense (forward: x and the weights) or with their rows dense (gradients: dx takes the weights so, dW both operands).
+//
+// Tiles of 256 x 256 by a pair of CTAs (each holds half of the rows of A and of B in its shared memory and 128 x 256 sums in its
+// tensor memory), or of 128 x 128 by one CTA where those would leave SMs idle.  One warp starts tensor copies into a ring of stages
+// of 128 bytes of the contraction, swizzled by 128 bytes; one thread of the pair issues the products; eight warps take the sums of one buffer of
+// tensor memory through the epilogue while the products of the next tile go to the other.  Where tiles are few and the contraction long
+// it is split, the parts' sums are kept in fp32 and joined in order by a second launch.
+// Every wait is bounded; one that gives up leaves kErrTimeout in the workspace's header and ends the kernel.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include <mutex>
+
+#include "linear_common.cuh"
+
+namespace vmb {
+
+namespace {
+
+constexpr int kTcThreads = 320, kTcStages = 6, kTcEpiWarps = 8;
+constexpr int kTcA = 128 * 128;  // bytes of A in a stage, and of B: 128 rows of 128 bytes of the contraction
+constexpr int kTcStage = 2 * kTcA;
+constexpr int kTcSmem = 1024 + kTcStages * kTcStage + kTcEpiWarps * 4096;
+
+struct TcKernel {
+    CUtensorMap ta, tb;
+    GemmEpilogue e;
+    float* partial;  // [splits][M][N]
+    unsigned* err;
+    long long M;
+    int N;
+    int tiles_m, tiles_n, splits, kblocks, kper, units;
+    bool vec;
+};
+
+// Tensor-memory matrix descriptors of operands swizzled by 128 bytes.  The contraction dense: rows of 128 bytes, eight rows every 1024
+// bytes, a step of 32 bytes along the contraction moves the start.  The rows dense: 64 rows every 128 x 64 bytes, eight steps of the
+// contraction every 1024.
+__device__ __forceinline__ uint64_t tc_desc(uint32_t addr, bool rows_dense) {
+    const uint64_t lead = rows_dense ? (8192 >> 4) : 1;
+    return (uint64_t)((addr >> 4) & 0x3FFF) | lead << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+
+// fp32 sums of bf16 (or e4m3) A and B; bits 15 and 16: rows dense.
+template <int CG, int BN, bool kBits8, bool kArow, bool kBrow> constexpr uint32_t tc_idesc() {
+    return (1u << 4) | (kBits8 ? 0u : 1u << 7 | 1u << 10) | (kArow ? 1u << 15 : 0u) | (kBrow ? 1u << 16 : 0u) | (uint32_t)(BN >> 3) << 17 |
+           (uint32_t)((128 * CG) >> 4) << 24;
+}
+
+template <int CG, bool kBits8> __device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+    if constexpr (CG == 2 && kBits8)
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add));
+    else if constexpr (CG == 2)
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add));
+    else if constexpr (kBits8)
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add));
+    else
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add));
+}
+
+// The products issued so far arrive at `bar` of every CTA of the pair when they are done.
+template <int CG> __device__ __forceinline__ void tc_commit(uint32_t bar) {
+    if constexpr (CG == 2) {
+        const uint16_t both = 3;
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(both) : "memory");
+    } else {
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    }
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t in_first_cta(uint32_t addr) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
+}
+
+// A box of the map from (x, y) into this CTA's shared memory; its bytes count at `bar`, which may be the first CTA's.
+template <int CG> __device__ __forceinline__ void tc_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    if constexpr (CG == 2)
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                     "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
+                     : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                     "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
+                     : "memory");
+}
+
+__device__ __forceinline__ bool tc_test(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(done)
+                 : "r"(bar), "r"(parity)
+                 : "memory");
+    return done != 0;
+}
+// (the sums of a tile may take long: kTcSumsNs)
+constexpr uint64_t kTcSumsNs = 4ull * 1000 * 1000 * 1000;
+__device__ __forceinline__ bool tc_wait(uint32_t bar, uint32_t parity, unsigned* err, uint64_t limit = kWaitLimitNs) {
+    if (tc_test(bar, parity)) return true;
+    const uint64_t t0 = globaltimer_ns();
+    for (;;) {
+        if (tc_test(bar, parity)) return true;
+        if (globaltimer_ns() - t0 > limit) {
+            atomicOr(err, kErrTimeout);
+            return false;
+        }
+    }
+}
+
+__device__ __forceinline__ void tmem_load32(uint32_t (&r)[32], uint32_t addr) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,"
+        "%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+          "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]),
+          "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+struct TcUnit {
+    int m, n, split;
+};
+// Units in order: the parts of a tile, then tiles down the rows within bands of 16 (the band's rows of A and all of B pass through the L2 cache once).
+__device__ __forceinline__ TcUnit tc_unit(const TcKernel& k, int u) {
+    TcUnit t;
+    t.split = u % k.splits;
+    const int tile = u / k.splits, band = tile / (16 * k.tiles_n), in = tile - band * 16 * k.tiles_n;
+    const int high = min(16, k.tiles_m - band * 16);
+    t.m = band * 16 + in % high;
+    t.n = in / high;
+    return t;
+}
+
+template <int CG, int BN, bool kBits8, bool kArow, bool kBrow> __global__ void __launch_bounds__(kTcThreads, 1) gemm_tc_kernel(const __grid_constant__ TcKernel k) {
+    static_assert(BN == 128 * CG, "128 rows of B in each CTA");
+    constexpr int kCols = 2 * BN, kElems = kBits8 ? 128 : 64;  // columns of tensor memory; elements of the contraction in a stage
+    extern __shared__ char smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * kTcStages + 4];
+    __shared__ uint32_t s_tmem;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * kTcStages, sums_full = empty + 8 * kTcStages, sums_empty = sums_full + 16;
+    if (tid == 0) {
+        for (int i = 0; i < kTcStages; ++i) mbarrier_init(full + 8 * i, 1), mbarrier_init(empty + 8 * i, 1);
+        for (int i = 0; i < 2; ++i) mbarrier_init(sums_full + 8 * i, 1), mbarrier_init(sums_empty + 8 * i, CG * kTcEpiWarps);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        if constexpr (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "n"(kCols));
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "n"(kCols));
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    if constexpr (CG == 2) cluster_barrier();
+    else __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = s_tmem;
+    pdl_wait();
+    pdl_launch_dependents();
+    const int first = blockIdx.x / CG, step = gridDim.x / CG;
+
+    if (warp == 0) {
+        if (lane == 0) {  // copies
+            uint32_t stage = 0, phase = 0;
+            bool ok = true;
+            for (int u = first; u < k.units && ok; u += step) {
+                const TcUnit t = tc_unit(k, u);
+                const int m0 = t.m * 128 * CG + (int)rank * 128, n0 = t.n * BN + (int)rank * 128;
+                const int kb1 = min(k.kblocks, (t.split + 1) * k.kper);
+                for (int kb = t.split * k.kper; kb < kb1; ++kb) {
+                    if (!(ok = tc_wait(empty + 8 * stage, phase ^ 1, k.err))) break;
+                    const uint32_t a = base + stage * kTcStage, b = a + kTcA;
+                    const uint32_t bar = CG == 2 ? in_first_cta(full + 8 * stage) : full + 8 * stage;
+                    if (rank == 0) mbarrier_expect_tx(full + 8 * stage, CG * kTcStage);
+                    if constexpr (kArow) {
+                        tc_load<CG>(a, &k.ta, m0, kb * kElems, bar);
+                        tc_load<CG>(a + 8192, &k.ta, m0 + 64, kb * kElems, bar);
+                    } else {
+                        tc_load<CG>(a, &k.ta, kb * kElems, m0, bar);
+                    }
+                    if constexpr (kBrow) {
+                        tc_load<CG>(b, &k.tb, n0, kb * kElems, bar);
+                        tc_load<CG>(b + 8192, &k.tb, n0 + 64, kb * kElems, bar);
+                    } else {
+                        tc_load<CG>(b, &k.tb, kb * kElems, n0, bar);
+                    }
+                    if (++stage == kTcStages) stage = 0, phase ^= 1;
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {  // products
+            constexpr uint32_t idesc = tc_idesc<CG, BN, kBits8, kArow, kBrow>();
+            constexpr uint64_t astep = (kArow ? 2048 : 32) >> 4, bstep = (kBrow ? 2048 : 32) >> 4;
+            uint32_t stage = 0, phase = 0, buf = 0, bphase = 0;
+            bool ok = true;
+            for (int u = first; u < k.units && ok; u += step) {
+                const TcUnit t = tc_unit(k, u);
+                if (!(ok = tc_wait(sums_empty + 8 * buf, bphase ^ 1, k.err))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const int kb0 = t.split * k.kper, kb1 = min(k.kblocks, kb0 + k.kper);
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (!(ok = tc_wait(full + 8 * stage, phase, k.err))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t a = tc_desc(base + stage * kTcStage, kArow), b = tc_desc(base + stage * kTcStage + kTcA, kBrow);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) tc_mma<CG, kBits8>(tmem + buf * BN, a + i * astep, b + i * bstep, idesc, kb > kb0 || i > 0);
+                    tc_commit<CG>(empty + 8 * stage);
+                    if (++stage == kTcStages) stage = 0, phase ^= 1;
+                }
+                tc_commit<CG>(sums_full + 8 * buf);
+                buf ^= 1;
+                if (buf == 0) bphase ^= 1;
+            }
+        }
+    } else {  // sums: 32 rows and half of the columns for each warp
+        const int quad = warp & 3, half = (warp - 2) >> 2;
+        char* stage = smem_raw + (base - smem_u32(smem_raw)) + kTcStages * kTcStage + (warp - 2) * 4096;
+        uint32_t buf = 0, bphase = 0;
+        for (int u = first; u < k.units; u += step) {
+            const TcUnit t = tc_unit(k, u);
+            const long long m0 = (long long)t.m * 128 * CG + rank * 128 + quad * 32;
+            if (!tc_wait(sums_full + 8 * buf, bphase, k.err, kTcSumsNs)) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+            for (int c = 0; c < BN / 2; c += 32) {
+                uint32_t r[32];
+                const int col = half * (BN / 2) + c;
+                tmem_load32(r, tmem + buf * BN + col + ((uint32_t)(quad * 32) << 16));
+                if (c + 32 == BN / 2) {  // the buffer may be used again
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        if constexpr (CG == 2)
+                            asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_first_cta(sums_empty + 8 * buf)) : "memory");
+                        else
+                            mbarrier_arrive(sums_empty + 8 * buf);
+                    }
+                }
+                const int n0 = t.n * BN + col;
+                if (n0 >= k.N) continue;
+                // from a row in each lane to eight columns of a row in each: pieces of 16 bytes, turned by the row so that neither side has conflicts
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    *reinterpret_cast<uint4*>(stage + lane * 128 + ((q ^ (lane & 7)) << 4)) = make_uint4(r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]);
+                __syncwarp();
+                const int n = n0 + (lane & 3) * 8;
+                float scale[8], bias[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    scale[i] = k.e.col_scale && n + i < k.N ? k.e.col_scale[n + i] : 1.0f;
+                    bias[i] = k.e.bias && n + i < k.N ? k.e.bias[n + i] : 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int row = (lane >> 2) + 8 * i, u0 = (lane & 3) * 2;
+                    const long long m = m0 + row;
+                    const float4 x = *reinterpret_cast<const float4*>(stage + row * 128 + ((u0 ^ (row & 7)) << 4));
+                    const float4 y = *reinterpret_cast<const float4*>(stage + row * 128 + (((u0 + 1) ^ (row & 7)) << 4));
+                    if (m >= k.M || n >= k.N) continue;
+                    float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                    const long long at = m * k.N + n;
+                    if (k.splits > 1) {
+                        float* p = k.partial + (long long)t.split * k.M * k.N + at;
+                        if (k.vec) {
+                            *reinterpret_cast<float4*>(p) = x;
+                            *reinterpret_cast<float4*>(p + 4) = y;
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                if (n + j < k.N) p[j] = v[j];
+                        }
+                        continue;
+                    }
+                    const float rs = k.e.row_scale ? k.e.row_scale[m] : 1.0f;
+                    if (k.vec) {
+                        finish<8>(k.e, v, scale, bias, rs, at);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            float one[1] = {v[j]};
+                            const float s1[1] = {scale[j]}, b1[1] = {bias[j]};
+                            if (n + j < k.N) finish<1>(k.e, one, s1, b1, rs, at + j);
+                        }
+                    }
+                }
+                __syncwarp();
+            }
+            buf ^= 1;
+            if (buf == 0) bphase ^= 1;
+        }
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    if constexpr (CG == 2) cluster_barrier();
+    else __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (warp == 1) {
+        if constexpr (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kCols));
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kCols));
+    }
+}
+
+// The parts of a split contraction in order, and the epilogue.
+template <int V> __global__ void __launch_bounds__(256) gemm_join_kernel(GemmEpilogue e, const float* partial, int splits, long long M, int N) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const long long item = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int per = (N + V - 1) / V;
+    if (item >= M * per) return;
+    const long long m = item / per;
+    const int n = (int)(item - m * per) * V;
+    const long long at = m * N + n;
+    float v[V], scale[V], bias[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = 0.0f;
+    for (int s = 0; s < splits; ++s) {
+        float p[V];
+        if constexpr (V == 8) {
+            const float4 x = *reinterpret_cast<const float4*>(partial + (long long)s * M * N + at), y = *reinterpret_cast<const float4*>(partial + (long long)s * M * N + at + 4);
+            p[0] = x.x, p[1] = x.y, p[2] = x.z, p[3] = x.w, p[4] = y.x, p[5] = y.y, p[6] = y.z, p[7] = y.w;
+        } else {
+            p[0] = partial[(long long)s * M * N + at];
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] += p[i];
+    }
+    column_terms<V>(e, n, scale, bias);
+    finish<V>(e, v, scale, bias, e.row_scale ? e.row_scale[m] : 1.0f, at);
+}
+
+struct TcPlan {
+    int cg, tiles_m, tiles_n, splits, kblocks, kper;
+};
+long long up(long long a, long long b) { return (a + b - 1) / b; }
+
+// By estimated clocks: a stage of the contraction takes a pair 512 of them for 256 x 256 sums and one CTA 300 for 128 x 128 (its operands' bytes in shared
+// memory bound it there), a tile 2000 to begin and end, a join 5000 and 8 bytes of traffic for each part's sum.
+TcPlan tc_plan(long long M, int N, long long K, bool bits8) {
+    const int sms = device_sm_count();
+    const long long kblocks = up(K, bits8 ? 128 : 64);
+    TcPlan best{};
+    double least = 0.0;
+    for (int cg = 2; cg >= 1; --cg) {
+        const long long tm = up(M, 128 * cg), tn = up(N, 128 * cg), slots = sms / cg;
+        for (long long want = 1; want <= 64; ++want) {
+            const long long kper = up(kblocks, want), splits = up(kblocks, kper);
+            if (splits != want || (want > 1 && (kper < 4 || tm * tn * want > 2 * slots))) continue;
+            double t = (double)up(tm * tn * splits, slots) * (kper * (cg == 2 ? 512.0 : 300.0) + 2000.0);
+            if (splits > 1) t += 5000.0 + (double)M * N * splits * 8.0 / 3500.0;
+            if (best.cg == 0 || t < least) least = t, best = TcPlan{cg, (int)tm, (int)tn, (int)splits, (int)kblocks, (int)kper};
+        }
+    }
+    return best;
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 encoder() {
+    static std::once_flag once;
+    static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+    std::call_once(once, [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q{};
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+    });
+    return fn;
+}
+
+// Boxes of 128 bytes: of the contraction and 128 rows, or of 64 rows and 64 steps of the contraction.
+bool encode(CUtensorMap* m, const void* base, long long rows, long long K, long long r, long long c, bool bits8, bool* rows_dense) {
+    const long long es = bits8 ? 1 : 2;
+    if (reinterpret_cast<uintptr_t>(base) & 15) return false;
+    *rows_dense = c != 1;
+    if (*rows_dense && (bits8 || r != 1)) return false;
+    const long long ld = *rows_dense ? c : r;
+    if (ld <= 0 || ld * es % 16 || ld * es >= (1LL << 40)) return false;
+    const PFN_cuTensorMapEncodeTiled_v12000 enc = encoder();
+    if (!enc || refuse_tensor_maps()) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)(*rows_dense ? rows : K), (cuuint64_t)(*rows_dense ? K : rows)};
+    const cuuint64_t strides[1] = {(cuuint64_t)(ld * es)};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / es), *rows_dense ? 64u : 128u}, estr[2] = {1, 1};
+    return enc(m, bits8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int CG> const void* tc_kernel(bool bits8, bool arow, bool brow) {
+    constexpr int BN = 128 * CG;
+    if (bits8) return (const void*)gemm_tc_kernel<CG, BN, true, false, false>;
+    if (arow) return (const void*)gemm_tc_kernel<CG, BN, false, true, true>;
+    return brow ? (const void*)gemm_tc_kernel<CG, BN, false, false, true> : (const void*)gemm_tc_kernel<CG, BN, false, false, false>;
+}
+
+}  // namespace
+
+size_t gemm_partial_bytes(long long M, int N, long long K, bool bits8) {
+    if (K == 0) return 0;
+    const TcPlan p = tc_plan(M, N, K, bits8);
+    return p.splits > 1 ? align_up((size_t)p.splits * M * N * 4, 256) : 0;
+}
+
+vmb_status launch_gemm_tc(const GemmProblem& p, bool bits8, float* partial, unsigned* err, cudaStream_t stream, bool* taken) {
+    *taken = false;
+    if (p.K < 1 || p.K > (1 << 30) || p.M > (1 << 30)) return VMB_OK;
+    const TcPlan plan = tc_plan(p.M, p.N, p.K, bits8);
+    if ((long long)plan.tiles_m * plan.tiles_n * plan.splits > (1 << 30)) return VMB_OK;
+    TcKernel k;
+    bool arow = false, brow = false;
+    if (!encode(&k.ta, p.A, p.M, p.K, p.a_r, p.a_c, bits8, &arow) || !encode(&k.tb, p.B, p.N, p.K, p.b_r, p.b_c, bits8, &brow) || (arow && !brow)) return VMB_OK;
+    k.e = p.e, k.partial = partial, k.err = err, k.M = p.M, k.N = p.N;
+    k.tiles_m = plan.tiles_m, k.tiles_n = plan.tiles_n, k.splits = plan.splits, k.kblocks = plan.kblocks, k.kper = plan.kper;
+    k.units = plan.tiles_m * plan.tiles_n * plan.splits;
+    k.vec = epilogue_vectors(p);
+    const void* fn = plan.cg == 2 ? tc_kernel<2>(bits8, arow, brow) : tc_kernel<1>(bits8, arow, brow);
+    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem) != cudaSuccess) return VMB_ERR_CUDA;
+    const int slots = device_sm_count() / plan.cg;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)((k.units < slots ? k.units : slots) * plan.cg));
+    cfg.blockDim = dim3(kTcThreads);
+    cfg.dynamicSmemBytes = kTcSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = plan.cg, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr, cfg.numAttrs = plan.cg == 2 ? 2 : 1;
+    void* args[] = {&k};
+    *taken = true;
+    if (cudaLaunchKernelExC(&cfg, fn, args) != cudaSuccess) return VMB_ERR_CUDA;
+    if (plan.splits == 1) return VMB_OK;
+    GemmEpilogue e = p.e;
+    const float* parts = partial;
+    int splits = plan.splits, N = p.N;
+    long long M = p.M;
+    void* jargs[] = {&e, &parts, &splits, &M, &N};
+    const long long items = M * (k.vec ? up(N, 8) : N);
+    const void* join = k.vec ? (const void*)gemm_join_kernel<8> : (const void*)gemm_join_kernel<1>;
+    return launch_kernel(join, dim3((unsigned)up(items, 256)), dim3(256), 0, jargs, stream) == cudaSuccess ? VMB_OK : VMB_ERR_CUDA;
+}
+
+}  // namespace vmb

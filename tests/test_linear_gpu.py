@@ -44,6 +44,8 @@ def product(x, w, bias, act, residual, xs=None, ws=None):
     return (y if residual is None else y + residual.double()), z
 
 
+# many tiles for each SM, with ragged edges
+LARGE = [(2500, 200, 2600), (4096, 64, 2056), (1025, 1032, 5000), (3000, 2048, 2304)]
 SIZES = [(1, 64, 64), (1, 200, 104), (2, 512, 8), (3, 72, 136), (7, 256, 300), (8, 128, 77), (16, 512, 256), (17, 96, 129), (32, 264, 200), (33, 64, 64),
          (64, 512, 256), (100, 136, 333), (128, 128, 256), (129, 192, 257), (200, 1024, 520), (256, 64, 512), (300, 320, 264), (513, 80, 1000), (1, 1, 1),
          (5, 3, 7), (70, 33, 50), (128, 1100, 40), (1000, 16, 24), (2, 0, 5)]
@@ -66,6 +68,26 @@ def test_bf16(vmb, M, K, N, act, bias, residual):
     close(y, want, K)
     close(pre, z, K)
     assert torch.equal(vmb.vmb_linear_fwd(x, w, b, act=act, residual=res)[0], y)
+
+
+@pytest.mark.parametrize("M,K,N", LARGE)
+def test_many_tiles(vmb, M, K, N):
+    r = rand(M + K + N)
+    x, w, b, res, dy = r(M, K).to(BF16), (r(N, K) / K ** 0.5).to(BF16), r(N), r(M, N).to(BF16), r(M, N).to(BF16)
+    y, pre = vmb.vmb_linear_fwd(x, w, b, act="gelu", residual=res, want_pre=True)
+    want, z = product(x, w, b, "gelu", res)
+    close(y, want, K)
+    close(pre, z, K)
+    (x8, xs), (w8, ws) = eight(r(M, K // 16 * 16)), eight(r(N, K // 16 * 16) / K ** 0.5)
+    close(vmb.vmb_linear_fwd(x8, w8, b, act="silu", x_scale=xs, weight_scale=ws)[0], product(x8, w8, b, "silu", None, xs, ws)[0], K)
+    if N % 8 == 0:
+        d = vmb.vmb_linear_bwd(x, w, dy, want_bias=True)
+        assert ref.rel(d["x"], dy.double() @ w.double()) <= tol(N) and ref.rel(d["weight"], dy.double().t() @ x.double()) <= tol(M)
+        # a mistake in one tile: no element is off by more than its rounding and a sum's 2^-20 of its terms (dx: N terms of 1 / sqrt(K); dweight: M of one)
+        dx, dw = dy.double() @ w.double(), dy.double().t() @ x.double()
+        assert ((d["x"].double() - dx).abs() <= 2.0 ** -8 * dx.abs() + N * 2.0 ** -20).all()
+        assert ((d["weight"].double() - dw).abs() <= 2.0 ** -8 * dw.abs() + M * 2.0 ** -20).all()
+    assert vmb.vmb_read_status(vmb.layer_workspace()) == vmb.VMB_OK
 
 
 @pytest.mark.parametrize("M,K,N", [s for s in SIZES if s[1]])
