@@ -31,37 +31,51 @@ __device__ __forceinline__ float act_of(float z, int act) {
 __device__ __forceinline__ float slope_of(float z, int act) {
     return act == VMB_ACT_SILU ? activate_slope<VMB_ACT_SILU>(z) : act == VMB_ACT_GELU ? activate_slope<VMB_ACT_GELU>(z) : 1.0f;
 }
-template <int ACT, int V> __device__ __forceinline__ void activate_all(float (&v)[V]) {
+// The factors and the bias of V columns from n on.
+template <int V> struct ColumnTerms {
+    float scale[V], bias[V];
+    __device__ __forceinline__ void load(const GemmEpilogue& e, int n) {
+        const auto take = [n](float (&v)[V], const float* p, float other) {
+            if (p && V == 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+                const float4 a = *reinterpret_cast<const float4*>(p + n), b = *reinterpret_cast<const float4*>(p + n + V / 2);
+                const float all[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = activate<ACT>(v[i]);
-}
-
-// V sums of row m from column n on, all in range and 16-byte aligned (V 8) or one.
-template <int V> __device__ __forceinline__ void finish(const GemmEpilogue& e, float (&v)[V], const float (&scale)[V], const float (&bias)[V], float row_scale,
-                                                        long long at) {
-    if (e.row_scale) {
+                for (int i = 0; i < V; ++i) v[i] = all[i];
+            } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = v[i] * (row_scale * scale[i]);
+                for (int i = 0; i < V; ++i) v[i] = p ? p[n + i] : other;
+            }
+        };
+        take(scale, e.col_scale, 1.0f);
+        take(bias, e.bias, 0.0f);
     }
+};
+
+template <int ACT> __device__ __forceinline__ void activate_all(float (&v)[8]) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] += bias[i];
+    for (int i = 0; i < 8; i += 2) {
+        const float2 y = activate2<ACT>(make_float2(v[i], v[i + 1]));
+        v[i] = y.x, v[i + 1] = y.y;
+    }
+}
+template <int ACT> __device__ __forceinline__ void activate_all(float (&v)[1]) { v[0] = activate<ACT>(v[0]); }
+
+// The sums of V columns of a row (8: in range, 16-byte aligned): the output is at `at`; `residual` holds the residual's values there.
+template <int V>
+__device__ __forceinline__ void finish(const GemmEpilogue& e, float (&v)[V], const ColumnTerms<V>& t, float row_scale, const Vec<__nv_bfloat16, V>& residual, long long at) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = e.row_scale ? fmaf(v[i], row_scale * t.scale[i], t.bias[i]) : v[i] + t.bias[i];
     if (e.pre) store_vec<__nv_bfloat16, V>(e.pre + at, v);
-    if (e.act == VMB_ACT_SILU) activate_all<VMB_ACT_SILU, V>(v);
-    else if (e.act == VMB_ACT_GELU) activate_all<VMB_ACT_GELU, V>(v);
+    if (e.act == VMB_ACT_SILU) activate_all<VMB_ACT_SILU>(v);
+    else if (e.act == VMB_ACT_GELU) activate_all<VMB_ACT_GELU>(v);
     if (e.residual) {
-        float r[V];
-        load_vec<__nv_bfloat16, V>(r, e.residual + at);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] += r[i];
+        for (int i = 0; i < V; ++i) v[i] += __bfloat162float(residual.v[i]);
     }
     store_vec<__nv_bfloat16, V>(e.out + at, v);
 }
-template <int V> __device__ __forceinline__ void column_terms(const GemmEpilogue& e, int n, float (&scale)[V], float (&bias)[V]) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        scale[i] = e.col_scale ? e.col_scale[n + i] : 1.0f;
-        bias[i] = e.bias ? e.bias[n + i] : 0.0f;
-    }
+template <int V> __device__ __forceinline__ Vec<__nv_bfloat16, V> residual_at(const GemmEpilogue& e, long long at) {
+    return e.residual ? *reinterpret_cast<const Vec<__nv_bfloat16, V>*>(e.residual + at) : Vec<__nv_bfloat16, V>{};
 }
 // Rows of vectors of eight bf16: out, pre and residual may be read and written in 16 bytes.
 inline bool epilogue_vectors(const GemmProblem& p) {

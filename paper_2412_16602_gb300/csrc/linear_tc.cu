@@ -117,6 +117,7 @@ __device__ __forceinline__ bool tc_wait(uint32_t bar, uint32_t parity, unsigned*
     }
 }
 
+// 32 columns of the warp's 32 lanes; they are there after tmem_wait32.
 __device__ __forceinline__ void tmem_load32(uint32_t (&r)[32], uint32_t addr) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,"
@@ -125,7 +126,14 @@ __device__ __forceinline__ void tmem_load32(uint32_t (&r)[32], uint32_t addr) {
           "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]),
           "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(addr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_wait32(uint32_t (&r)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
+                   "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]),
+                   "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+                 :
+                 : "memory");
 }
 
 struct TcUnit {
@@ -232,18 +240,40 @@ template <int CG, int BN, bool kBits8, bool kArow, bool kBrow> __global__ void _
     } else {  // sums: 32 rows and half of the columns for each warp
         const int quad = warp & 3, half = (warp - 2) >> 2;
         char* stage = smem_raw + (base - smem_u32(smem_raw)) + kTcStages * kTcStage + (warp - 2) * 4096;
+        const int low = lane >> 2, col8 = (lane & 3) * 8;  // after the turn: rows low + 8 i, eight columns from col8
         uint32_t buf = 0, bphase = 0;
         for (int u = first; u < k.units; u += step) {
             const TcUnit t = tc_unit(k, u);
-            const long long m0 = (long long)t.m * 128 * CG + rank * 128 + quad * 32;
+            const long long m0 = (long long)t.m * 128 * CG + rank * 128 + quad * 32 + low;
+            const int ncol = t.n * BN + half * (BN / 2) + col8;
+            float rs[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) rs[i] = k.e.row_scale && m0 + 8 * i < k.M ? k.e.row_scale[m0 + 8 * i] : 1.0f;
             if (!tc_wait(sums_full + 8 * buf, bphase, k.err, kTcSumsNs)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t sums = tmem + buf * BN + half * (BN / 2) + ((uint32_t)(quad * 32) << 16);
+            uint32_t r[32];
+            tmem_load32(r, sums);
 #pragma unroll 1
             for (int c = 0; c < BN / 2; c += 32) {
-                uint32_t r[32];
-                const int col = half * (BN / 2) + c;
-                tmem_load32(r, tmem + buf * BN + col + ((uint32_t)(quad * 32) << 16));
-                if (c + 32 == BN / 2) {  // the buffer may be used again
+                const int n = ncol + c;
+                const bool whole = k.vec && n < k.N && k.splits == 1;
+                ColumnTerms<8> terms;
+                Vec<__nv_bfloat16, 8> residual[4];
+                if (whole) {  // on their way while the sums are turned
+                    terms.load(k.e, n);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (m0 + 8 * i < k.M) residual[i] = residual_at<8>(k.e, (m0 + 8 * i) * k.N + n);
+                }
+                tmem_wait32(r);
+                // from a row in each lane to eight columns of a row in each: pieces of 16 bytes, turned by the row so that neither side has conflicts
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    *reinterpret_cast<uint4*>(stage + lane * 128 + ((q ^ (lane & 7)) << 4)) = make_uint4(r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]);
+                if (c + 32 < BN / 2) {
+                    tmem_load32(r, sums + c + 32);
+                } else {  // the buffer may be used again
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) {
@@ -253,50 +283,35 @@ template <int CG, int BN, bool kBits8, bool kArow, bool kBrow> __global__ void _
                             mbarrier_arrive(sums_empty + 8 * buf);
                     }
                 }
-                const int n0 = t.n * BN + col;
-                if (n0 >= k.N) continue;
-                // from a row in each lane to eight columns of a row in each: pieces of 16 bytes, turned by the row so that neither side has conflicts
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    *reinterpret_cast<uint4*>(stage + lane * 128 + ((q ^ (lane & 7)) << 4)) = make_uint4(r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]);
                 __syncwarp();
-                const int n = n0 + (lane & 3) * 8;
-                float scale[8], bias[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    scale[i] = k.e.col_scale && n + i < k.N ? k.e.col_scale[n + i] : 1.0f;
-                    bias[i] = k.e.bias && n + i < k.N ? k.e.bias[n + i] : 0.0f;
-                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int row = (lane >> 2) + 8 * i, u0 = (lane & 3) * 2;
-                    const long long m = m0 + row;
-                    const float4 x = *reinterpret_cast<const float4*>(stage + row * 128 + ((u0 ^ (row & 7)) << 4));
-                    const float4 y = *reinterpret_cast<const float4*>(stage + row * 128 + (((u0 + 1) ^ (row & 7)) << 4));
+                    const int row = low + 8 * i, u0 = (lane & 3) * 2;
+                    const long long m = m0 + 8 * i, at = m * k.N + n;
+                    float v[8];
+                    *reinterpret_cast<float4*>(&v[0]) = *reinterpret_cast<const float4*>(stage + row * 128 + ((u0 ^ (row & 7)) << 4));
+                    *reinterpret_cast<float4*>(&v[4]) = *reinterpret_cast<const float4*>(stage + row * 128 + (((u0 + 1) ^ (row & 7)) << 4));
                     if (m >= k.M || n >= k.N) continue;
-                    float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-                    const long long at = m * k.N + n;
-                    if (k.splits > 1) {
+                    if (whole) {
+                        finish<8>(k.e, v, terms, rs[i], residual[i], at);
+                    } else if (k.splits > 1) {
                         float* p = k.partial + (long long)t.split * k.M * k.N + at;
                         if (k.vec) {
-                            *reinterpret_cast<float4*>(p) = x;
-                            *reinterpret_cast<float4*>(p + 4) = y;
+                            *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+                            *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
                         } else {
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
                                 if (n + j < k.N) p[j] = v[j];
                         }
-                        continue;
-                    }
-                    const float rs = k.e.row_scale ? k.e.row_scale[m] : 1.0f;
-                    if (k.vec) {
-                        finish<8>(k.e, v, scale, bias, rs, at);
                     } else {
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
+                            if (n + j >= k.N) break;
                             float one[1] = {v[j]};
-                            const float s1[1] = {scale[j]}, b1[1] = {bias[j]};
-                            if (n + j < k.N) finish<1>(k.e, one, s1, b1, rs, at + j);
+                            ColumnTerms<1> t1;
+                            t1.load(k.e, n + j);
+                            finish<1>(k.e, one, t1, rs[i], residual_at<1>(k.e, at + j), at + j);
                         }
                     }
                 }
@@ -327,22 +342,21 @@ template <int V> __global__ void __launch_bounds__(256) gemm_join_kernel(GemmEpi
     const long long m = item / per;
     const int n = (int)(item - m * per) * V;
     const long long at = m * N + n;
-    float v[V], scale[V], bias[V];
+    ColumnTerms<V> terms;
+    terms.load(e, n);
+    const Vec<__nv_bfloat16, V> residual = residual_at<V>(e, at);
+    float v[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = 0.0f;
+#pragma unroll 4
     for (int s = 0; s < splits; ++s) {
         float p[V];
-        if constexpr (V == 8) {
-            const float4 x = *reinterpret_cast<const float4*>(partial + (long long)s * M * N + at), y = *reinterpret_cast<const float4*>(partial + (long long)s * M * N + at + 4);
-            p[0] = x.x, p[1] = x.y, p[2] = x.z, p[3] = x.w, p[4] = y.x, p[5] = y.y, p[6] = y.z, p[7] = y.w;
-        } else {
-            p[0] = partial[(long long)s * M * N + at];
-        }
+        load_vec<float, (V < 4 ? V : 4)>(*reinterpret_cast<float(*)[V < 4 ? V : 4]>(&p[0]), partial + (long long)s * M * N + at);
+        if constexpr (V == 8) load_vec<float, 4>(*reinterpret_cast<float(*)[4]>(&p[4]), partial + (long long)s * M * N + at + 4);
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] += p[i];
     }
-    column_terms<V>(e, n, scale, bias);
-    finish<V>(e, v, scale, bias, e.row_scale ? e.row_scale[m] : 1.0f, at);
+    finish<V>(e, v, terms, e.row_scale ? e.row_scale[m] : 1.0f, residual, at);
 }
 
 struct TcPlan {
