@@ -18,10 +18,11 @@ namespace vmb {
 
 namespace {
 
-constexpr int kTcThreads = 320, kTcStages = 6, kTcEpiWarps = 8;
+constexpr int kTcEpiWarps = 8, kTcThreads = 32 * (2 + kTcEpiWarps), kTcStages = 5;
 constexpr int kTcA = 128 * 128;  // bytes of A in a stage, and of B: 128 rows of 128 bytes of the contraction
 constexpr int kTcStage = 2 * kTcA;
-constexpr int kTcSmem = 1024 + kTcStages * kTcStage + kTcEpiWarps * 4096;
+constexpr int kTcEpiBytes = 4096 + 1024;  // of each warp of the epilogue: 32 x 64 outputs on their way, factors and biases of 128 columns
+constexpr int kTcSmem = 1024 + kTcStages * kTcStage + kTcEpiWarps * kTcEpiBytes;
 
 struct TcKernel {
     CUtensorMap ta, tb;
@@ -150,6 +151,118 @@ __device__ __forceinline__ TcUnit tc_unit(const TcKernel& k, int u) {
     return t;
 }
 
+// The rows and columns that a warp has of a unit; a lane's row.
+struct TcRows {
+    int m0, n0, split;
+    bool on;
+    long long at;  // of the row's first column in the output
+    float scale;
+};
+
+template <int ACT> __device__ __forceinline__ void activate_pairs(float2 (&v)[16]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = activate2<ACT>(v[i]);
+}
+__device__ __forceinline__ uint32_t bf16_pair(float2 v) {
+    const __nv_bfloat162 p = __float22bfloat162_rn(v);
+    return *reinterpret_cast<const uint32_t*>(&p);
+}
+
+// The sums of 32 columns of a lane's row, from column c of its warp's on, with their factors and bias.
+template <int COLS> __device__ __forceinline__ void tc_scale(const TcKernel& k, float2 (&v)[16], const TcRows& t, int c, const uint32_t (&r)[32], const float* terms) {
+    const float2 rs = make_float2(t.scale, t.scale);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        const float4 b = *reinterpret_cast<const float4*>(terms + COLS + c + 4 * q);
+        v[2 * q] = make_float2(__uint_as_float(r[4 * q]), __uint_as_float(r[4 * q + 1]));
+        v[2 * q + 1] = make_float2(__uint_as_float(r[4 * q + 2]), __uint_as_float(r[4 * q + 3]));
+        if (k.e.row_scale) {
+            const float4 f = *reinterpret_cast<const float4*>(terms + c + 4 * q);
+            v[2 * q] = __ffma2_rn(v[2 * q], __fmul2_rn(make_float2(f.x, f.y), rs), make_float2(b.x, b.y));
+            v[2 * q + 1] = __ffma2_rn(v[2 * q + 1], __fmul2_rn(make_float2(f.z, f.w), rs), make_float2(b.z, b.w));
+        } else {
+            v[2 * q] = __fadd2_rn(v[2 * q], make_float2(b.x, b.y));
+            v[2 * q + 1] = __fadd2_rn(v[2 * q + 1], make_float2(b.z, b.w));
+        }
+    }
+}
+// A part's sums as they are.
+__device__ __forceinline__ void tc_part(const TcKernel& k, const TcRows& t, int c, const uint32_t (&r)[32]) {
+    const int n = t.n0 + c;
+    float* p = k.partial + (long long)t.split * k.M * k.N + t.at + c;
+    if (!t.on) return;
+    if (k.vec) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (n + 4 * q < k.N) reinterpret_cast<uint4*>(p)[q] = make_uint4(r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (n + j < k.N) p[j] = __uint_as_float(r[j]);
+    }
+}
+// Shared memory: 32 rows of 64 outputs, in pieces of 16 bytes turned by the row: neither a lane for each row nor eight lanes for a row have conflicts.
+__device__ __forceinline__ uint4* tc_piece(char* stage, int row, int piece) { return reinterpret_cast<uint4*>(stage + row * 128 + ((piece ^ (row & 7)) << 4)); }
+// To (kStore) or from the output's (residual's) rows, eight lanes to a row; n: the first of the 64 columns.
+template <bool kStore> __device__ __forceinline__ void tc_rows(const TcKernel& k, __nv_bfloat16* p, const TcRows& t, int n, char* stage) {
+    const int lane = threadIdx.x & 31, low = lane >> 3, piece = lane & 7;
+    if (n + 8 * piece >= k.N) return;
+    p += (long long)(t.m0 + low) * k.N + n + 8 * piece;
+    if constexpr (kStore) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (t.m0 + low + 4 * i < k.M) *reinterpret_cast<uint4*>(p + (long long)(4 * i) * k.N) = *tc_piece(stage, low + 4 * i, piece);
+    } else {
+        uint4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (t.m0 + low + 4 * i < k.M) v[i] = *reinterpret_cast<const uint4*>(p + (long long)(4 * i) * k.N);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) *tc_piece(stage, low + 4 * i, piece) = v[i];
+    }
+}
+// The epilogue of 32 columns of a lane's row, from column c of its warp's on; where the output's rows allow 16 bytes it is left in shared memory, where
+// the residual is.
+__device__ __forceinline__ void tc_finish(const TcKernel& k, const TcRows& t, int c, float2 (&v)[16], char* stage) {
+    const int n = t.n0 + c, lane = threadIdx.x & 31, first = (c & 32) / 8;
+    const long long at = t.at + c;
+    if (k.e.pre && t.on) {
+        if (k.vec) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (n + 8 * q < k.N)
+                    reinterpret_cast<uint4*>(k.e.pre + at)[q] = make_uint4(bf16_pair(v[4 * q]), bf16_pair(v[4 * q + 1]), bf16_pair(v[4 * q + 2]), bf16_pair(v[4 * q + 3]));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (n + j < k.N) k.e.pre[at + j] = __float2bfloat16_rn(j & 1 ? v[j / 2].y : v[j / 2].x);
+        }
+    }
+    if (k.e.act == VMB_ACT_SILU) activate_pairs<VMB_ACT_SILU>(v);
+    else if (k.e.act == VMB_ACT_GELU) activate_pairs<VMB_ACT_GELU>(v);
+    if (!k.vec) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (t.on && n + j < k.N) {
+                float y = j & 1 ? v[j / 2].y : v[j / 2].x;
+                if (k.e.residual) y += __bfloat162float(k.e.residual[at + j]);
+                k.e.out[at + j] = __float2bfloat16_rn(y);
+            }
+        return;
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        uint4* p = tc_piece(stage, lane, first + q);
+        if (k.e.residual) {
+            const uint4 r = *p;
+            const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[4 * q + j] = __fadd2_rn(v[4 * q + j], make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u)));
+        }
+        *p = make_uint4(bf16_pair(v[4 * q]), bf16_pair(v[4 * q + 1]), bf16_pair(v[4 * q + 2]), bf16_pair(v[4 * q + 3]));
+    }
+}
+
 template <int CG, int BN, bool kBits8, bool kArow, bool kBrow> __global__ void __launch_bounds__(kTcThreads, 1) gemm_tc_kernel(const __grid_constant__ TcKernel k) {
     static_assert(BN == 128 * CG, "128 rows of B in each CTA");
     constexpr int kCols = 2 * BN, kElems = kBits8 ? 128 : 64;  // columns of tensor memory; elements of the contraction in a stage
@@ -237,41 +350,52 @@ template <int CG, int BN, bool kBits8, bool kArow, bool kBrow> __global__ void _
                 if (buf == 0) bphase ^= 1;
             }
         }
-    } else {  // sums: 32 rows and half of the columns for each warp
-        const int quad = warp & 3, half = (warp - 2) >> 2;
-        char* stage = smem_raw + (base - smem_u32(smem_raw)) + kTcStages * kTcStage + (warp - 2) * 4096;
-        const int low = lane >> 2, col8 = (lane & 3) * 8;  // after the turn: rows low + 8 i, eight columns from col8
+    } else {  // sums: 32 rows, one in each lane, and half of the columns for each warp
+        constexpr int COLS = BN / 2;
+        const int quad = warp & 3, part = (warp - 2) >> 2;
+        char* stage = smem_raw + (base - smem_u32(smem_raw)) + kTcStages * kTcStage + (warp - 2) * kTcEpiBytes;
+        float* terms = reinterpret_cast<float*>(stage + 4096);  // of the warp's columns: factors, biases
         uint32_t buf = 0, bphase = 0;
         for (int u = first; u < k.units; u += step) {
             const TcUnit t = tc_unit(k, u);
-            const long long m0 = (long long)t.m * 128 * CG + rank * 128 + quad * 32 + low;
-            const int ncol = t.n * BN + half * (BN / 2) + col8;
-            float rs[4];
+            TcRows at;
+            at.m0 = t.m * 128 * CG + (int)rank * 128 + quad * 32;
+            at.n0 = t.n * BN + part * COLS;
+            at.split = t.split;
+            const int m = at.m0 + lane;
+            at.on = m < k.M;
+            at.at = (long long)m * k.N + at.n0;
+            at.scale = k.e.row_scale && at.on ? k.e.row_scale[m] : 1.0f;
+            __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) rs[i] = k.e.row_scale && m0 + 8 * i < k.M ? k.e.row_scale[m0 + 8 * i] : 1.0f;
+            for (int j = lane; j < COLS; j += 32) {
+                const bool in = at.n0 + j < k.N;
+                terms[j] = in && k.e.col_scale ? k.e.col_scale[at.n0 + j] : 1.0f;
+                terms[COLS + j] = in && k.e.bias ? k.e.bias[at.n0 + j] : 0.0f;
+            }
+            __syncwarp();
             if (!tc_wait(sums_full + 8 * buf, bphase, k.err, kTcSumsNs)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t sums = tmem + buf * BN + half * (BN / 2) + ((uint32_t)(quad * 32) << 16);
+            const uint32_t sums = tmem + buf * BN + part * COLS + ((uint32_t)(quad * 32) << 16);
+            const bool whole = k.vec && k.splits == 1 && at.m0 < k.M;
             uint32_t r[32];
             tmem_load32(r, sums);
 #pragma unroll 1
-            for (int c = 0; c < BN / 2; c += 32) {
-                const int n = ncol + c;
-                const bool whole = k.vec && n < k.N && k.splits == 1;
-                ColumnTerms<8> terms;
-                Vec<__nv_bfloat16, 8> residual[4];
-                if (whole) {  // on their way while the sums are turned
-                    terms.load(k.e, n);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (m0 + 8 * i < k.M) residual[i] = residual_at<8>(k.e, (m0 + 8 * i) * k.N + n);
+            for (int c = 0; c < COLS; c += 32) {
+                const int n = at.n0 + c;
+                const bool in = n < k.N && at.m0 < k.M;
+                if (whole && k.e.residual && !(c & 32)) {
+                    tc_rows<false>(k, const_cast<__nv_bfloat16*>(k.e.residual), at, n, stage);
+                    __syncwarp();
                 }
+                float2 v[16];
                 tmem_wait32(r);
-                // from a row in each lane to eight columns of a row in each: pieces of 16 bytes, turned by the row so that neither side has conflicts
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    *reinterpret_cast<uint4*>(stage + lane * 128 + ((q ^ (lane & 7)) << 4)) = make_uint4(r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]);
-                if (c + 32 < BN / 2) {
+                if (k.splits > 1) {
+                    if (in) tc_part(k, at, c, r);
+                } else {
+                    tc_scale<COLS>(k, v, at, c, r, terms);
+                }
+                if (c + 32 < COLS) {
                     tmem_load32(r, sums + c + 32);
                 } else {  // the buffer may be used again
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -283,39 +407,12 @@ template <int CG, int BN, bool kBits8, bool kArow, bool kBrow> __global__ void _
                             mbarrier_arrive(sums_empty + 8 * buf);
                     }
                 }
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int row = low + 8 * i, u0 = (lane & 3) * 2;
-                    const long long m = m0 + 8 * i, at = m * k.N + n;
-                    float v[8];
-                    *reinterpret_cast<float4*>(&v[0]) = *reinterpret_cast<const float4*>(stage + row * 128 + ((u0 ^ (row & 7)) << 4));
-                    *reinterpret_cast<float4*>(&v[4]) = *reinterpret_cast<const float4*>(stage + row * 128 + (((u0 + 1) ^ (row & 7)) << 4));
-                    if (m >= k.M || n >= k.N) continue;
-                    if (whole) {
-                        finish<8>(k.e, v, terms, rs[i], residual[i], at);
-                    } else if (k.splits > 1) {
-                        float* p = k.partial + (long long)t.split * k.M * k.N + at;
-                        if (k.vec) {
-                            *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-                            *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                if (n + j < k.N) p[j] = v[j];
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            if (n + j >= k.N) break;
-                            float one[1] = {v[j]};
-                            ColumnTerms<1> t1;
-                            t1.load(k.e, n + j);
-                            finish<1>(k.e, one, t1, rs[i], residual_at<1>(k.e, at + j), at + j);
-                        }
-                    }
+                if (k.splits == 1 && in) tc_finish(k, at, c, v, stage);
+                if (whole && (c & 32)) {
+                    __syncwarp();
+                    tc_rows<true>(k, k.e.out, at, n - 32, stage);
+                    __syncwarp();
                 }
-                __syncwarp();
             }
             buf ^= 1;
             if (buf == 0) bphase ^= 1;
