@@ -13,21 +13,26 @@ namespace vmb {
 // 1 / (1 + e^-z): e^-z overflows to infinity, whose reciprocal is the limit.
 __device__ __forceinline__ float logistic(float z) { return rcp(1.0f + ex2(-z * kLog2e)); }
 
-// The normal distribution's tail: Phi(-a) = e^(-a^2 / 2) m(a) for a >= 0, m(a) = t (p0 + p1 t + .. + p4 t^4) with t = 1 / (1 + 0.38 a),
-// the p by linear programming for the least relative error over [0, 14]: 3.6e-5, and it keeps that where Phi is small (beyond 14
-// e^(-a^2 / 2) is below the smallest float).
-// For outputs in bf16.
-constexpr float kTailC = 0.38f, kTail0 = 0.15122510492801666f, kTail1 = 0.15782970190048218f, kTail2 = 0.09197915345430374f,
-                kTail3 = 0.18887709081172943f, kTail4 = -0.08992857486009598f, kGaussLog2 = -0.5f * kLog2e;
-__device__ __forceinline__ float normal_tail(float a, float e) {
-    const float t = rcp(fmaf(kTailC, a, 1.0f));
-    return e * (t * fmaf(fmaf(fmaf(fmaf(kTail4, t, kTail3), t, kTail2), t, kTail1), t, kTail0));
+// The normal distribution's tail as a power of two: log2 Phi(b) for b in [-13.2, 0] is a polynomial of degree eight in b, by linear programming
+// for the least error, 1.8e-4 of its power (with the coefficients and sums in fp32 1.5e-4): Phi keeps 12 bits also where it is small.  Below
+// -13.2 it is less than the smallest float.  For outputs in bf16; one exponential, where a quotient of polynomials takes a reciprocal too.
+constexpr float kTailEnd = -13.2f, kTail0 = -1.0001838207244873f, kTail1 = 1.1490356922149658f, kTail2 = -0.4627901613712311f, kTail3 = 0.05079496651887894f,
+                kTail4 = 0.00741631118580699f, kTail5 = 0.0007434896542690694f, kTail6 = 4.7549950977554545e-05f, kTail7 = 1.7312547697656555e-06f, kTail8 = 2.716298652671867e-08f;
+__device__ __forceinline__ float relu(float z) {  // NaN stays
+    float y;
+    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(z));
+    return y;
 }
 
 template <int ACT> __device__ __forceinline__ float activate(float z) {
     if constexpr (ACT == VMB_ACT_SILU) return z * logistic(z);
     // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
-    if constexpr (ACT == VMB_ACT_GELU) return fmaf(-fabsf(z), normal_tail(fabsf(z), ex2(kGaussLog2 * z * z)), fmaxf(z, 0.0f));
+    if constexpr (ACT == VMB_ACT_GELU) {
+        const float b = fmaxf(-fabsf(z), kTailEnd);
+        float p = fmaf(kTail8, b, kTail7);
+        p = fmaf(fmaf(fmaf(fmaf(p, b, kTail6), b, kTail5), b, kTail4), b, kTail3);
+        return fmaf(ex2(fmaf(fmaf(fmaf(p, b, kTail2), b, kTail1), b, kTail0)), b, relu(z));
+    }
     return z;
 }
 template <int ACT> __device__ __forceinline__ float activate_slope(float z) {
@@ -36,7 +41,7 @@ template <int ACT> __device__ __forceinline__ float activate_slope(float z) {
         return s * fmaf(z, 1.0f - s, 1.0f);
     }
     // Phi(z) + z phi(z): its terms cancel for z < 0, and sums of it are kept in fp32
-    if constexpr (ACT == VMB_ACT_GELU) return fmaf(z * 0.39894228040143268f, ex2(kGaussLog2 * z * z), 0.5f * erfcf(-0.70710678118654752f * z));
+    if constexpr (ACT == VMB_ACT_GELU) return fmaf(z * 0.39894228040143268f, ex2(-0.5f * kLog2e * z * z), 0.5f * erfcf(-0.70710678118654752f * z));
     return 1.0f;
 }
 // Two values at once, in packed arithmetic.
@@ -47,14 +52,16 @@ template <int ACT> __device__ __forceinline__ float2 activate2(float2 z) {
         return __fmul2_rn(z, make_float2(rcp(d.x), rcp(d.y)));
     }
     if constexpr (ACT == VMB_ACT_GELU) {
-        const float2 a = make_float2(fabsf(z.x), fabsf(z.y)), d = __ffma2_rn(a, all(kTailC), all(1.0f)), t = make_float2(rcp(d.x), rcp(d.y));
-        const float2 q = __fmul2_rn(__fmul2_rn(z, all(kGaussLog2)), z);
-        float2 p = __ffma2_rn(t, all(kTail4), all(kTail3));
-        p = __ffma2_rn(p, t, all(kTail2));
-        p = __ffma2_rn(p, t, all(kTail1));
-        p = __ffma2_rn(p, t, all(kTail0));
-        p = __fmul2_rn(__fmul2_rn(p, t), make_float2(ex2(q.x), ex2(q.y)));
-        return __ffma2_rn(__fmul2_rn(p, all(-1.0f)), a, make_float2(fmaxf(z.x, 0.0f), fmaxf(z.y, 0.0f)));
+        const float2 b = make_float2(fmaxf(-fabsf(z.x), kTailEnd), fmaxf(-fabsf(z.y), kTailEnd));
+        float2 p = __ffma2_rn(b, all(kTail8), all(kTail7));
+        p = __ffma2_rn(p, b, all(kTail6));
+        p = __ffma2_rn(p, b, all(kTail5));
+        p = __ffma2_rn(p, b, all(kTail4));
+        p = __ffma2_rn(p, b, all(kTail3));
+        p = __ffma2_rn(p, b, all(kTail2));
+        p = __ffma2_rn(p, b, all(kTail1));
+        p = __ffma2_rn(p, b, all(kTail0));
+        return __ffma2_rn(make_float2(ex2(p.x), ex2(p.y)), b, make_float2(relu(z.x), relu(z.y)));
     }
     return z;
 }

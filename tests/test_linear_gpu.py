@@ -171,6 +171,15 @@ def test_what_is_not_finite_stays_in_its_row(vmb):
         close(y[rest], product(x[rest], w, None, "none", None)[0], 128 * 16)  # (weights of order one: sums of order 2^3.5)
 
 
+def test_activations_of_what_is_not_finite(vmb):
+    bias = torch.tensor([float("inf"), float("-inf"), float("nan"), 0.0, -300.0, 300.0, -0.0, 3.0], device="cuda")
+    for M in (1, 40, 200):
+        x, w = torch.zeros(M, 8, device="cuda", dtype=BF16), torch.zeros(8, 8, device="cuda", dtype=BF16)
+        for act in ("silu", "gelu"):
+            y = vmb.vmb_linear_fwd(x, w, bias, act=act)[0].float()
+            assert (y[:, 0] == float("inf")).all() and y[:, 2].isnan().all() and not y[:, [3, 4, 6]].any() and (y[:, 5] == 300).all(), act
+
+
 def test_empty(vmb):
     r = rand(9)
     assert vmb.vmb_linear_fwd(r(0, 8).to(BF16), r(4, 8).to(BF16))[0].shape == (0, 4)
