@@ -12,124 +12,165 @@ namespace vmb {
 
 namespace {
 
-constexpr int kTok = 32;  // tokens of a stage
+// Two lanes hold the states of a channel, so that a warp has 16 channels and a CTA the 64 of a tile.  A lane of the pair reads and prepares
+// one token of every two (step size, its product with x, skip, gate), in blocks of 16 tokens whose values were asked for a block
+// before, and hands them to the other by shuffles.  B and C of 32 tokens are in shared memory in fp32.
+constexpr int kFwdThreads = 2 * kScanCh, kTok = 32, kBlk = 16, kMine = kBlk / 2;
 
-template <typename T, int NP> struct ScanSmem {
-    static constexpr int array = kTok * scan_pitch<T>(), slot = 3 * array, bc = kTok * 2 * NP * 4;
-    static constexpr int bytes = 2 * slot + 2 * bc;
-};
-
-template <typename T, int NP, bool kLocal> __global__ void __launch_bounds__(kScanThreads, 2) token_scan_kernel(ScanKernel k) {
-    constexpr int SPL = NP / 4;
-    using L = ScanSmem<T, NP>;
-    extern __shared__ __align__(16) char smem[];
+template <typename T, int NP, bool kLocal> __global__ void __launch_bounds__(kFwdThreads, 4) token_scan_kernel(ScanKernel k) {
+    constexpr int SPL = NP / 2, P = Pairs<SPL>::P, kEach = kTok * 2 * NP / kFwdThreads;
+    __shared__ __align__(16) float bcs[2][kTok * 2 * NP];
     pdl_wait();
     pdl_launch_dependents();
     const TokenScanArgs& a = k.a;
-    const int tile = blockIdx.x % k.tiles, tid = threadIdx.x, q = tid & 3, ch = tid >> 2, c0 = tile * kScanCh, d = c0 + ch, n0 = q * SPL;
-    const int cols = min(kScanCh, a.D - c0);
+    const int tile = blockIdx.x % k.tiles, tid = threadIdx.x, p = tid & 1, c0 = tile * kScanCh, d = c0 + (tid >> 1), n0 = p * SPL;
     const long long slot = blockIdx.x / k.tiles;
     if (slot >= k.slots) {  // rows before the first and behind the last sequence
         const long long lo = min(max((long long)a.offsets[0], 0LL), a.total), hi = min(max((long long)a.offsets[a.B], lo), a.total);
+        const int cols = min(kScanCh, a.D - c0);
         for (long long r = slot - k.slots; r < a.total - (hi - lo); r += kClearBlocks)
-            for (int c = tid; c < cols; c += kScanThreads) ((T*)a.y)[(r < lo ? r : r + hi - lo) * a.D + c0 + c] = io<T>::to(0.0f);
+            for (int c = tid; c < cols; c += kFwdThreads) ((T*)a.y)[(r < lo ? r : r + hi - lo) * a.D + c0 + c] = io<T>::to(0.0f);
         return;
     }
     const ScanSegment g = scan_segment(k, slot);
     if (!g.live || (kLocal && g.s == g.segs - 1)) return;  // (nothing follows the last segment)
-    char* bcs = smem + 2 * L::slot;
     const bool on = d < a.D, gate = !kLocal && a.z;
+    const int dd = on ? d : a.D - 1;  // (lanes behind the last channel keep their warp's shuffles whole)
     Pairs<SPL> A2, h;
-    A2.zero(), h.zero();
-    if (on) {
-        A2.load_some(a.A + (long long)d * a.N + n0, n0, a.N);
+    A2.load_some(a.A + (long long)dd * a.N + n0, n0, a.N);
 #pragma unroll
-        for (int p = 0; p < Pairs<SPL>::P; ++p) A2.v[p] = __fmul2_rn(A2.v[p], twice(kLog2e));
-    }
-    const float bias = on && a.bias ? a.bias[d] : 0.0f, skip = on && a.skip ? a.skip[d] : 0.0f;
-    const T *x = scan_row<T>(a.x, a, g, a.x_b, a.x_t) + c0, *raw = scan_row<T>(a.delta, a, g, a.d_b, a.d_t) + c0;
-    const T* z = gate ? scan_row<T>(a.z, a, g, a.z_b, a.z_t) + c0 : nullptr;
-    const T *Bm = scan_row<T>(a.Bm, a, g, a.B_b, a.B_t), *Cm = scan_row<T>(a.Cm, a, g, a.C_b, a.C_t);
-    const int stages = (g.len + kTok - 1) / kTok;
-    RowsBC<T, NP, kTok> bc;
-    auto fetch = [&](int i) {  // copies of stage i under way, its B and C in registers
-        if (i < stages) {
-            char* s = smem + (i & 1) * L::slot;
-            const int t0 = i * kTok, left = g.len - t0;
-            stage_rows<T>(s, x + t0 * a.x_t, a.x_t, kTok, left, cols, k.vec);
-            stage_rows<T>(s + L::array, raw + t0 * a.d_t, a.d_t, kTok, left, cols, k.vec);
-            if (gate) stage_rows<T>(s + 2 * L::array, z + t0 * a.z_t, a.z_t, kTok, left, cols, k.vec);
-            bc.load(Bm + t0 * a.B_t, a.B_t, a.N, Cm + t0 * a.C_t, a.C_t, kLocal ? 0 : a.N, left);
+    for (int i = 0; i < P; ++i) A2.v[i] = __fmul2_rn(A2.v[i], twice(kLog2e));
+    h.zero();
+    const float bias = a.bias ? a.bias[dd] : 0.0f, skip = !kLocal && a.skip ? a.skip[dd] : 0.0f;
+    // this lane's next token of each array, and its value of B or C in this thread's next row of the stage
+    const int xs = (int)a.x_t, ds = (int)a.d_t, zs = (int)a.z_t;
+    const T *x = scan_row<T>(a.x, a, g, a.x_b, a.x_t) + p * a.x_t + dd, *raw = scan_row<T>(a.delta, a, g, a.d_b, a.d_t) + p * a.d_t + dd;
+    const T* z = gate ? scan_row<T>(a.z, a, g, a.z_b, a.z_t) + p * a.z_t + dd : nullptr;
+    T* y = (T*)a.y + (g.first + p) * a.D + d;
+    constexpr int kRows = kFwdThreads / (2 * NP);
+    const int bn = tid % (2 * NP), brow = tid / (2 * NP), bs = (int)(bn < NP ? a.B_t : a.C_t);
+    const bool bin = bn < NP ? bn < a.N : !kLocal && bn - NP < a.N;
+    const T* bc = bn < NP ? scan_row<T>(a.Bm, a, g, a.B_b, a.B_t) + bn : scan_row<T>(a.Cm, a, g, a.C_b, a.C_t) + (bn - NP);
+    bc += (long long)brow * bs;
+    const int blocks = (g.len + kBlk - 1) / kBlk;
+
+    T rx[kMine], rd[kMine], rz[kMine], rbc[kEach];
+    auto load = [&](int left) {  // `left` tokens, the block's among them (rows behind the last: the last again)
+        if (left >= kBlk) {
+#pragma unroll
+            for (int j = 0; j < kMine; ++j) {
+                rx[j] = x[2 * j * xs], rd[j] = raw[2 * j * ds];
+                if (gate) rz[j] = z[2 * j * zs];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kMine; ++j) {
+                const int t = min(2 * j, left - 1 - p);
+                rx[j] = x[t * xs], rd[j] = raw[t * ds];
+                if (gate) rz[j] = z[t * zs];
+            }
         }
-        cp_async_commit();
+        x += (long long)kBlk * xs, raw += (long long)kBlk * ds;
+        if (gate) z += (long long)kBlk * zs;
     };
-    fetch(0);
-    bc.store((float*)bcs);
-    fetch(1);
-    if (!kLocal && on) {
-        if (a.initial) h.load_some(a.initial + ((long long)g.b * a.D + d) * a.N + n0, n0, a.N);
+    auto load_bc = [&](int left) {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) rbc[j] = bin && brow + j * kRows < left ? bc[j * kRows * bs] : io<T>::to(0.0f);
+        bc += (long long)kTok * bs;
+    };
+    auto store_bc = [&](float* s) {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) s[tid + j * kFwdThreads] = io<T>::cvt(rbc[j]);
+    };
+    if (blocks > 0) {
+        load_bc(g.len);
+        load(g.len);
+    }
+    if (!kLocal) {
+        if (a.initial) h.load_some(a.initial + ((long long)g.b * a.D + dd) * a.N + n0, n0, a.N);
         for (int s = 0; s < g.s; ++s) {
-            const long long at = (g.place + s) * a.D + d;
+            const long long at = (g.place + s) * a.D + dd;
             Pairs<SPL> l, e;
             l.load(k.local + at * NP + n0);
             decays(e, A2, k.decay[at]);
 #pragma unroll
-            for (int p = 0; p < Pairs<SPL>::P; ++p) h.v[p] = __ffma2_rn(e.v[p], h.v[p], l.v[p]);
+            for (int i = 0; i < P; ++i) h.v[i] = __ffma2_rn(e.v[i], h.v[i], l.v[i]);
         }
     }
-    cp_async_wait<1>();
+    if (blocks > 0) store_bc(bcs[0]);
     __syncthreads();
     float sum = 0.0f;  // of this lane's step sizes
-    for (int i = 0; i < stages; ++i) {
-        char* s = smem + (i & 1) * L::slot;
-        const float* rows = (const float*)(bcs + (i & 1) * L::bc);
-        const int t0 = i * kTok;
+    const int from0 = tid & 30, from1 = from0 | 1;
+    for (int b = 0; b < blocks; ++b) {
+        const int t0 = b * kBlk, left = g.len - t0;
+        if (!(b & 1)) load_bc(left - kTok);
+        float dt[kMine], dtx[kMine], out[kMine];
+        T zv[kMine];
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) {
+            const float xv = io<T>::cvt(rx[j]);
+            dt[j] = io<T>::cvt(rd[j]) + bias;
+            if (a.softplus) dt[j] = softplus(dt[j]);
+            dtx[j] = dt[j] * xv;
+            out[j] = skip * xv;
+            if (gate) zv[j] = rz[j];
+        }
+        if (left < kBlk) {
+#pragma unroll
+            for (int j = 0; j < kMine; ++j)
+                if (2 * j + p >= left) dt[j] = dtx[j] = 0.0f;
+        }
+        if (left > kBlk) load(left - kBlk);
         if (!kLocal && a.saved && on && t0 % kScanChunk == 0)
             h.store_some(a.saved + ((g.chunk + ((long long)g.s * k.seg + t0) / kScanChunk) * a.D + d) * a.N + n0, n0, a.N);
-#pragma unroll 2
-        for (int t = 0; t < kTok; t += 4) {
-            const float xv = staged<T>(s, t + q, ch);
-            float dt = staged<T>(s + L::array, t + q, ch) + bias;
-            if (a.softplus) dt = softplus(dt);
-            if (t0 + t + q >= g.len) dt = 0.0f;
-            const float dtx = dt * xv;
-            float out[4];
+        const float* rows = bcs[(b >> 1) & 1] + (b & 1) * kBlk * 2 * NP + n0;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const float dtu = from_lane(dt, u), dxu = from_lane(dtx, u);
+        for (int j = 0; j < kMine; ++j) {
+            float part[2];
+            if (kLocal) sum += dt[j];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const float dtu = __shfl_sync(0xffffffffu, dt[j], u ? from1 : from0), dxu = __shfl_sync(0xffffffffu, dtx[j], u ? from1 : from0);
                 Pairs<SPL> B, C, e;
-                B.load(rows + (t + u) * 2 * NP + n0);
+                B.load(rows + (2 * j + u) * 2 * NP);
+                if (!kLocal) C.load(rows + (2 * j + u) * 2 * NP + NP);
                 decays(e, A2, dtu);
                 float2 acc = make_float2(0.0f, 0.0f);
-                if (!kLocal) C.load(rows + (t + u) * 2 * NP + NP + n0);
 #pragma unroll
-                for (int p = 0; p < Pairs<SPL>::P; ++p) {
-                    h.v[p] = __ffma2_rn(e.v[p], h.v[p], __fmul2_rn(twice(dxu), B.v[p]));
-                    if (!kLocal) acc = __ffma2_rn(C.v[p], h.v[p], acc);
+                for (int i = 0; i < P; ++i) {
+                    h.v[i] = __ffma2_rn(e.v[i], h.v[i], __fmul2_rn(twice(dxu), B.v[i]));
+                    if (!kLocal) acc = i == 0 ? __fmul2_rn(C.v[i], h.v[i]) : __ffma2_rn(C.v[i], h.v[i], acc);
                 }
-                out[u] = acc.x + acc.y;
+                part[u] = acc.x + acc.y;
             }
-            if constexpr (kLocal) {
-                sum += dt;
-            } else {
-                float y = fmaf(skip, xv, quad_sums(out[0], out[1], out[2], out[3]));
-                if (gate) y *= activate<VMB_ACT_SILU>(staged<T>(s + 2 * L::array, t + q, ch));
-                restage<T>(s, t + q, ch, y);
-            }
+            if (!kLocal) out[j] += (p ? part[1] : part[0]) + __shfl_xor_sync(0xffffffffu, p ? part[0] : part[1], 1);
         }
-        if (i + 1 < stages) bc.store((float*)(bcs + ((i + 1) & 1) * L::bc));
-        cp_async_wait<0>();
-        __syncthreads();
-        if (!kLocal) unstage_rows<T>((T*)a.y + (g.first + t0) * a.D + c0, s, a.D, kTok, g.len - t0, cols, k.vec);
-        fetch(i + 2);
+        if (!kLocal) {
+            if (gate) {
+#pragma unroll
+                for (int j = 0; j < kMine; ++j) out[j] *= activate<VMB_ACT_SILU>(io<T>::cvt(zv[j]));
+            }
+            if (on && left >= kBlk) {
+#pragma unroll
+                for (int j = 0; j < kMine; ++j) y[2 * j * a.D] = io<T>::to(out[j]);
+            } else if (on) {
+#pragma unroll
+                for (int j = 0; j < kMine; ++j)
+                    if (2 * j + p < left) y[2 * j * a.D] = io<T>::to(out[j]);
+            }
+            y += (long long)kBlk * a.D;
+        }
+        if (b & 1) {
+            store_bc(bcs[((b >> 1) + 1) & 1]);
+            __syncthreads();
+        }
     }
     if constexpr (kLocal) {
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
         if (!on) return;
         const long long at = slot * a.D + d;
         h.store(k.local + at * NP + n0);
-        if (q == 0) k.decay[at] = sum;
+        if (p == 0) k.decay[at] = sum;
     } else if (on && a.final && g.s == g.segs - 1) {
         h.store_some(a.final + ((long long)g.b * a.D + d) * a.N + n0, n0, a.N);
     }
@@ -197,15 +238,12 @@ bool vec16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 template <typename T, int NP> vmb_status run_scan(const ScanKernel& k0, unsigned grid, bool cut, cudaStream_t stream) {
     ScanKernel k = k0;
-    constexpr int bytes = ScanSmem<T, NP>::bytes;
     const void *local = (const void*)token_scan_kernel<T, NP, true>, *full = (const void*)token_scan_kernel<T, NP, false>;
-    if (bytes > 48 * 1024)
-        for (const void* fn : {local, full})
-            if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return VMB_ERR_CUDA;
     void* args[] = {&k};
-    if (cut && launch_kernel(local, dim3((unsigned)((long long)k.slots * k.tiles)), dim3(kScanThreads), bytes, args, stream) != cudaSuccess)
+    const unsigned first = (unsigned)((long long)k.slots * k.tiles);
+    if (cut && launch_kernel(local, dim3(first), dim3(kFwdThreads), 0, args, stream, first >= resident_ctas(local, kFwdThreads, 0)) != cudaSuccess)
         return VMB_ERR_CUDA;
-    return launch_kernel(full, dim3(grid), dim3(kScanThreads), bytes, args, stream) == cudaSuccess ? VMB_OK : VMB_ERR_CUDA;
+    return launch_kernel(full, dim3(grid), dim3(kFwdThreads), 0, args, stream, grid >= resident_ctas(full, kFwdThreads, 0)) == cudaSuccess ? VMB_OK : VMB_ERR_CUDA;
 }
 
 // Tokens of a forward segment: the whole sequence where the sequences fill the SMs, else such that there are about four CTAs on

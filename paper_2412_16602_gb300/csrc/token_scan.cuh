@@ -169,9 +169,12 @@ template <int SPL> struct Pairs {
     }
     // from shared memory or a padded row of global memory
     __device__ __forceinline__ void load(const float* s) {
-        if constexpr (SPL == 4) {
-            const float4 x = *reinterpret_cast<const float4*>(s);
-            v[0] = make_float2(x.x, x.y), v[1] = make_float2(x.z, x.w);
+        if constexpr (SPL >= 4) {
+#pragma unroll
+            for (int i = 0; i < SPL / 4; ++i) {
+                const float4 x = reinterpret_cast<const float4*>(s)[i];
+                v[2 * i] = make_float2(x.x, x.y), v[2 * i + 1] = make_float2(x.z, x.w);
+            }
         } else if constexpr (SPL == 2) {
             v[0] = *reinterpret_cast<const float2*>(s);
         } else {
@@ -179,8 +182,10 @@ template <int SPL> struct Pairs {
         }
     }
     __device__ __forceinline__ void store(float* s) const {
-        if constexpr (SPL == 4) *reinterpret_cast<float4*>(s) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
-        else if constexpr (SPL == 2) *reinterpret_cast<float2*>(s) = v[0];
+        if constexpr (SPL >= 4) {
+#pragma unroll
+            for (int i = 0; i < SPL / 4; ++i) reinterpret_cast<float4*>(s)[i] = make_float4(v[2 * i].x, v[2 * i].y, v[2 * i + 1].x, v[2 * i + 1].y);
+        } else if constexpr (SPL == 2) *reinterpret_cast<float2*>(s) = v[0];
         else s[0] = v[0].x;
     }
     // from and to a row of N values at its n0-th

@@ -379,8 +379,9 @@ template <typename T, int NP> vmb_status run_grad(const ScanKernel& k0, cudaStre
         return VMB_ERR_CUDA;
     void* args[] = {&k};
     const unsigned grid = (unsigned)((long long)k.slots * k.tiles);
-    if (k.seg < a.T && launch_kernel(adjoint, dim3(grid), dim3(kScanThreads), abytes, args, stream) != cudaSuccess) return VMB_ERR_CUDA;
-    if (launch_kernel(grad, dim3(grid + (a.offsets ? (unsigned)(kClearBlocks * k.tiles) : 0u)), dim3(kScanThreads), gbytes, args, stream) != cudaSuccess)
+    if (k.seg < a.T && launch_kernel(adjoint, dim3(grid), dim3(kScanThreads), abytes, args, stream, grid >= resident_ctas(adjoint, kScanThreads, abytes)) != cudaSuccess) return VMB_ERR_CUDA;
+    if (launch_kernel(grad, dim3(grid + (a.offsets ? (unsigned)(kClearBlocks * k.tiles) : 0u)), dim3(kScanThreads), gbytes, args, stream,
+                      grid >= resident_ctas(grad, kScanThreads, gbytes)) != cudaSuccess)
         return VMB_ERR_CUDA;
     if (a.total > 0 && launch_kernel((const void*)token_scan_bc_kernel<T, NP>, dim3((unsigned)((a.total + 7) / 8)), dim3(256), 0, args, stream) != cudaSuccess)
         return VMB_ERR_CUDA;

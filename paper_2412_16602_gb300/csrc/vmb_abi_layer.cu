@@ -87,11 +87,16 @@ vmb_status scan_args(TokenScanArgs& a, const void* x, const void* delta, const f
     if (!A || (a.total > 0 && (!x || !delta || !Bm || !Cm))) return VMB_ERR_INVALID_ARG;
     if (!aligned({x, delta, Bm, Cm, z}, esize(a.dtype)) || !aligned({A, Dskip, delta_bias}, 4)) return VMB_ERR_MISALIGNED;
     a.x = x, a.delta = delta, a.A = A, a.Bm = Bm, a.Cm = Cm, a.skip = Dskip, a.bias = delta_bias, a.z = z;
-    return take_strides(strides, 0, a.D, a.T, packed, &a.x_b, &a.x_t) && take_strides(strides, 1, a.D, a.T, packed, &a.d_b, &a.d_t) &&
-                   take_strides(strides, 2, a.N, a.T, packed, &a.B_b, &a.B_t) && take_strides(strides, 3, a.N, a.T, packed, &a.C_b, &a.C_t) &&
-                   take_strides(strides, 4, a.D, a.T, packed, &a.z_b, &a.z_t)
-               ? VMB_OK
-               : VMB_ERR_INVALID_ARG;
+    if (!take_strides(strides, 0, a.D, a.T, packed, &a.x_b, &a.x_t) || !take_strides(strides, 1, a.D, a.T, packed, &a.d_b, &a.d_t) ||
+        !take_strides(strides, 2, a.N, a.T, packed, &a.B_b, &a.B_t) || !take_strides(strides, 3, a.N, a.T, packed, &a.C_b, &a.C_t) ||
+        !take_strides(strides, 4, a.D, a.T, packed, &a.z_b, &a.z_t))
+        return VMB_ERR_INVALID_ARG;
+    // (places within a stage of 64 tokens are counted in 32 bits; a stride between tokens that there are not has no meaning)
+    for (long long* t : {&a.x_t, &a.d_t, &a.B_t, &a.C_t, &a.z_t}) {
+        if (a.total <= 1 || (!packed && a.T == 1)) *t = 0;
+        if (*t >= (1 << 24)) return VMB_ERR_UNSUPPORTED;
+    }
+    return VMB_OK;
 }
 
 // ------------------------------------------------------------ norm and product
