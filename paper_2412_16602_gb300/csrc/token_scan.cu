@@ -3,7 +3,7 @@
 //   dt = softplus(delta + bias),  h_t = exp(dt A) h_(t-1) + dt x B_t,  y = C_t . h_t + D x,  y silu(z) with a gate.
 //
 // N exponentials, N / 2 packed products for each of four uses, and two more exponentials for the step size and the gate per
-// channel and token bound it: the MUFU and issue slots, not the bytes.  Sequences too few to fill the SMs are cut into segments:
+// channel and token bound it: the issue slots and the FMA and MUFU pipes (0.62 of the slots, 0.40 and 0.38 of the pipes), not the bytes.  Sequences too few to fill the SMs are cut into segments:
 // a first launch takes each segment from a zero state and leaves its last state and the sum of its step sizes (the product of
 // its decays is the exponential of A times that sum), and each segment of the second launch joins those before it.
 #include "token_scan.cuh"
@@ -12,18 +12,20 @@ namespace vmb {
 
 namespace {
 
-// Two lanes hold the states of a channel, so that a warp has 16 channels and a CTA the 64 of a tile.  A lane of the pair reads and prepares
-// one token of every two (step size, its product with x, skip, gate), in blocks of 16 tokens whose values were asked for a block
-// before, and hands them to the other by shuffles.  B and C of 32 tokens are in shared memory in fp32.
-constexpr int kFwdThreads = 2 * kScanCh, kTok = 32, kBlk = 16, kMine = kBlk / 2;
+// Two lanes hold the states of a channel; a CTA takes the 64 channels of a tile.  A lane of the pair reads and prepares one token of every
+// two (step size, its product with x, skip, gate), in blocks of 8 tokens whose values were asked for a block before, and hands
+// them to the other by shuffles.  B and C of 32 tokens are in shared memory in fp32.
+// 38 sequences of 2048 tokens of 1024 channels and 16 states, bf16, with a gate: 438 us, 68 instructions a token, warp and lane pair; one lane for
+// a channel takes the same with all SMs full and longer with fewer sequences, four took 939 us.
+constexpr int kLanes = 2, kFwdThreads = kLanes * kScanCh, kTok = 32, kBlk = 8, kPer = kTok / kBlk, kMine = kBlk / kLanes;
 
 template <typename T, int NP, bool kLocal> __global__ void __launch_bounds__(kFwdThreads, 4) token_scan_kernel(ScanKernel k) {
-    constexpr int SPL = NP / 2, P = Pairs<SPL>::P, kEach = kTok * 2 * NP / kFwdThreads;
+    constexpr int SPL = NP / kLanes, P = Pairs<SPL>::P, kEach = kTok * 2 * NP / kFwdThreads;
     __shared__ __align__(16) float bcs[2][kTok * 2 * NP];
     pdl_wait();
     pdl_launch_dependents();
     const TokenScanArgs& a = k.a;
-    const int tile = blockIdx.x % k.tiles, tid = threadIdx.x, p = tid & 1, c0 = tile * kScanCh, d = c0 + (tid >> 1), n0 = p * SPL;
+    const int tile = blockIdx.x % k.tiles, tid = threadIdx.x, p = tid & 1, c0 = tile * kScanCh, d = c0 + tid / kLanes, n0 = p * SPL;
     const long long slot = blockIdx.x / k.tiles;
     if (slot >= k.slots) {  // rows before the first and behind the last sequence
         const long long lo = min(max((long long)a.offsets[0], 0LL), a.total), hi = min(max((long long)a.offsets[a.B], lo), a.total);
@@ -59,13 +61,13 @@ template <typename T, int NP, bool kLocal> __global__ void __launch_bounds__(kFw
         if (left >= kBlk) {
 #pragma unroll
             for (int j = 0; j < kMine; ++j) {
-                rx[j] = x[2 * j * xs], rd[j] = raw[2 * j * ds];
-                if (gate) rz[j] = z[2 * j * zs];
+                rx[j] = x[kLanes * j * xs], rd[j] = raw[kLanes * j * ds];
+                if (gate) rz[j] = z[kLanes * j * zs];
             }
         } else {
 #pragma unroll
             for (int j = 0; j < kMine; ++j) {
-                const int t = min(2 * j, left - 1 - p);
+                const int t = min(kLanes * j, left - 1 - p);
                 rx[j] = x[t * xs], rd[j] = raw[t * ds];
                 if (gate) rz[j] = z[t * zs];
             }
@@ -88,6 +90,7 @@ template <typename T, int NP, bool kLocal> __global__ void __launch_bounds__(kFw
     }
     if (!kLocal) {
         if (a.initial) h.load_some(a.initial + ((long long)g.b * a.D + dd) * a.N + n0, n0, a.N);
+#pragma unroll 4
         for (int s = 0; s < g.s; ++s) {
             const long long at = (g.place + s) * a.D + dd;
             Pairs<SPL> l, e;
@@ -103,7 +106,7 @@ template <typename T, int NP, bool kLocal> __global__ void __launch_bounds__(kFw
     const int from0 = tid & 30, from1 = from0 | 1;
     for (int b = 0; b < blocks; ++b) {
         const int t0 = b * kBlk, left = g.len - t0;
-        if (!(b & 1)) load_bc(left - kTok);
+        if (b % kPer == 0) load_bc(left - kTok);
         float dt[kMine], dtx[kMine], out[kMine];
         T zv[kMine];
 #pragma unroll
@@ -118,27 +121,33 @@ template <typename T, int NP, bool kLocal> __global__ void __launch_bounds__(kFw
         if (left < kBlk) {
 #pragma unroll
             for (int j = 0; j < kMine; ++j)
-                if (2 * j + p >= left) dt[j] = dtx[j] = 0.0f;
+                if (kLanes * j + p >= left) dt[j] = dtx[j] = 0.0f;
         }
         if (left > kBlk) load(left - kBlk);
         if (!kLocal && a.saved && on && t0 % kScanChunk == 0)
             h.store_some(a.saved + ((g.chunk + ((long long)g.s * k.seg + t0) / kScanChunk) * a.D + d) * a.N + n0, n0, a.N);
-        const float* rows = bcs[(b >> 1) & 1] + (b & 1) * kBlk * 2 * NP + n0;
+        const float* rows = bcs[(b / kPer) & 1] + (b % kPer) * kBlk * 2 * NP + n0;
 #pragma unroll
         for (int j = 0; j < kMine; ++j) {
-            float part[2];
+            float part[kLanes];
             if (kLocal) sum += dt[j];
+            Pairs<SPL> e[kLanes], in[kLanes];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+            for (int u = 0; u < kLanes; ++u) {
                 const float dtu = __shfl_sync(0xffffffffu, dt[j], u ? from1 : from0), dxu = __shfl_sync(0xffffffffu, dtx[j], u ? from1 : from0);
-                Pairs<SPL> B, C, e;
-                B.load(rows + (2 * j + u) * 2 * NP);
-                if (!kLocal) C.load(rows + (2 * j + u) * 2 * NP + NP);
-                decays(e, A2, dtu);
+                in[u].load(rows + (kLanes * j + u) * 2 * NP);
+                decays(e[u], A2, dtu);
+#pragma unroll
+                for (int i = 0; i < P; ++i) in[u].v[i] = __fmul2_rn(twice(dxu), in[u].v[i]);
+            }
+#pragma unroll
+            for (int u = 0; u < kLanes; ++u) {
+                Pairs<SPL> C;
+                if (!kLocal) C.load(rows + (kLanes * j + u) * 2 * NP + NP);
                 float2 acc = make_float2(0.0f, 0.0f);
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
-                    h.v[i] = __ffma2_rn(e.v[i], h.v[i], __fmul2_rn(twice(dxu), B.v[i]));
+                    h.v[i] = __ffma2_rn(e[u].v[i], h.v[i], in[u].v[i]);
                     if (!kLocal) acc = i == 0 ? __fmul2_rn(C.v[i], h.v[i]) : __ffma2_rn(C.v[i], h.v[i], acc);
                 }
                 part[u] = acc.x + acc.y;
@@ -152,16 +161,16 @@ template <typename T, int NP, bool kLocal> __global__ void __launch_bounds__(kFw
             }
             if (on && left >= kBlk) {
 #pragma unroll
-                for (int j = 0; j < kMine; ++j) y[2 * j * a.D] = io<T>::to(out[j]);
+                for (int j = 0; j < kMine; ++j) y[kLanes * j * a.D] = io<T>::to(out[j]);
             } else if (on) {
 #pragma unroll
                 for (int j = 0; j < kMine; ++j)
-                    if (2 * j + p < left) y[2 * j * a.D] = io<T>::to(out[j]);
+                    if (kLanes * j + p < left) y[kLanes * j * a.D] = io<T>::to(out[j]);
             }
             y += (long long)kBlk * a.D;
         }
-        if (b & 1) {
-            store_bc(bcs[((b >> 1) + 1) & 1]);
+        if (b % kPer == kPer - 1) {
+            store_bc(bcs[(b / kPer + 1) & 1]);
             __syncthreads();
         }
     }
@@ -241,23 +250,40 @@ template <typename T, int NP> vmb_status run_scan(const ScanKernel& k0, unsigned
     const void *local = (const void*)token_scan_kernel<T, NP, true>, *full = (const void*)token_scan_kernel<T, NP, false>;
     void* args[] = {&k};
     const unsigned first = (unsigned)((long long)k.slots * k.tiles);
+    // (grids below a wave are not launched early: they would fill the SMs that are free first)
     if (cut && launch_kernel(local, dim3(first), dim3(kFwdThreads), 0, args, stream, first >= resident_ctas(local, kFwdThreads, 0)) != cudaSuccess)
         return VMB_ERR_CUDA;
     return launch_kernel(full, dim3(grid), dim3(kFwdThreads), 0, args, stream, grid >= resident_ctas(full, kFwdThreads, 0)) == cudaSuccess ? VMB_OK : VMB_ERR_CUDA;
 }
+template <typename T> vmb_status run_scan(const ScanKernel& k, unsigned grid, bool cut, cudaStream_t stream) {
+    const int np = padded_states(k.a.N);
+    return np == 4 ? run_scan<T, 4>(k, grid, cut, stream) : np == 8 ? run_scan<T, 8>(k, grid, cut, stream) : run_scan<T, 16>(k, grid, cut, stream);
+}
 
-// Tokens of a forward segment: the whole sequence where the sequences fill the SMs, else such that there are about four CTAs on
-// each, at least two chunks long and at most 64 to a sequence (each joins those before it).
-int forward_segment(int B, int T, long long total, int D) {
-    const long long tiles = (D + kScanCh - 1) / kScanCh, fill = 2LL * device_sm_count();
-    const int whole = (T + kScanChunk - 1) / kScanChunk * kScanChunk;
-    if (B * tiles >= fill || T <= 4 * kScanChunk) return whole < kScanChunk ? kScanChunk : whole;
-    long long segs = (2 * fill + tiles - 1) / tiles;  // wanted over all sequences
-    long long seg = (total + segs - 1) / segs;
-    if (seg * 64 < T) seg = (T + 63) / 64;
-    seg = (seg + kScanChunk - 1) / kScanChunk * kScanChunk;
-    if (seg < 2 * kScanChunk) seg = 2 * kScanChunk;
-    return (int)(seg < whole ? seg : whole);
+// Tokens of a forward segment, a multiple of 64.  Dense: by estimated clocks.  With one to four CTAs on an SM a token takes 248, 262, 330 or
+// 395 of them (measured with 16 states and a gate; the third in between), and no more than four fit; cut sequences take 1.7 times that, for the first launch, and
+// 12000 for its start and the joins.  19 sequences of 1024 channels, two CTAs on each SM, stay whole (291 us, cut in three 359); of 512
+// channels, one on each, are cut (192 us, whole 275); a single one of 3136 tokens and 384 channels is cut in 49 (29 us, in 25 33, whole 295).
+// Packed: their lengths are not known here, the long ones are cut for balance, eight segments for each SM (24 of 1 to 4096 tokens and 1536
+// channels: 368 us, with four for each SM 428, whole 631).
+int forward_segment(int B, int T, long long total, bool packed, int D) {
+    const long long tiles = (D + kScanCh - 1) / kScanCh, sms = device_sm_count();
+    const auto chunks = [](long long t) { return t < 1 ? (long long)kScanChunk : (t + kScanChunk - 1) / kScanChunk * kScanChunk; };
+    if (packed) {
+        const long long segs = (8 * sms + tiles - 1) / tiles, seg = chunks((total + segs - 1) / segs), least = chunks((total + 63) / 64);
+        return (int)(seg > least ? seg : least);
+    }
+    const double per_token[4] = {248.0, 262.0, 330.0, 395.0};
+    long long best = chunks(T);
+    double least = -1.0;
+    for (int want = 1; want <= 64 && (want == 1 || best > kScanChunk); ++want) {
+        const long long seg = chunks((T + want - 1) / want), segs = (T + seg - 1) / seg, ctas = (long long)B * tiles * (segs > 1 ? segs : 1);
+        const long long full = ctas / (4 * sms), rest = ctas % (4 * sms);
+        const double token = 395.0 * full + (rest ? per_token[(rest + sms - 1) / sms - 1] : 0.0);
+        const double clocks = seg * token * (segs > 1 ? 1.7 : 1.0) + (segs > 1 ? 12000.0 : 0.0);
+        if (least < 0.0 || clocks < least) least = clocks, best = seg;
+    }
+    return (int)best;
 }
 
 }  // namespace
@@ -276,26 +302,21 @@ void token_scan_plan(ScanKernel& k, int seg) {
 }
 
 size_t token_scan_forward_bytes(int B, int T, long long total, bool packed, int D, int N) {
-    const int seg = forward_segment(B, T, total, D);
+    const int seg = forward_segment(B, T, total, packed, D);
     const long long slots = scan_slots(B, T, total, packed, seg);
     return 256 + align_up((size_t)slots * D * padded_states(N) * 4, 256) + align_up((size_t)slots * D * 4, 256);
 }
 
 vmb_status launch_token_scan_fwd(const TokenScanArgs& a, cudaStream_t stream) {
     ScanKernel k{a};
-    token_scan_plan(k, forward_segment(a.B, a.T, a.total, a.D));
+    token_scan_plan(k, forward_segment(a.B, a.T, a.total, a.offsets != nullptr, a.D));
     if (a.ws_bytes < token_scan_forward_bytes(a.B, a.T, a.total, a.offsets != nullptr, a.D, a.N)) return VMB_ERR_WORKSPACE;
     k.local = (float*)((char*)a.ws + 256);
     k.decay = (float*)((char*)k.local + align_up((size_t)k.slots * a.D * padded_states(a.N) * 4, 256));
     const bool cut = k.seg < a.T;
     const unsigned grid = (unsigned)(((long long)k.slots + (a.offsets ? kClearBlocks : 0)) * k.tiles);
     if (grid == 0) return VMB_OK;
-    const int np = padded_states(a.N);
-    if (a.dtype == VMB_BF16)
-        return np == 16  ? run_scan<__nv_bfloat16, 16>(k, grid, cut, stream)
-               : np == 8 ? run_scan<__nv_bfloat16, 8>(k, grid, cut, stream)
-                         : run_scan<__nv_bfloat16, 4>(k, grid, cut, stream);
-    return np == 16 ? run_scan<float, 16>(k, grid, cut, stream) : np == 8 ? run_scan<float, 8>(k, grid, cut, stream) : run_scan<float, 4>(k, grid, cut, stream);
+    return a.dtype == VMB_BF16 ? run_scan<__nv_bfloat16>(k, grid, cut, stream) : run_scan<float>(k, grid, cut, stream);
 }
 
 vmb_status launch_token_scan_step(const TokenScanArgs& a, cudaStream_t stream) {
