@@ -18,6 +18,8 @@ namespace {
 
 constexpr int kConvThreads = 128;
 constexpr int kConvBatch = 4;  // rows whose values are read before the first is used
+template <typename T> constexpr int conv_bwd_blocks_per_sm() { return sizeof(T) == 2 ? 4 : 3; }  // of the gradients: 128 and 168 registers
+constexpr int kConvRun = 16;   // rows of a run of the forward at most
 
 // How the threads of a launch lie over the channels: tx vectors side by side, ty runs of tokens, nb blocks over the channels.
 struct ConvGrid {
@@ -71,12 +73,36 @@ __device__ __forceinline__ void taps(float (&z)[V], float (&win)[W > 1 ? W - 1 :
 
 template <int V, int W>
 __device__ __forceinline__ void load_filter(float (&w)[W][V], float (&bias)[V], const ConvArgs& a, int c) {
+    const float* p = a.weight + (long long)c * W;  // [V][W], dense
+    if (V * W % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
+        for (int q = 0; q < V * W / 4; ++q) {
+            const float4 f = reinterpret_cast<const float4*>(p)[q];
+            const float all[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
-        for (int j = 0; j < W; ++j) w[j][i] = a.weight[(long long)(c + i) * W + j];
-        bias[i] = a.bias ? a.bias[c + i] : 0.0f;
+            for (int e = 0; e < 4; ++e) w[(4 * q + e) % W][(4 * q + e) / W] = all[e];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (int j = 0; j < W; ++j) w[j][i] = p[i * W + j];
     }
+    if (V % 4 == 0 && (reinterpret_cast<uintptr_t>(a.bias) & 15) == 0) {
+#pragma unroll
+        for (int q = 0; q < V / 4; ++q) {
+            const float4 f = a.bias ? reinterpret_cast<const float4*>(a.bias + c)[q] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            bias[4 * q % V] = f.x, bias[(4 * q + 1) % V] = f.y, bias[(4 * q + 2) % V] = f.z, bias[(4 * q + 3) % V] = f.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) bias[i] = a.bias ? a.bias[c + i] : 0.0f;
+    }
+}
+template <typename T, int V> __device__ __forceinline__ Vec<T, V> raw_vec(const T* p) { return *reinterpret_cast<const Vec<T, V>*>(p); }
+template <typename T, int V> __device__ __forceinline__ void widen(float (&out)[V], const Vec<T, V>& a) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) out[i] = io<T>::cvt(a.v[i]);
 }
 
 // The sequence of a packed row, -1 or B if none has it.
@@ -96,13 +122,33 @@ struct Place {
     long long start, end;   // of that sequence, in rows
     __device__ __forceinline__ bool none(int B) const { return b < 0 || b >= B; }
 };
-__device__ __forceinline__ Place place_of(const int* offsets, int B, long long total, long long row) {
+__device__ __forceinline__ Place place_in(const int* offsets, int B, long long total, long long row, int b) {
     Place p;
-    p.b = sequence_of(offsets, B, row);
+    p.b = b;
     p.start = p.b < 0 ? 0 : min(max((long long)offsets[p.b], 0LL), row);
     p.end = p.b >= B ? total : offsets[p.b + 1];
     if (p.end <= row || p.end > total) p.end = total;
     return p;
+}
+
+__device__ __forceinline__ Place place_of(const int* offsets, int B, long long total, long long row) {
+    return place_in(offsets, B, total, row, sequence_of(offsets, B, row));
+}
+// The same for the first rows of a block's runs: by a warp for each while they are few (32 offsets a round), else by a thread.
+__device__ __forceinline__ int first_sequence(const ConvArgs& a, const ConvGrid& g, long long first, int run, long long runs) {
+    __shared__ int seq[kConvThreads];
+    const int w = threadIdx.x >> 5;
+    if (g.ty <= 8) {
+        for (int r = w; r < g.ty; r += kConvThreads / 32) {
+            const int b = last_at_most(a.B, (first + r) * run, [&](int i) { return (long long)a.offsets[i]; });
+            if ((threadIdx.x & 31) == 0) seq[r] = b;
+        }
+    } else if (threadIdx.x < g.ty && first + threadIdx.x < runs) {
+        seq[threadIdx.x] = sequence_of(a.offsets, a.B, (first + threadIdx.x) * run);
+    }
+    __syncthreads();
+    const int ly = threadIdx.x / g.tx;
+    return ly < g.ty ? seq[ly] : 0;
 }
 
 // Final states: the last W - 1 inputs of sequence b, of the initial state where it is shorter.
@@ -135,40 +181,72 @@ template <typename T, int V, int W, int ACT, bool kPacked> __global__ void __lau
     const int c = (blockIdx.y * k.g.tx + lx) * V;
     pdl_wait();
     pdl_launch_dependents();
-    if (c >= a.C || ly >= k.g.ty) return;
     if (blockIdx.x >= k.tile_blocks) {
         const long long b = (long long)(blockIdx.x - k.tile_blocks) * k.g.ty + ly;
-        if (b < a.B) last_inputs<T, V, W>(a, (int)b, c);
+        if (b < a.B && c < a.C && ly < k.g.ty) last_inputs<T, V, W>(a, (int)b, c);
         return;
     }
     const long long run = (long long)blockIdx.x * k.g.ty + ly;
-    if (run >= k.runs) return;
-    float w[W][V], bias[V], win[W > 1 ? W - 1 : 1][V];
-    load_filter<V, W>(w, bias, a, c);
-    const T *x, *initial = (const T*)a.initial;
-    T* y;
-    long long row, left;  // (packed: the row of all; dense: the place in the sequence)
-    Place at{0, 0, 0};
-    if constexpr (kPacked) {
-        row = run * k.run;
-        left = min((long long)k.run, a.total - row);
-        x = (const T*)a.x + row * a.x_t + c;
-        y = (T*)a.y + row * a.C + c;
-        at = place_of(a.offsets, a.B, a.total, row);
-        if (!at.none(a.B)) window_before<T, V, W>(win, x, a.x_t, initial ? initial + (long long)at.b * (W - 1) * a.C + c : nullptr, a.C, row - at.start);
-    } else {
-        const int b = (int)(run / k.runs_per);
-        row = (run - (long long)b * k.runs_per) * k.run;
-        left = min((long long)k.run, a.T - row);
-        x = (const T*)a.x + b * a.x_b + row * a.x_t + c;
-        y = (T*)a.y + ((long long)b * a.T + row) * a.C + c;
-        window_before<T, V, W>(win, x, a.x_t, initial ? initial + (long long)b * (W - 1) * a.C + c : nullptr, a.C, row);
+    const bool on = c < a.C && ly < k.g.ty && run < k.runs;
+    const T *x = (const T*)a.x, *initial = (const T*)a.initial;
+    T* y = nullptr;
+    long long row = 0, left = 0, before = 0;  // (packed: the row of all; dense: the place in the sequence; rows of x that lie before it)
+    if (on) {
+        int b = 0;
+        if constexpr (kPacked) {
+            row = run * k.run;
+            left = min((long long)k.run, a.total - row);
+            x += row * a.x_t + c;
+            y = (T*)a.y + row * a.C + c;
+        } else {
+            b = (int)(run / k.runs_per);
+            row = (run - (long long)b * k.runs_per) * k.run;
+            left = min((long long)k.run, a.T - row);
+            x += b * a.x_b + row * a.x_t + c;
+            y = (T*)a.y + ((long long)b * a.T + row) * a.C + c;
+            if (initial) initial += (long long)b * (W - 1) * a.C + c;
+        }
+        before = row;
     }
-    for (long long r = 0; r < left; r += kConvBatch) {
-        float in[kConvBatch][V];
+    // the first rows and those before them are asked for before the sequence is known
+    Vec<T, V> in[kConvBatch], old[W > 1 ? W - 1 : 1];
+    auto fetch = [&](long long r) {
 #pragma unroll
         for (int u = 0; u < kConvBatch; ++u)
-            if (r + u < left) load_vec<T, V>(in[u], x + (r + u) * a.x_t);
+            if (r + u < left) in[u] = raw_vec<T, V>(x + (r + u) * a.x_t);
+    };
+    fetch(0);
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+        old[j] = Vec<T, V>{};
+        if (on && before - (W - 1) + j >= 0) old[j] = raw_vec<T, V>(x + (long long)(j - (W - 1)) * a.x_t);
+    }
+    Place at{0, 0, 0};
+    long long place = row;  // in the sequence
+    if constexpr (kPacked) {
+        const int b = first_sequence(a, k.g, (long long)blockIdx.x * k.g.ty, k.run, k.runs);
+        if (on) {
+            at = place_in(a.offsets, a.B, a.total, row, b);
+            place = row - at.start;
+            if (initial && !at.none(a.B)) initial += (long long)at.b * (W - 1) * a.C + c;
+        }
+    }
+    if (!on) return;
+    float w[W][V], bias[V], win[W > 1 ? W - 1 : 1][V];
+    load_filter<V, W>(w, bias, a, c);
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+        widen<T, V>(win[j], old[j]);
+        const long long q = place - (W - 1) + j;
+        if (kPacked && at.none(a.B)) continue;
+        if (q < 0) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) win[j][i] = 0.0f;
+            if (initial) load_vec<T, V>(win[j], initial + (long long)(W - 1 + q) * a.C);
+        }
+    }
+    for (long long r = 0; r < left; r += kConvBatch) {
+        if (r) fetch(r);
 #pragma unroll
         for (int u = 0; u < kConvBatch; ++u) {
             if (r + u >= left) break;
@@ -176,12 +254,13 @@ template <typename T, int V, int W, int ACT, bool kPacked> __global__ void __lau
                 if (row + r + u == at.end) {
                     at = place_of(a.offsets, a.B, a.total, row + r + u);
                     if (!at.none(a.B))
-                        window_before<T, V, W>(win, x + (r + u) * a.x_t, a.x_t, initial ? initial + (long long)at.b * (W - 1) * a.C + c : nullptr, a.C,
+                        window_before<T, V, W>(win, x + (r + u) * a.x_t, a.x_t, a.initial ? (const T*)a.initial + (long long)at.b * (W - 1) * a.C + c : nullptr, a.C,
                                                row + r + u - at.start);
                 }
             }
-            float z[V];
-            taps<V, W>(z, win, in[u], w, bias);
+            float z[V], cur[V];
+            widen<T, V>(cur, in[u]);
+            taps<V, W>(z, win, cur, w, bias);
 #pragma unroll
             for (int i = 0; i < V; ++i) z[i] = kPacked && at.none(a.B) ? 0.0f : activate<ACT>(z[i]);
             store_vec<T, V>(y + (r + u) * a.C, z);
@@ -191,7 +270,7 @@ template <typename T, int V, int W, int ACT, bool kPacked> __global__ void __lau
 
 // Gradients.  A thread walks its run and the W - 1 rows behind it; `acc` holds the sums of dx of the last W - 1 rows, whose later
 // rows are still to come.  Its sums over the tokens go on from run to run and leave one row of partial sums.
-template <typename T, int V, int W, int ACT, bool kPacked> __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(ConvKernel k) {
+template <typename T, int V, int W, int ACT, bool kPacked> __global__ void __launch_bounds__(kConvThreads, conv_bwd_blocks_per_sm<T>()) conv_bwd_kernel(ConvKernel k) {
     const ConvArgs& a = k.a;
     const int lx = threadIdx.x % k.g.tx, ly = threadIdx.x / k.g.tx;
     const int c = (blockIdx.y * k.g.tx + lx) * V;
@@ -256,15 +335,79 @@ template <typename T, int V, int W, int ACT, bool kPacked> __global__ void __lau
             store_vec<T, V>(dx + r * a.C, o);
         };
         enter(0);
+        // a run whose rows, and the W - 1 behind them, are of one sequence: no row of it is among the sequence's last W - 1
+        if (left == k.run && !at.none(a.B) && seq0 + left + W - 1 <= at.end) {
+            float later[W > 1 ? W - 1 : 1][V];  // g of the last W - 1 rows
+            const int xs = (int)a.x_t;
+            // g of a row, its input taken into the window
+            auto slope_row = [&](float (&g)[V], const Vec<T, V>& rx, const Vec<T, V>& rg, bool sums) {
+                float cur[V], z[V];
+                widen<T, V>(cur, rx);
+                widen<T, V>(g, rg);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float s = bias[i];
+#pragma unroll
+                    for (int j = 0; j < W - 1; ++j) s = fmaf(w[j][i], win[j][i], s);
+                    z[i] = fmaf(w[W - 1][i], cur[i], s);
+                    g[i] *= activate_slope<ACT>(z[i]);
+                    if (sums) {
+#pragma unroll
+                        for (int j = 0; j < W - 1; ++j) dw[j][i] = fmaf(g[i], win[j][i], dw[j][i]);
+                        dw[W - 1][i] = fmaf(g[i], cur[i], dw[W - 1][i]);
+                        db[i] += g[i];
+                    }
+#pragma unroll
+                    for (int j = 0; j + 2 < W; ++j) win[j][i] = win[j + 1][i];
+                    if (W > 1) win[W > 1 ? W - 2 : 0][i] = cur[i];
+                }
+            };
+            // dx of the row W - 1 before the one whose g this is
+            auto emit = [&](const float (&g)[V], T* p, bool out) {
+                float o[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    o[i] = w[0][i] * g[i];
+#pragma unroll
+                    for (int j = 0; j < W - 1; ++j) o[i] = fmaf(w[W - 1 - j][i], later[j][i], o[i]);
+#pragma unroll
+                    for (int j = 0; j + 2 < W; ++j) later[j][i] = later[j + 1][i];
+                    if (W > 1) later[W > 1 ? W - 2 : 0][i] = g[i];
+                }
+                if (out) store_vec<T, V>(p, o);
+            };
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+                for (int i = 0; i < V; ++i) later[j][i] = 0.0f;
+            T* out = dx - (W - 1) * a.C;
+#pragma unroll 1
+            for (int r = 0; r < k.run; r += kConvBatch) {
+                Vec<T, V> rx[kConvBatch], rg[kConvBatch];
+#pragma unroll
+                for (int u = 0; u < kConvBatch; ++u) rx[u] = raw_vec<T, V>(x + u * xs), rg[u] = raw_vec<T, V>(dy + u * a.C);
+#pragma unroll
+                for (int u = 0; u < kConvBatch; ++u) {
+                    float g[V];
+                    slope_row(g, rx[u], rg[u], true);
+                    emit(g, out + u * a.C, r + u >= W - 1);
+                }
+                x += (long long)kConvBatch * xs, dy += (long long)kConvBatch * a.C, out += (long long)kConvBatch * a.C;
+            }
+#pragma unroll
+            for (int u = 0; u < W - 1; ++u) {
+                float g[V];
+                slope_row(g, raw_vec<T, V>(x + u * xs), raw_vec<T, V>(dy + u * a.C), false);
+                emit(g, out + u * a.C, true);
+            }
+            continue;
+        }
         const long long last = min(left + W - 1, stop);
         for (long long r0 = 0; r0 < last; r0 += kConvBatch) {
-            float in[kConvBatch][V], gy[kConvBatch][V];
+            Vec<T, V> raw[kConvBatch], rdy[kConvBatch];
 #pragma unroll
             for (int u = 0; u < kConvBatch; ++u)
-                if (r0 + u < last) {
-                    load_vec<T, V>(in[u], x + (r0 + u) * a.x_t);
-                    load_vec<T, V>(gy[u], dy + (r0 + u) * a.C);
-                }
+                if (r0 + u < last) raw[u] = raw_vec<T, V>(x + (r0 + u) * a.x_t), rdy[u] = raw_vec<T, V>(dy + (r0 + u) * a.C);
 #pragma unroll
             for (int u = 0; u < kConvBatch; ++u) {
                 const long long r = r0 + u;
@@ -284,19 +427,21 @@ template <typename T, int V, int W, int ACT, bool kPacked> __global__ void __lau
                     }
                     continue;
                 }
-                float z[V], old[W > 1 ? W - 1 : 1][V], g[V];
+                float z[V], old[W > 1 ? W - 1 : 1][V], g[V], in[V], gy[V];
+                widen<T, V>(in, raw[u]);
+                widen<T, V>(gy, rdy[u]);
 #pragma unroll
                 for (int j = 0; j < W - 1; ++j)
 #pragma unroll
                     for (int i = 0; i < V; ++i) old[j][i] = win[j][i];
-                taps<V, W>(z, win, in[u], w, bias);
+                taps<V, W>(z, win, in, w, bias);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    g[i] = gy[u][i] * activate_slope<ACT>(z[i]);
+                    g[i] = gy[i] * activate_slope<ACT>(z[i]);
                     if (r < left) {
 #pragma unroll
                         for (int j = 0; j < W - 1; ++j) dw[j][i] = fmaf(g[i], old[j][i], dw[j][i]);
-                        dw[W - 1][i] = fmaf(g[i], in[u][i], dw[W - 1][i]);
+                        dw[W - 1][i] = fmaf(g[i], in[i], dw[W - 1][i]);
                         db[i] += g[i];
                     }
 #pragma unroll
@@ -449,9 +594,9 @@ template <typename T, int V> const void* conv_fn(ConvWhat what, int W, vmb_act a
                     : conv_fn<T, V, 4, VMB_ACT_NONE>(what, packed);
 }
 
-// 16-byte vectors of channels, or single channels where rows or pointers do not allow them.
+// Vectors of four channels, or single channels where rows or pointers do not allow them.
 bool conv_vectors(const ConvArgs& a) {
-    const int V = a.dtype == VMB_BF16 ? 8 : 4;
+    const int V = 4;
     if (a.C % V || a.x_t % V || (!a.offsets && a.B > 1 && a.x_b % V)) return false;
     for (const void* p : {a.x, (const void*)a.y, a.initial, (const void*)a.final, a.dy, a.dfinal, (const void*)a.dx, (const void*)a.state})
         if (reinterpret_cast<uintptr_t>(p) & 15) return false;
@@ -459,7 +604,7 @@ bool conv_vectors(const ConvArgs& a) {
 }
 const void* conv_kernel(const ConvArgs& a, ConvWhat what, bool vec) {
     if (a.dtype == VMB_BF16)
-        return vec ? conv_fn<__nv_bfloat16, 8>(what, a.W, a.act, a.offsets != nullptr) : conv_fn<__nv_bfloat16, 1>(what, a.W, a.act, a.offsets != nullptr);
+        return vec ? conv_fn<__nv_bfloat16, 4>(what, a.W, a.act, a.offsets != nullptr) : conv_fn<__nv_bfloat16, 1>(what, a.W, a.act, a.offsets != nullptr);
     return vec ? conv_fn<float, 4>(what, a.W, a.act, a.offsets != nullptr) : conv_fn<float, 1>(what, a.W, a.act, a.offsets != nullptr);
 }
 
@@ -474,10 +619,9 @@ void conv_runs(ConvKernel& k, int most) {
     k.runs = a.offsets ? (a.total + k.run - 1) / k.run : (long long)a.B * k.runs_per;
 }
 
-constexpr int kConvBlocksPerSm = 6;  // of the gradients' launch
 unsigned conv_bwd_blocks(const ConvKernel& k) {
     const long long want = (k.runs + k.g.ty - 1) / k.g.ty;
-    long long most = (long long)device_sm_count() * kConvBlocksPerSm / k.g.nb;
+    long long most = (long long)device_sm_count() * (k.a.dtype == VMB_BF16 ? conv_bwd_blocks_per_sm<__nv_bfloat16>() : conv_bwd_blocks_per_sm<float>()) / k.g.nb;
     if (most < 1) most = 1;
     return (unsigned)(want < 1 ? 1 : want < most ? want : most);
 }
@@ -494,9 +638,9 @@ vmb_status launch_column_sums(const float* p, int rows, long long cols, int C, i
 // One row of partial sums for each run of threads of the gradients' launch, whichever vectors it takes.
 size_t conv_workspace_bytes(int, int, long long, bool, int C, int W, vmb_dtype dtype) {
     size_t most = 0;
-    for (int V : {1, dtype == VMB_BF16 ? 8 : 4}) {
+    for (int V : {1, 4}) {
         const ConvGrid g = conv_grid((C + V - 1) / V);
-        long long blocks = (long long)device_sm_count() * kConvBlocksPerSm / g.nb;
+        long long blocks = (long long)device_sm_count() * 4 / g.nb;
         if (blocks < 1) blocks = 1;
         const size_t n = (size_t)blocks * g.ty * (W + 1) * C * 4;
         if (n > most) most = n;
@@ -506,9 +650,9 @@ size_t conv_workspace_bytes(int, int, long long, bool, int C, int W, vmb_dtype d
 
 vmb_status launch_conv_fwd(const ConvArgs& a, cudaStream_t stream) {
     const bool vec = conv_vectors(a);
-    const int V = !vec ? 1 : a.dtype == VMB_BF16 ? 8 : 4;
+    const int V = !vec ? 1 : 4;
     ConvKernel k{a, conv_grid((a.C + V - 1) / V)};
-    conv_runs(k, 16);
+    conv_runs(k, kConvRun);
     k.tile_blocks = (unsigned)((k.runs + k.g.ty - 1) / k.g.ty);
     k.partial = nullptr;
     const unsigned states = a.final && a.W > 1 ? (unsigned)(((long long)a.B + k.g.ty - 1) / k.g.ty) : 0u;
@@ -520,7 +664,7 @@ vmb_status launch_conv_fwd(const ConvArgs& a, cudaStream_t stream) {
 
 vmb_status launch_conv_bwd(const ConvArgs& a, cudaStream_t stream) {
     const bool vec = conv_vectors(a);
-    const int V = !vec ? 1 : a.dtype == VMB_BF16 ? 8 : 4;
+    const int V = !vec ? 1 : 4;
     ConvKernel k{a, conv_grid((a.C + V - 1) / V)};
     conv_runs(k, 32);
     k.tile_blocks = conv_bwd_blocks(k);
@@ -543,7 +687,7 @@ vmb_status launch_conv_bwd(const ConvArgs& a, cudaStream_t stream) {
 
 vmb_status launch_conv_step(const ConvArgs& a, cudaStream_t stream) {
     const bool vec = conv_vectors(a);
-    const int V = !vec ? 1 : a.dtype == VMB_BF16 ? 8 : 4;
+    const int V = !vec ? 1 : 4;
     ConvKernel k{a, conv_grid((a.C + V - 1) / V)};
     void* args[] = {&k};
     return launch_kernel(conv_kernel(a, kStep, vec), dim3((unsigned)(((long long)a.B + k.g.ty - 1) / k.g.ty), (unsigned)k.g.nb), dim3(kConvThreads), 0, args,

@@ -159,6 +159,8 @@ vmb_status vmb_causal_conv_bwd(const void* x, const float* weight, const float* 
     if ((s = check_workspace(workspace)) != VMB_OK) return s;
     ConvArgs a{x, weight, bias, W > 1 ? initial_state : nullptr, offsets, nullptr, nullptr, B, T, total, C, W, 0, 0, act, dtype};
     if (!take_strides(strides, 0, C, T, offsets != nullptr, &a.x_b, &a.x_t)) return VMB_ERR_INVALID_ARG;
+    if (total <= 1 || (!offsets && T == 1)) a.x_t = 0;  // (no two tokens)
+    if (a.x_t >= (1 << 24)) return VMB_ERR_UNSUPPORTED;
     a.dy = dy, a.dfinal = W > 1 ? dfinal_state : nullptr, a.dx = dx, a.dweight = dweight, a.dbias = dbias;
     a.dinitial = W > 1 ? dinitial_state : nullptr, a.ws = workspace, a.ws_bytes = workspace_bytes;
     return launch_conv_bwd(a, stream);
