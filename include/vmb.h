@@ -635,7 +635,7 @@ vmb_status vmb_group_norm_bwd(const void* x, const float* weight, const float* b
  *   (the latter two may be NULL); strides: ten values, of x, delta, Bm, Cm, z; y [B, T, D] dense,
  *   final_state [B, D, N] fp32 or NULL.  N in 1..16 (VMB_ERR_UNSUPPORTED above).
  *   saved: NULL, or vmb_token_scan_saved_bytes(...) bytes (16-byte aligned) for the state before every
- *   64 tokens, which vmb_token_scan_bwd takes.
+ *   16 tokens, which vmb_token_scan_bwd takes.
  * vmb_token_scan_bwd - given dy (dense) and dfinal_state (or NULL): dx, ddelta, dBm, dCm, dz (shapes of the
  *   inputs, dense, dtype; dz where z is), dA, dDskip, ddelta_bias, dinitial_state (fp32; the last three may be NULL).
  * vmb_token_scan_step - T tokens (a few) of every row, `state` [pool, D, N] fp32 updated in place.

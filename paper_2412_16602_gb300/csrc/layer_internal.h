@@ -47,7 +47,7 @@ struct TokenScanArgs {
     const int* offsets;
     void* y;
     float* final;
-    float* saved;  // [slots of 64 tokens][D][N] or null: the state before each chunk
+    float* saved;  // [slots of 16 tokens][D][N] or null: the state before each
     int B, T;
     long long total;
     int D, N;
@@ -66,7 +66,8 @@ struct TokenScanArgs {
     const int* slots = nullptr;
     int pool = 0;
 };
-constexpr int kScanChunk = 64;  // tokens between two saved states
+constexpr int kScanChunk = 64;  // segments are of whole chunks of so many tokens
+constexpr int kScanSaved = 16;  // tokens between two saved states
 size_t token_scan_workspace_bytes(int B, int T, long long total, bool packed, int D, int N, bool grads, vmb_dtype dtype);
 // Chunks of `chunk` tokens that B sequences of up to T tokens (packed: of `total` tokens) have at most: the chunks of packed
 // sequence b start at place offsets[b] / chunk + b.

@@ -6,6 +6,8 @@
 // channel and token bound it: the issue slots and the FMA and MUFU pipes (0.62 of the slots, 0.40 and 0.38 of the pipes), not the bytes.  Sequences too few to fill the SMs are cut into segments:
 // a first launch takes each segment from a zero state and leaves its last state and the sum of its step sizes (the product of
 // its decays is the exponential of A times that sum), and each segment of the second launch joins those before it.
+#include <initializer_list>
+
 #include "token_scan.cuh"
 
 namespace vmb {
@@ -124,8 +126,11 @@ template <typename T, int NP, bool kLocal> __global__ void __launch_bounds__(kFw
                 if (kLanes * j + p >= left) dt[j] = dtx[j] = 0.0f;
         }
         if (left > kBlk) load(left - kBlk);
-        if (!kLocal && a.saved && on && t0 % kScanChunk == 0)
-            h.store_some(a.saved + ((g.chunk + ((long long)g.s * k.seg + t0) / kScanChunk) * a.D + d) * a.N + n0, n0, a.N);
+        if (!kLocal && a.saved && on && t0 % kScanSaved == 0) {
+            float* to = a.saved + ((g.chunk + ((long long)g.s * k.seg + t0) / kScanSaved) * a.D + d) * a.N + n0;
+            if (a.N == NP) h.store(to);  // (16-byte aligned)
+            else h.store_some(to, n0, a.N);
+        }
         const float* rows = bcs[(b / kPer) & 1] + (b % kPer) * kBlk * 2 * NP + n0;
 #pragma unroll
         for (int j = 0; j < kMine; ++j) {
@@ -299,6 +304,11 @@ void token_scan_plan(ScanKernel& k, int seg) {
     k.vec = a.D % V == 0 && a.x_t % V == 0 && a.d_t % V == 0 && (!a.z || a.z_t % V == 0) && vec16(a.x) && vec16(a.delta) && vec16(a.z) &&
             vec16(a.y) && vec16(a.dy) && vec16(a.dx) && vec16(a.ddelta) && vec16(a.dz);
     if (!a.offsets && a.B > 1) k.vec = k.vec && a.x_b % V == 0 && a.d_b % V == 0 && (!a.z || a.z_b % V == 0);
+    const size_t two = a.dtype == VMB_BF16 ? 3 : 7;
+    k.pair = ((a.D | a.x_t | a.d_t | a.z_t) & 1) == 0;
+    for (const void* p : {a.x, a.delta, a.z, a.dy, (const void*)a.dx, (const void*)a.ddelta, (const void*)a.dz})
+        k.pair = k.pair && (reinterpret_cast<uintptr_t>(p) & two) == 0;
+    if (!a.offsets && a.B > 1) k.pair = k.pair && ((a.x_b | a.d_b | a.z_b) & 1) == 0;
 }
 
 size_t token_scan_forward_bytes(int B, int T, long long total, bool packed, int D, int N) {

@@ -21,7 +21,7 @@ struct ScanKernel {
     int segs_per;     // segments of a sequence (dense)
     int slots;        // places of segments; packed: the segments of sequence b start at offsets[b] / seg + b
     int tiles;        // of channels
-    bool vec;         // rows allow copies of 16 bytes
+    bool vec, pair;   // rows allow copies of 16 bytes, and of two channels
     float* local;     // [slots][D][NP]: what a segment gives from a zero state (gradients: to the state before it)
     float* decay;     // [slots][D]: the sum of a segment's step sizes
     float* bc;        // gradients: [tiles][total][32]
@@ -60,7 +60,7 @@ __device__ __forceinline__ ScanSegment scan_segment(const ScanKernel& k, long lo
         bool bad;
         sequence_span(a.offsets, g.b, a.total, &s0, &e0, &bad);
         g.place = s0 / k.seg + g.b;
-        g.chunk = s0 / kScanChunk + g.b;
+        g.chunk = s0 / kScanSaved + g.b;
         g.s = (int)(slot - g.place);
         g.seq_len = e0 - s0;
         g.first = s0;
@@ -69,7 +69,7 @@ __device__ __forceinline__ ScanSegment scan_segment(const ScanKernel& k, long lo
         g.b = (int)(slot / k.segs_per);
         g.s = (int)(slot - (long long)g.b * k.segs_per);
         g.place = (long long)g.b * k.segs_per;
-        g.chunk = (long long)g.b * ((a.T + kScanChunk - 1) / kScanChunk);
+        g.chunk = (long long)g.b * ((a.T + kScanSaved - 1) / kScanSaved);
         g.seq_len = a.T;
         g.first = (long long)g.b * a.T;
     }

@@ -77,7 +77,7 @@ vmb_status scan_sizes(int B, int* T, int64_t total, bool packed, int D, int N, v
     *empty = D == 0 || (B == 0 && total == 0);
     // (segments, at least a chunk long, of all tiles of channels are counted in 32 bits, and so are partial sums' bytes in 64)
     long long n;
-    const long long slots = scan_slots(B, *T, total, packed, kScanChunk) + 64, tiles = ((long long)D + 31) / 32;
+    const long long slots = scan_slots(B, *T, total, packed, kScanSaved) + 64, tiles = ((long long)D + 31) / 32;
     if (!count(&n, {slots, tiles}) || n > INT_MAX || !count(&n, {slots, D, 18}) || !count(&n, {tiles, total, 32})) return VMB_ERR_UNSUPPORTED;
     return VMB_OK;
 }
@@ -191,7 +191,7 @@ size_t vmb_token_scan_workspace_bytes(int B, int T, int64_t total, int packed, i
 size_t vmb_token_scan_saved_bytes(int B, int T, int64_t total, int packed, int D, int N) {
     bool empty = false;
     if (scan_sizes(B, &T, total, packed != 0, D, N, VMB_F32, &empty) != VMB_OK) return 0;
-    return empty ? 256 : (size_t)scan_slots(B, T, total, packed != 0, kScanChunk) * D * N * 4 + 256;
+    return empty ? 256 : (size_t)scan_slots(B, T, total, packed != 0, kScanSaved) * D * N * 4 + 256;
 }
 
 vmb_status vmb_token_scan_fwd(const void* x, const void* delta, const float* A, const void* Bm, const void* Cm, const float* Dskip,

@@ -126,9 +126,9 @@ def test_sizes(vmb):
     ws = vmb.vmb_token_scan_workspace_bytes
     assert ws(1, 8, 9, False, 16, 16) == 0 and ws(1, 8, 8, False, 16, 17) == 0 and ws(0, 8, 0, False, 16, 16) == 256
     assert ws(2, 100, 200, False, 64, 16, True) > ws(2, 100, 200, False, 64, 16)
-    saved = vmb.vmb_token_scan_saved_bytes  # the states before every 64 tokens
-    assert saved(3, 65, 195, False, 8, 4) == 3 * 2 * 8 * 4 * 4 + 256
-    assert saved(3, 0, 195, True, 8, 4) == (195 // 64 + 3) * 8 * 4 * 4 + 256
+    saved = vmb.vmb_token_scan_saved_bytes  # the states before every 16 tokens
+    assert saved(3, 65, 195, False, 8, 4) == 3 * 5 * 8 * 4 * 4 + 256
+    assert saved(3, 0, 195, True, 8, 4) == (195 // 16 + 3) * 8 * 4 * 4 + 256
     assert vmb.vmb_causal_conv_workspace_bytes(1, 8, 9, False, 16, 4) == 0 and vmb.vmb_causal_conv_workspace_bytes(1, 8, 8, False, 16, 5) == 0
     assert vmb.vmb_rms_norm_workspace_bytes(4, 8193) == 0 and vmb.vmb_rms_norm_workspace_bytes(0, 64) == 256
     assert vmb.vmb_linear_workspace_bytes(-1, 8, 8) == 0 and vmb.vmb_linear_workspace_bytes(0, 8, 8) == 256
