@@ -24,7 +24,7 @@ BUILD_DIR = os.path.join(PKG, "_build")
 SOURCES = ["vmb_abi.cu", "cross_scan_merge.cu", "full_scan.cu", "full_ws_f32.cu", "full_ws_bf16.cu", "mean_scan.cu", "mean_backward.cu", "noalloc.cu",
            "scan_only.cu", "selection.cu", "small_map.cu", "vmb_abi_mixer.cu", "delta.cu", "delta_f32.cu", "delta_bf16.cu",
            "rotary.cu", "group_norm.cu", "vmb_abi_layer.cu", "causal_conv.cu", "token_scan.cu", "token_scan_grad.cu",
-           "rms_norm.cu", "linear.cu", "linear_tc.cu"]
+           "rms_norm.cu", "linear.cu", "linear_tc.cu", "linear_few.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

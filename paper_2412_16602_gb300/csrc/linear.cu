@@ -157,7 +157,9 @@ LinearLayout linear_layout(long long M, int K, int N, bool grads) {
 
 vmb_status launch_gemm(const GemmProblem& p, bool bits8, const LinearArgs& a, const LinearLayout& l, cudaStream_t stream) {
     bool taken = false;
-    const vmb_status s = launch_gemm_tc(p, bits8, (float*)((char*)a.ws + l.parts), &((WsHeader*)a.ws)->err, stream, &taken);
+    vmb_status s = launch_gemm_few(p, bits8, stream, &taken);
+    if (s != VMB_OK || taken) return s;
+    s = launch_gemm_tc(p, bits8, (float*)((char*)a.ws + l.parts), &((WsHeader*)a.ws)->err, stream, &taken);
     return s != VMB_OK || taken ? s : launch_gemm_any(p, bits8, stream);
 }
 

@@ -88,6 +88,8 @@ vmb_status launch_gemm_any(const GemmProblem& p, bool bits8, cudaStream_t stream
 // Operands that tensor copies can read: one stride is 1, the other a multiple of 16 bytes, as is the base (linear_tc.cu).  *taken is false where
 // they are not, and nothing was launched.  `partial`: what gemm_partial_bytes says, of this problem.
 vmb_status launch_gemm_tc(const GemmProblem& p, bool bits8, float* partial, unsigned* err, cudaStream_t stream, bool* taken);
+// Up to 32 rows of A, contractions dense in whole vectors of 16 bytes (linear_few.cu); *taken as above.
+vmb_status launch_gemm_few(const GemmProblem& p, bool bits8, cudaStream_t stream, bool* taken);
 size_t gemm_partial_bytes(long long M, int N, long long K, bool bits8);
 
 }  // namespace vmb

@@ -278,6 +278,10 @@ template <int CG, int BN, bool kBits8, bool kArow, bool kBrow> __global__ void _
         for (int i = 0; i < 2; ++i) mbarrier_init(sums_full + 8 * i, 1), mbarrier_init(sums_empty + 8 * i, CG * kTcEpiWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (tid == 32 * 3) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&k.ta)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&k.tb)) : "memory");
+    }
     if (warp == 1) {
         if constexpr (CG == 2) {
             asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "n"(kCols));
@@ -461,8 +465,9 @@ struct TcPlan {
 };
 long long up(long long a, long long b) { return (a + b - 1) / b; }
 
-// By estimated clocks: a stage of the contraction takes a pair 512 of them for 256 x 256 sums and one CTA 300 for 128 x 128 (its operands' bytes in shared
-// memory bound it there), a tile 2000 to begin and end, a join 5000 and 8 bytes of traffic for each part's sum.
+// By estimated clocks: a stage of the contraction takes a pair 512 of them for 256 x 256 sums and one CTA 300 for 128 x 128, a tile 2000 to begin and end, a
+// join 5000 and 8 bytes of traffic for each part's sum.  (128 x 2048 x 4096: 14.1 us so, by 32 CTAs in no parts 16.9; the bytes into an SM, 64 a clock, say 512 for
+// 128 x 128 too, but with that the split cases came out slower: 18.4.)
 TcPlan tc_plan(long long M, int N, long long K, bool bits8) {
     const int sms = device_sm_count();
     const long long kblocks = up(K, bits8 ? 128 : 64);

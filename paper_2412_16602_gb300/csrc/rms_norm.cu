@@ -5,9 +5,10 @@
 //   y = s r w;   in 8 bits: y / scale with scale = max |y| / 448 of the row (448: the largest e4m3 value).
 //   dx = r (w dy - n mean(w dy n)) + dsum, n = s r (the residual's gradient is the same),  dw = sum over rows of dy n.
 //
-// Bound by memory: each value is read once and held in registers between the sums and the output.  A row is held by a power of
-// two of threads, from one warp to 512, so that a thread has at most kVecs vectors of it; a block of 128 threads holds up to
-// four rows.
+// Bound by memory: each value is read once and held in registers between the sums and the output.  In the forward a row
+// belongs to one warp where 32 values a thread hold it, so that its sums need no barrier (16384 x 1536 in bf16 with the residual's addition: 31 us in two warps
+// of 24 values a thread, in one of 48 36 us; 8 bits 40 us, with 64 registers a thread); in the gradients, which hold six values for each and the next
+// row's, to as many threads as hold it in two or three vectors.
 #include <cuda_fp8.h>
 
 #include <initializer_list>
@@ -23,7 +24,6 @@ namespace {
 constexpr int kRmsBlock = 128;
 constexpr float kLeastScale = 7.888609052210118e-31f;  // 2^-100: rows of zeros keep a scale that can be divided by
 
-template <int V> constexpr int vecs_of() { return V == 1 ? 16 : 4; }  // vectors of a thread
 
 struct RmsKernel {
     RmsArgs a;
@@ -62,8 +62,7 @@ template <int V> __device__ __forceinline__ void store_e4m3(uint8_t* p, const fl
     }
 }
 
-template <typename T, int V, bool kBits8> __global__ void __launch_bounds__(512) rms_fwd_kernel(RmsKernel k) {
-    constexpr int NV = vecs_of<V>();
+template <typename T, int V, int NV, bool kBits8> __global__ void __launch_bounds__(512, kBits8 ? 2 : 1) rms_fwd_kernel(RmsKernel k) {
     __shared__ float scratch[32];
     const RmsArgs& a = k.a;
     pdl_wait();
@@ -74,21 +73,23 @@ template <typename T, int V, bool kBits8> __global__ void __launch_bounds__(512)
     const T *x = (const T*)a.x + row * a.C, *res = (const T*)a.residual + row * a.C;
     float s[NV][V];
     float ss = 0.0f;
+    Vec<T, V> rx[NV], rr[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int c = (lx + j * k.lanes) * V;
-#pragma unroll
-        for (int i = 0; i < V; ++i) s[j][i] = 0.0f;
+        rx[j] = rr[j] = Vec<T, V>{};
         if (live && c < a.C) {
-            load_vec<T, V>(s[j], x + c);
-            if (a.residual) {
-                float r[V];
-                load_vec<T, V>(r, res + c);
-#pragma unroll
-                for (int i = 0; i < V; ++i) s[j][i] = io<T>::cvt(io<T>::to(s[j][i] + r[i]));
-            }
+            rx[j] = *reinterpret_cast<const Vec<T, V>*>(x + c);
+            if (a.residual) rr[j] = *reinterpret_cast<const Vec<T, V>*>(res + c);
         }
     }
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            s[j][i] = io<T>::cvt(rx[j].v[i]);
+            if (a.residual) s[j][i] = io<T>::cvt(io<T>::to(s[j][i] + io<T>::cvt(rr[j].v[i])));
+        }
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int c = (lx + j * k.lanes) * V;
@@ -131,8 +132,7 @@ template <typename T, int V, bool kBits8> __global__ void __launch_bounds__(512)
 }
 
 // Gradients: a block takes rows in turn and keeps its sums of dw in registers, one row of partial sums at its end.
-template <typename T, int V> __global__ void __launch_bounds__(512) rms_bwd_kernel(RmsKernel k) {
-    constexpr int NV = vecs_of<V>();
+template <typename T, int V, int NV> __global__ void __launch_bounds__(512) rms_bwd_kernel(RmsKernel k) {
     __shared__ float scratch[32];
     const RmsArgs& a = k.a;
     pdl_wait();
@@ -143,37 +143,48 @@ template <typename T, int V> __global__ void __launch_bounds__(512) rms_bwd_kern
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < V; ++i) dw[j][i] = 0.0f;
-    for (long long r0 = (long long)blockIdx.x * k.rows_per; r0 < a.rows; r0 += (long long)gridDim.x * k.rows_per) {
-        const long long row = r0 + ly;
+    const long long step = (long long)gridDim.x * k.rows_per;
+    Vec<T, V> rx[NV], rd[NV], rg[NV];
+    float next = 0.0f;  // rstd of the row under way
+    auto load = [&](long long row) {
         const bool live = row < a.rows;
-        const float rstd = live ? a.rstd[row] : 0.0f;
-        float n[NV][V], d[NV][V], dot = 0.0f;
+        next = live ? a.rstd[row] : 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (lx + j * k.lanes) * V;
-#pragma unroll
-            for (int i = 0; i < V; ++i) n[j][i] = d[j][i] = 0.0f;
+            rx[j] = rd[j] = rg[j] = Vec<T, V>{};
             if (live && c < a.C) {
-                load_vec<T, V>(n[j], (const T*)a.x + row * a.C + c);
-                load_vec<T, V>(d[j], (const T*)a.dy + row * a.C + c);
+                rx[j] = *reinterpret_cast<const Vec<T, V>*>((const T*)a.x + row * a.C + c);
+                rd[j] = *reinterpret_cast<const Vec<T, V>*>((const T*)a.dy + row * a.C + c);
+                if (a.dsum) rg[j] = *reinterpret_cast<const Vec<T, V>*>((const T*)a.dsum + row * a.C + c);
             }
         }
+    };
+    load((long long)blockIdx.x * k.rows_per + ly);
+    for (long long r0 = (long long)blockIdx.x * k.rows_per; r0 < a.rows; r0 += step) {
+        const long long row = r0 + ly;
+        const bool live = row < a.rows;
+        const float rstd = next;
+        float n[NV][V], d[NV][V], dot = 0.0f;
+        Vec<T, V> more[NV];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (lx + j * k.lanes) * V;
-            if (!live || c >= a.C) continue;
+            more[j] = rg[j];
             float w[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) w[i] = 1.0f;
-            if (a.weight) load_vec<float, V>(w, a.weight + c);
+            if (a.weight && c < a.C) load_vec<float, V>(w, a.weight + c);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                n[j][i] *= rstd;
+                n[j][i] = io<T>::cvt(rx[j].v[i]) * rstd;
+                d[j][i] = io<T>::cvt(rd[j].v[i]);
                 dw[j][i] = fmaf(d[j][i], n[j][i], dw[j][i]);
                 d[j][i] *= w[i];
                 dot = fmaf(d[j][i], n[j][i], dot);
             }
         }
+        load(row + step);  // under way while this row's sum is joined
         dot = row_join<false>(dot, k.lanes, scratch) / (float)a.C;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -181,10 +192,7 @@ template <typename T, int V> __global__ void __launch_bounds__(512) rms_bwd_kern
             if (!live || c >= a.C) continue;
             float g[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) g[i] = 0.0f;
-            if (a.dsum) load_vec<T, V>(g, (const T*)a.dsum + row * a.C + c);
-#pragma unroll
-            for (int i = 0; i < V; ++i) g[i] = fmaf(rstd, fmaf(-n[j][i], dot, d[j][i]), g[i]);
+            for (int i = 0; i < V; ++i) g[i] = fmaf(rstd, fmaf(-n[j][i], dot, d[j][i]), io<T>::cvt(more[j].v[i]));
             store_vec<T, V>((T*)a.dx + row * a.C + c, g);
         }
     }
@@ -199,11 +207,35 @@ template <typename T, int V> __global__ void __launch_bounds__(512) rms_bwd_kern
     }
 }
 
-int rms_lanes(int C, int V) {
-    const int per = V * (V == 1 ? vecs_of<1>() : vecs_of<4>());
+// Vectors that a thread may hold of a row, and the threads of a row: a power of two of warps.
+// (8192 channels in 512 threads are two vectors of eight, four of four or sixteen single channels each.)
+constexpr int kFwdMost = 4;
+int rms_most(int V, bool grads) { return V == 1 ? 16 : !grads ? (V == 8 ? kFwdMost : 8) : V == 8 ? 2 : 3; }
+int rms_lanes(int C, int V, bool grads) {
     int lanes = 32;
-    while (lanes * per < C) lanes *= 2;
+    while (lanes < 512 && lanes * V * rms_most(V, grads) < C) lanes *= 2;
     return lanes;
+}
+// Vectors that a thread does hold: of these a kernel is made for each of a few numbers.
+int rms_vecs(int C, int V, int lanes) { return ((C + V - 1) / V + lanes - 1) / lanes; }
+template <typename T, int V, bool kBits8> const void* rms_fwd_fn(int nv) {
+    if constexpr (V == 1) return (const void*)rms_fwd_kernel<T, 1, 16, kBits8>;
+    else
+        return nv <= 1   ? (const void*)rms_fwd_kernel<T, V, 1, kBits8>
+               : nv <= 2 ? (const void*)rms_fwd_kernel<T, V, 2, kBits8>
+               : nv <= 3 ? (const void*)rms_fwd_kernel<T, V, 3, kBits8>
+               : nv <= 4 ? (const void*)rms_fwd_kernel<T, V, 4, kBits8>
+               : nv <= 6 ? (const void*)rms_fwd_kernel<T, V, 6, kBits8>
+                         : (const void*)rms_fwd_kernel<T, V, 8, kBits8>;
+}
+template <typename T, int V> const void* rms_bwd_fn(int nv) {
+    if constexpr (V == 1) return (const void*)rms_bwd_kernel<T, 1, 16>;
+    else if constexpr (V == 8) return nv <= 1 ? (const void*)rms_bwd_kernel<T, V, 1> : (const void*)rms_bwd_kernel<T, V, 2>;
+    else
+        return nv <= 1   ? (const void*)rms_bwd_kernel<T, V, 1>
+               : nv <= 2 ? (const void*)rms_bwd_kernel<T, V, 2>
+               : nv <= 3 ? (const void*)rms_bwd_kernel<T, V, 3>
+                         : (const void*)rms_bwd_kernel<T, V, 4>;
 }
 int rms_width(vmb_dtype dt) { return dt == VMB_BF16 ? 8 : 4; }
 
@@ -221,8 +253,8 @@ long long rms_bwd_blocks(long long rows, int rows_per, int block) {
     return want < most ? want : most;
 }
 
-void rms_shape(RmsKernel& k, int V, int* block) {
-    k.lanes = rms_lanes(k.a.C, V);
+void rms_shape(RmsKernel& k, int V, bool grads, int* block) {
+    k.lanes = rms_lanes(k.a.C, V, grads);
     *block = k.lanes > kRmsBlock ? k.lanes : kRmsBlock;
     k.rows_per = *block / k.lanes;
 }
@@ -232,7 +264,7 @@ void rms_shape(RmsKernel& k, int V, int* block) {
 size_t rms_workspace_bytes(long long rows, int C, vmb_dtype dtype) {
     size_t most = 0;
     for (int V : {1, rms_width(dtype)}) {
-        const int lanes = rms_lanes(C, V), block = lanes > kRmsBlock ? lanes : kRmsBlock;
+        const int lanes = rms_lanes(C, V, true), block = lanes > kRmsBlock ? lanes : kRmsBlock;
         const size_t n = (size_t)rms_bwd_blocks(rows, block / lanes, block) * (block / lanes) * C * 4;
         if (n > most) most = n;
     }
@@ -242,15 +274,16 @@ size_t rms_workspace_bytes(long long rows, int C, vmb_dtype dtype) {
 vmb_status launch_rms_fwd(const RmsArgs& a, cudaStream_t stream) {
     RmsKernel k{a};
     const bool vec = rms_vectors(a);
+    const int V = vec ? rms_width(a.dtype) : 1;
     int block;
-    rms_shape(k, vec ? rms_width(a.dtype) : 1, &block);
+    rms_shape(k, V, false, &block);
+    const int nv = rms_vecs(a.C, V, k.lanes);
     const void* fn;
     if (a.dtype == VMB_BF16)
-        fn = a.bits8 ? (vec ? (const void*)rms_fwd_kernel<__nv_bfloat16, 8, true> : (const void*)rms_fwd_kernel<__nv_bfloat16, 1, true>)
-                     : (vec ? (const void*)rms_fwd_kernel<__nv_bfloat16, 8, false> : (const void*)rms_fwd_kernel<__nv_bfloat16, 1, false>);
+        fn = a.bits8 ? (vec ? rms_fwd_fn<__nv_bfloat16, 8, true>(nv) : rms_fwd_fn<__nv_bfloat16, 1, true>(nv))
+                     : (vec ? rms_fwd_fn<__nv_bfloat16, 8, false>(nv) : rms_fwd_fn<__nv_bfloat16, 1, false>(nv));
     else
-        fn = a.bits8 ? (vec ? (const void*)rms_fwd_kernel<float, 4, true> : (const void*)rms_fwd_kernel<float, 1, true>)
-                     : (vec ? (const void*)rms_fwd_kernel<float, 4, false> : (const void*)rms_fwd_kernel<float, 1, false>);
+        fn = a.bits8 ? (vec ? rms_fwd_fn<float, 4, true>(nv) : rms_fwd_fn<float, 1, true>(nv)) : (vec ? rms_fwd_fn<float, 4, false>(nv) : rms_fwd_fn<float, 1, false>(nv));
     void* args[] = {&k};
     return launch_kernel(fn, dim3((unsigned)((a.rows + k.rows_per - 1) / k.rows_per)), dim3(block), 0, args, stream) == cudaSuccess ? VMB_OK : VMB_ERR_CUDA;
 }
@@ -258,8 +291,10 @@ vmb_status launch_rms_fwd(const RmsArgs& a, cudaStream_t stream) {
 vmb_status launch_rms_bwd(const RmsArgs& a, cudaStream_t stream) {
     RmsKernel k{a};
     const bool vec = rms_vectors(a);
+    const int V = vec ? rms_width(a.dtype) : 1;
     int block;
-    rms_shape(k, vec ? rms_width(a.dtype) : 1, &block);
+    rms_shape(k, V, true, &block);
+    const int nv = rms_vecs(a.C, V, k.lanes);
     const long long blocks = rms_bwd_blocks(a.rows, k.rows_per, block);
     const long long parts = blocks * k.rows_per;
     k.partial = nullptr;
@@ -267,8 +302,8 @@ vmb_status launch_rms_bwd(const RmsArgs& a, cudaStream_t stream) {
         if (a.ws_bytes < (size_t)parts * a.C * 4 + 256) return VMB_ERR_WORKSPACE;
         k.partial = (float*)((char*)a.ws + 256);
     }
-    const void* fn = a.dtype == VMB_BF16 ? (vec ? (const void*)rms_bwd_kernel<__nv_bfloat16, 8> : (const void*)rms_bwd_kernel<__nv_bfloat16, 1>)
-                                         : (vec ? (const void*)rms_bwd_kernel<float, 4> : (const void*)rms_bwd_kernel<float, 1>);
+    const void* fn = a.dtype == VMB_BF16 ? (vec ? rms_bwd_fn<__nv_bfloat16, 8>(nv) : rms_bwd_fn<__nv_bfloat16, 1>(nv))
+                                         : (vec ? rms_bwd_fn<float, 4>(nv) : rms_bwd_fn<float, 1>(nv));
     void* args[] = {&k};
     if (launch_kernel(fn, dim3((unsigned)blocks), dim3(block), 0, args, stream) != cudaSuccess) return VMB_ERR_CUDA;
     return a.dweight ? launch_column_sums(k.partial, (int)parts, a.C, a.C, 1, a.dweight, nullptr, 0, nullptr, stream) : VMB_OK;

@@ -280,8 +280,10 @@ class Workspace:
     being captured into a graph every call gets a buffer of its own, which the graph fills and holds: a kept one would be
     shared by the graph's replays and later calls, and one made during the capture is not filled before a replay."""
 
-    def __init__(self):
+    def __init__(self, header: int = 0):
+        """`header`: the bytes that have to be zero at first; 0: all."""
         self._local = threading.local()
+        self._header = header
 
     def buffers(self) -> dict:
         """(device index, raw stream) -> buffer, of the calling thread."""
@@ -298,7 +300,12 @@ class Workspace:
         buf = bufs.get(key)
         if buf is None or buf.numel() < nbytes or capturing:
             n = (max(nbytes, 256) + 255) // 256 * 256
-            buf = torch.zeros(n, dtype=torch.uint8, device=torch.device("cuda", index))
+            device = torch.device("cuda", index)
+            if self._header:  # (a call captured into a graph gets a buffer of its own: the rest is not filled at every replay)
+                buf = torch.empty(n, dtype=torch.uint8, device=device)
+                buf[:self._header].zero_()
+            else:
+                buf = torch.zeros(n, dtype=torch.uint8, device=device)
             if not capturing:
                 bufs[key] = buf
         return buf
@@ -796,7 +803,7 @@ _ACTS = {"none": VMB_ACT_NONE, "silu": VMB_ACT_SILU, "gelu": VMB_ACT_GELU}
 # workspaces of their own: the scans' must keep what the scans left in theirs
 _delta_ws = Workspace()
 _norm_ws = Workspace()
-_layer_ws = Workspace()
+_layer_ws = Workspace(header=256)
 
 
 # (a step of one token takes 2.5 us on the device: the marshalling below keeps to what it needs)
@@ -1172,6 +1179,11 @@ def _like(t, name: str, shape, dtype):
             raise ValueError(f"{name} must be {list(shape)} in the dtype of x")
 
 
+def _empty(x, dense):
+    """A dense tensor like x (one call into torch where x is dense itself)."""
+    return torch.empty_like(x) if dense else x.new_empty(x.shape)
+
+
 def _sequences(offsets, B, T):
     """(sequences, their length, tokens) of dense [B, T] or packed [1, tokens] inputs."""
     if offsets is None:
@@ -1289,8 +1301,9 @@ def vmb_causal_conv_step(x, weight, bias, state, *, act: str = "silu", slots=Non
     _like(state, "state", (state.shape[0], W - 1, C), x.dtype)
     _pool(state, slots, B)
     if y is None:
-        y = x.new_empty((B, T, C))
-    _like(y, "y", (B, T, C), x.dtype)
+        y = _empty(x, strides is None)
+    else:
+        _like(y, "y", (B, T, C), x.dtype)
     _one_device(x, weight, bias, state, slots, y)
     _check(lib.vmb_causal_conv_step(x.data_ptr(), weight.data_ptr(), _ptr(bias), strides, state.data_ptr(), _ptr(slots),
                                     y.data_ptr(), B, T, C, W, state.shape[0], a, code, _stream_of(x, stream)),
@@ -1407,8 +1420,9 @@ def vmb_token_scan_step(x, delta, A, Bm, Cm, Dskip, delta_bias, z, state, *, sof
     _float(state, "state", (state.shape[0], D, N))
     _pool(state, slots, B)
     if y is None:
-        y = x.new_empty((B, T, D))
-    _like(y, "y", (B, T, D), x.dtype)
+        y = _empty(x, x.is_contiguous())
+    else:
+        _like(y, "y", (B, T, D), x.dtype)
     _one_device(x, delta, A, Bm, Cm, Dskip, delta_bias, z, state, slots, y)
     _check(lib.vmb_token_scan_step(x.data_ptr(), delta.data_ptr(), A.data_ptr(), Bm.data_ptr(), Cm.data_ptr(), _ptr(Dskip),
                                    _ptr(delta_bias), _ptr(z), strides, state.data_ptr(), _ptr(slots), y.data_ptr(), B, T, D, N,
