@@ -613,6 +613,8 @@ vmb_status vmb_group_norm_bwd(const void* x, const float* weight, const float* b
  *   rows that no sequence holds are zero in the outputs and in the gradients.
  *   slots: NULL (row b uses state b; pool >= B), or int32 [B] on the device: the state of row b; rows
  *   whose slot is outside [0, pool) have none: their outputs are zero.  Slots in use are distinct.
+ *   At most 2^30 - 1 tokens, 2^24 sequences and 2^22 channels (VMB_ERR_UNSUPPORTED above), and for the
+ *   scan and the gradients of the convolution fewer than 2^24 elements between tokens.
  *   Gradients are deterministic: sums in a fixed order.
  *   Workspaces are 256-byte aligned, the first 256 bytes zero-filled before the first use; calls that
  *   share one must not overlap in time.
@@ -656,7 +658,10 @@ vmb_status vmb_group_norm_bwd(const void* x, const float* weight, const float* b
  *   [M, N] bf16 or NULL, y [M, N] bf16, pre [M, N] bf16 or NULL: z, for vmb_linear_bwd.
  *   x_scale, weight_scale: both NULL: x and weight are bf16; x_scale [M] and weight_scale [N] fp32: they are e4m3
  *   values to be multiplied by the scale of their row (what vmb_rms_norm_fwd writes in 8 bits).
- *   Products are exact and summed in fp32 by the tensor cores; one rounding, to y.
+ *   Products are exact and summed in fp32 by the tensor cores; one rounding, to y.  SiLU and GELU keep 12 bits, also
+ *   where they are small.  Any K, N and x_stride; rows of whole vectors of 16 bytes (K, x_stride and, for the gradients, N multiples of 8;
+ *   16 with e4m3) take the fast kernels.  Waits of the kernels are bounded; one that gave up is VMB_ERR_TIMEOUT in
+ *   vmb_read_status.
  * vmb_linear_bwd - given dy [M, N] bf16: dZ = dy act'(pre) (rounded to bf16; pre may be NULL without an
  *   activation), dx = dZ weight [M, K], dweight = dZ^T x [N, K] (bf16; either may be NULL), dbias [N] fp32 (or NULL) the
  *   sums of dZ before its rounding.

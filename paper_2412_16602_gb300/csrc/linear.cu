@@ -157,9 +157,7 @@ LinearLayout linear_layout(long long M, int K, int N, bool grads) {
 
 vmb_status launch_gemm(const GemmProblem& p, bool bits8, const LinearArgs& a, const LinearLayout& l, cudaStream_t stream) {
     bool taken = false;
-    vmb_status s = launch_gemm_few(p, bits8, stream, &taken);
-    if (s != VMB_OK || taken) return s;
-    s = launch_gemm_tc(p, bits8, (float*)((char*)a.ws + l.parts), &((WsHeader*)a.ws)->err, stream, &taken);
+    const vmb_status s = launch_gemm_tc(p, bits8, (float*)((char*)a.ws + l.parts), &((WsHeader*)a.ws)->err, stream, &taken);
     return s != VMB_OK || taken ? s : launch_gemm_any(p, bits8, stream);
 }
 
@@ -179,11 +177,14 @@ vmb_status launch_gemm_any(const GemmProblem& p0, bool bits8, cudaStream_t strea
 size_t linear_workspace_bytes(long long M, int K, int N, bool grads) { return linear_layout(M, K, N, grads).bytes; }
 
 vmb_status launch_linear_fwd(const LinearArgs& a, cudaStream_t stream) {
-    const LinearLayout l = linear_layout(a.M, a.K, a.N, false);
-    if (a.ws_bytes < l.bytes) return VMB_ERR_WORKSPACE;
+    if (a.ws_bytes < 256) return VMB_ERR_WORKSPACE;
     const GemmProblem p{a.x, a.weight, a.M, a.N, a.K, a.x_t, 1, a.K, 1,
                         {a.x_scale, a.weight_scale, a.bias, (const __nv_bfloat16*)a.residual, (__nv_bfloat16*)a.y, (__nv_bfloat16*)a.pre, a.act}};
-    return launch_gemm(p, a.x_scale != nullptr, a, l, stream);
+    bool taken = false;
+    const vmb_status s = launch_gemm_few(p, a.x_scale != nullptr, stream, &taken);
+    if (s != VMB_OK || taken) return s;
+    const LinearLayout l = linear_layout(a.M, a.K, a.N, false);
+    return a.ws_bytes < l.bytes ? VMB_ERR_WORKSPACE : launch_gemm(p, a.x_scale != nullptr, a, l, stream);
 }
 
 vmb_status launch_linear_bwd(const LinearArgs& a, cudaStream_t stream) {

@@ -474,10 +474,11 @@ TcPlan tc_plan(long long M, int N, long long K, bool bits8) {
     TcPlan best{};
     double least = 0.0;
     for (int cg = 2; cg >= 1; --cg) {
-        const long long tm = up(M, 128 * cg), tn = up(N, 128 * cg), slots = sms / cg;
+        const long long tm = up(M, 128 * cg), tn = up(N, 128 * cg), slots = sms > cg ? sms / cg : 1;  // (without a device there is one SM)
         for (long long want = 1; want <= 64; ++want) {
             const long long kper = up(kblocks, want), splits = up(kblocks, kper);
-            if (splits != want || (want > 1 && (kper < 4 || tm * tn * want > 2 * slots))) continue;
+            if (want > 1 && (kper < 4 || tm * tn * want > 2 * slots)) break;
+            if (splits != want) continue;
             double t = (double)up(tm * tn * splits, slots) * (kper * (cg == 2 ? 512.0 : 300.0) + 2000.0);
             if (splits > 1) t += 5000.0 + (double)M * N * splits * 8.0 / 3500.0;
             if (best.cg == 0 || t < least) least = t, best = TcPlan{cg, (int)tm, (int)tn, (int)splits, (int)kblocks, (int)kper};
@@ -544,7 +545,7 @@ vmb_status launch_gemm_tc(const GemmProblem& p, bool bits8, float* partial, unsi
     k.vec = epilogue_vectors(p);
     const void* fn = plan.cg == 2 ? tc_kernel<2>(bits8, arow, brow) : tc_kernel<1>(bits8, arow, brow);
     if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem) != cudaSuccess) return VMB_ERR_CUDA;
-    const int slots = device_sm_count() / plan.cg;
+    const int sms = device_sm_count(), slots = sms > plan.cg ? sms / plan.cg : 1;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)((k.units < slots ? k.units : slots) * plan.cg));
     cfg.blockDim = dim3(kTcThreads);

@@ -41,7 +41,7 @@ vmb_status token_sizes(int B, int* T, int64_t total, bool packed, int C, int W, 
     if (!dtype_ok(dt) || B < 0 || C < 0 || W < 0 || total < 0 || (!packed && *T < 0)) return VMB_ERR_INVALID_ARG;
     if (!packed && (!count(&n, {B, *T}) || n != total)) return VMB_ERR_INVALID_ARG;
     if (!count(&n, {total, C > W ? C : W}) || !count(&n, {B, W, C})) return VMB_ERR_INVALID_ARG;
-    if (total > INT_MAX / 2 || B > (1 << 24) || C > (1 << 24)) return VMB_ERR_UNSUPPORTED;
+    if (total > INT_MAX / 2 || B > (1 << 24) || C > (1 << 22)) return VMB_ERR_UNSUPPORTED;  // (rows and grids in 32 bits)
     if (packed) *T = (int)total;
     return VMB_OK;
 }

@@ -1024,7 +1024,7 @@ def _ints(values):
 
 def _rotary_out(x, out, name, dense):
     if out is None:
-        return torch.empty_like(x) if dense else x.new_empty(x.shape)
+        return torch.empty_like(x) if dense else torch.empty(x.shape, dtype=x.dtype, device=x.device)
     _dev(out, name)
     if out.shape != x.shape or out.dtype != x.dtype:
         raise ValueError(f"{name} must have the shape and dtype of its input")
@@ -1181,7 +1181,7 @@ def _like(t, name: str, shape, dtype):
 
 def _empty(x, dense):
     """A dense tensor like x (one call into torch where x is dense itself)."""
-    return torch.empty_like(x) if dense else x.new_empty(x.shape)
+    return torch.empty_like(x) if dense else torch.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
 def _sequences(offsets, B, T):
@@ -1256,8 +1256,9 @@ def vmb_causal_conv_fwd(x, weight, bias=None, *, act: str = "silu", initial_stat
         final_state = x.new_empty((n, W - 1, C))
     _like(final_state, "final_state", (n, W - 1, C), x.dtype)
     if y is None:
-        y = x.new_empty((B, T, C))
-    _like(y, "y", (B, T, C), x.dtype)
+        y = _empty(x, strides is None)
+    else:
+        _like(y, "y", (B, T, C), x.dtype)
     _one_device(x, weight, bias, initial_state, offsets, y, final_state)
     _check(lib.vmb_causal_conv_fwd(x.data_ptr(), weight.data_ptr(), _ptr(bias), strides, _ptr(initial_state), _ptr(offsets),
                                    y.data_ptr(), _ptr(final_state), n, T1, total, C, W, a, code, _stream_of(x, stream)),
@@ -1321,17 +1322,24 @@ def vmb_token_scan_saved_bytes(B: int, T: int, total: int, packed: bool, D: int,
 
 
 def _token_scan_inputs(x, delta, A, Bm, Cm, Dskip, delta_bias, z):
-    code = _dtype_code(x.dtype)
+    dtype = x.dtype
+    code = _dtype_code(dtype)
     if x.dim() != 3 or A.dim() != 2:
         raise ValueError("x [B, T, D] and A [D, N] expected")
-    B, T, D = x.shape
+    B, T, D = shape = x.shape
     N = A.shape[1]
-    strides = [*_rows(x, "x", B, T, D, x.dtype), *_rows(delta, "delta", B, T, D, x.dtype),
-               *_rows(Bm, "Bm", B, T, N, x.dtype), *_rows(Cm, "Cm", B, T, N, x.dtype)]
-    strides += [0, 0] if z is None else _rows(z, "z", B, T, D, x.dtype)
     _float(A, "A", (D, N))
     _float(Dskip, "Dskip", (D,))
     _float(delta_bias, "delta_bias", (D,))
+    states = (B, T, N)
+    if (x.is_contiguous() and delta.is_contiguous() and Bm.is_contiguous() and Cm.is_contiguous() and (z is None or z.is_contiguous())
+            and x.is_cuda and delta.is_cuda and Bm.is_cuda and Cm.is_cuda and (z is None or z.is_cuda)
+            and delta.shape == shape and Bm.shape == states and Cm.shape == states and (z is None or z.shape == shape)
+            and delta.dtype == dtype and Bm.dtype == dtype and Cm.dtype == dtype and (z is None or z.dtype == dtype)):
+        return B, T, D, N, code, None
+    strides = [*_rows(x, "x", B, T, D, dtype), *_rows(delta, "delta", B, T, D, dtype),
+               *_rows(Bm, "Bm", B, T, N, dtype), *_rows(Cm, "Cm", B, T, N, dtype)]
+    strides += [0, 0] if z is None else _rows(z, "z", B, T, D, dtype)
     return B, T, D, N, code, (ctypes.c_int64 * 10)(*strides)
 
 
@@ -1361,8 +1369,9 @@ def vmb_token_scan_fwd(x, delta, A, Bm, Cm, Dskip=None, delta_bias=None, z=None,
         final_state = torch.empty((n, D, N), dtype=torch.float32, device=x.device)
     _float(final_state, "final_state", (n, D, N))
     if y is None:
-        y = x.new_empty((B, T, D))
-    _like(y, "y", (B, T, D), x.dtype)
+        y = _empty(x, x.is_contiguous())
+    else:
+        _like(y, "y", (B, T, D), x.dtype)
     if saved is not None:
         _token_scan_saved(saved, n, T1, total, packed, D, N)
     elif want_saved:

@@ -180,6 +180,25 @@ def test_activations_of_what_is_not_finite(vmb):
             assert (y[:, 0] == float("inf")).all() and y[:, 2].isnan().all() and not y[:, [3, 4, 6]].any() and (y[:, 5] == 300).all(), act
 
 
+def test_rows_that_tensor_copies_refuse(vmb, force_plan):
+    """The kernel of any strides at sizes that the others take."""
+    r = rand(10)
+    x, w, b, res, dy = r(300, 264).to(BF16), (r(520, 264) / 16).to(BF16), r(520), r(300, 520).to(BF16), r(300, 520).to(BF16)
+    force_plan.refuse_tensor_maps()
+    close(vmb.vmb_linear_fwd(x, w, b, act="silu", residual=res)[0], product(x, w, b, "silu", res)[0], 264)
+    d = vmb.vmb_linear_bwd(x, w, dy)
+    assert ref.rel(d["x"], dy.double() @ w.double()) <= tol(520) and ref.rel(d["weight"], dy.double().t() @ x.double()) <= tol(300)
+
+
+def test_rows_of_x_all_the_same(vmb):
+    """x expanded from one row: a stride of zero between its rows."""
+    r = rand(11)
+    x, w = r(1, 64).to(BF16), (r(72, 64) / 8).to(BF16)
+    for M in (5, 50, 200):
+        y = vmb.vmb_linear_fwd(x.expand(M, 64), w)[0]
+        close(y, product(x.expand(M, 64), w, None, "none", None)[0], 64)
+
+
 def test_empty(vmb):
     r = rand(9)
     assert vmb.vmb_linear_fwd(r(0, 8).to(BF16), r(4, 8).to(BF16))[0].shape == (0, 4)
