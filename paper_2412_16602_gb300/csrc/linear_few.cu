@@ -4,7 +4,7 @@
 // at the same place in the contraction: which of its values meet in which product of a step is free as long as both sides agree,
 // so the fragments of mma.sync are whole vectors from global memory and nothing passes through shared memory but the warps' sums,
 // which are joined in order.  e4m3 values are widened to f16, which holds them exactly.
-// 1 x 2048 x 4096 in bf16: 16.8 MB.
+// 1 x 2048 x 4096 in bf16, 16.8 MB: 6.8 us (through tiles of 128 rows on the tensor cores 10.3), 32 rows 9.3; eight steps ahead instead of four 7.2.
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 

@@ -6,6 +6,13 @@
 // of 128 bytes of the contraction, swizzled by 128 bytes; one thread of the pair issues the products; eight warps take the sums of one buffer of
 // tensor memory through the epilogue while the products of the next tile go to the other.  Where tiles are few and the contraction long
 // it is split, the parts' sums are kept in fp32 and joined in order by a second launch.
+//
+// 8192^3 in bf16: 582 us, 1889 TFLOP/s (the library's product 542); 16384 x 1536 x 6144 in bf16 183 (165), in e4m3 109, with GELU 140.  Long contractions are
+// bound by the products and by the bytes into an SM alike (32 KB and 512 clocks a stage); short ones by the epilogue, whose two warps on each
+// scheduler wait for their own results in turn (0.35 instructions a clock): with a quarter of the products issued that last case takes the same.
+// Tried: outputs by tensor copies from shared memory (130 without GELU, 173 with it: each needs a proxy fence), sixteen warps (96 registers: 128 and 156), factors and biases
+// asked for a tile ahead (no change), four stages of the ring (8192^3 652).  Arrivals at the pair's barrier carry no release at the cluster's scope: what they
+// order are tensor-memory reads, by the tcgen05 fences; with it a warp waited for its stores (151 with GELU).
 // Every wait is bounded; one that gives up leaves kErrTimeout in the workspace's header and ends the kernel.
 #include <cuda.h>
 #include <cudaTypedefs.h>
@@ -98,7 +105,7 @@ template <int CG> __device__ __forceinline__ void tc_load(uint32_t dst, const CU
 
 __device__ __forceinline__ bool tc_test(uint32_t bar, uint32_t parity) {
     uint32_t done;
-    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
                  : "=r"(done)
                  : "r"(bar), "r"(parity)
                  : "memory");
@@ -406,7 +413,7 @@ template <int CG, int BN, bool kBits8, bool kArow, bool kBrow> __global__ void _
                     __syncwarp();
                     if (lane == 0) {
                         if constexpr (CG == 2)
-                            asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_first_cta(sums_empty + 8 * buf)) : "memory");
+                            asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(in_first_cta(sums_empty + 8 * buf)) : "memory");
                         else
                             mbarrier_arrive(sums_empty + 8 * buf);
                     }
