@@ -1,10 +1,9 @@
 // token_scan.cuh - what the forward and the gradients of the selective scan over tokens share: where a segment of a
-// sequence lies, the staging of its tokens, and the sums over the lanes of a channel.
+// sequence lies, the states of a lane, the sums over the lanes of a channel, and the staging of tokens in shared memory (adjoint).
 //
-// Channels lie side by side in a token's row.  A CTA takes 64 of them; four lanes hold the states of one channel, N / 4 each,
-// so that a warp has eight channels and the 32 values that B and C have for a token are read by all of them from shared
-// memory.  A lane prepares one token of every four (its step size, its product with x, its gate) and hands them to the other
-// three by shuffles.
+// Channels lie side by side in a token's row, and a CTA takes 64 of them, a tile.  The states of a channel lie in the lanes of a group, two in the
+// forward and four elsewhere; a lane prepares one token of every two or four (its step size, its product with x, its gate) and
+// hands them to the others by shuffles.
 #pragma once
 
 #include "layer_common.cuh"
@@ -13,7 +12,7 @@
 
 namespace vmb {
 
-constexpr int kScanCh = 64, kScanThreads = 256;
+constexpr int kScanCh = 64, kScanThreads = 256;  // channels of a tile; threads of the adjoint's CTAs
 
 struct ScanKernel {
     TokenScanArgs a;
@@ -111,29 +110,9 @@ __device__ __forceinline__ void stage_rows(char* dst, const T* src, long long ts
         }
     }
 }
-template <typename T>
-__device__ __forceinline__ void unstage_rows(T* dst, const char* src, long long ts, int tokens, int len, int cols, bool vec) {
-    constexpr int V = 16 / (int)sizeof(T), per = kScanCh / V;
-    if (vec) {
-        for (int i = threadIdx.x; i < tokens * per; i += kScanThreads) {
-            const int t = i / per, c = (i % per) * V;
-            if (t < len && c < cols)
-                *reinterpret_cast<uint4*>(dst + t * ts + c) = *reinterpret_cast<const uint4*>(src + t * scan_pitch<T>() + c * (int)sizeof(T));
-        }
-    } else {
-        for (int i = threadIdx.x; i < tokens * kScanCh; i += kScanThreads) {
-            const int t = i / kScanCh, c = i % kScanCh;
-            if (t < len && c < cols) dst[t * ts + c] = *reinterpret_cast<const T*>(src + t * scan_pitch<T>() + c * (int)sizeof(T));
-        }
-    }
-}
 template <typename T> __device__ __forceinline__ float staged(const char* p, int t, int c) {
     return io<T>::ld(reinterpret_cast<const T*>(p + t * scan_pitch<T>()) + c);
 }
-template <typename T> __device__ __forceinline__ void restage(char* p, int t, int c, float v) {
-    reinterpret_cast<T*>(p + t * scan_pitch<T>())[c] = io<T>::to(v);
-}
-
 // B and C of TOK rows in fp32, NP values each (NB and NC of them read, zeros behind and from row len on): loaded to registers, stored when
 // there is room.
 template <typename T, int NP, int TOK> struct RowsBC {

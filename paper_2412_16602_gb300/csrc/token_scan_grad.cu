@@ -11,12 +11,12 @@
 // decays up to a token is the exponential of A times the sum of the step sizes), and a segment of the second launch starts from
 // the joined sums of those behind it.  Three exponentials for each state, and the sums over the channels (a thread's two at once, a warp's
 // eight pairs by shuffles, a CTA's four warps through shared memory, the tiles by a third launch, in a fixed order) are what bounds it.
-#include "token_scan.cuh"
-
 //
 // 38 sequences of 2048 tokens of 1024 channels and 16 states with a gate: 2157 us in bf16, 2239 in fp32, 212 instructions for a token of 16 channels at 0.47 a clock and
 // scheduler.  With one channel a thread, eight tokens at a time and states kept every 64 tokens, so formed three times, 137 for eight channels: 2689
 // and 2940.  Decays formed again instead of kept, for three CTAs on an SM instead of two: 2191 and 2349.
+#include "token_scan.cuh"
+
 namespace vmb {
 
 namespace {
