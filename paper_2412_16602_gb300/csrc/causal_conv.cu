@@ -5,10 +5,10 @@
 //   y_t = act(z_t);   g_t = dy_t act'(z_t),   dx_t = sum_i w_(W - 1 - i) g_(t + i),   dw_j = sum_t g_t x_(t - W + 1 + j).
 //
 // The bytes are few: x is read and y written once.  A thread takes a vector of four channels and walks along a run of
-// tokens, the last W - 1 inputs in registers, so that only the W - 1 inputs before a run are read twice.  24576 x 1536 in bf16, four taps with SiLU: 45 us
-// dense (half the copy rate), 61 packed (the search for a run's sequence goes beside its first rows); fp32 54 (82%).  Gradients 94 and 111: filter, sums and
-// window fill the registers (128 and 168), so that few rows are on their way; runs inside one sequence, nearly all, take a path without
-// checks for its borders (129 and 124 without it).  Vectors of eight bf16 channels took 177 registers and were slower, rows of eight asked for at once too.
+// tokens, the last W - 1 inputs in registers, so that only the W - 1 inputs before a run are read twice.  24576 x 1536 in bf16, four taps with SiLU: 39 us
+// dense (58% of the copy rate), 42 packed (the search for a run's sequence goes beside its first rows); fp32 51 (87%) and 52.  Gradients 94 and 111: filter, sums
+// and window fill the registers (128 and 168), so that few rows are on their way.  Runs inside one sequence, nearly all, take a path without
+// checks for its borders (without it 59 packed, gradients 129 and 124); 80 registers, six blocks on an SM (without that limit 43 and 48).  Vectors of eight bf16 channels took 177 registers and were slower, rows of eight asked for at once too.
 #include <initializer_list>
 
 #include "layer_common.cuh"
@@ -178,7 +178,7 @@ template <typename T, int V, int W> __device__ __forceinline__ void last_inputs(
     }
 }
 
-template <typename T, int V, int W, int ACT, bool kPacked> __global__ void __launch_bounds__(kConvThreads) conv_fwd_kernel(ConvKernel k) {
+template <typename T, int V, int W, int ACT, bool kPacked> __global__ void __launch_bounds__(kConvThreads, 6) conv_fwd_kernel(ConvKernel k) {
     const ConvArgs& a = k.a;
     const int lx = threadIdx.x % k.g.tx, ly = threadIdx.x / k.g.tx;
     const int c = (blockIdx.y * k.g.tx + lx) * V;
@@ -247,6 +247,26 @@ template <typename T, int V, int W, int ACT, bool kPacked> __global__ void __lau
             for (int i = 0; i < V; ++i) win[j][i] = 0.0f;
             if (initial) load_vec<T, V>(win[j], initial + (long long)(W - 1 + q) * a.C);
         }
+    }
+    if (left == k.run && (!kPacked || (!at.none(a.B) && row + left <= at.end))) {  // a run inside one sequence
+#pragma unroll 1
+        for (int r = 0; r < k.run; r += kConvBatch) {
+            if (r) {
+#pragma unroll
+                for (int u = 0; u < kConvBatch; ++u) in[u] = raw_vec<T, V>(x + u * a.x_t);
+            }
+#pragma unroll
+            for (int u = 0; u < kConvBatch; ++u) {
+                float z[V], cur[V];
+                widen<T, V>(cur, in[u]);
+                taps<V, W>(z, win, cur, w, bias);
+#pragma unroll
+                for (int i = 0; i < V; ++i) z[i] = activate<ACT>(z[i]);
+                store_vec<T, V>(y + (long long)u * a.C, z);
+            }
+            x += kConvBatch * a.x_t, y += (long long)kConvBatch * a.C;
+        }
+        return;
     }
     for (long long r = 0; r < left; r += kConvBatch) {
         if (r) fetch(r);
