@@ -191,7 +191,8 @@ template <typename T, int NP, bool kLocal> __global__ void __launch_bounds__(kFw
 }
 
 // A few tokens of every row from the state in its slot, updated in place; four lanes a channel, two rows a thread, whose states are under way
-// together and which share A.  Bound by the states' bytes: 256 rows of 2048 channels, 67 MB, 19.2 us (one row a thread 22.8, four 25.0).
+// together and which share A.  Bound by the states' bytes: 256 rows of 2048 channels, 67 MB, 18.3 us (one row a thread
+// 22.8, four 25.0; with B and C one by one 19.2).
 constexpr int kStepRows = 2;
 template <typename T, int NP> __global__ void __launch_bounds__(128) token_scan_step_kernel(TokenScanArgs a, int tiles) {
     constexpr int SPL = NP / 4, P = Pairs<SPL>::P;
@@ -202,6 +203,9 @@ template <typename T, int NP> __global__ void __launch_bounds__(128) token_scan_
     const bool on = d < a.D;
     const int dd = on ? d : a.D - 1;  // (lanes behind the last channel keep their warp's shuffles whole)
     const bool whole = a.N == NP && (reinterpret_cast<uintptr_t>(a.state) & 15) == 0 && (reinterpret_cast<uintptr_t>(a.A) & 15) == 0;
+    // B and C in whole vectors of a lane's states
+    const bool vec = a.N == NP && ((a.B_b | a.B_t | a.C_b | a.C_t) & (SPL - 1)) == 0 &&
+                     ((reinterpret_cast<uintptr_t>(a.Bm) | reinterpret_cast<uintptr_t>(a.Cm)) & (SPL * sizeof(T) - 1)) == 0;
     const int rows = (int)min((long long)kStepRows, a.B - b0);
     long long slot[kStepRows];
 #pragma unroll
@@ -237,6 +241,16 @@ template <typename T, int NP> __global__ void __launch_bounds__(128) token_scan_
             dt[r] = io<T>::ld((const T*)a.delta + b * a.d_b + t * a.d_t + dd);
             if (a.z) zv[r] = io<T>::ld((const T*)a.z + b * a.z_b + t * a.z_t + dd);
             const T *Bm = (const T*)a.Bm + b * a.B_b + t * a.B_t + n0, *Cm = (const T*)a.Cm + b * a.C_b + t * a.C_t + n0;
+            if (vec) {
+                float v[SPL];
+                load_vec<T, SPL>(v, Bm);
+#pragma unroll
+                for (int p = 0; p < P; ++p) B[r].v[p] = make_float2(v[2 * p], SPL > 1 ? v[2 * p + (SPL > 1)] : 0.0f);
+                load_vec<T, SPL>(v, Cm);
+#pragma unroll
+                for (int p = 0; p < P; ++p) C[r].v[p] = make_float2(v[2 * p], SPL > 1 ? v[2 * p + (SPL > 1)] : 0.0f);
+                continue;
+            }
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 const bool one = n0 + 2 * p < a.N, two = SPL > 1 && n0 + 2 * p + 1 < a.N;

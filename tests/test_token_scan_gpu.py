@@ -128,6 +128,19 @@ def test_steps(vmb, B, T, D, N, dtype, gate, slots):
     assert not y[[i for i in range(B) if at[i] < 0]].any()
 
 
+@pytest.mark.parametrize("B,T,D,N,dtype", [(3, 2, 40, 16, BF16), (2, 1, 24, 8, F32), (5, 1, 33, 16, F32)])
+def test_steps_of_strided_rows(vmb, B, T, D, N, dtype):
+    """Parts of wider rows, B and C from an odd place in theirs."""
+    ins, init, _, _ = make(10, B, T, D, N, dtype, half=True)
+    state = init.clone()
+    y = vmb.vmb_token_scan_step(*ins, state)
+    yr, lr = ref.scan(*d(ins), *d([init]))
+    assert ref.rel(y, yr) <= tol(T, dtype) and ref.rel(state, lr) <= tol(T)
+    dense = [t if t is None or t.dim() < 3 else t.contiguous() for t in ins]
+    again = init.clone()
+    assert torch.equal(vmb.vmb_token_scan_step(*dense, again), y) and torch.equal(again, state)
+
+
 def test_no_softplus_no_skip_no_bias(vmb):
     ins, init, dy, _ = make(5, 2, 50, 24, 16, F32)
     ins[1], ins[5], ins[6] = ins[1].abs() * 0.1, None, None
