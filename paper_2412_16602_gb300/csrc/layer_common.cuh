@@ -68,7 +68,8 @@ template <int ACT> __device__ __forceinline__ float2 activate2(float2 z) {
 
 // ------------------------------------------------------------ vectors of channels
 
-template <typename T, int V> struct alignas(sizeof(T) * V) Vec { T v[V]; };
+// (no more than 16 bytes: what the checks of pointers ask for, though the device has loads of 32 bytes that need more)
+template <typename T, int V> struct alignas(sizeof(T) * V < 16 ? sizeof(T) * V : 16) Vec { T v[V]; };
 
 template <typename T, int V> __device__ __forceinline__ void load_vec(float (&out)[V], const T* p) {
     const Vec<T, V> a = *reinterpret_cast<const Vec<T, V>*>(p);
