@@ -103,26 +103,12 @@ template <int CG> __device__ __forceinline__ void tc_load(uint32_t dst, const CU
                      : "memory");
 }
 
-__device__ __forceinline__ bool tc_test(uint32_t bar, uint32_t parity) {
-    uint32_t done;
-    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-                 : "=r"(done)
-                 : "r"(bar), "r"(parity)
-                 : "memory");
-    return done != 0;
-}
 // (the sums of a tile may take long: kTcSumsNs)
 constexpr uint64_t kTcSumsNs = 4ull * 1000 * 1000 * 1000;
 __device__ __forceinline__ bool tc_wait(uint32_t bar, uint32_t parity, unsigned* err, uint64_t limit = kWaitLimitNs) {
-    if (tc_test(bar, parity)) return true;
-    const uint64_t t0 = globaltimer_ns();
-    for (;;) {
-        if (tc_test(bar, parity)) return true;
-        if (globaltimer_ns() - t0 > limit) {
-            atomicOr(err, kErrTimeout);
-            return false;
-        }
-    }
+    if (mbarrier_wait(bar, parity, limit)) return true;
+    atomicOr(err, kErrTimeout);
+    return false;
 }
 
 // 32 columns of the warp's 32 lanes; they are there after tmem_wait32.

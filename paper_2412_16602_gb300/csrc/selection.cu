@@ -93,19 +93,7 @@ __device__ __forceinline__ void mma_tf32(uint32_t tmem, uint64_t da, uint64_t db
 }
 
 // Wait (bounded by 1 s of wall time) for the given phase of an mbarrier.
-__device__ __forceinline__ bool mbar_wait(uint32_t mbar, uint32_t phase) {
-    const uint64_t t0 = globaltimer_ns();
-    for (;;) {
-        uint32_t done;
-        asm volatile(
-            "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-            : "=r"(done)
-            : "r"(mbar), "r"(phase)
-            : "memory");
-        if (done) return true;
-        if (globaltimer_ns() - t0 > 1000000000ull) return false;
-    }
-}
+__device__ __forceinline__ bool mbar_wait(uint32_t mbar, uint32_t phase) { return mbarrier_wait(mbar, phase, 1000000000ull); }
 
 // NBUF operand buffers: with two, the tensor cores work on a chunk while the next
 // one is converted and stored, which takes the products' latency off the chain of

@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "bounded_wait.h"
+
 namespace vmb {
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -411,12 +413,7 @@ __device__ __forceinline__ bool mbarrier_test(uint32_t bar, uint32_t parity) {
 // Wait for the phase with the given parity to complete, bounded by `limit_ns`
 // of wall time (false: the wait gave up).
 __device__ __forceinline__ bool mbarrier_wait(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
-    if (mbarrier_test(bar, parity)) return true;
-    const uint64_t t0 = globaltimer_ns();
-    for (;;) {
-        if (mbarrier_test(bar, parity)) return true;
-        if (globaltimer_ns() - t0 > limit_ns) return false;
-    }
+    return bounded_wait([=] { return mbarrier_test(bar, parity); }, [] { return globaltimer_ns(); }, limit_ns);
 }
 // Tiled 3-D tensor copy (innermost coordinate x first) into shared memory,
 // completing `bar`'s transaction count with the box's bytes.  Elements of the
