@@ -40,6 +40,7 @@ struct TcKernel {
     int N;
     int tiles_m, tiles_n, splits, kblocks, kper, units;
     bool vec;
+    bool drop;  // test hook: the sums of a CTA's first unit are not handed over, so every wait for them runs out
 };
 
 // Tensor-memory matrix descriptors of operands swizzled by 128 bytes.  The contraction dense: rows of 128 bytes, eight rows every 1024
@@ -342,7 +343,7 @@ template <int CG, int BN, bool kBits8, bool kArow, bool kBrow> __global__ void _
                     tc_commit<CG>(empty + 8 * stage);
                     if (++stage == kTcStages) stage = 0, phase ^= 1;
                 }
-                tc_commit<CG>(sums_full + 8 * buf);
+                if (!(k.drop && u == first)) tc_commit<CG>(sums_full + 8 * buf);
                 buf ^= 1;
                 if (buf == 0) bphase ^= 1;
             }
@@ -371,7 +372,8 @@ template <int CG, int BN, bool kBits8, bool kArow, bool kBrow> __global__ void _
                 terms[COLS + j] = in && k.e.bias ? k.e.bias[at.n0 + j] : 0.0f;
             }
             __syncwarp();
-            if (!tc_wait(sums_full + 8 * buf, bphase, k.err, kTcSumsNs)) break;
+            // (one answer for the warp: a lane that gave up alone would leave the others in loads of the whole warp)
+            if (!__all_sync(0xffffffffu, tc_wait(sums_full + 8 * buf, bphase, k.err, kTcSumsNs))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t sums = tmem + buf * BN + part * COLS + ((uint32_t)(quad * 32) << 16);
             const bool whole = k.vec && k.splits == 1 && at.m0 < k.M;
@@ -536,6 +538,7 @@ vmb_status launch_gemm_tc(const GemmProblem& p, bool bits8, float* partial, unsi
     k.tiles_m = plan.tiles_m, k.tiles_n = plan.tiles_n, k.splits = plan.splits, k.kblocks = plan.kblocks, k.kper = plan.kper;
     k.units = plan.tiles_m * plan.tiles_n * plan.splits;
     k.vec = epilogue_vectors(p);
+    k.drop = drop_sums();
     const void* fn = plan.cg == 2 ? tc_kernel<2>(bits8, arow, brow) : tc_kernel<1>(bits8, arow, brow);
     if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem) != cudaSuccess) return VMB_ERR_CUDA;
     const int sms = device_sm_count(), slots = sms > plan.cg ? sms / plan.cg : 1;

@@ -12,7 +12,7 @@
 namespace vmb {
 
 namespace {
-std::atomic<int> g_force_shape{-1}, g_force_chunks{0}, g_force_tc{0}, g_force_steps{0}, g_refuse_maps{0};
+std::atomic<int> g_force_shape{-1}, g_force_chunks{0}, g_force_tc{0}, g_force_steps{0}, g_refuse_maps{0}, g_drop_sums{0};
 }  // namespace
 
 int forced_full_shape(int* chunks) {
@@ -22,6 +22,7 @@ int forced_full_shape(int* chunks) {
 int forced_mean_chunk() { return g_force_tc.load(std::memory_order_relaxed); }
 int forced_mean_steps() { return g_force_steps.load(std::memory_order_relaxed); }
 bool refuse_tensor_maps() { return g_refuse_maps.load(std::memory_order_relaxed) != 0; }
+bool drop_sums() { return g_drop_sums.load(std::memory_order_relaxed) != 0; }
 
 int device_sm_count() {
     static std::mutex mu;
@@ -758,6 +759,11 @@ int vmb_testing_force_mean_chunk(int tc) {
 
 int vmb_testing_refuse_tensor_maps(int on) {
     g_refuse_maps.store(on != 0, std::memory_order_relaxed);
+    return 0;
+}
+
+int vmb_testing_drop_sums(int on) {
+    g_drop_sums.store(on != 0, std::memory_order_relaxed);
     return 0;
 }
 

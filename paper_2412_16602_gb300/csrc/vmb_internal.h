@@ -165,6 +165,7 @@ int forced_full_shape(int* chunks);
 int forced_mean_chunk();
 int forced_mean_steps();
 bool refuse_tensor_maps();
+bool drop_sums();
 
 vmb_status plan_full(const ScanArgs& a, ScanPlan* plan);
 vmb_status plan_mean(const ScanArgs& a, ScanPlan* plan);

@@ -54,6 +54,11 @@ int vmb_testing_force_mean_steps(int steps);
  * would (0 restores it).  Returns 0. */
 int vmb_testing_refuse_tensor_maps(int on);
 
+/* Let the matrix product on the tensor cores keep the sums of each CTA's first tile from
+ * its epilogue (1), so that every wait for them runs out, after 4 s (0 restores it).
+ * Returns 0. */
+int vmb_testing_drop_sums(int on);
+
 /* Workspace bytes of the plan one scan call with these exact flags would run
  * (vmb_scan_workspace_bytes returns the larger over the two Bbar forms).
  * 0 for invalid arguments. */
