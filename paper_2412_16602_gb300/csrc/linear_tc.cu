@@ -322,6 +322,12 @@ template <int CG, int BN, bool kBits8, bool kArow, bool kBrow> __global__ void _
                     if (++stage == kTcStages) stage = 0, phase ^= 1;
                 }
             }
+            // Every stage is empty before this CTA leaves: the arrivals that say so reach both CTAs of a pair, in whatever order with those for the sums,
+            // and must find the barriers of a CTA that is still there.  (After a wait that ran out the epilogue's, of 4 s, cover copies under way.)
+            for (int i = 0; i < kTcStages && ok; ++i) {
+                ok = tc_wait(empty + 8 * stage, phase ^ 1, k.err);
+                if (++stage == kTcStages) stage = 0, phase ^= 1;
+            }
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {  // products
