@@ -1598,15 +1598,18 @@ def vmb_linear_bwd(x, weight, dy, pre=None, *, act: str = "none", want_x: bool =
 
 @_on_its_stream
 def vmb_read_status(workspace=None, device=None, stream=None) -> int:
-    """Synchronise and return (then clear) the device error word of a workspace; without one, of the default workspaces
-    that the calling thread's scans have used on the device (VMB_OK, or an error of one of them)."""
+    """Synchronise and return (then clear) the device error word of a workspace; without one, of all default workspaces that
+    the calling thread's calls have used on the device: the scans', the delta rule's, and those of the layer around the scan
+    over tokens (VMB_OK, or an error of one of them).  A call captured into a graph has a default workspace that nobody else
+    can reach: give it one (`workspace=`) to read its status after a replay."""
     if workspace is not None:
         return int(lib.vmb_read_status(_ptr(workspace), _stream(stream)))
     dev = torch.device("cuda" if device is None else device)
     index = torch.cuda.current_device() if dev.index is None else dev.index
     _default_ws.get(256, dev)
     torch.cuda.synchronize(index)
-    found = [int(lib.vmb_read_status(_ptr(buf), _stream(stream))) for (i, _), buf in _default_ws.buffers().items() if i == index]
+    found = [int(lib.vmb_read_status(_ptr(buf), _stream(stream)))
+             for kept in (_default_ws, _delta_ws, _layer_ws) for (i, _), buf in kept.buffers().items() if i == index]
     return next((status for status in found if status != VMB_OK), VMB_OK)
 
 
