@@ -293,6 +293,14 @@ class Workspace:
             self._local.bufs = {}
             return self._local.bufs
 
+    def outgrown(self) -> dict:
+        """The same of the calling thread's buffers that were outgrown: their headers, for the errors that nobody has read."""
+        try:
+            return self._local.left
+        except AttributeError:
+            self._local.left = {}
+            return self._local.left
+
     def get(self, nbytes: int, device: torch.device) -> torch.Tensor:
         index = torch.cuda.current_device() if device.index is None else device.index
         bufs, key = self.buffers(), (index, _raw_stream(index))
@@ -307,6 +315,9 @@ class Workspace:
             else:
                 buf = torch.zeros(n, dtype=torch.uint8, device=device)
             if not capturing:
+                old, left = bufs.get(key), self.outgrown()
+                if old is not None:
+                    left[key] = left[key] | old[:256] if key in left else old[:256].clone()
                 bufs[key] = buf
         return buf
 
@@ -1609,7 +1620,8 @@ def vmb_read_status(workspace=None, device=None, stream=None) -> int:
     _default_ws.get(256, dev)
     torch.cuda.synchronize(index)
     found = [int(lib.vmb_read_status(_ptr(buf), _stream(stream)))
-             for kept in (_default_ws, _delta_ws, _layer_ws) for (i, _), buf in kept.buffers().items() if i == index]
+             for kept in (_default_ws, _delta_ws, _layer_ws) for bufs in (kept.buffers(), kept.outgrown())
+             for (i, _), buf in bufs.items() if i == index]
     return next((status for status in found if status != VMB_OK), VMB_OK)
 
 

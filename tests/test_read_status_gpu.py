@@ -51,3 +51,21 @@ def test_of_a_captured_call(vmb):
         offsets[2] = last
         graph.replay()
         assert vmb.vmb_read_status(ws) == want
+
+
+@pytest.mark.parametrize("own_stream", [False, True])
+def test_of_a_workspace_that_was_outgrown(vmb, own_stream, monkeypatch):
+    """Two small calls that go wrong, each with a larger one after it, before anybody asks."""
+    monkeypatch.setattr(vmb.vmb, "_layer_ws", vmb.vmb.Workspace(header=256))
+    stream = torch.cuda.Stream() if own_stream else None
+    torch.cuda.synchronize()
+    for last, n in ((T + 1, 3000), (T, 30000), (T + 1, 100000)):
+        scan(vmb, last, stream=stream)
+        x, A, B = torch.zeros(1, n, D, device="cuda"), -torch.rand(D, N, device="cuda"), torch.zeros(1, n, N, device="cuda")
+        torch.cuda.synchronize()
+        before = vmb.layer_workspace(stream=stream).numel()
+        vmb.vmb_token_scan_fwd(x, x, A, B, B, stream=stream)
+        torch.cuda.synchronize()
+        assert vmb.layer_workspace(stream=stream).numel() > before
+    assert vmb.vmb_read_status() == vmb.VMB_ERR_BOUNDS
+    assert vmb.vmb_read_status() == vmb.VMB_OK  # cleared
