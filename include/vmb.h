@@ -615,7 +615,8 @@ vmb_status vmb_group_norm_bwd(const void* x, const float* weight, const float* b
  *   whose slot is outside [0, pool) have none: their outputs are zero.  Slots in use are distinct.
  *   At most 2^30 - 1 tokens, 2^24 sequences and 2^22 channels (VMB_ERR_UNSUPPORTED above), and for the
  *   scan and the gradients of the convolution fewer than 2^24 elements between tokens.
- *   Gradients are deterministic: sums in a fixed order.
+ *   Gradients are deterministic: sums in a fixed order.  Those of an empty problem (no tokens, rows or channels) are
+ *   written too, as zeros, where they have elements: sums of nothing.
  *   Workspaces are 256-byte aligned, the first 256 bytes zero-filled before the first use; calls that
  *   share one must not overlap in time.
  *

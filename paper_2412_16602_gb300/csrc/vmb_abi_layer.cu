@@ -56,6 +56,17 @@ bool take_strides(const int64_t* strides, int i, long long width, int T, bool pa
     return true;
 }
 
+// What an empty problem leaves of its gradients: sums of nothing.  Outputs may be null.
+struct Cleared {
+    void* p;
+    size_t bytes;
+};
+vmb_status clear(std::initializer_list<Cleared> outs, cudaStream_t stream) {
+    for (const Cleared& o : outs)
+        if (o.p && o.bytes && cudaMemsetAsync(o.p, 0, o.bytes, stream) != cudaSuccess) return VMB_ERR_CUDA;
+    return VMB_OK;
+}
+
 // ------------------------------------------------------------ convolution
 
 vmb_status conv_sizes(int B, int* T, int64_t total, bool packed, int C, int W, vmb_act act, vmb_dtype dt, bool* empty) {
@@ -151,7 +162,8 @@ vmb_status vmb_causal_conv_bwd(const void* x, const float* weight, const float* 
                                size_t workspace_bytes, cudaStream_t stream) {
     bool empty = false;
     vmb_status s = conv_sizes(B, &T, total, offsets != nullptr, C, W, act, dtype, &empty);
-    if (s != VMB_OK || empty) return s;
+    if (s != VMB_OK) return s;
+    if (empty) return clear({{dweight, (size_t)C * W * 4}, {dbias, (size_t)C * 4}}, stream);
     if (!weight || !dweight || (total > 0 && (!x || !dy || !dx || dx == x || dx == dy))) return VMB_ERR_INVALID_ARG;
     if (dinitial_state && (dinitial_state == dfinal_state || dinitial_state == initial_state)) return VMB_ERR_INVALID_ARG;
     if (!aligned({x, dy, dx, initial_state, dfinal_state, dinitial_state}, esize(dtype)) || !aligned({weight, bias, dweight, dbias, offsets}, 4))
@@ -224,7 +236,9 @@ vmb_status vmb_token_scan_bwd(const void* x, const void* delta, const float* A, 
     const bool packed = offsets != nullptr;
     vmb_status s = scan_sizes(B, &T, total, packed, D, N, dtype, &empty);
     if (s != VMB_OK || (flags & ~VMB_FLAG_SOFTPLUS)) return s != VMB_OK ? s : VMB_ERR_INVALID_ARG;
-    if (empty) return VMB_OK;
+    if (empty)  // (without channels B's and C's gradients have elements still)
+        return clear({{dA, (size_t)D * N * 4}, {dDskip, (size_t)D * 4}, {ddelta_bias, (size_t)D * 4}, {dBm, (size_t)total * N * esize(dtype)},
+                      {dCm, (size_t)total * N * esize(dtype)}}, stream);
     TokenScanArgs a{};
     a.B = B, a.T = T, a.total = total, a.D = D, a.N = N, a.dtype = dtype, a.softplus = (flags & VMB_FLAG_SOFTPLUS) != 0;
     if ((s = scan_args(a, x, delta, A, Bm, Cm, Dskip, delta_bias, z, strides, packed)) != VMB_OK) return s;
@@ -285,7 +299,8 @@ vmb_status vmb_rms_norm_bwd(const void* x, const float* weight, const float* rst
                             int64_t rows, int C, vmb_dtype dtype, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
     bool empty = false;
     vmb_status s = rms_sizes(rows, C, dtype, &empty);
-    if (s != VMB_OK || empty) return s;
+    if (s != VMB_OK) return s;
+    if (empty) return clear({{dweight, (size_t)C * 4}}, stream);
     if (!x || !rstd || !dy || !dx || dx == x || dx == dy || dx == dsum) return VMB_ERR_INVALID_ARG;
     if (!aligned({x, dy, dsum, dx}, esize(dtype)) || !aligned({weight, rstd, dweight}, 4)) return VMB_ERR_MISALIGNED;
     if ((s = check_workspace(workspace)) != VMB_OK) return s;
@@ -325,7 +340,7 @@ vmb_status vmb_linear_bwd(const void* x, int64_t x_stride, const void* weight, c
     vmb_status s = linear_sizes(M, K, N, &empty);
     if (s != VMB_OK) return s;
     if (!act_ok(act) || x_stride < 0) return VMB_ERR_INVALID_ARG;
-    if (empty) return VMB_OK;
+    if (empty) return clear({{dx, (size_t)M * K * 2}, {dweight, (size_t)N * K * 2}, {dbias, (size_t)N * 4}}, stream);
     if (!dy || (act != VMB_ACT_NONE && !pre) || (K > 0 && ((dx && !weight) || (dweight && !x)))) return VMB_ERR_INVALID_ARG;
     for (const void* out : {dx, dweight})
         if (out && (out == x || out == weight || out == pre || out == dy)) return VMB_ERR_INVALID_ARG;

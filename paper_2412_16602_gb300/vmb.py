@@ -1289,8 +1289,7 @@ def vmb_causal_conv_bwd(x, weight, bias, dy, *, act: str = "silu", initial_state
     if dy is None:
         raise ValueError("dy is needed")
     _like(dy, "dy", (B, T, C), x.dtype)
-    new = torch.empty_like if total or n else torch.zeros_like  # (an empty problem launches nothing)
-    out = dict(x=x.new_empty((B, T, C)), weight=new(weight), bias=None if bias is None else new(bias))
+    out = dict(x=x.new_empty((B, T, C)), weight=torch.empty_like(weight), bias=None if bias is None else torch.empty_like(bias))
     if want_initial:
         out["initial_state"] = x.new_empty((n, W - 1, C))
     _one_device(x, weight, bias, dy, initial_state, dfinal_state, offsets)
@@ -1409,9 +1408,8 @@ def vmb_token_scan_bwd(x, delta, A, Bm, Cm, Dskip, delta_bias, z, dy, saved, *, 
         raise ValueError("dy and the forward's saved are needed")
     _like(dy, "dy", (B, T, D), x.dtype)
     _token_scan_saved(saved, n, T1, total, packed, D, N)
-    new = torch.empty if total or n else torch.zeros  # (an empty problem launches nothing)
     dev = x.device
-    out = {k: None if t is None else new(t.shape, dtype=t.dtype, device=dev)
+    out = {k: None if t is None else torch.empty(t.shape, dtype=t.dtype, device=dev)
            for k, t in (("x", x), ("delta", delta), ("A", A), ("B", Bm), ("C", Cm), ("Dskip", Dskip), ("delta_bias", delta_bias),
                         ("z", z))}
     if want_initial:
@@ -1511,8 +1509,7 @@ def vmb_rms_norm_bwd(x, weight, rstd, dy, *, dsum=None, workspace=None, stream=N
     _float(rstd, "rstd", x.shape[:-1])
     _like(dy, "dy", x.shape, x.dtype)
     _like(dsum, "dsum", x.shape, x.dtype)
-    new = torch.empty_like if x.numel() else torch.zeros_like  # (an empty problem launches nothing: sums of nothing)
-    out = dict(x=torch.empty_like(x), weight=None if weight is None else new(weight))
+    out = dict(x=torch.empty_like(x), weight=None if weight is None else torch.empty_like(weight))
     _one_device(x, weight, rstd, dy, dsum)
     ws = _layer_workspace(workspace, x, "vmb_rms_norm_workspace_bytes", rows, C, code)
     _check(lib.vmb_rms_norm_bwd(x.data_ptr(), _ptr(weight), rstd.data_ptr(), dy.data_ptr(), _ptr(dsum), out["x"].data_ptr(),
@@ -1594,11 +1591,10 @@ def vmb_linear_bwd(x, weight, dy, pre=None, *, act: str = "none", want_x: bool =
             _dev(t, name)
             if t.shape != shape or t.dtype != torch.bfloat16:
                 raise ValueError(f"{name} must be bfloat16 {list(shape)}")
-    new = torch.empty if M and N else torch.zeros  # (an empty problem launches nothing: sums of nothing)
     dev = x.device
-    out = dict(x=new(x.shape, dtype=x.dtype, device=dev) if want_x else None,
-               weight=new((N, K), dtype=x.dtype, device=dev) if want_weight else None,
-               bias=new((N,), dtype=torch.float32, device=dev) if want_bias else None)
+    out = dict(x=torch.empty(x.shape, dtype=x.dtype, device=dev) if want_x else None,
+               weight=torch.empty((N, K), dtype=x.dtype, device=dev) if want_weight else None,
+               bias=torch.empty((N,), dtype=torch.float32, device=dev) if want_bias else None)
     _one_device(x, weight, dy, pre)
     ws = _layer_workspace(workspace, x, "vmb_linear_workspace_bytes", M, K, N, 1)
     _check(lib.vmb_linear_bwd(x.data_ptr(), x_t, weight.data_ptr(), _ptr(pre), dy.data_ptr(), _ptr(out["x"]), _ptr(out["weight"]),
