@@ -648,7 +648,8 @@ vmb_status vmb_group_norm_bwd(const void* x, const float* weight, const float* b
  *   x, residual (or NULL), sum (with a residual) [rows, C] dense (dtype), weight [C] fp32 or NULL (1).
  *   scale NULL: y [rows, C] (dtype).  scale [rows] fp32: y holds 8-bit e4m3 values whose products with
  *   their row's scale are the norm's output: scale = max |y| / 448, 2^-100 at least.
- *   rstd [rows] fp32 or NULL.  C <= 8192 (VMB_ERR_UNSUPPORTED above).
+ *   rstd [rows] fp32 or NULL.  C <= 8192 (VMB_ERR_UNSUPPORTED above); rows of no channels have no scale and no rstd
+ *   (VMB_ERR_INVALID_ARG where one is wanted).
  * vmb_rms_norm_bwd - given dy, and dsum (or NULL), the gradient that reaches s on its own: dx [rows, C], the
  *   gradient of x and of the residual alike, and dweight [C] fp32 (or NULL).  x: what was normalised (the forward's sum,
  *   if it had a residual); rstd: the forward's.

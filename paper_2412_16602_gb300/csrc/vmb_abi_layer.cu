@@ -287,6 +287,7 @@ vmb_status vmb_rms_norm_fwd(const void* x, const void* residual, const float* we
     const vmb_status s = rms_sizes(rows, C, dtype, &empty);
     if (s != VMB_OK) return s;
     if (!(eps >= 0.0f)) return VMB_ERR_INVALID_ARG;
+    if (rows > 0 && C == 0 && (scale || rstd)) return VMB_ERR_INVALID_ARG;  // (no channels have no mean)
     if (empty) return VMB_OK;
     if (!x || !y || x == y || y == residual || (residual && (!sum || sum == y || sum == x || sum == residual))) return VMB_ERR_INVALID_ARG;
     if (!aligned({x, residual, sum}, esize(dtype)) || (!scale && !aligned({y}, esize(dtype))) || !aligned({weight, scale, rstd}, 4))

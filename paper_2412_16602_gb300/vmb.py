@@ -1459,7 +1459,7 @@ def _rms_inputs(x, weight):
         raise ValueError("x must be [..., C]")
     C = x.shape[-1]
     _float(weight, "weight", (C,))
-    return x.numel() // C if C else 0, C, _dtype_code(x.dtype)
+    return x.numel() // C if C else x.shape[:-1].numel(), C, _dtype_code(x.dtype)
 
 
 @_on_its_stream
