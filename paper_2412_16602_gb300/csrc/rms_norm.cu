@@ -49,6 +49,13 @@ template <bool kMax> __device__ __forceinline__ float row_join(float v, int lane
     return v;
 }
 
+// v / d with inv = 1 / d rounded: the product with inv, corrected by the remainder, which is the quotient rounded once (a product alone is off by
+// up to two roundings, and one value in 6 million got the other of two neighbouring 8-bit values).  An infinite d has inv = 0 and no remainder.
+__device__ __forceinline__ float quotient(float v, float d, float inv) {
+    const float q = v * inv;
+    return inv > 0.0f ? fmaf(fmaf(-q, d, v), inv, q) : q;
+}
+
 // 8-bit values of V floats, rounded to nearest even, beyond 448 (by a rounding of the division) to 448.
 template <int V> __device__ __forceinline__ void store_e4m3(uint8_t* p, const float (&v)[V]) {
     if constexpr (V == 1) {
@@ -125,7 +132,7 @@ template <typename T, int V, int NV, bool kBits8> __global__ void __launch_bound
             const int c = (lx + j * k.lanes) * V;
             if (!live || c >= a.C) continue;
 #pragma unroll
-            for (int i = 0; i < V; ++i) s[j][i] *= inv;
+            for (int i = 0; i < V; ++i) s[j][i] = quotient(s[j][i], scale, inv);
             store_e4m3<V>((uint8_t*)a.y + row * a.C + c, s[j]);
         }
     }
