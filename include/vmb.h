@@ -608,9 +608,10 @@ vmb_status vmb_group_norm_bwd(const void* x, const float* weight, const float* b
  *   between tokens (parts of one projection's output); channels are dense.
  *   offsets: NULL, or int32 [B + 1] on the device: B packed sequences, sequence b is rows
  *   offsets[b] .. offsets[b + 1] - 1 of `total` tokens (the batch dimension is then 1; T and batch
- *   strides are unused).  Without offsets total is B * T.  Offsets that decrease or leave [0, total]
- *   are cut to what is in range (the scan reports them as VMB_ERR_BOUNDS through vmb_read_status);
- *   rows that no sequence holds are zero in the outputs and in the gradients.
+ *   strides are unused).  Without offsets total is B * T.  Offsets that leave [0, total] are cut to what is in
+ *   range; where they decrease, what a call writes for the sequences and rows concerned is undefined, but in range.  The
+ *   scan and, where there are tokens, its gradients report both as VMB_ERR_BOUNDS through vmb_read_status.  Rows that no sequence holds are
+ *   zero in the outputs and in the gradients.
  *   slots: NULL (row b uses state b; pool >= B), or int32 [B] on the device: the state of row b; rows
  *   whose slot is outside [0, pool) have none: their outputs are zero.  Slots in use are distinct.
  *   At most 2^30 - 1 tokens, 2^24 sequences and 2^22 channels (VMB_ERR_UNSUPPORTED above), and for the

@@ -160,8 +160,7 @@ template <typename T, int V, int W> __device__ __forceinline__ void last_inputs(
     const T* x = (const T*)a.x + c;
     if (a.offsets) {
         long long end;
-        bool bad;
-        sequence_span(a.offsets, b, a.total, &start, &end, &bad);
+        sequence_span(a.offsets, b, a.total, &start, &end);
         len = end - start;
         x += start * a.x_t;
     } else {
@@ -500,8 +499,7 @@ template <typename T, int W, int ACT> __global__ void __launch_bounds__(128) con
     const T* x = (const T*)a.x + c;
     if (a.offsets) {
         long long end;
-        bool bad;
-        sequence_span(a.offsets, b, a.total, &start, &end, &bad);
+        sequence_span(a.offsets, b, a.total, &start, &end);
         len = end - start;
         x += start * a.x_t;
     } else {

@@ -101,12 +101,11 @@ template <typename F> __device__ __forceinline__ int last_at_most(int n, long lo
     return lo;
 }
 
-// offsets[b] and offsets[b + 1] cut to [0, total], the end not before the start; *bad is set when that changed them.
-__device__ __forceinline__ void sequence_span(const int* offsets, int b, long long total, long long* start, long long* end, bool* bad) {
+// offsets[b] and offsets[b + 1] cut to [0, total], the end not before the start.
+__device__ __forceinline__ void sequence_span(const int* offsets, int b, long long total, long long* start, long long* end) {
     const long long s = offsets[b], e = offsets[b + 1];
-    const long long s1 = s < 0 ? 0 : s > total ? total : s, e1 = e < s1 ? s1 : e > total ? total : e;
-    *bad = s1 != s || e1 != e;
-    *start = s1, *end = e1;
+    *start = s < 0 ? 0 : s > total ? total : s;
+    *end = e < *start ? *start : e > total ? total : e;
 }
 
 }  // namespace vmb

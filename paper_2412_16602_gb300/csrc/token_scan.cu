@@ -30,6 +30,7 @@ template <typename T, int NP, bool kLocal> __global__ void __launch_bounds__(kFw
     const int tile = blockIdx.x % k.tiles, tid = threadIdx.x, p = tid & 1, c0 = tile * kScanCh, d = c0 + tid / kLanes, n0 = p * SPL;
     const long long slot = blockIdx.x / k.tiles;
     if (slot >= k.slots) {  // rows before the first and behind the last sequence
+        check_offsets(a, (slot - k.slots) * k.tiles + tile, (long long)kClearBlocks * k.tiles);
         const long long lo = min(max((long long)a.offsets[0], 0LL), a.total), hi = min(max((long long)a.offsets[a.B], lo), a.total);
         const int cols = min(kScanCh, a.D - c0);
         for (long long r = slot - k.slots; r < a.total - (hi - lo); r += kClearBlocks)

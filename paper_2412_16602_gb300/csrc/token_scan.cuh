@@ -56,14 +56,12 @@ __device__ __forceinline__ ScanSegment scan_segment(const ScanKernel& k, long lo
         g.live = false;
         if (g.b < 0 || g.b >= a.B) return g;
         long long s0, e0;
-        bool bad;
-        sequence_span(a.offsets, g.b, a.total, &s0, &e0, &bad);
+        sequence_span(a.offsets, g.b, a.total, &s0, &e0);
         g.place = s0 / k.seg + g.b;
         g.chunk = s0 / kScanSaved + g.b;
         g.s = (int)(slot - g.place);
         g.seq_len = e0 - s0;
         g.first = s0;
-        if (bad && g.s == 0 && threadIdx.x == 0) atomicOr(&((WsHeader*)a.ws)->err, kErrBounds);
     } else {
         g.b = (int)(slot / k.segs_per);
         g.s = (int)(slot - (long long)g.b * k.segs_per);
@@ -79,6 +77,17 @@ __device__ __forceinline__ ScanSegment scan_segment(const ScanKernel& k, long lo
     g.first += off;
     g.len = (int)(g.seq_len - off < k.seg ? g.seq_len - off : k.seg);
     return g;
+}
+
+// Packed sequences: reports offsets that decrease or leave the tokens; `blocks` blocks of a launch share them out (a segment does not see all of
+// them: where they decrease, a place may belong to two sequences).
+__device__ __forceinline__ void check_offsets(const TokenScanArgs& a, long long block, long long blocks) {
+    bool bad = false;
+    for (long long i = block * blockDim.x + threadIdx.x; i <= a.B; i += blocks * blockDim.x) {
+        const int o = a.offsets[i];
+        bad |= o < 0 || o > a.total || (i > 0 && o < a.offsets[i - 1]);
+    }
+    if (bad) atomicOr(&((WsHeader*)a.ws)->err, kErrBounds);
 }
 
 // The first element of a tensor's row `first` in a segment (batch rows may be strided in dense inputs).

@@ -422,6 +422,7 @@ template <typename T, int NP> __global__ void __launch_bounds__(256) token_scan_
     pdl_wait();
     pdl_launch_dependents();
     const TokenScanArgs& a = k.a;
+    if (a.offsets) check_offsets(a, blockIdx.x, gridDim.x);
     const int lane = threadIdx.x & 31;
     const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (row >= a.total) return;
