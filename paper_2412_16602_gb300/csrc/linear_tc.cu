@@ -20,6 +20,7 @@
 #include <mutex>
 
 #include "linear_common.cuh"
+#include "vmb_testing.h"
 
 namespace vmb {
 
@@ -574,3 +575,9 @@ vmb_status launch_gemm_tc(const GemmProblem& p, bool bits8, float* partial, unsi
 }
 
 }  // namespace vmb
+
+extern "C" int vmb_testing_linear_plan(long long M, int N, long long K, int bits8, int* out) {
+    const vmb::TcPlan p = vmb::tc_plan(M, N, K, bits8 != 0);
+    out[0] = p.cg, out[1] = p.splits;
+    return 0;
+}
