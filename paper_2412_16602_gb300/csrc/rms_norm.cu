@@ -227,6 +227,11 @@ int rms_lanes(int C, int V, bool grads) {
 int rms_vecs(int C, int V, int lanes) { return ((C + V - 1) / V + lanes - 1) / lanes; }
 template <typename T, int V, bool kBits8> const void* rms_fwd_fn(int nv) {
     if constexpr (V == 1) return (const void*)rms_fwd_kernel<T, 1, 16, kBits8>;
+    else if constexpr (V == 8)  // (no more than kFwdMost)
+        return nv <= 1   ? (const void*)rms_fwd_kernel<T, V, 1, kBits8>
+               : nv <= 2 ? (const void*)rms_fwd_kernel<T, V, 2, kBits8>
+               : nv <= 3 ? (const void*)rms_fwd_kernel<T, V, 3, kBits8>
+                         : (const void*)rms_fwd_kernel<T, V, 4, kBits8>;
     else
         return nv <= 1   ? (const void*)rms_fwd_kernel<T, V, 1, kBits8>
                : nv <= 2 ? (const void*)rms_fwd_kernel<T, V, 2, kBits8>

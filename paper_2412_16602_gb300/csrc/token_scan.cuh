@@ -122,30 +122,21 @@ __device__ __forceinline__ void stage_rows(char* dst, const T* src, long long ts
 template <typename T> __device__ __forceinline__ float staged(const char* p, int t, int c) {
     return io<T>::ld(reinterpret_cast<const T*>(p + t * scan_pitch<T>()) + c);
 }
-// B and C of TOK rows in fp32, NP values each (NB and NC of them read, zeros behind and from row len on): loaded to registers, stored when
-// there is room.
-template <typename T, int NP, int TOK> struct RowsBC {
-    static constexpr int kEach = (TOK * NP * 2 + kScanThreads - 1) / kScanThreads;
+// C of TOK rows in fp32, NP values each (N of them read, zeros behind and from row len on).
+template <typename T, int NP, int TOK> __device__ __forceinline__ void stage_states(float* dst, const T* C, long long C_t, int N, int len) {
+    constexpr int kEach = (TOK * NP + kScanThreads - 1) / kScanThreads;
     float v[kEach];
-    __device__ __forceinline__ void load(const T* B, long long B_t, int NB, const T* C, long long C_t, int NC, int len) {
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-            const int i = threadIdx.x + j * kScanThreads, t = i / (2 * NP), n = i % (2 * NP);
-            v[j] = 0.0f;
-            if (t < TOK && t < len) {
-                if (n < NB) v[j] = io<T>::ld(B + t * B_t + n);
-                else if (n >= NP && n - NP < NC) v[j] = io<T>::ld(C + t * C_t + n - NP);
-            }
-        }
+    for (int j = 0; j < kEach; ++j) {
+        const int i = threadIdx.x + j * kScanThreads, t = i / NP, n = i % NP;
+        v[j] = t < TOK && t < len && n < N ? io<T>::ld(C + t * C_t + n) : 0.0f;
     }
-    __device__ __forceinline__ void store(float* s) const {
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-            const int i = threadIdx.x + j * kScanThreads;
-            if (i < TOK * NP * 2) s[i] = v[j];
-        }
+    for (int j = 0; j < kEach; ++j) {
+        const int i = threadIdx.x + j * kScanThreads;
+        if (i < TOK * NP) dst[i] = v[j];
     }
-};
+}
 
 // A lane's states, in pairs: SPL = NP / 4 of them (one state alone is paired with a zero).
 template <int SPL> struct Pairs {

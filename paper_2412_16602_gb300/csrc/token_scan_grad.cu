@@ -24,7 +24,7 @@ namespace {
 // ------------------------------------------------------------ the adjoint of each segment alone
 
 template <typename T, int NP> struct AdjointSmem {
-    static constexpr int array = 32 * scan_pitch<T>(), bytes = 3 * array + 32 * 2 * NP * 4;
+    static constexpr int array = 32 * scan_pitch<T>(), bytes = 3 * array + 32 * NP * 4;
 };
 
 template <typename T, int NP> __global__ void __launch_bounds__(kScanThreads, 2) token_scan_adjoint_kernel(ScanKernel k) {
@@ -52,15 +52,13 @@ template <typename T, int NP> __global__ void __launch_bounds__(kScanThreads, 2)
     const T *raw = scan_row<T>(a.delta, a, g, a.d_b, a.d_t) + c0, *dy = (const T*)a.dy + g.first * a.D + c0;
     const T *z = a.z ? scan_row<T>(a.z, a, g, a.z_b, a.z_t) + c0 : nullptr, *Cm = scan_row<T>(a.Cm, a, g, a.C_b, a.C_t);
     float sum = 0.0f;  // of the channel's step sizes
-    RowsBC<T, NP, TOK> bc;
     for (int t0 = 0; t0 < g.len; t0 += TOK) {
         const int left = g.len - t0;
         if (t0) __syncthreads();
         stage_rows<T>(smem, dy + (long long)t0 * a.D, a.D, TOK, left, cols, k.vec);
         stage_rows<T>(smem + L::array, raw + t0 * a.d_t, a.d_t, TOK, left, cols, k.vec);
         if (z) stage_rows<T>(smem + 2 * L::array, z + t0 * a.z_t, a.z_t, TOK, left, cols, k.vec);
-        bc.load(nullptr, 0, 0, Cm + t0 * a.C_t, a.C_t, a.N, left);
-        bc.store(rows);
+        stage_states<T, NP, TOK>(rows, Cm + t0 * a.C_t, a.C_t, a.N, left);
         cp_async_commit();
         cp_async_wait<0>();
         __syncthreads();
@@ -75,7 +73,7 @@ template <typename T, int NP> __global__ void __launch_bounds__(kScanThreads, 2)
                 const float gu = from_lane(gy, u);
                 sum += from_lane(dt, u);
                 Pairs<SPL> C, e;
-                C.load(rows + (t + u) * 2 * NP + NP + n0);
+                C.load(rows + (t + u) * NP + n0);
                 decays(e, A2, sum);
 #pragma unroll
                 for (int p = 0; p < Pairs<SPL>::P; ++p) acc.v[p] = __ffma2_rn(e.v[p], __fmul2_rn(C.v[p], twice(gu)), acc.v[p]);
