@@ -603,7 +603,8 @@ vmb_status vmb_group_norm_bwd(const void* x, const float* weight, const float* b
  * and 6, without the map's directions): the projections, the short causal convolution, the scan
  * with its gate, and the norm before them.  Channels last: x [B, T, C].  Activations have the storage
  * type `dtype`; filters, A, D, biases, norm weights, the states of the scan and the gradients of all these are fp32,
- * and so is all arithmetic.
+ * and so is all arithmetic, with the device's approximate exponential (2^-22) and reciprocal in SiLU, softplus
+ * and the decays.
  *   strides: NULL (dense), or host values, two for each tensor: the elements between batch rows and
  *   between tokens (parts of one projection's output); channels are dense.
  *   offsets: NULL, or int32 [B + 1] on the device: B packed sequences, sequence b is rows
@@ -640,6 +641,11 @@ vmb_status vmb_group_norm_bwd(const void* x, const float* weight, const float* b
  *   final_state [B, D, N] fp32 or NULL.  N in 1..16 (VMB_ERR_UNSUPPORTED above).
  *   saved: NULL, or vmb_token_scan_saved_bytes(...) bytes (16-byte aligned) for the state before every
  *   16 tokens, which vmb_token_scan_bwd takes.
+ *   A decay is taken as 2^(dt A'), A' = A log2 e rounded to fp32: off by 2^-22 and 2^-23 |dt A| of itself, and
+ *   over a segment of a cut sequence (64 tokens or more) as the power of the sum of its step sizes.  Outputs, states
+ *   and gradients are off by that over the tokens that a state remembers, more than a recurrence in fp32 with a full
+ *   exponential.  Where dt A is positive and its sum over a segment passes 88, they may be infinite or NaN though
+ *   the recurrence token by token is finite.
  * vmb_token_scan_bwd - given dy (dense) and dfinal_state (or NULL): dx, ddelta, dBm, dCm, dz (shapes of the
  *   inputs, dense, dtype; dz where z is), dA, dDskip, ddelta_bias, dinitial_state (fp32; the last three may be NULL).
  * vmb_token_scan_step - T tokens (a few) of every row, `state` [pool, D, N] fp32 updated in place.
@@ -649,8 +655,8 @@ vmb_status vmb_group_norm_bwd(const void* x, const float* weight, const float* b
  *   x, residual (or NULL), sum (with a residual) [rows, C] dense (dtype), weight [C] fp32 or NULL (1).
  *   scale NULL: y [rows, C] (dtype).  scale [rows] fp32: y holds 8-bit e4m3 values whose products with
  *   their row's scale are the norm's output: scale = max |y| / 448, 2^-100 at least.
- *   rstd [rows] fp32 or NULL.  C <= 8192 (VMB_ERR_UNSUPPORTED above); rows of no channels have no scale and no rstd
- *   (VMB_ERR_INVALID_ARG where one is wanted).
+ *   rstd [rows] fp32 or NULL.  Squares are summed in fp32: values are below 2^57.  C <= 8192 (VMB_ERR_UNSUPPORTED
+ *   above); rows of no channels have no scale and no rstd (VMB_ERR_INVALID_ARG where one is wanted).
  * vmb_rms_norm_bwd - given dy, and dsum (or NULL), the gradient that reaches s on its own: dx [rows, C], the
  *   gradient of x and of the residual alike, and dweight [C] fp32 (or NULL).  x: what was normalised (the forward's sum,
  *   if it had a residual); rstd: the forward's.
@@ -662,11 +668,11 @@ vmb_status vmb_group_norm_bwd(const void* x, const float* weight, const float* b
  *   x_scale, weight_scale: both NULL: x and weight are bf16; x_scale [M] and weight_scale [N] fp32: they are e4m3
  *   values to be multiplied by the scale of their row (what vmb_rms_norm_fwd writes in 8 bits).
  *   Products are exact and summed in fp32 by the tensor cores; one rounding, to y.  SiLU and GELU keep 12 bits, also
- *   where they are small.  Any K, N and x_stride; rows of whole vectors of 16 bytes (K, x_stride and, for the gradients, N multiples of 8;
+ *   where they are small (below 2^-119 they may be zero).  Any K, N and x_stride; rows of whole vectors of 16 bytes (K, x_stride and, for the gradients, N multiples of 8;
  *   16 with e4m3) take the fast kernels.  Waits of the kernels are bounded; one that gave up is VMB_ERR_TIMEOUT in
  *   vmb_read_status.
- * vmb_linear_bwd - given dy [M, N] bf16: dZ = dy act'(pre) (rounded to bf16; pre may be NULL without an
- *   activation), dx = dZ weight [M, K], dweight = dZ^T x [N, K] (bf16; either may be NULL), dbias [N] fp32 (or NULL) the
+ * vmb_linear_bwd - given dy [M, N] bf16: dZ = dy act'(pre) (rounded to bf16, the slope at z as pre holds it, rounded
+ *   too; pre may be NULL without an activation), dx = dZ weight [M, K], dweight = dZ^T x [N, K] (bf16; either may be NULL), dbias [N] fp32 (or NULL) the
  *   sums of dZ before its rounding.
  */
 size_t vmb_causal_conv_workspace_bytes(int B, int T, int64_t total, int packed, int C, int W, vmb_dtype dtype);
