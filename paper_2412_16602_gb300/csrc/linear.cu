@@ -3,8 +3,9 @@
 //   z = x W^T + bias, y = act(z) + residual;   dZ = dy act'(z) (bf16),  dx = dZ W,  dW = dZ^T x,  dbias = sum over rows of dZ.
 //
 // linear_tc.cu has the products of many rows, linear_few.cu those of few; here are dZ with the sums of its columns (bound by memory; 8192 x 4096
-// with SiLU about 30 us) and, for what tensor copies cannot read:
-// gemm_any_kernel takes operands of any strides: those that tensor copies cannot read (rows that do not start on 16 bytes).
+// with SiLU 32 us; with GELU 66, by erfcf in its slope) and, for what tensor copies cannot read:
+// gemm_any_kernel takes operands of any strides: those that tensor copies cannot read (rows that do not start on 16 bytes), element by element
+// through shared memory, which bounds it: 4096 x 1023 x 4096 952 us (36 TFLOP/s), 16 x 1001 x 1024 152 us.
 #include <cuda_fp8.h>
 
 #include "linear_common.cuh"

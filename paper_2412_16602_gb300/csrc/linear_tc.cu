@@ -7,9 +7,9 @@
 // tensor memory through the epilogue while the products of the next tile go to the other.  Where tiles are few and the contraction long
 // it is split, the parts' sums are kept in fp32 and joined in order by a second launch.
 //
-// 8192^3 in bf16: 582 us, 1889 TFLOP/s (the library's product 542); 16384 x 1536 x 6144 in bf16 183 (165), in e4m3 109, with GELU 140.  Long contractions are
+// 8192^3 in bf16: 582 us, 1889 TFLOP/s (the library's product 542); 16384 x 1536 x 6144 in bf16 183 (165), in e4m3 102 to 109, with SiLU 113, with GELU 140.  Long contractions are
 // bound by the products and by the bytes into an SM alike (32 KB and 512 clocks a stage); short ones by the epilogue, whose two warps on each
-// scheduler wait for their own results in turn (0.35 instructions a clock): with a quarter of the products issued that last case takes the same.
+// scheduler wait for their own results in turn (0.39 instructions a clock): with a quarter of the products issued that last case takes the same.
 // Tried: outputs by tensor copies from shared memory (130 without GELU, 173 with it: each needs a proxy fence), sixteen warps (96 registers: 128 and 156), factors and biases
 // asked for a tile ahead (no change), four stages of the ring (8192^3 652).  Arrivals at the pair's barrier carry no release at the cluster's scope: what they
 // order are tensor-memory reads, by the tcgen05 fences; with it a warp waited for its stores (151 with GELU).
